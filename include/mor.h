@@ -15,7 +15,7 @@
  *     (a cudaStream_t passed as void*, NULL = the default stream) and the call returns.
  *   - Argument problems are reported synchronously and nothing is launched.  Conditions
  *     found on the device (non-finite inputs) are reported in mor_tensor_stats_t.
- *   - Inputs are row-major BF16 with the last dimension contiguous.
+ *   - Inputs are row-major with the last dimension contiguous; BF16 where nothing else is said.
  */
 #ifndef MOR_H_
 #define MOR_H_
@@ -284,6 +284,128 @@ MOR_API mor_status_t mor_analyze_quantize_host(const mor_tensor_desc_t* host_des
 #define MOR_STATIC_SCRATCH_BYTES (2 * 1024 * 1024)
 MOR_API mor_status_t mor_analyze_quantize_static(const mor_tensor_desc_t* host_desc, const mor_outputs_t* host_out,
                                          void* cuda_stream);
+
+/* ------------------------------------------------------------------ 4-bit operands and their products ----
+ * The next step down from the 8-bit codes above: microscaled 4-bit floating point (the block formats that the
+ * introduction's prior recipes use), made along the reduction axis of the product an operand enters.
+ * Codes are E2M1 (+-0, .5, 1, 1.5, 2, 3, 4, 6; round to nearest even, saturating), two to a byte with the even
+ * element in the low half.
+ *   E8M0_32  blocks of 32; a = max|x| of the block; e = floor(log2 a) - 2 held to -127..127; scale byte e + 127
+ *            (0 for a block of zeros); code = E2M1(x * 2^-e).  tensor_scale is 1.
+ *   E4M3_16  blocks of 16; A = max|x| of the tensor, at least 2^-88; t = fl32(A / 2688) is the tensor scale;
+ *            s = E4M3(fl32(448 a / A)), saturating, is the block scale; code = E2M1(fl32(x * fl32(1 / fl32(s t)))), zero
+ *            where s is zero.  A value is fl32(fl32(code * s) * t).
+ * NaN and infinities take part in no maximum; the scale byte of their block is NaN (0xFF, 0x7F) and its codes are
+ * zero, so that everything the block enters is NaN. */
+typedef enum { MOR_FP4_E4M3_16 = 0, MOR_FP4_E8M0_32 = 1 } mor_fp4_format_t;
+typedef enum { MOR_DTYPE_BF16 = 0, MOR_DTYPE_F32 = 1 } mor_dtype_t;
+
+/* A stack of `batch` matrices [rows, cols] in 4 bits, blocks along cols (the reduction axis).  codes: row i of matrix b
+ * starts at byte (b * rows + i) * ld.  scales: tiles of 128 rows x 4 blocks, 512 bytes each, ordered
+ * [batch][ceil(rows / 128)][ceil(blocks / 4)] with blocks = ceil(cols / block length); inside a tile the byte of a row
+ * and a block is at (row % 32) * 16 + (row / 32 % 4) * 4 + block % 4, the order in which the tensor cores take
+ * them.  Codes past cols up to the next multiple of 32 and every byte of the tiles are written (zeros where there is no
+ * element). */
+typedef struct mor_fp4_matrix {
+    uint8_t* codes;         /* DEVICE, 16-byte aligned                                        */
+    uint8_t* scales;        /* DEVICE, 16-byte aligned                                        */
+    float*   tensor_scale;  /* DEVICE, one float for the whole stack                          */
+    int64_t  batch, rows, cols;
+    int64_t  ld;            /* bytes between rows; >= ceil(cols / 32) * 16; multiple of 16    */
+    int32_t  format;        /* mor_fp4_format_t                                               */
+} mor_fp4_matrix_t;
+
+/* Bytes of the two arrays of such a stack (ld the smallest allowed); 0 on a bad argument. */
+MOR_API size_t mor_fp4_scale_bytes(int64_t batch, int64_t rows, int64_t cols, int format);
+
+/* What is quantised: a stack of matrices [batch][rows, cols], or rows of one matrix gathered on the way. */
+typedef struct mor_fp4_quantize_desc {
+    const void* x;          /* DEVICE, row-major, aligned to its element; full speed where x, ld and batch_stride
+                               are multiples of 32 bytes                                      */
+    int32_t dtype;          /* mor_dtype_t                                                    */
+    int32_t format;         /* mor_fp4_format_t                                               */
+    int64_t batch, rows, cols, ld, batch_stride;   /* in elements; ld >= cols                 */
+    const float* amax;      /* DEVICE, optional (E4M3_16): A if the caller has it (larger values saturate).  NULL = the
+                               library takes it from the data with one extra read             */
+    const int32_t* slot_of_row;  /* DEVICE, optional: out row i is weight[slot] * x[slot / top], slot = slot_of_row[i],
+                               zero where the slot is negative (batch must be 1)              */
+    const int32_t* row_of_slot;  /* DEVICE [rows * top], with slot_of_row: negative = the slot has no row           */
+    int64_t out_rows;       /* with slot_of_row: its length                                   */
+    int32_t top;            /* with slot_of_row: slots per row of x                           */
+    int32_t weight_dtype;   /* mor_dtype_t of weight                                          */
+    const void* weight;     /* DEVICE [rows * top], optional                                  */
+} mor_fp4_quantize_desc_t;
+
+/* Quantises along cols (host_rows: [batch][out rows, cols]), along rows (host_cols: the transposes [batch][cols, out rows],
+ * blocks along the rows of x), or both from one read; either may be NULL.  The caller fills every field of the
+ * outputs; format and shape must match.  Both get the same tensor scale.
+ * `workspace`: at least MOR_FP4_WORKSPACE_BYTES of DEVICE scratch, 16-byte aligned, no initialisation needed; may be NULL
+ * where amax is given or the format is E8M0_32. */
+#define MOR_FP4_WORKSPACE_BYTES 4096
+MOR_API mor_status_t mor_fp4_quantize(const mor_fp4_quantize_desc_t* host_desc, const mor_fp4_matrix_t* host_rows,
+                                      const mor_fp4_matrix_t* host_cols, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* The values of a stack, [batch][rows, ld_out] in `dtype` (mor_dtype_t), rounded once. */
+MOR_API mor_status_t mor_fp4_dequantize(const mor_fp4_matrix_t* host_in, void* out, int dtype, int64_t ld_out, void* cuda_stream);
+
+/* How a product is cut into groups (experts).
+ *   NONE    out[m, n] = sum_k a[m, k] b[n, k]
+ *   ROWS    rows starts[g] .. starts[g+1] of a meet matrix g of b; rows of out past starts[groups] are left untouched
+ *   REDUCE  group g sums over k in starts[g] .. starts[g+1]: out[g, m, n]; an empty group is zero            */
+typedef enum { MOR_GROUP_NONE = 0, MOR_GROUP_ROWS = 1, MOR_GROUP_REDUCE = 2 } mor_grouping_t;
+#define MOR_MAX_GROUPS 1024
+
+/* Product of 4-bit operands of one format on the tensor cores, accumulated in binary32, times both tensor scales. */
+typedef struct mor_fp4_matmul_desc {
+    mor_fp4_matrix_t a;     /* [1][M, K]                                                      */
+    mor_fp4_matrix_t b;     /* [1][N, K]; ROWS: [groups][N, K]                                */
+    void*   out;            /* DEVICE [M, ldo]; REDUCE: [groups][M, ldo]; 16-byte aligned     */
+    int32_t out_dtype;      /* mor_dtype_t                                                    */
+    int32_t grouping;       /* mor_grouping_t                                                 */
+    int64_t ldo;            /* elements between rows of out; >= N; a multiple of 16 bytes     */
+    const int32_t* starts;  /* DEVICE [groups + 1], multiples of 128 from 0 up, at most M (ROWS) or K (REDUCE)   */
+    int32_t groups;
+    uint32_t* status;       /* DEVICE, optional: set to MOR_ERR_TIMEOUT when a bounded wait ran out (never cleared)   */
+} mor_fp4_matmul_desc_t;
+MOR_API mor_status_t mor_fp4_matmul(const mor_fp4_matmul_desc_t* host_desc, void* cuda_stream);
+
+/* ------------------------------------------------------------------------- tokens sorted by expert ----
+ * A token has `top` slots, slot = token * top + j, each with an expert id and a weight.  Sorting gives every slot with an
+ * id of 0 .. experts-1 a row: an expert's rows are consecutive, in slot order, and start at a multiple of `align`.  Slots
+ * with any other id (masked tokens, dropped slots) have no row. */
+
+/* Rows that n_slots slots can take at most: each of up to min(n_slots, experts) experts may leave align-1 rows empty. */
+MOR_API int64_t mor_expert_rows(int64_t n_slots, int experts, int align);
+MOR_API size_t mor_expert_workspace_bytes(int64_t n_slots, int experts);
+
+/* ids [n_slots] -> starts [experts + 1], row_of_slot [n_slots] (-1: none), slot_of_row [mor_expert_rows()] (-1: empty).
+ * All DEVICE int32.  experts <= MOR_MAX_GROUPS, n_slots < 2^30. */
+MOR_API mor_status_t mor_expert_sort(const int32_t* ids, int64_t n_slots, int experts, int align, int32_t* starts,
+                                     int32_t* row_of_slot, int32_t* slot_of_row, void* workspace, size_t workspace_bytes,
+                                     void* cuda_stream);
+
+/* Rows of a token matrix and of the matrix sorted by expert, and what connects them. */
+typedef struct mor_expert_desc {
+    int64_t tokens, rows, hidden;  /* rows = mor_expert_rows()                                */
+    int32_t top;
+    int32_t dtype;                 /* mor_dtype_t of every matrix                             */
+    const int32_t* row_of_slot;    /* DEVICE [tokens * top]                                   */
+    const int32_t* slot_of_row;    /* DEVICE [rows]                                           */
+    const void* weight;            /* DEVICE [tokens * top], optional (NULL = 1)              */
+    int32_t weight_dtype;          /* mor_dtype_t                                             */
+} mor_expert_desc_t;
+
+/* out[row] = weight[slot] * x[token] for every row with a slot, zero for the others (products in binary32, one rounding). */
+MOR_API mor_status_t mor_expert_gather(const mor_expert_desc_t* host_desc, const void* x, int64_t ldx, void* out, int64_t ldo,
+                                       void* cuda_stream);
+/* out[token] = sum over its slots, in order, of weight[slot] * ys[row] (binary32 sums, one rounding); the gradient of a gather
+ * without weights. */
+MOR_API mor_status_t mor_expert_combine(const mor_expert_desc_t* host_desc, const void* ys, int64_t ldy, void* out, int64_t ldo,
+                                        void* cuda_stream);
+/* The gradient of combine: dys[row] = weight[slot] * dy[token] (zero for rows without a slot; dys may be NULL) and
+ * dweight[slot] = <dy[token], ys[row]> in weight_dtype (0 for slots without a row; may be NULL, ys is then not read). */
+MOR_API mor_status_t mor_expert_combine_grad(const mor_expert_desc_t* host_desc, const void* dy, int64_t lddy, const void* ys,
+                                             int64_t ldy, void* dys, int64_t lddys, void* dweight, void* cuda_stream);
 
 MOR_API const char* mor_status_string(mor_status_t status);
 MOR_API int mor_version(void);

@@ -7,6 +7,8 @@ library has not been built, the first call raises.
 Low level (one-to-one with ``include/mor.h``):
     mor_workspace_bytes, mor_analyze_quantize, mor_analyze_quantize_batched,
     mor_analyze_quantize_batched_ex, mor_select_stats, mor_select_stats_batched, mor_group_amax, mor_host_staging_bytes, mor_analyze_quantize_host,
+    mor_fp4_scale_bytes, mor_fp4_quantize, mor_fp4_dequantize, mor_fp4_matmul, mor_expert_rows, mor_expert_workspace_bytes,
+    mor_expert_sort, mor_expert_gather, mor_expert_combine, mor_expert_combine_grad (used through ``fp4`` and ``experts``),
     mor_status_string, mor_version
 
 Helpers that allocate outputs with torch and fill the descriptors:
@@ -33,6 +35,11 @@ MOR_SCALE_GAM, MOR_SCALE_E8M0, MOR_SCALE_FP32_AMAX = 0, 1, 2
 MOR_CRIT_TENSOR_MEAN_REL, MOR_CRIT_BLOCK_VS_E5M2, MOR_CRIT_BLOCK_MEAN_REL = 0, 1, 2
 MOR_FLAG_STRICT_TIES, MOR_FLAG_RANGE_MIN_INCLUDES_ZERO = 1, 2
 MOR_ERROR_BINS = 12
+MOR_FP4_E4M3_16, MOR_FP4_E8M0_32 = 0, 1
+MOR_DTYPE_BF16, MOR_DTYPE_F32 = 0, 1
+MOR_GROUP_NONE, MOR_GROUP_ROWS, MOR_GROUP_REDUCE = 0, 1, 2
+MOR_FP4_WORKSPACE_BYTES = 4096
+MOR_MAX_GROUPS = 1024
 
 
 class MorError(RuntimeError):
@@ -72,6 +79,28 @@ class mor_outputs_t(C.Structure):
 class mor_stage_events_t(C.Structure):
     _fields_ = [("amax_begin", C.c_void_p), ("main_begin", C.c_void_p), ("main_end", C.c_void_p),
                 ("finalise_end", C.c_void_p)]
+
+
+class mor_fp4_matrix_t(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("tensor_scale", C.c_void_p), ("batch", C.c_int64),
+                ("rows", C.c_int64), ("cols", C.c_int64), ("ld", C.c_int64), ("format", C.c_int32)]
+
+
+class mor_fp4_quantize_desc_t(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("dtype", C.c_int32), ("format", C.c_int32), ("batch", C.c_int64), ("rows", C.c_int64),
+                ("cols", C.c_int64), ("ld", C.c_int64), ("batch_stride", C.c_int64), ("amax", C.c_void_p),
+                ("slot_of_row", C.c_void_p), ("row_of_slot", C.c_void_p), ("out_rows", C.c_int64), ("top", C.c_int32),
+                ("weight_dtype", C.c_int32), ("weight", C.c_void_p)]
+
+
+class mor_fp4_matmul_desc_t(C.Structure):
+    _fields_ = [("a", mor_fp4_matrix_t), ("b", mor_fp4_matrix_t), ("out", C.c_void_p), ("out_dtype", C.c_int32),
+                ("grouping", C.c_int32), ("ldo", C.c_int64), ("starts", C.c_void_p), ("groups", C.c_int32), ("status", C.c_void_p)]
+
+
+class mor_expert_desc_t(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("rows", C.c_int64), ("hidden", C.c_int64), ("top", C.c_int32), ("dtype", C.c_int32),
+                ("row_of_slot", C.c_void_p), ("slot_of_row", C.c_void_p), ("weight", C.c_void_p), ("weight_dtype", C.c_int32)]
 
 
 BLOCK_STATS_DTYPE = np.dtype([("amax", "f4"), ("min_abs_nz", "f4"), ("nnz", "u4"), ("n_nonfinite", "u4"),
@@ -116,6 +145,26 @@ def load():
         L.mor_analyze_quantize_host.argtypes = [pd, po, C.c_void_p, C.c_size_t, C.c_void_p]
         L.mor_analyze_quantize_static.restype = C.c_int
         L.mor_analyze_quantize_static.argtypes = [pd, po, C.c_void_p]
+        vp, i32, i64 = C.c_void_p, C.c_int, C.c_int64
+        pm = C.POINTER(mor_fp4_matrix_t)
+        L.mor_fp4_scale_bytes.restype = C.c_size_t
+        L.mor_fp4_scale_bytes.argtypes = [i64, i64, i64, i32]
+        L.mor_fp4_quantize.restype = i32
+        L.mor_fp4_quantize.argtypes = [C.POINTER(mor_fp4_quantize_desc_t), pm, pm, vp, C.c_size_t, vp]
+        L.mor_fp4_dequantize.restype = i32
+        L.mor_fp4_dequantize.argtypes = [pm, vp, i32, i64, vp]
+        L.mor_fp4_matmul.restype = i32
+        L.mor_fp4_matmul.argtypes = [C.POINTER(mor_fp4_matmul_desc_t), vp]
+        L.mor_expert_rows.restype = i64
+        L.mor_expert_rows.argtypes = [i64, i32, i32]
+        L.mor_expert_workspace_bytes.restype = C.c_size_t
+        L.mor_expert_workspace_bytes.argtypes = [i64, i32]
+        L.mor_expert_sort.restype = i32
+        L.mor_expert_sort.argtypes = [vp, i64, i32, i32, vp, vp, vp, vp, C.c_size_t, vp]
+        pe = C.POINTER(mor_expert_desc_t)
+        L.mor_expert_gather.restype = L.mor_expert_combine.restype = L.mor_expert_combine_grad.restype = i32
+        L.mor_expert_gather.argtypes = L.mor_expert_combine.argtypes = [pe, vp, i64, vp, i64, vp]
+        L.mor_expert_combine_grad.argtypes = [pe, vp, i64, vp, i64, vp, i64, vp, vp]
         L.mor_status_string.restype = C.c_char_p
         L.mor_status_string.argtypes = [C.c_int]
         L.mor_version.restype = C.c_int
@@ -127,7 +176,9 @@ def load():
 EXPORTS = ["mor_workspace_bytes", "mor_analyze_quantize", "mor_analyze_quantize_batched",
            "mor_analyze_quantize_batched_ex", "mor_select_stats", "mor_select_stats_batched",
            "mor_group_amax", "mor_host_staging_bytes", "mor_analyze_quantize_host",
-           "mor_analyze_quantize_static", "mor_status_string", "mor_version"]
+           "mor_analyze_quantize_static", "mor_fp4_scale_bytes", "mor_fp4_quantize", "mor_fp4_dequantize", "mor_fp4_matmul",
+           "mor_expert_rows", "mor_expert_workspace_bytes", "mor_expert_sort", "mor_expert_gather", "mor_expert_combine",
+           "mor_expert_combine_grad", "mor_status_string", "mor_version"]
 
 
 # ------------------------------------------------------------------ C entry points ----

@@ -14,7 +14,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmor_b200.so")
 SOURCES = ["mor_api.cu", "mor_kernels.cu", "mor_static.cu", "mor_main.cu", "mor_main_tensor.cu", "mor_main_row128.cu",
-           "mor_main_blk128.cu", "mor_main_blk64.cu", "mor_main_col128.cu", "mor_main_channel.cu", "mor_main_dual.cu", "mor_main_colch.cu"]
+           "mor_main_blk128.cu", "mor_main_blk64.cu", "mor_main_col128.cu", "mor_main_channel.cu", "mor_main_dual.cu", "mor_main_colch.cu",
+           "fp4/mor_fp4_quant.cu", "fp4/mor_fp4_gemm.cu", "fp4/mor_experts.cu"]
 OBJ_DIR = os.path.join(HERE, "_build")
 
 
@@ -26,7 +27,8 @@ def nvcc_path() -> str:
 
 
 def _deps():
-    return [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "mor.h")]
+    files = [os.path.join(d, f) for d, _, names in os.walk(CSRC) for f in names]
+    return files + [os.path.join(ROOT, "include", "mor.h")]
 
 
 def needs_build() -> bool:
@@ -54,7 +56,7 @@ def build(force: bool = False, verbose: bool = False, lib: str = LIB, extra_flag
     newest = max(os.path.getmtime(d) for d in _deps() if d.endswith((".h", ".cuh")))
 
     def compile_one(src: str) -> str:
-        obj = os.path.join(obj_dir, src[:-3] + ".o")
+        obj = os.path.join(obj_dir, os.path.basename(src)[:-3] + ".o")
         path = os.path.join(CSRC, src)
         if force or verbose or not os.path.exists(obj) or os.path.getmtime(obj) < max(os.path.getmtime(path), newest):
             subprocess.run([nvcc_path(), *flags, "-c", path, "-o", obj], check=True)

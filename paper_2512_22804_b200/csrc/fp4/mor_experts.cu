@@ -1,0 +1,551 @@
+// Tokens sorted by expert and back: a stable counting sort of the slots, the gather of token rows, the weighted sum that brings
+// the experts' rows back, and the gradient of that sum.
+//
+// The sort moves a few bytes per slot and is bound by launches and dependent steps: one launch up to kOneBlockSlots slots, two
+// above.  The row movers are bound by memory and all work in token order: a token's row is read once for all of its slots,
+// and the rows on the sorted side are whole contiguous rows in any order, which costs nothing extra.
+#include "mor_fp4.cuh"
+
+namespace mor {
+namespace {
+
+// ------------------------------------------------------------------------------------------------ sort ----
+
+constexpr int kSortThreads = 1024;
+constexpr int kSortWarps = kSortThreads / 32;
+constexpr int64_t kOneBlockSlots = 4096;      // one CTA sorts these in four rounds of its threads; a second launch costs more
+constexpr int kMaxChunks = 148;
+
+struct SortParams {
+    const int32_t* ids;
+    int64_t n, chunk;          // slots; slots per CTA (a multiple of 1024)
+    int64_t capacity;
+    int32_t experts, align;
+    int32_t *starts, *row_of_slot, *slot_of_row;
+    int32_t* hist;             // [chunks][experts], of the chunks' slots per expert
+};
+
+// The part of a chunk that a warp walks: whole groups of 32 slots.
+__device__ __forceinline__ void warp_part(const SortParams& p, int64_t& first, int64_t& last)
+{
+    const int64_t begin = (int64_t)blockIdx.x * p.chunk, end = min(begin + p.chunk, p.n);
+    const int64_t per = (end - begin + kSortThreads - 1) / kSortThreads * 32;
+    first = min(begin + (threadIdx.x >> 5) * per, end);
+    last = min(first + per, end);
+}
+
+// Slots per (warp, expert) of this CTA's chunk.  Lanes with the same expert are found by a match; one of them adds.
+__device__ void count_slots(const SortParams& p, int32_t* counts)
+{
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    for (int i = threadIdx.x; i < kSortWarps * p.experts; i += kSortThreads) counts[i] = 0;
+    __syncthreads();
+    int64_t first, last;
+    warp_part(p, first, last);
+    for (int64_t at = first; at < last; at += 32) {
+        const int32_t id = at + lane < last ? p.ids[at + lane] : -1;
+        const uint32_t same = __match_any_sync(0xFFFFFFFFu, id);
+        if (id >= 0 && id < p.experts && lane == __ffs(same) - 1) counts[warp * p.experts + id] += __popc(same);
+        __syncwarp();
+    }
+    __syncthreads();
+}
+
+__global__ void __launch_bounds__(kSortThreads) expert_count_kernel(const __grid_constant__ SortParams p)
+{
+    extern __shared__ int32_t counts[];
+    cudaTriggerProgrammaticLaunchCompletion();
+    count_slots(p, counts);
+    for (int e = threadIdx.x; e < p.experts; e += kSortThreads) {
+        int32_t sum = 0;
+        for (int w = 0; w < kSortWarps; ++w) sum += counts[w * p.experts + e];
+        p.hist[(int64_t)blockIdx.x * p.experts + e] = sum;
+    }
+}
+
+// Inclusive sum over the CTA's threads.
+__device__ int32_t block_scan(int32_t v, int32_t* shared)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int32_t u = __shfl_up_sync(0xFFFFFFFFu, v, o);
+        if (lane >= o) v += u;
+    }
+    if (lane == 31) shared[warp] = v;
+    __syncthreads();
+    if (warp == 0) {
+        int32_t s = shared[lane];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int32_t u = __shfl_up_sync(0xFFFFFFFFu, s, o);
+            if (lane >= o) s += u;
+        }
+        shared[lane] = s;
+    }
+    __syncthreads();
+    return v + (warp > 0 ? shared[warp - 1] : 0);
+}
+
+__global__ void __launch_bounds__(kSortThreads) expert_place_kernel(const __grid_constant__ SortParams p)
+{
+    extern __shared__ int32_t counts[];                 // [warps][experts], then the next row of each
+    __shared__ int32_t scan[32];
+    __shared__ int32_t used[MOR_MAX_GROUPS + 1];        // first empty row of each expert; [experts]: first row past the last expert
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    count_slots(p, counts);
+    int32_t own = 0, before = 0, total = 0;
+    if (tid < p.experts)
+        for (int w = 0; w < kSortWarps; ++w) own += counts[w * p.experts + tid];
+    total = own;
+    if (gridDim.x > 1) {
+        cudaGridDependencySynchronize();
+        total = 0;
+        if (tid < p.experts)
+            for (uint32_t c = 0; c < gridDim.x; ++c) {
+                const int32_t h = __ldcg(p.hist + (int64_t)c * p.experts + tid);
+                if (c < blockIdx.x) before += h;
+                total += h;
+            }
+    }
+    const int32_t padded = (total + p.align - 1) / p.align * p.align;
+    const int32_t end = block_scan(tid < p.experts ? padded : 0, scan), start = end - padded;
+    if (tid < p.experts) {
+        if (blockIdx.x == 0) {
+            p.starts[tid] = start;
+            if (tid == p.experts - 1) p.starts[p.experts] = end;
+        }
+        used[tid] = start + total;
+        if (tid == p.experts - 1) used[p.experts] = end;
+        int32_t next = start + before;
+        for (int w = 0; w < kSortWarps; ++w) {
+            const int32_t c = counts[w * p.experts + tid];
+            counts[w * p.experts + tid] = next;
+            next += c;
+        }
+    }
+    __syncthreads();
+    int64_t first, last;
+    warp_part(p, first, last);
+    for (int64_t at = first; at < last; at += 32) {
+        const int64_t slot = at + lane;
+        const int32_t id = slot < last ? p.ids[slot] : -1;
+        const uint32_t same = __match_any_sync(0xFFFFFFFFu, id);
+        const bool has = id >= 0 && id < p.experts;
+        const int32_t next = has ? counts[warp * p.experts + id] : 0;
+        __syncwarp();
+        if (has && lane == __ffs(same) - 1) counts[warp * p.experts + id] = next + __popc(same);
+        __syncwarp();
+        const int32_t row = has ? next + __popc(same & ((1u << lane) - 1u)) : -1;
+        if (slot < last) p.row_of_slot[slot] = row;
+        if (has) p.slot_of_row[row] = (int32_t)slot;
+    }
+    // rows without a slot: those that alignment leaves behind each expert, and those past the last one
+    if (p.align > 1)
+        for (int e = blockIdx.x * kSortWarps + warp; e < p.experts; e += gridDim.x * kSortWarps) {
+            const int32_t stop = (used[e] + p.align - 1) / p.align * p.align;
+            for (int32_t r = used[e] + lane; r < stop; r += 32) p.slot_of_row[r] = -1;
+        }
+    for (int64_t r = used[p.experts] + (int64_t)blockIdx.x * kSortThreads + tid; r < p.capacity; r += (int64_t)gridDim.x * kSortThreads)
+        p.slot_of_row[r] = -1;
+}
+
+// ---------------------------------------------------------------------------------------- row movement ----
+
+struct MoveParams {
+    int64_t tokens, rows, hidden;
+    int64_t ld_token, ld_row, ld_out;
+    uint32_t top;
+    int32_t weight_dtype;
+    uint32_t token_blocks;     // gather and gradient: CTAs from here on clear the rows without a slot
+    const int32_t *row_of_slot, *slot_of_row;
+    const void* weight;
+    const void *tokens_in, *rows_in;   // token side (x, dy), row side (ys)
+    void* out;                         // gather: rows; combine: tokens; gradient: rows (dys, may be NULL)
+    void* dweight;
+};
+
+// What one thread moves at a time: BYTES bytes as 32-bit values.
+template <typename T, int BYTES> struct Piece {
+    static constexpr int kElems = BYTES / (int)sizeof(T);
+    static constexpr int kWords = BYTES < 4 ? 1 : BYTES / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const T* p)
+    {
+        if constexpr (BYTES == 32) ldg256(w, p);
+        else if constexpr (BYTES == 16) {
+            const uint4 q = *reinterpret_cast<const uint4*>(p);
+            w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+        } else if constexpr (BYTES == 4) w[0] = *reinterpret_cast<const uint32_t*>(p);
+        else w[0] = *reinterpret_cast<const uint16_t*>(p);
+    }
+    __device__ __forceinline__ void store(T* p) const
+    {
+        if constexpr (BYTES == 32) stg256(p, w);
+        else if constexpr (BYTES == 16) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        else if constexpr (BYTES == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
+        else *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
+    }
+    __device__ __forceinline__ float get(int i) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        else return i & 1 ? bf16_high(w[i >> 1]) : bf16_low(w[i >> 1]);
+    }
+    __device__ __forceinline__ void set_all(const float* v)
+    {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < kElems; ++i) w[i] = __float_as_uint(v[i]);
+        } else if constexpr (kElems == 1) w[0] = bf16x2_of(v[0], 0.f);
+        else {
+#pragma unroll
+            for (int i = 0; i < kElems; i += 2) w[i >> 1] = bf16x2_of(v[i], v[i + 1]);
+        }
+    }
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (uint32_t& u : w) u = 0;
+    }
+    __device__ __forceinline__ Piece scaled(float s) const
+    {
+        float v[kElems];
+        Piece r;
+#pragma unroll
+        for (int i = 0; i < kElems; ++i) v[i] = get(i) * s;
+        r.set_all(v);
+        return r;
+    }
+};
+
+// Zeroes the rows without a slot among this CTA's 256.
+template <typename T, int BYTES> __device__ void clear_rows(const MoveParams& p, T* out, uint32_t block)
+{
+    using P = Piece<T, BYTES>;
+    __shared__ uint32_t empty[8];
+    const int64_t base = (int64_t)block * 256;
+    for (int i = threadIdx.x; i < 256; i += blockDim.x) {           // blockDim.x is a multiple of 32
+        const bool none = base + i < p.rows && p.slot_of_row[base + i] < 0;
+        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, none);
+        if ((i & 31) == 0) empty[i >> 5] = mask;
+    }
+    __syncthreads();
+    P zero;
+    zero.clear();
+    for (int k = 0; k < 8; ++k)
+        for (uint32_t m = empty[k]; m != 0; m &= m - 1) {
+            T* to = out + (base + k * 32 + __ffs(m) - 1) * p.ld_out;
+            for (int64_t c = (int64_t)threadIdx.x * P::kElems; c < p.hidden; c += (int64_t)blockDim.x * P::kElems) zero.store(to + c);
+        }
+}
+
+template <typename T, int BYTES> __global__ void __launch_bounds__(256) expert_gather_kernel(const __grid_constant__ MoveParams p)
+{
+    using P = Piece<T, BYTES>;
+    T* out = static_cast<T*>(p.out);
+    if (blockIdx.x >= p.token_blocks) {
+        clear_rows<T, BYTES>(p, out, blockIdx.x - p.token_blocks);
+        return;
+    }
+    const int64_t token = blockIdx.x;
+    const T* x = static_cast<const T*>(p.tokens_in) + token * p.ld_token;
+    const int32_t* rows = p.row_of_slot + token * p.top;
+    for (int64_t c = (int64_t)threadIdx.x * P::kElems; c < p.hidden; c += (int64_t)blockDim.x * P::kElems) {
+        P v;
+        v.load(x + c);
+        for (uint32_t j = 0; j < p.top; ++j) {
+            const int32_t row = rows[j];
+            if (row < 0) continue;
+            T* to = out + (int64_t)row * p.ld_out + c;
+            if (p.weight == nullptr) v.store(to);
+            else v.scaled(weight_at(p.weight, p.weight_dtype, token * p.top + j)).store(to);
+        }
+    }
+}
+
+constexpr int kAtOnce = 4;      // slots whose rows are in flight together
+
+template <typename T, int BYTES> __global__ void __launch_bounds__(256) expert_combine_kernel(const __grid_constant__ MoveParams p)
+{
+    using P = Piece<T, BYTES>;
+    const int64_t token = blockIdx.x;
+    const T* ys = static_cast<const T*>(p.rows_in);
+    T* out = static_cast<T*>(p.out) + token * p.ld_out;
+    for (int64_t c = (int64_t)threadIdx.x * P::kElems; c < p.hidden; c += (int64_t)blockDim.x * P::kElems) {
+        float sum[P::kElems];
+#pragma unroll
+        for (float& s : sum) s = 0.f;
+        for (uint32_t j0 = 0; j0 < p.top; j0 += kAtOnce) {
+            P v[kAtOnce];
+            float w[kAtOnce];
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+                const int64_t slot = token * p.top + j0 + j;
+                const int32_t row = j0 + j < p.top ? p.row_of_slot[slot] : -1;
+                w[j] = 0.f;
+                v[j].clear();
+                if (row >= 0) {
+                    v[j].load(ys + (int64_t)row * p.ld_row + c);
+                    w[j] = p.weight == nullptr ? 1.f : weight_at(p.weight, p.weight_dtype, slot);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+                for (int i = 0; i < P::kElems; ++i) sum[i] = fmaf(w[j], v[j].get(i), sum[i]);
+        }
+        P r;
+        r.set_all(sum);
+        r.store(out + c);
+    }
+}
+
+// The sums over hidden of <dy, ys> are taken per thread in column order, then over the CTA in a fixed tree: the result
+// does not change from run to run.
+template <typename T, int BYTES> __global__ void __launch_bounds__(256) expert_grad_kernel(const __grid_constant__ MoveParams p)
+{
+    using P = Piece<T, BYTES>;
+    T* out = static_cast<T*>(p.out);
+    if (blockIdx.x >= p.token_blocks) {
+        clear_rows<T, BYTES>(p, out, blockIdx.x - p.token_blocks);
+        return;
+    }
+    __shared__ float part[kAtOnce][8];
+    const int64_t token = blockIdx.x;
+    const T* dy = static_cast<const T*>(p.tokens_in) + token * p.ld_token;
+    const T* ys = static_cast<const T*>(p.rows_in);
+    const int warps = blockDim.x >> 5;
+    for (uint32_t j0 = 0; j0 < p.top; j0 += kAtOnce) {
+        float dot[kAtOnce], w[kAtOnce];
+        int32_t row[kAtOnce];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            const int64_t slot = token * p.top + j0 + j;
+            row[j] = j0 + j < p.top ? p.row_of_slot[slot] : -1;
+            w[j] = row[j] < 0 || p.weight == nullptr ? 1.f : weight_at(p.weight, p.weight_dtype, slot);
+            dot[j] = 0.f;
+        }
+        for (int64_t c = (int64_t)threadIdx.x * P::kElems; c < p.hidden; c += (int64_t)blockDim.x * P::kElems) {
+            P g, v[kAtOnce];
+            g.load(dy + c);
+            if (p.dweight != nullptr) {
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j)
+                    if (row[j] >= 0) v[j].load(ys + (int64_t)row[j] * p.ld_row + c);
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j)
+                    if (row[j] >= 0)
+#pragma unroll
+                        for (int i = 0; i < P::kElems; ++i) dot[j] = fmaf(g.get(i), v[j].get(i), dot[j]);
+            }
+            if (out != nullptr) {
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j)
+                    if (row[j] >= 0) {
+                        T* to = out + (int64_t)row[j] * p.ld_out + c;
+                        if (p.weight == nullptr) g.store(to);
+                        else g.scaled(w[j]).store(to);
+                    }
+            }
+        }
+        if (p.dweight == nullptr) continue;
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) dot[j] += __shfl_xor_sync(0xFFFFFFFFu, dot[j], o);
+            if ((threadIdx.x & 31) == 0) part[j][threadIdx.x >> 5] = dot[j];
+        }
+        __syncthreads();
+        if (threadIdx.x < kAtOnce && j0 + threadIdx.x < p.top) {
+            float s = part[threadIdx.x][0];
+            for (int k = 1; k < warps; ++k) s += part[threadIdx.x][k];
+            const int64_t slot = token * p.top + j0 + threadIdx.x;
+            if (p.weight_dtype == MOR_DTYPE_BF16) static_cast<__nv_bfloat16*>(p.dweight)[slot] = __float2bfloat16(s);
+            else static_cast<float*>(p.dweight)[slot] = s;
+        }
+        __syncthreads();
+    }
+}
+
+enum Move : int { MOVE_GATHER, MOVE_COMBINE, MOVE_GRAD };
+
+template <typename T, int BYTES> cudaError_t move_launch(const MoveParams& p, Move what, uint32_t grid, cudaStream_t st)
+{
+    const int64_t pieces = ceil_div(p.hidden, BYTES / (int64_t)sizeof(T));
+    const uint32_t threads = pieces >= 256 ? 256u : (uint32_t)(ceil_div(pieces, 32) * 32);
+    if (what == MOVE_GATHER) return launch(expert_gather_kernel<T, BYTES>, grid, threads, 0, st, false, p);
+    if (what == MOVE_COMBINE) return launch(expert_combine_kernel<T, BYTES>, grid, threads, 0, st, false, p);
+    return launch(expert_grad_kernel<T, BYTES>, grid, threads, 0, st, false, p);
+}
+template <typename T> cudaError_t move_access(const MoveParams& p, Move what, uint32_t grid, int access, cudaStream_t st)
+{
+    // vector pieces must not run past a row: the width has to be a multiple too
+    const int64_t width = p.hidden * (int64_t)sizeof(T);
+    if (access == 32 && width % 32 == 0) return move_launch<T, 32>(p, what, grid, st);
+    if (access >= 16 && width % 16 == 0) return move_launch<T, 16>(p, what, grid, st);
+    return move_launch<T, (int)sizeof(T)>(p, what, grid, st);
+}
+
+// Checks what all movers share and fills the parameters.
+mor_status_t move_params(const mor_expert_desc_t* d, MoveParams& p)
+{
+    if (d == nullptr || !is_dtype(d->dtype) || d->top < 1) return MOR_ERR_INVALID_ARG;
+    if (d->tokens < 0 || d->rows < 0 || d->hidden < 0 || d->tokens >= (1ll << 30) || d->rows >= (1ll << 31) || d->hidden >= (1ll << 31)) return MOR_ERR_INVALID_ARG;
+    if (d->tokens * d->top >= (1ll << 30)) return MOR_ERR_INVALID_ARG;
+    if (d->weight != nullptr && !is_dtype(d->weight_dtype)) return MOR_ERR_INVALID_ARG;
+    if (d->weight != nullptr && !is_aligned(d->weight, dtype_bytes(d->weight_dtype))) return MOR_ERR_ALIGNMENT;
+    if (d->tokens > 0 && d->row_of_slot == nullptr) return MOR_ERR_INVALID_ARG;
+    if (d->rows > 0 && d->slot_of_row == nullptr) return MOR_ERR_INVALID_ARG;
+    p = MoveParams{};
+    p.tokens = d->tokens;
+    p.rows = d->rows;
+    p.hidden = d->hidden;
+    p.top = (uint32_t)d->top;
+    p.weight = d->weight;
+    p.weight_dtype = d->weight_dtype;
+    p.row_of_slot = d->row_of_slot;
+    p.slot_of_row = d->slot_of_row;
+    return MOR_OK;
+}
+
+// A matrix argument: pointer, pitch, alignment; `access` is narrowed to what it allows.
+mor_status_t check_rows(const void* m, int64_t rows, int64_t ld, const mor_expert_desc_t& d, int& access)
+{
+    const int es = (int)dtype_bytes(d.dtype);
+    if (ld < d.hidden || (rows > 0 && d.hidden > 0 && m == nullptr)) return MOR_ERR_INVALID_ARG;
+    if (!is_aligned(m, es)) return MOR_ERR_ALIGNMENT;
+    const int a = access_bytes(m, ld * es, 0, es);
+    access = a < access ? a : access;
+    return MOR_OK;
+}
+
+mor_status_t move_run(const mor_expert_desc_t& d, const MoveParams& p, Move what, uint32_t grid, int access, void* cuda_stream)
+{
+    if (grid == 0 || p.hidden == 0) return MOR_OK;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const cudaError_t e = d.dtype == MOR_DTYPE_BF16 ? move_access<__nv_bfloat16>(p, what, grid, access, st) : move_access<float>(p, what, grid, access, st);
+    return e == cudaSuccess ? MOR_OK : MOR_ERR_CUDA;
+}
+
+bool sort_args_ok(int64_t n_slots, int experts, int align)
+{
+    return n_slots >= 0 && n_slots < (1ll << 30) && experts >= 1 && experts <= MOR_MAX_GROUPS && align >= 1 && align <= 4096 &&
+           n_slots + (n_slots < experts ? n_slots : experts) * (int64_t)(align - 1) < (1ll << 31);
+}
+
+}  // namespace
+}  // namespace mor
+
+using namespace mor;
+
+extern "C" {
+
+int64_t mor_expert_rows(int64_t n_slots, int experts, int align)
+{
+    if (!sort_args_ok(n_slots, experts, align)) return -1;
+    return (n_slots + (n_slots < experts ? n_slots : experts) * (int64_t)(align - 1)) / align * align;
+}
+
+size_t mor_expert_workspace_bytes(int64_t n_slots, int experts)
+{
+    if (!sort_args_ok(n_slots, experts, 1)) return 0;
+    return n_slots <= kOneBlockSlots ? 256 : (size_t)kMaxChunks * experts * sizeof(int32_t);
+}
+
+mor_status_t mor_expert_sort(const int32_t* ids, int64_t n_slots, int experts, int align, int32_t* starts, int32_t* row_of_slot,
+                             int32_t* slot_of_row, void* workspace, size_t workspace_bytes, void* cuda_stream)
+{
+    if (!sort_args_ok(n_slots, experts, align) || starts == nullptr) return MOR_ERR_INVALID_ARG;
+    if (n_slots > 0 && (ids == nullptr || row_of_slot == nullptr || slot_of_row == nullptr)) return MOR_ERR_INVALID_ARG;
+    if (!is_aligned(ids, 4) || !is_aligned(starts, 4) || !is_aligned(row_of_slot, 4) || !is_aligned(slot_of_row, 4)) return MOR_ERR_ALIGNMENT;
+    SortParams p = {};
+    uint32_t chunks = 1;
+    p.chunk = kOneBlockSlots;
+    if (n_slots > kOneBlockSlots) {
+        if (workspace == nullptr || workspace_bytes < mor_expert_workspace_bytes(n_slots, experts)) return MOR_ERR_WORKSPACE;
+        if (!is_aligned(workspace, 16)) return MOR_ERR_ALIGNMENT;
+        p.chunk = ceil_div(ceil_div(n_slots, kMaxChunks), kSortThreads) * kSortThreads;
+        chunks = (uint32_t)ceil_div(n_slots, p.chunk);
+    }
+    p.ids = ids;
+    p.n = n_slots;
+    p.capacity = mor_expert_rows(n_slots, experts, align);
+    p.experts = experts;
+    p.align = align;
+    p.starts = starts;
+    p.row_of_slot = row_of_slot;
+    p.slot_of_row = slot_of_row;
+    p.hist = static_cast<int32_t*>(workspace);
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const size_t smem = (size_t)kSortWarps * experts * sizeof(int32_t);
+    static std::atomic<uint64_t> done_count{0}, done_place{0};
+    const int most = kSortWarps * MOR_MAX_GROUPS * (int)sizeof(int32_t);
+    if (!allow_smem(expert_place_kernel, most, done_place)) return MOR_ERR_CUDA;
+    if (chunks > 1) {
+        if (!allow_smem(expert_count_kernel, most, done_count)) return MOR_ERR_CUDA;
+        if (launch(expert_count_kernel, chunks, kSortThreads, smem, st, false, p) != cudaSuccess) return MOR_ERR_CUDA;
+    }
+    return launch(expert_place_kernel, chunks, kSortThreads, smem, st, chunks > 1, p) == cudaSuccess ? MOR_OK : MOR_ERR_CUDA;
+}
+
+mor_status_t mor_expert_gather(const mor_expert_desc_t* host_desc, const void* x, int64_t ldx, void* out, int64_t ldo, void* cuda_stream)
+{
+    MoveParams p;
+    mor_status_t s = move_params(host_desc, p);
+    if (s != MOR_OK) return s;
+    int access = 32;
+    if ((s = check_rows(x, p.tokens, ldx, *host_desc, access)) != MOR_OK) return s;
+    if ((s = check_rows(out, p.rows, ldo, *host_desc, access)) != MOR_OK) return s;
+    p.tokens_in = x;
+    p.ld_token = ldx;
+    p.out = out;
+    p.ld_out = ldo;
+    p.token_blocks = (uint32_t)p.tokens;
+    return move_run(*host_desc, p, MOVE_GATHER, p.token_blocks + (uint32_t)ceil_div(p.rows, 256), access, cuda_stream);
+}
+
+mor_status_t mor_expert_combine(const mor_expert_desc_t* host_desc, const void* ys, int64_t ldy, void* out, int64_t ldo, void* cuda_stream)
+{
+    MoveParams p;
+    mor_status_t s = move_params(host_desc, p);
+    if (s != MOR_OK) return s;
+    int access = 32;
+    if ((s = check_rows(ys, p.rows, ldy, *host_desc, access)) != MOR_OK) return s;
+    if ((s = check_rows(out, p.tokens, ldo, *host_desc, access)) != MOR_OK) return s;
+    p.rows_in = ys;
+    p.ld_row = ldy;
+    p.out = out;
+    p.ld_out = ldo;
+    return move_run(*host_desc, p, MOVE_COMBINE, (uint32_t)p.tokens, access, cuda_stream);
+}
+
+mor_status_t mor_expert_combine_grad(const mor_expert_desc_t* host_desc, const void* dy, int64_t lddy, const void* ys, int64_t ldy,
+                                     void* dys, int64_t lddys, void* dweight, void* cuda_stream)
+{
+    MoveParams p;
+    mor_status_t s = move_params(host_desc, p);
+    if (s != MOR_OK) return s;
+    if (dys == nullptr && dweight == nullptr) return MOR_ERR_INVALID_ARG;
+    if (dweight != nullptr && !is_dtype(host_desc->weight_dtype)) return MOR_ERR_INVALID_ARG;
+    if (dweight != nullptr && !is_aligned(dweight, dtype_bytes(host_desc->weight_dtype))) return MOR_ERR_ALIGNMENT;
+    int access = 32;
+    if ((s = check_rows(dy, p.tokens, lddy, *host_desc, access)) != MOR_OK) return s;
+    if (dweight != nullptr && (s = check_rows(ys, p.rows, ldy, *host_desc, access)) != MOR_OK) return s;
+    if (dys != nullptr && (s = check_rows(dys, p.rows, lddys, *host_desc, access)) != MOR_OK) return s;
+    p.tokens_in = dy;
+    p.ld_token = lddy;
+    p.rows_in = ys;
+    p.ld_row = ldy;
+    p.out = dys;
+    p.ld_out = lddys;
+    p.dweight = dweight;
+    p.token_blocks = (uint32_t)p.tokens;
+    const uint32_t clear = dys != nullptr ? (uint32_t)ceil_div(p.rows, 256) : 0;
+    if (p.hidden == 0 && dweight != nullptr && p.tokens > 0) {     // sums over nothing
+        const size_t n = (size_t)p.tokens * p.top * dtype_bytes(host_desc->weight_dtype);
+        return cudaMemsetAsync(dweight, 0, n, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? MOR_OK : MOR_ERR_CUDA;
+    }
+    return move_run(*host_desc, p, MOVE_GRAD, p.token_blocks + clear, access, cuda_stream);
+}
+
+}  // extern "C"

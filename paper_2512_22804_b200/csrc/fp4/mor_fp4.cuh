@@ -1,0 +1,222 @@
+// What the 4-bit kernels share: the E2M1 and scale conversions of one unit (32 consecutive elements), vector accesses,
+// the layout of the scale tiles, and the host-side checks of an operand.
+#pragma once
+#include <atomic>
+#include <utility>
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "mor.h"
+
+namespace mor {
+namespace {
+
+constexpr int kUnit = 32;                 // elements one thread converts at a time: two E4M3_16 blocks or one E8M0_32 block
+constexpr int kScaleTile = 512;           // bytes of a scale tile: 128 rows x 4 blocks
+
+template <int FMT> struct Fp4 {
+    static constexpr int kBlock = FMT == MOR_FP4_E4M3_16 ? 16 : 32;
+    static constexpr int kBlocksPerUnit = kUnit / kBlock;
+};
+
+// Byte of a row and a block inside its scale tile.
+__device__ __forceinline__ int scale_at(int row, int block) { return (row & 31) * 16 + ((row >> 5) & 3) * 4 + (block & 3); }
+
+// What a thread needs of the tensor's maximum.
+struct TensorScale {
+    float t;        // tensor scale
+    float den;      // A * 2^-16 (block scales are fl(448 a / A); both sides carry 2^-16 so that 448 a cannot overflow)
+};
+__device__ __forceinline__ TensorScale tensor_scale_of(float amax)
+{
+    const float a = fmaxf(amax, 0x1p-88f);      // below 2^-88 the reciprocal of s * t could overflow
+    return {__fdiv_rn(a, 2688.0f), a * 0x1p-16f};
+}
+
+// Largest magnitude; NaN if any element is NaN (then, and for infinities, the result is not below infinity).
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(b)));
+    return r;
+}
+template <int N> __device__ __forceinline__ float amax_of(const float* v)
+{
+    float m0 = 0.f, m1 = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; i += 2) { m0 = max_nan(m0, v[i]); m1 = max_nan(m1, v[i + 1]); }
+    return max_nan(m0, m1);
+}
+
+// Eight E2M1 codes of v[0..7] * q, the first in the lowest four bits.
+__device__ __forceinline__ uint32_t e2m1x8(const float* v, float q)
+{
+    uint32_t r;
+    asm("{ .reg .b8 b0, b1, b2, b3;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n"
+        "mov.b32 %0, {b0, b1, b2, b3}; }"
+        : "=r"(r)
+        : "f"(v[0] * q), "f"(v[1] * q), "f"(v[2] * q), "f"(v[3] * q), "f"(v[4] * q), "f"(v[5] * q), "f"(v[6] * q), "f"(v[7] * q));
+    return r;
+}
+
+// Two E4M3 codes of (lo, hi) and the values they stand for.
+__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi, float& dlo, float& dhi)
+{
+    uint16_t c;
+    uint32_t h;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(hi), "f"(lo));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(c));
+    const __half2 d = *reinterpret_cast<__half2*>(&h);
+    dlo = __low2float(d);
+    dhi = __high2float(d);
+    return c;
+}
+
+// Codes (16 bytes) and scale bytes (low byte first) of one unit.
+template <int FMT> __device__ __forceinline__ uint4 quantise_unit(const float* v, const TensorScale& ts, uint32_t& scales)
+{
+    uint4 c;
+    if constexpr (FMT == MOR_FP4_E8M0_32) {
+        const float a = amax_of<32>(v);
+        const bool bad = !(a < INFINITY);
+        // floor(log2 a) - 2 with a bias of 127 is the exponent field less two; the fields 0 (subnormal or zero), 1 and 2 meet
+        // the bound at 0
+        const int byte = max((int)(__float_as_uint(a) >> 23) - 2, 0);
+        const float q = __uint_as_float((uint32_t)(254 - byte) << 23);
+        scales = bad ? 0xFFu : (uint32_t)byte;
+        c = make_uint4(e2m1x8(v, q), e2m1x8(v + 8, q), e2m1x8(v + 16, q), e2m1x8(v + 24, q));
+        if (bad) c = make_uint4(0, 0, 0, 0);
+    } else {
+        const float a0 = amax_of<16>(v), a1 = amax_of<16>(v + 16);
+        const bool bad0 = !(a0 < INFINITY), bad1 = !(a1 < INFINITY);
+        float s0, s1;
+        scales = e4m3x2(__fdiv_rn(a0 * (448.0f / 65536.0f), ts.den), __fdiv_rn(a1 * (448.0f / 65536.0f), ts.den), s0, s1);
+        const float q0 = s0 == 0.f ? 0.f : __frcp_rn(s0 * ts.t), q1 = s1 == 0.f ? 0.f : __frcp_rn(s1 * ts.t);
+        c = make_uint4(e2m1x8(v, q0), e2m1x8(v + 8, q0), e2m1x8(v + 16, q1), e2m1x8(v + 24, q1));
+        if (bad0) { c.x = c.y = 0; scales = (scales & 0xFF00u) | 0x7Fu; }
+        if (bad1) { c.z = c.w = 0; scales = (scales & 0x00FFu) | 0x7F00u; }
+    }
+    return c;
+}
+
+// Value of a scale byte.
+template <int FMT> __device__ __forceinline__ float scale_value(uint32_t byte)
+{
+    if constexpr (FMT == MOR_FP4_E8M0_32) {
+        if (byte == 0xFFu) return __uint_as_float(0x7FC00000u);
+        return byte == 0 ? 0x1p-127f : __uint_as_float(byte << 23);
+    } else {
+        uint32_t h;
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)byte));
+        return __low2float(*reinterpret_cast<__half2*>(&h));
+    }
+}
+
+// Two E2M1 codes (a byte) as values, the low half first.
+__device__ __forceinline__ float2 e2m1x2_value(uint32_t byte)
+{
+    uint32_t h;
+    asm("{ .reg .b8 b, z0, z1, z2; mov.b32 {b, z0, z1, z2}, %1; cvt.rn.f16x2.e2m1x2 %0, b; }" : "=r"(h) : "r"(byte));
+    return __half22float2(*reinterpret_cast<__half2*>(&h));
+}
+
+// ---- vector accesses: 32 bytes (one sector) per thread, 16 bytes, or one element
+
+__device__ __forceinline__ void ldg256(uint32_t* r, const void* p)
+{
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "l"(p));
+}
+__device__ __forceinline__ void stg256(void* p, const uint32_t* r)
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+__device__ __forceinline__ float bf16_low(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+__device__ __forceinline__ uint32_t bf16x2_of(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ float weight_at(const void* w, int dtype, int64_t i)
+{
+    return dtype == MOR_DTYPE_BF16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(w)[i]) : static_cast<const float*>(w)[i];
+}
+
+// ---- host side
+
+inline bool is_dtype(int d) { return d == MOR_DTYPE_BF16 || d == MOR_DTYPE_F32; }
+inline size_t dtype_bytes(int d) { return d == MOR_DTYPE_BF16 ? 2 : 4; }
+inline bool is_aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int64_t scale_blocks(int64_t cols, int format) { return ceil_div(cols, format == MOR_FP4_E4M3_16 ? 16 : 32); }
+inline int64_t scale_ktiles(int64_t cols, int format) { return ceil_div(scale_blocks(cols, format), 4); }
+
+// Widest access that base, pitch and batch pitch (bytes) allow: 32, 16, or `element`.
+inline int access_bytes(const void* p, int64_t pitch, int64_t batch_pitch, int element)
+{
+    const uint64_t all = reinterpret_cast<uintptr_t>(p) | (uint64_t)pitch | (uint64_t)batch_pitch;
+    return all % 32 == 0 ? 32 : all % 16 == 0 ? 16 : element;
+}
+
+// Sizes that every index computation of the kernels can hold.
+inline bool shape_ok(int64_t batch, int64_t rows, int64_t cols)
+{
+    const int64_t lim = (int64_t)1 << 31;
+    if (batch < 0 || rows < 0 || cols < 0 || batch >= lim || rows >= lim - 128 || cols >= lim - 128) return false;
+    const int64_t tiles = ceil_div(rows, 128) * ceil_div(cols, 64);
+    return tiles < lim && (batch == 0 || tiles == 0 || batch <= (lim - 1) / tiles);
+}
+
+inline mor_status_t check_matrix(const mor_fp4_matrix_t& m)
+{
+    if (!shape_ok(m.batch, m.rows, m.cols)) return MOR_ERR_INVALID_ARG;
+    if (m.format != MOR_FP4_E4M3_16 && m.format != MOR_FP4_E8M0_32) return MOR_ERR_INVALID_ARG;
+    if (m.ld < ceil_div(m.cols, 32) * 16) return MOR_ERR_INVALID_ARG;
+    if (m.tensor_scale == nullptr) return MOR_ERR_INVALID_ARG;
+    const bool empty = m.batch == 0 || m.rows == 0 || m.cols == 0;
+    if (!empty && (m.codes == nullptr || m.scales == nullptr)) return MOR_ERR_INVALID_ARG;
+    if (m.ld % 16 != 0 || !is_aligned(m.codes, 16) || !is_aligned(m.scales, 16) || !is_aligned(m.tensor_scale, 4)) return MOR_ERR_ALIGNMENT;
+    return MOR_OK;
+}
+
+// Lets a kernel use more than 48 KiB of dynamic shared memory, once per device and kernel (`done`: a bit per device).
+template <typename K> inline bool allow_smem(K kernel, int bytes, std::atomic<uint64_t>& done)
+{
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return false;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (done.load(std::memory_order_acquire) & bit) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+    if (dev < 64) done.fetch_or(bit, std::memory_order_release);
+    return true;
+}
+
+// One launch; `overlap` lets it start while the stream's previous kernel ends (it then waits before it reads what that wrote).
+template <typename... P, typename... A>
+inline cudaError_t launch(void (*kernel)(P...), uint32_t grid, uint32_t block, size_t smem, cudaStream_t stream, bool overlap, A&&... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = overlap ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...);
+}
+
+}  // namespace
+}  // namespace mor

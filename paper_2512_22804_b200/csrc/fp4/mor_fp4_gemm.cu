@@ -1,0 +1,592 @@
+// Products of microscaled 4-bit operands on the tensor cores: out[m, n] = ta tb sum_k (ca sa)(cb sb).
+//
+// Two kernels share the pipeline: a thread copies 256 elements of the reduction axis at a time (128 bytes of codes per row,
+// swizzled, and the scale tiles) into a ring of stages, a thread moves a stage's scales to tensor memory and issues the
+// matrix instructions (64 elements each), other warps read the accumulators out.  Block scales are applied by the tensor cores;
+// the two tensor scales are one factor at the end.
+//   wide    tiles of 256 x 256 by a pair of CTAs (each holds half of both operands' rows) or 128 x 256 by one; persistent
+//   narrow  128 rows of b (a weight's outputs) x 16..128 rows of a (tokens): the product is taken transposed, so that the
+//           instruction's 128 rows are all weights; the reduction axis is split over a cluster, whose partial sums are added in rank
+//           order through distributed shared memory.
+#include "mor_fp4.cuh"
+#include "mor_internal.h"
+#include "mor_tcgen05.cuh"
+
+namespace mor {
+namespace {
+
+constexpr int kStageElems = 256;                     // of the reduction axis per stage: 128 bytes of codes, the swizzle's width
+constexpr uint32_t kFull = 0xFFFFFFFFu;
+constexpr int kCtrlBytes = 1024;
+constexpr int kMaxSmem = 227 * 1024;
+
+struct GemmParams {
+    CUtensorMap a, b, sa, sb;
+    int64_t m, n, k, ldo;
+    int32_t a_row_tiles, b_row_tiles, a_ktiles, b_ktiles;
+    const float *ta, *tb;
+    const int32_t* starts;
+    int32_t groups, grouping;
+    int32_t m_tiles, n_tiles;        // of the whole output (ROWS: the most there can be)
+    int32_t access;                  // bytes of a vector store
+    void* out;
+    uint32_t* status;
+    uint32_t skip_tile;              // test hook: this tile's first load is left out
+    long long wait_cycles;
+};
+
+// After a wait ran out: report, and leave copies and matrix instructions in flight the time to end before shared and tensor
+// memory go away (they take microseconds).
+__device__ __noinline__ void give_up(volatile uint32_t* abort_flag, uint32_t* status)
+{
+    *abort_flag = 1;
+    if (status != nullptr) atomicExch(status, (uint32_t)MOR_ERR_TIMEOUT);
+}
+__device__ __noinline__ void drain()
+{
+    const long long t0 = clock64();
+    while (clock64() - t0 < 400000) {}
+}
+
+template <int CG, int NT, int FMT> struct Wide {
+    static constexpr bool kNv = FMT == MOR_FP4_E4M3_16;
+    static constexpr int kSf = kNv ? 4 : 2;                          // scale tiles per stage and 128 rows
+    static constexpr int kGroupsB = NT / 128;
+    static constexpr int kBytesA = 128 * 128, kBytesB = NT / CG * 128;
+    static constexpr int kBytesSa = kSf * kScaleTile, kBytesSb = kGroupsB * kSf * kScaleTile;
+    static constexpr int kStage = kBytesA + kBytesB + kBytesSa + kBytesSb;
+    static constexpr int kSfCols = kSf * 4 * (1 + kGroupsB);         // tensor memory columns of a stage's scales
+    static constexpr int kFit = (kMaxSmem - kCtrlBytes - 1024) / kStage, kFitTmem = (512 - NT) / kSfCols;
+    static constexpr int kStages = kFit < kFitTmem ? kFit : kFitTmem;
+    static constexpr int kSmem = kStages * kStage + kCtrlBytes + 1024;
+};
+constexpr int kWideThreads = 384;      // copy, issue, tensor memory, idle; eight warps that read the accumulators out
+
+struct WideCtrl {
+    uint64_t full[8], empty[8], acc_full, acc_empty;
+    uint32_t tmem, abort;
+};
+static_assert(sizeof(WideCtrl) <= kCtrlBytes, "control block");
+
+// One output tile and the part of the reduction axis that it sums over.
+struct TileAt {
+    int m, n, group;        // tile row, tile column; matrix of b (ROWS) or of out (REDUCE)
+    int k0, len;
+};
+
+// Tiles are walked in bands of eight tile rows, column by column inside a band, so that the CTAs that run at the same time share
+// rows of both operands in L2.
+__device__ __forceinline__ void in_bands(int t, int m_tiles, int n_tiles, int& m, int& n)
+{
+    const int band = t / (8 * n_tiles), in = t - band * 8 * n_tiles, height = min(8, m_tiles - band * 8);
+    n = in / height;
+    m = band * 8 + in % height;
+}
+
+template <int GROUP> __device__ __forceinline__ bool tile_at(const GemmParams& p, const int32_t* starts, int t, TileAt& at)
+{
+    if constexpr (GROUP == MOR_GROUP_NONE) {
+        if (t >= p.m_tiles * p.n_tiles) return false;
+        in_bands(t, p.m_tiles, p.n_tiles, at.m, at.n);
+        at.group = 0;
+        at.k0 = 0;
+        at.len = (int)p.k;
+    } else if constexpr (GROUP == MOR_GROUP_ROWS) {
+        const int m_tiles = min(starts[p.groups] / 128, p.m_tiles);
+        if (t >= m_tiles * p.n_tiles) return false;
+        in_bands(t, m_tiles, p.n_tiles, at.m, at.n);
+        int lo = 0, hi = p.groups - 1;                  // the last group that starts at or before the tile's first row
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (starts[mid] <= at.m * 128) lo = mid;
+            else hi = mid - 1;
+        }
+        at.group = lo;
+        at.k0 = 0;
+        at.len = (int)p.k;
+    } else {
+        const int per = p.m_tiles * p.n_tiles;
+        if (t >= per * p.groups) return false;
+        at.group = t / per;
+        in_bands(t - at.group * per, p.m_tiles, p.n_tiles, at.m, at.n);
+        at.k0 = max(starts[at.group], 0) & ~127;        // copies have to start on whole scale tiles whatever the array holds
+        at.len = min(starts[at.group + 1], (int)p.k) - at.k0;
+    }
+    return true;
+}
+
+// Eight (BF16: sixteen) or fewer neighbouring values of one output row.
+template <typename T> __device__ __forceinline__ void store_row32(T* to, const uint32_t* acc, float scale, int n, int access)
+{
+    constexpr int kWords = 32 * sizeof(T) / 4;
+    uint32_t w[kWords];
+#pragma unroll
+    for (int j = 0; j < kWords; ++j) {
+        if constexpr (sizeof(T) == 2) w[j] = bf16x2_of(__uint_as_float(acc[2 * j]) * scale, __uint_as_float(acc[2 * j + 1]) * scale);
+        else w[j] = __float_as_uint(__uint_as_float(acc[j]) * scale);
+    }
+    if (n >= 32 && access == 32) {
+#pragma unroll
+        for (int j = 0; j < kWords; j += 8) stg256(reinterpret_cast<uint32_t*>(to) + j, w + j);
+    } else if (n >= 32) {
+#pragma unroll
+        for (int j = 0; j < kWords; j += 4) *reinterpret_cast<uint4*>(reinterpret_cast<uint32_t*>(to) + j) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            if (j >= n) break;
+            if constexpr (sizeof(T) == 2) reinterpret_cast<uint16_t*>(to)[j] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
+            else reinterpret_cast<uint32_t*>(to)[j] = w[j];
+        }
+    }
+}
+
+template <int CG, int NT, int FMT, typename T, int GROUP>
+__global__ void __launch_bounds__(kWideThreads, 1) fp4_wide_kernel(const __grid_constant__ GemmParams p)
+{
+    using W = Wide<CG, NT, FMT>;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ int32_t starts_s[GROUP == MOR_GROUP_NONE ? 1 : MOR_MAX_GROUPS + 1];
+    uint8_t* smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+    WideCtrl& C = *reinterpret_cast<WideCtrl*>(smem + W::kStages * W::kStage);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < W::kStages; ++s) {
+            mbar_init(&C.full[s], 1);
+            mbar_init(&C.empty[s], 1);
+        }
+        mbar_init(&C.acc_full, 1);
+        mbar_init(&C.acc_empty, 8 * CG);
+        C.abort = 0;
+        fence_mbar_init();
+        if (p.k > 0) {
+            prefetch_map(&p.a);
+            prefetch_map(&p.b);
+            prefetch_map(&p.sa);
+            prefetch_map(&p.sb);
+        }
+    }
+    if (warp == 2) tmem_alloc<CG>(&C.tmem, 512);
+    tc_fence_before();
+    cudaGridDependencySynchronize();
+    if constexpr (GROUP != MOR_GROUP_NONE)
+        for (int i = threadIdx.x; i <= p.groups; i += kWideThreads) starts_s[i] = p.starts[i];
+    if constexpr (CG == 2) cluster_sync();
+    else __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = C.tmem;
+    const int first = blockIdx.x / CG, step = gridDim.x / CG;
+    TileAt at;
+
+    if (warp == 0 && lane == 0) {                                   // ---- copies
+        uint32_t it = 0;
+        bool ok = true;
+        for (int t = first; ok && tile_at<GROUP>(p, starts_s, t, at); t += step) {
+            const int stages = (at.len + kStageElems - 1) / kStageElems;
+            const int row_a = at.m * 128 * CG + (int)rank * 128, row_b = at.n * NT + (int)rank * (NT / CG);
+            const int za = 0, zb = GROUP == MOR_GROUP_ROWS ? at.group : 0;
+            for (int s = 0; s < stages; ++s, ++it) {
+                const uint32_t slot = it % W::kStages;
+                if (it >= W::kStages && !mbar_wait(&C.empty[slot], (it / W::kStages - 1u) & 1u, &C.abort, p.wait_cycles)) {
+                    give_up(&C.abort, p.status);
+                    ok = false;
+                    break;
+                }
+                const uint32_t base = smem_addr(smem) + slot * W::kStage;
+                uint32_t bar = smem_addr(&C.full[slot]);
+                if (rank == 0) mbar_arrive_expect_tx(&C.full[slot], CG * W::kStage);
+                if constexpr (CG == 2) bar = map_rank(bar, 0);
+                const int k = at.k0 + s * kStageElems, ktile = k / (W::kNv ? 64 : 128);
+                if (!(t == (int)p.skip_tile && s == 0)) load_tile_3d<CG>(base, &p.a, k / 2, row_a, za, bar);
+                load_tile_3d<CG>(base + W::kBytesA, &p.b, k / 2, row_b, zb, bar);
+                const uint32_t sf = base + W::kBytesA + W::kBytesB;
+                load_tile_2d<CG>(sf, &p.sa, 0, (za * p.a_row_tiles + row_a / 128) * p.a_ktiles + ktile, bar);
+#pragma unroll
+                for (int g = 0; g < W::kGroupsB; ++g)
+                    load_tile_2d<CG>(sf + W::kBytesSa + g * W::kSf * kScaleTile, &p.sb, 0,
+                                     (zb * p.b_row_tiles + at.n * (NT / 128) + g) * p.b_ktiles + ktile, bar);
+            }
+        }
+    } else if (warp == 1 && lane == 0 && rank == 0) {               // ---- matrix instructions
+        uint32_t it = 0, done = 0;
+        bool ok = true;
+        for (int t = first; ok && tile_at<GROUP>(p, starts_s, t, at); t += step) {
+            const int stages = (at.len + kStageElems - 1) / kStageElems;
+            if (stages <= 0) continue;
+            if (done > 0 && !mbar_wait(&C.acc_empty, (done - 1u) & 1u, &C.abort, p.wait_cycles)) ok = false;
+            tc_fence_after();
+            for (int s = 0; ok && s < stages; ++s, ++it) {
+                const uint32_t slot = it % W::kStages;
+                if (!mbar_wait(&C.full[slot], (it / W::kStages) & 1u, &C.abort, p.wait_cycles)) {
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                const uint32_t base = smem_addr(smem) + slot * W::kStage, sf = base + W::kBytesA + W::kBytesB;
+                const uint32_t tsa = tmem + NT + slot * W::kSfCols, tsb = tsa + 4 * W::kSf;
+                const int steps = min(4, (at.len - s * kStageElems + 63) / 64);
+#pragma unroll
+                for (int j = 0; j < W::kSf; ++j) {
+                    copy_scales<CG>(tsa + 4 * j, scales_desc(sf + j * kScaleTile));
+#pragma unroll
+                    for (int g = 0; g < W::kGroupsB; ++g)
+                        copy_scales<CG>(tsb + (j * W::kGroupsB + g) * 4, scales_desc(sf + W::kBytesSa + (g * W::kSf + j) * kScaleTile));
+                }
+                const uint64_t da = codes_desc(base), db = codes_desc(base + W::kBytesA);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (j >= steps) break;
+                    const int tile = W::kNv ? j : j >> 1, byte = W::kNv ? 0 : 2 * (j & 1);
+                    mma_fp4<CG, W::kNv>(tmem, da + 2 * j, db + 2 * j, fp4_idesc(128 * CG, NT, W::kNv, byte), tsa + 4 * tile,
+                                        tsb + 4 * W::kGroupsB * tile, s > 0 || j > 0);
+                }
+                tc_commit<CG>(smem_addr(&C.empty[slot]));
+            }
+            if (ok) {
+                tc_commit<CG>(smem_addr(&C.acc_full));
+                ++done;
+            } else {
+                give_up(&C.abort, p.status);
+            }
+        }
+    } else if (warp >= 4) {                                         // ---- accumulators out
+        const int half = (warp - 4) >> 2;
+        const float scale = p.k > 0 ? *p.ta * *p.tb : 0.f;
+        const uint32_t lanes = (uint32_t)(warp & 3) << 21;
+        constexpr int kCols = NT / 2;
+        uint32_t acc[kCols], done = 0;
+        bool ok = true;
+        for (int t = first; ok && tile_at<GROUP>(p, starts_s, t, at); t += step) {
+            const int64_t row = (int64_t)at.m * 128 * CG + rank * 128 + (warp & 3) * 32 + lane;
+            const int64_t col = (int64_t)at.n * NT + half * kCols;
+            if (at.len > 0) {
+                ok = mbar_wait(&C.acc_full, done & 1u, &C.abort, p.wait_cycles);
+                ok = __all_sync(kFull, ok);
+                if (!ok) {
+                    if (lane == 0) give_up(&C.abort, p.status);
+                    break;
+                }
+                tc_fence_after();
+#pragma unroll
+                for (int j = 0; j < kCols; j += 32) tmem_load32(acc + j, tmem + lanes + half * kCols + j);
+                tc_wait_ld();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if constexpr (CG == 2) mbar_arrive_cluster(map_rank(smem_addr(&C.acc_empty), 0));
+                    else mbar_arrive(&C.acc_empty);
+                }
+                ++done;
+            } else {
+#pragma unroll
+                for (uint32_t& v : acc) v = 0;
+            }
+            if (row < p.m) {
+                T* out = static_cast<T*>(p.out) + ((GROUP == MOR_GROUP_REDUCE ? (int64_t)at.group * p.m : 0) + row) * p.ldo + col;
+                const float f = at.len > 0 ? scale : 0.f;
+#pragma unroll
+                for (int j = 0; j < kCols; j += 32)
+                    if (col + j < p.n) store_row32<T>(out + j, acc + j, f, (int)min((int64_t)32, p.n - col - j), p.access);
+            }
+            __syncwarp();
+        }
+    }
+    __syncwarp();
+    __syncthreads();
+    if (*(volatile uint32_t*)&C.abort) drain();
+    if constexpr (CG == 2) cluster_sync();
+    if (warp == 2) {
+        tc_fence_after();
+        tmem_free<CG>(tmem, 512);
+    }
+}
+
+// ---- narrow
+
+template <int NT, int FMT> struct Narrow {
+    static constexpr bool kNv = FMT == MOR_FP4_E4M3_16;
+    static constexpr int kSf = kNv ? 4 : 2;
+    static constexpr int kBytesA = 128 * 128, kBytesB = NT * 128;
+    static constexpr int kBytesSf = kSf * kScaleTile;
+    static constexpr int kStage = kBytesA + kBytesB + 2 * kBytesSf;
+    static constexpr int kSfCols = 8 * kSf;
+    static constexpr int kAcc = NT < 32 ? 32 : NT;
+    static constexpr int kTmem = 256;                               // two CTAs share an SM
+    static constexpr int kFit = (kMaxSmem / 2 - kCtrlBytes - 2048) / kStage, kFitTmem = (kTmem - kAcc) / kSfCols;
+    static constexpr int kStages = kFit < kFitTmem ? kFit : kFitTmem;
+    static constexpr int kSmem = kStages * kStage + kCtrlBytes + 1024;
+    static_assert(NT * 512 <= kStages * kStage, "the partial sums fit the ring");
+};
+constexpr int kNarrowThreads = 192;    // copy, issue, four warps that read the accumulators out
+constexpr int kMaxSplit = 8;
+
+template <int NT, int FMT, typename T> __global__ void __launch_bounds__(kNarrowThreads, 2) fp4_narrow_kernel(const __grid_constant__ GemmParams p)
+{
+    using W = Narrow<NT, FMT>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+    WideCtrl& C = *reinterpret_cast<WideCtrl*>(smem + W::kStages * W::kStage);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t split;
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(split));
+    const uint32_t rank = cluster_rank();
+    const int tile = blockIdx.x / split, feature0 = tile % p.n_tiles * 128, token0 = tile / p.n_tiles * NT;
+    const int all = (int)((p.k + kStageElems - 1) / kStageElems);
+    const int begin = (int)((int64_t)all * rank / split), end = (int)((int64_t)all * (rank + 1) / split);
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < W::kStages; ++s) {
+            mbar_init(&C.full[s], 1);
+            mbar_init(&C.empty[s], 1);
+        }
+        mbar_init(&C.acc_full, 1);
+        C.abort = 0;
+        fence_mbar_init();
+        if (p.k > 0) {
+            prefetch_map(&p.a);
+            prefetch_map(&p.b);
+            prefetch_map(&p.sa);
+            prefetch_map(&p.sb);
+        }
+    }
+    if (warp == 1) tmem_alloc<1>(&C.tmem, W::kTmem);
+    tc_fence_before();
+    cudaGridDependencySynchronize();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = C.tmem;
+
+    if (warp == 0 && lane == 0) {
+        for (int s = begin; s < end; ++s) {
+            const uint32_t it = (uint32_t)(s - begin), slot = it % W::kStages;
+            if (it >= W::kStages && !mbar_wait(&C.empty[slot], (it / W::kStages - 1u) & 1u, &C.abort, p.wait_cycles)) {
+                give_up(&C.abort, p.status);
+                break;
+            }
+            const uint32_t base = smem_addr(smem) + slot * W::kStage, bar = smem_addr(&C.full[slot]);
+            mbar_arrive_expect_tx(&C.full[slot], W::kStage);
+            const int k = s * kStageElems, ktile = k / (W::kNv ? 64 : 128);
+            if (!(tile == (int)p.skip_tile && s == begin)) load_tile_3d<1>(base, &p.b, k / 2, feature0, 0, bar);
+            load_tile_3d<1>(base + W::kBytesA, &p.a, k / 2, token0, 0, bar);
+            load_tile_2d<1>(base + W::kBytesA + W::kBytesB, &p.sb, 0, feature0 / 128 * p.b_ktiles + ktile, bar);
+            load_tile_2d<1>(base + W::kBytesA + W::kBytesB + W::kBytesSf, &p.sa, 0, token0 / 128 * p.a_ktiles + ktile, bar);
+        }
+    } else if (warp == 1 && lane == 0) {
+        bool ok = true;
+        for (int s = begin; s < end; ++s) {
+            const uint32_t it = (uint32_t)(s - begin), slot = it % W::kStages;
+            if (!mbar_wait(&C.full[slot], (it / W::kStages) & 1u, &C.abort, p.wait_cycles)) {
+                give_up(&C.abort, p.status);
+                ok = false;
+                break;
+            }
+            tc_fence_after();
+            const uint32_t base = smem_addr(smem) + slot * W::kStage, sf = base + W::kBytesA + W::kBytesB;
+            const uint32_t tsa = tmem + W::kAcc + slot * W::kSfCols, tsb = tsa + 4 * W::kSf;
+            const int steps = (int)min((int64_t)4, (p.k - (int64_t)s * kStageElems + 63) / 64);
+#pragma unroll
+            for (int j = 0; j < W::kSf; ++j) {
+                copy_scales<1>(tsa + 4 * j, scales_desc(sf + j * kScaleTile));
+                copy_scales<1>(tsb + 4 * j, scales_desc(sf + W::kBytesSf + j * kScaleTile));
+            }
+            const uint64_t da = codes_desc(base), db = codes_desc(base + W::kBytesA);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (j >= steps) break;
+                const int t = W::kNv ? j : j >> 1, byte = W::kNv ? 0 : 2 * (j & 1);
+                mma_fp4<1, W::kNv>(tmem, da + 2 * j, db + 2 * j, fp4_idesc(128, NT, W::kNv, byte), tsa + 4 * t, tsb + 4 * t, it > 0 || j > 0);
+            }
+            tc_commit<1>(smem_addr(&C.empty[slot]));
+        }
+        if (ok) tc_commit<1>(smem_addr(&C.acc_full));
+    }
+    __syncwarp();
+    const int part = warp & 3, feature = part * 32 + lane;            // a warp reads the 32 lanes of its number modulo 4
+    float* sums = reinterpret_cast<float*>(smem);
+    bool ok = true;
+    if (warp >= 2) {
+        if (begin < end) {
+            ok = __all_sync(kFull, mbar_wait(&C.acc_full, 0, &C.abort, p.wait_cycles));
+            if (!ok && lane == 0) give_up(&C.abort, p.status);
+            tc_fence_after();
+        }
+        if (ok) {
+            const uint32_t lanes = (uint32_t)part << 21;
+#pragma unroll
+            for (int j = 0; j < NT; j += 16) {
+                uint32_t acc[16];
+                if (begin < end) {
+                    tmem_load16(acc, tmem + lanes + j);
+                    tc_wait_ld();
+                } else {
+#pragma unroll
+                    for (uint32_t& v : acc) v = 0;
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sums[(j + i) * 128 + feature] = __uint_as_float(acc[i]);
+            }
+        }
+    }
+    tc_fence_before();
+    cluster_sync();
+    if (warp >= 2 && ok) {
+        const float scale = p.k > 0 ? *p.ta * *p.tb : 0.f;
+        const int64_t f = (int64_t)feature0 + feature;
+        if (f < p.n)
+            for (int j = (int)rank; j < NT && token0 + j < p.m; j += (int)split) {
+                const uint32_t from = smem_addr(sums + j * 128 + feature);
+                float s = 0.f;
+                for (uint32_t r = 0; r < split; ++r) s += lds_cluster(map_rank(from, r));
+                T* to = static_cast<T*>(p.out) + (int64_t)(token0 + j) * p.ldo + f;
+                if constexpr (sizeof(T) == 2) *to = __float2bfloat16(s * scale);
+                else *to = s * scale;
+            }
+    }
+    __syncwarp();
+    if (*(volatile uint32_t*)&C.abort) drain();
+    cluster_sync();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_free<1>(tmem, W::kTmem);
+    }
+}
+
+// ---- host side
+
+bool encode_codes(CUtensorMap& map, const mor_fp4_matrix_t& m, uint32_t box_rows, EncodeTiledFn enc)
+{
+    const cuuint64_t dims[3] = {(cuuint64_t)(ceil_div(m.cols, 32) * 16), (cuuint64_t)m.rows, (cuuint64_t)m.batch};
+    const cuuint64_t strides[2] = {(cuuint64_t)m.ld, (cuuint64_t)m.ld * (cuuint64_t)m.rows};
+    const cuuint32_t box[3] = {128, box_rows, 1}, estr[3] = {1, 1, 1};
+    return enc(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, m.codes, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// The scale tiles of the whole stack as rows of 512 bytes.
+bool encode_scales(CUtensorMap& map, const mor_fp4_matrix_t& m, uint32_t tiles, EncodeTiledFn enc)
+{
+    const cuuint64_t all = (cuuint64_t)(m.batch * ceil_div(m.rows, 128) * scale_ktiles(m.cols, m.format));
+    const cuuint64_t dims[2] = {kScaleTile / 4, all}, strides[1] = {kScaleTile};
+    const cuuint32_t box[2] = {kScaleTile / 4, tiles}, estr[2] = {1, 1};
+    return enc(&map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, m.scales, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+cudaError_t launch_cluster(void (*kernel)(GemmParams), uint32_t grid, uint32_t block, size_t smem, uint32_t cluster, cudaStream_t st, const GemmParams& p)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster;
+    at[1].val.clusterDim.y = 1;
+    at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, p);
+}
+
+template <int CG, int NT, int FMT, typename T, int GROUP>
+mor_status_t run_wide(GemmParams& p, const mor_fp4_matrix_t& a, const mor_fp4_matrix_t& b, EncodeTiledFn enc, cudaStream_t st)
+{
+    using W = Wide<CG, NT, FMT>;
+    static_assert(W::kStages >= 2 && W::kStages <= 8, "ring");
+    static std::atomic<uint64_t> done{0};
+    if (p.k > 0 && !(encode_codes(p.a, a, 128, enc) && encode_codes(p.b, b, NT / CG, enc) && encode_scales(p.sa, a, W::kSf, enc) && encode_scales(p.sb, b, W::kSf, enc)))
+        return MOR_ERR_CUDA;
+    const int64_t mt = ceil_div(p.m, 128 * CG), nt = ceil_div(p.n, NT), groups = GROUP == MOR_GROUP_REDUCE ? p.groups : 1;
+    if (mt * nt * groups >= (1ll << 31) - 1024) return MOR_ERR_UNSUPPORTED;
+    p.m_tiles = (int32_t)mt;
+    p.n_tiles = (int32_t)nt;
+    auto* kernel = fp4_wide_kernel<CG, NT, FMT, T, GROUP>;
+    if (!allow_smem(kernel, W::kSmem, done)) return MOR_ERR_CUDA;
+    const int64_t tiles = mt * nt * groups, most = 148 / CG;
+    const uint32_t grid = (uint32_t)((tiles < most ? tiles : most) * CG);
+    return launch_cluster(kernel, grid, kWideThreads, W::kSmem, CG, st, p) == cudaSuccess ? MOR_OK : MOR_ERR_CUDA;
+}
+
+template <int NT, int FMT, typename T>
+mor_status_t run_narrow(GemmParams& p, const mor_fp4_matrix_t& a, const mor_fp4_matrix_t& b, EncodeTiledFn enc, cudaStream_t st)
+{
+    using W = Narrow<NT, FMT>;
+    static_assert(W::kStages >= 2 && W::kStages <= 8, "ring");
+    static std::atomic<uint64_t> done{0};
+    if (p.k > 0 && !(encode_codes(p.a, a, NT, enc) && encode_codes(p.b, b, 128, enc) && encode_scales(p.sa, a, W::kSf, enc) && encode_scales(p.sb, b, W::kSf, enc)))
+        return MOR_ERR_CUDA;
+    const int64_t nt = ceil_div(p.n, 128), mt = ceil_div(p.m, NT), stages = ceil_div(p.k, kStageElems);
+    if (nt * mt >= (1ll << 31) / kMaxSplit) return MOR_ERR_UNSUPPORTED;
+    p.n_tiles = (int32_t)nt;
+    p.m_tiles = (int32_t)mt;
+    int64_t split = 148 * 2 / (nt * mt);
+    split = split > kMaxSplit ? kMaxSplit : split;
+    split = split > stages ? stages : split;
+    split = split < 1 ? 1 : split;
+    auto* kernel = fp4_narrow_kernel<NT, FMT, T>;
+    if (!allow_smem(kernel, W::kSmem, done)) return MOR_ERR_CUDA;
+    return launch_cluster(kernel, (uint32_t)(nt * mt * split), kNarrowThreads, W::kSmem, (uint32_t)split, st, p) == cudaSuccess ? MOR_OK : MOR_ERR_CUDA;
+}
+
+template <int FMT, typename T> mor_status_t run_format(GemmParams& p, const mor_fp4_matrix_t& a, const mor_fp4_matrix_t& b, EncodeTiledFn enc, cudaStream_t st)
+{
+    if (p.grouping == MOR_GROUP_ROWS) return run_wide<1, 256, FMT, T, MOR_GROUP_ROWS>(p, a, b, enc, st);
+    if (p.grouping == MOR_GROUP_REDUCE) return run_wide<2, 256, FMT, T, MOR_GROUP_REDUCE>(p, a, b, enc, st);
+    if (p.m <= 16) return run_narrow<16, FMT, T>(p, a, b, enc, st);
+    if (p.m <= 32) return run_narrow<32, FMT, T>(p, a, b, enc, st);
+    if (p.m <= 64) return run_narrow<64, FMT, T>(p, a, b, enc, st);
+    if (p.m <= 128) return run_narrow<128, FMT, T>(p, a, b, enc, st);
+    return run_wide<2, 256, FMT, T, MOR_GROUP_NONE>(p, a, b, enc, st);
+}
+
+}  // namespace
+}  // namespace mor
+
+using namespace mor;
+
+extern "C" mor_status_t mor_fp4_matmul(const mor_fp4_matmul_desc_t* host_desc, void* cuda_stream)
+{
+    if (host_desc == nullptr) return MOR_ERR_INVALID_ARG;
+    const mor_fp4_matmul_desc_t& d = *host_desc;
+    const bool rows = d.grouping == MOR_GROUP_ROWS, reduce = d.grouping == MOR_GROUP_REDUCE;
+    if (!is_dtype(d.out_dtype) || (d.grouping != MOR_GROUP_NONE && !rows && !reduce)) return MOR_ERR_INVALID_ARG;
+    mor_status_t s = check_matrix(d.a);
+    if (s != MOR_OK) return s;
+    if ((s = check_matrix(d.b)) != MOR_OK) return s;
+    if (d.a.format != d.b.format || d.a.cols != d.b.cols || d.a.batch != 1) return MOR_ERR_INVALID_ARG;
+    if (d.grouping != MOR_GROUP_NONE && (d.groups < 1 || d.groups > MOR_MAX_GROUPS || d.starts == nullptr)) return MOR_ERR_INVALID_ARG;
+    if (d.b.batch != (rows ? d.groups : 1)) return MOR_ERR_INVALID_ARG;
+    if (d.ldo < d.b.rows) return MOR_ERR_INVALID_ARG;
+    const int es = (int)dtype_bytes(d.out_dtype);
+    if (!is_aligned(d.out, 16) || d.ldo * es % 16 != 0 || !is_aligned(d.starts, 4) || !is_aligned(d.status, 4)) return MOR_ERR_ALIGNMENT;
+    if (d.a.rows == 0 || d.b.rows == 0) return MOR_OK;
+    if (d.out == nullptr) return MOR_ERR_INVALID_ARG;
+    EncodeTiledFn enc = encode_tiled_fn();
+    if (enc == nullptr) return MOR_ERR_CUDA;
+
+    GemmParams p = {};
+    p.m = d.a.rows;
+    p.n = d.b.rows;
+    p.k = d.a.cols;
+    p.ldo = d.ldo;
+    p.a_row_tiles = (int32_t)ceil_div(d.a.rows, 128);
+    p.b_row_tiles = (int32_t)ceil_div(d.b.rows, 128);
+    p.a_ktiles = p.b_ktiles = (int32_t)scale_ktiles(d.a.cols, d.a.format);
+    p.ta = d.a.tensor_scale;
+    p.tb = d.b.tensor_scale;
+    p.starts = d.starts;
+    p.groups = d.groups;
+    p.grouping = d.grouping;
+    p.access = access_bytes(d.out, d.ldo * es, 0, 16);
+    p.out = d.out;
+    p.status = d.status;
+    test_hook_main(p.skip_tile, p.wait_cycles);
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (d.a.format == MOR_FP4_E4M3_16)
+        return d.out_dtype == MOR_DTYPE_BF16 ? run_format<MOR_FP4_E4M3_16, __nv_bfloat16>(p, d.a, d.b, enc, st) : run_format<MOR_FP4_E4M3_16, float>(p, d.a, d.b, enc, st);
+    return d.out_dtype == MOR_DTYPE_BF16 ? run_format<MOR_FP4_E8M0_32, __nv_bfloat16>(p, d.a, d.b, enc, st) : run_format<MOR_FP4_E8M0_32, float>(p, d.a, d.b, enc, st);
+}

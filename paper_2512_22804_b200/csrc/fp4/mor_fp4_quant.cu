@@ -1,0 +1,561 @@
+// Quantisation to microscaled 4-bit codes, along the rows, along the columns, or both from one read, and its inverse.
+//
+// Both directions are bound by memory: per element 2 (or 4) bytes in, 0.5 + 1/16 (or 1/32) out per direction; the tensor maximum
+// of E4M3_16 costs one more read unless the caller has it.  One CTA takes a tile of 128 x 128 elements, so that the
+// scale tiles it writes (128 rows x 4 blocks) are whole and leave as 16-byte stores, and in the column direction the codes of a
+// transposed row leave 64 bytes at a time.  A thread takes units of 32 consecutive elements: one or two blocks, so a block's
+// maximum needs no exchange between threads.  For the column direction the tile goes through shared memory once, in the
+// input's own type where no weight is applied.
+#include "mor_fp4.cuh"
+
+namespace mor {
+namespace {
+
+constexpr int kQThreads = 256;
+constexpr int kAmaxMaxBlocks = MOR_FP4_WORKSPACE_BYTES / 4;
+constexpr int64_t kSelfAmaxElems = 32768;     // up to here every CTA takes the maximum of the whole tensor by itself: one launch
+                                              // instead of two (a CTA reads 32768 elements from L2 in about 1 us)
+
+enum Mode : int { PLAIN = 0, GATHER = 1, WEIGHTED = 2 };
+
+struct QuantParams {
+    const void* x;
+    int64_t ld, batch_stride;          // elements
+    int64_t rows, cols;                // of the output matrix along the rows
+    int64_t x_rows;                    // of x, over the whole stack when it is contiguous in rows
+    uint32_t row_tiles, col_tiles;
+    int32_t access;                    // bytes of a vector load: 32, 16, or one element
+    const float* amax;
+    const float* partial;              // maxima per CTA of the amax kernel
+    uint32_t n_partial;                // 0 with partial == NULL and amax == NULL: the CTA takes the maximum itself
+    int64_t batch;
+    const int32_t* slot_of_row;
+    const int32_t* row_of_slot;
+    uint32_t top;
+    int32_t weight_dtype;
+    const void* weight;
+    uint8_t *r_codes, *r_scales, *c_codes, *c_scales;
+    int64_t r_ld, c_ld;
+    uint32_t r_ktiles, c_ktiles, c_row_tiles;
+    float *r_t, *c_t;
+};
+
+template <typename T> struct Raw;
+template <> struct Raw<__nv_bfloat16> { uint32_t w[16]; };
+template <> struct Raw<float> { uint32_t w[32]; };
+
+// One unit from global memory; elements from n on are zero.
+template <typename T> __device__ __forceinline__ void load_unit(Raw<T>& r, const T* p, int n, int access)
+{
+    constexpr int kWords = sizeof(Raw<T>) / 4;
+    if (n >= kUnit && access == 32) {
+#pragma unroll
+        for (int i = 0; i < kWords; i += 8) ldg256(r.w + i, reinterpret_cast<const uint32_t*>(p) + i);
+    } else if (n >= kUnit && access == 16) {
+#pragma unroll
+        for (int i = 0; i < kWords; i += 4) {
+            const uint4 q = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint32_t*>(p) + i);
+            r.w[i] = q.x; r.w[i + 1] = q.y; r.w[i + 2] = q.z; r.w[i + 3] = q.w;
+        }
+    } else if constexpr (sizeof(T) == 2) {
+        const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+            const uint32_t lo = 2 * i < n ? h[2 * i] : 0, hi = 2 * i + 1 < n ? h[2 * i + 1] : 0;
+            r.w[i] = lo | (hi << 16);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) r.w[i] = i < n ? reinterpret_cast<const uint32_t*>(p)[i] : 0;
+    }
+}
+template <typename T> __device__ __forceinline__ void unpack(const Raw<T>& r, float* v)
+{
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) { v[2 * i] = bf16_low(r.w[i]); v[2 * i + 1] = bf16_high(r.w[i]); }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r.w[i]);
+    }
+}
+
+__device__ __forceinline__ float block_max(float m, float* shared)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = m;
+    __syncthreads();
+    float r = shared[0];
+#pragma unroll
+    for (int i = 1; i < kQThreads / 32; ++i) r = fmaxf(r, shared[i]);
+    __syncthreads();
+    return r;
+}
+
+// Largest finite magnitude of a unit, times the weight of each slot that has a row.  The maximum over slots of fl(w x) is
+// fl(max|w| * max|x|), since rounding is monotonic; only where that is not finite are the products looked at one by one.
+template <typename T, int MODE> __device__ __noinline__ float unit_max_careful(const Raw<T>& r, const QuantParams& p, int64_t token)
+{
+    float v[kUnit], m = 0.f;
+    unpack<T>(r, v);
+    const int slots = MODE == PLAIN ? 1 : (int)p.top;
+    for (int j = 0; j < slots; ++j) {
+        if (MODE != PLAIN && p.row_of_slot[token * p.top + j] < 0) continue;
+        const float w = MODE == WEIGHTED ? weight_at(p.weight, p.weight_dtype, token * p.top + j) : 1.f;
+#pragma unroll
+        for (int i = 0; i < kUnit; ++i) {
+            const float a = fabsf(v[i] * w);
+            if (a < INFINITY) m = fmaxf(m, a);
+        }
+    }
+    return m;
+}
+template <typename T, int MODE> __device__ __forceinline__ float unit_max(const Raw<T>& r, const QuantParams& p, int64_t token)
+{
+    float v[kUnit], w = 1.f;
+    unpack<T>(r, v);
+    const float a = amax_of<kUnit>(v);
+    if constexpr (MODE != PLAIN) {
+        w = -1.f;
+        for (uint32_t j = 0; j < p.top; ++j)
+            if (p.row_of_slot[token * p.top + j] >= 0) w = fmaxf(w, MODE == WEIGHTED ? fabsf(weight_at(p.weight, p.weight_dtype, token * p.top + j)) : 1.f);
+        if (w < 0.f && MODE == GATHER) return 0.f;
+    }
+    const float m = a * w;
+    return m >= 0.f && m < INFINITY ? m : unit_max_careful<T, MODE>(r, p, token);
+}
+
+// The largest magnitude of the whole tensor, one part per CTA (they are joined by the kernel that quantises: no counter to
+// clear, no atomics).  A thread keeps two units in flight.
+template <typename T, int MODE> __global__ void __launch_bounds__(kQThreads) fp4_amax_kernel(const __grid_constant__ QuantParams p, float* part)
+{
+    __shared__ float red[kQThreads / 32];
+    cudaTriggerProgrammaticLaunchCompletion();
+    const int64_t units = (p.cols + kUnit - 1) / kUnit;
+    const int64_t step = (int64_t)gridDim.x * kQThreads, drow = step / units, dunit = step % units;
+    const int64_t first = (int64_t)blockIdx.x * kQThreads + threadIdx.x;
+    int64_t row = first / units, unit = first % units;
+    const int64_t rows = p.x_rows * p.batch;
+    const T* x = static_cast<const T*>(p.x);
+    float m = 0.f;
+    auto address = [&](int64_t r, int64_t u) {
+        return x + (p.batch == 1 ? r * p.ld : (r / p.x_rows) * p.batch_stride + (r % p.x_rows) * p.ld) + u * kUnit;
+    };
+    auto advance = [&](int64_t& r, int64_t& u) {
+        r += drow;
+        u += dunit;
+        if (u >= units) { u -= units; ++r; }
+    };
+    while (row < rows) {
+        Raw<T> a, b;
+        int64_t row2 = row, unit2 = unit;
+        advance(row2, unit2);
+        load_unit<T>(a, address(row, unit), (int)min((int64_t)kUnit, p.cols - unit * kUnit), p.access);
+        const bool two = row2 < rows;
+        if (two) load_unit<T>(b, address(row2, unit2), (int)min((int64_t)kUnit, p.cols - unit2 * kUnit), p.access);
+        m = fmaxf(m, unit_max<T, MODE>(a, p, row));
+        if (two) m = fmaxf(m, unit_max<T, MODE>(b, p, row2));
+        row = row2;
+        unit = unit2;
+        advance(row, unit);
+    }
+    m = block_max(m, red);
+    if (threadIdx.x == 0) part[blockIdx.x] = m;
+}
+
+// Pitches of the tile in shared memory: a row of 128 elements and 16 bytes, so that a warp that walks down the columns and one
+// that writes 16-byte pieces of several rows both meet few bank conflicts.
+template <bool NARROW> struct Tile { static constexpr int kPitch = 128 * (NARROW ? 2 : 4) + 16; };
+constexpr int kStagePitch = 80;       // 64 bytes of codes of one transposed row
+
+template <typename T, int FMT, bool ROWS, bool COLS, int MODE>
+__global__ void __launch_bounds__(kQThreads) fp4_quant_kernel(const __grid_constant__ QuantParams p)
+{
+    constexpr bool kNarrow = sizeof(T) == 2 && MODE != WEIGHTED;          // the tile keeps the input's BF16 values
+    constexpr int kPitch = Tile<kNarrow>::kPitch;
+    constexpr int kTiles = FMT == MOR_FP4_E4M3_16 ? 2 : 1;                // scale tiles per 128 elements
+    constexpr int kPerUnit = Fp4<FMT>::kBlocksPerUnit;
+    __shared__ float red[kQThreads / 32];
+    __shared__ __align__(16) uint8_t row_scales[ROWS ? kTiles * kScaleTile : 16];
+    __shared__ __align__(16) uint8_t col_scales[COLS ? kTiles * kScaleTile : 16];
+    extern __shared__ __align__(16) uint8_t dyn[];                        // COLS: tile, then the codes of the transposed rows
+    const int tid = threadIdx.x;
+    const uint32_t per = p.row_tiles * p.col_tiles;
+    const uint32_t batch = blockIdx.x / per, in_batch = blockIdx.x % per;
+    const uint32_t row_tile = in_batch / p.col_tiles, col_tile = in_batch % p.col_tiles;
+    const T* x = static_cast<const T*>(p.x) + (int64_t)batch * p.batch_stride;
+
+    // both units' loads first: the tile is in flight while the tensor maximum is waited for
+    Raw<T> raw[2];
+    float weight[2] = {1.f, 1.f};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int at = tid + i * kQThreads;
+        const int64_t row = (int64_t)row_tile * 128 + (at >> 2), col = (int64_t)col_tile * 128 + (at & 3) * kUnit;
+        int64_t src = row;
+        bool have = row < p.rows && col < p.cols;
+        if constexpr (MODE != PLAIN) {
+            const int32_t slot = row < p.rows ? p.slot_of_row[row] : -1;
+            have = have && slot >= 0;
+            src = have ? slot / (int32_t)p.top : 0;
+            if (MODE == WEIGHTED && have) weight[i] = weight_at(p.weight, p.weight_dtype, slot);
+        }
+        if (have) load_unit<T>(raw[i], x + src * p.ld + col, (int)min((int64_t)kUnit, p.cols - col), p.access);
+        else
+#pragma unroll
+            for (uint32_t& w : raw[i].w) w = 0;
+    }
+
+    TensorScale ts = {1.f, 1.f};
+    if constexpr (FMT == MOR_FP4_E4M3_16) {
+        float amax = 0.f;
+        if (p.amax != nullptr) {
+            amax = *p.amax;
+        } else if (p.partial != nullptr) {
+            cudaGridDependencySynchronize();
+            for (uint32_t i = tid; i < p.n_partial; i += kQThreads) amax = fmaxf(amax, __ldcg(p.partial + i));
+            amax = block_max(amax, red);
+        } else {
+            const int64_t units = (p.cols + kUnit - 1) / kUnit;
+            for (int64_t i = tid; i < units * p.x_rows * p.batch; i += kQThreads) {
+                const int64_t r = i / units, u = i % units;
+                Raw<T> a;
+                load_unit<T>(a, static_cast<const T*>(p.x) + (r / p.x_rows) * p.batch_stride + (r % p.x_rows) * p.ld + u * kUnit,
+                             (int)min((int64_t)kUnit, p.cols - u * kUnit), p.access);
+                amax = fmaxf(amax, unit_max<T, PLAIN>(a, p, 0));
+            }
+            amax = block_max(amax, red);
+        }
+        ts = tensor_scale_of(amax);
+    }
+    if (blockIdx.x == 0 && tid == 0) {
+        if (ROWS) *p.r_t = ts.t;
+        if (COLS) *p.c_t = ts.t;
+    }
+
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int at = tid + i * kQThreads, lrow = at >> 2, u = at & 3;
+        const int64_t row = (int64_t)row_tile * 128 + lrow, col = (int64_t)col_tile * 128 + u * kUnit;
+        float v[kUnit];
+        unpack<T>(raw[i], v);
+        if constexpr (MODE == WEIGHTED) {
+#pragma unroll
+            for (float& e : v) e *= weight[i];
+        }
+        if constexpr (COLS) {
+            uint8_t* to = dyn + lrow * kPitch + u * kUnit * (kNarrow ? 2 : 4);
+            if constexpr (kNarrow) {
+#pragma unroll
+                for (int j = 0; j < 16; j += 4)
+                    *reinterpret_cast<uint4*>(to + 4 * j) = make_uint4(raw[i].w[j], raw[i].w[j + 1], raw[i].w[j + 2], raw[i].w[j + 3]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4*>(to + 4 * j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+            }
+        }
+        if constexpr (ROWS) {
+            uint32_t scales;
+            const uint4 codes = quantise_unit<FMT>(v, ts, scales);
+            if (row < p.rows && col < p.cols)
+                *reinterpret_cast<uint4*>(p.r_codes + ((int64_t)batch * p.rows + row) * p.r_ld + col / 2) = codes;
+            uint8_t* s = row_scales + ((u * kPerUnit) >> 2) * kScaleTile + scale_at(lrow, u * kPerUnit);
+            if constexpr (kPerUnit == 2) *reinterpret_cast<uint16_t*>(s) = row < p.rows && col < p.cols ? (uint16_t)scales : 0;
+            else *s = row < p.rows && col < p.cols ? (uint8_t)scales : 0;
+        }
+    }
+    __syncthreads();
+    if constexpr (ROWS) {
+        const uint32_t ktile = col_tile * kTiles + (tid >> 5);
+        if (tid < kTiles * 32 && ktile < p.r_ktiles)
+            *reinterpret_cast<uint4*>(p.r_scales + (((int64_t)batch * p.row_tiles + row_tile) * p.r_ktiles + ktile) * kScaleTile + (tid & 31) * 16) =
+                *reinterpret_cast<const uint4*>(row_scales + tid * 16);
+    }
+    if constexpr (COLS) {
+        uint8_t* stage = dyn + 128 * kPitch;
+        auto put = [&](int lcol, int u, const float* v) {
+            uint32_t scales;
+            const uint4 codes = quantise_unit<FMT>(v, ts, scales);
+            *reinterpret_cast<uint4*>(stage + lcol * kStagePitch + u * 16) = codes;
+            const bool in = (int64_t)col_tile * 128 + lcol < p.cols && (int64_t)row_tile * 128 + u * kUnit < p.rows;
+            uint8_t* s = col_scales + ((u * kPerUnit) >> 2) * kScaleTile + scale_at(lcol, u * kPerUnit);
+            if constexpr (kPerUnit == 2) *reinterpret_cast<uint16_t*>(s) = in ? (uint16_t)scales : 0;
+            else *s = in ? (uint8_t)scales : 0;
+        };
+        if constexpr (kNarrow) {             // two neighbouring columns (one word) over 32 rows
+            const int pair = tid & 63, u = tid >> 6;
+            uint32_t w[kUnit];
+            float v[kUnit];
+#pragma unroll
+            for (int i = 0; i < kUnit; ++i) w[i] = *reinterpret_cast<const uint32_t*>(dyn + (u * kUnit + i) * kPitch + pair * 4);
+#pragma unroll
+            for (int i = 0; i < kUnit; ++i) v[i] = bf16_low(w[i]);
+            put(2 * pair, u, v);
+#pragma unroll
+            for (int i = 0; i < kUnit; ++i) v[i] = bf16_high(w[i]);
+            put(2 * pair + 1, u, v);
+        } else {
+#pragma unroll 1
+            for (int half = 0; half < 2; ++half) {
+                const int lcol = tid & 127, u = (tid >> 7) + 2 * half;
+                float v[kUnit];
+#pragma unroll
+                for (int i = 0; i < kUnit; ++i) v[i] = *reinterpret_cast<const float*>(dyn + (u * kUnit + i) * kPitch + lcol * 4);
+                put(lcol, u, v);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int at = tid + i * kQThreads, lcol = at >> 2, u = at & 3;
+            const int64_t col = (int64_t)col_tile * 128 + lcol, row = (int64_t)row_tile * 128 + u * kUnit;
+            if (col < p.cols && row < p.rows)
+                *reinterpret_cast<uint4*>(p.c_codes + ((int64_t)batch * p.cols + col) * p.c_ld + row / 2) =
+                    *reinterpret_cast<const uint4*>(stage + lcol * kStagePitch + u * 16);
+        }
+        const uint32_t ktile = row_tile * kTiles + (tid >> 5);
+        if (tid < kTiles * 32 && ktile < p.c_ktiles)
+            *reinterpret_cast<uint4*>(p.c_scales + (((int64_t)batch * p.c_row_tiles + col_tile) * p.c_ktiles + ktile) * kScaleTile + (tid & 31) * 16) =
+                *reinterpret_cast<const uint4*>(col_scales + tid * 16);
+    }
+}
+
+struct DequantParams {
+    const uint8_t *codes, *scales;
+    const float* t;
+    int64_t rows, cols, ld, ldo;
+    uint32_t row_tiles, col_tiles, ktiles;
+    int32_t access;
+    void* out;
+};
+
+// The inverse: 0.5 + 1/16 (1/32) bytes in, 2 (4) out per element.  The tile's scales come in whole scale tiles; a thread
+// turns 16 bytes of codes into 32 values.
+template <typename T, int FMT> __global__ void __launch_bounds__(kQThreads) fp4_dequant_kernel(const __grid_constant__ DequantParams p)
+{
+    constexpr int kTiles = FMT == MOR_FP4_E4M3_16 ? 2 : 1;
+    constexpr int kPerUnit = Fp4<FMT>::kBlocksPerUnit;
+    __shared__ __align__(16) uint8_t scales[kTiles * kScaleTile];
+    const int tid = threadIdx.x;
+    const uint32_t per = p.row_tiles * p.col_tiles;
+    const uint32_t batch = blockIdx.x / per, in_batch = blockIdx.x % per;
+    const uint32_t row_tile = in_batch / p.col_tiles, col_tile = in_batch % p.col_tiles;
+    uint4 codes[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int at = tid + i * kQThreads;
+        const int64_t row = (int64_t)row_tile * 128 + (at >> 2), col = (int64_t)col_tile * 128 + (at & 3) * kUnit;
+        if (row < p.rows && col < p.cols) codes[i] = *reinterpret_cast<const uint4*>(p.codes + ((int64_t)batch * p.rows + row) * p.ld + col / 2);
+    }
+    const uint32_t ktile = col_tile * kTiles + (tid >> 5);
+    if (tid < kTiles * 32 && ktile < p.ktiles)
+        *reinterpret_cast<uint4*>(scales + tid * 16) =
+            *reinterpret_cast<const uint4*>(p.scales + (((int64_t)batch * p.row_tiles + row_tile) * p.ktiles + ktile) * kScaleTile + (tid & 31) * 16);
+    const float t = *p.t;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int at = tid + i * kQThreads, lrow = at >> 2, u = at & 3;
+        const int64_t row = (int64_t)row_tile * 128 + lrow, col = (int64_t)col_tile * 128 + u * kUnit;
+        if (row >= p.rows || col >= p.cols) continue;
+        const uint8_t* s = scales + ((u * kPerUnit) >> 2) * kScaleTile + scale_at(lrow, u * kPerUnit);
+        const float s0 = scale_value<FMT>(s[0]), s1 = kPerUnit == 2 ? scale_value<FMT>(s[kPerUnit - 1]) : s0;
+        const uint32_t c[4] = {codes[i].x, codes[i].y, codes[i].z, codes[i].w};
+        float v[kUnit];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const float2 d = e2m1x2_value((c[j >> 2] >> (8 * (j & 3))) & 0xFFu);
+            const float sc = j < 8 ? s0 : s1;
+            v[2 * j] = (d.x * sc) * t;
+            v[2 * j + 1] = (d.y * sc) * t;
+        }
+        T* to = static_cast<T*>(p.out) + ((int64_t)batch * p.rows + row) * p.ldo + col;
+        const int n = (int)min((int64_t)kUnit, p.cols - col);
+        constexpr int kWords = kUnit * sizeof(T) / 4;
+        uint32_t w[kWords];
+#pragma unroll
+        for (int j = 0; j < kWords; ++j) {
+            if constexpr (sizeof(T) == 2) w[j] = bf16x2_of(v[2 * j], v[2 * j + 1]);
+            else w[j] = __float_as_uint(v[j]);
+        }
+        if (n == kUnit && p.access == 32) {
+#pragma unroll
+            for (int j = 0; j < kWords; j += 8) stg256(reinterpret_cast<uint32_t*>(to) + j, w + j);
+        } else if (n == kUnit && p.access == 16) {
+#pragma unroll
+            for (int j = 0; j < kWords; j += 4) *reinterpret_cast<uint4*>(reinterpret_cast<uint32_t*>(to) + j) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kUnit; ++j) {
+                if (j >= n) break;
+                if constexpr (sizeof(T) == 2) reinterpret_cast<uint16_t*>(to)[j] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
+                else reinterpret_cast<uint32_t*>(to)[j] = w[j];
+            }
+        }
+    }
+}
+
+template <typename T, int FMT, bool ROWS, bool COLS, int MODE> cudaError_t quant_launch(const QuantParams& p, uint32_t grid, cudaStream_t st)
+{
+    constexpr bool kNarrow = sizeof(T) == 2 && MODE != WEIGHTED;
+    constexpr int smem = COLS ? 128 * Tile<kNarrow>::kPitch + 128 * kStagePitch : 0;
+    static std::atomic<uint64_t> done{0};
+    if (smem > 0 && !allow_smem(fp4_quant_kernel<T, FMT, ROWS, COLS, MODE>, smem, done)) return cudaErrorInvalidValue;
+    return launch(fp4_quant_kernel<T, FMT, ROWS, COLS, MODE>, grid, kQThreads, smem, st, p.partial != nullptr, p);
+}
+template <typename T, int FMT, int MODE> cudaError_t quant_dirs(const QuantParams& p, uint32_t grid, cudaStream_t st)
+{
+    if (p.r_codes != nullptr && p.c_codes != nullptr) return quant_launch<T, FMT, true, true, MODE>(p, grid, st);
+    if (p.r_codes != nullptr) return quant_launch<T, FMT, true, false, MODE>(p, grid, st);
+    return quant_launch<T, FMT, false, true, MODE>(p, grid, st);
+}
+template <typename T, int MODE> cudaError_t quant_all(const QuantParams& p, int format, uint32_t amax_grid, uint32_t grid, float* part, cudaStream_t st)
+{
+    if (amax_grid > 0) {
+        const cudaError_t e = launch(fp4_amax_kernel<T, MODE>, amax_grid, kQThreads, 0, st, false, p, part);
+        if (e != cudaSuccess) return e;
+    }
+    return format == MOR_FP4_E4M3_16 ? quant_dirs<T, MOR_FP4_E4M3_16, MODE>(p, grid, st) : quant_dirs<T, MOR_FP4_E8M0_32, MODE>(p, grid, st);
+}
+template <typename T> cudaError_t quant_mode(const QuantParams& p, int format, uint32_t amax_grid, uint32_t grid, float* part, cudaStream_t st)
+{
+    if (p.slot_of_row == nullptr) return quant_all<T, PLAIN>(p, format, amax_grid, grid, part, st);
+    if (p.weight == nullptr) return quant_all<T, GATHER>(p, format, amax_grid, grid, part, st);
+    return quant_all<T, WEIGHTED>(p, format, amax_grid, grid, part, st);
+}
+
+}  // namespace
+}  // namespace mor
+
+using namespace mor;
+
+extern "C" {
+
+size_t mor_fp4_scale_bytes(int64_t batch, int64_t rows, int64_t cols, int format)
+{
+    if (!shape_ok(batch, rows, cols) || (format != MOR_FP4_E4M3_16 && format != MOR_FP4_E8M0_32)) return 0;
+    return (size_t)batch * ceil_div(rows, 128) * scale_ktiles(cols, format) * kScaleTile;
+}
+
+mor_status_t mor_fp4_quantize(const mor_fp4_quantize_desc_t* host_desc, const mor_fp4_matrix_t* host_rows,
+                              const mor_fp4_matrix_t* host_cols, void* workspace, size_t workspace_bytes, void* cuda_stream)
+{
+    if (host_desc == nullptr || (host_rows == nullptr && host_cols == nullptr)) return MOR_ERR_INVALID_ARG;
+    const mor_fp4_quantize_desc_t& d = *host_desc;
+    const bool gather = d.slot_of_row != nullptr;
+    if (!is_dtype(d.dtype) || (d.format != MOR_FP4_E4M3_16 && d.format != MOR_FP4_E8M0_32)) return MOR_ERR_INVALID_ARG;
+    if (!shape_ok(d.batch, d.rows, d.cols) || d.ld < d.cols || d.batch_stride < 0) return MOR_ERR_INVALID_ARG;
+    if (gather && (d.batch != 1 || d.top < 1 || d.row_of_slot == nullptr || !shape_ok(1, d.out_rows, d.cols))) return MOR_ERR_INVALID_ARG;
+    if (gather && d.weight != nullptr && !is_dtype(d.weight_dtype)) return MOR_ERR_INVALID_ARG;
+    if (!gather && d.weight != nullptr) return MOR_ERR_INVALID_ARG;
+    const int64_t rows = gather ? d.out_rows : d.rows;
+    const bool empty = d.batch == 0 || rows == 0 || d.cols == 0;
+    if (!empty && d.x == nullptr && d.rows > 0) return MOR_ERR_INVALID_ARG;
+    const int es = (int)dtype_bytes(d.dtype);
+    if (!is_aligned(d.x, es)) return MOR_ERR_ALIGNMENT;
+    if (host_rows != nullptr) {
+        const mor_status_t s = check_matrix(*host_rows);
+        if (s != MOR_OK) return s;
+        if (host_rows->batch != d.batch || host_rows->rows != rows || host_rows->cols != d.cols || host_rows->format != d.format) return MOR_ERR_INVALID_ARG;
+    }
+    if (host_cols != nullptr) {
+        const mor_status_t s = check_matrix(*host_cols);
+        if (s != MOR_OK) return s;
+        if (host_cols->batch != d.batch || host_cols->rows != d.cols || host_cols->cols != rows || host_cols->format != d.format) return MOR_ERR_INVALID_ARG;
+    }
+    const int64_t elems = d.batch * d.rows * d.cols;
+    const bool want_amax = d.format == MOR_FP4_E4M3_16 && d.amax == nullptr;
+    const bool amax_kernel = want_amax && (gather || elems > kSelfAmaxElems);
+    if (want_amax) {
+        if (workspace == nullptr || workspace_bytes < MOR_FP4_WORKSPACE_BYTES) return MOR_ERR_WORKSPACE;
+        if (!is_aligned(workspace, 16)) return MOR_ERR_ALIGNMENT;
+    }
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (empty) return MOR_OK;
+
+    QuantParams p = {};
+    p.x = d.x;
+    p.ld = d.ld;
+    p.batch_stride = d.batch_stride;
+    p.rows = rows;
+    p.cols = d.cols;
+    p.x_rows = d.rows;
+    p.batch = d.batch;
+    p.row_tiles = (uint32_t)ceil_div(rows, 128);
+    p.col_tiles = (uint32_t)ceil_div(d.cols, 128);
+    p.access = access_bytes(d.x, d.ld * es, d.batch > 1 ? d.batch_stride * es : 0, es);
+    p.amax = d.format == MOR_FP4_E4M3_16 ? d.amax : nullptr;
+    p.slot_of_row = d.slot_of_row;
+    p.row_of_slot = d.row_of_slot;
+    p.top = (uint32_t)(gather ? d.top : 1);
+    p.weight = d.weight;
+    p.weight_dtype = d.weight_dtype;
+    if (host_rows != nullptr) {
+        p.r_codes = host_rows->codes;
+        p.r_scales = host_rows->scales;
+        p.r_ld = host_rows->ld;
+        p.r_t = host_rows->tensor_scale;
+        p.r_ktiles = (uint32_t)scale_ktiles(d.cols, d.format);
+    }
+    if (host_cols != nullptr) {
+        p.c_codes = host_cols->codes;
+        p.c_scales = host_cols->scales;
+        p.c_ld = host_cols->ld;
+        p.c_t = host_cols->tensor_scale;
+        p.c_ktiles = (uint32_t)scale_ktiles(rows, d.format);
+        p.c_row_tiles = p.col_tiles;
+    }
+    uint32_t amax_grid = 0;
+    if (amax_kernel) {
+        const int64_t units = d.batch * d.rows * ceil_div(d.cols, kUnit);
+        const int64_t want = ceil_div(units, 2 * kQThreads);
+        amax_grid = (uint32_t)(want < 1 ? 1 : want > 148 * 4 ? 148 * 4 : want);
+        static_assert(148 * 4 <= kAmaxMaxBlocks, "parts fit the workspace");
+        p.partial = static_cast<const float*>(workspace);
+        p.n_partial = amax_grid;
+    }
+    const uint32_t grid = (uint32_t)(d.batch * p.row_tiles * p.col_tiles);
+    const cudaError_t e = d.dtype == MOR_DTYPE_BF16 ? quant_mode<__nv_bfloat16>(p, d.format, amax_grid, grid, static_cast<float*>(workspace), st)
+                                                    : quant_mode<float>(p, d.format, amax_grid, grid, static_cast<float*>(workspace), st);
+    return e == cudaSuccess ? MOR_OK : MOR_ERR_CUDA;
+}
+
+mor_status_t mor_fp4_dequantize(const mor_fp4_matrix_t* host_in, void* out, int dtype, int64_t ld_out, void* cuda_stream)
+{
+    if (host_in == nullptr || !is_dtype(dtype)) return MOR_ERR_INVALID_ARG;
+    const mor_fp4_matrix_t& m = *host_in;
+    const mor_status_t s = check_matrix(m);
+    if (s != MOR_OK) return s;
+    if (ld_out < m.cols) return MOR_ERR_INVALID_ARG;
+    const int es = (int)dtype_bytes(dtype);
+    if (!is_aligned(out, es)) return MOR_ERR_ALIGNMENT;
+    if (m.batch == 0 || m.rows == 0 || m.cols == 0) return MOR_OK;
+    if (out == nullptr) return MOR_ERR_INVALID_ARG;
+    DequantParams p = {};
+    p.codes = m.codes;
+    p.scales = m.scales;
+    p.t = m.tensor_scale;
+    p.rows = m.rows;
+    p.cols = m.cols;
+    p.ld = m.ld;
+    p.ldo = ld_out;
+    p.row_tiles = (uint32_t)ceil_div(m.rows, 128);
+    p.col_tiles = (uint32_t)ceil_div(m.cols, 128);
+    p.ktiles = (uint32_t)scale_ktiles(m.cols, m.format);
+    p.access = access_bytes(out, ld_out * es, 0, es);
+    p.out = out;
+    const uint32_t grid = (uint32_t)(m.batch * p.row_tiles * p.col_tiles);
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const bool nv = m.format == MOR_FP4_E4M3_16;
+    cudaError_t e;
+    if (dtype == MOR_DTYPE_BF16)
+        e = nv ? launch(fp4_dequant_kernel<__nv_bfloat16, MOR_FP4_E4M3_16>, grid, kQThreads, 0, st, false, p)
+               : launch(fp4_dequant_kernel<__nv_bfloat16, MOR_FP4_E8M0_32>, grid, kQThreads, 0, st, false, p);
+    else
+        e = nv ? launch(fp4_dequant_kernel<float, MOR_FP4_E4M3_16>, grid, kQThreads, 0, st, false, p)
+               : launch(fp4_dequant_kernel<float, MOR_FP4_E8M0_32>, grid, kQThreads, 0, st, false, p);
+    return e == cudaSuccess ? MOR_OK : MOR_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -8,6 +8,23 @@
 #include "mor_internal.h"
 
 namespace mor {
+
+EncodeTiledFn encode_tiled_fn()
+{
+    static std::atomic<EncodeTiledFn> cached{nullptr};   // host threads may race here: every one stores the same address
+    EncodeTiledFn fn = cached.load(std::memory_order_acquire);
+    if (fn == nullptr) {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess) {
+            fn = reinterpret_cast<EncodeTiledFn>(p);
+            cached.store(fn, std::memory_order_release);
+        }
+    }
+    return fn;
+}
+
 namespace {
 
 constexpr size_t kAlign = 256;
@@ -131,28 +148,7 @@ mor_status_t check_out(const mor_tensor_desc_t& d, const Shape& s, const mor_out
     return MOR_OK;
 }
 
-// ---- TMA descriptors (cuTensorMapEncodeTiled, reached through the runtime so that the library
-// does not link against the driver library)
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_tiled_fn()
-{
-    static std::atomic<EncodeTiledFn> cached{nullptr};   // host threads may race here: every one stores the same address
-    EncodeTiledFn fn = cached.load(std::memory_order_acquire);
-    if (fn == nullptr) {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess) {
-            fn = reinterpret_cast<EncodeTiledFn>(p);
-            cached.store(fn, std::memory_order_release);
-        }
-    }
-    return fn;
-}
+// ---- TMA descriptors
 
 // One descriptor for the BF16 input [rows, cols] with row pitch ld (box 128 x 128 elements; elements
 // past the edge read as zero) and one for the codes [rows, cols] bytes with row pitch codes_ld (box
@@ -453,6 +449,13 @@ mor_status_t make_item(const mor_tensor_desc_t* d, const mor_outputs_t& o, bool 
 }
 
 }  // namespace
+
+void test_hook_main(uint32_t& tile, long long& wait_cycles)
+{
+    tile = g_test_skip_tile.load(std::memory_order_relaxed);
+    wait_cycles = g_test_wait_cycles.load(std::memory_order_relaxed);
+}
+
 }  // namespace mor
 
 using namespace mor;
@@ -717,6 +720,6 @@ const char* mor_status_string(mor_status_t status)
     return "unknown status";
 }
 
-int mor_version(void) { return 100; }
+int mor_version(void) { return 110; }
 
 }  // extern "C"

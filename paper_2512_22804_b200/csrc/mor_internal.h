@@ -18,6 +18,15 @@ extern "C" MOR_API void mor_test_skip_prepass_tile_load(uint32_t tile, long long
 
 namespace mor {
 
+// cuTensorMapEncodeTiled, reached through the runtime so that the library does not link against the driver library (NULL if
+// the driver lacks it).
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_tiled_fn();
+// What mor_test_skip_tile_load() has set.
+void test_hook_main(uint32_t& tile, long long& wait_cycles);
+
 // The main kernel works on tiles of 128 rows x 128 columns (32 KiB of BF16), whatever the
 // partition: a tile is one 128x128 block, or four 64x64 blocks, or 128 one-row blocks of 128
 // elements, or a piece of the single block of the per-tensor partition.  Tiles are numbered row-major over the tile

@@ -1,0 +1,224 @@
+"""Sorting by expert, the row movers and the 4-bit expert layer against plain statements of them.
+
+Sorting and plain copies are compared exactly.  A weighted sum of `top` rows is taken in binary32 in slot order: |error| <= top *
+2^-24 * sum |w y|; a dot product over `hidden` values is summed in binary32 in some order: |error| <= hidden * 2^-24 * sum |dy y|.
+Each is then rounded once to the result's type, so the result lies between the rounded ends of that interval.
+"""
+import numpy as np
+import pytest
+
+from tests import plain_fp4 as plain
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def experts():
+    from paper_2512_22804_b200 import experts
+
+    return experts
+
+
+def cuda(x, dtype=None):
+    import torch
+
+    t = torch.from_numpy(np.ascontiguousarray(x)).cuda()
+    return t if dtype is None else t.to(dtype)
+
+
+def draw_ids(tokens, top, n, seed, masked=0.1):
+    rng = np.random.default_rng(seed)
+    p = rng.random(n) ** 3 + 1e-3
+    ids = rng.choice(n, (tokens, top), p=p / p.sum()).astype(np.int32)
+    ids[rng.random((tokens, top)) < masked] = -1
+    return ids
+
+
+CASES = [(1, 1, 1), (1, 8, 128), (3, 2, 5), (100, 4, 64), (4096, 1, 7), (1025, 4, 1024), (2048, 2, 33), (5000, 3, 16), (40000, 4, 64), (30000, 8, 1024)]
+
+
+@pytest.mark.parametrize("align", [1, 128])
+@pytest.mark.parametrize("tokens,top,n", CASES)
+def test_sort(experts, tokens, top, n, align):
+    ids = draw_ids(tokens, top, n, tokens + n)
+    plan = experts.sort(cuda(ids), n, align)
+    starts, row, slot = plain.sort(ids, n, align)
+    assert np.array_equal(plan.starts.cpu().numpy(), starts)
+    assert np.array_equal(plan.row.cpu().numpy(), row)
+    assert np.array_equal(plan.slot.cpu().numpy(), slot)
+
+
+@pytest.mark.parametrize("fill", [-1, 5, -2**31, 2**31 - 1, 0, 4])
+def test_sort_of_ids_that_name_no_expert_and_of_one_expert(experts, fill):
+    for tokens in (7, 3000):
+        ids = np.full((tokens, 2), fill, np.int32)
+        plan = experts.sort(cuda(ids), 5, 128)
+        starts, row, slot = plain.sort(ids, 5, 128)
+        for got, want in ((plan.starts, starts), (plan.row, row), (plan.slot, slot)):
+            assert np.array_equal(got.cpu().numpy(), want)
+
+
+def test_sort_of_nothing(experts):
+    import torch
+
+    plan = experts.sort(torch.zeros(0, 4, dtype=torch.int32, device="cuda"), 6, 128)
+    assert plan.starts.tolist() == [0] * 7 and plan.slot.numel() == 0
+    x = torch.zeros(0, 64, device="cuda", dtype=torch.bfloat16)
+    assert experts.gather(x, plan).shape == (0, 64) and experts.combine(x, plan).shape == (0, 64)
+
+
+def matrices(experts, tokens, top, n, hidden, align, dtype, seed):
+    import torch
+
+    rng = np.random.default_rng(seed)
+    ids = draw_ids(tokens, top, n, seed)
+    plan = experts.sort(cuda(ids), n, align)
+    _, row, slot = plain.sort(ids, n, align)
+    d = torch.bfloat16 if dtype == "bf16" else torch.float32
+
+    def matrix(r):
+        x = rng.standard_normal((r, hidden)).astype(np.float32)
+        x = plain.bf16(x) if dtype == "bf16" else x
+        return x, cuda(x, d)
+
+    return plan, row, slot, matrix
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("weights", [None, "bf16", "fp32"])
+@pytest.mark.parametrize("tokens,top,n,hidden,align", [(1, 8, 16, 4096, 1), (37, 2, 5, 1, 1), (100, 3, 9, 33, 128), (300, 5, 64, 520, 1), (64, 9, 4, 24, 128),
+                                                       (130, 1, 3, 2056, 128)])
+def test_gather_combine_and_gradient(experts, tokens, top, n, hidden, align, weights, dtype):
+    import torch
+
+    plan, row, slot, matrix = matrices(experts, tokens, top, n, hidden, align, dtype, tokens + top)
+    w = np.random.default_rng(1).random((tokens, top)).astype(np.float32)
+    w = plain.bf16(w) if weights == "bf16" else w
+    tw = None if weights is None else cuda(w, torch.bfloat16 if weights == "bf16" else torch.float32)
+    one = w if weights is not None else np.ones_like(w)
+    x, tx = matrix(tokens)
+    ys, tys = matrix(len(slot))
+    dy, tdy = matrix(tokens)
+    def rnd(v, to=dtype):
+        return plain.bf16(v.astype(np.float32)) if to == "bf16" else v.astype(np.float32)
+
+    def within(got, want, room, to):
+        got = got.float().cpu().numpy()
+        return (rnd(want - room, to) <= got).all() and (got <= rnd(want + room, to)).all()
+
+    def spread(v):
+        out = np.zeros((len(slot), hidden), np.float32)
+        at = slot >= 0
+        out[at] = rnd(v[slot[at] // top] * one.reshape(-1)[slot[at]][:, None])
+        return out
+
+    assert np.array_equal(experts.gather(tx, plan, tw).float().cpu().numpy(), spread(x))
+    taken = np.where((row >= 0)[..., None], ys.astype(np.float64)[np.maximum(row, 0)], 0.0)
+    want = (taken * one[..., None]).sum(1)
+    assert within(experts.combine(tys, plan, tw), want, top * 2.0 ** -24 * (np.abs(taken) * one[..., None]).sum(1), dtype)
+    if weights is None:
+        return
+    dys, dw = experts.combine_grad(tdy, tys, plan, tw)
+    assert np.array_equal(dys.float().cpu().numpy(), spread(dy))
+    terms = taken * dy.astype(np.float64)[:, None, :]
+    want = terms.sum(-1)
+    assert within(dw, want, hidden * 2.0 ** -24 * np.abs(terms).sum(-1), weights)
+    none, again = experts.combine_grad(tdy, tys, plan, tw, rows=False)
+    assert none is None and torch.equal(again, dw)
+
+
+def test_nan_of_an_empty_row_goes_nowhere_and_strides(experts):
+    import torch
+
+    plan, row, slot, matrix = matrices(experts, 50, 2, 4, 96, 128, "bf16", 3)
+    ys, tys = matrix(len(slot))
+    tys[torch.from_numpy(slot < 0).cuda()] = float("nan")
+    y = experts.combine(tys, plan)
+    assert torch.isfinite(y).all()
+    masked = (row < 0).all(1)
+    assert not y[torch.from_numpy(masked).cuda()].any()
+    wide = torch.zeros(len(slot), 131, dtype=torch.bfloat16, device="cuda")   # odd pitch and start: one element at a time
+    wide[:, 1:97] = tys
+    assert torch.equal(experts.combine(wide[:, 1:97], plan), y)
+    x, tx = matrix(50)
+    wide = torch.zeros(50, 104, dtype=torch.bfloat16, device="cuda")          # 16-byte pitch
+    wide[:, 8:] = tx
+    assert torch.equal(experts.gather(wide[:, 8:], plan), experts.gather(tx, plan))
+
+
+@pytest.mark.parametrize("fmt", ["e4m3_16", "e8m0_32"])
+@pytest.mark.parametrize("weighted", [False, True])
+def test_quantised_gather_equals_gather_then_quantise(experts, fmt, weighted):
+    """The rows that quantisation gathers on the way, against the plain quantiser on the gathered 32-bit rows."""
+    import torch
+
+    from paper_2512_22804_b200 import fp4
+
+    for tokens, hidden in ((40, 96), (300, 333)):
+        plan, row, slot, matrix = matrices(experts, tokens, 3, 6, hidden, 128, "bf16", tokens)
+        x, tx = matrix(tokens)
+        w = np.random.default_rng(2).random((tokens, 3)).astype(np.float32)
+        rows = np.zeros((len(slot), hidden), np.float32)
+        at = slot >= 0
+        rows[at] = x[slot[at] // 3] * (w.reshape(-1)[slot[at]][:, None] if weighted else np.float32(1))
+        r, c = fp4.quantize(tx, fmt, cols=True, gather=plan, weight=cuda(w) if weighted else None)
+        for op, v in ((r, rows), (c, np.ascontiguousarray(rows.T))):
+            codes, byte, t = plain.quantize(v, fmt)
+            assert np.array_equal(op.codes.cpu().numpy().reshape(v.shape[0], -1), plain.packed(codes))
+            assert np.array_equal(op.scales.cpu().numpy().reshape(-1), plain.tiled(byte))
+            assert op.tensor_scale.item() == t
+
+
+@pytest.mark.parametrize("fmt", ["e4m3_16", "e8m0_32"])
+@pytest.mark.parametrize("tokens,top,n,k,m", [(1, 2, 8, 64, 40), (50, 3, 6, 300, 136), (400, 2, 4, 257, 264)])
+def test_expert_layer_and_its_gradient(experts, fmt, tokens, top, n, k, m):
+    """Against the formula on quantised values, in 64 bits.  The rows of the product are rounded to BF16 (at most 2^-8)
+    before they are combined, the result once more: 2^-7 of the sum of magnitudes covers both (the sums' own 2^-16 beside what the
+    products of both roundings leave)."""
+    import torch
+
+    from paper_2512_22804_b200 import fp4
+
+    rng = np.random.default_rng(tokens)
+    ids = draw_ids(tokens, top, n, tokens + 1)
+    _, row, slot = plain.sort(ids, n, 128)
+    starts = plain.sort(ids, n, 128)[0]
+    x, w = plain.bf16(rng.standard_normal((tokens, k)).astype(np.float32)), plain.bf16(rng.standard_normal((n, m, k)).astype(np.float32) * np.float32(0.1))
+    g = plain.bf16(rng.standard_normal((tokens, m)).astype(np.float32))
+    wt = plain.bf16(rng.random((tokens, top)).astype(np.float32))
+    tx, tw, twt = (cuda(v, torch.bfloat16).requires_grad_() for v in (x, w, wt))
+    y = experts.linear(tx, tw, cuda(ids), twt, fmt)
+    dx, dw, dwt = torch.autograd.grad(y, (tx, tw, twt), cuda(g, torch.bfloat16))
+    fp4.check()
+
+    def v(z):
+        return plain.values(*plain.quantize(z, fmt), fmt)
+
+    def near(got, want, size):
+        assert (np.abs(got.detach().double().cpu().numpy() - want) <= 2.0 ** -7 * size + 1e-30).all()
+
+    at = slot >= 0
+    rows, grows = np.zeros((len(slot), k), np.float32), np.zeros((len(slot), m), np.float32)
+    rows[at] = x[slot[at] // top]
+    grows[at] = g[slot[at] // top] * wt.reshape(-1)[slot[at]][:, None]
+    qw = v(w.reshape(n * m, k)).reshape(n, m, k)
+    # blocks of the transposes run inside one expert's matrix; the tensor maximum is that of the whole stack
+    amax = np.abs(w).max()
+    qwt = np.stack([plain.values(*plain.quantize(np.ascontiguousarray(w[e].T), fmt, amax), fmt) for e in range(n)])
+    qx, qg, qxt, qgt = v(rows), v(grows), v(np.ascontiguousarray(rows.T)), v(np.ascontiguousarray(grows.T))
+    ys, sy = np.zeros((len(slot), m)), np.zeros((len(slot), m))
+    dxs, sx = np.zeros((len(slot), k)), np.zeros((len(slot), k))
+    for e in range(n):
+        p = slice(starts[e], starts[e + 1])
+        ys[p], sy[p] = qx[p] @ qw[e].T, np.abs(qx[p]) @ np.abs(qw[e]).T
+        dxs[p], sx[p] = qg[p] @ qwt[e].T, np.abs(qg[p]) @ np.abs(qwt[e]).T
+        near(dw[e], qgt[:, p] @ qxt[:, p].T, np.abs(qgt[:, p]) @ np.abs(qxt[:, p]).T)
+
+    def taken(z):
+        return np.where((row >= 0)[..., None], z[np.maximum(row, 0)], 0.0)
+
+    near(y, (taken(ys) * wt[..., None]).sum(1), (taken(sy) * wt[..., None]).sum(1))
+    near(dx, taken(dxs).sum(1), taken(sx).sum(1))
+    near(dwt, (taken(ys) * g[:, None, :]).sum(-1), (taken(sy) * np.abs(g)[:, None, :]).sum(-1))
+    stored, _ = fp4.quantize(tw.detach(), fmt)                       # serving: the weight quantised once
+    assert torch.equal(experts.linear(tx.detach(), stored, cuda(ids), twt.detach()), y)
