@@ -48,6 +48,14 @@ __device__ __noinline__ void drain()
     while (clock64() - t0 < 400000) {}
 }
 
+// A whole warp's bounded wait; false (and everything is told to stop) when it ran out for any lane.
+template <typename Ctl> __device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, Ctl& C, const GemmParams& p)
+{
+    const bool ok = __all_sync(kFull, mbar_wait(bar, parity, &C.abort, p.wait_cycles));
+    if (!ok) give_up(&C.abort, p.status);
+    return ok;
+}
+
 template <int CG, int NT, int FMT> struct Wide {
     static constexpr bool kNv = FMT == MOR_FP4_E4M3_16;
     static constexpr int kSf = kNv ? 4 : 2;                          // scale tiles per stage and 128 rows
@@ -149,7 +157,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) fp4_wide_kernel(const __grid_
     __shared__ int32_t starts_s[GROUP == MOR_GROUP_NONE ? 1 : MOR_MAX_GROUPS + 1];
     uint8_t* smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
     WideCtrl& C = *reinterpret_cast<WideCtrl*>(smem + W::kStages * W::kStage);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = warp_number(), lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0;
 
     if (threadIdx.x == 0) {
@@ -180,76 +188,77 @@ __global__ void __launch_bounds__(kWideThreads, 1) fp4_wide_kernel(const __grid_
     const int first = blockIdx.x / CG, step = gridDim.x / CG;
     TileAt at;
 
-    if (warp == 0 && lane == 0) {                                   // ---- copies
-        uint32_t it = 0;
+    if (warp == 0) {                                                // ---- copies
+        uint32_t slot = 0, lap = 0;
         bool ok = true;
         for (int t = first; ok && tile_at<GROUP>(p, starts_s, t, at); t += step) {
             const int stages = (at.len + kStageElems - 1) / kStageElems;
             const int row_a = at.m * 128 * CG + (int)rank * 128, row_b = at.n * NT + (int)rank * (NT / CG);
             const int za = 0, zb = GROUP == MOR_GROUP_ROWS ? at.group : 0;
-            for (int s = 0; s < stages; ++s, ++it) {
-                const uint32_t slot = it % W::kStages;
-                if (it >= W::kStages && !mbar_wait(&C.empty[slot], (it / W::kStages - 1u) & 1u, &C.abort, p.wait_cycles)) {
-                    give_up(&C.abort, p.status);
+            const int sa = (za * p.a_row_tiles + row_a / 128) * p.a_ktiles, sb = (zb * p.b_row_tiles + at.n * (NT / 128)) * p.b_ktiles;
+            for (int s = 0; s < stages; ++s) {
+                if (lap > 0 && !wait_warp(&C.empty[slot], (lap - 1u) & 1u, C, p)) {
                     ok = false;
                     break;
                 }
-                const uint32_t base = smem_addr(smem) + slot * W::kStage;
-                uint32_t bar = smem_addr(&C.full[slot]);
-                if (rank == 0) mbar_arrive_expect_tx(&C.full[slot], CG * W::kStage);
-                if constexpr (CG == 2) bar = map_rank(bar, 0);
-                const int k = at.k0 + s * kStageElems, ktile = k / (W::kNv ? 64 : 128);
-                if (!(t == (int)p.skip_tile && s == 0)) load_tile_3d<CG>(base, &p.a, k / 2, row_a, za, bar);
-                load_tile_3d<CG>(base + W::kBytesA, &p.b, k / 2, row_b, zb, bar);
-                const uint32_t sf = base + W::kBytesA + W::kBytesB;
-                load_tile_2d<CG>(sf, &p.sa, 0, (za * p.a_row_tiles + row_a / 128) * p.a_ktiles + ktile, bar);
+                if (elect_one()) {
+                    const uint32_t base = smem_addr(smem) + slot * W::kStage;
+                    uint32_t bar = smem_addr(&C.full[slot]);
+                    if (rank == 0) mbar_arrive_expect_tx(&C.full[slot], CG * W::kStage);
+                    if constexpr (CG == 2) bar = map_rank(bar, 0);
+                    const int k = at.k0 + s * kStageElems, ktile = k / (W::kNv ? 64 : 128);
+                    if (!(t == (int)p.skip_tile && s == 0)) load_tile_3d<CG>(base, &p.a, k / 2, row_a, za, bar);
+                    load_tile_3d<CG>(base + W::kBytesA, &p.b, k / 2, row_b, zb, bar);
+                    const uint32_t sf = base + W::kBytesA + W::kBytesB;
+                    load_tile_2d<CG>(sf, &p.sa, 0, sa + ktile, bar);
 #pragma unroll
-                for (int g = 0; g < W::kGroupsB; ++g)
-                    load_tile_2d<CG>(sf + W::kBytesSa + g * W::kSf * kScaleTile, &p.sb, 0,
-                                     (zb * p.b_row_tiles + at.n * (NT / 128) + g) * p.b_ktiles + ktile, bar);
+                    for (int g = 0; g < W::kGroupsB; ++g)
+                        load_tile_2d<CG>(sf + W::kBytesSa + g * W::kSf * kScaleTile, &p.sb, 0, sb + g * p.b_ktiles + ktile, bar);
+                }
+                __syncwarp();
+                if (++slot == W::kStages) { slot = 0; ++lap; }
             }
         }
-    } else if (warp == 1 && lane == 0 && rank == 0) {               // ---- matrix instructions
-        uint32_t it = 0, done = 0;
+    } else if (warp == 1 && rank == 0) {                            // ---- matrix instructions
+        uint32_t slot = 0, lap = 0, done = 0;
         bool ok = true;
         for (int t = first; ok && tile_at<GROUP>(p, starts_s, t, at); t += step) {
             const int stages = (at.len + kStageElems - 1) / kStageElems;
             if (stages <= 0) continue;
-            if (done > 0 && !mbar_wait(&C.acc_empty, (done - 1u) & 1u, &C.abort, p.wait_cycles)) ok = false;
+            if (done > 0) ok = wait_warp(&C.acc_empty, (done - 1u) & 1u, C, p);
             tc_fence_after();
-            for (int s = 0; ok && s < stages; ++s, ++it) {
-                const uint32_t slot = it % W::kStages;
-                if (!mbar_wait(&C.full[slot], (it / W::kStages) & 1u, &C.abort, p.wait_cycles)) {
+            for (int s = 0; ok && s < stages; ++s) {
+                if (!wait_warp(&C.full[slot], lap & 1u, C, p)) {
                     ok = false;
                     break;
                 }
                 tc_fence_after();
-                const uint32_t base = smem_addr(smem) + slot * W::kStage, sf = base + W::kBytesA + W::kBytesB;
-                const uint32_t tsa = tmem + NT + slot * W::kSfCols, tsb = tsa + 4 * W::kSf;
                 const int steps = min(4, (at.len - s * kStageElems + 63) / 64);
+                if (elect_one()) {
+                    const uint32_t base = smem_addr(smem) + slot * W::kStage, sf = base + W::kBytesA + W::kBytesB;
+                    const uint32_t tsa = tmem + NT + slot * W::kSfCols, tsb = tsa + 4 * W::kSf;
+                    const uint64_t da = codes_desc(base), db = codes_desc(base + W::kBytesA), ds = scales_desc(sf);
 #pragma unroll
-                for (int j = 0; j < W::kSf; ++j) {
-                    copy_scales<CG>(tsa + 4 * j, scales_desc(sf + j * kScaleTile));
+                    for (int j = 0; j < W::kSf; ++j) {
+                        copy_scales<CG>(tsa + 4 * j, ds + j * (kScaleTile >> 4));
 #pragma unroll
-                    for (int g = 0; g < W::kGroupsB; ++g)
-                        copy_scales<CG>(tsb + (j * W::kGroupsB + g) * 4, scales_desc(sf + W::kBytesSa + (g * W::kSf + j) * kScaleTile));
+                        for (int g = 0; g < W::kGroupsB; ++g)
+                            copy_scales<CG>(tsb + (j * W::kGroupsB + g) * 4, ds + ((W::kBytesSa + (g * W::kSf + j) * kScaleTile) >> 4));
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (j >= steps) break;
+                        const int tile = W::kNv ? j : j >> 1, byte = W::kNv ? 0 : 2 * (j & 1);
+                        mma_fp4<CG, W::kNv>(tmem, da + 2 * j, db + 2 * j, fp4_idesc(128 * CG, NT, W::kNv, byte), tsa + 4 * tile,
+                                            tsb + 4 * W::kGroupsB * tile, s > 0 || j > 0);
+                    }
+                    tc_commit<CG>(smem_addr(&C.empty[slot]));
+                    if (s == stages - 1) tc_commit<CG>(smem_addr(&C.acc_full));
                 }
-                const uint64_t da = codes_desc(base), db = codes_desc(base + W::kBytesA);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (j >= steps) break;
-                    const int tile = W::kNv ? j : j >> 1, byte = W::kNv ? 0 : 2 * (j & 1);
-                    mma_fp4<CG, W::kNv>(tmem, da + 2 * j, db + 2 * j, fp4_idesc(128 * CG, NT, W::kNv, byte), tsa + 4 * tile,
-                                        tsb + 4 * W::kGroupsB * tile, s > 0 || j > 0);
-                }
-                tc_commit<CG>(smem_addr(&C.empty[slot]));
+                __syncwarp();
+                if (++slot == W::kStages) { slot = 0; ++lap; }
             }
-            if (ok) {
-                tc_commit<CG>(smem_addr(&C.acc_full));
-                ++done;
-            } else {
-                give_up(&C.abort, p.status);
-            }
+            ++done;
         }
     } else if (warp >= 4) {                                         // ---- accumulators out
         const int half = (warp - 4) >> 2;
@@ -262,12 +271,8 @@ __global__ void __launch_bounds__(kWideThreads, 1) fp4_wide_kernel(const __grid_
             const int64_t row = (int64_t)at.m * 128 * CG + rank * 128 + (warp & 3) * 32 + lane;
             const int64_t col = (int64_t)at.n * NT + half * kCols;
             if (at.len > 0) {
-                ok = mbar_wait(&C.acc_full, done & 1u, &C.abort, p.wait_cycles);
-                ok = __all_sync(kFull, ok);
-                if (!ok) {
-                    if (lane == 0) give_up(&C.abort, p.status);
-                    break;
-                }
+                ok = wait_warp(&C.acc_full, done & 1u, C, p);
+                if (!ok) break;
                 tc_fence_after();
 #pragma unroll
                 for (int j = 0; j < kCols; j += 32) tmem_load32(acc + j, tmem + lanes + half * kCols + j);
@@ -328,7 +333,7 @@ template <int NT, int FMT, typename T> __global__ void __launch_bounds__(kNarrow
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
     WideCtrl& C = *reinterpret_cast<WideCtrl*>(smem + W::kStages * W::kStage);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = warp_number(), lane = threadIdx.x & 31;
     uint32_t split;
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(split));
     const uint32_t rank = cluster_rank();
@@ -358,49 +363,49 @@ template <int NT, int FMT, typename T> __global__ void __launch_bounds__(kNarrow
     tc_fence_after();
     const uint32_t tmem = C.tmem;
 
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
+        uint32_t slot = 0, lap = 0;
         for (int s = begin; s < end; ++s) {
-            const uint32_t it = (uint32_t)(s - begin), slot = it % W::kStages;
-            if (it >= W::kStages && !mbar_wait(&C.empty[slot], (it / W::kStages - 1u) & 1u, &C.abort, p.wait_cycles)) {
-                give_up(&C.abort, p.status);
-                break;
+            if (lap > 0 && !wait_warp(&C.empty[slot], (lap - 1u) & 1u, C, p)) break;
+            if (elect_one()) {
+                const uint32_t base = smem_addr(smem) + slot * W::kStage, bar = smem_addr(&C.full[slot]);
+                mbar_arrive_expect_tx(&C.full[slot], W::kStage);
+                const int k = s * kStageElems, ktile = k / (W::kNv ? 64 : 128);
+                if (!(tile == (int)p.skip_tile && s == begin)) load_tile_3d<1>(base, &p.b, k / 2, feature0, 0, bar);
+                load_tile_3d<1>(base + W::kBytesA, &p.a, k / 2, token0, 0, bar);
+                load_tile_2d<1>(base + W::kBytesA + W::kBytesB, &p.sb, 0, feature0 / 128 * p.b_ktiles + ktile, bar);
+                load_tile_2d<1>(base + W::kBytesA + W::kBytesB + W::kBytesSf, &p.sa, 0, token0 / 128 * p.a_ktiles + ktile, bar);
             }
-            const uint32_t base = smem_addr(smem) + slot * W::kStage, bar = smem_addr(&C.full[slot]);
-            mbar_arrive_expect_tx(&C.full[slot], W::kStage);
-            const int k = s * kStageElems, ktile = k / (W::kNv ? 64 : 128);
-            if (!(tile == (int)p.skip_tile && s == begin)) load_tile_3d<1>(base, &p.b, k / 2, feature0, 0, bar);
-            load_tile_3d<1>(base + W::kBytesA, &p.a, k / 2, token0, 0, bar);
-            load_tile_2d<1>(base + W::kBytesA + W::kBytesB, &p.sb, 0, feature0 / 128 * p.b_ktiles + ktile, bar);
-            load_tile_2d<1>(base + W::kBytesA + W::kBytesB + W::kBytesSf, &p.sa, 0, token0 / 128 * p.a_ktiles + ktile, bar);
+            __syncwarp();
+            if (++slot == W::kStages) { slot = 0; ++lap; }
         }
-    } else if (warp == 1 && lane == 0) {
-        bool ok = true;
+    } else if (warp == 1) {
+        uint32_t slot = 0, lap = 0;
         for (int s = begin; s < end; ++s) {
-            const uint32_t it = (uint32_t)(s - begin), slot = it % W::kStages;
-            if (!mbar_wait(&C.full[slot], (it / W::kStages) & 1u, &C.abort, p.wait_cycles)) {
-                give_up(&C.abort, p.status);
-                ok = false;
-                break;
-            }
+            if (!wait_warp(&C.full[slot], lap & 1u, C, p)) break;
             tc_fence_after();
-            const uint32_t base = smem_addr(smem) + slot * W::kStage, sf = base + W::kBytesA + W::kBytesB;
-            const uint32_t tsa = tmem + W::kAcc + slot * W::kSfCols, tsb = tsa + 4 * W::kSf;
             const int steps = (int)min((int64_t)4, (p.k - (int64_t)s * kStageElems + 63) / 64);
+            if (elect_one()) {
+                const uint32_t base = smem_addr(smem) + slot * W::kStage, sf = base + W::kBytesA + W::kBytesB;
+                const uint32_t tsa = tmem + W::kAcc + slot * W::kSfCols, tsb = tsa + 4 * W::kSf;
+                const uint64_t da = codes_desc(base), db = codes_desc(base + W::kBytesA), ds = scales_desc(sf);
 #pragma unroll
-            for (int j = 0; j < W::kSf; ++j) {
-                copy_scales<1>(tsa + 4 * j, scales_desc(sf + j * kScaleTile));
-                copy_scales<1>(tsb + 4 * j, scales_desc(sf + W::kBytesSf + j * kScaleTile));
-            }
-            const uint64_t da = codes_desc(base), db = codes_desc(base + W::kBytesA);
+                for (int j = 0; j < W::kSf; ++j) {
+                    copy_scales<1>(tsa + 4 * j, ds + j * (kScaleTile >> 4));
+                    copy_scales<1>(tsb + 4 * j, ds + ((W::kBytesSf + j * kScaleTile) >> 4));
+                }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (j >= steps) break;
-                const int t = W::kNv ? j : j >> 1, byte = W::kNv ? 0 : 2 * (j & 1);
-                mma_fp4<1, W::kNv>(tmem, da + 2 * j, db + 2 * j, fp4_idesc(128, NT, W::kNv, byte), tsa + 4 * t, tsb + 4 * t, it > 0 || j > 0);
+                for (int j = 0; j < 4; ++j) {
+                    if (j >= steps) break;
+                    const int t = W::kNv ? j : j >> 1, byte = W::kNv ? 0 : 2 * (j & 1);
+                    mma_fp4<1, W::kNv>(tmem, da + 2 * j, db + 2 * j, fp4_idesc(128, NT, W::kNv, byte), tsa + 4 * t, tsb + 4 * t, s > begin || j > 0);
+                }
+                tc_commit<1>(smem_addr(&C.empty[slot]));
+                if (s == end - 1) tc_commit<1>(smem_addr(&C.acc_full));
             }
-            tc_commit<1>(smem_addr(&C.empty[slot]));
+            __syncwarp();
+            if (++slot == W::kStages) { slot = 0; ++lap; }
         }
-        if (ok) tc_commit<1>(smem_addr(&C.acc_full));
     }
     __syncwarp();
     const int part = warp & 3, feature = part * 32 + lane;            // a warp reads the 32 lanes of its number modulo 4
@@ -408,8 +413,7 @@ template <int NT, int FMT, typename T> __global__ void __launch_bounds__(kNarrow
     bool ok = true;
     if (warp >= 2) {
         if (begin < end) {
-            ok = __all_sync(kFull, mbar_wait(&C.acc_full, 0, &C.abort, p.wait_cycles));
-            if (!ok && lane == 0) give_up(&C.abort, p.status);
+            ok = wait_warp(&C.acc_full, 0, C, p);
             tc_fence_after();
         }
         if (ok) {

@@ -35,6 +35,17 @@ __device__ __forceinline__ float lds_cluster(uint32_t addr)
     return v;
 }
 
+// Warp number and choice of a thread in forms that the compiler knows to be the same for the whole warp: tensor-core and copy
+// instructions take their operands from uniform registers, and moving each one there from per-thread registers costs more than the
+// instruction.
+__device__ __forceinline__ int warp_number() { return __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0); }
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t p;
+    asm volatile("{ .reg .pred p; elect.sync _|p, 0xFFFFFFFF; selp.u32 %0, 1, 0, p; }" : "=r"(p));
+    return p != 0;
+}
+
 // Tile copies; `bar` is a shared-window address, with CG = 2 that of the pair's leading CTA.
 template <int CG> __device__ __forceinline__ void load_tile_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar)
 {
