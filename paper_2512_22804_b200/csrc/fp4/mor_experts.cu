@@ -165,59 +165,6 @@ struct MoveParams {
     void* dweight;
 };
 
-// What one thread moves at a time: BYTES bytes as 32-bit values.
-template <typename T, int BYTES> struct Piece {
-    static constexpr int kElems = BYTES / (int)sizeof(T);
-    static constexpr int kWords = BYTES < 4 ? 1 : BYTES / 4;
-    uint32_t w[kWords];
-    __device__ __forceinline__ void load(const T* p)
-    {
-        if constexpr (BYTES == 32) ldg256(w, p);
-        else if constexpr (BYTES == 16) {
-            const uint4 q = *reinterpret_cast<const uint4*>(p);
-            w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
-        } else if constexpr (BYTES == 4) w[0] = *reinterpret_cast<const uint32_t*>(p);
-        else w[0] = *reinterpret_cast<const uint16_t*>(p);
-    }
-    __device__ __forceinline__ void store(T* p) const
-    {
-        if constexpr (BYTES == 32) stg256(p, w);
-        else if constexpr (BYTES == 16) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-        else if constexpr (BYTES == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
-        else *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
-    }
-    __device__ __forceinline__ float get(int i) const
-    {
-        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
-        else return i & 1 ? bf16_high(w[i >> 1]) : bf16_low(w[i >> 1]);
-    }
-    __device__ __forceinline__ void set_all(const float* v)
-    {
-        if constexpr (sizeof(T) == 4) {
-#pragma unroll
-            for (int i = 0; i < kElems; ++i) w[i] = __float_as_uint(v[i]);
-        } else if constexpr (kElems == 1) w[0] = bf16x2_of(v[0], 0.f);
-        else {
-#pragma unroll
-            for (int i = 0; i < kElems; i += 2) w[i >> 1] = bf16x2_of(v[i], v[i + 1]);
-        }
-    }
-    __device__ __forceinline__ void clear()
-    {
-#pragma unroll
-        for (uint32_t& u : w) u = 0;
-    }
-    __device__ __forceinline__ Piece scaled(float s) const
-    {
-        float v[kElems];
-        Piece r;
-#pragma unroll
-        for (int i = 0; i < kElems; ++i) v[i] = get(i) * s;
-        r.set_all(v);
-        return r;
-    }
-};
-
 // Zeroes the rows without a slot among this CTA's 256.
 template <typename T, int BYTES> __device__ void clear_rows(const MoveParams& p, T* out, uint32_t block)
 {

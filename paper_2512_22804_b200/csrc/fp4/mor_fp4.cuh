@@ -29,11 +29,32 @@ __device__ __forceinline__ int scale_at(int row, int block) { return (row & 31) 
 struct TensorScale {
     float t;        // tensor scale
     float den;      // A * 2^-16 (block scales are fl(448 a / A); both sides carry 2^-16 so that 448 a cannot overflow)
+    float inv;      // fl(1 / den)
 };
 __device__ __forceinline__ TensorScale tensor_scale_of(float amax)
 {
     const float a = fmaxf(amax, 0x1p-88f);      // below 2^-88 the reciprocal of s * t could overflow
-    return {__fdiv_rn(a, 2688.0f), a * 0x1p-16f};
+    return {__fdiv_rn(a, 2688.0f), a * 0x1p-16f, __frcp_rn(a * 0x1p-16f)};
+}
+// fl(448 a / A): the product with the rounded reciprocal, corrected once by its exact remainder, is the correctly rounded
+// quotient (P. Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor", 1990).  What exceeds
+// 512 saturates anyway and is held there, so that no infinity meets a zero.
+__device__ __forceinline__ float block_quotient(float a, const TensorScale& ts)
+{
+    const float num = a * (448.0f / 65536.0f), q = fminf(num * ts.inv, 512.0f);
+    return fmaf(fmaf(-q, ts.den, num), ts.inv, q);
+}
+// fl(1 / fl(s t)) for the value s of each E4M3 code (zero for zero).
+__device__ __forceinline__ void fill_factors(float* factors, float t, int tid)
+{
+    if (tid < 127) {
+        uint32_t h;
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)tid));
+        const float s = __low2float(*reinterpret_cast<__half2*>(&h));
+        factors[tid] = tid == 0 ? 0.f : __frcp_rn(s * t);
+    } else if (tid == 127) {
+        factors[127] = 0.f;
+    }
 }
 
 // Largest magnitude; NaN if any element is NaN (then, and for infinities, the result is not below infinity).
@@ -50,55 +71,63 @@ template <int N> __device__ __forceinline__ float amax_of(const float* v)
     for (int i = 0; i < N; i += 2) { m0 = max_nan(m0, v[i]); m1 = max_nan(m1, v[i + 1]); }
     return max_nan(m0, m1);
 }
+// The same for pairs of BF16, each half by itself; the signs of the result mean nothing.
+__device__ __forceinline__ uint32_t max_nan_pairs(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+template <int N> __device__ __forceinline__ uint32_t amax_of_words(const uint32_t* w)
+{
+    if constexpr (N == 1) return w[0];
+    else return max_nan_pairs(amax_of_words<N / 2>(w), amax_of_words<N - N / 2>(w + N / 2));
+}
+__device__ __forceinline__ float amax_of_pair(uint32_t m)
+{
+    return max_nan(fabsf(__uint_as_float(m << 16)), __uint_as_float(m & 0xFFFF0000u));
+}
 
 // Eight E2M1 codes of v[0..7] * q, the first in the lowest four bits.
 __device__ __forceinline__ uint32_t e2m1x8(const float* v, float q)
 {
     uint32_t r;
     asm("{ .reg .b8 b0, b1, b2, b3;\n"
-        "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n"
-        "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n"
-        "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n"
-        "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n"
+        ".reg .b64 q, p0, p1, p2, p3;\n"
+        ".reg .f32 x0, x1, x2, x3, x4, x5, x6, x7;\n"
+        "mov.b64 q, {%9, %9};\n"
+        "mov.b64 p0, {%1, %2};\nmov.b64 p1, {%3, %4};\nmov.b64 p2, {%5, %6};\nmov.b64 p3, {%7, %8};\n"
+        "mul.rn.f32x2 p0, p0, q;\nmul.rn.f32x2 p1, p1, q;\nmul.rn.f32x2 p2, p2, q;\nmul.rn.f32x2 p3, p3, q;\n"
+        "mov.b64 {x0, x1}, p0;\nmov.b64 {x2, x3}, p1;\nmov.b64 {x4, x5}, p2;\nmov.b64 {x6, x7}, p3;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b0, x1, x0;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b1, x3, x2;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b2, x5, x4;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b3, x7, x6;\n"
         "mov.b32 %0, {b0, b1, b2, b3}; }"
         : "=r"(r)
-        : "f"(v[0] * q), "f"(v[1] * q), "f"(v[2] * q), "f"(v[3] * q), "f"(v[4] * q), "f"(v[5] * q), "f"(v[6] * q), "f"(v[7] * q));
+        : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(q));
     return r;
 }
 
-// Two E4M3 codes of (lo, hi) and the values they stand for.
-__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi, float& dlo, float& dhi)
-{
-    uint16_t c;
-    uint32_t h;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(hi), "f"(lo));
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(c));
-    const __half2 d = *reinterpret_cast<__half2*>(&h);
-    dlo = __low2float(d);
-    dhi = __high2float(d);
-    return c;
-}
-
-// Codes (16 bytes) and scale bytes (low byte first) of one unit.
-template <int FMT> __device__ __forceinline__ uint4 quantise_unit(const float* v, const TensorScale& ts, uint32_t& scales)
+// Codes (16 bytes) and scale bytes (low byte first) of one unit, given the largest magnitude of each of its blocks.
+template <int FMT> __device__ __forceinline__ uint4 quantise_unit(const float* v, const float* a, const TensorScale& ts, const float* factors, uint32_t& scales)
 {
     uint4 c;
     if constexpr (FMT == MOR_FP4_E8M0_32) {
-        const float a = amax_of<32>(v);
-        const bool bad = !(a < INFINITY);
+        const bool bad = !(a[0] < INFINITY);
         // floor(log2 a) - 2 with a bias of 127 is the exponent field less two; the fields 0 (subnormal or zero), 1 and 2 meet
         // the bound at 0
-        const int byte = max((int)(__float_as_uint(a) >> 23) - 2, 0);
+        const int byte = max((int)(__float_as_uint(a[0]) >> 23) - 2, 0);
         const float q = __uint_as_float((uint32_t)(254 - byte) << 23);
         scales = bad ? 0xFFu : (uint32_t)byte;
         c = make_uint4(e2m1x8(v, q), e2m1x8(v + 8, q), e2m1x8(v + 16, q), e2m1x8(v + 24, q));
         if (bad) c = make_uint4(0, 0, 0, 0);
     } else {
-        const float a0 = amax_of<16>(v), a1 = amax_of<16>(v + 16);
-        const bool bad0 = !(a0 < INFINITY), bad1 = !(a1 < INFINITY);
-        float s0, s1;
-        scales = e4m3x2(__fdiv_rn(a0 * (448.0f / 65536.0f), ts.den), __fdiv_rn(a1 * (448.0f / 65536.0f), ts.den), s0, s1);
-        const float q0 = s0 == 0.f ? 0.f : __frcp_rn(s0 * ts.t), q1 = s1 == 0.f ? 0.f : __frcp_rn(s1 * ts.t);
+        const bool bad0 = !(a[0] < INFINITY), bad1 = !(a[1] < INFINITY);
+        uint16_t s;
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(s) : "f"(block_quotient(a[1], ts)), "f"(block_quotient(a[0], ts)));
+        scales = s;
+        const float q0 = factors[s & 127], q1 = factors[(s >> 8) & 127];
         c = make_uint4(e2m1x8(v, q0), e2m1x8(v + 8, q0), e2m1x8(v + 16, q1), e2m1x8(v + 24, q1));
         if (bad0) { c.x = c.y = 0; scales = (scales & 0xFF00u) | 0x7Fu; }
         if (bad1) { c.z = c.w = 0; scales = (scales & 0x00FFu) | 0x7F00u; }
@@ -151,6 +180,59 @@ __device__ __forceinline__ float weight_at(const void* w, int dtype, int64_t i)
 {
     return dtype == MOR_DTYPE_BF16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(w)[i]) : static_cast<const float*>(w)[i];
 }
+
+// What one thread moves at a time: BYTES bytes as 32-bit values.
+template <typename T, int BYTES> struct Piece {
+    static constexpr int kElems = BYTES / (int)sizeof(T);
+    static constexpr int kWords = BYTES < 4 ? 1 : BYTES / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const T* p)
+    {
+        if constexpr (BYTES == 32) ldg256(w, p);
+        else if constexpr (BYTES == 16) {
+            const uint4 q = *reinterpret_cast<const uint4*>(p);
+            w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+        } else if constexpr (BYTES == 4) w[0] = *reinterpret_cast<const uint32_t*>(p);
+        else w[0] = *reinterpret_cast<const uint16_t*>(p);
+    }
+    __device__ __forceinline__ void store(T* p) const
+    {
+        if constexpr (BYTES == 32) stg256(p, w);
+        else if constexpr (BYTES == 16) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        else if constexpr (BYTES == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
+        else *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
+    }
+    __device__ __forceinline__ float get(int i) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        else return i & 1 ? bf16_high(w[i >> 1]) : bf16_low(w[i >> 1]);
+    }
+    __device__ __forceinline__ void set_all(const float* v)
+    {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < kElems; ++i) w[i] = __float_as_uint(v[i]);
+        } else if constexpr (kElems == 1) w[0] = bf16x2_of(v[0], 0.f);
+        else {
+#pragma unroll
+            for (int i = 0; i < kElems; i += 2) w[i >> 1] = bf16x2_of(v[i], v[i + 1]);
+        }
+    }
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (uint32_t& u : w) u = 0;
+    }
+    __device__ __forceinline__ Piece scaled(float s) const
+    {
+        float v[kElems];
+        Piece r;
+#pragma unroll
+        for (int i = 0; i < kElems; ++i) v[i] = get(i) * s;
+        r.set_all(v);
+        return r;
+    }
+};
 
 // ---- host side
 

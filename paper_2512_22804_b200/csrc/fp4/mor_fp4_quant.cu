@@ -6,6 +6,8 @@
 // transposed row leave 64 bytes at a time.  A thread takes units of 32 consecutive elements: one or two blocks, so a block's
 // maximum needs no exchange between threads.  For the column direction the tile goes through shared memory once, in the
 // input's own type where no weight is applied.
+#include <type_traits>
+
 #include "mor_fp4.cuh"
 
 namespace mor {
@@ -93,90 +95,103 @@ __device__ __forceinline__ float block_max(float m, float* shared)
     return r;
 }
 
-// Largest finite magnitude of a unit, times the weight of each slot that has a row.  The maximum over slots of fl(w x) is
+// Largest finite magnitude of a piece, times the weight of each slot that has a row.  The maximum over slots of fl(w x) is
 // fl(max|w| * max|x|), since rounding is monotonic; only where that is not finite are the products looked at one by one.
-template <typename T, int MODE> __device__ __noinline__ float unit_max_careful(const Raw<T>& r, const QuantParams& p, int64_t token)
+template <typename T, int BYTES, int MODE> __device__ __noinline__ float piece_max_careful(const Piece<T, BYTES> v, const QuantParams& p, int64_t token)
 {
-    float v[kUnit], m = 0.f;
-    unpack<T>(r, v);
+    float m = 0.f;
     const int slots = MODE == PLAIN ? 1 : (int)p.top;
     for (int j = 0; j < slots; ++j) {
         if (MODE != PLAIN && p.row_of_slot[token * p.top + j] < 0) continue;
         const float w = MODE == WEIGHTED ? weight_at(p.weight, p.weight_dtype, token * p.top + j) : 1.f;
 #pragma unroll
-        for (int i = 0; i < kUnit; ++i) {
-            const float a = fabsf(v[i] * w);
+        for (int i = 0; i < Piece<T, BYTES>::kElems; ++i) {
+            const float a = fabsf(v.get(i) * w);
             if (a < INFINITY) m = fmaxf(m, a);
         }
     }
     return m;
 }
-template <typename T, int MODE> __device__ __forceinline__ float unit_max(const Raw<T>& r, const QuantParams& p, int64_t token)
+// Largest |weight| among the token's slots that have a row; -1 if none has.
+template <int MODE> __device__ __forceinline__ float token_weight(const QuantParams& p, int64_t token)
 {
-    float v[kUnit], w = 1.f;
-    unpack<T>(r, v);
-    const float a = amax_of<kUnit>(v);
-    if constexpr (MODE != PLAIN) {
-        w = -1.f;
-        for (uint32_t j = 0; j < p.top; ++j)
-            if (p.row_of_slot[token * p.top + j] >= 0) w = fmaxf(w, MODE == WEIGHTED ? fabsf(weight_at(p.weight, p.weight_dtype, token * p.top + j)) : 1.f);
-        if (w < 0.f && MODE == GATHER) return 0.f;
+    if constexpr (MODE == PLAIN) return 1.f;
+    float w = -1.f;
+    for (uint32_t j = 0; j < p.top; ++j)
+        if (p.row_of_slot[token * p.top + j] >= 0) w = fmaxf(w, MODE == WEIGHTED ? fabsf(weight_at(p.weight, p.weight_dtype, token * p.top + j)) : 1.f);
+    return w;
+}
+template <typename T, int BYTES, int MODE> __device__ __forceinline__ float piece_max(const Piece<T, BYTES>& v, const QuantParams& p, int64_t token)
+{
+    float a = 0.f;
+    if constexpr (sizeof(T) == 2 && BYTES >= 4) {
+        a = amax_of_pair(amax_of_words<BYTES / 4>(v.w));
+    } else {
+#pragma unroll
+        for (int i = 0; i < Piece<T, BYTES>::kElems; ++i) a = max_nan(a, v.get(i));
     }
+    const float w = token_weight<MODE>(p, token);
+    if (MODE == GATHER && w < 0.f) return 0.f;
     const float m = a * w;
-    return m >= 0.f && m < INFINITY ? m : unit_max_careful<T, MODE>(r, p, token);
+    return m >= 0.f && m < INFINITY ? m : piece_max_careful<T, BYTES, MODE>(v, p, token);
 }
 
 // The largest magnitude of the whole tensor, one part per CTA (they are joined by the kernel that quantises: no counter to
-// clear, no atomics).  A thread keeps two units in flight.
-template <typename T, int MODE> __global__ void __launch_bounds__(kQThreads) fp4_amax_kernel(const __grid_constant__ QuantParams p, float* part)
+// clear, no atomics).  Bound by memory: a warp reads 1 KiB at a time (32 bytes a lane), a thread keeps four pieces in flight.
+template <typename T, int BYTES, int MODE> __global__ void __launch_bounds__(kQThreads) fp4_amax_kernel(const __grid_constant__ QuantParams p, float* part)
 {
+    using P = Piece<T, BYTES>;
+    constexpr int kFlight = 4;
     __shared__ float red[kQThreads / 32];
     cudaTriggerProgrammaticLaunchCompletion();
-    const int64_t units = (p.cols + kUnit - 1) / kUnit;
-    const int64_t step = (int64_t)gridDim.x * kQThreads, drow = step / units, dunit = step % units;
-    const int64_t first = (int64_t)blockIdx.x * kQThreads + threadIdx.x;
-    int64_t row = first / units, unit = first % units;
-    const int64_t rows = p.x_rows * p.batch;
     const T* x = static_cast<const T*>(p.x);
+    const bool flat = MODE == PLAIN && p.ld == p.cols && (p.batch == 1 || p.batch_stride == p.x_rows * p.ld);
+    const int64_t rows = flat ? 1 : p.x_rows * p.batch, cols = flat ? p.x_rows * p.batch * p.cols : p.cols;
+    const int64_t per = cols / P::kElems;                            // cols is a whole number of pieces
+    const int64_t step = (int64_t)gridDim.x * kQThreads, drow = step / per, dpiece = step % per;
+    const int64_t first = (int64_t)blockIdx.x * kQThreads + threadIdx.x;
+    int64_t row = first / per, at = first % per;
     float m = 0.f;
-    auto address = [&](int64_t r, int64_t u) {
-        return x + (p.batch == 1 ? r * p.ld : (r / p.x_rows) * p.batch_stride + (r % p.x_rows) * p.ld) + u * kUnit;
-    };
-    auto advance = [&](int64_t& r, int64_t& u) {
-        r += drow;
-        u += dunit;
-        if (u >= units) { u -= units; ++r; }
-    };
     while (row < rows) {
-        Raw<T> a, b;
-        int64_t row2 = row, unit2 = unit;
-        advance(row2, unit2);
-        load_unit<T>(a, address(row, unit), (int)min((int64_t)kUnit, p.cols - unit * kUnit), p.access);
-        const bool two = row2 < rows;
-        if (two) load_unit<T>(b, address(row2, unit2), (int)min((int64_t)kUnit, p.cols - unit2 * kUnit), p.access);
-        m = fmaxf(m, unit_max<T, MODE>(a, p, row));
-        if (two) m = fmaxf(m, unit_max<T, MODE>(b, p, row2));
-        row = row2;
-        unit = unit2;
-        advance(row, unit);
+        P v[kFlight];
+        int64_t token[kFlight];
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i) {
+            token[i] = row;
+            v[i].clear();
+            if (row < rows) v[i].load(x + (p.batch == 1 || flat ? row * p.ld : (row / p.x_rows) * p.batch_stride + (row % p.x_rows) * p.ld) + at * P::kElems);
+            row += drow;
+            at += dpiece;
+            if (at >= per) { at -= per; ++row; }
+        }
+#pragma unroll
+        for (int i = 0; i < kFlight; ++i)
+            if (token[i] < rows) m = fmaxf(m, piece_max<T, BYTES, MODE>(v[i], p, token[i]));
     }
     m = block_max(m, red);
     if (threadIdx.x == 0) part[blockIdx.x] = m;
 }
 
-// Pitches of the tile in shared memory: a row of 128 elements and 16 bytes, so that a warp that walks down the columns and one
-// that writes 16-byte pieces of several rows both meet few bank conflicts.
-template <bool NARROW> struct Tile { static constexpr int kPitch = 128 * (NARROW ? 2 : 4) + 16; };
-constexpr int kStagePitch = 80;       // 64 bytes of codes of one transposed row
+// The tile in shared memory (COLS): rows of 128 elements without padding, their 16-byte chunks permuted, so that neither the
+// threads that write units of two rows at a time nor those that walk down neighbouring columns meet bank conflicts: chunk c of
+// row r is at c ^ (c / 8) ^ 2 (r & 1) for 16-bit elements (units of four chunks), c ^ (c / 8 + 4 (r & 1)) for 32-bit ones (eight).
+template <bool NARROW> struct Tile {
+    static constexpr int kPitch = 128 * (NARROW ? 2 : 4);
+    static __device__ __forceinline__ int chunk(int row, int c) { return NARROW ? c ^ (c >> 3) ^ ((row & 1) << 1) : c ^ ((c >> 3) | ((row & 1) << 2)); }
+};
+// Codes of the transposed rows on their way out, 64 bytes each, permuted to the same end (even columns first).
+__device__ __forceinline__ int stage_at(int lcol, int u) { return ((lcol >> 1) + 64 * (lcol & 1)) * 64 + ((u ^ ((lcol >> 2) & 3)) * 16); }
 
 template <typename T, int FMT, bool ROWS, bool COLS, int MODE>
-__global__ void __launch_bounds__(kQThreads) fp4_quant_kernel(const __grid_constant__ QuantParams p)
+__global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED ? 3 : 2) fp4_quant_kernel(const __grid_constant__ QuantParams p)
 {
     constexpr bool kNarrow = sizeof(T) == 2 && MODE != WEIGHTED;          // the tile keeps the input's BF16 values
-    constexpr int kPitch = Tile<kNarrow>::kPitch;
+    using L = Tile<kNarrow>;
+    constexpr int kPitch = L::kPitch;
     constexpr int kTiles = FMT == MOR_FP4_E4M3_16 ? 2 : 1;                // scale tiles per 128 elements
     constexpr int kPerUnit = Fp4<FMT>::kBlocksPerUnit;
     __shared__ float red[kQThreads / 32];
+    __shared__ float factors[FMT == MOR_FP4_E4M3_16 ? 128 : 1];
     __shared__ __align__(16) uint8_t row_scales[ROWS ? kTiles * kScaleTile : 16];
     __shared__ __align__(16) uint8_t col_scales[COLS ? kTiles * kScaleTile : 16];
     extern __shared__ __align__(16) uint8_t dyn[];                        // COLS: tile, then the codes of the transposed rows
@@ -189,6 +204,29 @@ __global__ void __launch_bounds__(kQThreads) fp4_quant_kernel(const __grid_const
     // both units' loads first: the tile is in flight while the tensor maximum is waited for
     Raw<T> raw[2];
     float weight[2] = {1.f, 1.f};
+    constexpr int kInPitch = 128 * (int)sizeof(T) + 16;
+    if (p.access < 16) {        // rows that start anywhere: neighbouring lanes take neighbouring elements, through shared memory
+        for (int r = tid >> 5; r < 128; r += kQThreads / 32) {
+            const int64_t row = (int64_t)row_tile * 128 + r;
+            int64_t src = row;
+            bool have = row < p.rows;
+            if constexpr (MODE != PLAIN) {
+                const int32_t slot = have ? p.slot_of_row[row] : -1;
+                have = slot >= 0;
+                src = have ? slot / (int32_t)p.top : 0;
+            }
+            const T* from = x + src * p.ld + (int64_t)col_tile * 128;
+            Piece<T, (int)sizeof(T)> v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[j].clear();
+                if (have && (int64_t)col_tile * 128 + j * 32 + (tid & 31) < p.cols) v[j].load(from + j * 32 + (tid & 31));
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j].store(reinterpret_cast<T*>(dyn + r * kInPitch) + j * 32 + (tid & 31));
+        }
+        __syncthreads();
+    }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int at = tid + i * kQThreads;
@@ -201,13 +239,20 @@ __global__ void __launch_bounds__(kQThreads) fp4_quant_kernel(const __grid_const
             src = have ? slot / (int32_t)p.top : 0;
             if (MODE == WEIGHTED && have) weight[i] = weight_at(p.weight, p.weight_dtype, slot);
         }
-        if (have) load_unit<T>(raw[i], x + src * p.ld + col, (int)min((int64_t)kUnit, p.cols - col), p.access);
+        if (p.access < 16) {
+#pragma unroll
+            for (int j = 0; j < (int)sizeof(Raw<T>) / 4; j += 4) {
+                const uint4 q = *reinterpret_cast<const uint4*>(dyn + (at >> 2) * kInPitch + (at & 3) * kUnit * sizeof(T) + j * 4);
+                raw[i].w[j] = q.x; raw[i].w[j + 1] = q.y; raw[i].w[j + 2] = q.z; raw[i].w[j + 3] = q.w;
+            }
+        } else if (have) load_unit<T>(raw[i], x + src * p.ld + col, (int)min((int64_t)kUnit, p.cols - col), p.access);
         else
 #pragma unroll
             for (uint32_t& w : raw[i].w) w = 0;
     }
+    if (COLS && p.access < 16) __syncthreads();           // the tile takes the same memory
 
-    TensorScale ts = {1.f, 1.f};
+    TensorScale ts = {1.f, 1.f, 1.f};
     if constexpr (FMT == MOR_FP4_E4M3_16) {
         float amax = 0.f;
         if (p.amax != nullptr) {
@@ -217,17 +262,24 @@ __global__ void __launch_bounds__(kQThreads) fp4_quant_kernel(const __grid_const
             for (uint32_t i = tid; i < p.n_partial; i += kQThreads) amax = fmaxf(amax, __ldcg(p.partial + i));
             amax = block_max(amax, red);
         } else {
-            const int64_t units = (p.cols + kUnit - 1) / kUnit;
-            for (int64_t i = tid; i < units * p.x_rows * p.batch; i += kQThreads) {
-                const int64_t r = i / units, u = i % units;
-                Raw<T> a;
-                load_unit<T>(a, static_cast<const T*>(p.x) + (r / p.x_rows) * p.batch_stride + (r % p.x_rows) * p.ld + u * kUnit,
-                             (int)min((int64_t)kUnit, p.cols - u * kUnit), p.access);
-                amax = fmaxf(amax, unit_max<T, PLAIN>(a, p, 0));
-            }
+            const bool wide = p.access >= 16 && p.cols * (int64_t)sizeof(T) % 16 == 0;
+            auto scan = [&](auto bytes) {
+                using P = Piece<T, decltype(bytes)::value>;
+                const int64_t per = p.cols / P::kElems;
+                for (int64_t i = tid; i < per * p.x_rows * p.batch; i += kQThreads) {
+                    const int64_t r = i / per;
+                    P v;
+                    v.load(static_cast<const T*>(p.x) + (r / p.x_rows) * p.batch_stride + (r % p.x_rows) * p.ld + (i % per) * P::kElems);
+                    amax = fmaxf(amax, piece_max<T, decltype(bytes)::value, PLAIN>(v, p, 0));
+                }
+            };
+            if (wide) scan(std::integral_constant<int, 16>{});
+            else scan(std::integral_constant<int, (int)sizeof(T)>{});
             amax = block_max(amax, red);
         }
         ts = tensor_scale_of(amax);
+        fill_factors(factors, ts.t, tid);
+        __syncthreads();
     }
     if (blockIdx.x == 0 && tid == 0) {
         if (ROWS) *p.r_t = ts.t;
@@ -245,19 +297,25 @@ __global__ void __launch_bounds__(kQThreads) fp4_quant_kernel(const __grid_const
             for (float& e : v) e *= weight[i];
         }
         if constexpr (COLS) {
-            uint8_t* to = dyn + lrow * kPitch + u * kUnit * (kNarrow ? 2 : 4);
+            uint8_t* to = dyn + lrow * kPitch;
             if constexpr (kNarrow) {
 #pragma unroll
-                for (int j = 0; j < 16; j += 4)
-                    *reinterpret_cast<uint4*>(to + 4 * j) = make_uint4(raw[i].w[j], raw[i].w[j + 1], raw[i].w[j + 2], raw[i].w[j + 3]);
+                for (int j = 0; j < 4; ++j)
+                    *reinterpret_cast<uint4*>(to + L::chunk(lrow, u * 4 + j) * 16) = make_uint4(raw[i].w[4 * j], raw[i].w[4 * j + 1], raw[i].w[4 * j + 2], raw[i].w[4 * j + 3]);
             } else {
 #pragma unroll
-                for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4*>(to + 4 * j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                for (int j = 0; j < 8; ++j) *reinterpret_cast<float4*>(to + L::chunk(lrow, u * 8 + j) * 16) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
             }
         }
         if constexpr (ROWS) {
             uint32_t scales;
-            const uint4 codes = quantise_unit<FMT>(v, ts, scales);
+            float a[kPerUnit];
+#pragma unroll
+            for (int k = 0; k < kPerUnit; ++k) {
+                if constexpr (kNarrow) a[k] = amax_of_pair(amax_of_words<16 / kPerUnit>(raw[i].w + k * (16 / kPerUnit)));
+                else a[k] = amax_of<kUnit / kPerUnit>(v + k * (kUnit / kPerUnit));
+            }
+            const uint4 codes = quantise_unit<FMT>(v, a, ts, factors, scales);
             if (row < p.rows && col < p.cols)
                 *reinterpret_cast<uint4*>(p.r_codes + ((int64_t)batch * p.rows + row) * p.r_ld + col / 2) = codes;
             uint8_t* s = row_scales + ((u * kPerUnit) >> 2) * kScaleTile + scale_at(lrow, u * kPerUnit);
@@ -274,10 +332,10 @@ __global__ void __launch_bounds__(kQThreads) fp4_quant_kernel(const __grid_const
     }
     if constexpr (COLS) {
         uint8_t* stage = dyn + 128 * kPitch;
-        auto put = [&](int lcol, int u, const float* v) {
+        auto put = [&](int lcol, int u, const float* v, const float* a) {
             uint32_t scales;
-            const uint4 codes = quantise_unit<FMT>(v, ts, scales);
-            *reinterpret_cast<uint4*>(stage + lcol * kStagePitch + u * 16) = codes;
+            const uint4 codes = quantise_unit<FMT>(v, a, ts, factors, scales);
+            *reinterpret_cast<uint4*>(stage + stage_at(lcol, u)) = codes;
             const bool in = (int64_t)col_tile * 128 + lcol < p.cols && (int64_t)row_tile * 128 + u * kUnit < p.rows;
             uint8_t* s = col_scales + ((u * kPerUnit) >> 2) * kScaleTile + scale_at(lcol, u * kPerUnit);
             if constexpr (kPerUnit == 2) *reinterpret_cast<uint16_t*>(s) = in ? (uint16_t)scales : 0;
@@ -285,24 +343,34 @@ __global__ void __launch_bounds__(kQThreads) fp4_quant_kernel(const __grid_const
         };
         if constexpr (kNarrow) {             // two neighbouring columns (one word) over 32 rows
             const int pair = tid & 63, u = tid >> 6;
-            uint32_t w[kUnit];
-            float v[kUnit];
+            const uint8_t* from[2] = {dyn + u * kUnit * kPitch + L::chunk(0, pair >> 2) * 16 + (pair & 3) * 4,
+                                      dyn + u * kUnit * kPitch + L::chunk(1, pair >> 2) * 16 + (pair & 3) * 4};
+            uint32_t w[kUnit], m[kPerUnit];
+            float v[kUnit], a[kPerUnit];
 #pragma unroll
-            for (int i = 0; i < kUnit; ++i) w[i] = *reinterpret_cast<const uint32_t*>(dyn + (u * kUnit + i) * kPitch + pair * 4);
+            for (int i = 0; i < kUnit; ++i) w[i] = *reinterpret_cast<const uint32_t*>(from[i & 1] + i * kPitch);
+#pragma unroll
+            for (int k = 0; k < kPerUnit; ++k) m[k] = amax_of_words<kUnit / kPerUnit>(w + k * (kUnit / kPerUnit));
+#pragma unroll
+            for (int k = 0; k < kPerUnit; ++k) a[k] = fabsf(bf16_low(m[k]));
 #pragma unroll
             for (int i = 0; i < kUnit; ++i) v[i] = bf16_low(w[i]);
-            put(2 * pair, u, v);
+            put(2 * pair, u, v, a);
+#pragma unroll
+            for (int k = 0; k < kPerUnit; ++k) a[k] = fabsf(bf16_high(m[k]));
 #pragma unroll
             for (int i = 0; i < kUnit; ++i) v[i] = bf16_high(w[i]);
-            put(2 * pair + 1, u, v);
+            put(2 * pair + 1, u, v, a);
         } else {
 #pragma unroll 1
             for (int half = 0; half < 2; ++half) {
                 const int lcol = tid & 127, u = (tid >> 7) + 2 * half;
-                float v[kUnit];
+                float v[kUnit], a[kPerUnit];
 #pragma unroll
-                for (int i = 0; i < kUnit; ++i) v[i] = *reinterpret_cast<const float*>(dyn + (u * kUnit + i) * kPitch + lcol * 4);
-                put(lcol, u, v);
+                for (int i = 0; i < kUnit; ++i) v[i] = *reinterpret_cast<const float*>(dyn + (u * kUnit + i) * kPitch + L::chunk(i & 1, lcol >> 2) * 16 + (lcol & 3) * 4);
+#pragma unroll
+                for (int k = 0; k < kPerUnit; ++k) a[k] = amax_of<kUnit / kPerUnit>(v + k * (kUnit / kPerUnit));
+                put(lcol, u, v, a);
             }
         }
         __syncthreads();
@@ -312,7 +380,7 @@ __global__ void __launch_bounds__(kQThreads) fp4_quant_kernel(const __grid_const
             const int64_t col = (int64_t)col_tile * 128 + lcol, row = (int64_t)row_tile * 128 + u * kUnit;
             if (col < p.cols && row < p.rows)
                 *reinterpret_cast<uint4*>(p.c_codes + ((int64_t)batch * p.cols + col) * p.c_ld + row / 2) =
-                    *reinterpret_cast<const uint4*>(stage + lcol * kStagePitch + u * 16);
+                    *reinterpret_cast<const uint4*>(stage + stage_at(lcol, u));
         }
         const uint32_t ktile = row_tile * kTiles + (tid >> 5);
         if (tid < kTiles * 32 && ktile < p.c_ktiles)
@@ -336,6 +404,8 @@ template <typename T, int FMT> __global__ void __launch_bounds__(kQThreads) fp4_
 {
     constexpr int kTiles = FMT == MOR_FP4_E4M3_16 ? 2 : 1;
     constexpr int kPerUnit = Fp4<FMT>::kBlocksPerUnit;
+    constexpr int kPitch = 128 * (int)sizeof(T) + 16;
+    extern __shared__ __align__(16) uint8_t dyn[];                  // rows that start anywhere: the tile's values
     __shared__ __align__(16) uint8_t scales[kTiles * kScaleTile];
     const int tid = threadIdx.x;
     const uint32_t per = p.row_tiles * p.col_tiles;
@@ -379,10 +449,14 @@ template <typename T, int FMT> __global__ void __launch_bounds__(kQThreads) fp4_
             if constexpr (sizeof(T) == 2) w[j] = bf16x2_of(v[2 * j], v[2 * j + 1]);
             else w[j] = __float_as_uint(v[j]);
         }
-        if (n == kUnit && p.access == 32) {
+        if (p.access < 16) {
+#pragma unroll
+            for (int j = 0; j < kWords; j += 4)
+                *reinterpret_cast<uint4*>(dyn + lrow * kPitch + u * kUnit * sizeof(T) + 4 * j) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
+        } else if (n == kUnit && p.access == 32) {
 #pragma unroll
             for (int j = 0; j < kWords; j += 8) stg256(reinterpret_cast<uint32_t*>(to) + j, w + j);
-        } else if (n == kUnit && p.access == 16) {
+        } else if (n == kUnit) {
 #pragma unroll
             for (int j = 0; j < kWords; j += 4) *reinterpret_cast<uint4*>(reinterpret_cast<uint32_t*>(to) + j) = make_uint4(w[j], w[j + 1], w[j + 2], w[j + 3]);
         } else {
@@ -394,14 +468,28 @@ template <typename T, int FMT> __global__ void __launch_bounds__(kQThreads) fp4_
             }
         }
     }
+    if (p.access >= 16) return;
+    __syncthreads();
+    for (int r = tid >> 5; r < 128; r += kQThreads / 32) {
+        const int64_t row = (int64_t)row_tile * 128 + r;
+        if (row >= p.rows) break;
+        const T* from = reinterpret_cast<const T*>(dyn + r * kPitch);
+        T* to = static_cast<T*>(p.out) + ((int64_t)batch * p.rows + row) * p.ldo + (int64_t)col_tile * 128;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int c = j * 32 + (tid & 31);
+            if ((int64_t)col_tile * 128 + c < p.cols) to[c] = from[c];
+        }
+    }
 }
 
 template <typename T, int FMT, bool ROWS, bool COLS, int MODE> cudaError_t quant_launch(const QuantParams& p, uint32_t grid, cudaStream_t st)
 {
     constexpr bool kNarrow = sizeof(T) == 2 && MODE != WEIGHTED;
-    constexpr int smem = COLS ? 128 * Tile<kNarrow>::kPitch + 128 * kStagePitch : 0;
+    constexpr int most = COLS ? 128 * Tile<kNarrow>::kPitch + 128 * 64 : 128 * (128 * (int)sizeof(T) + 16);
+    const int smem = COLS || p.access < 16 ? most : 0;
     static std::atomic<uint64_t> done{0};
-    if (smem > 0 && !allow_smem(fp4_quant_kernel<T, FMT, ROWS, COLS, MODE>, smem, done)) return cudaErrorInvalidValue;
+    if (smem > 0 && !allow_smem(fp4_quant_kernel<T, FMT, ROWS, COLS, MODE>, most, done)) return cudaErrorInvalidValue;
     return launch(fp4_quant_kernel<T, FMT, ROWS, COLS, MODE>, grid, kQThreads, smem, st, p.partial != nullptr, p);
 }
 template <typename T, int FMT, int MODE> cudaError_t quant_dirs(const QuantParams& p, uint32_t grid, cudaStream_t st)
@@ -413,7 +501,10 @@ template <typename T, int FMT, int MODE> cudaError_t quant_dirs(const QuantParam
 template <typename T, int MODE> cudaError_t quant_all(const QuantParams& p, int format, uint32_t amax_grid, uint32_t grid, float* part, cudaStream_t st)
 {
     if (amax_grid > 0) {
-        const cudaError_t e = launch(fp4_amax_kernel<T, MODE>, amax_grid, kQThreads, 0, st, false, p, part);
+        const int64_t width = p.cols * (int64_t)sizeof(T);
+        const cudaError_t e = p.access == 32 && width % 32 == 0   ? launch(fp4_amax_kernel<T, 32, MODE>, amax_grid, kQThreads, 0, st, false, p, part)
+                              : p.access >= 16 && width % 16 == 0 ? launch(fp4_amax_kernel<T, 16, MODE>, amax_grid, kQThreads, 0, st, false, p, part)
+                                                                  : launch(fp4_amax_kernel<T, (int)sizeof(T), MODE>, amax_grid, kQThreads, 0, st, false, p, part);
         if (e != cudaSuccess) return e;
     }
     return format == MOR_FP4_E4M3_16 ? quant_dirs<T, MOR_FP4_E4M3_16, MODE>(p, grid, st) : quant_dirs<T, MOR_FP4_E8M0_32, MODE>(p, grid, st);
@@ -508,8 +599,7 @@ mor_status_t mor_fp4_quantize(const mor_fp4_quantize_desc_t* host_desc, const mo
     }
     uint32_t amax_grid = 0;
     if (amax_kernel) {
-        const int64_t units = d.batch * d.rows * ceil_div(d.cols, kUnit);
-        const int64_t want = ceil_div(units, 2 * kQThreads);
+        const int64_t want = ceil_div(elems, 32 * kQThreads);
         amax_grid = (uint32_t)(want < 1 ? 1 : want > 148 * 4 ? 148 * 4 : want);
         static_assert(148 * 4 <= kAmaxMaxBlocks, "parts fit the workspace");
         p.partial = static_cast<const float*>(workspace);
@@ -548,13 +638,17 @@ mor_status_t mor_fp4_dequantize(const mor_fp4_matrix_t* host_in, void* out, int 
     const uint32_t grid = (uint32_t)(m.batch * p.row_tiles * p.col_tiles);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const bool nv = m.format == MOR_FP4_E4M3_16;
+    auto run = [&](auto kernel, int element, std::atomic<uint64_t>& done) {
+        const int smem = p.access < 16 ? 128 * (128 * element + 16) : 0;
+        if (smem > 0 && !allow_smem(kernel, smem, done)) return cudaErrorInvalidValue;
+        return launch(kernel, grid, kQThreads, smem, st, false, p);
+    };
+    static std::atomic<uint64_t> done[4];
     cudaError_t e;
     if (dtype == MOR_DTYPE_BF16)
-        e = nv ? launch(fp4_dequant_kernel<__nv_bfloat16, MOR_FP4_E4M3_16>, grid, kQThreads, 0, st, false, p)
-               : launch(fp4_dequant_kernel<__nv_bfloat16, MOR_FP4_E8M0_32>, grid, kQThreads, 0, st, false, p);
+        e = nv ? run(fp4_dequant_kernel<__nv_bfloat16, MOR_FP4_E4M3_16>, 2, done[0]) : run(fp4_dequant_kernel<__nv_bfloat16, MOR_FP4_E8M0_32>, 2, done[1]);
     else
-        e = nv ? launch(fp4_dequant_kernel<float, MOR_FP4_E4M3_16>, grid, kQThreads, 0, st, false, p)
-               : launch(fp4_dequant_kernel<float, MOR_FP4_E8M0_32>, grid, kQThreads, 0, st, false, p);
+        e = nv ? run(fp4_dequant_kernel<float, MOR_FP4_E4M3_16>, 4, done[2]) : run(fp4_dequant_kernel<float, MOR_FP4_E8M0_32>, 4, done[3]);
     return e == cudaSuccess ? MOR_OK : MOR_ERR_CUDA;
 }
 

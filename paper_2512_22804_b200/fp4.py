@@ -115,6 +115,13 @@ class Operand:
         return self._keep[0][at:at + 4].view(torch.float32)
 
 
+def _status_word(device, index: int) -> torch.Tensor:
+    w = _status.get(index)
+    if w is None:
+        w = _status[index] = torch.zeros(1, dtype=torch.int32, device=device)
+    return w
+
+
 def quantize(x: torch.Tensor, format: str, *, rows: bool = True, cols: bool = False, amax=None, gather=None, weight=None):
     """(operand along the rows or None, operand of the transpose or None) of x [R, C] or [batch, R, C], BF16 or FP32.
 
@@ -166,13 +173,6 @@ def dequantize(op: Operand, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor
     out = torch.empty(shape, dtype=dtype, device=op._keep[0].device)
     _check(_b.load().mor_fp4_dequantize(C.byref(c), out.data_ptr(), _dtype(dtype, "dtype"), c.cols, _raw_stream(op.device)), "mor_fp4_dequantize")
     return out
-
-
-def _status_word(device, index: int) -> torch.Tensor:
-    w = _status.get(index)
-    if w is None:
-        w = _status[index] = torch.zeros(1, dtype=torch.int32, device=device)
-    return w
 
 
 def check(device=None) -> None:

@@ -154,7 +154,7 @@ def test_quantised_gather_equals_gather_then_quantise(experts, fmt, weighted):
 
     from paper_2512_22804_b200 import fp4
 
-    for tokens, hidden in ((40, 96), (300, 333)):
+    for tokens, hidden in ((40, 96), (300, 333), (1100, 1544)):
         plan, row, slot, matrix = matrices(experts, tokens, 3, 6, hidden, 128, "bf16", tokens)
         x, tx = matrix(tokens)
         w = np.random.default_rng(2).random((tokens, 3)).astype(np.float32)

@@ -53,7 +53,7 @@ def check_operand(op, x, fmt, amax=None):
     return codes, byte, t
 
 
-SHAPES = [(1, 1), (1, 16), (1, 4096), (2, 33), (3, 100), (128, 128), (129, 64), (127, 257), (300, 96), (40, 1000), (1000, 40), (5, 14336)]
+SHAPES = [(1, 1), (1, 16), (1, 4096), (2, 33), (3, 100), (128, 128), (129, 64), (127, 257), (300, 96), (40, 1000), (1000, 40), (5, 14336), (2500, 2056), (2305, 2184), (130, 38000)]
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
