@@ -157,7 +157,7 @@ struct MoveParams {
     int64_t ld_token, ld_row, ld_out;
     uint32_t top;
     int32_t weight_dtype;
-    uint32_t token_blocks;     // gather and gradient: CTAs from here on clear the rows without a slot
+    uint32_t clear_blocks;     // gather and gradient: the first CTAs clear the rows without a slot
     const int32_t *row_of_slot, *slot_of_row;
     const void* weight;
     const void *tokens_in, *rows_in;   // token side (x, dy), row side (ys)
@@ -165,52 +165,62 @@ struct MoveParams {
     void* dweight;
 };
 
-// Zeroes the rows without a slot among this CTA's 256.
+// Zeroes the rows without a slot among this CTA's kClearRows.  Masked tokens leave all their empty rows at the end, so a CTA
+// takes few of them (256 rows of 8 KiB by one CTA took longer than the rest of the gather), and these CTAs come first.
+constexpr int kClearRows = 16;
 template <typename T, int BYTES> __device__ void clear_rows(const MoveParams& p, T* out, uint32_t block)
 {
     using P = Piece<T, BYTES>;
-    __shared__ uint32_t empty[8];
-    const int64_t base = (int64_t)block * 256;
-    for (int i = threadIdx.x; i < 256; i += blockDim.x) {           // blockDim.x is a multiple of 32
-        const bool none = base + i < p.rows && p.slot_of_row[base + i] < 0;
-        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, none);
-        if ((i & 31) == 0) empty[i >> 5] = mask;
-    }
-    __syncthreads();
+    const int64_t row = (int64_t)block * kClearRows + (threadIdx.x & 31);
+    const bool none = (threadIdx.x & 31) < kClearRows && row < p.rows && p.slot_of_row[row] < 0;
     P zero;
     zero.clear();
-    for (int k = 0; k < 8; ++k)
-        for (uint32_t m = empty[k]; m != 0; m &= m - 1) {
-            T* to = out + (base + k * 32 + __ffs(m) - 1) * p.ld_out;
-            for (int64_t c = (int64_t)threadIdx.x * P::kElems; c < p.hidden; c += (int64_t)blockDim.x * P::kElems) zero.store(to + c);
-        }
+    for (uint32_t m = __ballot_sync(0xFFFFFFFFu, none); m != 0; m &= m - 1) {
+        T* to = out + ((int64_t)block * kClearRows + __ffs(m) - 1) * p.ld_out;
+        for (int64_t c = (int64_t)threadIdx.x * P::kElems; c < p.hidden; c += (int64_t)blockDim.x * P::kElems) zero.store(to + c);
+    }
 }
+
+constexpr int kAtOnce = 4;      // slots whose rows are in flight together
+
+// Rows (-1: none) and weights of kAtOnce slots of a token.
+struct Slots {
+    int32_t row[kAtOnce];
+    float w[kAtOnce];
+    __device__ __forceinline__ Slots(const MoveParams& p, int64_t token, uint32_t first)
+    {
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) row[j] = first + j < p.top ? p.row_of_slot[token * p.top + first + j] : -1;
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) w[j] = row[j] < 0 || p.weight == nullptr ? 1.f : weight_at(p.weight, p.weight_dtype, token * p.top + first + j);
+    }
+};
 
 template <typename T, int BYTES> __global__ void __launch_bounds__(256) expert_gather_kernel(const __grid_constant__ MoveParams p)
 {
     using P = Piece<T, BYTES>;
     T* out = static_cast<T*>(p.out);
-    if (blockIdx.x >= p.token_blocks) {
-        clear_rows<T, BYTES>(p, out, blockIdx.x - p.token_blocks);
+    if (blockIdx.x < p.clear_blocks) {
+        clear_rows<T, BYTES>(p, out, blockIdx.x);
         return;
     }
-    const int64_t token = blockIdx.x;
+    const int64_t token = blockIdx.x - p.clear_blocks;
     const T* x = static_cast<const T*>(p.tokens_in) + token * p.ld_token;
-    const int32_t* rows = p.row_of_slot + token * p.top;
-    for (int64_t c = (int64_t)threadIdx.x * P::kElems; c < p.hidden; c += (int64_t)blockDim.x * P::kElems) {
-        P v;
-        v.load(x + c);
-        for (uint32_t j = 0; j < p.top; ++j) {
-            const int32_t row = rows[j];
-            if (row < 0) continue;
-            T* to = out + (int64_t)row * p.ld_out + c;
-            if (p.weight == nullptr) v.store(to);
-            else v.scaled(weight_at(p.weight, p.weight_dtype, token * p.top + j)).store(to);
+    for (uint32_t j0 = 0; j0 < p.top; j0 += kAtOnce) {
+        const Slots s(p, token, j0);
+        for (int64_t c = (int64_t)threadIdx.x * P::kElems; c < p.hidden; c += (int64_t)blockDim.x * P::kElems) {
+            P v;
+            v.load(x + c);
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+                if (s.row[j] < 0) continue;
+                T* to = out + (int64_t)s.row[j] * p.ld_out + c;
+                if (p.weight == nullptr) v.store(to);
+                else v.scaled(s.w[j]).store(to);
+            }
         }
     }
 }
-
-constexpr int kAtOnce = 4;      // slots whose rows are in flight together
 
 template <typename T, int BYTES> __global__ void __launch_bounds__(256) expert_combine_kernel(const __grid_constant__ MoveParams p)
 {
@@ -223,23 +233,17 @@ template <typename T, int BYTES> __global__ void __launch_bounds__(256) expert_c
 #pragma unroll
         for (float& s : sum) s = 0.f;
         for (uint32_t j0 = 0; j0 < p.top; j0 += kAtOnce) {
+            const Slots s(p, token, j0);
             P v[kAtOnce];
-            float w[kAtOnce];
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j) {
-                const int64_t slot = token * p.top + j0 + j;
-                const int32_t row = j0 + j < p.top ? p.row_of_slot[slot] : -1;
-                w[j] = 0.f;
                 v[j].clear();
-                if (row >= 0) {
-                    v[j].load(ys + (int64_t)row * p.ld_row + c);
-                    w[j] = p.weight == nullptr ? 1.f : weight_at(p.weight, p.weight_dtype, slot);
-                }
+                if (s.row[j] >= 0) v[j].load(ys + (int64_t)s.row[j] * p.ld_row + c);
             }
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j)
 #pragma unroll
-                for (int i = 0; i < P::kElems; ++i) sum[i] = fmaf(w[j], v[j].get(i), sum[i]);
+                for (int i = 0; i < P::kElems; ++i) sum[i] = fmaf(s.w[j], v[j].get(i), sum[i]);
         }
         P r;
         r.set_all(sum);
@@ -248,51 +252,49 @@ template <typename T, int BYTES> __global__ void __launch_bounds__(256) expert_c
 }
 
 // The sums over hidden of <dy, ys> are taken per thread in column order, then over the CTA in a fixed tree: the result
-// does not change from run to run.
-template <typename T, int BYTES> __global__ void __launch_bounds__(256) expert_grad_kernel(const __grid_constant__ MoveParams p)
+// does not change from run to run.  Four CTAs an SM (64 registers): with the 118 that the compiler would take, two, and not enough
+// rows are in flight.
+template <typename T, int BYTES> __global__ void __launch_bounds__(256, 4) expert_grad_kernel(const __grid_constant__ MoveParams p)
 {
     using P = Piece<T, BYTES>;
     T* out = static_cast<T*>(p.out);
-    if (blockIdx.x >= p.token_blocks) {
-        clear_rows<T, BYTES>(p, out, blockIdx.x - p.token_blocks);
+    if (blockIdx.x < p.clear_blocks) {
+        clear_rows<T, BYTES>(p, out, blockIdx.x);
         return;
     }
     __shared__ float part[kAtOnce][8];
-    const int64_t token = blockIdx.x;
+    const int64_t token = blockIdx.x - p.clear_blocks;
     const T* dy = static_cast<const T*>(p.tokens_in) + token * p.ld_token;
     const T* ys = static_cast<const T*>(p.rows_in);
     const int warps = blockDim.x >> 5;
     for (uint32_t j0 = 0; j0 < p.top; j0 += kAtOnce) {
-        float dot[kAtOnce], w[kAtOnce];
-        int32_t row[kAtOnce];
+        const Slots s(p, token, j0);
+        float dot[kAtOnce];
 #pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) {
-            const int64_t slot = token * p.top + j0 + j;
-            row[j] = j0 + j < p.top ? p.row_of_slot[slot] : -1;
-            w[j] = row[j] < 0 || p.weight == nullptr ? 1.f : weight_at(p.weight, p.weight_dtype, slot);
-            dot[j] = 0.f;
-        }
+        for (float& d : dot) d = 0.f;
         for (int64_t c = (int64_t)threadIdx.x * P::kElems; c < p.hidden; c += (int64_t)blockDim.x * P::kElems) {
             P g, v[kAtOnce];
             g.load(dy + c);
             if (p.dweight != nullptr) {
 #pragma unroll
                 for (int j = 0; j < kAtOnce; ++j)
-                    if (row[j] >= 0) v[j].load(ys + (int64_t)row[j] * p.ld_row + c);
-#pragma unroll
-                for (int j = 0; j < kAtOnce; ++j)
-                    if (row[j] >= 0)
-#pragma unroll
-                        for (int i = 0; i < P::kElems; ++i) dot[j] = fmaf(g.get(i), v[j].get(i), dot[j]);
+                    if (s.row[j] >= 0) v[j].load(ys + (int64_t)s.row[j] * p.ld_row + c);
             }
             if (out != nullptr) {
 #pragma unroll
                 for (int j = 0; j < kAtOnce; ++j)
-                    if (row[j] >= 0) {
-                        T* to = out + (int64_t)row[j] * p.ld_out + c;
+                    if (s.row[j] >= 0) {
+                        T* to = out + (int64_t)s.row[j] * p.ld_out + c;
                         if (p.weight == nullptr) g.store(to);
-                        else g.scaled(w[j]).store(to);
+                        else g.scaled(s.w[j]).store(to);
                     }
+            }
+            if (p.dweight != nullptr) {
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j)
+                    if (s.row[j] >= 0)
+#pragma unroll
+                        for (int i = 0; i < P::kElems; ++i) dot[j] = fmaf(g.get(i), v[j].get(i), dot[j]);
             }
         }
         if (p.dweight == nullptr) continue;
@@ -304,13 +306,13 @@ template <typename T, int BYTES> __global__ void __launch_bounds__(256) expert_g
         }
         __syncthreads();
         if (threadIdx.x < kAtOnce && j0 + threadIdx.x < p.top) {
-            float s = part[threadIdx.x][0];
-            for (int k = 1; k < warps; ++k) s += part[threadIdx.x][k];
+            float sum = part[threadIdx.x][0];
+            for (int k = 1; k < warps; ++k) sum += part[threadIdx.x][k];
             const int64_t slot = token * p.top + j0 + threadIdx.x;
-            if (p.weight_dtype == MOR_DTYPE_BF16) static_cast<__nv_bfloat16*>(p.dweight)[slot] = __float2bfloat16(s);
-            else static_cast<float*>(p.dweight)[slot] = s;
+            if (p.weight_dtype == MOR_DTYPE_BF16) static_cast<__nv_bfloat16*>(p.dweight)[slot] = __float2bfloat16(sum);
+            else static_cast<float*>(p.dweight)[slot] = sum;
         }
-        __syncthreads();
+        if (j0 + kAtOnce < p.top) __syncthreads();
     }
 }
 
@@ -447,8 +449,8 @@ mor_status_t mor_expert_gather(const mor_expert_desc_t* host_desc, const void* x
     p.ld_token = ldx;
     p.out = out;
     p.ld_out = ldo;
-    p.token_blocks = (uint32_t)p.tokens;
-    return move_run(*host_desc, p, MOVE_GATHER, p.token_blocks + (uint32_t)ceil_div(p.rows, 256), access, cuda_stream);
+    p.clear_blocks = (uint32_t)ceil_div(p.rows, kClearRows);
+    return move_run(*host_desc, p, MOVE_GATHER, p.clear_blocks + (uint32_t)p.tokens, access, cuda_stream);
 }
 
 mor_status_t mor_expert_combine(const mor_expert_desc_t* host_desc, const void* ys, int64_t ldy, void* out, int64_t ldo, void* cuda_stream)
@@ -486,13 +488,12 @@ mor_status_t mor_expert_combine_grad(const mor_expert_desc_t* host_desc, const v
     p.out = dys;
     p.ld_out = lddys;
     p.dweight = dweight;
-    p.token_blocks = (uint32_t)p.tokens;
-    const uint32_t clear = dys != nullptr ? (uint32_t)ceil_div(p.rows, 256) : 0;
+    p.clear_blocks = dys != nullptr ? (uint32_t)ceil_div(p.rows, kClearRows) : 0;
     if (p.hidden == 0 && dweight != nullptr && p.tokens > 0) {     // sums over nothing
         const size_t n = (size_t)p.tokens * p.top * dtype_bytes(host_desc->weight_dtype);
         return cudaMemsetAsync(dweight, 0, n, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? MOR_OK : MOR_ERR_CUDA;
     }
-    return move_run(*host_desc, p, MOVE_GRAD, p.token_blocks + clear, access, cuda_stream);
+    return move_run(*host_desc, p, MOVE_GRAD, p.clear_blocks + (uint32_t)p.tokens, access, cuda_stream);
 }
 
 }  // extern "C"

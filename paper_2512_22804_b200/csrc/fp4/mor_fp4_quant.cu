@@ -183,7 +183,7 @@ template <bool NARROW> struct Tile {
 __device__ __forceinline__ int stage_at(int lcol, int u) { return ((lcol >> 1) + 64 * (lcol & 1)) * 64 + ((u ^ ((lcol >> 2) & 3)) * 16); }
 
 template <typename T, int FMT, bool ROWS, bool COLS, int MODE>
-__global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED ? 3 : 2) fp4_quant_kernel(const __grid_constant__ QuantParams p)
+__global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED ? 4 : 2) fp4_quant_kernel(const __grid_constant__ QuantParams p)
 {
     constexpr bool kNarrow = sizeof(T) == 2 && MODE != WEIGHTED;          // the tile keeps the input's BF16 values
     using L = Tile<kNarrow>;
