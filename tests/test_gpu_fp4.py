@@ -209,7 +209,7 @@ def grouped(counts, hidden, fmt, fp4, seed):
     return plan, starts, rows, x
 
 
-COUNTS = [[1], [128], [0, 5, 0], [130, 0, 1, 256, 300], [7] * 40]
+COUNTS = [[1], [128], [0, 5, 0], [130, 0, 1, 256, 300], [7] * 40, [500, 129, 700]]
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
