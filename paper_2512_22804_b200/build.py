@@ -1,4 +1,5 @@
-"""Builds ``libmor_b200.so`` (the C-ABI library with the sm_100a kernels) in-tree with nvcc.
+"""Builds ``libmor_b200.so`` (the C-ABI library with the sm_100a kernels) in-tree with nvcc, and on top of it ``_ops.so`` (the
+4-bit operators and the routing as torch operators: host code only) with g++.
 
 Run as ``python -m paper_2512_22804_b200.build``.  nvcc cross-compiles, so no GPU is needed.
 """
@@ -17,6 +18,8 @@ SOURCES = ["mor_api.cu", "mor_kernels.cu", "mor_static.cu", "mor_main.cu", "mor_
            "mor_main_blk128.cu", "mor_main_blk64.cu", "mor_main_col128.cu", "mor_main_channel.cu", "mor_main_dual.cu", "mor_main_colch.cu",
            "fp4/mor_fp4_quant.cu", "fp4/mor_fp4_gemm.cu", "fp4/mor_experts.cu"]
 OBJ_DIR = os.path.join(HERE, "_build")
+OPS_SOURCE = os.path.join(CSRC, "ops", "mor_ops.cpp")
+OPS = os.path.join(HERE, "_ops.so")
 
 
 def nvcc_path() -> str:
@@ -27,7 +30,7 @@ def nvcc_path() -> str:
 
 
 def _deps():
-    files = [os.path.join(d, f) for d, _, names in os.walk(CSRC) for f in names]
+    files = [os.path.join(d, f) for d, _, names in os.walk(CSRC) for f in names if f.endswith((".cu", ".cuh", ".h"))]
     return files + [os.path.join(ROOT, "include", "mor.h")]
 
 
@@ -42,6 +45,7 @@ def build(force: bool = False, verbose: bool = False, lib: str = LIB, extra_flag
     """Compile every source file to an object (side by side: the main kernel's instantiations are spread over
     several files for that purpose) and link the shared library."""
     if not force and lib == LIB and not needs_build():
+        build_ops()
         return lib
     from concurrent.futures import ThreadPoolExecutor
 
@@ -65,7 +69,29 @@ def build(force: bool = False, verbose: bool = False, lib: str = LIB, extra_flag
     with ThreadPoolExecutor(max_workers=min(len(SOURCES), os.cpu_count() or 4)) as pool:
         objs = list(pool.map(compile_one, SOURCES))
     subprocess.run([nvcc_path(), "-gencode", "arch=compute_100a,code=sm_100a", "-shared", *objs, "-o", lib], check=True)
+    if lib == LIB:
+        build_ops(force)
     return lib
+
+
+def build_ops(force: bool = False) -> str:
+    """Compile the torch operators against the installed torch; they find ``libmor_b200.so`` beside themselves."""
+    header = os.path.join(ROOT, "include", "mor.h")
+    if not force and os.path.exists(OPS) and os.path.getmtime(OPS) > max(os.path.getmtime(OPS_SOURCE), os.path.getmtime(header)):
+        return OPS
+    import sysconfig
+
+    import torch
+
+    t = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(nvcc_path()))
+    include = [os.path.join(ROOT, "include"), os.path.join(t, "include"), os.path.join(t, "include", "torch", "csrc", "api", "include"),
+               sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
+    subprocess.run([shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-DTORCH_EXTENSION_NAME=_ops",
+                    "-DTORCH_API_INCLUDE_EXTENSION_H", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                    *[f"-I{d}" for d in include], OPS_SOURCE, "-o", OPS, f"-L{os.path.join(t, 'lib')}", "-ltorch", "-ltorch_cpu", "-ltorch_python",
+                    "-lc10", "-lc10_cuda", f"-L{HERE}", "-l:libmor_b200.so", "-Wl,-rpath,$ORIGIN"], check=True)
+    return OPS
 
 
 if __name__ == "__main__":

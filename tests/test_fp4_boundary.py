@@ -148,7 +148,7 @@ def test_gradient_of_nothing_is_refused(lib):
     assert lib.mor_expert_combine_grad(C.byref(moves()), 0x3000, 64, 0x4000, 64, None, 64, None, None) == INVALID
 
 
-def test_python_refusals():
+def test_python_refusals(lib):
     import torch
 
     from paper_2512_22804_b200 import experts, fp4
@@ -160,6 +160,12 @@ def test_python_refusals():
         fp4.quantize(x, "e2m1")
     with pytest.raises(ValueError, match="batch"):
         fp4.quantize(x[0], "e8m0_32")
+    with pytest.raises(TypeError):
+        fp4.quantize(x.half(), 7.5)
+    with pytest.raises(ValueError, match="codes"):
+        fp4.Operand(x.to(torch.uint8), x.to(torch.uint8), 5, 8, "e8m0_32", torch.ones(1))
+    with pytest.raises(TypeError, match="uint8"):
+        fp4.Operand(x, x, 4, 8, "e8m0_32", torch.ones(1))
     with pytest.raises(ValueError, match="int32"):
         experts.sort(torch.zeros(4, 2, dtype=torch.int64), 4)
     with pytest.raises(ValueError, match="n_in"):
