@@ -292,7 +292,7 @@ MOR_API mor_status_t mor_analyze_quantize_static(const mor_tensor_desc_t* host_d
  * element in the low half.
  *   E8M0_32  blocks of 32; a = max|x| of the block; e = floor(log2 a) - 2 held to -127..127; scale byte e + 127
  *            (0 for a block of zeros); code = E2M1(x * 2^-e).  tensor_scale is 1.
- *   E4M3_16  blocks of 16; A = max|x| of the tensor, at least 2^-88; t = fl32(A / 2688) is the tensor scale;
+ *   E4M3_16  blocks of 16; A = max|x| of the tensor, at least 2^-88; t = fl32(A * fl32(1 / 2688)) is the tensor scale;
  *            s = E4M3(fl32(448 a / A)), saturating, is the block scale; code = E2M1(fl32(x * fl32(1 / fl32(s t)))), zero
  *            where s is zero.  A value is fl32(fl32(code * s) * t).
  * NaN and infinities take part in no maximum; the scale byte of their block is NaN (0xFF, 0x7F) and its codes are

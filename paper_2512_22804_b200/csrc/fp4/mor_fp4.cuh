@@ -34,7 +34,7 @@ struct TensorScale {
 __device__ __forceinline__ TensorScale tensor_scale_of(float amax)
 {
     const float a = fmaxf(amax, 0x1p-88f);      // below 2^-88 the reciprocal of s * t could overflow
-    return {__fdiv_rn(a, 2688.0f), a * 0x1p-16f, __frcp_rn(a * 0x1p-16f)};
+    return {a * (1.0f / 2688.0f), a * 0x1p-16f, __frcp_rn(a * 0x1p-16f)};
 }
 // fl(448 a / A): the product with the rounded reciprocal, corrected once by its exact remainder, is the correctly rounded
 // quotient (P. Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor", 1990).  What exceeds

@@ -52,7 +52,7 @@ def quantize(x, fmt, amax=None):
     else:
         top = mag.max(initial=0) if amax is None else amax
         top = max(F(top), F(2.0 ** -88))
-        t = F(top) / F(2688)
+        t = F(top) * (F(1) / F(2688))
         s = (a.astype(F) * F(448 / 65536)) / (F(top) * F(2.0 ** -16))
         code = nearest_even(np.minimum(s, F(448)).astype(np.float64), E4M3[:127]).astype(np.uint8)
         byte = np.where(bad, 127, code).astype(np.uint8)
