@@ -388,11 +388,12 @@ MOR_API mor_status_t mor_expert_sort(const int32_t* ids, int64_t n_slots, int ex
 typedef struct mor_expert_desc {
     int64_t tokens, rows, hidden;  /* rows = mor_expert_rows()                                */
     int32_t top;
-    int32_t dtype;                 /* mor_dtype_t of every matrix                             */
+    int32_t dtype;                 /* mor_dtype_t of every matrix but ys                      */
     const int32_t* row_of_slot;    /* DEVICE [tokens * top]                                   */
     const int32_t* slot_of_row;    /* DEVICE [rows]                                           */
     const void* weight;            /* DEVICE [tokens * top], optional (NULL = 1)              */
     int32_t weight_dtype;          /* mor_dtype_t                                             */
+    int32_t ys_dtype;              /* mor_dtype_t of ys: dtype, or FP32 beside BF16           */
 } mor_expert_desc_t;
 
 /* out[row] = weight[slot] * x[token] for every row with a slot, zero for the others (products in binary32, one rounding). */

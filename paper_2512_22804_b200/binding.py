@@ -100,7 +100,7 @@ class mor_fp4_matmul_desc_t(C.Structure):
 
 class mor_expert_desc_t(C.Structure):
     _fields_ = [("tokens", C.c_int64), ("rows", C.c_int64), ("hidden", C.c_int64), ("top", C.c_int32), ("dtype", C.c_int32),
-                ("row_of_slot", C.c_void_p), ("slot_of_row", C.c_void_p), ("weight", C.c_void_p), ("weight_dtype", C.c_int32)]
+                ("row_of_slot", C.c_void_p), ("slot_of_row", C.c_void_p), ("weight", C.c_void_p), ("weight_dtype", C.c_int32), ("ys_dtype", C.c_int32)]
 
 
 BLOCK_STATS_DTYPE = np.dtype([("amax", "f4"), ("min_abs_nz", "f4"), ("nnz", "u4"), ("n_nonfinite", "u4"),

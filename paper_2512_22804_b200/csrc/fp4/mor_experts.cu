@@ -222,11 +222,12 @@ template <typename T, int BYTES> __global__ void __launch_bounds__(256) expert_g
     }
 }
 
-template <typename T, int BYTES> __global__ void __launch_bounds__(256) expert_combine_kernel(const __grid_constant__ MoveParams p)
+template <typename T, typename R, int BYTES> __global__ void __launch_bounds__(256) expert_combine_kernel(const __grid_constant__ MoveParams p)
 {
     using P = Piece<T, BYTES>;
+    using Q = Piece<R, BYTES / (int)sizeof(T) * (int)sizeof(R)>;
     const int64_t token = blockIdx.x;
-    const T* ys = static_cast<const T*>(p.rows_in);
+    const R* ys = static_cast<const R*>(p.rows_in);
     T* out = static_cast<T*>(p.out) + token * p.ld_out;
     for (int64_t c = (int64_t)threadIdx.x * P::kElems; c < p.hidden; c += (int64_t)blockDim.x * P::kElems) {
         float sum[P::kElems];
@@ -234,7 +235,7 @@ template <typename T, int BYTES> __global__ void __launch_bounds__(256) expert_c
         for (float& s : sum) s = 0.f;
         for (uint32_t j0 = 0; j0 < p.top; j0 += kAtOnce) {
             const Slots s(p, token, j0);
-            P v[kAtOnce];
+            Q v[kAtOnce];
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j) {
                 v[j].clear();
@@ -254,9 +255,10 @@ template <typename T, int BYTES> __global__ void __launch_bounds__(256) expert_c
 // The sums over hidden of <dy, ys> are taken per thread in column order, then over the CTA in a fixed tree: the result
 // does not change from run to run.  Four CTAs an SM (64 registers): with the 118 that the compiler would take, two, and not enough
 // rows are in flight.
-template <typename T, int BYTES> __global__ void __launch_bounds__(256, 4) expert_grad_kernel(const __grid_constant__ MoveParams p)
+template <typename T, typename R, int BYTES> __global__ void __launch_bounds__(256, 4) expert_grad_kernel(const __grid_constant__ MoveParams p)
 {
     using P = Piece<T, BYTES>;
+    using Q = Piece<R, BYTES / (int)sizeof(T) * (int)sizeof(R)>;
     T* out = static_cast<T*>(p.out);
     if (blockIdx.x < p.clear_blocks) {
         clear_rows<T, BYTES>(p, out, blockIdx.x);
@@ -265,7 +267,7 @@ template <typename T, int BYTES> __global__ void __launch_bounds__(256, 4) exper
     __shared__ float part[kAtOnce][8];
     const int64_t token = blockIdx.x - p.clear_blocks;
     const T* dy = static_cast<const T*>(p.tokens_in) + token * p.ld_token;
-    const T* ys = static_cast<const T*>(p.rows_in);
+    const R* ys = static_cast<const R*>(p.rows_in);
     const int warps = blockDim.x >> 5;
     for (uint32_t j0 = 0; j0 < p.top; j0 += kAtOnce) {
         const Slots s(p, token, j0);
@@ -273,7 +275,8 @@ template <typename T, int BYTES> __global__ void __launch_bounds__(256, 4) exper
 #pragma unroll
         for (float& d : dot) d = 0.f;
         for (int64_t c = (int64_t)threadIdx.x * P::kElems; c < p.hidden; c += (int64_t)blockDim.x * P::kElems) {
-            P g, v[kAtOnce];
+            P g;
+            Q v[kAtOnce];
             g.load(dy + c);
             if (p.dweight != nullptr) {
 #pragma unroll
@@ -318,27 +321,31 @@ template <typename T, int BYTES> __global__ void __launch_bounds__(256, 4) exper
 
 enum Move : int { MOVE_GATHER, MOVE_COMBINE, MOVE_GRAD };
 
-template <typename T, int BYTES> cudaError_t move_launch(const MoveParams& p, Move what, uint32_t grid, cudaStream_t st)
+template <typename T, typename R, int BYTES> cudaError_t move_launch(const MoveParams& p, Move what, uint32_t grid, cudaStream_t st)
 {
     const int64_t pieces = ceil_div(p.hidden, BYTES / (int64_t)sizeof(T));
     const uint32_t threads = pieces >= 256 ? 256u : (uint32_t)(ceil_div(pieces, 32) * 32);
-    if (what == MOVE_GATHER) return launch(expert_gather_kernel<T, BYTES>, grid, threads, 0, st, false, p);
-    if (what == MOVE_COMBINE) return launch(expert_combine_kernel<T, BYTES>, grid, threads, 0, st, false, p);
-    return launch(expert_grad_kernel<T, BYTES>, grid, threads, 0, st, false, p);
+    if constexpr (sizeof(T) == sizeof(R))
+        if (what == MOVE_GATHER) return launch(expert_gather_kernel<T, BYTES>, grid, threads, 0, st, false, p);
+    if (what == MOVE_COMBINE) return launch(expert_combine_kernel<T, R, BYTES>, grid, threads, 0, st, false, p);
+    return launch(expert_grad_kernel<T, R, BYTES>, grid, threads, 0, st, false, p);
 }
-template <typename T> cudaError_t move_access(const MoveParams& p, Move what, uint32_t grid, int access, cudaStream_t st)
+template <typename T, typename R> cudaError_t move_access(const MoveParams& p, Move what, uint32_t grid, int access, cudaStream_t st)
 {
-    // vector pieces must not run past a row: the width has to be a multiple too
+    // vector pieces must not run past a row: the width has to be a multiple too.  Beside rows of FP32 a token's piece is 16 bytes, so that
+    // the registers of four rows' pieces stay the same.
     const int64_t width = p.hidden * (int64_t)sizeof(T);
-    if (access == 32 && width % 32 == 0) return move_launch<T, 32>(p, what, grid, st);
-    if (access >= 16 && width % 16 == 0) return move_launch<T, 16>(p, what, grid, st);
-    return move_launch<T, (int)sizeof(T)>(p, what, grid, st);
+    if constexpr (sizeof(T) == sizeof(R))
+        if (access == 32 && width % 32 == 0) return move_launch<T, R, 32>(p, what, grid, st);
+    if (access >= 16 && width % 16 == 0) return move_launch<T, R, 16>(p, what, grid, st);
+    return move_launch<T, R, (int)sizeof(T)>(p, what, grid, st);
 }
 
 // Checks what all movers share and fills the parameters.
 mor_status_t move_params(const mor_expert_desc_t* d, MoveParams& p)
 {
-    if (d == nullptr || !is_dtype(d->dtype) || d->top < 1) return MOR_ERR_INVALID_ARG;
+    if (d == nullptr || !is_dtype(d->dtype) || !is_dtype(d->ys_dtype) || d->top < 1) return MOR_ERR_INVALID_ARG;
+    if (d->dtype == MOR_DTYPE_F32 && d->ys_dtype != MOR_DTYPE_F32) return MOR_ERR_INVALID_ARG;
     if (d->tokens < 0 || d->rows < 0 || d->hidden < 0 || d->tokens >= (1ll << 30) || d->rows >= (1ll << 31) || d->hidden >= (1ll << 31)) return MOR_ERR_INVALID_ARG;
     if (d->tokens * d->top >= (1ll << 30)) return MOR_ERR_INVALID_ARG;
     if (d->weight != nullptr && !is_dtype(d->weight_dtype)) return MOR_ERR_INVALID_ARG;
@@ -358,9 +365,9 @@ mor_status_t move_params(const mor_expert_desc_t* d, MoveParams& p)
 }
 
 // A matrix argument: pointer, pitch, alignment; `access` is narrowed to what it allows.
-mor_status_t check_rows(const void* m, int64_t rows, int64_t ld, const mor_expert_desc_t& d, int& access)
+mor_status_t check_rows(const void* m, int64_t rows, int64_t ld, const mor_expert_desc_t& d, int dtype, int& access)
 {
-    const int es = (int)dtype_bytes(d.dtype);
+    const int es = (int)dtype_bytes(dtype);
     if (ld < d.hidden || (rows > 0 && d.hidden > 0 && m == nullptr)) return MOR_ERR_INVALID_ARG;
     if (!is_aligned(m, es)) return MOR_ERR_ALIGNMENT;
     const int a = access_bytes(m, ld * es, 0, es);
@@ -372,7 +379,10 @@ mor_status_t move_run(const mor_expert_desc_t& d, const MoveParams& p, Move what
 {
     if (grid == 0 || p.hidden == 0) return MOR_OK;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    const cudaError_t e = d.dtype == MOR_DTYPE_BF16 ? move_access<__nv_bfloat16>(p, what, grid, access, st) : move_access<float>(p, what, grid, access, st);
+    const bool mixed = what != MOVE_GATHER && d.dtype == MOR_DTYPE_BF16 && d.ys_dtype == MOR_DTYPE_F32;
+    const cudaError_t e = mixed                       ? move_access<__nv_bfloat16, float>(p, what, grid, access, st)
+                          : d.dtype == MOR_DTYPE_BF16 ? move_access<__nv_bfloat16, __nv_bfloat16>(p, what, grid, access, st)
+                                                      : move_access<float, float>(p, what, grid, access, st);
     return e == cudaSuccess ? MOR_OK : MOR_ERR_CUDA;
 }
 
@@ -443,8 +453,8 @@ mor_status_t mor_expert_gather(const mor_expert_desc_t* host_desc, const void* x
     mor_status_t s = move_params(host_desc, p);
     if (s != MOR_OK) return s;
     int access = 32;
-    if ((s = check_rows(x, p.tokens, ldx, *host_desc, access)) != MOR_OK) return s;
-    if ((s = check_rows(out, p.rows, ldo, *host_desc, access)) != MOR_OK) return s;
+    if ((s = check_rows(x, p.tokens, ldx, *host_desc, host_desc->dtype, access)) != MOR_OK) return s;
+    if ((s = check_rows(out, p.rows, ldo, *host_desc, host_desc->dtype, access)) != MOR_OK) return s;
     p.tokens_in = x;
     p.ld_token = ldx;
     p.out = out;
@@ -459,8 +469,8 @@ mor_status_t mor_expert_combine(const mor_expert_desc_t* host_desc, const void* 
     mor_status_t s = move_params(host_desc, p);
     if (s != MOR_OK) return s;
     int access = 32;
-    if ((s = check_rows(ys, p.rows, ldy, *host_desc, access)) != MOR_OK) return s;
-    if ((s = check_rows(out, p.tokens, ldo, *host_desc, access)) != MOR_OK) return s;
+    if ((s = check_rows(ys, p.rows, ldy, *host_desc, host_desc->ys_dtype, access)) != MOR_OK) return s;
+    if ((s = check_rows(out, p.tokens, ldo, *host_desc, host_desc->dtype, access)) != MOR_OK) return s;
     p.rows_in = ys;
     p.ld_row = ldy;
     p.out = out;
@@ -478,9 +488,9 @@ mor_status_t mor_expert_combine_grad(const mor_expert_desc_t* host_desc, const v
     if (dweight != nullptr && !is_dtype(host_desc->weight_dtype)) return MOR_ERR_INVALID_ARG;
     if (dweight != nullptr && !is_aligned(dweight, dtype_bytes(host_desc->weight_dtype))) return MOR_ERR_ALIGNMENT;
     int access = 32;
-    if ((s = check_rows(dy, p.tokens, lddy, *host_desc, access)) != MOR_OK) return s;
-    if (dweight != nullptr && (s = check_rows(ys, p.rows, ldy, *host_desc, access)) != MOR_OK) return s;
-    if (dys != nullptr && (s = check_rows(dys, p.rows, lddys, *host_desc, access)) != MOR_OK) return s;
+    if ((s = check_rows(dy, p.tokens, lddy, *host_desc, host_desc->dtype, access)) != MOR_OK) return s;
+    if (dweight != nullptr && (s = check_rows(ys, p.rows, ldy, *host_desc, host_desc->ys_dtype, access)) != MOR_OK) return s;
+    if (dys != nullptr && (s = check_rows(dys, p.rows, lddys, *host_desc, host_desc->dtype, access)) != MOR_OK) return s;
     p.tokens_in = dy;
     p.ld_token = lddy;
     p.rows_in = ys;

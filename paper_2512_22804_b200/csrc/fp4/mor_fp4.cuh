@@ -188,8 +188,10 @@ template <typename T, int BYTES> struct Piece {
     uint32_t w[kWords];
     __device__ __forceinline__ void load(const T* p)
     {
-        if constexpr (BYTES == 32) ldg256(w, p);
-        else if constexpr (BYTES == 16) {
+        if constexpr (BYTES >= 32) {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 8) ldg256(w + i, reinterpret_cast<const uint32_t*>(p) + i);
+        } else if constexpr (BYTES == 16) {
             const uint4 q = *reinterpret_cast<const uint4*>(p);
             w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
         } else if constexpr (BYTES == 4) w[0] = *reinterpret_cast<const uint32_t*>(p);
@@ -197,8 +199,10 @@ template <typename T, int BYTES> struct Piece {
     }
     __device__ __forceinline__ void store(T* p) const
     {
-        if constexpr (BYTES == 32) stg256(p, w);
-        else if constexpr (BYTES == 16) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        if constexpr (BYTES >= 32) {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 8) stg256(reinterpret_cast<uint32_t*>(p) + i, w + i);
+        } else if constexpr (BYTES == 16) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
         else if constexpr (BYTES == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
         else *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
     }

@@ -269,7 +269,7 @@ mor_expert_desc_t expert_desc(const Routes& p, const Tensor& m, const std::optio
     d.rows = p.rows();
     d.hidden = m.size(1);
     d.top = (int32_t)p.top;
-    d.dtype = dtype_of(m.scalar_type(), what);
+    d.dtype = d.ys_dtype = dtype_of(m.scalar_type(), what);
     d.row_of_slot = ptr<int32_t>(p.row);
     d.slot_of_row = ptr<int32_t>(p.slot);
     if (weight) {
@@ -288,20 +288,23 @@ Tensor gather(const Tensor& x, const Routes& p, const std::optional<Tensor>& wei
     check(mor_expert_gather(&d, x.data_ptr(), ld(x), out.data_ptr(), x.size(1), stream()), "mor_expert_gather");
     return out;
 }
-Tensor combine(const Tensor& ys, const Routes& p, const std::optional<Tensor>& weight)
+Tensor combine(const Tensor& ys, const Routes& p, const std::optional<Tensor>& weight, at::ScalarType type)
 {
-    const mor_expert_desc_t d = expert_desc(p, ys, weight, "ys");
+    mor_expert_desc_t d = expert_desc(p, ys, weight, "ys");
+    d.dtype = dtype_of(type, "out_dtype");
+    want(d.dtype == d.ys_dtype || d.ys_dtype == MOR_DTYPE_F32, "out_dtype: ys's type, or BF16 from FP32, is wanted");
     want(ys.size(0) == p.rows(), "ys: the plan's rows are wanted");
-    const Tensor out = at::empty({p.tokens(), ys.size(1)}, ys.options().requires_grad(false));
+    const Tensor out = at::empty({p.tokens(), ys.size(1)}, ys.options().dtype(type).requires_grad(false));
     check(mor_expert_combine(&d, ys.data_ptr(), ld(ys), out.data_ptr(), ys.size(1), stream()), "mor_expert_combine");
     return out;
 }
 std::pair<std::optional<Tensor>, Tensor> combine_grad(const Tensor& dy, const Tensor& ys, const Routes& p, const Tensor& weight, bool rows)
 {
-    const mor_expert_desc_t d = expert_desc(p, dy, weight, "dy");
+    mor_expert_desc_t d = expert_desc(p, dy, weight, "dy");
+    d.ys_dtype = dtype_of(ys.scalar_type(), "ys");
     on_gpu(ys, "ys");
-    want(dy.size(0) == p.tokens() && ys.dim() == 2 && ys.size(0) == p.rows() && ys.size(1) == dy.size(1) && ys.scalar_type() == dy.scalar_type(),
-         "dy: [tokens, hidden] and ys: [plan rows, hidden] of one type are wanted");
+    want(dy.size(0) == p.tokens() && ys.dim() == 2 && ys.size(0) == p.rows() && ys.size(1) == dy.size(1) && (d.ys_dtype == d.dtype || d.ys_dtype == MOR_DTYPE_F32),
+         "dy: [tokens, hidden] and ys: [plan rows, hidden] of its type or FP32 are wanted");
     rows_contiguous(ys, "ys");
     std::optional<Tensor> dys;
     if (rows) dys = at::empty({p.rows(), dy.size(1)}, dy.options().requires_grad(false));
@@ -356,12 +359,14 @@ Tensor linear(const Tensor& x, const Tensor& w, const py::handle& format)
     return y.reshape(shape);
 }
 
+// The experts' rows stay in 32 bits until they are combined: rounded to BF16 they would halve what is written and read, but the sum
+// and above all the weights' gradient (a dot product with them) would be up to half again as far off as the rounding of their result.
 Tensor expert_forward(const Tensor& x, const Matrix& w, const Routes& plan, const Tensor& weight, bool cols, Tensor* ys, Tensor* a_t)
 {
     const Pair a = quantize_(x, w.c.format, true, cols, std::nullopt, &plan, std::nullopt);
-    *ys = matmul_rows_(*a.rows, w, plan, x.scalar_type());
+    *ys = matmul_rows_(*a.rows, w, plan, at::kFloat);
     if (cols) *a_t = a.cols->buf;
-    return combine(*ys, plan, weight);
+    return combine(*ys, plan, weight, x.scalar_type());
 }
 
 struct ExpertFn : torch::autograd::Function<ExpertFn> {
@@ -395,7 +400,7 @@ struct ExpertFn : torch::autograd::Function<ExpertFn> {
         if (need_weight) dweight = combine_grad(dy, ctx->saved_data["ys"].toTensor(), plan, weight, false).second;
         if (need_x || need_w) {
             const Pair g = quantize_(dy, format, need_x, need_w, std::nullopt, &plan, weight);
-            if (need_x) dx = combine(matmul_rows_(*g.rows, Matrix::over(ctx->saved_data["b"].toTensor(), e, k, n, format), plan, (at::ScalarType)s[4]), plan, std::nullopt);
+            if (need_x) dx = combine(matmul_rows_(*g.rows, Matrix::over(ctx->saved_data["b"].toTensor(), e, k, n, format), plan, (at::ScalarType)s[4]), plan, std::nullopt, (at::ScalarType)s[4]);
             if (need_w) dw = matmul_reduce_(*g.cols, Matrix::over(ctx->saved_data["a"].toTensor(), 1, k, plan.rows(), format), plan, (at::ScalarType)s[5]);
         }
         return {dx, dw, Tensor(), dweight, Tensor(), Tensor(), Tensor(), Tensor()};
@@ -460,7 +465,9 @@ PYBIND11_MODULE(_ops, m)
     m.def("status_word", [](const Tensor& like) { return status_word(like); });
     m.def("sort", &sort_slots, py::arg("ids"), py::arg("n_experts"), py::arg("align") = 1);
     m.def("gather", &gather, py::arg("x"), py::arg("plan"), py::arg("weight") = py::none());
-    m.def("combine", &combine, py::arg("ys"), py::arg("plan"), py::arg("weight") = py::none());
+    m.def("combine", [](const Tensor& ys, const Routes& p, const optional<Tensor>& w, const py::object& t) {
+        return combine(ys, p, w, t.is_none() ? ys.scalar_type() : t.cast<at::ScalarType>());
+    }, py::arg("ys"), py::arg("plan"), py::arg("weight") = py::none(), py::arg("out_dtype") = py::none());
     m.def("combine_grad", &combine_grad, py::arg("dy"), py::arg("ys"), py::arg("plan"), py::arg("weight"), py::kw_only(), py::arg("rows") = true);
     m.def("expert_linear", &expert_linear, py::arg("x"), py::arg("w"), py::arg("ids"), py::arg("weight"), py::arg("format") = py::none());
 }

@@ -10,10 +10,11 @@
     each expert's first row a multiple of align.
 ``gather(x, plan, weight=None)``
     [plan rows, hidden]: each row the token row of its slot, times weight [tokens, top] if given; zero where it has no slot.
-``combine(ys, plan, weight=None)``
-    [tokens, hidden]: the sum over each token's slots of weight (1 if not given) times the slot's row of ys.
+``combine(ys, plan, weight=None, out_dtype=None)``
+    [tokens, hidden]: the sum over each token's slots of weight (1 if not given) times the slot's row of ys, in ys's type or, from FP32, in
+    BF16.
 ``combine_grad(dy, ys, plan, weight, *, rows=True)``
-    (dys or None, dweight): the gradients of combine(ys, plan, weight) for dy.
+    (dys or None, dweight): the gradients of combine(ys, plan, weight) for dy; ys in dy's type or FP32.
 ``linear(x, w, ids, weight, format=None)``
     y[t] = sum over j of weight[t, j] * Q(x[t]) Q(w[ids[t, j]])^T for x [tokens, n_in].  w is a tensor [experts, n_out, n_in]
     (differentiable in x, w and weight; the rounding is passed straight through) or, for serving, a stored stack (``fp4.Operand`` with one

@@ -136,6 +136,7 @@ def moves(**kw):
     (moves(row_of_slot=None), 0x3000, 64, 0x4000, 64, INVALID), (moves(slot_of_row=None), 0x3000, 64, 0x4000, 64, INVALID),
     (moves(weight=0x5000, weight_dtype=9), 0x3000, 64, 0x4000, 64, INVALID), (moves(weight=0x5001), 0x3000, 64, 0x4000, 64, ALIGN),
     (moves(), 0x3000, 63, 0x4000, 64, INVALID), (moves(), None, 64, 0x4000, 64, INVALID), (moves(), 0x3001, 64, 0x4000, 64, ALIGN),
+    (moves(ys_dtype=3), 0x3000, 64, 0x4000, 64, INVALID), (moves(dtype=1, ys_dtype=0), 0x3000, 64, 0x4000, 64, INVALID),
     (moves(), 0x3000, 64, 0x4000, 1, INVALID), (moves(), 0x3000, 64, None, 64, INVALID)])
 def test_movers_refuse(lib, d, x, ldx, out, ldo, want):
     assert lib.mor_expert_gather(C.byref(d), x, ldx, out, ldo, None) == want

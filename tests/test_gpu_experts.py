@@ -127,6 +127,26 @@ def test_gather_combine_and_gradient(experts, tokens, top, n, hidden, align, wei
     assert none is None and torch.equal(again, dw)
 
 
+@pytest.mark.parametrize("tokens,top,n,hidden", [(37, 2, 5, 1), (100, 3, 9, 33), (300, 5, 64, 520)])
+def test_rows_of_32_bits_beside_tokens_of_16(experts, tokens, top, n, hidden):
+    import torch
+
+    plan, row, slot, matrix = matrices(experts, tokens, top, n, hidden, 128, "bf16", tokens)
+    dy, tdy = matrix(tokens)
+    rng = np.random.default_rng(4)
+    ys = rng.standard_normal((len(slot), hidden)).astype(np.float32)
+    w = rng.random((tokens, top)).astype(np.float32)
+    tys, tw = cuda(ys), cuda(w)
+    taken = np.where((row >= 0)[..., None], ys.astype(np.float64)[np.maximum(row, 0)], 0.0)
+    want, room = (taken * w[..., None]).sum(1), top * 2.0 ** -24 * (np.abs(taken) * w[..., None]).sum(1)
+    y = experts.combine(tys, plan, tw, torch.bfloat16).float().cpu().numpy()
+    assert (plain.bf16((want - room).astype(np.float32)) <= y).all() and (y <= plain.bf16((want + room).astype(np.float32))).all()
+    dys, dw = experts.combine_grad(tdy, tys, plan, tw)
+    terms = taken * dy.astype(np.float64)[:, None, :]
+    assert (np.abs(dw.double().cpu().numpy() - terms.sum(-1)) <= hidden * 2.0 ** -24 * np.abs(terms).sum(-1)).all()
+    assert dys.dtype == torch.bfloat16 and torch.equal(dys, experts.gather(tdy, plan, tw))
+
+
 def test_nan_of_an_empty_row_goes_nowhere_and_strides(experts):
     import torch
 
@@ -172,9 +192,9 @@ def test_quantised_gather_equals_gather_then_quantise(experts, fmt, weighted):
 @pytest.mark.parametrize("fmt", ["e4m3_16", "e8m0_32"])
 @pytest.mark.parametrize("tokens,top,n,k,m", [(1, 2, 8, 64, 40), (50, 3, 6, 300, 136), (400, 2, 4, 257, 264)])
 def test_expert_layer_and_its_gradient(experts, fmt, tokens, top, n, k, m):
-    """Against the formula on quantised values, in 64 bits.  The rows of the product are rounded to BF16 (at most 2^-8)
-    before they are combined, the result once more: 2^-7 of the sum of magnitudes covers both (the sums' own 2^-16 beside what the
-    products of both roundings leave)."""
+    """Against the formula on quantised values, in 64 bits.  The rows of the gradient's product are rounded to BF16 (at
+    most 2^-8) before they are added, every result once: 2^-7 of the sum of magnitudes covers both (the sums' own 2^-16 beside what
+    the products of both roundings leave)."""
     import torch
 
     from paper_2512_22804_b200 import fp4
