@@ -109,8 +109,38 @@ __device__ __forceinline__ uint32_t e2m1x8(const float* v, float q)
     return r;
 }
 
-// Codes (16 bytes) and scale bytes (low byte first) of one unit, given the largest magnitude of each of its blocks.
-template <int FMT> __device__ __forceinline__ uint4 quantise_unit(const float* v, const float* a, const TensorScale& ts, const float* factors, uint32_t& scales)
+// The same for eight BF16 values.  They are widened by the mixed-precision subtract x - 0 (keeps -0), which runs beside the integer
+// pipe that shifts and masks would add to, the pipe that bounds these kernels.
+__device__ __forceinline__ uint32_t e2m1x8(const uint16_t* h, float q)
+{
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) asm("sub.f32.bf16 %0, %1, %2;" : "=f"(v[i]) : "h"(h[i]), "f"(0.0f));
+    return e2m1x8(v, q);
+}
+// Eight E2M1 codes of BF16 values times a power of two, widened and multiplied in one instruction each (the sum with -0 keeps
+// the sign of a zero).
+__device__ __forceinline__ uint32_t e2m1x8_power(const uint16_t* h, uint16_t q)
+{
+    uint32_t r;
+    asm("{ .reg .b8 b0, b1, b2, b3;\n"
+        ".reg .f32 x0, x1, x2, x3, x4, x5, x6, x7;\n"
+        "fma.rn.f32.bf16 x0, %1, %9, %10;\nfma.rn.f32.bf16 x1, %2, %9, %10;\nfma.rn.f32.bf16 x2, %3, %9, %10;\nfma.rn.f32.bf16 x3, %4, %9, %10;\n"
+        "fma.rn.f32.bf16 x4, %5, %9, %10;\nfma.rn.f32.bf16 x5, %6, %9, %10;\nfma.rn.f32.bf16 x6, %7, %9, %10;\nfma.rn.f32.bf16 x7, %8, %9, %10;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b0, x1, x0;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b1, x3, x2;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b2, x5, x4;\n"
+        "cvt.rn.satfinite.e2m1x2.f32 b3, x7, x6;\n"
+        "mov.b32 %0, {b0, b1, b2, b3}; }"
+        : "=r"(r)
+        : "h"(h[0]), "h"(h[1]), "h"(h[2]), "h"(h[3]), "h"(h[4]), "h"(h[5]), "h"(h[6]), "h"(h[7]), "h"(q), "f"(-0.0f));
+    return r;
+}
+__device__ __forceinline__ uint32_t e2m1x8_power(const float* v, uint16_t q) { return e2m1x8(v, __uint_as_float((uint32_t)q << 16)); }
+
+// Codes (16 bytes) and scale bytes (low byte first) of one unit (FP32 or BF16 values), given the largest magnitude of each of its
+// blocks.
+template <int FMT, typename V> __device__ __forceinline__ uint4 quantise_unit(const V* v, const float* a, const TensorScale& ts, const float* factors, uint32_t& scales)
 {
     uint4 c;
     if constexpr (FMT == MOR_FP4_E8M0_32) {
@@ -118,9 +148,9 @@ template <int FMT> __device__ __forceinline__ uint4 quantise_unit(const float* v
         // floor(log2 a) - 2 with a bias of 127 is the exponent field less two; the fields 0 (subnormal or zero), 1 and 2 meet
         // the bound at 0
         const int byte = max((int)(__float_as_uint(a[0]) >> 23) - 2, 0);
-        const float q = __uint_as_float((uint32_t)(254 - byte) << 23);
+        const uint16_t q = (uint16_t)((254 - byte) << 7);           // 2^-e as a BF16
         scales = bad ? 0xFFu : (uint32_t)byte;
-        c = make_uint4(e2m1x8(v, q), e2m1x8(v + 8, q), e2m1x8(v + 16, q), e2m1x8(v + 24, q));
+        c = make_uint4(e2m1x8_power(v, q), e2m1x8_power(v + 8, q), e2m1x8_power(v + 16, q), e2m1x8_power(v + 24, q));
         if (bad) c = make_uint4(0, 0, 0, 0);
     } else {
         const bool bad0 = !(a[0] < INFINITY), bad1 = !(a[1] < INFINITY);
@@ -155,6 +185,9 @@ __device__ __forceinline__ float2 e2m1x2_value(uint32_t byte)
     asm("{ .reg .b8 b, z0, z1, z2; mov.b32 {b, z0, z1, z2}, %1; cvt.rn.f16x2.e2m1x2 %0, b; }" : "=r"(h) : "r"(byte));
     return __half22float2(*reinterpret_cast<__half2*>(&h));
 }
+
+__device__ __forceinline__ uint16_t low_half(uint32_t w) { return (uint16_t)w; }
+__device__ __forceinline__ uint16_t high_half(uint32_t w) { return (uint16_t)(w >> 16); }
 
 // ---- vector accesses: 32 bytes (one sector) per thread, 16 bytes, or one element
 

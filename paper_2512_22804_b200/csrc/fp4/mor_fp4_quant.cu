@@ -290,8 +290,14 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED 
     for (int i = 0; i < 2; ++i) {
         const int at = tid + i * kQThreads, lrow = at >> 2, u = at & 3;
         const int64_t row = (int64_t)row_tile * 128 + lrow, col = (int64_t)col_tile * 128 + u * kUnit;
-        float v[kUnit];
-        unpack<T>(raw[i], v);
+        using V = std::conditional_t<kNarrow, uint16_t, float>;             // BF16 as it came, or FP32
+        V v[kUnit];
+        if constexpr (kNarrow) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) { v[2 * j] = low_half(raw[i].w[j]); v[2 * j + 1] = high_half(raw[i].w[j]); }
+        } else {
+            unpack<T>(raw[i], v);
+        }
         if constexpr (MODE == WEIGHTED) {
 #pragma unroll
             for (float& e : v) e *= weight[i];
@@ -332,7 +338,7 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED 
     }
     if constexpr (COLS) {
         uint8_t* stage = dyn + 128 * kPitch;
-        auto put = [&](int lcol, int u, const float* v, const float* a) {
+        auto put = [&](int lcol, int u, const auto* v, const float* a) {
             uint32_t scales;
             const uint4 codes = quantise_unit<FMT>(v, a, ts, factors, scales);
             *reinterpret_cast<uint4*>(stage + stage_at(lcol, u)) = codes;
@@ -346,7 +352,8 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED 
             const uint8_t* from[2] = {dyn + u * kUnit * kPitch + L::chunk(0, pair >> 2) * 16 + (pair & 3) * 4,
                                       dyn + u * kUnit * kPitch + L::chunk(1, pair >> 2) * 16 + (pair & 3) * 4};
             uint32_t w[kUnit], m[kPerUnit];
-            float v[kUnit], a[kPerUnit];
+            uint16_t v[kUnit];
+            float a[kPerUnit];
 #pragma unroll
             for (int i = 0; i < kUnit; ++i) w[i] = *reinterpret_cast<const uint32_t*>(from[i & 1] + i * kPitch);
 #pragma unroll
@@ -354,12 +361,12 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED 
 #pragma unroll
             for (int k = 0; k < kPerUnit; ++k) a[k] = fabsf(bf16_low(m[k]));
 #pragma unroll
-            for (int i = 0; i < kUnit; ++i) v[i] = bf16_low(w[i]);
+            for (int i = 0; i < kUnit; ++i) v[i] = low_half(w[i]);
             put(2 * pair, u, v, a);
 #pragma unroll
             for (int k = 0; k < kPerUnit; ++k) a[k] = fabsf(bf16_high(m[k]));
 #pragma unroll
-            for (int i = 0; i < kUnit; ++i) v[i] = bf16_high(w[i]);
+            for (int i = 0; i < kUnit; ++i) v[i] = high_half(w[i]);
             put(2 * pair + 1, u, v, a);
         } else {
 #pragma unroll 1
