@@ -109,59 +109,86 @@ __device__ __forceinline__ uint32_t e2m1x8(const float* v, float q)
     return r;
 }
 
-// The same for eight BF16 values.  They are widened by the mixed-precision subtract x - 0 (keeps -0), which runs beside the integer
-// pipe that shifts and masks would add to, the pipe that bounds these kernels.
-__device__ __forceinline__ uint32_t e2m1x8(const uint16_t* h, float q)
-{
-    float v[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) asm("sub.f32.bf16 %0, %1, %2;" : "=f"(v[i]) : "h"(h[i]), "f"(0.0f));
-    return e2m1x8(v, q);
-}
-// Eight E2M1 codes of BF16 values times a power of two, widened and multiplied in one instruction each (the sum with -0 keeps
-// the sign of a zero).
-__device__ __forceinline__ uint32_t e2m1x8_power(const uint16_t* h, uint16_t q)
+// The same for BF16 values where they lie in words, without taking the halves apart first (that costs an integer instruction per
+// element, and the integer pipe is what bounds these kernels): PAIRS, the two halves of four words one after the other;
+// LOW or HIGH, that half of eight words.  Widened by the mixed-precision subtract x - 0 (keeps -0), multiplied in pairs, cast in
+// pairs: two instructions per element.
+enum Halves : int { PAIRS = 0, LOW = 1, HIGH = 2 };
+#define MOR_TAKE_PAIRS                                                                                                                \
+    "mov.b32 {h0, h1}, %1;\nmov.b32 {h2, h3}, %2;\nmov.b32 {h4, h5}, %3;\nmov.b32 {h6, h7}, %4;\n"
+#define MOR_TAKE_LOW                                                                                                                  \
+    "mov.b32 {h0, g}, %1;\nmov.b32 {h1, g}, %2;\nmov.b32 {h2, g}, %3;\nmov.b32 {h3, g}, %4;\n"                                      \
+    "mov.b32 {h4, g}, %5;\nmov.b32 {h5, g}, %6;\nmov.b32 {h6, g}, %7;\nmov.b32 {h7, g}, %8;\n"
+#define MOR_TAKE_HIGH                                                                                                                 \
+    "mov.b32 {g, h0}, %1;\nmov.b32 {g, h1}, %2;\nmov.b32 {g, h2}, %3;\nmov.b32 {g, h3}, %4;\n"                                      \
+    "mov.b32 {g, h4}, %5;\nmov.b32 {g, h5}, %6;\nmov.b32 {g, h6}, %7;\nmov.b32 {g, h7}, %8;\n"
+#define MOR_REGS ".reg .b8 b0, b1, b2, b3;\n.reg .b16 h0, h1, h2, h3, h4, h5, h6, h7, g;\n.reg .f32 x0, x1, x2, x3, x4, x5, x6, x7;\n"
+#define MOR_CAST                                                                                                                      \
+    "cvt.rn.satfinite.e2m1x2.f32 b0, x1, x0;\ncvt.rn.satfinite.e2m1x2.f32 b1, x3, x2;\n"                                             \
+    "cvt.rn.satfinite.e2m1x2.f32 b2, x5, x4;\ncvt.rn.satfinite.e2m1x2.f32 b3, x7, x6;\nmov.b32 %0, {b0, b1, b2, b3}; }"
+#define MOR_WIDEN                                                                                                                     \
+    ".reg .b64 q, p0, p1, p2, p3;\nmov.b64 q, {%9, %9};\n"                                                                           \
+    "sub.f32.bf16 x0, h0, %10;\nsub.f32.bf16 x1, h1, %10;\nsub.f32.bf16 x2, h2, %10;\nsub.f32.bf16 x3, h3, %10;\n"                  \
+    "sub.f32.bf16 x4, h4, %10;\nsub.f32.bf16 x5, h5, %10;\nsub.f32.bf16 x6, h6, %10;\nsub.f32.bf16 x7, h7, %10;\n"                  \
+    "mov.b64 p0, {x0, x1};\nmov.b64 p1, {x2, x3};\nmov.b64 p2, {x4, x5};\nmov.b64 p3, {x6, x7};\n"                                  \
+    "mul.rn.f32x2 p0, p0, q;\nmul.rn.f32x2 p1, p1, q;\nmul.rn.f32x2 p2, p2, q;\nmul.rn.f32x2 p3, p3, q;\n"                          \
+    "mov.b64 {x0, x1}, p0;\nmov.b64 {x2, x3}, p1;\nmov.b64 {x4, x5}, p2;\nmov.b64 {x6, x7}, p3;\n"
+template <int WHICH> __device__ __forceinline__ uint32_t e2m1x8_of(const uint32_t* w, float q)
 {
     uint32_t r;
-    asm("{ .reg .b8 b0, b1, b2, b3;\n"
-        ".reg .f32 x0, x1, x2, x3, x4, x5, x6, x7;\n"
-        "fma.rn.f32.bf16 x0, %1, %9, %10;\nfma.rn.f32.bf16 x1, %2, %9, %10;\nfma.rn.f32.bf16 x2, %3, %9, %10;\nfma.rn.f32.bf16 x3, %4, %9, %10;\n"
-        "fma.rn.f32.bf16 x4, %5, %9, %10;\nfma.rn.f32.bf16 x5, %6, %9, %10;\nfma.rn.f32.bf16 x6, %7, %9, %10;\nfma.rn.f32.bf16 x7, %8, %9, %10;\n"
-        "cvt.rn.satfinite.e2m1x2.f32 b0, x1, x0;\n"
-        "cvt.rn.satfinite.e2m1x2.f32 b1, x3, x2;\n"
-        "cvt.rn.satfinite.e2m1x2.f32 b2, x5, x4;\n"
-        "cvt.rn.satfinite.e2m1x2.f32 b3, x7, x6;\n"
-        "mov.b32 %0, {b0, b1, b2, b3}; }"
-        : "=r"(r)
-        : "h"(h[0]), "h"(h[1]), "h"(h[2]), "h"(h[3]), "h"(h[4]), "h"(h[5]), "h"(h[6]), "h"(h[7]), "h"(q), "f"(-0.0f));
+    constexpr int k = WHICH == PAIRS ? 0 : 1;                         // PAIRS uses four words only
+#define MOR_ASM(TAKE)                                                                                                                 \
+    asm("{ " MOR_REGS TAKE MOR_WIDEN MOR_CAST                                                                                         \
+        : "=r"(r) : "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4 * k]), "r"(w[5 * k]), "r"(w[6 * k]), "r"(w[7 * k]), "f"(q), "f"(0.0f))
+    if constexpr (WHICH == PAIRS) MOR_ASM(MOR_TAKE_PAIRS);
+    else if constexpr (WHICH == LOW) MOR_ASM(MOR_TAKE_LOW);
+    else MOR_ASM(MOR_TAKE_HIGH);
     return r;
 }
-__device__ __forceinline__ uint32_t e2m1x8_power(const float* v, uint16_t q) { return e2m1x8(v, __uint_as_float((uint32_t)q << 16)); }
+#undef MOR_ASM
+#undef MOR_WIDEN
+#undef MOR_CAST
+#undef MOR_REGS
+#undef MOR_TAKE_HIGH
+#undef MOR_TAKE_LOW
+#undef MOR_TAKE_PAIRS
 
-// Codes (16 bytes) and scale bytes (low byte first) of one unit (FP32 or BF16 values), given the largest magnitude of each of its
-// blocks.
-template <int FMT, typename V> __device__ __forceinline__ uint4 quantise_unit(const V* v, const float* a, const TensorScale& ts, const float* factors, uint32_t& scales)
+// Where the 32 values of a unit are: FP32 registers, or BF16 in words.
+struct UnitF32 {
+    const float* v;
+    __device__ __forceinline__ uint32_t cast8(int i, float q) const { return e2m1x8(v + 8 * i, q); }
+};
+template <int WHICH> struct UnitBf16 {
+    const uint32_t* w;
+    __device__ __forceinline__ uint32_t cast8(int i, float q) const { return e2m1x8_of<WHICH>(w + (WHICH == PAIRS ? 4 : 8) * i, q); }
+};
+
+// Codes (16 bytes) and scale bytes (low byte first) of one unit, given the largest magnitude of each of its blocks.
+template <int FMT, typename U> __device__ __forceinline__ uint4 quantise_unit(const U& unit, const float* a, const TensorScale& ts, const float* factors, uint32_t& scales)
 {
-    uint4 c;
+    float q0, q1;
+    bool bad0, bad1;
     if constexpr (FMT == MOR_FP4_E8M0_32) {
-        const bool bad = !(a[0] < INFINITY);
+        bad0 = bad1 = !(a[0] < INFINITY);
         // floor(log2 a) - 2 with a bias of 127 is the exponent field less two; the fields 0 (subnormal or zero), 1 and 2 meet
         // the bound at 0
         const int byte = max((int)(__float_as_uint(a[0]) >> 23) - 2, 0);
-        const uint16_t q = (uint16_t)((254 - byte) << 7);           // 2^-e as a BF16
-        scales = bad ? 0xFFu : (uint32_t)byte;
-        c = make_uint4(e2m1x8_power(v, q), e2m1x8_power(v + 8, q), e2m1x8_power(v + 16, q), e2m1x8_power(v + 24, q));
-        if (bad) c = make_uint4(0, 0, 0, 0);
+        q0 = q1 = __uint_as_float((uint32_t)(254 - byte) << 23);
+        scales = bad0 ? 0xFFu : (uint32_t)byte;
     } else {
-        const bool bad0 = !(a[0] < INFINITY), bad1 = !(a[1] < INFINITY);
+        bad0 = !(a[0] < INFINITY);
+        bad1 = !(a[1] < INFINITY);
         uint16_t s;
         asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(s) : "f"(block_quotient(a[1], ts)), "f"(block_quotient(a[0], ts)));
         scales = s;
-        const float q0 = factors[s & 127], q1 = factors[(s >> 8) & 127];
-        c = make_uint4(e2m1x8(v, q0), e2m1x8(v + 8, q0), e2m1x8(v + 16, q1), e2m1x8(v + 24, q1));
-        if (bad0) { c.x = c.y = 0; scales = (scales & 0xFF00u) | 0x7Fu; }
-        if (bad1) { c.z = c.w = 0; scales = (scales & 0x00FFu) | 0x7F00u; }
+        q0 = factors[s & 127];
+        q1 = factors[(s >> 8) & 127];
+        if (bad0) scales = (scales & 0xFF00u) | 0x7Fu;
+        if (bad1) scales = (scales & 0x00FFu) | 0x7F00u;
     }
+    uint4 c = make_uint4(unit.cast8(0, q0), unit.cast8(1, q0), unit.cast8(2, q1), unit.cast8(3, q1));
+    if (bad0) c.x = c.y = 0;
+    if (bad1) c.z = c.w = 0;
     return c;
 }
 
@@ -185,9 +212,6 @@ __device__ __forceinline__ float2 e2m1x2_value(uint32_t byte)
     asm("{ .reg .b8 b, z0, z1, z2; mov.b32 {b, z0, z1, z2}, %1; cvt.rn.f16x2.e2m1x2 %0, b; }" : "=r"(h) : "r"(byte));
     return __half22float2(*reinterpret_cast<__half2*>(&h));
 }
-
-__device__ __forceinline__ uint16_t low_half(uint32_t w) { return (uint16_t)w; }
-__device__ __forceinline__ uint16_t high_half(uint32_t w) { return (uint16_t)(w >> 16); }
 
 // ---- vector accesses: 32 bytes (one sector) per thread, 16 bytes, or one element
 

@@ -290,14 +290,8 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED 
     for (int i = 0; i < 2; ++i) {
         const int at = tid + i * kQThreads, lrow = at >> 2, u = at & 3;
         const int64_t row = (int64_t)row_tile * 128 + lrow, col = (int64_t)col_tile * 128 + u * kUnit;
-        using V = std::conditional_t<kNarrow, uint16_t, float>;             // BF16 as it came, or FP32
-        V v[kUnit];
-        if constexpr (kNarrow) {
-#pragma unroll
-            for (int j = 0; j < 16; ++j) { v[2 * j] = low_half(raw[i].w[j]); v[2 * j + 1] = high_half(raw[i].w[j]); }
-        } else {
-            unpack<T>(raw[i], v);
-        }
+        float v[kNarrow ? 1 : kUnit];                                       // FP32, or BF16 as it came
+        if constexpr (!kNarrow) unpack<T>(raw[i], v);
         if constexpr (MODE == WEIGHTED) {
 #pragma unroll
             for (float& e : v) e *= weight[i];
@@ -321,7 +315,9 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED 
                 if constexpr (kNarrow) a[k] = amax_of_pair(amax_of_words<16 / kPerUnit>(raw[i].w + k * (16 / kPerUnit)));
                 else a[k] = amax_of<kUnit / kPerUnit>(v + k * (kUnit / kPerUnit));
             }
-            const uint4 codes = quantise_unit<FMT>(v, a, ts, factors, scales);
+            uint4 codes;
+            if constexpr (kNarrow) codes = quantise_unit<FMT>(UnitBf16<PAIRS>{raw[i].w}, a, ts, factors, scales);
+            else codes = quantise_unit<FMT>(UnitF32{v}, a, ts, factors, scales);
             if (row < p.rows && col < p.cols)
                 *reinterpret_cast<uint4*>(p.r_codes + ((int64_t)batch * p.rows + row) * p.r_ld + col / 2) = codes;
             uint8_t* s = row_scales + ((u * kPerUnit) >> 2) * kScaleTile + scale_at(lrow, u * kPerUnit);
@@ -338,9 +334,9 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED 
     }
     if constexpr (COLS) {
         uint8_t* stage = dyn + 128 * kPitch;
-        auto put = [&](int lcol, int u, const auto* v, const float* a) {
+        auto put = [&](int lcol, int u, const auto& unit, const float* a) {
             uint32_t scales;
-            const uint4 codes = quantise_unit<FMT>(v, a, ts, factors, scales);
+            const uint4 codes = quantise_unit<FMT>(unit, a, ts, factors, scales);
             *reinterpret_cast<uint4*>(stage + stage_at(lcol, u)) = codes;
             const bool in = (int64_t)col_tile * 128 + lcol < p.cols && (int64_t)row_tile * 128 + u * kUnit < p.rows;
             uint8_t* s = col_scales + ((u * kPerUnit) >> 2) * kScaleTile + scale_at(lcol, u * kPerUnit);
@@ -352,7 +348,6 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED 
             const uint8_t* from[2] = {dyn + u * kUnit * kPitch + L::chunk(0, pair >> 2) * 16 + (pair & 3) * 4,
                                       dyn + u * kUnit * kPitch + L::chunk(1, pair >> 2) * 16 + (pair & 3) * 4};
             uint32_t w[kUnit], m[kPerUnit];
-            uint16_t v[kUnit];
             float a[kPerUnit];
 #pragma unroll
             for (int i = 0; i < kUnit; ++i) w[i] = *reinterpret_cast<const uint32_t*>(from[i & 1] + i * kPitch);
@@ -360,14 +355,10 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED 
             for (int k = 0; k < kPerUnit; ++k) m[k] = amax_of_words<kUnit / kPerUnit>(w + k * (kUnit / kPerUnit));
 #pragma unroll
             for (int k = 0; k < kPerUnit; ++k) a[k] = fabsf(bf16_low(m[k]));
-#pragma unroll
-            for (int i = 0; i < kUnit; ++i) v[i] = low_half(w[i]);
-            put(2 * pair, u, v, a);
+            put(2 * pair, u, UnitBf16<LOW>{w}, a);
 #pragma unroll
             for (int k = 0; k < kPerUnit; ++k) a[k] = fabsf(bf16_high(m[k]));
-#pragma unroll
-            for (int i = 0; i < kUnit; ++i) v[i] = high_half(w[i]);
-            put(2 * pair + 1, u, v, a);
+            put(2 * pair + 1, u, UnitBf16<HIGH>{w}, a);
         } else {
 #pragma unroll 1
             for (int half = 0; half < 2; ++half) {
@@ -377,7 +368,7 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED 
                 for (int i = 0; i < kUnit; ++i) v[i] = *reinterpret_cast<const float*>(dyn + (u * kUnit + i) * kPitch + L::chunk(i & 1, lcol >> 2) * 16 + (lcol & 3) * 4);
 #pragma unroll
                 for (int k = 0; k < kPerUnit; ++k) a[k] = amax_of<kUnit / kPerUnit>(v + k * (kUnit / kPerUnit));
-                put(lcol, u, v, a);
+                put(lcol, u, UnitF32{v}, a);
             }
         }
         __syncthreads();
@@ -393,6 +384,191 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED 
         if (tid < kTiles * 32 && ktile < p.c_ktiles)
             *reinterpret_cast<uint4*>(p.c_scales + (((int64_t)batch * p.c_row_tiles + col_tile) * p.c_ktiles + ktile) * kScaleTile + (tid & 31) * 16) =
                 *reinterpret_cast<const uint4*>(col_scales + tid * 16);
+    }
+}
+
+// ---- large BF16 tensors in the column direction: the same tiles, streamed
+//
+// Persistent CTAs, three an SM.  While a tile is converted, the next one is on its way into the other half of the shared
+// memory (asynchronous 16-byte copies to the permuted chunks, zero-filled past the edges), so loads never wait for arithmetic: with
+// one tile per CTA the loads stood still for most of its life (8192 x 14336 E4M3_16, columns alone: 66 us, streamed 56 us).
+// Gathered rows stay with one tile per CTA: looked up a tile ahead they came to 57 us instead of 45 (36,700 rows of 2048).
+__device__ __forceinline__ void copy_async16(uint32_t dst, const void* src, int bytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+constexpr int kStreamTile = 128 * Tile<true>::kPitch;
+constexpr int kStreamSmem = 2 * kStreamTile + 128 * 64;
+constexpr uint32_t kStreamTiles = 148 * 4;      // below, every tile has a CTA of its own and there is nothing to stream
+
+// Where a CTA is in the grid of tiles; advanced by its stride without divisions.
+struct TileWalk {
+    uint32_t batch, row, col;
+    __device__ __forceinline__ TileWalk(const QuantParams& p, uint32_t tile)
+    {
+        const uint32_t per = p.row_tiles * p.col_tiles;
+        batch = tile / per;
+        row = tile % per / p.col_tiles;
+        col = tile % per % p.col_tiles;
+    }
+    __device__ __forceinline__ void advance(const QuantParams& p, const TileWalk& step)
+    {
+        batch += step.batch;
+        row += step.row;
+        col += step.col;
+        if (col >= p.col_tiles) { col -= p.col_tiles; ++row; }
+        if (row >= p.row_tiles) { row -= p.row_tiles; ++batch; }
+    }
+};
+
+// The arithmetic of a tile is about five instructions per element; addresses are formed once per tile and thread and stepped
+// by constants, since 64-bit products per access came to as much again.
+template <int FMT, bool ROWS>
+__global__ void __launch_bounds__(kQThreads, 3) fp4_stream_kernel(const __grid_constant__ QuantParams p, uint32_t tiles)
+{
+    using L = Tile<true>;
+    constexpr int kTiles = FMT == MOR_FP4_E4M3_16 ? 2 : 1;
+    constexpr int kPerUnit = Fp4<FMT>::kBlocksPerUnit;
+    constexpr int kCopies = 128 * 16 / kQThreads;                         // 16-byte chunks per thread and tile
+    __shared__ float red[kQThreads / 32];
+    __shared__ float factors[FMT == MOR_FP4_E4M3_16 ? 128 : 1];
+    __shared__ __align__(16) uint8_t row_scales[ROWS ? kTiles * kScaleTile : 16];
+    __shared__ __align__(16) uint8_t col_scales[kTiles * kScaleTile];
+    extern __shared__ __align__(16) uint8_t dyn[];                        // two tiles, then the codes of the transposed rows
+    const int tid = threadIdx.x;
+
+    // copies: chunk tid % 16 of rows tid / 16 + 16 i (all of one parity, so at one place in the permutation)
+    const int c_row = tid >> 4, c_chunk = tid & 15;
+    const uint32_t c_to = (uint32_t)__cvta_generic_to_shared(dyn) + c_row * L::kPitch + L::chunk(c_row, c_chunk) * 16;
+    const int64_t c_step = 32 * p.ld;                                     // bytes between this thread's rows
+    auto fetch = [&](const TileWalk& t, bool have, uint32_t to) {
+        if (have) {
+            const int64_t col = (int64_t)t.col * 128 + c_chunk * 8, row = (int64_t)t.row * 128 + c_row;
+            const char* from = static_cast<const char*>(p.x) + 2 * ((int64_t)t.batch * p.batch_stride + row * p.ld + col);
+            const int room = (int)max((int64_t)0, min((int64_t)8, p.cols - col)) * 2;         // bytes of the chunk inside the row
+            const int left = (int)min((int64_t)128, p.rows - row);                            // rows from the thread's first on
+            if (room == 16 && left > 16 * (kCopies - 1)) {
+#pragma unroll
+                for (int i = 0; i < kCopies; ++i, from += c_step) copy_async16(to + i * 16 * L::kPitch, from, 16);
+            } else {
+                const char* at = from;
+#pragma unroll 1
+                for (int i = 0; i < kCopies; ++i, at += c_step) {
+                    const bool in = 16 * i < left && room > 0;
+                    copy_async16(to + i * 16 * L::kPitch, in ? at : static_cast<const char*>(p.x), in ? room : 0);
+                }
+            }
+        }
+        copy_async_commit();
+    };
+    const TileWalk step(p, gridDim.x);
+    TileWalk now(p, blockIdx.x), next = now;
+    uint32_t tile = blockIdx.x;
+    fetch(now, tile < tiles, c_to);
+    next.advance(p, step);
+
+    TensorScale ts = {1.f, 1.f, 1.f};
+    if constexpr (FMT == MOR_FP4_E4M3_16) {
+        float amax = 0.f;
+        if (p.amax != nullptr) {
+            amax = *p.amax;
+        } else {
+            cudaGridDependencySynchronize();
+            for (uint32_t i = tid; i < p.n_partial; i += kQThreads) amax = fmaxf(amax, __ldcg(p.partial + i));
+            amax = block_max(amax, red);
+        }
+        ts = tensor_scale_of(amax);
+        fill_factors(factors, ts.t, tid);                                  // read after the loop's first barrier
+    }
+    if (blockIdx.x == 0 && tid == 0) {
+        if (ROWS) *p.r_t = ts.t;
+        *p.c_t = ts.t;
+    }
+
+    // rows: unit tid % 4 of rows tid / 4 and 64 + tid / 4; columns: two neighbours (one word) over the 32 rows of unit tid / 64
+    const int r_row = tid >> 2, r_unit = tid & 3, pair = tid & 63, unit = tid >> 6;
+    uint8_t* const stage = dyn + 2 * kStreamTile;
+    uint32_t half = 0;                                                     // byte offset of the tile at hand
+    for (; tile < tiles; tile += gridDim.x) {
+        fetch(next, tile + gridDim.x < tiles, c_to + (half ^ kStreamTile));
+        copy_async_wait<1>();
+        __syncthreads();
+        const uint8_t* in = dyn + half;
+        const int rows_left = (int)min((int64_t)128, p.rows - (int64_t)now.row * 128), cols_left = (int)min((int64_t)128, p.cols - (int64_t)now.col * 128);
+        if constexpr (ROWS) {
+            uint8_t* to = p.r_codes + ((int64_t)now.batch * p.rows + (int64_t)now.row * 128 + r_row) * p.r_ld + now.col * 64 + r_unit * 16;
+            const uint8_t* from = in + r_row * L::kPitch;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                uint32_t w[16], scales;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint4 q = *reinterpret_cast<const uint4*>(from + i * 64 * L::kPitch + L::chunk(r_row, r_unit * 4 + j) * 16);
+                    w[4 * j] = q.x; w[4 * j + 1] = q.y; w[4 * j + 2] = q.z; w[4 * j + 3] = q.w;
+                }
+                float a[kPerUnit];
+#pragma unroll
+                for (int k = 0; k < kPerUnit; ++k) a[k] = amax_of_pair(amax_of_words<16 / kPerUnit>(w + k * (16 / kPerUnit)));
+                const uint4 codes = quantise_unit<FMT>(UnitBf16<PAIRS>{w}, a, ts, factors, scales);
+                const bool inside = r_row + 64 * i < rows_left && r_unit * kUnit < cols_left;
+                if (inside) *reinterpret_cast<uint4*>(to + i * 64 * p.r_ld) = codes;
+                uint8_t* s = row_scales + ((r_unit * kPerUnit) >> 2) * kScaleTile + scale_at(r_row + 64 * i, r_unit * kPerUnit);
+                if constexpr (kPerUnit == 2) *reinterpret_cast<uint16_t*>(s) = inside ? (uint16_t)scales : 0;
+                else *s = inside ? (uint8_t)scales : 0;
+            }
+        }
+        {
+            const uint8_t* from[2] = {in + unit * kUnit * L::kPitch + L::chunk(0, pair >> 2) * 16 + (pair & 3) * 4,
+                                      in + unit * kUnit * L::kPitch + L::chunk(1, pair >> 2) * 16 + (pair & 3) * 4};
+            uint32_t w[kUnit], m[kPerUnit];
+#pragma unroll
+            for (int i = 0; i < kUnit; ++i) w[i] = *reinterpret_cast<const uint32_t*>(from[i & 1] + i * L::kPitch);
+#pragma unroll
+            for (int k = 0; k < kPerUnit; ++k) m[k] = amax_of_words<kUnit / kPerUnit>(w + k * (kUnit / kPerUnit));
+            auto put = [&](int lcol, const auto& values, const float* a) {
+                uint32_t scales;
+                const uint4 codes = quantise_unit<FMT>(values, a, ts, factors, scales);
+                *reinterpret_cast<uint4*>(stage + stage_at(lcol, unit)) = codes;
+                const bool inside = lcol < cols_left && unit * kUnit < rows_left;
+                uint8_t* s = col_scales + ((unit * kPerUnit) >> 2) * kScaleTile + scale_at(lcol, unit * kPerUnit);
+                if constexpr (kPerUnit == 2) *reinterpret_cast<uint16_t*>(s) = inside ? (uint16_t)scales : 0;
+                else *s = inside ? (uint8_t)scales : 0;
+            };
+            float a[kPerUnit];
+#pragma unroll
+            for (int k = 0; k < kPerUnit; ++k) a[k] = fabsf(bf16_low(m[k]));
+            put(2 * pair, UnitBf16<LOW>{w}, a);
+#pragma unroll
+            for (int k = 0; k < kPerUnit; ++k) a[k] = fabsf(bf16_high(m[k]));
+            put(2 * pair + 1, UnitBf16<HIGH>{w}, a);
+        }
+        __syncthreads();
+        {
+            uint8_t* to = p.c_codes + ((int64_t)now.batch * p.cols + (int64_t)now.col * 128 + r_row) * p.c_ld + now.row * 64 + r_unit * 16;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (r_row + 64 * i < cols_left && r_unit * kUnit < rows_left)
+                    *reinterpret_cast<uint4*>(to + i * 64 * p.c_ld) = *reinterpret_cast<const uint4*>(stage + stage_at(r_row + 64 * i, r_unit));
+        }
+        if (ROWS && tid < kTiles * 32) {
+            const uint32_t ktile = now.col * kTiles + (tid >> 5);
+            if (ktile < p.r_ktiles)
+                *reinterpret_cast<uint4*>(p.r_scales + (((int64_t)now.batch * p.row_tiles + now.row) * p.r_ktiles + ktile) * kScaleTile + (tid & 31) * 16) =
+                    *reinterpret_cast<const uint4*>(row_scales + tid * 16);
+        }
+        if (tid >= 128 && tid < 128 + kTiles * 32) {
+            const int t = tid - 128;
+            const uint32_t ktile = now.row * kTiles + (t >> 5);
+            if (ktile < p.c_ktiles)
+                *reinterpret_cast<uint4*>(p.c_scales + (((int64_t)now.batch * p.c_row_tiles + now.col) * p.c_ktiles + ktile) * kScaleTile + (t & 31) * 16) =
+                    *reinterpret_cast<const uint4*>(col_scales + t * 16);
+        }
+        now = next;
+        next.advance(p, step);
+        half ^= kStreamTile;
     }
 }
 
@@ -492,6 +668,13 @@ template <typename T, int FMT> __global__ void __launch_bounds__(kQThreads) fp4_
 
 template <typename T, int FMT, bool ROWS, bool COLS, int MODE> cudaError_t quant_launch(const QuantParams& p, uint32_t grid, cudaStream_t st)
 {
+    if constexpr (sizeof(T) == 2 && COLS && MODE == PLAIN) {
+        if (p.access >= 16 && grid >= kStreamTiles && (FMT == MOR_FP4_E8M0_32 || p.amax != nullptr || p.partial != nullptr)) {
+            static std::atomic<uint64_t> stream_done{0};
+            if (!allow_smem(fp4_stream_kernel<FMT, ROWS>, kStreamSmem, stream_done)) return cudaErrorInvalidValue;
+            return launch(fp4_stream_kernel<FMT, ROWS>, grid < 148 * 3 ? grid : 148 * 3, kQThreads, kStreamSmem, st, p.partial != nullptr, p, grid);
+        }
+    }
     constexpr bool kNarrow = sizeof(T) == 2 && MODE != WEIGHTED;
     constexpr int most = COLS ? 128 * Tile<kNarrow>::kPitch + 128 * 64 : 128 * (128 * (int)sizeof(T) + 16);
     const int smem = COLS || p.access < 16 ? most : 0;
