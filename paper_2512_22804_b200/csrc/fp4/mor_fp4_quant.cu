@@ -33,7 +33,7 @@ struct QuantParams {
     int64_t batch;
     const int32_t* slot_of_row;
     const int32_t* row_of_slot;
-    uint32_t top;
+    uint32_t top, inv_top;             // inv_top = floor((2^32 - 1) / top), see token_of()
     int32_t weight_dtype;
     const void* weight;
     uint8_t *r_codes, *r_scales, *c_codes, *c_scales;
@@ -41,6 +41,13 @@ struct QuantParams {
     uint32_t r_ktiles, c_ktiles, c_row_tiles;
     float *r_t, *c_t;
 };
+
+// slot / top: the product with the rounded-down reciprocal is the quotient or one less.
+__device__ __forceinline__ int64_t token_of(uint32_t slot, const QuantParams& p)
+{
+    const uint32_t q = __umulhi(slot, p.inv_top);
+    return slot - q * p.top >= p.top ? q + 1 : q;
+}
 
 template <typename T> struct Raw;
 template <> struct Raw<__nv_bfloat16> { uint32_t w[16]; };
@@ -213,7 +220,7 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED 
             if constexpr (MODE != PLAIN) {
                 const int32_t slot = have ? p.slot_of_row[row] : -1;
                 have = slot >= 0;
-                src = have ? slot / (int32_t)p.top : 0;
+                src = have ? token_of((uint32_t)slot, p) : 0;
             }
             const T* from = x + src * p.ld + (int64_t)col_tile * 128;
             Piece<T, (int)sizeof(T)> v[4];
@@ -236,7 +243,7 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED 
         if constexpr (MODE != PLAIN) {
             const int32_t slot = row < p.rows ? p.slot_of_row[row] : -1;
             have = have && slot >= 0;
-            src = have ? slot / (int32_t)p.top : 0;
+            src = have ? token_of((uint32_t)slot, p) : 0;
             if (MODE == WEIGHTED && have) weight[i] = weight_at(p.weight, p.weight_dtype, slot);
         }
         if (p.access < 16) {
@@ -392,7 +399,6 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED 
 // Persistent CTAs, three an SM.  While a tile is converted, the next one is on its way into the other half of the shared
 // memory (asynchronous 16-byte copies to the permuted chunks, zero-filled past the edges), so loads never wait for arithmetic: with
 // one tile per CTA the loads stood still for most of its life (8192 x 14336 E4M3_16, columns alone: 66 us, streamed 56 us).
-// Gathered rows stay with one tile per CTA: looked up a tile ahead they came to 57 us instead of 45 (36,700 rows of 2048).
 __device__ __forceinline__ void copy_async16(uint32_t dst, const void* src, int bytes)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -426,39 +432,70 @@ struct TileWalk {
 
 // The arithmetic of a tile is about five instructions per element; addresses are formed once per tile and thread and stepped
 // by constants, since 64-bit products per access came to as much again.
-template <int FMT, bool ROWS>
+template <int FMT, bool ROWS, int MODE>
 __global__ void __launch_bounds__(kQThreads, 3) fp4_stream_kernel(const __grid_constant__ QuantParams p, uint32_t tiles)
 {
     using L = Tile<true>;
     constexpr int kTiles = FMT == MOR_FP4_E4M3_16 ? 2 : 1;
     constexpr int kPerUnit = Fp4<FMT>::kBlocksPerUnit;
-    constexpr int kCopies = 128 * 16 / kQThreads;                         // 16-byte chunks per thread and tile
+    // 16-byte chunks: chunk tid % 16 of every 16th row; gathered, four chunks of every 64th row, so that a thread looks up two
+    // rows (a quarter of a row is still two whole sectors)
+    constexpr int kRowsOf = MODE == PLAIN ? 8 : 2, kChunksOf = MODE == PLAIN ? 1 : 4, kRowStep = 128 / kRowsOf;
     __shared__ float red[kQThreads / 32];
     __shared__ float factors[FMT == MOR_FP4_E4M3_16 ? 128 : 1];
+    __shared__ __align__(16) float weights[MODE == WEIGHTED ? 2 * 128 : 4];
     __shared__ __align__(16) uint8_t row_scales[ROWS ? kTiles * kScaleTile : 16];
     __shared__ __align__(16) uint8_t col_scales[kTiles * kScaleTile];
     extern __shared__ __align__(16) uint8_t dyn[];                        // two tiles, then the codes of the transposed rows
     const int tid = threadIdx.x;
 
-    // copies: chunk tid % 16 of rows tid / 16 + 16 i (all of one parity, so at one place in the permutation)
-    const int c_row = tid >> 4, c_chunk = tid & 15;
-    const uint32_t c_to = (uint32_t)__cvta_generic_to_shared(dyn) + c_row * L::kPitch + L::chunk(c_row, c_chunk) * 16;
-    const int64_t c_step = 32 * p.ld;                                     // bytes between this thread's rows
-    auto fetch = [&](const TileWalk& t, bool have, uint32_t to) {
+    const int c_row = MODE == PLAIN ? tid >> 4 : tid >> 2, c_chunk = MODE == PLAIN ? tid & 15 : tid & 3;
+    const uint32_t c_to = (uint32_t)__cvta_generic_to_shared(dyn) + c_row * L::kPitch;
+    const int64_t c_step = 2 * kRowStep * p.ld;                           // bytes between this thread's rows
+    int32_t slot[MODE == PLAIN ? 1 : kRowsOf];                            // of the next tile to fetch
+    float weight[MODE == WEIGHTED ? kRowsOf : 1];
+    auto look_up = [&](const TileWalk& t, bool have) {
+        if constexpr (MODE != PLAIN) {
+#pragma unroll
+            for (int i = 0; i < kRowsOf; ++i) {
+                const int64_t row = (int64_t)t.row * 128 + c_row + kRowStep * i;
+                slot[i] = have && row < p.rows ? p.slot_of_row[row] : -1;
+                if constexpr (MODE == WEIGHTED) weight[i] = slot[i] >= 0 ? weight_at(p.weight, p.weight_dtype, slot[i]) : 0.f;
+            }
+        }
+    };
+    auto fetch = [&](const TileWalk& t, bool have, uint32_t half) {
         if (have) {
             const int64_t col = (int64_t)t.col * 128 + c_chunk * 8, row = (int64_t)t.row * 128 + c_row;
-            const char* from = static_cast<const char*>(p.x) + 2 * ((int64_t)t.batch * p.batch_stride + row * p.ld + col);
-            const int room = (int)max((int64_t)0, min((int64_t)8, p.cols - col)) * 2;         // bytes of the chunk inside the row
-            const int left = (int)min((int64_t)128, p.rows - row);                            // rows from the thread's first on
-            if (room == 16 && left > 16 * (kCopies - 1)) {
+            const char* x = static_cast<const char*>(p.x) + 2 * col;
+            const int cols = (int)max((int64_t)-128, min((int64_t)128, p.cols - col));        // from the thread's first chunk on
+            if constexpr (MODE == PLAIN) {
+                const char* from = x + 2 * ((int64_t)t.batch * p.batch_stride + row * p.ld);
+                const uint32_t to = c_to + half + L::chunk(c_row, c_chunk) * 16;              // all rows of one parity: one place
+                const int room = max(0, min(8, cols)) * 2, left = (int)min((int64_t)128, p.rows - row);
+                if (room == 16 && left > kRowStep * (kRowsOf - 1)) {
 #pragma unroll
-                for (int i = 0; i < kCopies; ++i, from += c_step) copy_async16(to + i * 16 * L::kPitch, from, 16);
-            } else {
-                const char* at = from;
+                    for (int i = 0; i < kRowsOf; ++i, from += c_step) copy_async16(to + i * kRowStep * L::kPitch, from, 16);
+                } else {
 #pragma unroll 1
-                for (int i = 0; i < kCopies; ++i, at += c_step) {
-                    const bool in = 16 * i < left && room > 0;
-                    copy_async16(to + i * 16 * L::kPitch, in ? at : static_cast<const char*>(p.x), in ? room : 0);
+                    for (int i = 0; i < kRowsOf; ++i, from += c_step) {
+                        const bool in = kRowStep * i < left && room > 0;
+                        copy_async16(to + i * kRowStep * L::kPitch, in ? from : static_cast<const char*>(p.x), in ? room : 0);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kRowsOf; ++i) {
+                    const bool in = slot[i] >= 0;
+                    const char* from = x + 2 * ((in ? token_of((uint32_t)slot[i], p) : 0) * p.ld);
+#pragma unroll
+                    for (int j0 = 0; j0 < kChunksOf; ++j0) {
+                        const int j = j0 ^ (c_row & 1);                                       // neighbouring rows in other banks
+                        const int room = in ? max(0, min(8, cols - 32 * j)) * 2 : 0;
+                        copy_async16(c_to + half + i * kRowStep * L::kPitch + L::chunk(c_row, c_chunk + 4 * j) * 16,
+                                     room > 0 ? from + 64 * j : static_cast<const char*>(p.x), room);
+                    }
+                    if (MODE == WEIGHTED && c_chunk == 0) weights[(half ? 128 : 0) + c_row + kRowStep * i] = weight[i];
                 }
             }
         }
@@ -467,8 +504,10 @@ __global__ void __launch_bounds__(kQThreads, 3) fp4_stream_kernel(const __grid_c
     const TileWalk step(p, gridDim.x);
     TileWalk now(p, blockIdx.x), next = now;
     uint32_t tile = blockIdx.x;
-    fetch(now, tile < tiles, c_to);
+    look_up(now, tile < tiles);
+    fetch(now, tile < tiles, 0);
     next.advance(p, step);
+    look_up(next, tile + gridDim.x < tiles);
 
     TensorScale ts = {1.f, 1.f, 1.f};
     if constexpr (FMT == MOR_FP4_E4M3_16) {
@@ -493,10 +532,14 @@ __global__ void __launch_bounds__(kQThreads, 3) fp4_stream_kernel(const __grid_c
     uint8_t* const stage = dyn + 2 * kStreamTile;
     uint32_t half = 0;                                                     // byte offset of the tile at hand
     for (; tile < tiles; tile += gridDim.x) {
-        fetch(next, tile + gridDim.x < tiles, c_to + (half ^ kStreamTile));
+        fetch(next, tile + gridDim.x < tiles, half ^ kStreamTile);
+        TileWalk after = next;
+        after.advance(p, step);
+        look_up(after, tile + 2 * (uint64_t)gridDim.x < tiles);
         copy_async_wait<1>();
         __syncthreads();
         const uint8_t* in = dyn + half;
+        const float* of_rows = weights + (half ? 128 : 0);
         const int rows_left = (int)min((int64_t)128, p.rows - (int64_t)now.row * 128), cols_left = (int)min((int64_t)128, p.cols - (int64_t)now.col * 128);
         if constexpr (ROWS) {
             uint8_t* to = p.r_codes + ((int64_t)now.batch * p.rows + (int64_t)now.row * 128 + r_row) * p.r_ld + now.col * 64 + r_unit * 16;
@@ -510,9 +553,20 @@ __global__ void __launch_bounds__(kQThreads, 3) fp4_stream_kernel(const __grid_c
                     w[4 * j] = q.x; w[4 * j + 1] = q.y; w[4 * j + 2] = q.z; w[4 * j + 3] = q.w;
                 }
                 float a[kPerUnit];
+                uint4 codes;
+                if constexpr (MODE == WEIGHTED) {
+                    const float f = of_rows[r_row + 64 * i];
+                    float v[kUnit];
 #pragma unroll
-                for (int k = 0; k < kPerUnit; ++k) a[k] = amax_of_pair(amax_of_words<16 / kPerUnit>(w + k * (16 / kPerUnit)));
-                const uint4 codes = quantise_unit<FMT>(UnitBf16<PAIRS>{w}, a, ts, factors, scales);
+                    for (int j = 0; j < 16; ++j) { v[2 * j] = bf16_low(w[j]) * f; v[2 * j + 1] = bf16_high(w[j]) * f; }
+#pragma unroll
+                    for (int k = 0; k < kPerUnit; ++k) a[k] = amax_of<kUnit / kPerUnit>(v + k * (kUnit / kPerUnit));
+                    codes = quantise_unit<FMT>(UnitF32{v}, a, ts, factors, scales);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < kPerUnit; ++k) a[k] = amax_of_pair(amax_of_words<16 / kPerUnit>(w + k * (16 / kPerUnit)));
+                    codes = quantise_unit<FMT>(UnitBf16<PAIRS>{w}, a, ts, factors, scales);
+                }
                 const bool inside = r_row + 64 * i < rows_left && r_unit * kUnit < cols_left;
                 if (inside) *reinterpret_cast<uint4*>(to + i * 64 * p.r_ld) = codes;
                 uint8_t* s = row_scales + ((r_unit * kPerUnit) >> 2) * kScaleTile + scale_at(r_row + 64 * i, r_unit * kPerUnit);
@@ -523,11 +577,9 @@ __global__ void __launch_bounds__(kQThreads, 3) fp4_stream_kernel(const __grid_c
         {
             const uint8_t* from[2] = {in + unit * kUnit * L::kPitch + L::chunk(0, pair >> 2) * 16 + (pair & 3) * 4,
                                       in + unit * kUnit * L::kPitch + L::chunk(1, pair >> 2) * 16 + (pair & 3) * 4};
-            uint32_t w[kUnit], m[kPerUnit];
+            uint32_t w[kUnit];
 #pragma unroll
             for (int i = 0; i < kUnit; ++i) w[i] = *reinterpret_cast<const uint32_t*>(from[i & 1] + i * L::kPitch);
-#pragma unroll
-            for (int k = 0; k < kPerUnit; ++k) m[k] = amax_of_words<kUnit / kPerUnit>(w + k * (kUnit / kPerUnit));
             auto put = [&](int lcol, const auto& values, const float* a) {
                 uint32_t scales;
                 const uint4 codes = quantise_unit<FMT>(values, a, ts, factors, scales);
@@ -538,12 +590,33 @@ __global__ void __launch_bounds__(kQThreads, 3) fp4_stream_kernel(const __grid_c
                 else *s = inside ? (uint8_t)scales : 0;
             };
             float a[kPerUnit];
+            if constexpr (MODE == WEIGHTED) {
 #pragma unroll
-            for (int k = 0; k < kPerUnit; ++k) a[k] = fabsf(bf16_low(m[k]));
-            put(2 * pair, UnitBf16<LOW>{w}, a);
+                for (int c = 0; c < 2; ++c) {
+                    float v[kUnit];
 #pragma unroll
-            for (int k = 0; k < kPerUnit; ++k) a[k] = fabsf(bf16_high(m[k]));
-            put(2 * pair + 1, UnitBf16<HIGH>{w}, a);
+                    for (int i = 0; i < kUnit; i += 4) {
+                        const float4 f = *reinterpret_cast<const float4*>(of_rows + unit * kUnit + i);
+                        v[i] = (c ? bf16_high(w[i]) : bf16_low(w[i])) * f.x;
+                        v[i + 1] = (c ? bf16_high(w[i + 1]) : bf16_low(w[i + 1])) * f.y;
+                        v[i + 2] = (c ? bf16_high(w[i + 2]) : bf16_low(w[i + 2])) * f.z;
+                        v[i + 3] = (c ? bf16_high(w[i + 3]) : bf16_low(w[i + 3])) * f.w;
+                    }
+#pragma unroll
+                    for (int k = 0; k < kPerUnit; ++k) a[k] = amax_of<kUnit / kPerUnit>(v + k * (kUnit / kPerUnit));
+                    put(2 * pair + c, UnitF32{v}, a);
+                }
+            } else {
+                uint32_t m[kPerUnit];
+#pragma unroll
+                for (int k = 0; k < kPerUnit; ++k) m[k] = amax_of_words<kUnit / kPerUnit>(w + k * (kUnit / kPerUnit));
+#pragma unroll
+                for (int k = 0; k < kPerUnit; ++k) a[k] = fabsf(bf16_low(m[k]));
+                put(2 * pair, UnitBf16<LOW>{w}, a);
+#pragma unroll
+                for (int k = 0; k < kPerUnit; ++k) a[k] = fabsf(bf16_high(m[k]));
+                put(2 * pair + 1, UnitBf16<HIGH>{w}, a);
+            }
         }
         __syncthreads();
         {
@@ -567,7 +640,7 @@ __global__ void __launch_bounds__(kQThreads, 3) fp4_stream_kernel(const __grid_c
                     *reinterpret_cast<const uint4*>(col_scales + t * 16);
         }
         now = next;
-        next.advance(p, step);
+        next = after;
         half ^= kStreamTile;
     }
 }
@@ -668,11 +741,11 @@ template <typename T, int FMT> __global__ void __launch_bounds__(kQThreads) fp4_
 
 template <typename T, int FMT, bool ROWS, bool COLS, int MODE> cudaError_t quant_launch(const QuantParams& p, uint32_t grid, cudaStream_t st)
 {
-    if constexpr (sizeof(T) == 2 && COLS && MODE == PLAIN) {
+    if constexpr (sizeof(T) == 2 && COLS) {
         if (p.access >= 16 && grid >= kStreamTiles && (FMT == MOR_FP4_E8M0_32 || p.amax != nullptr || p.partial != nullptr)) {
             static std::atomic<uint64_t> stream_done{0};
-            if (!allow_smem(fp4_stream_kernel<FMT, ROWS>, kStreamSmem, stream_done)) return cudaErrorInvalidValue;
-            return launch(fp4_stream_kernel<FMT, ROWS>, grid < 148 * 3 ? grid : 148 * 3, kQThreads, kStreamSmem, st, p.partial != nullptr, p, grid);
+            if (!allow_smem(fp4_stream_kernel<FMT, ROWS, MODE>, kStreamSmem, stream_done)) return cudaErrorInvalidValue;
+            return launch(fp4_stream_kernel<FMT, ROWS, MODE>, grid < 148 * 3 ? grid : 148 * 3, kQThreads, kStreamSmem, st, p.partial != nullptr, p, grid);
         }
     }
     constexpr bool kNarrow = sizeof(T) == 2 && MODE != WEIGHTED;
@@ -770,6 +843,7 @@ mor_status_t mor_fp4_quantize(const mor_fp4_quantize_desc_t* host_desc, const mo
     p.slot_of_row = d.slot_of_row;
     p.row_of_slot = d.row_of_slot;
     p.top = (uint32_t)(gather ? d.top : 1);
+    p.inv_top = 0xFFFFFFFFu / p.top;
     p.weight = d.weight;
     p.weight_dtype = d.weight_dtype;
     if (host_rows != nullptr) {
