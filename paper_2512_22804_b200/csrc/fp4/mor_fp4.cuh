@@ -251,6 +251,9 @@ template <typename T, int BYTES> struct Piece {
         } else if constexpr (BYTES == 16) {
             const uint4 q = *reinterpret_cast<const uint4*>(p);
             w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+        } else if constexpr (BYTES == 8) {
+            const uint2 q = *reinterpret_cast<const uint2*>(p);
+            w[0] = q.x; w[1] = q.y;
         } else if constexpr (BYTES == 4) w[0] = *reinterpret_cast<const uint32_t*>(p);
         else w[0] = *reinterpret_cast<const uint16_t*>(p);
     }
@@ -260,6 +263,7 @@ template <typename T, int BYTES> struct Piece {
 #pragma unroll
             for (int i = 0; i < kWords; i += 8) stg256(reinterpret_cast<uint32_t*>(p) + i, w + i);
         } else if constexpr (BYTES == 16) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        else if constexpr (BYTES == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
         else if constexpr (BYTES == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
         else *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
     }
@@ -304,11 +308,11 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t scale_blocks(int64_t cols, int format) { return ceil_div(cols, format == MOR_FP4_E4M3_16 ? 16 : 32); }
 inline int64_t scale_ktiles(int64_t cols, int format) { return ceil_div(scale_blocks(cols, format), 4); }
 
-// Widest access that base, pitch and batch pitch (bytes) allow: 32, 16, or `element`.
+// Widest access that base, pitch and batch pitch (bytes) allow: 32, 16, 8, 4, or `element`.
 inline int access_bytes(const void* p, int64_t pitch, int64_t batch_pitch, int element)
 {
     const uint64_t all = reinterpret_cast<uintptr_t>(p) | (uint64_t)pitch | (uint64_t)batch_pitch;
-    return all % 32 == 0 ? 32 : all % 16 == 0 ? 16 : element;
+    return all % 32 == 0 ? 32 : all % 16 == 0 ? 16 : all % 8 == 0 ? 8 : all % 4 == 0 ? 4 : element;
 }
 
 // Sizes that every index computation of the kernels can hold.

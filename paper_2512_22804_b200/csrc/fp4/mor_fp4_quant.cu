@@ -145,6 +145,7 @@ template <typename T, int BYTES, int MODE> __device__ __forceinline__ float piec
 
 // The largest magnitude of the whole tensor, one part per CTA (they are joined by the kernel that quantises: no counter to
 // clear, no atomics).  Bound by memory: a warp reads 1 KiB at a time (32 bytes a lane), a thread keeps four pieces in flight.
+__host__ __device__ inline bool contiguous(const QuantParams& p) { return p.ld == p.cols && (p.batch == 1 || p.batch_stride == p.x_rows * p.ld); }
 template <typename T, int BYTES, int MODE> __global__ void __launch_bounds__(kQThreads) fp4_amax_kernel(const __grid_constant__ QuantParams p, float* part)
 {
     using P = Piece<T, BYTES>;
@@ -152,12 +153,12 @@ template <typename T, int BYTES, int MODE> __global__ void __launch_bounds__(kQT
     __shared__ float red[kQThreads / 32];
     cudaTriggerProgrammaticLaunchCompletion();
     const T* x = static_cast<const T*>(p.x);
-    const bool flat = MODE == PLAIN && p.ld == p.cols && (p.batch == 1 || p.batch_stride == p.x_rows * p.ld);
+    const bool flat = MODE == PLAIN && contiguous(p);
     const int64_t rows = flat ? 1 : p.x_rows * p.batch, cols = flat ? p.x_rows * p.batch * p.cols : p.cols;
-    const int64_t per = cols / P::kElems;                            // cols is a whole number of pieces
-    const int64_t step = (int64_t)gridDim.x * kQThreads, drow = step / per, dpiece = step % per;
+    const int64_t per = cols / P::kElems;                            // whole pieces but for the end of a contiguous tensor
+    const int64_t step = (int64_t)gridDim.x * kQThreads, div = per > 0 ? per : 1, drow = step / div, dpiece = step % div;
     const int64_t first = (int64_t)blockIdx.x * kQThreads + threadIdx.x;
-    int64_t row = first / per, at = first % per;
+    int64_t row = per > 0 ? first / div : rows, at = first % div;
     float m = 0.f;
     while (row < rows) {
         P v[kFlight];
@@ -174,6 +175,11 @@ template <typename T, int BYTES, int MODE> __global__ void __launch_bounds__(kQT
 #pragma unroll
         for (int i = 0; i < kFlight; ++i)
             if (token[i] < rows) m = fmaxf(m, piece_max<T, BYTES, MODE>(v[i], p, token[i]));
+    }
+    if (flat && blockIdx.x == 0 && per * P::kElems + threadIdx.x < cols) {
+        Piece<T, (int)sizeof(T)> v;
+        v.load(x + per * P::kElems + threadIdx.x);
+        m = fmaxf(m, piece_max<T, (int)sizeof(T), PLAIN>(v, p, 0));
     }
     m = block_max(m, red);
     if (threadIdx.x == 0) part[blockIdx.x] = m;
@@ -212,26 +218,49 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED 
     Raw<T> raw[2];
     float weight[2] = {1.f, 1.f};
     constexpr int kInPitch = 128 * (int)sizeof(T) + 16;
-    if (p.access < 16) {        // rows that start anywhere: neighbouring lanes take neighbouring elements, through shared memory
-        for (int r = tid >> 5; r < 128; r += kQThreads / 32) {
-            const int64_t row = (int64_t)row_tile * 128 + r;
-            int64_t src = row;
-            bool have = row < p.rows;
-            if constexpr (MODE != PLAIN) {
-                const int32_t slot = have ? p.slot_of_row[row] : -1;
-                have = slot >= 0;
-                src = have ? token_of((uint32_t)slot, p) : 0;
-            }
-            const T* from = x + src * p.ld + (int64_t)col_tile * 128;
-            Piece<T, (int)sizeof(T)> v[4];
+    if (p.access < 16) {        // rows that start anywhere: neighbouring lanes take neighbouring pieces, through shared memory
+        auto take = [&](auto bytes) {
+            using P = Piece<T, decltype(bytes)::value>;
+            constexpr int kPieces = 128 / P::kElems / 32;                  // per lane and row
+            for (int r0 = (tid >> 5) * 16; r0 < (tid >> 5) * 16 + 16; r0 += 4) {
+                P v[4][kPieces];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                v[j].clear();
-                if (have && (int64_t)col_tile * 128 + j * 32 + (tid & 31) < p.cols) v[j].load(from + j * 32 + (tid & 31));
-            }
+                for (int i = 0; i < 4; ++i) {
+                    const int64_t row = (int64_t)row_tile * 128 + r0 + i;
+                    int64_t src = row;
+                    bool have = row < p.rows;
+                    if constexpr (MODE != PLAIN) {
+                        const int32_t slot = have ? p.slot_of_row[row] : -1;
+                        have = slot >= 0;
+                        src = have ? token_of((uint32_t)slot, p) : 0;
+                    }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j].store(reinterpret_cast<T*>(dyn + r * kInPitch) + j * 32 + (tid & 31));
-        }
+                    for (int j = 0; j < kPieces; ++j) {
+                        const int64_t col = (int64_t)col_tile * 128 + (j * 32 + (tid & 31)) * P::kElems;
+                        v[i][j].clear();
+                        if (have && col + P::kElems <= p.cols) {
+                            v[i][j].load(x + src * p.ld + col);
+                        } else if (have && col < p.cols) {                // the last piece of a row
+#pragma unroll
+                            for (int k = 0; k < P::kElems; ++k)
+                                if (col + k < p.cols) {
+                                    Piece<T, (int)sizeof(T)> one;
+                                    one.load(x + src * p.ld + col + k);
+                                    v[i][j].w[k * sizeof(T) / 4] |= one.w[0] << (8 * (k * sizeof(T) % 4));
+                                }
+                        }
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < kPieces; ++j)
+                        v[i][j].store(reinterpret_cast<T*>(dyn + (r0 + i) * kInPitch) + (j * 32 + (tid & 31)) * P::kElems);
+            }
+        };
+        if (p.access == 8) take(std::integral_constant<int, 8>{});
+        else if (p.access == 4) take(std::integral_constant<int, 4>{});
+        else if constexpr (sizeof(T) == 2) take(std::integral_constant<int, 2>{});
         __syncthreads();
     }
 #pragma unroll
@@ -764,10 +793,13 @@ template <typename T, int FMT, int MODE> cudaError_t quant_dirs(const QuantParam
 template <typename T, int MODE> cudaError_t quant_all(const QuantParams& p, int format, uint32_t amax_grid, uint32_t grid, float* part, cudaStream_t st)
 {
     if (amax_grid > 0) {
-        const int64_t width = p.cols * (int64_t)sizeof(T);
-        const cudaError_t e = p.access == 32 && width % 32 == 0   ? launch(fp4_amax_kernel<T, 32, MODE>, amax_grid, kQThreads, 0, st, false, p, part)
-                              : p.access >= 16 && width % 16 == 0 ? launch(fp4_amax_kernel<T, 16, MODE>, amax_grid, kQThreads, 0, st, false, p, part)
-                                                                  : launch(fp4_amax_kernel<T, (int)sizeof(T), MODE>, amax_grid, kQThreads, 0, st, false, p, part);
+        // rows that may be taken as one long one need no alignment but the first's
+        const bool flat = MODE == PLAIN && contiguous(p);
+        const int64_t width = flat ? 0 : p.cols * (int64_t)sizeof(T);
+        const int access = flat ? access_bytes(p.x, 0, 0, (int)sizeof(T)) : p.access;
+        const cudaError_t e = access == 32 && width % 32 == 0   ? launch(fp4_amax_kernel<T, 32, MODE>, amax_grid, kQThreads, 0, st, false, p, part)
+                              : access >= 16 && width % 16 == 0 ? launch(fp4_amax_kernel<T, 16, MODE>, amax_grid, kQThreads, 0, st, false, p, part)
+                                                                : launch(fp4_amax_kernel<T, (int)sizeof(T), MODE>, amax_grid, kQThreads, 0, st, false, p, part);
         if (e != cudaSuccess) return e;
     }
     return format == MOR_FP4_E4M3_16 ? quant_dirs<T, MOR_FP4_E4M3_16, MODE>(p, grid, st) : quant_dirs<T, MOR_FP4_E8M0_32, MODE>(p, grid, st);
