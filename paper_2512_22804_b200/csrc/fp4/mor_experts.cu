@@ -54,7 +54,7 @@ __device__ void count_slots(const SortParams& p, int32_t* counts)
 __global__ void __launch_bounds__(kSortThreads) expert_count_kernel(const __grid_constant__ SortParams p)
 {
     extern __shared__ int32_t counts[];
-    cudaTriggerProgrammaticLaunchCompletion();
+    wait_for_predecessor();
     count_slots(p, counts);
     for (int e = threadIdx.x; e < p.experts; e += kSortThreads) {
         int32_t sum = 0;
@@ -93,13 +93,14 @@ __global__ void __launch_bounds__(kSortThreads) expert_place_kernel(const __grid
     __shared__ int32_t scan[32];
     __shared__ int32_t used[MOR_MAX_GROUPS + 1];        // first empty row of each expert; [experts]: first row past the last expert
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (gridDim.x == 1) wait_for_predecessor();             // else the predecessor is the count, and the ids are older
     count_slots(p, counts);
     int32_t own = 0, before = 0, total = 0;
     if (tid < p.experts)
         for (int w = 0; w < kSortWarps; ++w) own += counts[w * p.experts + tid];
     total = own;
     if (gridDim.x > 1) {
-        cudaGridDependencySynchronize();
+        wait_for_predecessor();
         total = 0;
         if (tid < p.experts)
             for (uint32_t c = 0; c < gridDim.x; ++c) {
@@ -200,6 +201,7 @@ template <typename T, int BYTES> __global__ void __launch_bounds__(256) expert_g
 {
     using P = Piece<T, BYTES>;
     T* out = static_cast<T*>(p.out);
+    wait_for_predecessor();
     if (blockIdx.x < p.clear_blocks) {
         clear_rows<T, BYTES>(p, out, blockIdx.x);
         return;
@@ -226,6 +228,7 @@ template <typename T, typename R, int BYTES> __global__ void __launch_bounds__(2
 {
     using P = Piece<T, BYTES>;
     using Q = Piece<R, BYTES / (int)sizeof(T) * (int)sizeof(R)>;
+    wait_for_predecessor();
     const int64_t token = blockIdx.x;
     const R* ys = static_cast<const R*>(p.rows_in);
     T* out = static_cast<T*>(p.out) + token * p.ld_out;
@@ -260,6 +263,7 @@ template <typename T, typename R, int BYTES> __global__ void __launch_bounds__(2
     using P = Piece<T, BYTES>;
     using Q = Piece<R, BYTES / (int)sizeof(T) * (int)sizeof(R)>;
     T* out = static_cast<T*>(p.out);
+    wait_for_predecessor();
     if (blockIdx.x < p.clear_blocks) {
         clear_rows<T, BYTES>(p, out, blockIdx.x);
         return;
@@ -326,9 +330,9 @@ template <typename T, typename R, int BYTES> cudaError_t move_launch(const MoveP
     const int64_t pieces = ceil_div(p.hidden, BYTES / (int64_t)sizeof(T));
     const uint32_t threads = pieces >= 256 ? 256u : (uint32_t)(ceil_div(pieces, 32) * 32);
     if constexpr (sizeof(T) == sizeof(R))
-        if (what == MOVE_GATHER) return launch(expert_gather_kernel<T, BYTES>, grid, threads, 0, st, false, p);
-    if (what == MOVE_COMBINE) return launch(expert_combine_kernel<T, R, BYTES>, grid, threads, 0, st, false, p);
-    return launch(expert_grad_kernel<T, R, BYTES>, grid, threads, 0, st, false, p);
+        if (what == MOVE_GATHER) return launch(expert_gather_kernel<T, BYTES>, grid, threads, 0, st, true, p);
+    if (what == MOVE_COMBINE) return launch(expert_combine_kernel<T, R, BYTES>, grid, threads, 0, st, true, p);
+    return launch(expert_grad_kernel<T, R, BYTES>, grid, threads, 0, st, true, p);
 }
 template <typename T, typename R> cudaError_t move_access(const MoveParams& p, Move what, uint32_t grid, int access, cudaStream_t st)
 {
@@ -442,9 +446,9 @@ mor_status_t mor_expert_sort(const int32_t* ids, int64_t n_slots, int experts, i
     if (!allow_smem(expert_place_kernel, most, done_place)) return MOR_ERR_CUDA;
     if (chunks > 1) {
         if (!allow_smem(expert_count_kernel, most, done_count)) return MOR_ERR_CUDA;
-        if (launch(expert_count_kernel, chunks, kSortThreads, smem, st, false, p) != cudaSuccess) return MOR_ERR_CUDA;
+        if (launch(expert_count_kernel, chunks, kSortThreads, smem, st, true, p) != cudaSuccess) return MOR_ERR_CUDA;
     }
-    return launch(expert_place_kernel, chunks, kSortThreads, smem, st, chunks > 1, p) == cudaSuccess ? MOR_OK : MOR_ERR_CUDA;
+    return launch(expert_place_kernel, chunks, kSortThreads, smem, st, true, p) == cudaSuccess ? MOR_OK : MOR_ERR_CUDA;
 }
 
 mor_status_t mor_expert_gather(const mor_expert_desc_t* host_desc, const void* x, int64_t ldx, void* out, int64_t ldo, void* cuda_stream)

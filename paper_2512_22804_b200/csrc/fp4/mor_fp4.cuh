@@ -348,9 +348,22 @@ template <typename K> inline bool allow_smem(K kernel, int bytes, std::atomic<ui
     return true;
 }
 
-// One launch; `overlap` lets it start while the stream's previous kernel ends (it then waits before it reads what that wrote).
+// A kernel may be launched so that it starts while the stream's previous kernel ends; each calls this before it touches anything that
+// kernel may have written.  It lets the next kernel start only after its own wait, so that whatever starts early finds everything
+// older than its direct predecessor complete.
+__device__ __forceinline__ void wait_for_predecessor()
+{
+    cudaGridDependencySynchronize();
+    cudaTriggerProgrammaticLaunchCompletion();
+}
+
+// An early start saves two to four microseconds where a kernel is over soon or fills the GPU exactly.  One of many small CTAs should
+// not have it: its first CTAs crowd the multiprocessors that fall free first, and neighbouring tiles then run at different times for
+// the whole kernel (quantising 8192 x 14336 both ways and back: 239 us with early starts throughout, 213 without).
+constexpr uint32_t kEarlyGrid = 148 * 2;
+
 template <typename... P, typename... A>
-inline cudaError_t launch(void (*kernel)(P...), uint32_t grid, uint32_t block, size_t smem, cudaStream_t stream, bool overlap, A&&... args)
+inline cudaError_t launch(void (*kernel)(P...), uint32_t grid, uint32_t block, size_t smem, cudaStream_t stream, bool early, A&&... args)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid);
@@ -361,7 +374,7 @@ inline cudaError_t launch(void (*kernel)(P...), uint32_t grid, uint32_t block, s
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
-    cfg.numAttrs = overlap ? 1 : 0;
+    cfg.numAttrs = early ? 1 : 0;
     return cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...);
 }
 

@@ -217,7 +217,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) fp4_wide_kernel(const __grid_
     }
     if (warp == 2) tmem_alloc<CG>(&C.tmem, 512);
     tc_fence_before();
-    cudaGridDependencySynchronize();
+    wait_for_predecessor();
     fill_table<CG, GROUP>(p, table);
     if constexpr (CG == 2) cluster_sync();
     else __syncthreads();
@@ -396,7 +396,7 @@ template <int NT, int FMT, typename T> __global__ void __launch_bounds__(kNarrow
     }
     if (warp == 1) tmem_alloc<1>(&C.tmem, W::kTmem);
     tc_fence_before();
-    cudaGridDependencySynchronize();
+    wait_for_predecessor();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = C.tmem;

@@ -151,7 +151,7 @@ template <typename T, int BYTES, int MODE> __global__ void __launch_bounds__(kQT
     using P = Piece<T, BYTES>;
     constexpr int kFlight = 4;
     __shared__ float red[kQThreads / 32];
-    cudaTriggerProgrammaticLaunchCompletion();
+    wait_for_predecessor();
     const T* x = static_cast<const T*>(p.x);
     const bool flat = MODE == PLAIN && contiguous(p);
     const int64_t rows = flat ? 1 : p.x_rows * p.batch, cols = flat ? p.x_rows * p.batch * p.cols : p.cols;
@@ -214,7 +214,8 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED 
     const uint32_t row_tile = in_batch / p.col_tiles, col_tile = in_batch % p.col_tiles;
     const T* x = static_cast<const T*>(p.x) + (int64_t)batch * p.batch_stride;
 
-    // both units' loads first: the tile is in flight while the tensor maximum is waited for
+    // both units' loads first: the tile is in flight while the tensor maximum is waited for (x is older than the kernel that takes it)
+    if (FMT != MOR_FP4_E4M3_16 || p.partial == nullptr) wait_for_predecessor();
     Raw<T> raw[2];
     float weight[2] = {1.f, 1.f};
     constexpr int kInPitch = 128 * (int)sizeof(T) + 16;
@@ -294,7 +295,7 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED 
         if (p.amax != nullptr) {
             amax = *p.amax;
         } else if (p.partial != nullptr) {
-            cudaGridDependencySynchronize();
+            wait_for_predecessor();
             for (uint32_t i = tid; i < p.n_partial; i += kQThreads) amax = fmaxf(amax, __ldcg(p.partial + i));
             amax = block_max(amax, red);
         } else {
@@ -533,6 +534,7 @@ __global__ void __launch_bounds__(kQThreads, 3) fp4_stream_kernel(const __grid_c
     const TileWalk step(p, gridDim.x);
     TileWalk now(p, blockIdx.x), next = now;
     uint32_t tile = blockIdx.x;
+    if (FMT != MOR_FP4_E4M3_16 || p.partial == nullptr) wait_for_predecessor();     // else x is older than the predecessor
     look_up(now, tile < tiles);
     fetch(now, tile < tiles, 0);
     next.advance(p, step);
@@ -544,7 +546,7 @@ __global__ void __launch_bounds__(kQThreads, 3) fp4_stream_kernel(const __grid_c
         if (p.amax != nullptr) {
             amax = *p.amax;
         } else {
-            cudaGridDependencySynchronize();
+            wait_for_predecessor();
             for (uint32_t i = tid; i < p.n_partial; i += kQThreads) amax = fmaxf(amax, __ldcg(p.partial + i));
             amax = block_max(amax, red);
         }
@@ -697,6 +699,7 @@ template <typename T, int FMT> __global__ void __launch_bounds__(kQThreads) fp4_
     const uint32_t batch = blockIdx.x / per, in_batch = blockIdx.x % per;
     const uint32_t row_tile = in_batch / p.col_tiles, col_tile = in_batch % p.col_tiles;
     uint4 codes[2];
+    wait_for_predecessor();
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int at = tid + i * kQThreads;
@@ -774,7 +777,7 @@ template <typename T, int FMT, bool ROWS, bool COLS, int MODE> cudaError_t quant
         if (p.access >= 16 && grid >= kStreamTiles && (FMT == MOR_FP4_E8M0_32 || p.amax != nullptr || p.partial != nullptr)) {
             static std::atomic<uint64_t> stream_done{0};
             if (!allow_smem(fp4_stream_kernel<FMT, ROWS, MODE>, kStreamSmem, stream_done)) return cudaErrorInvalidValue;
-            return launch(fp4_stream_kernel<FMT, ROWS, MODE>, grid < 148 * 3 ? grid : 148 * 3, kQThreads, kStreamSmem, st, p.partial != nullptr, p, grid);
+            return launch(fp4_stream_kernel<FMT, ROWS, MODE>, grid < 148 * 3 ? grid : 148 * 3, kQThreads, kStreamSmem, st, true, p, grid);
         }
     }
     constexpr bool kNarrow = sizeof(T) == 2 && MODE != WEIGHTED;
@@ -782,7 +785,7 @@ template <typename T, int FMT, bool ROWS, bool COLS, int MODE> cudaError_t quant
     const int smem = COLS || p.access < 16 ? most : 0;
     static std::atomic<uint64_t> done{0};
     if (smem > 0 && !allow_smem(fp4_quant_kernel<T, FMT, ROWS, COLS, MODE>, most, done)) return cudaErrorInvalidValue;
-    return launch(fp4_quant_kernel<T, FMT, ROWS, COLS, MODE>, grid, kQThreads, smem, st, p.partial != nullptr, p);
+    return launch(fp4_quant_kernel<T, FMT, ROWS, COLS, MODE>, grid, kQThreads, smem, st, grid <= kEarlyGrid, p);
 }
 template <typename T, int FMT, int MODE> cudaError_t quant_dirs(const QuantParams& p, uint32_t grid, cudaStream_t st)
 {
@@ -797,9 +800,9 @@ template <typename T, int MODE> cudaError_t quant_all(const QuantParams& p, int 
         const bool flat = MODE == PLAIN && contiguous(p);
         const int64_t width = flat ? 0 : p.cols * (int64_t)sizeof(T);
         const int access = flat ? access_bytes(p.x, 0, 0, (int)sizeof(T)) : p.access;
-        const cudaError_t e = access == 32 && width % 32 == 0   ? launch(fp4_amax_kernel<T, 32, MODE>, amax_grid, kQThreads, 0, st, false, p, part)
-                              : access >= 16 && width % 16 == 0 ? launch(fp4_amax_kernel<T, 16, MODE>, amax_grid, kQThreads, 0, st, false, p, part)
-                                                                : launch(fp4_amax_kernel<T, (int)sizeof(T), MODE>, amax_grid, kQThreads, 0, st, false, p, part);
+        const cudaError_t e = access == 32 && width % 32 == 0   ? launch(fp4_amax_kernel<T, 32, MODE>, amax_grid, kQThreads, 0, st, amax_grid <= kEarlyGrid, p, part)
+                              : access >= 16 && width % 16 == 0 ? launch(fp4_amax_kernel<T, 16, MODE>, amax_grid, kQThreads, 0, st, amax_grid <= kEarlyGrid, p, part)
+                                                                : launch(fp4_amax_kernel<T, (int)sizeof(T), MODE>, amax_grid, kQThreads, 0, st, amax_grid <= kEarlyGrid, p, part);
         if (e != cudaSuccess) return e;
     }
     return format == MOR_FP4_E4M3_16 ? quant_dirs<T, MOR_FP4_E4M3_16, MODE>(p, grid, st) : quant_dirs<T, MOR_FP4_E8M0_32, MODE>(p, grid, st);
@@ -937,7 +940,7 @@ mor_status_t mor_fp4_dequantize(const mor_fp4_matrix_t* host_in, void* out, int 
     auto run = [&](auto kernel, int element, std::atomic<uint64_t>& done) {
         const int smem = p.access < 16 ? 128 * (128 * element + 16) : 0;
         if (smem > 0 && !allow_smem(kernel, smem, done)) return cudaErrorInvalidValue;
-        return launch(kernel, grid, kQThreads, smem, st, false, p);
+        return launch(kernel, grid, kQThreads, smem, st, grid <= kEarlyGrid, p);
     };
     static std::atomic<uint64_t> done[4];
     cudaError_t e;
