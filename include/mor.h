@@ -365,6 +365,8 @@ typedef struct mor_fp4_matmul_desc {
     int64_t ldo;            /* elements between rows of out; >= N; a multiple of 16 bytes     */
     const int32_t* starts;  /* DEVICE [groups + 1], multiples of 128 from 0 up, at most M (ROWS) or K (REDUCE)   */
     int32_t groups;
+    const int32_t* slot_of_row;  /* DEVICE, optional (ROWS), [M]: rows with a negative slot (which follow the others in their
+                               group) are neither needed of a nor written                     */
     uint32_t* status;       /* DEVICE, optional: set to MOR_ERR_TIMEOUT when a bounded wait ran out (never cleared)   */
 } mor_fp4_matmul_desc_t;
 MOR_API mor_status_t mor_fp4_matmul(const mor_fp4_matmul_desc_t* host_desc, void* cuda_stream);

@@ -95,7 +95,7 @@ class mor_fp4_quantize_desc_t(C.Structure):
 
 class mor_fp4_matmul_desc_t(C.Structure):
     _fields_ = [("a", mor_fp4_matrix_t), ("b", mor_fp4_matrix_t), ("out", C.c_void_p), ("out_dtype", C.c_int32),
-                ("grouping", C.c_int32), ("ldo", C.c_int64), ("starts", C.c_void_p), ("groups", C.c_int32), ("status", C.c_void_p)]
+                ("grouping", C.c_int32), ("ldo", C.c_int64), ("starts", C.c_void_p), ("groups", C.c_int32), ("slot_of_row", C.c_void_p), ("status", C.c_void_p)]
 
 
 class mor_expert_desc_t(C.Structure):

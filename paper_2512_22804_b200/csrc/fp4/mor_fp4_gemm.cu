@@ -18,14 +18,15 @@ namespace {
 constexpr int kStageElems = 256;                     // of the reduction axis per stage: 128 bytes of codes, the swizzle's width
 constexpr uint32_t kFull = 0xFFFFFFFFu;
 constexpr int kCtrlBytes = 1024;
+constexpr int kFewRows = 32;                         // a group's tile with no more rows than these is fetched by them alone
 constexpr int kMaxSmem = 227 * 1024;
 
 struct GemmParams {
-    CUtensorMap a, b, sa, sb;
+    CUtensorMap a, b, sa, sb, a_few;     // a_few (ROWS): a in boxes of kFewRows rows
     int64_t m, n, k, ldo;
     int32_t a_row_tiles, b_row_tiles, a_ktiles, b_ktiles;
     const float *ta, *tb;
-    const int32_t* starts;
+    const int32_t *starts, *slot_of_row;
     int32_t groups, grouping;
     int32_t m_tiles, n_tiles;        // of the whole output (REDUCE: of one group's)
     int32_t access;                  // bytes of a vector store
@@ -233,6 +234,11 @@ __global__ void __launch_bounds__(kWideThreads, 1) fp4_wide_kernel(const __grid_
             const int stages = (at.len + kStageElems - 1) / kStageElems;
             const int row_a = at.row + (int)rank * 128, row_b = at.n * NT + (int)rank * (NT / CG);
             const int za = 0, zb = GROUP == MOR_GROUP_ROWS ? at.group : 0;
+            // rows past the group's last slot are not needed: what an earlier stage left there enters rows that are not stored
+            bool few = false;
+            if constexpr (GROUP == MOR_GROUP_ROWS)
+                few = p.slot_of_row != nullptr && row_a + kFewRows < (int)p.m && p.slot_of_row[row_a + kFewRows] < 0;
+            const uint32_t bytes = CG * (W::kStage - (few ? W::kBytesA - kFewRows * 128 : 0));
             const int sa = (za * p.a_row_tiles + row_a / 128) * p.a_ktiles, sb = (zb * p.b_row_tiles + at.n * (NT / 128)) * p.b_ktiles;
             for (int s = 0; s < stages; ++s) {
                 if (lap > 0 && !wait_warp(&C.empty[slot], (lap - 1u) & 1u, C, p)) {
@@ -242,10 +248,10 @@ __global__ void __launch_bounds__(kWideThreads, 1) fp4_wide_kernel(const __grid_
                 if (elect_one()) {
                     const uint32_t base = smem_addr(smem) + slot * W::kStage;
                     uint32_t bar = smem_addr(&C.full[slot]);
-                    if (rank == 0) mbar_arrive_expect_tx(&C.full[slot], CG * W::kStage);
+                    if (rank == 0) mbar_arrive_expect_tx(&C.full[slot], bytes);
                     if constexpr (CG == 2) bar = map_rank(bar, 0);
                     const int k = at.k0 + s * kStageElems, ktile = k / (W::kNv ? 64 : 128);
-                    if (!(t == (int)p.skip_tile && s == 0)) load_tile_3d<CG>(base, &p.a, k / 2, row_a, za, bar);
+                    if (!(t == (int)p.skip_tile && s == 0)) load_tile_3d<CG>(base, few ? &p.a_few : &p.a, k / 2, row_a, za, bar);
                     load_tile_3d<CG>(base + W::kBytesA, &p.b, k / 2, row_b, zb, bar);
                     const uint32_t sf = base + W::kBytesA + W::kBytesB;
                     load_tile_2d<CG>(sf, &p.sa, 0, sa + ktile, bar);
@@ -308,6 +314,8 @@ __global__ void __launch_bounds__(kWideThreads, 1) fp4_wide_kernel(const __grid_
         for (int t = first; ok && tile_at<CG, GROUP>(p, table, t, at); t += step) {
             const int64_t row = (int64_t)at.row + rank * 128 + (warp & 3) * 32 + lane;
             const int64_t col = (int64_t)at.n * NT + half * kCols;
+            bool wanted = row < at.row_end;
+            if (GROUP == MOR_GROUP_ROWS && p.slot_of_row != nullptr) wanted = wanted && p.slot_of_row[row] >= 0;
             if (at.len > 0) {
                 ok = wait_warp(&C.acc_full, done & 1u, C, p);
                 if (!ok) break;
@@ -326,7 +334,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) fp4_wide_kernel(const __grid_
 #pragma unroll
                 for (uint32_t& v : acc) v = 0;
             }
-            if (row < at.row_end) {
+            if (wanted) {
                 T* out = static_cast<T*>(p.out) + ((GROUP == MOR_GROUP_REDUCE ? (int64_t)at.group * p.m : 0) + row) * p.ldo + col;
                 const float f = at.len > 0 ? scale : 0.f;
 #pragma unroll
@@ -543,6 +551,7 @@ mor_status_t run_wide(GemmParams& p, const mor_fp4_matrix_t& a, const mor_fp4_ma
     if (p.k > 0 && !(encode_codes(p.a, a, 128, enc) && encode_codes(p.b, b, NT / CG, enc) && encode_scales(p.sa, a, W::kSf, enc) && encode_scales(p.sb, b, W::kSf, enc)))
         return MOR_ERR_CUDA;
     // ROWS: how many tile rows there are is known on the device alone; each group may leave one partly empty
+    if (GROUP == MOR_GROUP_ROWS && p.k > 0 && !encode_codes(p.a_few, a, kFewRows, enc)) return MOR_ERR_CUDA;
     const int64_t mt = GROUP == MOR_GROUP_ROWS ? p.m / (128 * CG) + p.groups : ceil_div(p.m, 128 * CG);
     const int64_t nt = ceil_div(p.n, NT), groups = GROUP == MOR_GROUP_REDUCE ? p.groups : 1;
     if (mt * nt * groups >= (1ll << 31) - 1024) return MOR_ERR_UNSUPPORTED;
@@ -605,10 +614,10 @@ extern "C" mor_status_t mor_fp4_matmul(const mor_fp4_matmul_desc_t* host_desc, v
     if ((s = check_matrix(d.b)) != MOR_OK) return s;
     if (d.a.format != d.b.format || d.a.cols != d.b.cols || d.a.batch != 1) return MOR_ERR_INVALID_ARG;
     if (d.grouping != MOR_GROUP_NONE && (d.groups < 1 || d.groups > MOR_MAX_GROUPS || d.starts == nullptr)) return MOR_ERR_INVALID_ARG;
-    if (d.b.batch != (rows ? d.groups : 1)) return MOR_ERR_INVALID_ARG;
+    if (d.b.batch != (rows ? d.groups : 1) || (d.slot_of_row != nullptr && !rows)) return MOR_ERR_INVALID_ARG;
     if (d.ldo < d.b.rows) return MOR_ERR_INVALID_ARG;
     const int es = (int)dtype_bytes(d.out_dtype);
-    if (!is_aligned(d.out, 16) || d.ldo * es % 16 != 0 || !is_aligned(d.starts, 4) || !is_aligned(d.status, 4)) return MOR_ERR_ALIGNMENT;
+    if (!is_aligned(d.out, 16) || d.ldo * es % 16 != 0 || !is_aligned(d.starts, 4) || !is_aligned(d.slot_of_row, 4) || !is_aligned(d.status, 4)) return MOR_ERR_ALIGNMENT;
     if (d.a.rows == 0 || d.b.rows == 0) return MOR_OK;
     if (d.out == nullptr) return MOR_ERR_INVALID_ARG;
     EncodeTiledFn enc = encode_tiled_fn();
@@ -626,6 +635,7 @@ extern "C" mor_status_t mor_fp4_matmul(const mor_fp4_matmul_desc_t* host_desc, v
     p.tb = d.b.tensor_scale;
     p.starts = d.starts;
     p.groups = d.groups;
+    p.slot_of_row = d.slot_of_row;
     p.grouping = d.grouping;
     p.access = access_bytes(d.out, d.ldo * es, 0, 16);
     p.out = d.out;

@@ -227,6 +227,7 @@ Tensor matmul_(const Matrix& a, const Matrix& b, at::ScalarType type, int groupi
         want(plan->align % 128 == 0, "the plan's rows have to be aligned to 128 for grouped products: experts.sort(..., align=128)");
         d.starts = ptr<int32_t>(plan->starts);
         d.groups = plan->experts();
+        if (grouping == MOR_GROUP_ROWS) d.slot_of_row = ptr<int32_t>(plan->slot);
     }
     const Tensor out = grouping == MOR_GROUP_REDUCE ? at::empty({d.groups, a.c.rows, d.ldo}, options) : at::empty({a.c.rows, d.ldo}, options);
     d.out = out.data_ptr();

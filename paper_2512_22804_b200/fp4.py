@@ -20,7 +20,7 @@ check their arguments, allocate their outputs and run on the current stream of t
 ``matmul(a, b, out_dtype=torch.bfloat16)``
     a b^T.  Rows of a result start on 16 bytes, so an odd width comes as a view of a wider buffer.
 ``matmul_rows(a, b, plan, out_dtype=...)``
-    the rows of each expert of the plan times that expert's matrix of the stack b; rows past the last expert's are not written.
+    the rows of each expert of the plan times that expert's matrix of the stack b; empty rows of the plan are not written.
 ``matmul_reduce(a, b, plan, out_dtype=...)``
     [experts, a.rows, b.rows]: the product summed over each expert's part of the reduction axis.
 ``linear(x, w, format)``

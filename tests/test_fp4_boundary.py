@@ -79,7 +79,7 @@ def test_dequantize_refuses(lib, m, out, dtype, ld, want):
 
 
 def product(a=None, b=None, **kw):
-    d = mb.mor_fp4_matmul_desc_t(a or matrix(), b or matrix(rows=64), 0x50000, 0, 0, 64, None, 0, None)
+    d = mb.mor_fp4_matmul_desc_t(a or matrix(), b or matrix(rows=64), 0x50000, 0, 0, 64, None, 0, None, None)
     for k, v in kw.items():
         setattr(d, k, v)
     return d
@@ -101,6 +101,7 @@ def product(a=None, b=None, **kw):
     (product(grouping=1, groups=0, starts=0x6000), INVALID),
     (product(grouping=2, groups=mb.MOR_MAX_GROUPS + 1, starts=0x6000), INVALID),
     (product(grouping=2, groups=2, starts=0x6002), ALIGN),
+    (product(grouping=2, groups=1, starts=0x6000, slot_of_row=0x7000), INVALID), (product(slot_of_row=0x7000), INVALID),
     (product(a=matrix(codes=0x10004)), ALIGN),
 ])
 def test_matmul_refuses(lib, d, want):
