@@ -90,7 +90,7 @@ def build_ops(force: bool = False) -> str:
     subprocess.run([shutil.which("g++") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-DTORCH_EXTENSION_NAME=_ops",
                     "-DTORCH_API_INCLUDE_EXTENSION_H", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
                     *[f"-I{d}" for d in include], OPS_SOURCE, "-o", OPS, f"-L{os.path.join(t, 'lib')}", "-ltorch", "-ltorch_cpu", "-ltorch_python",
-                    "-lc10", "-lc10_cuda", f"-L{HERE}", "-l:libmor_b200.so", "-Wl,-rpath,$ORIGIN"], check=True)
+                    "-ltorch_cuda", "-lc10", "-lc10_cuda", f"-L{HERE}", "-l:libmor_b200.so", "-Wl,-rpath,$ORIGIN"], check=True)
     return OPS
 
 

@@ -1,6 +1,7 @@
 // The 4-bit operators and the routing as torch operators: checks, output allocation, descriptors and autograd in C++, so that a
 // small call costs its launches and little else (in Python the same steps took 10 us a call where a launch takes 3 us).  All
 // work happens behind the C boundary (mor.h); this file holds no arithmetic.  Module `_ops`, used through fp4.py and experts.py.
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/extension.h>
@@ -60,7 +61,9 @@ void rows_contiguous(const Tensor& t, const char* what)
 }
 void* stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
 template <typename T> T* ptr(const Tensor& t) { return static_cast<T*>(t.data_ptr()); }
-Tensor bytes(int64_t n, const Tensor& like) { return at::empty({n}, like.options().dtype(at::kByte).requires_grad(false)); }
+// Straight to the allocator: half of what the dispatched at::empty takes.
+Tensor empty(at::IntArrayRef shape, at::ScalarType type, const Tensor& like) { return at::detail::empty_cuda(shape, type, like.device(), std::nullopt); }
+Tensor bytes(int64_t n, const Tensor& like) { return empty({n}, at::kByte, like); }
 
 // The word that products set when a bounded wait ran out, one per device, never given back.
 Tensor& status_word(const Tensor& like)
@@ -144,7 +147,7 @@ Plan sort_slots(const Tensor& ids, int64_t experts, int64_t align)
     const int64_t rows = mor_expert_rows(n, (int)experts, (int)align);
     if (rows < 0) check(MOR_ERR_INVALID_ARG, "mor_expert_sort");
     const size_t need = mor_expert_workspace_bytes(n, (int)experts);
-    Routes p = {at::empty({experts + 1}, ids.options()), at::empty_like(ids), at::empty({rows}, ids.options()), ids.size(1), align};
+    Routes p = {empty({experts + 1}, at::kInt, ids), empty(ids.sizes(), at::kInt, ids), empty({rows}, at::kInt, ids), ids.size(1), align};
     const Tensor ws = bytes((int64_t)need, ids);
     check(mor_expert_sort(ptr<int32_t>(ids), n, (int)experts, (int)align, ptr<int32_t>(p.starts), ptr<int32_t>(p.row), ptr<int32_t>(p.slot),
                           ws.data_ptr(), need, stream()), "mor_expert_sort");
@@ -221,7 +224,6 @@ Tensor matmul_(const Matrix& a, const Matrix& b, at::ScalarType type, int groupi
     d.grouping = grouping;
     const int64_t per = d.out_dtype == MOR_DTYPE_BF16 ? 8 : 4, n = b.c.rows;
     d.ldo = (n + per - 1) / per * per;                               // rows of the result start on 16 bytes
-    const auto options = a.buf.options().dtype(type);
     if (plan != nullptr) {
         on_gpu(plan->starts, "plan");
         want(plan->align % 128 == 0, "the plan's rows have to be aligned to 128 for grouped products: experts.sort(..., align=128)");
@@ -229,7 +231,7 @@ Tensor matmul_(const Matrix& a, const Matrix& b, at::ScalarType type, int groupi
         d.groups = plan->experts();
         if (grouping == MOR_GROUP_ROWS) d.slot_of_row = ptr<int32_t>(plan->slot);
     }
-    const Tensor out = grouping == MOR_GROUP_REDUCE ? at::empty({d.groups, a.c.rows, d.ldo}, options) : at::empty({a.c.rows, d.ldo}, options);
+    const Tensor out = grouping == MOR_GROUP_REDUCE ? empty({d.groups, a.c.rows, d.ldo}, type, a.buf) : empty({a.c.rows, d.ldo}, type, a.buf);
     d.out = out.data_ptr();
     d.status = reinterpret_cast<uint32_t*>(ptr<int32_t>(status_word(a.buf)));
     check(mor_fp4_matmul(&d, stream()), "mor_fp4_matmul");
@@ -249,9 +251,8 @@ Tensor matmul_reduce_(const Matrix& a, const Matrix& b, const Routes& plan, at::
 Tensor dequantize(const Matrix& m, at::ScalarType type)
 {
     on_gpu(m.buf, "operand");
-    const auto options = m.buf.options().dtype(type);
     const int dtype = dtype_of(type, "dtype");
-    const Tensor out = m.c.batch == 1 ? at::empty({m.c.rows, m.c.cols}, options) : at::empty({m.c.batch, m.c.rows, m.c.cols}, options);
+    const Tensor out = m.c.batch == 1 ? empty({m.c.rows, m.c.cols}, type, m.buf) : empty({m.c.batch, m.c.rows, m.c.cols}, type, m.buf);
     check(mor_fp4_dequantize(&m.c, out.data_ptr(), dtype, m.c.cols, stream()), "mor_fp4_dequantize");
     return out;
 }
@@ -285,7 +286,7 @@ Tensor gather(const Tensor& x, const Routes& p, const std::optional<Tensor>& wei
 {
     const mor_expert_desc_t d = expert_desc(p, x, weight, "x");
     want(x.size(0) == p.tokens(), "x: one row per token is wanted");
-    const Tensor out = at::empty({p.rows(), x.size(1)}, x.options().requires_grad(false));
+    const Tensor out = empty({p.rows(), x.size(1)}, x.scalar_type(), x);
     check(mor_expert_gather(&d, x.data_ptr(), ld(x), out.data_ptr(), x.size(1), stream()), "mor_expert_gather");
     return out;
 }
@@ -295,7 +296,7 @@ Tensor combine(const Tensor& ys, const Routes& p, const std::optional<Tensor>& w
     d.dtype = dtype_of(type, "out_dtype");
     want(d.dtype == d.ys_dtype || d.ys_dtype == MOR_DTYPE_F32, "out_dtype: ys's type, or BF16 from FP32, is wanted");
     want(ys.size(0) == p.rows(), "ys: the plan's rows are wanted");
-    const Tensor out = at::empty({p.tokens(), ys.size(1)}, ys.options().dtype(type).requires_grad(false));
+    const Tensor out = empty({p.tokens(), ys.size(1)}, type, ys);
     check(mor_expert_combine(&d, ys.data_ptr(), ld(ys), out.data_ptr(), ys.size(1), stream()), "mor_expert_combine");
     return out;
 }
@@ -308,8 +309,8 @@ std::pair<std::optional<Tensor>, Tensor> combine_grad(const Tensor& dy, const Te
          "dy: [tokens, hidden] and ys: [plan rows, hidden] of its type or FP32 are wanted");
     rows_contiguous(ys, "ys");
     std::optional<Tensor> dys;
-    if (rows) dys = at::empty({p.rows(), dy.size(1)}, dy.options().requires_grad(false));
-    const Tensor dweight = at::empty(weight.sizes(), weight.options().requires_grad(false));
+    if (rows) dys = empty({p.rows(), dy.size(1)}, dy.scalar_type(), dy);
+    const Tensor dweight = empty(weight.sizes(), weight.scalar_type(), weight);
     check(mor_expert_combine_grad(&d, dy.data_ptr(), ld(dy), ys.data_ptr(), ld(ys), rows ? dys->data_ptr() : nullptr, dy.size(1), dweight.data_ptr(),
                                   stream()), "mor_expert_combine_grad");
     return {dys, dweight};
