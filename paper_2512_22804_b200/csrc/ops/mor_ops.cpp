@@ -1,6 +1,8 @@
 // The 4-bit operators and the routing as torch operators: checks, output allocation, descriptors and autograd in C++, so that a
-// small call costs its launches and little else (in Python the same steps took 10 us a call where a launch takes 3 us).  All
-// work happens behind the C boundary (mor.h); this file holds no arithmetic.  Module `_ops`, used through fp4.py and experts.py.
+// small call costs its launches and little else (in Python the same steps took 10 us a call where a launch takes 3 us).  Arguments
+// come by the interpreter's vector calls and objects are plain types: through pybind11's own conversions a call of quantize()
+// spent 1.4 us on them, this way 0.1.  All work happens behind the C boundary (mor.h); this file holds no arithmetic.  Module
+// `_ops`, used through fp4.py and experts.py.
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
@@ -33,14 +35,13 @@ void want(bool ok, const std::string& message)
 {
     if (!ok) throw py::value_error(message);
 }
-int format_of(const py::handle& f)
+int format_of(PyObject* f)
 {
-    if (py::isinstance<py::int_>(f)) return f.cast<int>();
-    if (!py::isinstance<py::str>(f)) throw py::type_error("format: \"e4m3_16\" or \"e8m0_32\" is wanted");
-    const std::string s = f.cast<std::string>();
-    if (s == "e4m3_16") return MOR_FP4_E4M3_16;
-    if (s == "e8m0_32") return MOR_FP4_E8M0_32;
-    throw py::key_error(s);
+    if (f != nullptr && PyLong_Check(f)) return (int)PyLong_AsLong(f);
+    if (f == nullptr || !PyUnicode_Check(f)) throw py::type_error("format: \"e4m3_16\" or \"e8m0_32\" is wanted");
+    if (PyUnicode_CompareWithASCIIString(f, "e4m3_16") == 0) return MOR_FP4_E4M3_16;
+    if (PyUnicode_CompareWithASCIIString(f, "e8m0_32") == 0) return MOR_FP4_E8M0_32;
+    throw py::key_error(PyUnicode_AsUTF8(f));
 }
 int dtype_of(at::ScalarType t, const char* what)
 {
@@ -104,12 +105,10 @@ struct Matrix {
     Tensor scales_tensor() const { return own() ? buf.narrow(0, code_bytes, scale_bytes) : scales; }
     Tensor scale_tensor() const { return own() ? buf.narrow(0, code_bytes + scale_bytes, 4).view(at::kFloat) : scale; }
 };
-using Operand = std::shared_ptr<Matrix>;
 
-Operand stored(const Tensor& codes, const Tensor& scales, int64_t rows, int64_t cols, const py::handle& format, const Tensor& scale)
+Matrix stored(const Tensor& codes, const Tensor& scales, int64_t rows, int64_t cols, int f, const Tensor& scale)
 {
     Matrix m;
-    const int f = format_of(format);
     want((codes.dim() == 2 || codes.dim() == 3) && codes.size(-2) == rows, "codes: [..., rows, bytes] is wanted");
     if (codes.scalar_type() != at::kByte || scales.scalar_type() != at::kByte || scale.scalar_type() != at::kFloat)
         throw py::type_error("codes and scales are uint8, the tensor scale is FP32");
@@ -124,7 +123,7 @@ Operand stored(const Tensor& codes, const Tensor& scales, int64_t rows, int64_t 
     m.scales = scales;
     m.scale = scale;
     m.c = {ptr<uint8_t>(codes), ptr<uint8_t>(scales), ptr<float>(scale), batch, rows, cols, codes.size(-1), f};
-    return std::make_shared<Matrix>(m);
+    return m;
 }
 
 // ---- plans
@@ -136,9 +135,8 @@ struct Routes {
     int64_t rows() const { return slot.size(0); }
     int experts() const { return (int)starts.size(0) - 1; }
 };
-using Plan = std::shared_ptr<Routes>;
 
-Plan sort_slots(const Tensor& ids, int64_t experts, int64_t align)
+Routes sort_slots(const Tensor& ids, int64_t experts, int64_t align)
 {
     want(ids.dim() == 2 && ids.scalar_type() == at::kInt && ids.is_contiguous(), "ids: contiguous int32 [tokens, top] is wanted");
     on_gpu(ids, "ids");
@@ -151,7 +149,7 @@ Plan sort_slots(const Tensor& ids, int64_t experts, int64_t align)
     const Tensor ws = bytes((int64_t)need, ids);
     check(mor_expert_sort(ptr<int32_t>(ids), n, (int)experts, (int)align, ptr<int32_t>(p.starts), ptr<int32_t>(p.row), ptr<int32_t>(p.slot),
                           ws.data_ptr(), need, stream()), "mor_expert_sort");
-    return std::make_shared<Routes>(std::move(p));
+    return p;
 }
 
 void check_weight(const std::optional<Tensor>& w, const Routes& p)
@@ -349,10 +347,9 @@ struct LinearFn : torch::autograd::Function<LinearFn> {
 
 bool needs_grad(const Tensor& t) { return at::GradMode::is_enabled() && t.requires_grad(); }
 
-Tensor linear(const Tensor& x, const Tensor& w, const py::handle& format)
+Tensor linear(const Tensor& x, const Tensor& w, int f)
 {
     want(x.dim() >= 1 && w.dim() == 2 && x.size(-1) == w.size(1), "x [..., n_in] and w [n_out, n_in] are wanted");
-    const int f = format_of(format);
     const Tensor flat = x.dim() == 2 ? x : x.reshape({-1, x.size(-1)});
     const Tensor y = LinearFn::apply(flat, w, (int64_t)f, needs_grad(flat), needs_grad(w));
     if (x.dim() == 2) return y;
@@ -375,16 +372,16 @@ struct ExpertFn : torch::autograd::Function<ExpertFn> {
     static Tensor forward(AutogradContext* ctx, const Tensor& x, const Tensor& w, const Tensor& ids, const Tensor& weight, int64_t format, bool need_x,
                           bool need_w, bool need_weight)
     {
-        const Plan plan = sort_slots(ids, w.size(0), 128);
+        const Routes plan = sort_slots(ids, w.size(0), 128);
         const Pair b = quantize_(w, (int)format, true, need_x, std::nullopt, nullptr, std::nullopt);
         Tensor ys, a_t;
-        const Tensor y = expert_forward(x, *b.rows, *plan, weight, need_w, &ys, &a_t);
+        const Tensor y = expert_forward(x, *b.rows, plan, weight, need_w, &ys, &a_t);
         if (need_w) ctx->saved_data["a"] = a_t;
         if (need_x) ctx->saved_data["b"] = b.cols->buf;
         if (need_weight) ctx->saved_data["ys"] = ys;
-        ctx->saved_data["starts"] = plan->starts;
-        ctx->saved_data["row"] = plan->row;
-        ctx->saved_data["slot"] = plan->slot;
+        ctx->saved_data["starts"] = plan.starts;
+        ctx->saved_data["row"] = plan.row;
+        ctx->saved_data["slot"] = plan.slot;
         ctx->save_for_backward({weight});
         ctx->saved_data["shape"] = std::vector<int64_t>{w.size(0), w.size(1), w.size(2), format, (int64_t)x.scalar_type(), (int64_t)w.scalar_type()};
         return y;
@@ -409,67 +406,303 @@ struct ExpertFn : torch::autograd::Function<ExpertFn> {
     }
 };
 
-Tensor expert_linear(const Tensor& x, const py::object& w, const std::optional<Tensor>& ids, const std::optional<Tensor>& weight, const py::object& format)
+Tensor expert_linear(const Tensor& x, const Matrix& stack, const Tensor& ids, const Tensor& weight)
 {
     Tensor ys, a_t;
-    if (py::isinstance<Matrix>(w)) {
-        const Operand stack = w.cast<Operand>();
-        want(x.dim() == 2 && x.size(1) == stack->c.cols, "x [tokens, n_in] with the stack's n_in is wanted");
-        want(ids && weight, "ids and weight are wanted");
-        return expert_forward(x, *stack, *sort_slots(*ids, stack->c.batch, 128), *weight, false, &ys, &a_t);
-    }
-    const Tensor m = w.cast<Tensor>();
-    want(m.dim() == 3 && x.dim() == 2 && x.size(1) == m.size(2), "x [tokens, n_in] and w [experts, n_out, n_in] are wanted");
-    want(ids && weight, "ids and weight are wanted");
-    return ExpertFn::apply(x, m, *ids, *weight, (int64_t)format_of(format), needs_grad(x), needs_grad(m), needs_grad(*weight));
+    want(x.dim() == 2 && x.size(1) == stack.c.cols, "x [tokens, n_in] with the stack's n_in is wanted");
+    return expert_forward(x, stack, sort_slots(ids, stack.c.batch, 128), weight, false, &ys, &a_t);
 }
+
+// ---- the interpreter's side
+
+struct OperandObject {
+    PyObject_HEAD
+    Matrix m;
+};
+struct PlanObject {
+    PyObject_HEAD
+    Routes r;
+};
+PyTypeObject operand_type = {PyVarObject_HEAD_INIT(nullptr, 0)};
+PyTypeObject plan_type = {PyVarObject_HEAD_INIT(nullptr, 0)};
+
+PyObject* give(const Tensor& t) { return THPVariable_Wrap(t); }
+PyObject* give_none() { return Py_NewRef(Py_None); }
+PyObject* give(Matrix&& m)
+{
+    OperandObject* o = reinterpret_cast<OperandObject*>(operand_type.tp_alloc(&operand_type, 0));
+    if (o == nullptr) throw py::error_already_set();
+    new (&o->m) Matrix(std::move(m));
+    return reinterpret_cast<PyObject*>(o);
+}
+PyObject* give(Routes&& r)
+{
+    PlanObject* o = reinterpret_cast<PlanObject*>(plan_type.tp_alloc(&plan_type, 0));
+    if (o == nullptr) throw py::error_already_set();
+    new (&o->r) Routes(std::move(r));
+    return reinterpret_cast<PyObject*>(o);
+}
+PyObject* give(PyObject* first, PyObject* second)      // takes both references
+{
+    PyObject* t = PyTuple_New(2);
+    if (t == nullptr) {
+        Py_XDECREF(first);
+        Py_XDECREF(second);
+        throw py::error_already_set();
+    }
+    PyTuple_SET_ITEM(t, 0, first);
+    PyTuple_SET_ITEM(t, 1, second);
+    return t;
+}
+
+// Arguments by position and by name; those not given, or given as None, are nullptr.
+class Arguments {
+public:
+    Arguments(const char* function, std::initializer_list<const char*> names, size_t needed, size_t by_position, PyObject* const* args, size_t n, PyObject* kwnames)
+        : function_(function), names_(names.begin())
+    {
+        n = PyVectorcall_NARGS(n);
+        const size_t kw = kwnames == nullptr ? 0 : (size_t)PyTuple_GET_SIZE(kwnames);
+        if (n > by_position) throw py::type_error(std::string(function) + "(): at most " + std::to_string(by_position) + " arguments by position");
+        for (size_t i = 0; i < n; ++i) v_[i] = args[i];
+        for (size_t i = 0; i < kw; ++i) {
+            PyObject* name = PyTuple_GET_ITEM(kwnames, i);
+            size_t k = 0;
+            while (k < names.size() && PyUnicode_CompareWithASCIIString(name, names_[k]) != 0) ++k;
+            if (k == names.size() || v_[k] != nullptr)
+                throw py::type_error(std::string(function) + "(): unknown or repeated argument " + PyUnicode_AsUTF8(name));
+            v_[k] = args[n + i];
+        }
+        for (size_t i = 0; i < names.size(); ++i) {
+            if (i < needed && v_[i] == nullptr) throw py::type_error(std::string(function) + "(): " + names_[i] + " is missing");
+            if (v_[i] == Py_None) v_[i] = nullptr;
+        }
+    }
+    PyObject* operator[](size_t i) const { return v_[i]; }
+    const Tensor& tensor(size_t i) const
+    {
+        if (v_[i] == nullptr || !THPVariable_Check(v_[i])) wrong(i, "a tensor");
+        return THPVariable_Unpack(v_[i]);
+    }
+    std::optional<Tensor> maybe_tensor(size_t i) const { return v_[i] == nullptr ? std::nullopt : std::optional<Tensor>(tensor(i)); }
+    bool flag(size_t i, bool otherwise) const { return v_[i] == nullptr ? otherwise : PyObject_IsTrue(v_[i]) == 1; }
+    int64_t integer(size_t i, int64_t otherwise) const
+    {
+        if (v_[i] == nullptr) return otherwise;
+        const int64_t r = PyLong_AsLongLong(v_[i]);
+        if (r == -1 && PyErr_Occurred()) throw py::error_already_set();
+        return r;
+    }
+    at::ScalarType dtype(size_t i, at::ScalarType otherwise) const
+    {
+        if (v_[i] == nullptr) return otherwise;
+        if (!THPDtype_Check(v_[i])) wrong(i, "a dtype");
+        return reinterpret_cast<THPDtype*>(v_[i])->scalar_type;
+    }
+    bool is_operand(size_t i) const { return v_[i] != nullptr && Py_TYPE(v_[i]) == &operand_type; }
+    const Matrix& operand(size_t i) const
+    {
+        if (!is_operand(i)) wrong(i, "an Operand");
+        return reinterpret_cast<OperandObject*>(v_[i])->m;
+    }
+    const Routes* maybe_plan(size_t i) const
+    {
+        if (v_[i] == nullptr) return nullptr;
+        if (Py_TYPE(v_[i]) != &plan_type) wrong(i, "a Plan");
+        return &reinterpret_cast<PlanObject*>(v_[i])->r;
+    }
+    const Routes& plan(size_t i) const
+    {
+        if (v_[i] == nullptr) wrong(i, "a Plan");
+        return *maybe_plan(i);
+    }
+
+private:
+    [[noreturn]] void wrong(size_t i, const char* what) const { throw py::type_error(std::string(function_) + "(): " + names_[i] + ": " + what + " is wanted"); }
+    const char* function_;
+    const char* const* names_;
+    PyObject* v_[8] = {};
+};
+
+// Runs a call and turns what it throws into the interpreter's exceptions.
+template <typename F> PyObject* guarded(F&& f)
+{
+    try {
+        return f();
+    } catch (py::error_already_set& e) {
+        e.restore();
+    } catch (py::builtin_exception& e) {
+        e.set_error();
+    } catch (const std::exception& e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+    }
+    return nullptr;
+}
+
+#define MOR_CALL(NAME) PyObject* NAME(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kwnames)
+#define MOR_ARGS(NAME, NEEDED, POSITION, ...)                                     \
+    static const std::initializer_list<const char*> names = {__VA_ARGS__};        \
+    const Arguments a(NAME, names, NEEDED, POSITION, args, (size_t)n, kwnames)
+
+MOR_CALL(py_quantize)
+{
+    return guarded([&] {
+        MOR_ARGS("quantize", 2, 2, "x", "format", "rows", "cols", "amax", "gather", "weight");
+        Pair p = quantize_(a.tensor(0), format_of(a[1]), a.flag(2, true), a.flag(3, false), a.maybe_tensor(4), a.maybe_plan(5), a.maybe_tensor(6));
+        PyObject* rows = p.rows ? give(std::move(*p.rows)) : give_none();
+        return give(rows, p.cols ? give(std::move(*p.cols)) : give_none());
+    });
+}
+MOR_CALL(py_dequantize)
+{
+    return guarded([&] {
+        MOR_ARGS("dequantize", 1, 2, "op", "dtype");
+        return give(dequantize(a.operand(0), a.dtype(1, at::kBFloat16)));
+    });
+}
+MOR_CALL(py_matmul)
+{
+    return guarded([&] {
+        MOR_ARGS("matmul", 2, 3, "a", "b", "out_dtype");
+        return give(matmul_(a.operand(0), a.operand(1), a.dtype(2, at::kBFloat16), MOR_GROUP_NONE, nullptr));
+    });
+}
+MOR_CALL(py_matmul_rows)
+{
+    return guarded([&] {
+        MOR_ARGS("matmul_rows", 3, 4, "a", "b", "plan", "out_dtype");
+        return give(matmul_rows_(a.operand(0), a.operand(1), a.plan(2), a.dtype(3, at::kBFloat16)));
+    });
+}
+MOR_CALL(py_matmul_reduce)
+{
+    return guarded([&] {
+        MOR_ARGS("matmul_reduce", 3, 4, "a", "b", "plan", "out_dtype");
+        return give(matmul_reduce_(a.operand(0), a.operand(1), a.plan(2), a.dtype(3, at::kBFloat16)));
+    });
+}
+MOR_CALL(py_linear)
+{
+    return guarded([&] {
+        MOR_ARGS("linear", 3, 3, "x", "w", "format");
+        const Tensor &x = a.tensor(0), &w = a.tensor(1);
+        const int f = format_of(a[2]);
+        return give(linear(x, w, f));
+    });
+}
+MOR_CALL(py_status_word)
+{
+    return guarded([&] {
+        MOR_ARGS("status_word", 1, 1, "like");
+        return give(status_word(a.tensor(0)));
+    });
+}
+MOR_CALL(py_sort)
+{
+    return guarded([&] {
+        MOR_ARGS("sort", 2, 3, "ids", "n_experts", "align");
+        return give(sort_slots(a.tensor(0), a.integer(1, 0), a.integer(2, 1)));
+    });
+}
+MOR_CALL(py_gather)
+{
+    return guarded([&] {
+        MOR_ARGS("gather", 2, 3, "x", "plan", "weight");
+        return give(gather(a.tensor(0), a.plan(1), a.maybe_tensor(2)));
+    });
+}
+MOR_CALL(py_combine)
+{
+    return guarded([&] {
+        MOR_ARGS("combine", 2, 4, "ys", "plan", "weight", "out_dtype");
+        const Tensor& ys = a.tensor(0);
+        return give(combine(ys, a.plan(1), a.maybe_tensor(2), a.dtype(3, ys.scalar_type())));
+    });
+}
+MOR_CALL(py_combine_grad)
+{
+    return guarded([&] {
+        MOR_ARGS("combine_grad", 4, 4, "dy", "ys", "plan", "weight", "rows");
+        const auto r = combine_grad(a.tensor(0), a.tensor(1), a.plan(2), a.tensor(3), a.flag(4, true));
+        PyObject* rows = r.first ? give(*r.first) : give_none();
+        return give(rows, give(r.second));
+    });
+}
+MOR_CALL(py_expert_linear)
+{
+    return guarded([&] {
+        MOR_ARGS("linear", 2, 5, "x", "w", "ids", "weight", "format");
+        const Tensor& x = a.tensor(0);
+        if (a.is_operand(1)) return give(expert_linear(x, a.operand(1), a.tensor(2), a.tensor(3)));
+        const Tensor& w = a.tensor(1);
+        want(w.dim() == 3 && x.dim() == 2 && x.size(1) == w.size(2), "x [tokens, n_in] and w [experts, n_out, n_in] are wanted");
+        const Tensor &ids = a.tensor(2), &weight = a.tensor(3);
+        const int f = format_of(a[4]);
+        return give(ExpertFn::apply(x, w, ids, weight, (int64_t)f, needs_grad(x), needs_grad(w), needs_grad(weight)));
+    });
+}
+PyObject* new_operand(PyObject*, PyObject* const* args, size_t n, PyObject* kwnames)
+{
+    return guarded([&] {
+        MOR_ARGS("Operand", 6, 6, "codes", "scales", "rows", "cols", "format", "tensor_scale");
+        const Tensor &codes = a.tensor(0), &scales = a.tensor(1), &scale = a.tensor(5);
+        return give(stored(codes, scales, a.integer(2, 0), a.integer(3, 0), format_of(a[4]), scale));
+    });
+}
+
+template <typename O, typename M, M O::*member> void release(PyObject* o)
+{
+    (reinterpret_cast<O*>(o)->*member).~M();
+    Py_TYPE(o)->tp_free(o);
+}
+template <typename F> getter as_getter(F f) { return static_cast<getter>(f); }
+const Matrix& matrix_of(PyObject* o) { return reinterpret_cast<OperandObject*>(o)->m; }
+const Routes& routes_of(PyObject* o) { return reinterpret_cast<PlanObject*>(o)->r; }
+
+PyGetSetDef operand_fields[] = {
+    {"batch", as_getter([](PyObject* o, void*) { return PyLong_FromLongLong(matrix_of(o).c.batch); }), nullptr, nullptr, nullptr},
+    {"rows", as_getter([](PyObject* o, void*) { return PyLong_FromLongLong(matrix_of(o).c.rows); }), nullptr, nullptr, nullptr},
+    {"cols", as_getter([](PyObject* o, void*) { return PyLong_FromLongLong(matrix_of(o).c.cols); }), nullptr, nullptr, nullptr},
+    {"format", as_getter([](PyObject* o, void*) { return PyUnicode_FromString(matrix_of(o).c.format == MOR_FP4_E4M3_16 ? "e4m3_16" : "e8m0_32"); }), nullptr, nullptr, nullptr},
+    {"codes", as_getter([](PyObject* o, void*) { return guarded([&] { return give(matrix_of(o).codes_tensor()); }); }), nullptr, "uint8 [batch, rows, bytes]", nullptr},
+    {"scales", as_getter([](PyObject* o, void*) { return guarded([&] { return give(matrix_of(o).scales_tensor()); }); }), nullptr, "uint8, in tiles", nullptr},
+    {"tensor_scale", as_getter([](PyObject* o, void*) { return guarded([&] { return give(matrix_of(o).scale_tensor()); }); }), nullptr, "one FP32", nullptr},
+    {nullptr, nullptr, nullptr, nullptr, nullptr}};
+PyGetSetDef plan_fields[] = {
+    {"starts", as_getter([](PyObject* o, void*) { return guarded([&] { return give(routes_of(o).starts); }); }), nullptr, "[experts + 1]", nullptr},
+    {"row", as_getter([](PyObject* o, void*) { return guarded([&] { return give(routes_of(o).row); }); }), nullptr, "[tokens, top], -1: none", nullptr},
+    {"slot", as_getter([](PyObject* o, void*) { return guarded([&] { return give(routes_of(o).slot); }); }), nullptr, "[rows], -1: an empty row", nullptr},
+    {"top", as_getter([](PyObject* o, void*) { return PyLong_FromLongLong(routes_of(o).top); }), nullptr, nullptr, nullptr},
+    {"align", as_getter([](PyObject* o, void*) { return PyLong_FromLongLong(routes_of(o).align); }), nullptr, nullptr, nullptr},
+    {nullptr, nullptr, nullptr, nullptr, nullptr}};
+
+#define MOR_METHOD(NAME, FUNCTION) {NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&FUNCTION)), METH_FASTCALL | METH_KEYWORDS, nullptr}
+PyMethodDef methods[] = {MOR_METHOD("quantize", py_quantize), MOR_METHOD("dequantize", py_dequantize), MOR_METHOD("matmul", py_matmul),
+                         MOR_METHOD("matmul_rows", py_matmul_rows), MOR_METHOD("matmul_reduce", py_matmul_reduce), MOR_METHOD("linear", py_linear),
+                         MOR_METHOD("status_word", py_status_word), MOR_METHOD("sort", py_sort), MOR_METHOD("gather", py_gather),
+                         MOR_METHOD("combine", py_combine), MOR_METHOD("combine_grad", py_combine_grad), MOR_METHOD("expert_linear", py_expert_linear),
+                         {nullptr, nullptr, 0, nullptr}};
 
 }  // namespace
 
 PYBIND11_MODULE(_ops, m)
 {
-    using std::optional;
-    py::class_<Matrix, Operand>(m, "Operand",
-                                "A stack of matrices [batch][rows, cols] in 4 bits, blocks along cols; Operand(codes, scales, rows, cols, format, "
-                                "tensor_scale) takes a caller's own tensors (a stored weight), laid out as include/mor.h says.")
-        .def(py::init([](const Tensor& codes, const Tensor& scales, int64_t rows, int64_t cols, const py::object& format, const Tensor& scale) {
-            return stored(codes, scales, rows, cols, format, scale);
-        }), py::arg("codes"), py::arg("scales"), py::arg("rows"), py::arg("cols"), py::arg("format"), py::arg("tensor_scale"))
-        .def_property_readonly("batch", [](const Matrix& o) { return o.c.batch; })
-        .def_property_readonly("rows", [](const Matrix& o) { return o.c.rows; })
-        .def_property_readonly("cols", [](const Matrix& o) { return o.c.cols; })
-        .def_property_readonly("format", [](const Matrix& o) { return o.c.format == MOR_FP4_E4M3_16 ? "e4m3_16" : "e8m0_32"; })
-        .def_property_readonly("codes", &Matrix::codes_tensor)
-        .def_property_readonly("scales", &Matrix::scales_tensor)
-        .def_property_readonly("tensor_scale", &Matrix::scale_tensor);
-    py::class_<Routes, Plan>(m, "Plan", "starts [experts + 1], row [tokens, top] (-1: none), slot [rows] (-1: an empty row)")
-        .def_readonly("starts", &Routes::starts)
-        .def_readonly("row", &Routes::row)
-        .def_readonly("slot", &Routes::slot)
-        .def_readonly("top", &Routes::top)
-        .def_readonly("align", &Routes::align);
-    auto one = [](optional<Matrix>& m) { return m ? std::make_shared<Matrix>(std::move(*m)) : nullptr; };
-    m.def("quantize", [one](const Tensor& x, const py::object& format, bool rows, bool cols, const optional<Tensor>& amax, const Plan& gather,
-                            const optional<Tensor>& weight) {
-        Pair p = quantize_(x, format_of(format), rows, cols, amax, gather.get(), weight);
-        return std::make_pair(one(p.rows), one(p.cols));
-    }, py::arg("x"), py::arg("format"), py::kw_only(), py::arg("rows") = true, py::arg("cols") = false, py::arg("amax") = py::none(),
-          py::arg("gather") = py::none(), py::arg("weight") = py::none());
-    m.def("dequantize", [](const Matrix& o, const py::object& dtype) { return dequantize(o, dtype.is_none() ? at::kBFloat16 : dtype.cast<at::ScalarType>()); },
-          py::arg("op"), py::arg("dtype") = py::none());
-    m.def("matmul", [](const Matrix& a, const Matrix& b, const py::object& t) { return matmul_(a, b, t.is_none() ? at::kBFloat16 : t.cast<at::ScalarType>(), MOR_GROUP_NONE, nullptr); },
-          py::arg("a"), py::arg("b"), py::arg("out_dtype") = py::none());
-    m.def("matmul_rows", [](const Matrix& a, const Matrix& b, const Routes& p, const py::object& t) { return matmul_rows_(a, b, p, t.is_none() ? at::kBFloat16 : t.cast<at::ScalarType>()); },
-          py::arg("a"), py::arg("b"), py::arg("plan"), py::arg("out_dtype") = py::none());
-    m.def("matmul_reduce", [](const Matrix& a, const Matrix& b, const Routes& p, const py::object& t) { return matmul_reduce_(a, b, p, t.is_none() ? at::kBFloat16 : t.cast<at::ScalarType>()); },
-          py::arg("a"), py::arg("b"), py::arg("plan"), py::arg("out_dtype") = py::none());
-    m.def("linear", &linear, py::arg("x"), py::arg("w"), py::arg("format"));
-    m.def("status_word", [](const Tensor& like) { return status_word(like); });
-    m.def("sort", &sort_slots, py::arg("ids"), py::arg("n_experts"), py::arg("align") = 1);
-    m.def("gather", &gather, py::arg("x"), py::arg("plan"), py::arg("weight") = py::none());
-    m.def("combine", [](const Tensor& ys, const Routes& p, const optional<Tensor>& w, const py::object& t) {
-        return combine(ys, p, w, t.is_none() ? ys.scalar_type() : t.cast<at::ScalarType>());
-    }, py::arg("ys"), py::arg("plan"), py::arg("weight") = py::none(), py::arg("out_dtype") = py::none());
-    m.def("combine_grad", &combine_grad, py::arg("dy"), py::arg("ys"), py::arg("plan"), py::arg("weight"), py::kw_only(), py::arg("rows") = true);
-    m.def("expert_linear", &expert_linear, py::arg("x"), py::arg("w"), py::arg("ids"), py::arg("weight"), py::arg("format") = py::none());
+    operand_type.tp_name = "paper_2512_22804_b200.fp4.Operand";
+    operand_type.tp_doc = "A stack of matrices [batch][rows, cols] in 4 bits, blocks along cols; Operand(codes, scales, rows, cols, format, tensor_scale) "
+                          "takes a caller's own tensors (a stored weight), laid out as include/mor.h says.";
+    operand_type.tp_basicsize = sizeof(OperandObject);
+    operand_type.tp_dealloc = release<OperandObject, Matrix, &OperandObject::m>;
+    operand_type.tp_flags = Py_TPFLAGS_DEFAULT;
+    operand_type.tp_getset = operand_fields;
+    operand_type.tp_vectorcall = new_operand;
+    plan_type.tp_name = "paper_2512_22804_b200.experts.Plan";
+    plan_type.tp_doc = "Where every slot's row is (made by sort).";
+    plan_type.tp_basicsize = sizeof(PlanObject);
+    plan_type.tp_dealloc = release<PlanObject, Routes, &PlanObject::r>;
+    plan_type.tp_flags = Py_TPFLAGS_DEFAULT | Py_TPFLAGS_DISALLOW_INSTANTIATION;
+    plan_type.tp_getset = plan_fields;
+    if (PyType_Ready(&operand_type) < 0 || PyType_Ready(&plan_type) < 0 || PyModule_AddFunctions(m.ptr(), methods) < 0 ||
+        PyModule_AddObjectRef(m.ptr(), "Operand", reinterpret_cast<PyObject*>(&operand_type)) < 0 ||
+        PyModule_AddObjectRef(m.ptr(), "Plan", reinterpret_cast<PyObject*>(&plan_type)) < 0)
+        throw py::error_already_set();
 }
