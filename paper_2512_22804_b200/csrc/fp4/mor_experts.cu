@@ -25,23 +25,25 @@ struct SortParams {
     int32_t* hist;             // [chunks][experts], of the chunks' slots per expert
 };
 
-// The part of a chunk that a warp walks: whole groups of 32 slots.
-__device__ __forceinline__ void warp_part(const SortParams& p, int64_t& first, int64_t& last)
+// The part of a chunk that a warp walks: whole groups of 32 slots.  Returns how many warps have a part.
+__device__ __forceinline__ int warp_part(const SortParams& p, int64_t& first, int64_t& last)
 {
     const int64_t begin = (int64_t)blockIdx.x * p.chunk, end = min(begin + p.chunk, p.n);
-    const int64_t per = (end - begin + kSortThreads - 1) / kSortThreads * 32;
+    const int per = (int)(end - begin + kSortThreads - 1) / kSortThreads * 32;
     first = min(begin + (threadIdx.x >> 5) * per, end);
     last = min(first + per, end);
+    return per == 0 ? 0 : ((int)(end - begin) + per - 1) / per;
 }
 
-// Slots per (warp, expert) of this CTA's chunk.  Lanes with the same expert are found by a match; one of them adds.
-__device__ void count_slots(const SortParams& p, int32_t* counts)
+// Slots per (warp, expert) of this CTA's chunk.  Lanes with the same expert are found by a match; one of them adds.  Returns how many
+// warps have counts.
+__device__ int count_slots(const SortParams& p, int32_t* counts)
 {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    for (int i = threadIdx.x; i < kSortWarps * p.experts; i += kSortThreads) counts[i] = 0;
-    __syncthreads();
     int64_t first, last;
-    warp_part(p, first, last);
+    const int warps = warp_part(p, first, last);
+    for (int i = threadIdx.x; i < warps * p.experts; i += kSortThreads) counts[i] = 0;
+    __syncthreads();
     for (int64_t at = first; at < last; at += 32) {
         const int32_t id = at + lane < last ? p.ids[at + lane] : -1;
         const uint32_t same = __match_any_sync(0xFFFFFFFFu, id);
@@ -49,16 +51,17 @@ __device__ void count_slots(const SortParams& p, int32_t* counts)
         __syncwarp();
     }
     __syncthreads();
+    return warps;
 }
 
 __global__ void __launch_bounds__(kSortThreads) expert_count_kernel(const __grid_constant__ SortParams p)
 {
     extern __shared__ int32_t counts[];
     wait_for_predecessor();
-    count_slots(p, counts);
+    const int warps = count_slots(p, counts);
     for (int e = threadIdx.x; e < p.experts; e += kSortThreads) {
         int32_t sum = 0;
-        for (int w = 0; w < kSortWarps; ++w) sum += counts[w * p.experts + e];
+        for (int w = 0; w < warps; ++w) sum += counts[w * p.experts + e];
         p.hist[(int64_t)blockIdx.x * p.experts + e] = sum;
     }
 }
@@ -94,10 +97,10 @@ __global__ void __launch_bounds__(kSortThreads) expert_place_kernel(const __grid
     __shared__ int32_t used[MOR_MAX_GROUPS + 1];        // first empty row of each expert; [experts]: first row past the last expert
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (gridDim.x == 1) wait_for_predecessor();             // else the predecessor is the count, and the ids are older
-    count_slots(p, counts);
+    const int warps = count_slots(p, counts);
     int32_t own = 0, before = 0, total = 0;
     if (tid < p.experts)
-        for (int w = 0; w < kSortWarps; ++w) own += counts[w * p.experts + tid];
+        for (int w = 0; w < warps; ++w) own += counts[w * p.experts + tid];
     total = own;
     if (gridDim.x > 1) {
         wait_for_predecessor();
@@ -119,7 +122,7 @@ __global__ void __launch_bounds__(kSortThreads) expert_place_kernel(const __grid
         used[tid] = start + total;
         if (tid == p.experts - 1) used[p.experts] = end;
         int32_t next = start + before;
-        for (int w = 0; w < kSortWarps; ++w) {
+        for (int w = 0; w < warps; ++w) {
             const int32_t c = counts[w * p.experts + tid];
             counts[w * p.experts + tid] = next;
             next += c;

@@ -579,7 +579,7 @@ mor_status_t run_narrow(GemmParams& p, const mor_fp4_matrix_t& a, const mor_fp4_
     int64_t split = 148 * 2 / (nt * mt);
     split = split > kMaxSplit ? kMaxSplit : split;
     split = split > stages ? stages : split;
-    split = split < 1 ? 1 : split;
+    split = split >= 8 ? 8 : split >= 4 ? 4 : split >= 2 ? 2 : 1;      // clusters of other sizes leave places empty (6144 x 4096 by 6: 9.8 us, by 4: 5.5)
     auto* kernel = fp4_narrow_kernel<NT, FMT, T>;
     if (!allow_smem(kernel, W::kSmem, done)) return MOR_ERR_CUDA;
     return launch_cluster(kernel, (uint32_t)(nt * mt * split), kNarrowThreads, W::kSmem, (uint32_t)split, st, p) == cudaSuccess ? MOR_OK : MOR_ERR_CUDA;
