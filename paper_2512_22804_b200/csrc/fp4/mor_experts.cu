@@ -491,7 +491,7 @@ mor_status_t mor_expert_combine_grad(const mor_expert_desc_t* host_desc, const v
     MoveParams p;
     mor_status_t s = move_params(host_desc, p);
     if (s != MOR_OK) return s;
-    if (dys == nullptr && dweight == nullptr) return MOR_ERR_INVALID_ARG;
+    if (p.tokens > 0 && p.hidden > 0 && dys == nullptr && dweight == nullptr) return MOR_ERR_INVALID_ARG;     // empty tensors have no address
     if (dweight != nullptr && !is_dtype(host_desc->weight_dtype)) return MOR_ERR_INVALID_ARG;
     if (dweight != nullptr && !is_aligned(dweight, dtype_bytes(host_desc->weight_dtype))) return MOR_ERR_ALIGNMENT;
     int access = 32;

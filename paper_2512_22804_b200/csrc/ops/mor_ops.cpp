@@ -5,6 +5,7 @@
 // `_ops`, used through fp4.py and experts.py.
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAFunctions.h>
+#include <c10/cuda/CUDAGraphsC10Utils.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/extension.h>
 
@@ -66,12 +67,17 @@ template <typename T> T* ptr(const Tensor& t) { return static_cast<T*>(t.data_pt
 Tensor empty(at::IntArrayRef shape, at::ScalarType type, const Tensor& like) { return at::detail::empty_cuda(shape, type, like.device(), std::nullopt); }
 Tensor bytes(int64_t n, const Tensor& like) { return empty({n}, at::kByte, like); }
 
-// The word that products set when a bounded wait ran out, one per device, never given back.
-Tensor& status_word(const Tensor& like)
+// The word that products set when a bounded wait ran out, one per device, never given back.  It is cleared before any stream uses it;
+// a first call inside a stream capture, where that cannot be waited for, goes without.
+Tensor status_word(const Tensor& like)
 {
     static std::vector<Tensor>* words = new std::vector<Tensor>(64);
     Tensor& w = words->at(like.get_device());
-    if (!w.defined()) w = at::zeros({1}, like.options().dtype(at::kInt).requires_grad(false));
+    if (!w.defined()) {
+        if (c10::cuda::currentStreamCaptureStatusMayInitCtx() != c10::cuda::CaptureStatus::None) return Tensor();
+        w = at::zeros({1}, like.options().dtype(at::kInt).requires_grad(false));
+        c10::cuda::getCurrentCUDAStream().synchronize();
+    }
     return w;
 }
 
@@ -231,7 +237,8 @@ Tensor matmul_(const Matrix& a, const Matrix& b, at::ScalarType type, int groupi
     }
     const Tensor out = grouping == MOR_GROUP_REDUCE ? empty({d.groups, a.c.rows, d.ldo}, type, a.buf) : empty({a.c.rows, d.ldo}, type, a.buf);
     d.out = out.data_ptr();
-    d.status = reinterpret_cast<uint32_t*>(ptr<int32_t>(status_word(a.buf)));
+    const Tensor status = status_word(a.buf);
+    d.status = status.defined() ? reinterpret_cast<uint32_t*>(ptr<int32_t>(status)) : nullptr;
     check(mor_fp4_matmul(&d, stream()), "mor_fp4_matmul");
     return d.ldo == n ? out : out.narrow(-1, 0, n);
 }

@@ -190,6 +190,22 @@ def test_quantised_gather_equals_gather_then_quantise(experts, fmt, weighted):
 
 
 @pytest.mark.parametrize("fmt", ["e4m3_16", "e8m0_32"])
+@pytest.mark.parametrize("tokens", [0, 1, 300])
+def test_expert_layer_where_no_token_has_an_expert(experts, fmt, tokens):
+    import torch
+
+    x = torch.ones(tokens, 64, device="cuda", dtype=torch.bfloat16, requires_grad=True)
+    w = torch.ones(4, 40, 64, device="cuda", dtype=torch.bfloat16, requires_grad=True)
+    weight = torch.ones(tokens, 2, device="cuda", requires_grad=True)
+    ids = torch.full((tokens, 2), -1, device="cuda", dtype=torch.int32)
+    y = experts.linear(x, w, ids, weight, fmt)
+    grads = torch.autograd.grad(y, (x, w, weight), torch.ones_like(y))
+    assert y.shape == (tokens, 40) and not y.any()
+    for g, t in zip(grads, (x, w, weight)):
+        assert g.shape == t.shape and not g.any()
+
+
+@pytest.mark.parametrize("fmt", ["e4m3_16", "e8m0_32"])
 @pytest.mark.parametrize("tokens,top,n,k,m", [(1, 2, 8, 64, 40), (50, 3, 6, 300, 136), (400, 2, 4, 257, 264)])
 def test_expert_layer_and_its_gradient(experts, fmt, tokens, top, n, k, m):
     """Against the formula on quantised values, in 64 bits.  The rows of the gradient's product are rounded to BF16 (at

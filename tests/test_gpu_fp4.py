@@ -276,6 +276,40 @@ def test_empty_operands(fp4):
     assert fp4.dequantize(at).shape == (64, 0)
 
 
+def test_a_captured_step_follows_its_inputs(fp4):
+    """Quantisation, product and layer inside a CUDA graph: replayed with other values in the same tensors."""
+    import torch
+
+    x, w = tensor(draw(40, 512, 1)), tensor(draw(264, 512, 2))
+    b = fp4.quantize(w, "e4m3_16")[0]
+
+    def step():
+        return fp4.matmul(fp4.quantize(x, "e4m3_16")[0], b), fp4.linear(x, w, "e8m0_32")
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for seed in (5, 6):
+        x.copy_(tensor(draw(40, 512, seed)))
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, want in zip(out, step()):
+            assert torch.equal(got, want)
+
+
+def test_gradients_of_no_tokens(fp4):
+    import torch
+
+    x = torch.zeros(0, 96, device="cuda", dtype=torch.bfloat16, requires_grad=True)
+    w = torch.ones(40, 96, device="cuda", dtype=torch.bfloat16, requires_grad=True)
+    for fmt in FORMATS:
+        y = fp4.linear(x, w, fmt)
+        dx, dw = torch.autograd.grad(y, (x, w), torch.zeros(0, 40, device="cuda", dtype=torch.bfloat16))
+        assert y.shape == (0, 40) and dx.shape == (0, 96) and not dw.any() and dw.shape == w.shape
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_linear_and_its_gradient(fp4, fmt):
     """y, dx and dw against the three products of values quantised along their reduction axes."""
