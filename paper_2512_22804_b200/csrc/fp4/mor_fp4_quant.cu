@@ -426,9 +426,11 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED 
 
 // ---- large BF16 tensors in the column direction: the same tiles, streamed
 //
-// Persistent CTAs, three an SM.  While a tile is converted, the next one is on its way into the other half of the shared
-// memory (asynchronous 16-byte copies to the permuted chunks, zero-filled past the edges), so loads never wait for arithmetic: with
-// one tile per CTA the loads stood still for most of its life (8192 x 14336 E4M3_16, columns alone: 66 us, streamed 56 us).
+// Persistent CTAs, two an SM.  While a tile is converted, the next one is on its way into the other half of the shared memory
+// (asynchronous 16-byte copies to the permuted chunks, zero-filled past the edges), so loads never wait for arithmetic: with one
+// tile per CTA the loads stood still for most of its life.  8192 x 14336, columns alone: E4M3_16 66 us with a CTA per tile, 49 us
+// (6.1 TB/s) streamed; both directions 60 us, E8M0_32 62 us.  Three CTAs an SM have a third fewer registers and form their
+// addresses anew all the time (64 and 68 us); a ring of three tiles in place of two gained nothing (63 us).
 __device__ __forceinline__ void copy_async16(uint32_t dst, const void* src, int bytes)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -463,7 +465,7 @@ struct TileWalk {
 // The arithmetic of a tile is about five instructions per element; addresses are formed once per tile and thread and stepped
 // by constants, since 64-bit products per access came to as much again.
 template <int FMT, bool ROWS, int MODE>
-__global__ void __launch_bounds__(kQThreads, 3) fp4_stream_kernel(const __grid_constant__ QuantParams p, uint32_t tiles)
+__global__ void __launch_bounds__(kQThreads, 2) fp4_stream_kernel(const __grid_constant__ QuantParams p, uint32_t tiles)
 {
     using L = Tile<true>;
     constexpr int kTiles = FMT == MOR_FP4_E4M3_16 ? 2 : 1;
@@ -777,7 +779,7 @@ template <typename T, int FMT, bool ROWS, bool COLS, int MODE> cudaError_t quant
         if (p.access >= 16 && grid >= kStreamTiles && (FMT == MOR_FP4_E8M0_32 || p.amax != nullptr || p.partial != nullptr)) {
             static std::atomic<uint64_t> stream_done{0};
             if (!allow_smem(fp4_stream_kernel<FMT, ROWS, MODE>, kStreamSmem, stream_done)) return cudaErrorInvalidValue;
-            return launch(fp4_stream_kernel<FMT, ROWS, MODE>, grid < 148 * 3 ? grid : 148 * 3, kQThreads, kStreamSmem, st, true, p, grid);
+            return launch(fp4_stream_kernel<FMT, ROWS, MODE>, grid < 148 * 2 ? grid : 148 * 2, kQThreads, kStreamSmem, st, true, p, grid);
         }
     }
     constexpr bool kNarrow = sizeof(T) == 2 && MODE != WEIGHTED;
