@@ -178,10 +178,27 @@ struct MoveParams {
     void* dweight;
 };
 
+// Rows that start anywhere or are no whole number of pieces (ANY): pieces are laid out from the aligned addresses of the row that is
+// written, what is read is shifted into place, and some forty elements at the ends go one by one, a thread each.
+template <typename T, typename R, int BYTES> struct Inner {
+    static constexpr int kElems = BYTES / (int)sizeof(T), kPer = 16 / (int)sizeof(R);
+    int64_t first, end;          // where whole pieces begin and end, far enough inside for any source's chunks
+    int edges;                   // elements outside
+    __device__ __forceinline__ Inner(const T* to, int64_t n)
+    {
+        static_assert(kElems >= kPer, "a piece is a chunk at least");
+        first = kElems + (kElems - phase_of(to)) % kElems;
+        end = n - kPer >= first ? first + (n - kPer - first) / kElems * kElems : first;
+        if (end == first) first = end = n;
+        edges = (int)(n - (end - first));
+    }
+    __device__ __forceinline__ int64_t edge(int i) const { return i < first ? i : i + (end - first); }
+};
+
 // Zeroes the rows without a slot among this CTA's kClearRows.  Masked tokens leave all their empty rows at the end, so a CTA
 // takes few of them (256 rows of 8 KiB by one CTA took longer than the rest of the gather), and these CTAs come first.
 constexpr int kClearRows = 16;
-template <typename T, int BYTES> __device__ void clear_rows(const MoveParams& p, T* out, uint32_t block)
+template <typename T, int BYTES, bool ANY> __device__ void clear_rows(const MoveParams& p, T* out, uint32_t block)
 {
     using P = Piece<T, BYTES>;
     const int64_t row = (int64_t)block * kClearRows + (threadIdx.x & 31);
@@ -190,7 +207,13 @@ template <typename T, int BYTES> __device__ void clear_rows(const MoveParams& p,
     zero.clear();
     for (uint32_t m = __ballot_sync(0xFFFFFFFFu, none); m != 0; m &= m - 1) {
         T* to = out + ((int64_t)block * kClearRows + __ffs(m) - 1) * p.ld_out;
-        for (int64_t c = (int64_t)threadIdx.x * P::kElems; c < p.hidden; c += (int64_t)blockDim.x * P::kElems) zero.store(to + c);
+        if constexpr (ANY) {
+            const Inner<T, T, BYTES> in(to, p.hidden);
+            for (int64_t c = in.first + (int64_t)threadIdx.x * P::kElems; c < in.end; c += (int64_t)blockDim.x * P::kElems) zero.store(to + c);
+            for (int i = threadIdx.x; i < in.edges; i += blockDim.x) Piece<T, (int)sizeof(T)>{}.store(to + in.edge(i));
+        } else {
+            for (int64_t c = (int64_t)threadIdx.x * P::kElems; c < p.hidden; c += (int64_t)blockDim.x * P::kElems) zero.store(to + c);
+        }
     }
 }
 
@@ -209,20 +232,46 @@ struct Slots {
     }
 };
 
-template <typename T, int BYTES> __global__ void __launch_bounds__(256) expert_gather_kernel(const __grid_constant__ MoveParams p)
+// A token's row to the rows of its slots, times their weights.
+template <typename T, int BYTES> __device__ __forceinline__ void spread_any(const MoveParams& p, const Slots& s, const T* x, T* out)
+{
+    using P = Piece<T, BYTES>;
+    using One = Piece<T, (int)sizeof(T)>;
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) {
+        if (s.row[j] < 0) continue;
+        T* to = out + (int64_t)s.row[j] * p.ld_out;
+        const Inner<T, T, BYTES> in(to, p.hidden);
+        for (int64_t c = in.first + (int64_t)threadIdx.x * P::kElems; c < in.end; c += (int64_t)blockDim.x * P::kElems) {
+            P v;
+            load_shifted<T, BYTES>(v.w, x + c);
+            if (p.weight == nullptr) v.store(to + c);
+            else v.scaled(s.w[j]).store(to + c);
+        }
+        for (int i = threadIdx.x; i < in.edges; i += blockDim.x) {
+            One v;
+            v.load(x + in.edge(i));
+            if (p.weight == nullptr) v.store(to + in.edge(i));
+            else v.scaled(s.w[j]).store(to + in.edge(i));
+        }
+    }
+}
+
+template <typename T, int BYTES, bool ANY> __global__ void __launch_bounds__(256) expert_gather_kernel(const __grid_constant__ MoveParams p)
 {
     using P = Piece<T, BYTES>;
     T* out = static_cast<T*>(p.out);
     wait_for_predecessor();
     if (blockIdx.x < p.clear_blocks) {
-        clear_rows<T, BYTES>(p, out, blockIdx.x);
+        clear_rows<T, BYTES, ANY>(p, out, blockIdx.x);
         return;
     }
     const int64_t token = blockIdx.x - p.clear_blocks;
     const T* x = static_cast<const T*>(p.tokens_in) + token * p.ld_token;
     for (uint32_t j0 = 0; j0 < p.top; j0 += kAtOnce) {
         const Slots s(p, token, j0);
-        for (int64_t c = (int64_t)threadIdx.x * P::kElems; c < p.hidden; c += (int64_t)blockDim.x * P::kElems) {
+        if constexpr (ANY) spread_any<T, BYTES>(p, s, x, out);
+        for (int64_t c = (int64_t)threadIdx.x * P::kElems; !ANY && c < p.hidden; c += (int64_t)blockDim.x * P::kElems) {
             P v;
             v.load(x + c);
 #pragma unroll
@@ -236,15 +285,16 @@ template <typename T, int BYTES> __global__ void __launch_bounds__(256) expert_g
     }
 }
 
-template <typename T, typename R, int BYTES> __global__ void __launch_bounds__(256) expert_combine_kernel(const __grid_constant__ MoveParams p)
+template <typename T, typename R, int BYTES, bool ANY> __global__ void __launch_bounds__(256) expert_combine_kernel(const __grid_constant__ MoveParams p)
 {
     using P = Piece<T, BYTES>;
-    using Q = Piece<R, BYTES / (int)sizeof(T) * (int)sizeof(R)>;
     wait_for_predecessor();
     const int64_t token = blockIdx.x;
     const R* ys = static_cast<const R*>(p.rows_in);
     T* out = static_cast<T*>(p.out) + token * p.ld_out;
-    for (int64_t c = (int64_t)threadIdx.x * P::kElems; c < p.hidden; c += (int64_t)blockDim.x * P::kElems) {
+    auto piece = [&](auto like, int64_t c) {
+        using P = decltype(like);
+        using Q = Piece<R, P::kElems * (int)sizeof(R)>;
         float sum[P::kElems];
 #pragma unroll
         for (float& s : sum) s = 0.f;
@@ -254,7 +304,10 @@ template <typename T, typename R, int BYTES> __global__ void __launch_bounds__(2
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j) {
                 v[j].clear();
-                if (s.row[j] >= 0) v[j].load(ys + (int64_t)s.row[j] * p.ld_row + c);
+                if (s.row[j] < 0) continue;
+                const R* from = ys + (int64_t)s.row[j] * p.ld_row + c;
+                if constexpr (ANY && P::kElems > 1) load_shifted<R, (int)sizeof(v[j].w)>(v[j].w, from);
+                else v[j].load(from);
             }
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j)
@@ -264,20 +317,27 @@ template <typename T, typename R, int BYTES> __global__ void __launch_bounds__(2
         P r;
         r.set_all(sum);
         r.store(out + c);
+    };
+    if constexpr (ANY) {
+        const Inner<T, R, BYTES> in(out, p.hidden);
+        for (int64_t c = in.first + (int64_t)threadIdx.x * P::kElems; c < in.end; c += (int64_t)blockDim.x * P::kElems) piece(P{}, c);
+        for (int i = threadIdx.x; i < in.edges; i += blockDim.x) piece(Piece<T, (int)sizeof(T)>{}, in.edge(i));
+    } else {
+        for (int64_t c = (int64_t)threadIdx.x * P::kElems; c < p.hidden; c += (int64_t)blockDim.x * P::kElems) piece(P{}, c);
     }
 }
 
 // The sums over hidden of <dy, ys> are taken per thread in column order, then over the CTA in a fixed tree: the result
 // does not change from run to run.  Four CTAs an SM (64 registers): with the 118 that the compiler would take, two, and not enough
 // rows are in flight.
-template <typename T, typename R, int BYTES> __global__ void __launch_bounds__(256, 4) expert_grad_kernel(const __grid_constant__ MoveParams p)
+template <typename T, typename R, int BYTES, bool ANY> __global__ void __launch_bounds__(256, 4) expert_grad_kernel(const __grid_constant__ MoveParams p)
 {
     using P = Piece<T, BYTES>;
     using Q = Piece<R, BYTES / (int)sizeof(T) * (int)sizeof(R)>;
     T* out = static_cast<T*>(p.out);
     wait_for_predecessor();
     if (blockIdx.x < p.clear_blocks) {
-        clear_rows<T, BYTES>(p, out, blockIdx.x);
+        clear_rows<T, BYTES, ANY>(p, out, blockIdx.x);
         return;
     }
     __shared__ float part[kAtOnce][8];
@@ -290,7 +350,36 @@ template <typename T, typename R, int BYTES> __global__ void __launch_bounds__(2
         float dot[kAtOnce];
 #pragma unroll
         for (float& d : dot) d = 0.f;
-        for (int64_t c = (int64_t)threadIdx.x * P::kElems; c < p.hidden; c += (int64_t)blockDim.x * P::kElems) {
+        if constexpr (ANY) {
+            if (out != nullptr) spread_any<T, BYTES>(p, s, dy, out);
+            // a pass of its own, so that the sums' order does not depend on where the written rows start
+            auto add = [&](auto like, int64_t c) {
+                using P = decltype(like);
+                using Q = Piece<R, P::kElems * (int)sizeof(R)>;
+                P g;
+                Q v[kAtOnce];
+                if constexpr (P::kElems > 1) load_shifted<T, (int)sizeof(g.w)>(g.w, dy + c);
+                else g.load(dy + c);
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j) {
+                    if (s.row[j] < 0) continue;
+                    const R* from = ys + (int64_t)s.row[j] * p.ld_row + c;
+                    if constexpr (P::kElems > 1) load_shifted<R, (int)sizeof(v[j].w)>(v[j].w, from);
+                    else v[j].load(from);
+                }
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j)
+                    if (s.row[j] >= 0)
+#pragma unroll
+                        for (int i = 0; i < P::kElems; ++i) dot[j] = fmaf(g.get(i), v[j].get(i), dot[j]);
+            };
+            if (p.dweight != nullptr) {
+                const Inner<T, R, BYTES> in(static_cast<const T*>(nullptr), p.hidden);
+                for (int64_t c = in.first + (int64_t)threadIdx.x * P::kElems; c < in.end; c += (int64_t)blockDim.x * P::kElems) add(P{}, c);
+                for (int i = threadIdx.x; i < in.edges; i += blockDim.x) add(Piece<T, (int)sizeof(T)>{}, in.edge(i));
+            }
+        }
+        for (int64_t c = (int64_t)threadIdx.x * P::kElems; !ANY && c < p.hidden; c += (int64_t)blockDim.x * P::kElems) {
             P g;
             Q v[kAtOnce];
             g.load(dy + c);
@@ -337,14 +426,14 @@ template <typename T, typename R, int BYTES> __global__ void __launch_bounds__(2
 
 enum Move : int { MOVE_GATHER, MOVE_COMBINE, MOVE_GRAD };
 
-template <typename T, typename R, int BYTES> cudaError_t move_launch(const MoveParams& p, Move what, uint32_t grid, cudaStream_t st)
+template <typename T, typename R, int BYTES, bool ANY> cudaError_t move_launch(const MoveParams& p, Move what, uint32_t grid, cudaStream_t st)
 {
     const int64_t pieces = ceil_div(p.hidden, BYTES / (int64_t)sizeof(T));
     const uint32_t threads = pieces >= 256 ? 256u : (uint32_t)(ceil_div(pieces, 32) * 32);
     if constexpr (sizeof(T) == sizeof(R))
-        if (what == MOVE_GATHER) return launch(expert_gather_kernel<T, BYTES>, grid, threads, 0, st, true, p);
-    if (what == MOVE_COMBINE) return launch(expert_combine_kernel<T, R, BYTES>, grid, threads, 0, st, true, p);
-    return launch(expert_grad_kernel<T, R, BYTES>, grid, threads, 0, st, true, p);
+        if (what == MOVE_GATHER) return launch(expert_gather_kernel<T, BYTES, ANY>, grid, threads, 0, st, true, p);
+    if (what == MOVE_COMBINE) return launch(expert_combine_kernel<T, R, BYTES, ANY>, grid, threads, 0, st, true, p);
+    return launch(expert_grad_kernel<T, R, BYTES, ANY>, grid, threads, 0, st, true, p);
 }
 template <typename T, typename R> cudaError_t move_access(const MoveParams& p, Move what, uint32_t grid, int access, cudaStream_t st)
 {
@@ -352,9 +441,9 @@ template <typename T, typename R> cudaError_t move_access(const MoveParams& p, M
     // the registers of four rows' pieces stay the same.
     const int64_t width = p.hidden * (int64_t)sizeof(T);
     if constexpr (sizeof(T) == sizeof(R))
-        if (access == 32 && width % 32 == 0) return move_launch<T, R, 32>(p, what, grid, st);
-    if (access >= 16 && width % 16 == 0) return move_launch<T, R, 16>(p, what, grid, st);
-    return move_launch<T, R, (int)sizeof(T)>(p, what, grid, st);
+        if (access == 32 && width % 32 == 0) return move_launch<T, R, 32, false>(p, what, grid, st);
+    if (access >= 16 && width % 16 == 0) return move_launch<T, R, 16, false>(p, what, grid, st);
+    return move_launch<T, R, 16, true>(p, what, grid, st);
 }
 
 // Checks what all movers share and fills the parameters.

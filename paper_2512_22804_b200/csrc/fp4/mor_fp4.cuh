@@ -251,9 +251,6 @@ template <typename T, int BYTES> struct Piece {
         } else if constexpr (BYTES == 16) {
             const uint4 q = *reinterpret_cast<const uint4*>(p);
             w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
-        } else if constexpr (BYTES == 8) {
-            const uint2 q = *reinterpret_cast<const uint2*>(p);
-            w[0] = q.x; w[1] = q.y;
         } else if constexpr (BYTES == 4) w[0] = *reinterpret_cast<const uint32_t*>(p);
         else w[0] = *reinterpret_cast<const uint16_t*>(p);
     }
@@ -263,7 +260,6 @@ template <typename T, int BYTES> struct Piece {
 #pragma unroll
             for (int i = 0; i < kWords; i += 8) stg256(reinterpret_cast<uint32_t*>(p) + i, w + i);
         } else if constexpr (BYTES == 16) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-        else if constexpr (BYTES == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
         else if constexpr (BYTES == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
         else *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
     }
@@ -299,12 +295,58 @@ template <typename T, int BYTES> struct Piece {
     }
 };
 
+// BYTES bytes from an address that need not be aligned, as words: the aligned 16-byte chunks that hold them (one more than there are
+// bytes for, unless the address is aligned), put in place by shifts.  Both ends' whole chunks have to be readable.
+template <typename T, int BYTES> __device__ __forceinline__ void load_shifted(uint32_t* w, const T* from)
+{
+    static_assert(BYTES % 16 == 0, "whole chunks");
+    constexpr int kWords = BYTES / 4;
+    const uint32_t phase = (uint32_t)reinterpret_cast<uintptr_t>(from) & 15u;
+    const uint4* chunks = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(from) - phase);
+    uint32_t v[kWords + 4];
+#pragma unroll
+    for (int i = 0; i < kWords; i += 4) {
+        const uint4 q = chunks[i / 4];
+        v[i] = q.x; v[i + 1] = q.y; v[i + 2] = q.z; v[i + 3] = q.w;
+    }
+    uint4 q = make_uint4(0, 0, 0, 0);
+    if (phase != 0) q = chunks[kWords / 4];
+    v[kWords] = q.x; v[kWords + 1] = q.y; v[kWords + 2] = q.z; v[kWords + 3] = q.w;
+#pragma unroll
+    for (int i = 0; i < kWords + 2; ++i) v[i] = phase & 8u ? v[i + 2] : v[i];
+#pragma unroll
+    for (int i = 0; i < kWords + 1; ++i) v[i] = phase & 4u ? v[i + 1] : v[i];
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = sizeof(T) == 4 ? v[i] : __funnelshift_r(v[i], v[i + 1], (phase & 2u) * 8u);
+}
+// How many elements an address lies past a 16-byte boundary.
+template <typename T> __device__ __forceinline__ int phase_of(const T* p) { return (int)((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T)); }
+// Elements [at, at + BYTES / sizeof(T)), at >= 0, of a row of n that may start anywhere; from n on they are zero.  Where the chunks would
+// reach past the row's ends, element by element.
+template <typename T, int BYTES> __device__ __forceinline__ void load_any(uint32_t* w, const T* row, int64_t at, int64_t n)
+{
+    constexpr int kElems = BYTES / (int)sizeof(T), kWords = BYTES / 4, kPer = 16 / (int)sizeof(T);
+    const int phase = phase_of(row + at);
+    if (at >= phase && at - phase + kElems + (phase != 0 ? kPer : 0) <= n) {
+        load_shifted<T, BYTES>(w, row + at);
+    } else if constexpr (sizeof(T) == 2) {
+        const uint16_t* h = reinterpret_cast<const uint16_t*>(row) + at;
+        const int left = (int)min((int64_t)kElems, n - at);
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = (2 * i < left ? h[2 * i] : 0u) | (2 * i + 1 < left ? (uint32_t)h[2 * i + 1] << 16 : 0u);
+    } else {
+        const int left = (int)min((int64_t)kElems, n - at);
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = i < left ? reinterpret_cast<const uint32_t*>(row)[at + i] : 0u;
+    }
+}
+
 // ---- host side
 
 inline bool is_dtype(int d) { return d == MOR_DTYPE_BF16 || d == MOR_DTYPE_F32; }
 inline size_t dtype_bytes(int d) { return d == MOR_DTYPE_BF16 ? 2 : 4; }
 inline bool is_aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+__host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t scale_blocks(int64_t cols, int format) { return ceil_div(cols, format == MOR_FP4_E4M3_16 ? 16 : 32); }
 inline int64_t scale_ktiles(int64_t cols, int format) { return ceil_div(scale_blocks(cols, format), 4); }
 

@@ -147,7 +147,7 @@ template <typename T, int BYTES, int MODE> __device__ __forceinline__ float piec
 // clear, no atomics).  Bound by memory: a warp reads 1 KiB at a time (32 bytes a lane), a thread keeps four pieces in flight; the grid
 // is resident as a whole.  8192 x 14336 BF16: 43 us (5.5 TB/s).
 __host__ __device__ inline bool contiguous(const QuantParams& p) { return p.ld == p.cols && (p.batch == 1 || p.batch_stride == p.x_rows * p.ld); }
-template <typename T, int BYTES, int MODE> __global__ void __launch_bounds__(kQThreads) fp4_amax_kernel(const __grid_constant__ QuantParams p, float* part)
+template <typename T, int BYTES, int MODE, bool ANY> __global__ void __launch_bounds__(kQThreads) fp4_amax_kernel(const __grid_constant__ QuantParams p, float* part)
 {
     using P = Piece<T, BYTES>;
     constexpr int kFlight = 4;
@@ -156,7 +156,7 @@ template <typename T, int BYTES, int MODE> __global__ void __launch_bounds__(kQT
     const T* x = static_cast<const T*>(p.x);
     const bool flat = MODE == PLAIN && contiguous(p);
     const int64_t rows = flat ? 1 : p.x_rows * p.batch, cols = flat ? p.x_rows * p.batch * p.cols : p.cols;
-    const int64_t per = cols / P::kElems;                            // whole pieces but for the end of a contiguous tensor
+    const int64_t per = ANY ? ceil_div(cols, P::kElems) : cols / P::kElems;     // whole pieces but for the end of a contiguous tensor
     const int64_t step = (int64_t)gridDim.x * kQThreads, div = per > 0 ? per : 1, drow = step / div, dpiece = step % div;
     const int64_t first = (int64_t)blockIdx.x * kQThreads + threadIdx.x;
     int64_t row = per > 0 ? first / div : rows, at = first % div;
@@ -168,7 +168,11 @@ template <typename T, int BYTES, int MODE> __global__ void __launch_bounds__(kQT
         for (int i = 0; i < kFlight; ++i) {
             token[i] = row;
             v[i].clear();
-            if (row < rows) v[i].load(x + (p.batch == 1 || flat ? row * p.ld : (row / p.x_rows) * p.batch_stride + (row % p.x_rows) * p.ld) + at * P::kElems);
+            if (row < rows) {
+                const T* from = x + (p.batch == 1 || flat ? row * p.ld : (row / p.x_rows) * p.batch_stride + (row % p.x_rows) * p.ld);
+                if constexpr (ANY) load_any<T, BYTES>(v[i].w, from, at * P::kElems, cols);
+                else v[i].load(from + at * P::kElems);
+            }
             row += drow;
             at += dpiece;
             if (at >= per) { at -= per; ++row; }
@@ -177,7 +181,7 @@ template <typename T, int BYTES, int MODE> __global__ void __launch_bounds__(kQT
         for (int i = 0; i < kFlight; ++i)
             if (token[i] < rows) m = fmaxf(m, piece_max<T, BYTES, MODE>(v[i], p, token[i]));
     }
-    if (flat && blockIdx.x == 0 && per * P::kElems + threadIdx.x < cols) {
+    if (!ANY && flat && blockIdx.x == 0 && per * P::kElems + threadIdx.x < cols) {
         Piece<T, (int)sizeof(T)> v;
         v.load(x + per * P::kElems + threadIdx.x);
         m = fmaxf(m, piece_max<T, (int)sizeof(T), PLAIN>(v, p, 0));
@@ -219,52 +223,6 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED 
     if (FMT != MOR_FP4_E4M3_16 || p.partial == nullptr) wait_for_predecessor();
     Raw<T> raw[2];
     float weight[2] = {1.f, 1.f};
-    constexpr int kInPitch = 128 * (int)sizeof(T) + 16;
-    if (p.access < 16) {        // rows that start anywhere: neighbouring lanes take neighbouring pieces, through shared memory
-        auto take = [&](auto bytes) {
-            using P = Piece<T, decltype(bytes)::value>;
-            constexpr int kPieces = 128 / P::kElems / 32;                  // per lane and row
-            for (int r0 = (tid >> 5) * 16; r0 < (tid >> 5) * 16 + 16; r0 += 4) {
-                P v[4][kPieces];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int64_t row = (int64_t)row_tile * 128 + r0 + i;
-                    int64_t src = row;
-                    bool have = row < p.rows;
-                    if constexpr (MODE != PLAIN) {
-                        const int32_t slot = have ? p.slot_of_row[row] : -1;
-                        have = slot >= 0;
-                        src = have ? token_of((uint32_t)slot, p) : 0;
-                    }
-#pragma unroll
-                    for (int j = 0; j < kPieces; ++j) {
-                        const int64_t col = (int64_t)col_tile * 128 + (j * 32 + (tid & 31)) * P::kElems;
-                        v[i][j].clear();
-                        if (have && col + P::kElems <= p.cols) {
-                            v[i][j].load(x + src * p.ld + col);
-                        } else if (have && col < p.cols) {                // the last piece of a row
-#pragma unroll
-                            for (int k = 0; k < P::kElems; ++k)
-                                if (col + k < p.cols) {
-                                    Piece<T, (int)sizeof(T)> one;
-                                    one.load(x + src * p.ld + col + k);
-                                    v[i][j].w[k * sizeof(T) / 4] |= one.w[0] << (8 * (k * sizeof(T) % 4));
-                                }
-                        }
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int j = 0; j < kPieces; ++j)
-                        v[i][j].store(reinterpret_cast<T*>(dyn + (r0 + i) * kInPitch) + (j * 32 + (tid & 31)) * P::kElems);
-            }
-        };
-        if (p.access == 8) take(std::integral_constant<int, 8>{});
-        else if (p.access == 4) take(std::integral_constant<int, 4>{});
-        else if constexpr (sizeof(T) == 2) take(std::integral_constant<int, 2>{});
-        __syncthreads();
-    }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         const int at = tid + i * kQThreads;
@@ -277,18 +235,12 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED 
             src = have ? token_of((uint32_t)slot, p) : 0;
             if (MODE == WEIGHTED && have) weight[i] = weight_at(p.weight, p.weight_dtype, slot);
         }
-        if (p.access < 16) {
-#pragma unroll
-            for (int j = 0; j < (int)sizeof(Raw<T>) / 4; j += 4) {
-                const uint4 q = *reinterpret_cast<const uint4*>(dyn + (at >> 2) * kInPitch + (at & 3) * kUnit * sizeof(T) + j * 4);
-                raw[i].w[j] = q.x; raw[i].w[j + 1] = q.y; raw[i].w[j + 2] = q.z; raw[i].w[j + 3] = q.w;
-            }
-        } else if (have) load_unit<T>(raw[i], x + src * p.ld + col, (int)min((int64_t)kUnit, p.cols - col), p.access);
+        if (have && p.access < 16) load_any<T, (int)sizeof(Raw<T>)>(raw[i].w, x + src * p.ld, col, p.cols);
+        else if (have) load_unit<T>(raw[i], x + src * p.ld + col, (int)min((int64_t)kUnit, p.cols - col), p.access);
         else
 #pragma unroll
             for (uint32_t& w : raw[i].w) w = 0;
     }
-    if (COLS && p.access < 16) __syncthreads();           // the tile takes the same memory
 
     TensorScale ts = {1.f, 1.f, 1.f};
     if constexpr (FMT == MOR_FP4_E4M3_16) {
@@ -300,19 +252,14 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED 
             for (uint32_t i = tid; i < p.n_partial; i += kQThreads) amax = fmaxf(amax, __ldcg(p.partial + i));
             amax = block_max(amax, red);
         } else {
-            const bool wide = p.access >= 16 && p.cols * (int64_t)sizeof(T) % 16 == 0;
-            auto scan = [&](auto bytes) {
-                using P = Piece<T, decltype(bytes)::value>;
-                const int64_t per = p.cols / P::kElems;
-                for (int64_t i = tid; i < per * p.x_rows * p.batch; i += kQThreads) {
-                    const int64_t r = i / per;
-                    P v;
-                    v.load(static_cast<const T*>(p.x) + (r / p.x_rows) * p.batch_stride + (r % p.x_rows) * p.ld + (i % per) * P::kElems);
-                    amax = fmaxf(amax, piece_max<T, decltype(bytes)::value, PLAIN>(v, p, 0));
-                }
-            };
-            if (wide) scan(std::integral_constant<int, 16>{});
-            else scan(std::integral_constant<int, (int)sizeof(T)>{});
+            using P = Piece<T, 16>;
+            const int64_t per = ceil_div(p.cols, P::kElems);
+            for (int64_t i = tid; i < per * p.x_rows * p.batch; i += kQThreads) {
+                const int64_t r = i / per;
+                P v;
+                load_any<T, 16>(v.w, static_cast<const T*>(p.x) + (r / p.x_rows) * p.batch_stride + (r % p.x_rows) * p.ld, i % per * P::kElems, p.cols);
+                amax = fmaxf(amax, piece_max<T, 16, PLAIN>(v, p, 0));
+            }
             amax = block_max(amax, red);
         }
         ts = tensor_scale_of(amax);
@@ -784,10 +731,9 @@ template <typename T, int FMT, bool ROWS, bool COLS, int MODE> cudaError_t quant
         }
     }
     constexpr bool kNarrow = sizeof(T) == 2 && MODE != WEIGHTED;
-    constexpr int most = COLS ? 128 * Tile<kNarrow>::kPitch + 128 * 64 : 128 * (128 * (int)sizeof(T) + 16);
-    const int smem = COLS || p.access < 16 ? most : 0;
+    constexpr int smem = COLS ? 128 * Tile<kNarrow>::kPitch + 128 * 64 : 0;
     static std::atomic<uint64_t> done{0};
-    if (smem > 0 && !allow_smem(fp4_quant_kernel<T, FMT, ROWS, COLS, MODE>, most, done)) return cudaErrorInvalidValue;
+    if (smem > 0 && !allow_smem(fp4_quant_kernel<T, FMT, ROWS, COLS, MODE>, smem, done)) return cudaErrorInvalidValue;
     return launch(fp4_quant_kernel<T, FMT, ROWS, COLS, MODE>, grid, kQThreads, smem, st, grid <= kEarlyGrid, p);
 }
 template <typename T, int FMT, int MODE> cudaError_t quant_dirs(const QuantParams& p, uint32_t grid, cudaStream_t st)
@@ -803,9 +749,9 @@ template <typename T, int MODE> cudaError_t quant_all(const QuantParams& p, int 
         const bool flat = MODE == PLAIN && contiguous(p);
         const int64_t width = flat ? 0 : p.cols * (int64_t)sizeof(T);
         const int access = flat ? access_bytes(p.x, 0, 0, (int)sizeof(T)) : p.access;
-        const cudaError_t e = access == 32 && width % 32 == 0   ? launch(fp4_amax_kernel<T, 32, MODE>, amax_grid, kQThreads, 0, st, true, p, part)
-                              : access >= 16 && width % 16 == 0 ? launch(fp4_amax_kernel<T, 16, MODE>, amax_grid, kQThreads, 0, st, true, p, part)
-                                                                : launch(fp4_amax_kernel<T, (int)sizeof(T), MODE>, amax_grid, kQThreads, 0, st, true, p, part);
+        const cudaError_t e = access == 32 && width % 32 == 0   ? launch(fp4_amax_kernel<T, 32, MODE, false>, amax_grid, kQThreads, 0, st, true, p, part)
+                              : access >= 16 && width % 16 == 0 ? launch(fp4_amax_kernel<T, 16, MODE, false>, amax_grid, kQThreads, 0, st, true, p, part)
+                                                                : launch(fp4_amax_kernel<T, 16, MODE, true>, amax_grid, kQThreads, 0, st, true, p, part);
         if (e != cudaSuccess) return e;
     }
     return format == MOR_FP4_E4M3_16 ? quant_dirs<T, MOR_FP4_E4M3_16, MODE>(p, grid, st) : quant_dirs<T, MOR_FP4_E8M0_32, MODE>(p, grid, st);

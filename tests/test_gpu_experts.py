@@ -127,6 +127,39 @@ def test_gather_combine_and_gradient(experts, tokens, top, n, hidden, align, wei
     assert none is None and torch.equal(again, dw)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("hidden", [30, 31, 264, 1001])
+def test_rows_that_start_anywhere(experts, hidden, dtype):
+    """Every offset from 16 bytes, odd pitches and widths: copies and weighted sums as from aligned rows, bit for bit."""
+    import torch
+
+    plan, row, slot, matrix = matrices(experts, 50, 5, 7, hidden, 1, dtype, hidden)
+    (_, x), (ys64, ys), (dy64, dy) = matrix(50), matrix(len(slot)), matrix(50)
+    w = torch.rand(50, 5, generator=torch.Generator().manual_seed(2)).cuda()
+
+    def moved(t, start, pitch):
+        wide = torch.full((t.shape[0], pitch), float("nan"), dtype=t.dtype, device="cuda")
+        wide[:, start : start + hidden] = t
+        return wide[:, start : start + hidden]
+
+    def even(t):                                       # whole pieces: the width and the pitch are multiples of 32 bytes
+        return torch.nn.functional.pad(t, (0, -hidden % 16))
+
+    spread, back = experts.gather(even(x), plan, w)[:, :hidden], experts.combine(even(ys), plan, w)[:, :hidden]
+    gys = experts.combine_grad(even(dy), even(ys), plan, w)[0][:, :hidden]
+    taken = np.where((row >= 0)[..., None], ys64.astype(np.float64)[np.maximum(row, 0)], 0.0)
+    terms = taken * dy64.astype(np.float64)[:, None, :]
+    room = hidden * 2.0 ** -24 * np.abs(terms).sum(-1)
+    for start in range(9):
+        pitch = hidden + start + start % 4
+        assert torch.equal(experts.gather(moved(x, start, pitch), plan, w), spread)
+        assert torch.equal(experts.combine(moved(ys, start, pitch), plan, w), back)
+        got, dw = experts.combine_grad(moved(dy, start, pitch + 1), moved(ys, start, pitch), plan, w)
+        assert torch.equal(got, gys)
+        dw = dw.cpu().numpy()
+        assert ((terms.sum(-1) - room).astype(np.float32) <= dw).all() and (dw <= (terms.sum(-1) + room).astype(np.float32)).all()
+
+
 @pytest.mark.parametrize("tokens,top,n,hidden", [(37, 2, 5, 1), (100, 3, 9, 33), (300, 5, 64, 520)])
 def test_rows_of_32_bits_beside_tokens_of_16(experts, tokens, top, n, hidden):
     import torch

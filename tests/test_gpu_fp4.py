@@ -138,6 +138,22 @@ def test_strides_alignment_and_stacks(fp4, fmt):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_rows_that_start_anywhere(fp4, fmt, dtype):
+    """Every offset from 16 bytes and odd pitches, from one tile to a tensor whose maximum is taken by a kernel of its own."""
+    import torch
+
+    for rows, cols in ((3, 20), (130, 150), (200, 301)):
+        x = draw(rows, cols, rows, "wide")
+        for start in range(9):
+            wide = torch.full((rows, cols + start + start % 3), 2.0 ** 60, dtype=torch.bfloat16 if dtype == "bf16" else torch.float32, device="cuda")
+            wide[:, start : start + cols] = tensor(x, dtype)
+            r, c = fp4.quantize(wide[:, start : start + cols], fmt, cols=True)
+            check_operand(r, x, fmt)
+            check_operand(c, x.T, fmt)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("rows,cols", [(1, 1), (1, 4096), (130, 100), (257, 1000)])
 def test_values_of_codes(fp4, fmt, rows, cols):
     import torch
