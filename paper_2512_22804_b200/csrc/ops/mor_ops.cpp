@@ -217,9 +217,7 @@ Pair quantize_(const Tensor& x, int format, bool rows, bool cols, const std::opt
     return out;
 }
 
-// Rows of the result have to start on 16 bytes; where they are padded at all, and where only kernels see them (`inner`), on 32: whole
-// sectors (3000 x 7001 x 1000 in FP32: 25 us against 40).
-Tensor matmul_(const Matrix& a, const Matrix& b, at::ScalarType type, int grouping, const Routes* plan, bool inner = false)
+Tensor matmul_(const Matrix& a, const Matrix& b, at::ScalarType type, int grouping, const Routes* plan)
 {
     want(a.buf.get_device() == b.buf.get_device(), "the operands are on different devices");
     on_gpu(a.buf, "a");
@@ -228,8 +226,8 @@ Tensor matmul_(const Matrix& a, const Matrix& b, at::ScalarType type, int groupi
     d.b = b.c;
     d.out_dtype = dtype_of(type, "out_dtype");
     d.grouping = grouping;
-    const int64_t per = d.out_dtype == MOR_DTYPE_BF16 ? 16 : 8, n = b.c.rows;
-    d.ldo = !inner && n % (per / 2) == 0 ? n : (n + per - 1) / per * per;
+    const int64_t per = d.out_dtype == MOR_DTYPE_BF16 ? 8 : 4, n = b.c.rows;
+    d.ldo = (n + per - 1) / per * per;                               // rows of the result start on 16 bytes
     if (plan != nullptr) {
         on_gpu(plan->starts, "plan");
         want(plan->align % 128 == 0, "the plan's rows have to be aligned to 128 for grouped products: experts.sort(..., align=128)");
@@ -244,10 +242,10 @@ Tensor matmul_(const Matrix& a, const Matrix& b, at::ScalarType type, int groupi
     check(mor_fp4_matmul(&d, stream()), "mor_fp4_matmul");
     return d.ldo == n ? out : out.narrow(-1, 0, n);
 }
-Tensor matmul_rows_(const Matrix& a, const Matrix& b, const Routes& plan, at::ScalarType type, bool inner = false)
+Tensor matmul_rows_(const Matrix& a, const Matrix& b, const Routes& plan, at::ScalarType type)
 {
     want(a.c.rows == plan.rows() && b.c.batch == plan.experts(), "a needs the plan's rows and b one matrix per expert");
-    return matmul_(a, b, type, MOR_GROUP_ROWS, &plan, inner);
+    return matmul_(a, b, type, MOR_GROUP_ROWS, &plan);
 }
 Tensor matmul_reduce_(const Matrix& a, const Matrix& b, const Routes& plan, at::ScalarType type)
 {
@@ -372,7 +370,7 @@ Tensor linear(const Tensor& x, const Tensor& w, int f)
 Tensor expert_forward(const Tensor& x, const Matrix& w, const Routes& plan, const Tensor& weight, bool cols, Tensor* ys, Tensor* a_t)
 {
     const Pair a = quantize_(x, w.c.format, true, cols, std::nullopt, &plan, std::nullopt);
-    *ys = matmul_rows_(*a.rows, w, plan, at::kFloat, true);
+    *ys = matmul_rows_(*a.rows, w, plan, at::kFloat);
     if (cols) *a_t = a.cols->buf;
     return combine(*ys, plan, weight, x.scalar_type());
 }
@@ -408,7 +406,7 @@ struct ExpertFn : torch::autograd::Function<ExpertFn> {
         if (need_weight) dweight = combine_grad(dy, ctx->saved_data["ys"].toTensor(), plan, weight, false).second;
         if (need_x || need_w) {
             const Pair g = quantize_(dy, format, need_x, need_w, std::nullopt, &plan, weight);
-            if (need_x) dx = combine(matmul_rows_(*g.rows, Matrix::over(ctx->saved_data["b"].toTensor(), e, k, n, format), plan, (at::ScalarType)s[4], true), plan, std::nullopt, (at::ScalarType)s[4]);
+            if (need_x) dx = combine(matmul_rows_(*g.rows, Matrix::over(ctx->saved_data["b"].toTensor(), e, k, n, format), plan, (at::ScalarType)s[4]), plan, std::nullopt, (at::ScalarType)s[4]);
             if (need_w) dw = matmul_reduce_(*g.cols, Matrix::over(ctx->saved_data["a"].toTensor(), 1, k, plan.rows(), format), plan, (at::ScalarType)s[5]);
         }
         return {dx, dw, Tensor(), dweight, Tensor(), Tensor(), Tensor(), Tensor()};

@@ -228,6 +228,23 @@ def grouped(counts, hidden, fmt, fp4, seed):
 COUNTS = [[1], [128], [0, 5, 0], [130, 0, 1, 256, 300], [7] * 40, [500, 129, 700]]
 
 
+@pytest.mark.parametrize("out", ["bf16", "fp32"])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_result_rows_that_start_half_a_sector_off(fp4, fmt, out):
+    """Rows of 16 bytes modulo 32: the same values as in rows that start on 32 bytes."""
+    import torch
+
+    d = torch.bfloat16 if out == "bf16" else torch.float32
+    n = 520 if out == "bf16" else 516
+    a = fp4.quantize(tensor(draw(300, 200, 1)), fmt, amax=torch.full((1,), 5.0, device="cuda"))[0]
+    w = tensor(draw(n + 24, 200, 2))
+    amax = torch.full((1,), 5.0, device="cuda")
+    got = fp4.matmul(a, fp4.quantize(w[:n], fmt, amax=amax)[0], d)
+    want = fp4.matmul(a, fp4.quantize(w[: n // 16 * 16 + 16], fmt, amax=amax)[0], d)
+    assert got.stride(0) * got.element_size() % 32 == 16 and want.stride(0) * want.element_size() % 32 == 0
+    assert torch.equal(got, want[:, :n])
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("counts", COUNTS, ids=str)
 @pytest.mark.parametrize("n,k", [(1, 64), (136, 300), (520, 257)])
