@@ -214,161 +214,165 @@ __global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 && MODE != WEIGHTED 
     __shared__ __align__(16) uint8_t col_scales[COLS ? kTiles * kScaleTile : 16];
     extern __shared__ __align__(16) uint8_t dyn[];                        // COLS: tile, then the codes of the transposed rows
     const int tid = threadIdx.x;
-    const uint32_t per = p.row_tiles * p.col_tiles;
-    const uint32_t batch = blockIdx.x / per, in_batch = blockIdx.x % per;
-    const uint32_t row_tile = in_batch / p.col_tiles, col_tile = in_batch % p.col_tiles;
-    const T* x = static_cast<const T*>(p.x) + (int64_t)batch * p.batch_stride;
-
-    // both units' loads first: the tile is in flight while the tensor maximum is waited for (x is older than the kernel that takes it)
-    if (FMT != MOR_FP4_E4M3_16 || p.partial == nullptr) wait_for_predecessor();
-    Raw<T> raw[2];
-    float weight[2] = {1.f, 1.f};
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int at = tid + i * kQThreads;
-        const int64_t row = (int64_t)row_tile * 128 + (at >> 2), col = (int64_t)col_tile * 128 + (at & 3) * kUnit;
-        int64_t src = row;
-        bool have = row < p.rows && col < p.cols;
-        if constexpr (MODE != PLAIN) {
-            const int32_t slot = row < p.rows ? p.slot_of_row[row] : -1;
-            have = have && slot >= 0;
-            src = have ? token_of((uint32_t)slot, p) : 0;
-            if (MODE == WEIGHTED && have) weight[i] = weight_at(p.weight, p.weight_dtype, slot);
-        }
-        if (have && p.access < 16) load_any<T, (int)sizeof(Raw<T>)>(raw[i].w, x + src * p.ld, col, p.cols);
-        else if (have) load_unit<T>(raw[i], x + src * p.ld + col, (int)min((int64_t)kUnit, p.cols - col), p.access);
-        else
-#pragma unroll
-            for (uint32_t& w : raw[i].w) w = 0;
-    }
-
+    const uint32_t per = p.row_tiles * p.col_tiles, tiles = per * (uint32_t)p.batch;
     TensorScale ts = {1.f, 1.f, 1.f};
-    if constexpr (FMT == MOR_FP4_E4M3_16) {
-        float amax = 0.f;
-        if (p.amax != nullptr) {
-            amax = *p.amax;
-        } else if (p.partial != nullptr) {
-            wait_for_predecessor();
-            for (uint32_t i = tid; i < p.n_partial; i += kQThreads) amax = fmaxf(amax, __ldcg(p.partial + i));
-            amax = block_max(amax, red);
-        } else {
-            using P = Piece<T, 16>;
-            const int64_t per = ceil_div(p.cols, P::kElems);
-            for (int64_t i = tid; i < per * p.x_rows * p.batch; i += kQThreads) {
-                const int64_t r = i / per;
-                P v;
-                load_any<T, 16>(v.w, static_cast<const T*>(p.x) + (r / p.x_rows) * p.batch_stride + (r % p.x_rows) * p.ld, i % per * P::kElems, p.cols);
-                amax = fmaxf(amax, piece_max<T, 16, PLAIN>(v, p, 0));
-            }
-            amax = block_max(amax, red);
-        }
-        ts = tensor_scale_of(amax);
-        fill_factors(factors, ts.t, tid);
-        __syncthreads();
-    }
-    if (blockIdx.x == 0 && tid == 0) {
-        if (ROWS) *p.r_t = ts.t;
-        if (COLS) *p.c_t = ts.t;
-    }
+    for (uint64_t tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const uint32_t batch = (uint32_t)tile / per, in_batch = (uint32_t)tile % per;
+        const uint32_t row_tile = in_batch / p.col_tiles, col_tile = in_batch % p.col_tiles;
+        const T* x = static_cast<const T*>(p.x) + (int64_t)batch * p.batch_stride;
 
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int at = tid + i * kQThreads, lrow = at >> 2, u = at & 3;
-        const int64_t row = (int64_t)row_tile * 128 + lrow, col = (int64_t)col_tile * 128 + u * kUnit;
-        float v[kNarrow ? 1 : kUnit];                                       // FP32, or BF16 as it came
-        if constexpr (!kNarrow) unpack<T>(raw[i], v);
-        if constexpr (MODE == WEIGHTED) {
-#pragma unroll
-            for (float& e : v) e *= weight[i];
-        }
-        if constexpr (COLS) {
-            uint8_t* to = dyn + lrow * kPitch;
-            if constexpr (kNarrow) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    *reinterpret_cast<uint4*>(to + L::chunk(lrow, u * 4 + j) * 16) = make_uint4(raw[i].w[4 * j], raw[i].w[4 * j + 1], raw[i].w[4 * j + 2], raw[i].w[4 * j + 3]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) *reinterpret_cast<float4*>(to + L::chunk(lrow, u * 8 + j) * 16) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-            }
-        }
-        if constexpr (ROWS) {
-            uint32_t scales;
-            float a[kPerUnit];
-#pragma unroll
-            for (int k = 0; k < kPerUnit; ++k) {
-                if constexpr (kNarrow) a[k] = amax_of_pair(amax_of_words<16 / kPerUnit>(raw[i].w + k * (16 / kPerUnit)));
-                else a[k] = amax_of<kUnit / kPerUnit>(v + k * (kUnit / kPerUnit));
-            }
-            uint4 codes;
-            if constexpr (kNarrow) codes = quantise_unit<FMT>(UnitBf16<PAIRS>{raw[i].w}, a, ts, factors, scales);
-            else codes = quantise_unit<FMT>(UnitF32{v}, a, ts, factors, scales);
-            if (row < p.rows && col < p.cols)
-                *reinterpret_cast<uint4*>(p.r_codes + ((int64_t)batch * p.rows + row) * p.r_ld + col / 2) = codes;
-            uint8_t* s = row_scales + ((u * kPerUnit) >> 2) * kScaleTile + scale_at(lrow, u * kPerUnit);
-            if constexpr (kPerUnit == 2) *reinterpret_cast<uint16_t*>(s) = row < p.rows && col < p.cols ? (uint16_t)scales : 0;
-            else *s = row < p.rows && col < p.cols ? (uint8_t)scales : 0;
-        }
-    }
-    __syncthreads();
-    if constexpr (ROWS) {
-        const uint32_t ktile = col_tile * kTiles + (tid >> 5);
-        if (tid < kTiles * 32 && ktile < p.r_ktiles)
-            *reinterpret_cast<uint4*>(p.r_scales + (((int64_t)batch * p.row_tiles + row_tile) * p.r_ktiles + ktile) * kScaleTile + (tid & 31) * 16) =
-                *reinterpret_cast<const uint4*>(row_scales + tid * 16);
-    }
-    if constexpr (COLS) {
-        uint8_t* stage = dyn + 128 * kPitch;
-        auto put = [&](int lcol, int u, const auto& unit, const float* a) {
-            uint32_t scales;
-            const uint4 codes = quantise_unit<FMT>(unit, a, ts, factors, scales);
-            *reinterpret_cast<uint4*>(stage + stage_at(lcol, u)) = codes;
-            const bool in = (int64_t)col_tile * 128 + lcol < p.cols && (int64_t)row_tile * 128 + u * kUnit < p.rows;
-            uint8_t* s = col_scales + ((u * kPerUnit) >> 2) * kScaleTile + scale_at(lcol, u * kPerUnit);
-            if constexpr (kPerUnit == 2) *reinterpret_cast<uint16_t*>(s) = in ? (uint16_t)scales : 0;
-            else *s = in ? (uint8_t)scales : 0;
-        };
-        if constexpr (kNarrow) {             // two neighbouring columns (one word) over 32 rows
-            const int pair = tid & 63, u = tid >> 6;
-            const uint8_t* from[2] = {dyn + u * kUnit * kPitch + L::chunk(0, pair >> 2) * 16 + (pair & 3) * 4,
-                                      dyn + u * kUnit * kPitch + L::chunk(1, pair >> 2) * 16 + (pair & 3) * 4};
-            uint32_t w[kUnit], m[kPerUnit];
-            float a[kPerUnit];
-#pragma unroll
-            for (int i = 0; i < kUnit; ++i) w[i] = *reinterpret_cast<const uint32_t*>(from[i & 1] + i * kPitch);
-#pragma unroll
-            for (int k = 0; k < kPerUnit; ++k) m[k] = amax_of_words<kUnit / kPerUnit>(w + k * (kUnit / kPerUnit));
-#pragma unroll
-            for (int k = 0; k < kPerUnit; ++k) a[k] = fabsf(bf16_low(m[k]));
-            put(2 * pair, u, UnitBf16<LOW>{w}, a);
-#pragma unroll
-            for (int k = 0; k < kPerUnit; ++k) a[k] = fabsf(bf16_high(m[k]));
-            put(2 * pair + 1, u, UnitBf16<HIGH>{w}, a);
-        } else {
-#pragma unroll 1
-            for (int half = 0; half < 2; ++half) {
-                const int lcol = tid & 127, u = (tid >> 7) + 2 * half;
-                float v[kUnit], a[kPerUnit];
-#pragma unroll
-                for (int i = 0; i < kUnit; ++i) v[i] = *reinterpret_cast<const float*>(dyn + (u * kUnit + i) * kPitch + L::chunk(i & 1, lcol >> 2) * 16 + (lcol & 3) * 4);
-#pragma unroll
-                for (int k = 0; k < kPerUnit; ++k) a[k] = amax_of<kUnit / kPerUnit>(v + k * (kUnit / kPerUnit));
-                put(lcol, u, UnitF32{v}, a);
-            }
-        }
-        __syncthreads();
+        // both units' loads first: the tile is in flight while the tensor maximum is waited for (x is older than the kernel that takes it)
+        const bool first = tile == blockIdx.x;
+        if (first && (FMT != MOR_FP4_E4M3_16 || p.partial == nullptr)) wait_for_predecessor();
+        Raw<T> raw[2];
+        float weight[2] = {1.f, 1.f};
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const int at = tid + i * kQThreads, lcol = at >> 2, u = at & 3;
-            const int64_t col = (int64_t)col_tile * 128 + lcol, row = (int64_t)row_tile * 128 + u * kUnit;
-            if (col < p.cols && row < p.rows)
-                *reinterpret_cast<uint4*>(p.c_codes + ((int64_t)batch * p.cols + col) * p.c_ld + row / 2) =
-                    *reinterpret_cast<const uint4*>(stage + stage_at(lcol, u));
+            const int at = tid + i * kQThreads;
+            const int64_t row = (int64_t)row_tile * 128 + (at >> 2), col = (int64_t)col_tile * 128 + (at & 3) * kUnit;
+            int64_t src = row;
+            bool have = row < p.rows && col < p.cols;
+            if constexpr (MODE != PLAIN) {
+                const int32_t slot = row < p.rows ? p.slot_of_row[row] : -1;
+                have = have && slot >= 0;
+                src = have ? token_of((uint32_t)slot, p) : 0;
+                if (MODE == WEIGHTED && have) weight[i] = weight_at(p.weight, p.weight_dtype, slot);
+            }
+            if (have && p.access < 16) load_any<T, (int)sizeof(Raw<T>)>(raw[i].w, x + src * p.ld, col, p.cols);
+            else if (have) load_unit<T>(raw[i], x + src * p.ld + col, (int)min((int64_t)kUnit, p.cols - col), p.access);
+            else
+#pragma unroll
+                for (uint32_t& w : raw[i].w) w = 0;
         }
-        const uint32_t ktile = row_tile * kTiles + (tid >> 5);
-        if (tid < kTiles * 32 && ktile < p.c_ktiles)
-            *reinterpret_cast<uint4*>(p.c_scales + (((int64_t)batch * p.c_row_tiles + col_tile) * p.c_ktiles + ktile) * kScaleTile + (tid & 31) * 16) =
-                *reinterpret_cast<const uint4*>(col_scales + tid * 16);
+
+        if (FMT == MOR_FP4_E4M3_16 && first) {
+            float amax = 0.f;
+            if (p.amax != nullptr) {
+                amax = *p.amax;
+            } else if (p.partial != nullptr) {
+                wait_for_predecessor();
+                for (uint32_t i = tid; i < p.n_partial; i += kQThreads) amax = fmaxf(amax, __ldcg(p.partial + i));
+                amax = block_max(amax, red);
+            } else {
+                using P = Piece<T, 16>;
+                const int64_t per = ceil_div(p.cols, P::kElems);
+                for (int64_t i = tid; i < per * p.x_rows * p.batch; i += kQThreads) {
+                    const int64_t r = i / per;
+                    P v;
+                    load_any<T, 16>(v.w, static_cast<const T*>(p.x) + (r / p.x_rows) * p.batch_stride + (r % p.x_rows) * p.ld, i % per * P::kElems, p.cols);
+                    amax = fmaxf(amax, piece_max<T, 16, PLAIN>(v, p, 0));
+                }
+                amax = block_max(amax, red);
+            }
+            ts = tensor_scale_of(amax);
+            fill_factors(factors, ts.t, tid);
+            __syncthreads();
+        }
+        if (tile == 0 && tid == 0) {
+            if (ROWS) *p.r_t = ts.t;
+            if (COLS) *p.c_t = ts.t;
+        }
+
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int at = tid + i * kQThreads, lrow = at >> 2, u = at & 3;
+            const int64_t row = (int64_t)row_tile * 128 + lrow, col = (int64_t)col_tile * 128 + u * kUnit;
+            float v[kNarrow ? 1 : kUnit];                                       // FP32, or BF16 as it came
+            if constexpr (!kNarrow) unpack<T>(raw[i], v);
+            if constexpr (MODE == WEIGHTED) {
+#pragma unroll
+                for (float& e : v) e *= weight[i];
+            }
+            if constexpr (COLS) {
+                uint8_t* to = dyn + lrow * kPitch;
+                if constexpr (kNarrow) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        *reinterpret_cast<uint4*>(to + L::chunk(lrow, u * 4 + j) * 16) = make_uint4(raw[i].w[4 * j], raw[i].w[4 * j + 1], raw[i].w[4 * j + 2], raw[i].w[4 * j + 3]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) *reinterpret_cast<float4*>(to + L::chunk(lrow, u * 8 + j) * 16) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                }
+            }
+            if constexpr (ROWS) {
+                uint32_t scales;
+                float a[kPerUnit];
+#pragma unroll
+                for (int k = 0; k < kPerUnit; ++k) {
+                    if constexpr (kNarrow) a[k] = amax_of_pair(amax_of_words<16 / kPerUnit>(raw[i].w + k * (16 / kPerUnit)));
+                    else a[k] = amax_of<kUnit / kPerUnit>(v + k * (kUnit / kPerUnit));
+                }
+                uint4 codes;
+                if constexpr (kNarrow) codes = quantise_unit<FMT>(UnitBf16<PAIRS>{raw[i].w}, a, ts, factors, scales);
+                else codes = quantise_unit<FMT>(UnitF32{v}, a, ts, factors, scales);
+                if (row < p.rows && col < p.cols)
+                    *reinterpret_cast<uint4*>(p.r_codes + ((int64_t)batch * p.rows + row) * p.r_ld + col / 2) = codes;
+                uint8_t* s = row_scales + ((u * kPerUnit) >> 2) * kScaleTile + scale_at(lrow, u * kPerUnit);
+                if constexpr (kPerUnit == 2) *reinterpret_cast<uint16_t*>(s) = row < p.rows && col < p.cols ? (uint16_t)scales : 0;
+                else *s = row < p.rows && col < p.cols ? (uint8_t)scales : 0;
+            }
+        }
+        __syncthreads();
+        if constexpr (ROWS) {
+            const uint32_t ktile = col_tile * kTiles + (tid >> 5);
+            if (tid < kTiles * 32 && ktile < p.r_ktiles)
+                *reinterpret_cast<uint4*>(p.r_scales + (((int64_t)batch * p.row_tiles + row_tile) * p.r_ktiles + ktile) * kScaleTile + (tid & 31) * 16) =
+                    *reinterpret_cast<const uint4*>(row_scales + tid * 16);
+        }
+        if constexpr (COLS) {
+            uint8_t* stage = dyn + 128 * kPitch;
+            auto put = [&](int lcol, int u, const auto& unit, const float* a) {
+                uint32_t scales;
+                const uint4 codes = quantise_unit<FMT>(unit, a, ts, factors, scales);
+                *reinterpret_cast<uint4*>(stage + stage_at(lcol, u)) = codes;
+                const bool in = (int64_t)col_tile * 128 + lcol < p.cols && (int64_t)row_tile * 128 + u * kUnit < p.rows;
+                uint8_t* s = col_scales + ((u * kPerUnit) >> 2) * kScaleTile + scale_at(lcol, u * kPerUnit);
+                if constexpr (kPerUnit == 2) *reinterpret_cast<uint16_t*>(s) = in ? (uint16_t)scales : 0;
+                else *s = in ? (uint8_t)scales : 0;
+            };
+            if constexpr (kNarrow) {             // two neighbouring columns (one word) over 32 rows
+                const int pair = tid & 63, u = tid >> 6;
+                const uint8_t* from[2] = {dyn + u * kUnit * kPitch + L::chunk(0, pair >> 2) * 16 + (pair & 3) * 4,
+                                          dyn + u * kUnit * kPitch + L::chunk(1, pair >> 2) * 16 + (pair & 3) * 4};
+                uint32_t w[kUnit], m[kPerUnit];
+                float a[kPerUnit];
+#pragma unroll
+                for (int i = 0; i < kUnit; ++i) w[i] = *reinterpret_cast<const uint32_t*>(from[i & 1] + i * kPitch);
+#pragma unroll
+                for (int k = 0; k < kPerUnit; ++k) m[k] = amax_of_words<kUnit / kPerUnit>(w + k * (kUnit / kPerUnit));
+#pragma unroll
+                for (int k = 0; k < kPerUnit; ++k) a[k] = fabsf(bf16_low(m[k]));
+                put(2 * pair, u, UnitBf16<LOW>{w}, a);
+#pragma unroll
+                for (int k = 0; k < kPerUnit; ++k) a[k] = fabsf(bf16_high(m[k]));
+                put(2 * pair + 1, u, UnitBf16<HIGH>{w}, a);
+            } else {
+#pragma unroll 1
+                for (int half = 0; half < 2; ++half) {
+                    const int lcol = tid & 127, u = (tid >> 7) + 2 * half;
+                    float v[kUnit], a[kPerUnit];
+#pragma unroll
+                    for (int i = 0; i < kUnit; ++i) v[i] = *reinterpret_cast<const float*>(dyn + (u * kUnit + i) * kPitch + L::chunk(i & 1, lcol >> 2) * 16 + (lcol & 3) * 4);
+#pragma unroll
+                    for (int k = 0; k < kPerUnit; ++k) a[k] = amax_of<kUnit / kPerUnit>(v + k * (kUnit / kPerUnit));
+                    put(lcol, u, UnitF32{v}, a);
+                }
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int at = tid + i * kQThreads, lcol = at >> 2, u = at & 3;
+                const int64_t col = (int64_t)col_tile * 128 + lcol, row = (int64_t)row_tile * 128 + u * kUnit;
+                if (col < p.cols && row < p.rows)
+                    *reinterpret_cast<uint4*>(p.c_codes + ((int64_t)batch * p.cols + col) * p.c_ld + row / 2) =
+                        *reinterpret_cast<const uint4*>(stage + stage_at(lcol, u));
+            }
+            const uint32_t ktile = row_tile * kTiles + (tid >> 5);
+            if (tid < kTiles * 32 && ktile < p.c_ktiles)
+                *reinterpret_cast<uint4*>(p.c_scales + (((int64_t)batch * p.c_row_tiles + col_tile) * p.c_ktiles + ktile) * kScaleTile + (tid & 31) * 16) =
+                    *reinterpret_cast<const uint4*>(col_scales + tid * 16);
+        }
+        __syncthreads();
     }
 }
 
@@ -734,7 +738,12 @@ template <typename T, int FMT, bool ROWS, bool COLS, int MODE> cudaError_t quant
     constexpr int smem = COLS ? 128 * Tile<kNarrow>::kPitch + 128 * 64 : 0;
     static std::atomic<uint64_t> done{0};
     if (smem > 0 && !allow_smem(fp4_quant_kernel<T, FMT, ROWS, COLS, MODE>, smem, done)) return cudaErrorInvalidValue;
-    return launch(fp4_quant_kernel<T, FMT, ROWS, COLS, MODE>, grid, kQThreads, smem, st, grid <= kEarlyGrid, p);
+    // As many CTAs as are resident, each walking its tiles: the tensor's scale and its table are made once a CTA (8192 x 14336 E4M3_16 rows
+    // with the maximum 91 us, 104 with a CTA per tile; 4096 x 4096 15 and 18.5), and the kernel may start early (4096 x 4096 E8M0_32
+    // 8.0 us and 10.3).  E8M0_32 has nothing to share, and a CTA per tile is ahead beyond 2048 tiles (FP32 8192 x 14336: 89 us and 95).
+    constexpr uint32_t most = 148 * (kNarrow ? 4 : 2);
+    const bool walk = FMT == MOR_FP4_E4M3_16 || grid <= 2048;
+    return launch(fp4_quant_kernel<T, FMT, ROWS, COLS, MODE>, walk && grid > most ? most : grid, kQThreads, smem, st, walk, p);
 }
 template <typename T, int FMT, int MODE> cudaError_t quant_dirs(const QuantParams& p, uint32_t grid, cudaStream_t st)
 {
