@@ -92,6 +92,9 @@ __device__ int32_t block_scan(int32_t v, int32_t* shared)
     return v + (warp > 0 ? shared[warp - 1] : 0);
 }
 
+// Each CTA finds where every expert starts (from all chunks' counts) and where its own warps' slots of that expert go, and walks its
+// slots once more: a slot's row is its expert's next place for the warp plus its rank among the lanes with the same expert.  No atomics,
+// so equal experts keep slot order.  32768 slots of 64 experts, both kernels: 9 us, all of it latency.
 __global__ void __launch_bounds__(kSortThreads) expert_place_kernel(const __grid_constant__ SortParams p)
 {
     extern __shared__ int32_t counts[];                 // [warps][experts], then the next row of each
@@ -257,6 +260,8 @@ template <typename T, int BYTES> __device__ __forceinline__ void spread_any(cons
     }
 }
 
+// A token is read once and written to each of its rows.  Bound by memory, mostly by what it writes: 8192 tokens of 4096 BF16, top 4 of 64,
+// 54 us (336 MB, 6.2 TB/s); 4095 wide 61 us (one element at a time: 123 us).
 template <typename T, int BYTES, bool ANY> __global__ void __launch_bounds__(256) expert_gather_kernel(const __grid_constant__ MoveParams p)
 {
     using P = Piece<T, BYTES>;
@@ -285,6 +290,8 @@ template <typename T, int BYTES, bool ANY> __global__ void __launch_bounds__(256
     }
 }
 
+// A token's rows are in flight together and summed in slot order in FP32.  Bound by memory: the same sizes 56 us (336 MB, 6.0 TB/s); 4095
+// wide 82 us (one element at a time: 133 us).
 template <typename T, typename R, int BYTES, bool ANY> __global__ void __launch_bounds__(256) expert_combine_kernel(const __grid_constant__ MoveParams p)
 {
     using P = Piece<T, BYTES>;
@@ -328,7 +335,8 @@ template <typename T, typename R, int BYTES, bool ANY> __global__ void __launch_
 }
 
 // The sums over hidden of <dy, ys> are taken per thread in column order, then over the CTA in a fixed tree: the result
-// does not change from run to run.  Four CTAs an SM (64 registers): with the 118 that the compiler would take, two, and not enough
+// does not change from run to run.  Bound by memory: the same sizes 93 us (604 MB, 6.5 TB/s); 4095 wide, where dy is read once for the
+// sums and once for the rows, 170 us (one element at a time: 237 us).  Four CTAs an SM (64 registers): with the 118 that the compiler would take, two, and not enough
 // rows are in flight.
 template <typename T, typename R, int BYTES, bool ANY> __global__ void __launch_bounds__(256, 4) expert_grad_kernel(const __grid_constant__ MoveParams p)
 {

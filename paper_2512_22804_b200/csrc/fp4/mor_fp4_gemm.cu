@@ -209,6 +209,13 @@ template <typename T, int COLS> __device__ __forceinline__ void store_row_off16(
     *reinterpret_cast<uint4*>(out + kWords - 4) = four(kWords - 4);
 }
 
+// Wide.  A pair's tile of 256 x 256 fetches 2 x 128 rows of either operand per CTA, the least per product that tensor memory holds
+// with a stage's scales; one accumulator set, handed over after its registers are filled, so that the stores run under the next tile's
+// products.  8192 x 14336 x 4096 E4M3_16 -> BF16: 190-200 us (4.8-5.0 PFLOP/s) in a short run, 226 us at the 1000 W cap (1.4 GHz);
+// 8192 x 4096 x 8192: 100 us (5.5 PFLOP/s).  Its copies alone take 142 us (54 bytes a clock and SM from L2), its products alone 157 us,
+// and without the result's stores it is 30 us faster.  256 x 192 tiles with two accumulator sets: 215 us.
+// Groups of rows, 28,700 rows over 32 groups, E8M0_32: 2048 -> 1024 40 us, 1024 -> 2048 53 us, 29 us each without the stores (64 and 127 MB);
+// groups of the reduction axis, 32 results of 1024 x 2048: 62 us.
 template <int CG, int NT, int FMT, typename T, int GROUP>
 __global__ void __launch_bounds__(kWideThreads, 1) fp4_wide_kernel(const __grid_constant__ GemmParams p)
 {
@@ -397,6 +404,9 @@ template <int NT, int FMT> struct Narrow {
 constexpr int kNarrowThreads = 192;    // copy, issue, four warps that read the accumulators out
 constexpr int kMaxSplit = 8;
 
+// Bound by the read of the weights: 3.2 us and then 6.5 TB/s (14336 rows of b, K from 4096 to 65536).  Two CTAs an SM keep a ring of copies in
+// flight each; the split over a cluster fills the SMs where there are few tiles (16 x 14336 x 4096: 7.0 us with its launch), and adding
+// the parts in rank order keeps the result the same from run to run.
 template <int NT, int FMT, typename T> __global__ void __launch_bounds__(kNarrowThreads, 2) fp4_narrow_kernel(const __grid_constant__ GemmParams p)
 {
     using W = Narrow<NT, FMT>;
