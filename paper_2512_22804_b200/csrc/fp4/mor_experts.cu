@@ -184,7 +184,8 @@ struct MoveParams {
 // Rows that start anywhere or are no whole number of pieces (ANY): pieces are laid out from the aligned addresses of the row that is
 // written, what is read is shifted into place, and some forty elements at the ends go one by one, a thread each.
 template <typename T, typename R, int BYTES> struct Inner {
-    static constexpr int kElems = BYTES / (int)sizeof(T), kPer = 16 / (int)sizeof(R);
+    // kPer: elements that a chunk of either type may reach past a piece's
+    static constexpr int kElems = BYTES / (int)sizeof(T), kPer = 16 / (int)(sizeof(T) < sizeof(R) ? sizeof(T) : sizeof(R));
     int64_t first, end;          // where whole pieces begin and end, far enough inside for any source's chunks
     int edges;                   // elements outside
     __device__ __forceinline__ Inner(const T* to, int64_t n)

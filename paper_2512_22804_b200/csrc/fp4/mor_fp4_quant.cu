@@ -1,7 +1,7 @@
 // Quantisation to microscaled 4-bit codes, along the rows, along the columns, or both from one read, and its inverse.
 //
 // Both directions are bound by memory: per element 2 (or 4) bytes in, 0.5 + 1/16 (or 1/32) out per direction; the tensor maximum
-// of E4M3_16 costs one more read unless the caller has it.  One CTA takes a tile of 128 x 128 elements, so that the
+// of E4M3_16 costs one more read unless the caller has it.  A CTA takes tiles of 128 x 128 elements, so that the
 // scale tiles it writes (128 rows x 4 blocks) are whole and leave as 16-byte stores, and in the column direction the codes of a
 // transposed row leave 64 bytes at a time.  A thread takes units of 32 consecutive elements: one or two blocks, so a block's
 // maximum needs no exchange between threads.  For the column direction the tile goes through shared memory once, in the

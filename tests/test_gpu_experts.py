@@ -180,6 +180,31 @@ def test_rows_of_32_bits_beside_tokens_of_16(experts, tokens, top, n, hidden):
     assert dys.dtype == torch.bfloat16 and torch.equal(dys, experts.gather(tdy, plan, tw))
 
 
+@pytest.mark.parametrize("hidden", [36, 43, 267, 1030])
+def test_rows_of_32_bits_beside_tokens_of_16_that_start_anywhere(experts, hidden):
+    import torch
+
+    plan, row, slot, matrix = matrices(experts, 40, 3, 6, hidden, 1, "bf16", hidden)
+    dy, tdy = matrix(40)
+    rng = np.random.default_rng(5)
+    ys = rng.standard_normal((len(slot), hidden)).astype(np.float32)
+    w = rng.random((40, 3)).astype(np.float32)
+    tw = cuda(w)
+    taken = np.where((row >= 0)[..., None], ys.astype(np.float64)[np.maximum(row, 0)], 0.0)
+    want, room = (taken * w[..., None]).sum(1), 3 * 2.0 ** -24 * (np.abs(taken) * w[..., None]).sum(1)
+    terms = taken * dy.astype(np.float64)[:, None, :]
+    for start in range(9):
+        wide = torch.full((40, hidden + start + 1), float("nan"), dtype=torch.bfloat16, device="cuda")
+        wide[:, start : start + hidden] = tdy
+        rows = torch.full((len(slot), hidden + start % 5), float("nan"), device="cuda")
+        rows[:, start % 5 :] = cuda(ys)
+        y = experts.combine(rows[:, start % 5 :], plan, tw, torch.bfloat16).float().cpu().numpy()
+        assert (plain.bf16((want - room).astype(np.float32)) <= y).all() and (y <= plain.bf16((want + room).astype(np.float32))).all()
+        dys, dw = experts.combine_grad(wide[:, start : start + hidden], rows[:, start % 5 :], plan, tw)
+        assert (np.abs(dw.double().cpu().numpy() - terms.sum(-1)) <= hidden * 2.0 ** -24 * np.abs(terms).sum(-1)).all()
+        assert torch.equal(dys, experts.gather(tdy, plan, tw))
+
+
 def test_nan_of_an_empty_row_goes_nowhere_and_strides(experts):
     import torch
 
