@@ -238,19 +238,22 @@ __device__ __forceinline__ float weight_at(const void* w, int dtype, int64_t i)
     return dtype == MOR_DTYPE_BF16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(w)[i]) : static_cast<const float*>(w)[i];
 }
 
-// What one thread moves at a time: BYTES bytes as 32-bit values.
-template <typename T, int BYTES> struct Piece {
+// What one thread moves at a time: BYTES bytes as 32-bit values.  LOAD: bytes of a load at most, where an address is a multiple of fewer.
+template <typename T, int BYTES, int LOAD = BYTES> struct Piece {
     static constexpr int kElems = BYTES / (int)sizeof(T);
     static constexpr int kWords = BYTES < 4 ? 1 : BYTES / 4;
     uint32_t w[kWords];
     __device__ __forceinline__ void load(const T* p)
     {
-        if constexpr (BYTES >= 32) {
+        if constexpr (BYTES >= 32 && LOAD >= 32) {
 #pragma unroll
             for (int i = 0; i < kWords; i += 8) ldg256(w + i, reinterpret_cast<const uint32_t*>(p) + i);
-        } else if constexpr (BYTES == 16) {
-            const uint4 q = *reinterpret_cast<const uint4*>(p);
-            w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+        } else if constexpr (BYTES >= 16) {
+#pragma unroll
+            for (int i = 0; i < kWords; i += 4) {
+                const uint4 q = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint32_t*>(p) + i);
+                w[i] = q.x; w[i + 1] = q.y; w[i + 2] = q.z; w[i + 3] = q.w;
+            }
         } else if constexpr (BYTES == 4) w[0] = *reinterpret_cast<const uint32_t*>(p);
         else w[0] = *reinterpret_cast<const uint16_t*>(p);
     }

@@ -205,6 +205,32 @@ def test_rows_of_32_bits_beside_tokens_of_16_that_start_anywhere(experts, hidden
         assert torch.equal(dys, experts.gather(tdy, plan, tw))
 
 
+@pytest.mark.parametrize("hidden", [8, 40, 264])
+def test_rows_of_32_bits_beside_tokens_of_16_from_every_start(experts, hidden):
+    """Widths of whole pieces: FP32 rows that start 4, 8, .. 32 bytes past a multiple of 32, with pitches that keep or shift the start."""
+    import torch
+
+    plan, row, slot, matrix = matrices(experts, 40, 3, 6, hidden, 1, "bf16", hidden)
+    dy, tdy = matrix(40)
+    rng = np.random.default_rng(6)
+    ys = rng.standard_normal((len(slot), hidden)).astype(np.float32)
+    w = rng.random((40, 3)).astype(np.float32)
+    tw = cuda(w)
+    taken = np.where((row >= 0)[..., None], ys.astype(np.float64)[np.maximum(row, 0)], 0.0)
+    want, room = (taken * w[..., None]).sum(1), 3 * 2.0 ** -24 * (np.abs(taken) * w[..., None]).sum(1)
+    terms = taken * dy.astype(np.float64)[:, None, :]
+    for start in range(9):
+        for more in (8, 12, 9):                        # the pitch: a multiple of 32 bytes, of 16, of 4
+            rows = torch.full((len(slot), hidden + more), float("nan"), device="cuda")
+            rows[:, start : start + hidden] = cuda(ys)
+            rows = rows[:, start : start + hidden]
+            y = experts.combine(rows, plan, tw, torch.bfloat16).float().cpu().numpy()
+            assert (plain.bf16((want - room).astype(np.float32)) <= y).all() and (y <= plain.bf16((want + room).astype(np.float32))).all()
+            dys, dw = experts.combine_grad(tdy, rows, plan, tw)
+            assert (np.abs(dw.double().cpu().numpy() - terms.sum(-1)) <= hidden * 2.0 ** -24 * np.abs(terms).sum(-1)).all()
+            assert torch.equal(dys, experts.gather(tdy, plan, tw))
+
+
 def test_nan_of_an_empty_row_goes_nowhere_and_strides(experts):
     import torch
 
