@@ -1,0 +1,111 @@
+"""The 4-bit layers as autograd and serving code meets them: gradients with any strides, results that are changed in place, saved tensors,
+second derivatives, streams, modes and errors."""
+import os
+import subprocess
+import sys
+
+import numpy as np
+import pytest
+
+from tests import plain_fp4 as plain
+
+pytestmark = pytest.mark.gpu
+FORMATS = ["e4m3_16", "e8m0_32"]
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def fp4():
+    from paper_2512_22804_b200 import fp4
+
+    return fp4
+
+
+@pytest.fixture(scope="module")
+def experts():
+    from paper_2512_22804_b200 import experts
+
+    return experts
+
+
+def drawn(shape, seed, dtype="bf16", scale=1.0):
+    import torch
+
+    t = torch.from_numpy((np.random.default_rng(seed).standard_normal(shape) * scale).astype(np.float32)).cuda()
+    return t.to(torch.bfloat16) if dtype == "bf16" else t
+
+
+def layer(which, fmt, tokens, n_out, seed=0, n_in=96):
+    """(inputs that take a gradient, call) of a linear layer or an expert layer."""
+    import torch
+
+    from paper_2512_22804_b200 import experts, fp4
+
+    x = drawn((tokens, n_in), seed).requires_grad_()
+    if which == "linear":
+        w = drawn((n_out, n_in), seed + 1, scale=0.1).requires_grad_()
+        return (x, w), lambda: fp4.linear(x, w, fmt)
+    w = drawn((3, n_out, n_in), seed + 1, scale=0.1).requires_grad_()
+    weight = torch.rand(tokens, 2, generator=torch.Generator().manual_seed(seed)).cuda().requires_grad_()
+    ids = torch.from_numpy(np.random.default_rng(seed).integers(-1, 3, (tokens, 2)).astype(np.int32)).cuda()
+    return (x, w, weight), lambda: experts.linear(x, w, ids, weight, fmt)
+
+
+# ------------------------------------------------------------------------------------- 32-bit rows, and one rounding
+
+def between(got, want, room, dtype):
+    """got lies between the rounded ends of want -+ room."""
+    low, high = ((want + s * room).astype(np.float32) for s in (-1, 1))
+    if dtype == "bf16":
+        low, high = plain.bf16(low), plain.bf16(high)
+    got = got.detach().float().cpu().numpy()
+    return bool((low <= got).all() and (got <= high).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("tokens,top,n,k,m", [(1, 2, 8, 64, 40), (50, 3, 6, 300, 136), (400, 4, 4, 257, 264)])
+def test_expert_layer_rounds_once(fp4, experts, fmt, dtype, tokens, top, n, k, m):
+    """Against the formula on quantised values in 64 bits.  A product's row is a 32-bit sum (2^-16 of the sum of magnitudes), `top` of them
+    are added with weights in 32 bits (top * 2^-24 more), a dot product over m columns adds m * 2^-24; each result is rounded once."""
+    import torch
+
+    rng = np.random.default_rng(tokens)
+    ids = rng.integers(-1, n, (tokens, top)).astype(np.int32)
+    starts, row, slot = plain.sort(ids, n, 128)
+    rnd = plain.bf16 if dtype == "bf16" else (lambda z: z)
+    x, w, g = (rnd(rng.standard_normal(s).astype(np.float32)) for s in ((tokens, k), (n, m, k), (tokens, m)))
+    wt = rng.random((tokens, top)).astype(np.float32)
+    d = torch.bfloat16 if dtype == "bf16" else torch.float32
+    tx, tw, twt, tg = (torch.from_numpy(v).cuda() for v in (x, w, wt, g))
+    tx, tw, twt = tx.to(d).requires_grad_(), tw.to(d).requires_grad_(), twt.requires_grad_()
+    y = experts.linear(tx, tw, torch.from_numpy(ids).cuda(), twt, fmt)
+    dx, dw, dwt = torch.autograd.grad(y, (tx, tw, twt), tg.to(d))
+    assert y.dtype == dx.dtype == dw.dtype == d and dwt.dtype == torch.float32
+    fp4.check()
+
+    def v(z, amax=None):
+        return plain.values(*plain.quantize(z, fmt, amax), fmt)
+
+    at = slot >= 0
+    rows, grows = np.zeros((len(slot), k), np.float32), np.zeros((len(slot), m), np.float32)
+    rows[at] = x[slot[at] // top]
+    grows[at] = g[slot[at] // top] * wt.reshape(-1)[slot[at]][:, None]
+    amax = np.abs(w).max()
+    qw = v(w.reshape(n * m, k)).reshape(n, m, k)
+    qwt = np.stack([v(np.ascontiguousarray(w[e].T), amax) for e in range(n)])
+    qx, qg, qxt, qgt = v(rows), v(grows), v(np.ascontiguousarray(rows.T)), v(np.ascontiguousarray(grows.T))
+    ys, sy, dxs, sx = (np.zeros((len(slot), c)) for c in (m, m, k, k))
+    for e in range(n):
+        p = slice(starts[e], starts[e + 1])
+        ys[p], sy[p] = qx[p] @ qw[e].T, np.abs(qx[p]) @ np.abs(qw[e]).T
+        dxs[p], sx[p] = qg[p] @ qwt[e].T, np.abs(qg[p]) @ np.abs(qwt[e]).T
+        assert between(dw[e], qgt[:, p] @ qxt[:, p].T, 2.0 ** -16 * np.abs(qgt[:, p]) @ np.abs(qxt[:, p]).T, dtype)
+
+    def taken(z):
+        return np.where((row >= 0)[..., None], z[np.maximum(row, 0)], 0.0)
+
+    some = 2.0 ** -16 + top * 2.0 ** -24
+    assert between(y, (taken(ys) * wt[..., None]).sum(1), some * (taken(sy) * wt[..., None]).sum(1), dtype)
+    assert between(dwt, (taken(ys) * g[:, None, :]).sum(-1), (2.0 ** -16 + m * 2.0 ** -24) * (taken(sy) * np.abs(g)[:, None, :]).sum(-1), "fp32")
+    assert between(dx, taken(dxs).sum(1), some * taken(sx).sum(1), dtype)
