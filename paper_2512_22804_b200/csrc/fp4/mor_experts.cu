@@ -291,9 +291,13 @@ template <typename T, int BYTES, bool ANY> __global__ void __launch_bounds__(256
     }
 }
 
+// What is read of a row beside N elements of a token.  FP32 rows beside BF16 tokens come by 16 bytes, which is all that the tokens' access
+// promises of their start (8192 tokens, top 4, 4096 wide: sum 93 us, 99 by 32 bytes where the rows start on those; gradient 132 both ways).
+template <typename T, typename R, int N> using RowPiece = Piece<R, N * (int)sizeof(R), sizeof(T) == sizeof(R) ? N * (int)sizeof(R) : 16>;
+
 // A token's rows are in flight together and summed in slot order in FP32.  Bound by memory: the same sizes 56 us (336 MB, 6.0 TB/s); 4095
 // wide 82 us (one element at a time: 133 us).
-template <typename T, typename R, int BYTES, bool ANY, int LOAD> __global__ void __launch_bounds__(256) expert_combine_kernel(const __grid_constant__ MoveParams p)
+template <typename T, typename R, int BYTES, bool ANY> __global__ void __launch_bounds__(256) expert_combine_kernel(const __grid_constant__ MoveParams p)
 {
     using P = Piece<T, BYTES>;
     wait_for_predecessor();
@@ -302,7 +306,7 @@ template <typename T, typename R, int BYTES, bool ANY, int LOAD> __global__ void
     T* out = static_cast<T*>(p.out) + token * p.ld_out;
     auto piece = [&](auto like, int64_t c) {
         using P = decltype(like);
-        using Q = Piece<R, P::kElems * (int)sizeof(R), LOAD>;
+        using Q = RowPiece<T, R, P::kElems>;
         float sum[P::kElems];
 #pragma unroll
         for (float& s : sum) s = 0.f;
@@ -339,10 +343,10 @@ template <typename T, typename R, int BYTES, bool ANY, int LOAD> __global__ void
 // does not change from run to run.  Bound by memory: the same sizes 93 us (604 MB, 6.5 TB/s); 4095 wide, where dy is read once for the
 // sums and once for the rows, 170 us (one element at a time: 237 us).  Four CTAs an SM (64 registers): with the 118 that the compiler would take, two, and not enough
 // rows are in flight.
-template <typename T, typename R, int BYTES, bool ANY, int LOAD> __global__ void __launch_bounds__(256, 4) expert_grad_kernel(const __grid_constant__ MoveParams p)
+template <typename T, typename R, int BYTES, bool ANY> __global__ void __launch_bounds__(256, 4) expert_grad_kernel(const __grid_constant__ MoveParams p)
 {
     using P = Piece<T, BYTES>;
-    using Q = Piece<R, BYTES / (int)sizeof(T) * (int)sizeof(R), LOAD>;
+    using Q = RowPiece<T, R, P::kElems>;
     T* out = static_cast<T*>(p.out);
     wait_for_predecessor();
     if (blockIdx.x < p.clear_blocks) {
@@ -435,29 +439,24 @@ template <typename T, typename R, int BYTES, bool ANY, int LOAD> __global__ void
 
 enum Move : int { MOVE_GATHER, MOVE_COMBINE, MOVE_GRAD };
 
-// LOAD: bytes of a load from the rows that are read (R).
-template <typename T, typename R, int BYTES, bool ANY, int LOAD> cudaError_t move_launch(const MoveParams& p, Move what, uint32_t grid, cudaStream_t st)
+template <typename T, typename R, int BYTES, bool ANY> cudaError_t move_launch(const MoveParams& p, Move what, uint32_t grid, cudaStream_t st)
 {
     const int64_t pieces = ceil_div(p.hidden, BYTES / (int64_t)sizeof(T));
     const uint32_t threads = pieces >= 256 ? 256u : (uint32_t)(ceil_div(pieces, 32) * 32);
     if constexpr (sizeof(T) == sizeof(R))
         if (what == MOVE_GATHER) return launch(expert_gather_kernel<T, BYTES, ANY>, grid, threads, 0, st, true, p);
-    if (what == MOVE_COMBINE) return launch(expert_combine_kernel<T, R, BYTES, ANY, LOAD>, grid, threads, 0, st, true, p);
-    return launch(expert_grad_kernel<T, R, BYTES, ANY, LOAD>, grid, threads, 0, st, true, p);
+    if (what == MOVE_COMBINE) return launch(expert_combine_kernel<T, R, BYTES, ANY>, grid, threads, 0, st, true, p);
+    return launch(expert_grad_kernel<T, R, BYTES, ANY>, grid, threads, 0, st, true, p);
 }
-template <typename T, typename R> cudaError_t move_access(const MoveParams& p, Move what, uint32_t grid, int access, int row_access, cudaStream_t st)
+template <typename T, typename R> cudaError_t move_access(const MoveParams& p, Move what, uint32_t grid, int access, cudaStream_t st)
 {
     // vector pieces must not run past a row: the width has to be a multiple too.  Beside rows of FP32 a token's piece is 16 bytes, so that
-    // the registers of four rows' pieces stay the same; a row's piece is then 32 bytes, one load where the rows' own start and pitch are
-    // multiples of that, two where they are multiples of 16 alone.
+    // the registers of four rows' pieces stay the same.
     const int64_t width = p.hidden * (int64_t)sizeof(T);
-    if (access < 16 || width % 16 != 0) return move_launch<T, R, 16, true, 16>(p, what, grid, st);
-    if constexpr (sizeof(T) == sizeof(R)) {
-        if (access == 32 && width % 32 == 0) return move_launch<T, R, 32, false, 32>(p, what, grid, st);
-    } else {
-        if (row_access == 32) return move_launch<T, R, 16, false, 32>(p, what, grid, st);
-    }
-    return move_launch<T, R, 16, false, 16>(p, what, grid, st);
+    if constexpr (sizeof(T) == sizeof(R))
+        if (access == 32 && width % 32 == 0) return move_launch<T, R, 32, false>(p, what, grid, st);
+    if (access >= 16 && width % 16 == 0) return move_launch<T, R, 16, false>(p, what, grid, st);
+    return move_launch<T, R, 16, true>(p, what, grid, st);
 }
 
 // Checks what all movers share and fills the parameters.
@@ -494,15 +493,14 @@ mor_status_t check_rows(const void* m, int64_t rows, int64_t ld, const mor_exper
     return MOR_OK;
 }
 
-// `access`: bytes of an access that every matrix allows; `row_access`: that the rows which are read allow.
-mor_status_t move_run(const mor_expert_desc_t& d, const MoveParams& p, Move what, uint32_t grid, int access, int row_access, void* cuda_stream)
+mor_status_t move_run(const mor_expert_desc_t& d, const MoveParams& p, Move what, uint32_t grid, int access, void* cuda_stream)
 {
     if (grid == 0 || p.hidden == 0) return MOR_OK;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const bool mixed = what != MOVE_GATHER && d.dtype == MOR_DTYPE_BF16 && d.ys_dtype == MOR_DTYPE_F32;
-    const cudaError_t e = mixed                       ? move_access<__nv_bfloat16, float>(p, what, grid, access, row_access, st)
-                          : d.dtype == MOR_DTYPE_BF16 ? move_access<__nv_bfloat16, __nv_bfloat16>(p, what, grid, access, row_access, st)
-                                                      : move_access<float, float>(p, what, grid, access, row_access, st);
+    const cudaError_t e = mixed                       ? move_access<__nv_bfloat16, float>(p, what, grid, access, st)
+                          : d.dtype == MOR_DTYPE_BF16 ? move_access<__nv_bfloat16, __nv_bfloat16>(p, what, grid, access, st)
+                                                      : move_access<float, float>(p, what, grid, access, st);
     return e == cudaSuccess ? MOR_OK : MOR_ERR_CUDA;
 }
 
@@ -580,7 +578,7 @@ mor_status_t mor_expert_gather(const mor_expert_desc_t* host_desc, const void* x
     p.out = out;
     p.ld_out = ldo;
     p.clear_blocks = (uint32_t)ceil_div(p.rows, kClearRows);
-    return move_run(*host_desc, p, MOVE_GATHER, p.clear_blocks + (uint32_t)p.tokens, access, access, cuda_stream);
+    return move_run(*host_desc, p, MOVE_GATHER, p.clear_blocks + (uint32_t)p.tokens, access, cuda_stream);
 }
 
 mor_status_t mor_expert_combine(const mor_expert_desc_t* host_desc, const void* ys, int64_t ldy, void* out, int64_t ldo, void* cuda_stream)
@@ -588,15 +586,14 @@ mor_status_t mor_expert_combine(const mor_expert_desc_t* host_desc, const void* 
     MoveParams p;
     mor_status_t s = move_params(host_desc, p);
     if (s != MOR_OK) return s;
-    int row_access = 32;
-    if ((s = check_rows(ys, p.rows, ldy, *host_desc, host_desc->ys_dtype, row_access)) != MOR_OK) return s;
-    int access = row_access;
+    int access = 32;
+    if ((s = check_rows(ys, p.rows, ldy, *host_desc, host_desc->ys_dtype, access)) != MOR_OK) return s;
     if ((s = check_rows(out, p.tokens, ldo, *host_desc, host_desc->dtype, access)) != MOR_OK) return s;
     p.rows_in = ys;
     p.ld_row = ldy;
     p.out = out;
     p.ld_out = ldo;
-    return move_run(*host_desc, p, MOVE_COMBINE, (uint32_t)p.tokens, access, row_access, cuda_stream);
+    return move_run(*host_desc, p, MOVE_COMBINE, (uint32_t)p.tokens, access, cuda_stream);
 }
 
 mor_status_t mor_expert_combine_grad(const mor_expert_desc_t* host_desc, const void* dy, int64_t lddy, const void* ys, int64_t ldy,
@@ -608,10 +605,9 @@ mor_status_t mor_expert_combine_grad(const mor_expert_desc_t* host_desc, const v
     if (p.tokens > 0 && p.hidden > 0 && dys == nullptr && dweight == nullptr) return MOR_ERR_INVALID_ARG;     // empty tensors have no address
     if (dweight != nullptr && !is_dtype(host_desc->weight_dtype)) return MOR_ERR_INVALID_ARG;
     if (dweight != nullptr && !is_aligned(dweight, dtype_bytes(host_desc->weight_dtype))) return MOR_ERR_ALIGNMENT;
-    int access = 32, row_access = 32;
+    int access = 32;
     if ((s = check_rows(dy, p.tokens, lddy, *host_desc, host_desc->dtype, access)) != MOR_OK) return s;
-    if (dweight != nullptr && (s = check_rows(ys, p.rows, ldy, *host_desc, host_desc->ys_dtype, row_access)) != MOR_OK) return s;
-    access = row_access < access ? row_access : access;
+    if (dweight != nullptr && (s = check_rows(ys, p.rows, ldy, *host_desc, host_desc->ys_dtype, access)) != MOR_OK) return s;
     if (dys != nullptr && (s = check_rows(dys, p.rows, lddys, *host_desc, host_desc->dtype, access)) != MOR_OK) return s;
     p.tokens_in = dy;
     p.ld_token = lddy;
@@ -625,7 +621,7 @@ mor_status_t mor_expert_combine_grad(const mor_expert_desc_t* host_desc, const v
         const size_t n = (size_t)p.tokens * p.top * dtype_bytes(host_desc->weight_dtype);
         return cudaMemsetAsync(dweight, 0, n, static_cast<cudaStream_t>(cuda_stream)) == cudaSuccess ? MOR_OK : MOR_ERR_CUDA;
     }
-    return move_run(*host_desc, p, MOVE_GRAD, p.clear_blocks + (uint32_t)p.tokens, access, row_access, cuda_stream);
+    return move_run(*host_desc, p, MOVE_GRAD, p.clear_blocks + (uint32_t)p.tokens, access, cuda_stream);
 }
 
 }  // extern "C"
