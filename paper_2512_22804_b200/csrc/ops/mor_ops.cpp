@@ -323,14 +323,20 @@ std::pair<std::optional<Tensor>, Tensor> combine_grad(const Tensor& dy, const Te
 
 // ---- layers
 
-Tensor last_contiguous(const Tensor& t) { return t.size(-1) <= 1 || t.stride(-1) == 1 ? t : t.contiguous(); }
+// A layer takes tensors of any strides, as torch's own do; the operators need the elements of a row side by side and rows that do not overlap (the
+// gradient of a sum over tokens is one row with a stride of zero), and others are copied first.
+Tensor apart(const Tensor& t)
+{
+    const bool ok = (t.size(-1) <= 1 || t.stride(-1) == 1) && (t.size(-2) <= 1 || t.stride(-2) >= t.size(-1));
+    return ok ? t : t.contiguous();
+}
 
 // What a backward pass keeps of an operand is its buffer; the shape is known.
 struct LinearFn : torch::autograd::Function<LinearFn> {
     static Tensor forward(AutogradContext* ctx, const Tensor& x, const Tensor& w, int64_t format, bool need_x, bool need_w)
     {
-        const Pair a = quantize_(x, (int)format, true, need_w, std::nullopt, nullptr, std::nullopt);
-        const Pair b = quantize_(w, (int)format, true, need_x, std::nullopt, nullptr, std::nullopt);
+        const Pair a = quantize_(apart(x), (int)format, true, need_w, std::nullopt, nullptr, std::nullopt);
+        const Pair b = quantize_(apart(w), (int)format, true, need_x, std::nullopt, nullptr, std::nullopt);
         if (need_w) ctx->saved_data["a"] = a.cols->buf;
         if (need_x) ctx->saved_data["b"] = b.cols->buf;
         ctx->saved_data["shape"] = std::vector<int64_t>{x.size(0), w.size(0), x.size(1), format, (int64_t)x.scalar_type(), (int64_t)w.scalar_type()};
@@ -344,7 +350,7 @@ struct LinearFn : torch::autograd::Function<LinearFn> {
         const bool need_x = ctx->needs_input_grad(0), need_w = ctx->needs_input_grad(1);
         Tensor dx, dw;
         if (need_x || need_w) {
-            const Pair g = quantize_(last_contiguous(grads[0]), format, need_x, need_w, std::nullopt, nullptr, std::nullopt);
+            const Pair g = quantize_(apart(grads[0]), format, need_x, need_w, std::nullopt, nullptr, std::nullopt);
             if (need_x) dx = matmul_(*g.rows, Matrix::over(ctx->saved_data["b"].toTensor(), 1, k, n, format), (at::ScalarType)s[4], MOR_GROUP_NONE, nullptr);
             if (need_w) dw = matmul_(*g.cols, Matrix::over(ctx->saved_data["a"].toTensor(), 1, k, m, format), (at::ScalarType)s[5], MOR_GROUP_NONE, nullptr);
         }
@@ -370,7 +376,7 @@ Tensor linear(const Tensor& x, const Tensor& w, int f)
 // gradient (a dot product with them) would be up to half again as far off.
 Tensor expert_forward(const Tensor& x, const Matrix& w, const Routes& plan, const Tensor& weight, bool cols, Tensor* ys, Tensor* a_t)
 {
-    const Pair a = quantize_(x, w.c.format, true, cols, std::nullopt, &plan, std::nullopt);
+    const Pair a = quantize_(apart(x), w.c.format, true, cols, std::nullopt, &plan, std::nullopt);
     *ys = matmul_rows_(*a.rows, w, plan, at::kFloat);
     if (cols) *a_t = a.cols->buf;
     return combine(*ys, plan, weight, x.scalar_type());
@@ -381,7 +387,7 @@ struct ExpertFn : torch::autograd::Function<ExpertFn> {
                           bool need_w, bool need_weight)
     {
         const Routes plan = sort_slots(ids, w.size(0), 128);
-        const Pair b = quantize_(w, (int)format, true, need_x, std::nullopt, nullptr, std::nullopt);
+        const Pair b = quantize_(apart(w), (int)format, true, need_x, std::nullopt, nullptr, std::nullopt);
         Tensor ys, a_t;
         const Tensor y = expert_forward(x, *b.rows, plan, weight, need_w, &ys, &a_t);
         if (need_w) ctx->saved_data["a"] = a_t;
@@ -400,7 +406,7 @@ struct ExpertFn : torch::autograd::Function<ExpertFn> {
         const int64_t e = s[0], n = s[1], k = s[2];
         const int format = (int)s[3];
         const bool need_x = ctx->needs_input_grad(0), need_w = ctx->needs_input_grad(1), need_weight = ctx->needs_input_grad(3);
-        const Tensor weight = ctx->get_saved_variables()[0], dy = last_contiguous(grads[0]);
+        const Tensor weight = ctx->get_saved_variables()[0], dy = apart(grads[0]);
         const Tensor row = ctx->saved_data["row"].toTensor();
         const Routes plan = {ctx->saved_data["starts"].toTensor(), row, ctx->saved_data["slot"].toTensor(), row.size(1), 128};
         Tensor dx, dw, dweight;

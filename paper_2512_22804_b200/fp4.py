@@ -25,7 +25,8 @@ check their arguments, allocate their outputs and run on the current stream of t
     [experts, a.rows, b.rows]: the product summed over each expert's part of the reduction axis.
 ``linear(x, w, format)``
     x [..., n_in] times w [n_out, n_in] transposed; every operand of the product and of its two gradients is quantised along that
-    product's reduction axis, and the rounding is passed straight through in the backward pass.
+    product's reduction axis, and the rounding is passed straight through in the backward pass.  x, w and the gradient may have any strides
+    (rows that overlap or are not contiguous are copied first; the other calls refuse them).
 
 There is no CPU path: importing this module raises if the operators have not been built.
 """

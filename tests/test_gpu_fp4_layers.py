@@ -51,6 +51,67 @@ def layer(which, fmt, tokens, n_out, seed=0, n_in=96):
     return (x, w, weight), lambda: experts.linear(x, w, ids, weight, fmt)
 
 
+# ------------------------------------------------------------------------------------- gradients with any strides
+
+@pytest.mark.parametrize("which", ["linear", "experts"])
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("tokens,n_out", [(1, 40), (50, 40), (300, 137), (50, 1), (1, 1)])
+def test_broadcast_gradients(fp4, which, fmt, tokens, n_out):
+    """Sums over the tokens (and over everything) hand back gradients with row strides of zero: the same as dense ones."""
+    import torch
+
+    inputs, call = layer(which, fmt, tokens, n_out)
+    v = drawn((n_out,), 7)
+    got = torch.autograd.grad((call().sum(0) * v).sum(), inputs)
+    want = torch.autograd.grad(call(), inputs, v.expand(tokens, n_out).contiguous())
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    got = torch.autograd.grad(call().sum(), inputs)
+    want = torch.autograd.grad(call(), inputs, torch.ones(tokens, n_out, device="cuda", dtype=torch.bfloat16))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    got = torch.autograd.grad(call(), inputs, drawn((n_out, tokens), 8).t())
+    want = torch.autograd.grad(call(), inputs, drawn((n_out, tokens), 8).t().contiguous())
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    if n_out == 1:
+        got = torch.autograd.grad(call().squeeze(-1).sum(), inputs)
+        want = torch.autograd.grad(call(), inputs, torch.ones(tokens, 1, device="cuda", dtype=torch.bfloat16))
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_broadcast_gradients_of_three_dimensions(fp4, fmt):
+    import torch
+
+    x, w, v = drawn((4, 30, 96), 1).requires_grad_(), drawn((40, 96), 2).requires_grad_(), drawn((40,), 3)
+    got = torch.autograd.grad((fp4.linear(x, w, fmt).sum((0, 1)) * v).sum(), (x, w))
+    want = torch.autograd.grad(fp4.linear(x, w, fmt), (x, w), v.expand(4, 30, 40).contiguous())
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("which", ["linear", "experts"])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_inputs_with_any_strides(fp4, which, fmt):
+    import torch
+
+    inputs, _ = layer(which, fmt, 50, 40)
+    x, w = (t.detach() for t in inputs[:2])
+    ids, weight = torch.arange(100, device="cuda", dtype=torch.int32).view(50, 2) % 3, torch.rand(50, 2, device="cuda")
+
+    def call(x, w):
+        from paper_2512_22804_b200 import experts
+
+        return fp4.linear(x, w, fmt) if which == "linear" else experts.linear(x, w, ids, weight, fmt)
+
+    row, column = x[:1].expand(50, -1), x.t().contiguous().t()
+    for v in (row, column, x[:, :1].expand(-1, 96)):
+        for u in (w, w.transpose(-1, -2).contiguous().transpose(-1, -2), w[..., :1, :].expand_as(w)):
+            tv, tu = (t.detach().requires_grad_() for t in (v, u))
+            dv, du = (t.contiguous().requires_grad_() for t in (v, u))
+            y, want = call(tv, tu), call(dv, du)
+            assert torch.equal(y, want)
+            for a, b in zip(torch.autograd.grad(y.sum(), (tv, tu)), torch.autograd.grad(want.sum(), (dv, du))):
+                assert torch.equal(a, b)
+
+
 # ------------------------------------------------------------------------------------- 32-bit rows, and one rounding
 
 def between(got, want, room, dtype):
