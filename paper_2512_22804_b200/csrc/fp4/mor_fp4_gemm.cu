@@ -162,13 +162,33 @@ template <int CG, int GROUP> __device__ __forceinline__ bool tile_at(const GemmP
     return true;
 }
 
-template <typename T> __device__ __forceinline__ uint32_t out_word(const uint32_t* acc, float scale, int j)
+// Both tensor scales, as two factors of a sum.  Where their product is a normal number it is the one factor.  Operands of small values would
+// lose its digits (each scale may be 2^-99) though the results are normal numbers, and those of large ones would make sums of zero NaN; there
+// the scales are applied one after the other, the smaller first: E4M3_16 sums are multiples of 2^-20 below 2^55, so that this step neither overflows
+// before the result does nor reaches the subnormal numbers.
+struct OutScale {
+    float first, then;
+    __device__ __forceinline__ OutScale() : first(0.f), then(1.f) {}
+    __device__ __forceinline__ OutScale(float a, float b) : first(a * b), then(1.f)
+    {
+        const float size = fabsf(first);
+        if (size < 0x1p-126f || size == INFINITY) {
+            const bool order = fabsf(a) <= fabsf(b);
+            first = order ? a : b;
+            then = order ? b : a;
+        }
+    }
+    __device__ __forceinline__ float of(float sum) const { return sum * first * then; }
+    __device__ __forceinline__ float of(uint32_t sum) const { return of(__uint_as_float(sum)); }
+};
+
+template <typename T> __device__ __forceinline__ uint32_t out_word(const uint32_t* acc, const OutScale& scale, int j)
 {
-    if constexpr (sizeof(T) == 2) return bf16x2_of(__uint_as_float(acc[2 * j]) * scale, __uint_as_float(acc[2 * j + 1]) * scale);
-    else return __float_as_uint(__uint_as_float(acc[j]) * scale);
+    if constexpr (sizeof(T) == 2) return bf16x2_of(scale.of(acc[2 * j]), scale.of(acc[2 * j + 1]));
+    else return __float_as_uint(scale.of(acc[j]));
 }
 // 32 neighbouring values of one output row, or the first n of them.
-template <typename T> __device__ __forceinline__ void store_row32(T* to, const uint32_t* acc, float scale, int n)
+template <typename T> __device__ __forceinline__ void store_row32(T* to, const uint32_t* acc, const OutScale& scale, int n)
 {
     constexpr int kWords = 32 * sizeof(T) / 4;
     uint32_t w[kWords];
@@ -191,7 +211,7 @@ template <typename T> __device__ __forceinline__ void store_row32(T* to, const u
 }
 // COLS values of a row that starts 16 bytes past a sector of 32: half a sector at both ends, whole ones between, where 16-byte stores alone
 // would write every sector in two parts (8192 x 14328 x 4096 BF16: 196 us, 223 by 16 bytes; 3000 x 7004 x 1000 FP32: 27 us, 40).
-template <typename T, int COLS> __device__ __forceinline__ void store_row_off16(T* to, const uint32_t* acc, float scale)
+template <typename T, int COLS> __device__ __forceinline__ void store_row_off16(T* to, const uint32_t* acc, const OutScale& scale)
 {
     constexpr int kWords = COLS * sizeof(T) / 4;
     uint32_t* const out = reinterpret_cast<uint32_t*>(to);
@@ -333,7 +353,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) fp4_wide_kernel(const __grid_
         }
     } else if (warp >= 4) {                                         // ---- accumulators out
         const int half = (warp - 4) >> 2;
-        const float scale = p.k > 0 ? *p.ta * *p.tb : 0.f;
+        const OutScale scale = p.k > 0 ? OutScale(*p.ta, *p.tb) : OutScale();
         const uint32_t lanes = (uint32_t)(warp & 3) << 21;
         constexpr int kCols = NT / 2;
         uint32_t acc[kCols], done = 0;
@@ -363,7 +383,7 @@ __global__ void __launch_bounds__(kWideThreads, 1) fp4_wide_kernel(const __grid_
             }
             if (wanted) {
                 T* out = static_cast<T*>(p.out) + ((GROUP == MOR_GROUP_REDUCE ? (int64_t)at.group * p.m : 0) + row) * p.ldo + col;
-                const float f = at.len > 0 ? scale : 0.f;
+                const OutScale f = at.len > 0 ? scale : OutScale();
                 if ((reinterpret_cast<uintptr_t>(out) & 31) != 0 && col + kCols <= p.n) {
                     store_row_off16<T, kCols>(out, acc, f);
                 } else {
@@ -516,7 +536,7 @@ template <int NT, int FMT, typename T> __global__ void __launch_bounds__(kNarrow
     tc_fence_before();
     cluster_sync();
     if (warp >= 2 && ok) {
-        const float scale = p.k > 0 ? *p.ta * *p.tb : 0.f;
+        const OutScale scale = p.k > 0 ? OutScale(*p.ta, *p.tb) : OutScale();
         const int64_t f = (int64_t)feature0 + feature;
         if (f < p.n)
             for (int j = (int)rank; j < NT && token0 + j < p.m; j += (int)split) {
@@ -524,8 +544,8 @@ template <int NT, int FMT, typename T> __global__ void __launch_bounds__(kNarrow
                 float s = 0.f;
                 for (uint32_t r = 0; r < split; ++r) s += lds_cluster(map_rank(from, r));
                 T* to = static_cast<T*>(p.out) + (int64_t)(token0 + j) * p.ldo + f;
-                if constexpr (sizeof(T) == 2) *to = __float2bfloat16(s * scale);
-                else *to = s * scale;
+                if constexpr (sizeof(T) == 2) *to = __float2bfloat16(scale.of(s));
+                else *to = scale.of(s);
             }
     }
     __syncwarp();

@@ -112,6 +112,33 @@ def test_inputs_with_any_strides(fp4, which, fmt):
                 assert torch.equal(a, b)
 
 
+# ------------------------------------------------------------------------------------- operands far from one
+
+@pytest.mark.parametrize("m", [5, 300])
+@pytest.mark.parametrize("ea,eb", [(-60, -60), (-70, -30), (-51, -52), (-85, 60), (100, -80), (60, 40)])
+def test_products_of_operands_far_from_one(fp4, m, ea, eb):
+    """|x| about 2^ea and 2^eb: the product of the tensor scales alone need not be a normal number, the results are."""
+    import torch
+
+    xa, xb = (plain.bf16((np.random.default_rng(s).standard_normal((r, 300)) * 2.0 ** e).astype(np.float32)) for s, r, e in ((1, m, ea), (2, 140, eb)))
+    a, b = (fp4.quantize(torch.from_numpy(v).cuda().to(torch.bfloat16), "e4m3_16")[0] for v in (xa, xb))
+    va, vb = (plain.values(*plain.quantize(v, "e4m3_16"), "e4m3_16") for v in (xa, xb))
+    y = fp4.matmul(a, b, torch.float32).cpu().numpy().astype(np.float64)
+    assert (np.abs(y - va @ vb.T) <= np.abs(va) @ np.abs(vb).T * 2.0 ** -16 + 2.0 ** -149).all()
+
+
+def test_zero_rows_beside_large_operands(fp4):
+    """Both tensor scales together pass the largest number; rows of zeros still give zero."""
+    import torch
+
+    x = torch.zeros(200, 64, device="cuda", dtype=torch.bfloat16)
+    x[0] = 2.0 ** 90
+    a = fp4.quantize(x, "e4m3_16")[0]
+    for part in (x[:4], x):
+        y = fp4.matmul(fp4.quantize(part, "e4m3_16")[0], a, torch.float32)
+        assert torch.isinf(y[0, 0]) and not y[1:].any() and not y[0, 1:].any()
+
+
 # ------------------------------------------------------------------------------------- 32-bit rows, and one rounding
 
 def between(got, want, room, dtype):
