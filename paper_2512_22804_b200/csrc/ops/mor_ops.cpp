@@ -331,14 +331,14 @@ Tensor apart(const Tensor& t)
     return ok ? t : t.contiguous();
 }
 
-// What a backward pass keeps of an operand is its buffer; the shape is known.
+// What a backward pass keeps of an operand is its buffer; the shape is known.  Every tensor that is kept goes through save_for_backward, so that hooks
+// on saved tensors (checkpoints, offloading) see it and a backward pass gives it back.
 struct LinearFn : torch::autograd::Function<LinearFn> {
     static Tensor forward(AutogradContext* ctx, const Tensor& x, const Tensor& w, int64_t format, bool need_x, bool need_w)
     {
         const Pair a = quantize_(apart(x), (int)format, true, need_w, std::nullopt, nullptr, std::nullopt);
         const Pair b = quantize_(apart(w), (int)format, true, need_x, std::nullopt, nullptr, std::nullopt);
-        if (need_w) ctx->saved_data["a"] = a.cols->buf;
-        if (need_x) ctx->saved_data["b"] = b.cols->buf;
+        ctx->save_for_backward({need_w ? a.cols->buf : Tensor(), need_x ? b.cols->buf : Tensor()});
         ctx->saved_data["shape"] = std::vector<int64_t>{x.size(0), w.size(0), x.size(1), format, (int64_t)x.scalar_type(), (int64_t)w.scalar_type()};
         return matmul_(*a.rows, *b.rows, x.scalar_type(), MOR_GROUP_NONE, nullptr);
     }
@@ -348,11 +348,12 @@ struct LinearFn : torch::autograd::Function<LinearFn> {
         const int64_t m = s[0], n = s[1], k = s[2];
         const int format = (int)s[3];
         const bool need_x = ctx->needs_input_grad(0), need_w = ctx->needs_input_grad(1);
+        const variable_list kept = ctx->get_saved_variables();
         Tensor dx, dw;
         if (need_x || need_w) {
             const Pair g = quantize_(apart(grads[0]), format, need_x, need_w, std::nullopt, nullptr, std::nullopt);
-            if (need_x) dx = matmul_(*g.rows, Matrix::over(ctx->saved_data["b"].toTensor(), 1, k, n, format), (at::ScalarType)s[4], MOR_GROUP_NONE, nullptr);
-            if (need_w) dw = matmul_(*g.cols, Matrix::over(ctx->saved_data["a"].toTensor(), 1, k, m, format), (at::ScalarType)s[5], MOR_GROUP_NONE, nullptr);
+            if (need_x) dx = matmul_(*g.rows, Matrix::over(kept[1], 1, k, n, format), (at::ScalarType)s[4], MOR_GROUP_NONE, nullptr);
+            if (need_w) dw = matmul_(*g.cols, Matrix::over(kept[0], 1, k, m, format), (at::ScalarType)s[5], MOR_GROUP_NONE, nullptr);
         }
         return {dx, dw, Tensor(), Tensor(), Tensor()};
     }
@@ -390,13 +391,7 @@ struct ExpertFn : torch::autograd::Function<ExpertFn> {
         const Pair b = quantize_(apart(w), (int)format, true, need_x, std::nullopt, nullptr, std::nullopt);
         Tensor ys, a_t;
         const Tensor y = expert_forward(x, *b.rows, plan, weight, need_w, &ys, &a_t);
-        if (need_w) ctx->saved_data["a"] = a_t;
-        if (need_x) ctx->saved_data["b"] = b.cols->buf;
-        if (need_weight) ctx->saved_data["ys"] = ys;
-        ctx->saved_data["starts"] = plan.starts;
-        ctx->saved_data["row"] = plan.row;
-        ctx->saved_data["slot"] = plan.slot;
-        ctx->save_for_backward({weight});
+        ctx->save_for_backward({weight, a_t, need_x ? b.cols->buf : Tensor(), need_weight ? ys : Tensor(), plan.starts, plan.row, plan.slot});
         ctx->saved_data["shape"] = std::vector<int64_t>{w.size(0), w.size(1), w.size(2), format, (int64_t)x.scalar_type(), (int64_t)w.scalar_type()};
         return y;
     }
@@ -406,15 +401,15 @@ struct ExpertFn : torch::autograd::Function<ExpertFn> {
         const int64_t e = s[0], n = s[1], k = s[2];
         const int format = (int)s[3];
         const bool need_x = ctx->needs_input_grad(0), need_w = ctx->needs_input_grad(1), need_weight = ctx->needs_input_grad(3);
-        const Tensor weight = ctx->get_saved_variables()[0], dy = apart(grads[0]);
-        const Tensor row = ctx->saved_data["row"].toTensor();
-        const Routes plan = {ctx->saved_data["starts"].toTensor(), row, ctx->saved_data["slot"].toTensor(), row.size(1), 128};
+        const variable_list kept = ctx->get_saved_variables();
+        const Tensor &weight = kept[0], &a_t = kept[1], &b_t = kept[2], &ys = kept[3], dy = apart(grads[0]);
+        const Routes plan = {kept[4], kept[5], kept[6], kept[5].size(1), 128};
         Tensor dx, dw, dweight;
-        if (need_weight) dweight = combine_grad(dy, ctx->saved_data["ys"].toTensor(), plan, weight, false).second;
+        if (need_weight) dweight = combine_grad(dy, ys, plan, weight, false).second;
         if (need_x || need_w) {
             const Pair g = quantize_(dy, format, need_x, need_w, std::nullopt, &plan, weight);
-            if (need_x) dx = combine(matmul_rows_(*g.rows, Matrix::over(ctx->saved_data["b"].toTensor(), e, k, n, format), plan, at::kFloat), plan, std::nullopt, (at::ScalarType)s[4]);
-            if (need_w) dw = matmul_reduce_(*g.cols, Matrix::over(ctx->saved_data["a"].toTensor(), 1, k, plan.rows(), format), plan, (at::ScalarType)s[5]);
+            if (need_x) dx = combine(matmul_rows_(*g.rows, Matrix::over(b_t, e, k, n, format), plan, at::kFloat), plan, std::nullopt, (at::ScalarType)s[4]);
+            if (need_w) dw = matmul_reduce_(*g.cols, Matrix::over(a_t, 1, k, plan.rows(), format), plan, (at::ScalarType)s[5]);
         }
         return {dx, dw, Tensor(), dweight, Tensor(), Tensor(), Tensor(), Tensor()};
     }

@@ -112,6 +112,39 @@ def test_inputs_with_any_strides(fp4, which, fmt):
                 assert torch.equal(a, b)
 
 
+# ------------------------------------------------------------------------------------- what is kept for the backward pass
+
+@pytest.mark.parametrize("which", ["linear", "experts"])
+def test_hooks_on_saved_tensors_see_what_is_kept(fp4, which):
+    """All that a backward pass needs goes through the hooks: a layer whose saved tensors are taken to the host keeps nothing on the GPU."""
+    import torch
+
+    tokens, n_out, n_in = 2048, 1024, 1024
+    inputs, call = layer(which, "e8m0_32", tokens, n_out, n_in=n_in)
+    dy = drawn((tokens, n_out), 9)
+    want = torch.autograd.grad(call(), inputs, dy)
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    with torch.autograd.graph.save_on_cpu():
+        y = call()
+    assert torch.cuda.memory_allocated() - before <= y.numel() * 2 + 65536
+    got = torch.autograd.grad(y, inputs, dy)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("which", ["linear", "experts"])
+def test_a_second_backward_pass_needs_retain_graph(fp4, which):
+    import torch
+
+    inputs, call = layer(which, "e8m0_32", 50, 40)
+    y, dy = call(), drawn((50, 40), 9)
+    first = torch.autograd.grad(y, inputs, dy, retain_graph=True)
+    second = torch.autograd.grad(y, inputs, dy)
+    assert all(torch.equal(a, b) for a, b in zip(first, second))
+    with pytest.raises(RuntimeError, match="second time"):
+        torch.autograd.grad(y, inputs, dy)
+
+
 # ------------------------------------------------------------------------------------- operands far from one
 
 @pytest.mark.parametrize("m", [5, 300])
