@@ -235,12 +235,15 @@ Tensor matmul_(const Matrix& a, const Matrix& b, at::ScalarType type, int groupi
         d.groups = plan->experts();
         if (grouping == MOR_GROUP_ROWS) d.slot_of_row = ptr<int32_t>(plan->slot);
     }
-    const Tensor out = grouping == MOR_GROUP_REDUCE ? empty({d.groups, a.c.rows, d.ldo}, type, a.buf) : empty({a.c.rows, d.ldo}, type, a.buf);
+    // not a view of a wider tensor: autograd forbids changes in place of views that a layer returns
+    const int64_t m = a.c.rows, size[3] = {d.groups, m, n}, pitch[3] = {m * d.ldo, d.ldo, 1};
+    const int skip = grouping == MOR_GROUP_REDUCE ? 0 : 1;
+    const Tensor out = at::detail::empty_strided_cuda(at::IntArrayRef(size + skip, 3 - skip), at::IntArrayRef(pitch + skip, 3 - skip), type, a.buf.device());
     d.out = out.data_ptr();
     const Tensor status = status_word(a.buf);
     d.status = status.defined() ? reinterpret_cast<uint32_t*>(ptr<int32_t>(status)) : nullptr;
     check(mor_fp4_matmul(&d, stream()), "mor_fp4_matmul");
-    return d.ldo == n ? out : out.narrow(-1, 0, n);
+    return out;
 }
 Tensor matmul_rows_(const Matrix& a, const Matrix& b, const Routes& plan, at::ScalarType type)
 {

@@ -18,7 +18,7 @@ check their arguments, allocate their outputs and run on the current stream of t
 ``dequantize(op, dtype=torch.bfloat16)``
     the values: [rows, cols], or [batch, rows, cols] for a stack of more than one.
 ``matmul(a, b, out_dtype=torch.bfloat16)``
-    a b^T.  Rows of a result start on 16 bytes, so an odd width comes as a view of a wider buffer.
+    a b^T.  Rows of a result start on multiples of 16 bytes, so one of another width has a row stride above its width.
 ``matmul_rows(a, b, plan, out_dtype=...)``
     the rows of each expert of the plan times that expert's matrix of the stack b; empty rows of the plan are not written.
 ``matmul_reduce(a, b, plan, out_dtype=...)``

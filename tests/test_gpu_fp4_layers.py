@@ -112,6 +112,29 @@ def test_inputs_with_any_strides(fp4, which, fmt):
                 assert torch.equal(a, b)
 
 
+# ------------------------------------------------------------------------------------- results that are changed in place
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("tokens", [5, 200])
+@pytest.mark.parametrize("n_out", [136, 137])
+def test_results_change_in_place(fp4, fmt, tokens, n_out):
+    import torch
+
+    (x, w), call = layer("linear", fmt, tokens, n_out)
+    bias, dy = drawn((n_out,), 5).requires_grad_(), drawn((tokens, n_out), 6)
+    y = call()
+    y.add_(bias)
+    torch.relu_(y)
+    want = torch.relu(call() + bias)
+    assert torch.equal(y, want)
+    for a, b in zip(torch.autograd.grad(y, (x, w, bias), dy), torch.autograd.grad(want, (x, w, bias), dy)):
+        assert torch.equal(a, b)
+    x3 = x.detach().reshape(1, tokens, -1)
+    y3 = fp4.linear(x3.requires_grad_(), w, fmt)
+    y3 += bias
+    assert torch.equal(torch.relu(y3[0]), want)
+
+
 # ------------------------------------------------------------------------------------- what is kept for the backward pass
 
 @pytest.mark.parametrize("which", ["linear", "experts"])
