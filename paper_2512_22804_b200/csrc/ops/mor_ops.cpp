@@ -7,6 +7,7 @@
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAGraphsC10Utils.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/extension.h>
 
 #include <memory>
@@ -334,6 +335,29 @@ Tensor apart(const Tensor& t)
     return ok ? t : t.contiguous();
 }
 
+// Marks a result that has no derivative (and that nothing else shares): whoever differentiates it meets `message` instead of a missing term.
+// `edges` lead to what it depends on, so that a pass towards any of that comes by.
+void no_derivative(Tensor& out, torch::autograd::edge_list edges, const std::string& message)
+{
+    if (!out.defined()) return;
+    const std::shared_ptr<torch::autograd::Node> node(new torch::autograd::Error(message, std::move(edges)), torch::autograd::deleteNode);
+    torch::autograd::create_gradient_edge(out, node);
+}
+void add_edge(torch::autograd::edge_list& edges, const Tensor& t)
+{
+    if (t.defined() && t.requires_grad()) edges.push_back(torch::autograd::impl::gradient_edge(t));
+}
+// The same for results of a backward pass that keeps a graph (create_graph): they depend on the layer's inputs and on the gradient.
+void once_differentiable(std::initializer_list<Tensor*> results, const Tensor& grad, const char* layer)
+{
+    if (!at::GradMode::is_enabled()) return;
+    torch::autograd::edge_list edges;
+    for (const torch::autograd::Edge& e : torch::autograd::get_current_node()->next_edges())
+        if (e.is_valid()) edges.push_back(e);
+    add_edge(edges, grad);
+    for (Tensor* t : results) no_derivative(*t, edges, std::string(layer) + " cannot be differentiated twice");
+}
+
 // What a backward pass keeps of an operand is its buffer; the shape is known.  Every tensor that is kept goes through save_for_backward, so that hooks
 // on saved tensors (checkpoints, offloading) see it and a backward pass gives it back.
 struct LinearFn : torch::autograd::Function<LinearFn> {
@@ -358,6 +382,7 @@ struct LinearFn : torch::autograd::Function<LinearFn> {
             if (need_x) dx = matmul_(*g.rows, Matrix::over(kept[1], 1, k, n, format), (at::ScalarType)s[4], MOR_GROUP_NONE, nullptr);
             if (need_w) dw = matmul_(*g.cols, Matrix::over(kept[0], 1, k, m, format), (at::ScalarType)s[5], MOR_GROUP_NONE, nullptr);
         }
+        once_differentiable({&dx, &dw}, grads[0], "fp4.linear");
         return {dx, dw, Tensor(), Tensor(), Tensor()};
     }
 };
@@ -414,6 +439,7 @@ struct ExpertFn : torch::autograd::Function<ExpertFn> {
             if (need_x) dx = combine(matmul_rows_(*g.rows, Matrix::over(b_t, e, k, n, format), plan, at::kFloat), plan, std::nullopt, (at::ScalarType)s[4]);
             if (need_w) dw = matmul_reduce_(*g.cols, Matrix::over(a_t, 1, k, plan.rows(), format), plan, (at::ScalarType)s[5]);
         }
+        once_differentiable({&dx, &dw, &dweight}, grads[0], "experts.linear");
         return {dx, dw, Tensor(), dweight, Tensor(), Tensor(), Tensor(), Tensor()};
     }
 };

@@ -20,6 +20,8 @@
     (differentiable in x, w and weight; the rounding is passed straight through) or, for serving, a stored stack (``fp4.Operand`` with one
     matrix per expert; format is then its own).
 
+Gradients: linear has its own, of x, w and weight, once (its backward pass cannot be differentiated again).
+
 The formulas are those of ``include/mor.h``.
 """
 from __future__ import annotations

@@ -168,6 +168,23 @@ def test_a_second_backward_pass_needs_retain_graph(fp4, which):
         torch.autograd.grad(y, inputs, dy)
 
 
+# ------------------------------------------------------------------------------------- what has no derivative
+
+@pytest.mark.parametrize("which", ["linear", "experts"])
+def test_a_second_derivative_is_refused(fp4, which):
+    import torch
+
+    inputs, call = layer(which, "e8m0_32", 50, 40)
+    dy = drawn((50, 40), 9)
+    plain_grads = torch.autograd.grad(call(), inputs, dy)
+    grads = torch.autograd.grad(call(), inputs, dy, create_graph=True)
+    assert all(torch.equal(a, b) for a, b in zip(grads, plain_grads))
+    for g in grads:
+        loss = (g.float() ** 2).sum() + sum((t.float() ** 2).sum() for t in inputs)      # another path keeps the graph alive
+        with pytest.raises(RuntimeError, match="twice"):
+            torch.autograd.grad(loss, inputs, retain_graph=True)
+
+
 # ------------------------------------------------------------------------------------- operands far from one
 
 @pytest.mark.parametrize("m", [5, 300])
