@@ -562,6 +562,17 @@ private:
     PyObject* v_[8] = {};
 };
 
+// A result of a call that has no gradient of its own.
+PyObject* give(Tensor out, std::initializer_list<Tensor> inputs, const char* call)
+{
+    if (at::GradMode::is_enabled()) {
+        torch::autograd::edge_list edges;
+        for (const Tensor& t : inputs) add_edge(edges, t);
+        if (!edges.empty()) no_derivative(out, std::move(edges), std::string(call) + " has no gradient: see its module's documentation");
+    }
+    return give(out);
+}
+
 // Runs a call and turns what it throws into the interpreter's exceptions.
 template <typename F> PyObject* guarded(F&& f)
 {
@@ -646,7 +657,8 @@ MOR_CALL(py_gather)
 {
     return guarded([&] {
         MOR_ARGS("gather", 2, 3, "x", "plan", "weight");
-        return give(gather(a.tensor(0), a.plan(1), a.maybe_tensor(2)));
+        const std::optional<Tensor> weight = a.maybe_tensor(2);
+        return give(gather(a.tensor(0), a.plan(1), weight), {a.tensor(0), weight.value_or(Tensor())}, "experts.gather");
     });
 }
 MOR_CALL(py_combine)
@@ -654,16 +666,18 @@ MOR_CALL(py_combine)
     return guarded([&] {
         MOR_ARGS("combine", 2, 4, "ys", "plan", "weight", "out_dtype");
         const Tensor& ys = a.tensor(0);
-        return give(combine(ys, a.plan(1), a.maybe_tensor(2), a.dtype(3, ys.scalar_type())));
+        const std::optional<Tensor> weight = a.maybe_tensor(2);
+        return give(combine(ys, a.plan(1), weight, a.dtype(3, ys.scalar_type())), {ys, weight.value_or(Tensor())}, "experts.combine");
     });
 }
 MOR_CALL(py_combine_grad)
 {
     return guarded([&] {
         MOR_ARGS("combine_grad", 4, 4, "dy", "ys", "plan", "weight", "rows");
-        const auto r = combine_grad(a.tensor(0), a.tensor(1), a.plan(2), a.tensor(3), a.flag(4, true));
-        PyObject* rows = r.first ? give(*r.first) : give_none();
-        return give(rows, give(r.second));
+        const Tensor &dy = a.tensor(0), &ys = a.tensor(1), &weight = a.tensor(3);
+        const auto r = combine_grad(dy, ys, a.plan(2), weight, a.flag(4, true));
+        PyObject* rows = r.first ? give(*r.first, {dy, weight}, "experts.combine_grad") : give_none();
+        return give(rows, give(r.second, {dy, ys}, "experts.combine_grad"));
     });
 }
 MOR_CALL(py_expert_linear)
@@ -671,7 +685,8 @@ MOR_CALL(py_expert_linear)
     return guarded([&] {
         MOR_ARGS("linear", 2, 5, "x", "w", "ids", "weight", "format");
         const Tensor& x = a.tensor(0);
-        if (a.is_operand(1)) return give(expert_linear(x, a.operand(1), a.tensor(2), a.tensor(3)));
+        if (a.is_operand(1))
+            return give(expert_linear(x, a.operand(1), a.tensor(2), a.tensor(3)), {x, a.tensor(3)}, "experts.linear with a stored stack");
         const Tensor& w = a.tensor(1);
         want(w.dim() == 3 && x.dim() == 2 && x.size(1) == w.size(2), "x [tokens, n_in] and w [experts, n_out, n_in] are wanted");
         const Tensor &ids = a.tensor(2), &weight = a.tensor(3);

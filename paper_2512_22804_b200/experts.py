@@ -20,7 +20,9 @@
     (differentiable in x, w and weight; the rounding is passed straight through) or, for serving, a stored stack (``fp4.Operand`` with one
     matrix per expert; format is then its own).
 
-Gradients: linear has its own, of x, w and weight, once (its backward pass cannot be differentiated again).
+Gradients: linear has its own, of x, w and weight, once (its backward pass cannot be differentiated again).  gather, combine, combine_grad and linear
+with a stored stack have none: what they make of tensors that require a gradient raises when it is differentiated.  In a
+torch.autograd.Function of a caller's own, the gradient of gather(x, plan) is combine(dxs, plan) and that of combine is combine_grad.
 
 The formulas are those of ``include/mor.h``.
 """

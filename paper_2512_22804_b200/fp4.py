@@ -28,7 +28,8 @@ check their arguments, allocate their outputs and run on the current stream of t
     product's reduction axis, and the rounding is passed straight through in the backward pass.  x, w and the gradient may have any strides
     (rows that overlap or are not contiguous are copied first; the other calls refuse them).
 
-Gradients: linear has its own, of x and w, once (its backward pass cannot be differentiated again).
+Gradients: linear has its own, of x and w, once (its backward pass cannot be differentiated again).  An ``Operand`` carries none: nothing that is
+made of it through dequantize and matmul is differentiable in what was quantised.
 
 There is no CPU path: importing this module raises if the operators have not been built.
 """

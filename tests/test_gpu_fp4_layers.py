@@ -185,6 +185,24 @@ def test_a_second_derivative_is_refused(fp4, which):
             torch.autograd.grad(loss, inputs, retain_graph=True)
 
 
+def test_what_has_no_gradient_says_so(fp4, experts):
+    import torch
+
+    x, ys = drawn((20, 64), 1).requires_grad_(), drawn((40, 64), 2).requires_grad_()
+    weight = torch.rand(20, 2, device="cuda", requires_grad=True)
+    ids = torch.arange(40, device="cuda", dtype=torch.int32).view(20, 2) % 4
+    plan = experts.sort(ids, 4)
+    stored = fp4.quantize(drawn((4, 24, 64), 3), "e8m0_32")[0]
+    plan_rows = experts.gather(x, plan)
+    for out in (plan_rows, experts.gather(x.detach(), plan, weight), experts.combine(ys, plan), experts.combine(ys.detach(), plan, weight),
+                *experts.combine_grad(x, ys, plan, weight.detach()), experts.linear(x, stored, ids, weight.detach())):
+        with pytest.raises(RuntimeError, match="gradient"):
+            out.float().sum().backward()
+    with torch.no_grad():
+        assert not experts.gather(x, plan).requires_grad and torch.equal(experts.gather(x, plan), plan_rows)
+    assert not experts.gather(x.detach(), plan).requires_grad
+
+
 # ------------------------------------------------------------------------------------- operands far from one
 
 @pytest.mark.parametrize("m", [5, 300])
