@@ -50,9 +50,14 @@ __all__ = ["Operand", "quantize", "dequantize", "matmul", "matmul_rows", "matmul
 
 
 def check(device=None) -> None:
-    """Raises if a product on this device gave up a bounded wait since the last check (synchronises)."""
-    word = _status_word(torch.empty(0, device="cuda" if device is None else device))
-    status = int(word.item())
-    word.zero_()
-    if status != _b.MOR_OK:
-        raise _b.MorError(status, "mor_fp4_matmul")
+    """Raises if a product on this device gave up a bounded wait since the last check; its result is then undefined.  Waits for all of the
+    device's streams."""
+    device = torch.device("cuda" if device is None else device)
+    with torch.cuda.device(device):
+        word = _status_word(torch.empty(0, device="cuda"))
+        torch.cuda.synchronize()
+        status = int(word.item())
+        if status != _b.MOR_OK:
+            word.zero_()
+            torch.cuda.synchronize()
+            raise _b.MorError(status, "mor_fp4_matmul")

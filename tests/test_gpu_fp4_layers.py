@@ -203,6 +203,38 @@ def test_what_has_no_gradient_says_so(fp4, experts):
     assert not experts.gather(x.detach(), plan).requires_grad
 
 
+# ------------------------------------------------------------------------------------- streams, modes, errors
+
+def test_check_waits_for_every_stream(fp4):
+    """A product on another stream whose bounded wait runs out after some 50 ms (a host-set hook leaves out one tile's copy)."""
+    import ctypes
+
+    import torch
+
+    from paper_2512_22804_b200 import binding as mb
+
+    hook = mb.load().mor_test_skip_tile_load
+    hook.argtypes, hook.restype = [ctypes.c_uint32, ctypes.c_longlong], None
+    a, b = (fp4.quantize(drawn((n, 512), n), "e8m0_32")[0] for n in (300, 264))
+    fp4.matmul(a, b)
+    fp4.check()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    hook(0, 100_000_000)
+    try:
+        with torch.cuda.stream(side):
+            fp4.matmul(a, b)
+    finally:
+        hook(0xFFFFFFFF, 0)
+    try:
+        with pytest.raises(mb.MorError) as e:
+            fp4.check()
+        assert e.value.status == mb.MOR_ERR_TIMEOUT
+    finally:
+        torch.cuda.synchronize()
+    fp4.check()
+
+
 # ------------------------------------------------------------------------------------- operands far from one
 
 @pytest.mark.parametrize("m", [5, 300])
