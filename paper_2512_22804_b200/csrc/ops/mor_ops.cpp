@@ -11,6 +11,7 @@
 #include <torch/extension.h>
 
 #include <memory>
+#include <mutex>
 #include <optional>
 #include <string>
 
@@ -69,16 +70,24 @@ Tensor empty(at::IntArrayRef shape, at::ScalarType type, const Tensor& like) { r
 Tensor bytes(int64_t n, const Tensor& like) { return empty({n}, at::kByte, like); }
 
 // The word that products set when a bounded wait ran out, one per device, never given back.  It is cleared before any stream uses it;
-// a first call inside a stream capture, where that cannot be waited for, goes without.
+// a first call inside a stream capture, where that cannot be waited for, goes without.  It is an ordinary tensor whatever mode the first call
+// runs in, and autograd's threads may come here beside the caller's: the first to be ready gives the word.
 Tensor status_word(const Tensor& like)
 {
     static std::vector<Tensor>* words = new std::vector<Tensor>(64);
-    Tensor& w = words->at(like.get_device());
-    if (!w.defined()) {
-        if (c10::cuda::currentStreamCaptureStatusMayInitCtx() != c10::cuda::CaptureStatus::None) return Tensor();
-        w = at::zeros({1}, like.options().dtype(at::kInt).requires_grad(false));
-        c10::cuda::getCurrentCUDAStream().synchronize();
+    static std::mutex* lock = new std::mutex;
+    {
+        const std::lock_guard<std::mutex> hold(*lock);
+        const Tensor& w = words->at(like.get_device());
+        if (w.defined()) return w;
     }
+    if (c10::cuda::currentStreamCaptureStatusMayInitCtx() != c10::cuda::CaptureStatus::None) return Tensor();
+    const c10::InferenceMode ordinary(false);
+    const Tensor fresh = at::zeros({1}, at::TensorOptions(like.device()).dtype(at::kInt));
+    c10::cuda::getCurrentCUDAStream(like.device().index()).synchronize();
+    const std::lock_guard<std::mutex> hold(*lock);
+    Tensor& w = words->at(like.get_device());
+    if (!w.defined()) w = fresh;
     return w;
 }
 

@@ -235,6 +235,27 @@ def test_check_waits_for_every_stream(fp4):
     fp4.check()
 
 
+def in_fresh_process(code):
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
+
+
+def test_check_after_a_first_product_in_inference_mode():
+    in_fresh_process("""
+import torch
+from paper_2512_22804_b200 import fp4
+x = torch.randn(20, 64, device="cuda").to(torch.bfloat16)
+with torch.inference_mode():
+    a = fp4.quantize(x, "e8m0_32")[0]
+    y = fp4.matmul(a, a)
+fp4.check()
+with torch.inference_mode():
+    fp4.check()
+fp4.check("cuda:0")
+fp4.check(0)
+""")
+
+
 # ------------------------------------------------------------------------------------- operands far from one
 
 @pytest.mark.parametrize("m", [5, 300])
