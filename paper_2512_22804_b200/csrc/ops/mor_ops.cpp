@@ -591,8 +591,8 @@ template <typename F> PyObject* guarded(F&& f)
         e.restore();
     } catch (py::builtin_exception& e) {
         e.set_error();
-    } catch (const std::exception& e) {
-        PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (const std::exception&) {
+        torch::translate_exception_to_python(std::current_exception());       // torch's own errors as torch's own types (OutOfMemoryError)
     }
     return nullptr;
 }

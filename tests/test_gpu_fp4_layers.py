@@ -256,6 +256,15 @@ fp4.check(0)
 """)
 
 
+def test_running_out_of_memory_is_torchs_error(fp4):
+    """2 TB of result: refused by the allocator, as for torch's own product."""
+    import torch
+
+    a = fp4.quantize(torch.zeros(1 << 20, 32, device="cuda", dtype=torch.bfloat16), "e8m0_32")[0]
+    with pytest.raises(torch.OutOfMemoryError):
+        fp4.matmul(a, a)
+
+
 # ------------------------------------------------------------------------------------- operands far from one
 
 @pytest.mark.parametrize("m", [5, 300])
