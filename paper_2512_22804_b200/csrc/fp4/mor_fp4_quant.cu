@@ -630,6 +630,15 @@ __global__ void __launch_bounds__(kQThreads, 2) fp4_stream_kernel(const __grid_c
     }
 }
 
+// A tensor without elements has no codes, but a tensor scale like any other.
+__global__ void fp4_empty_kernel(int format, const float* amax, float* r_t, float* c_t)
+{
+    wait_for_predecessor();
+    const float t = format == MOR_FP4_E4M3_16 ? tensor_scale_of(amax != nullptr ? *amax : 0.f).t : 1.f;
+    if (r_t != nullptr) *r_t = t;
+    if (c_t != nullptr) *c_t = t;
+}
+
 struct DequantParams {
     const uint8_t *codes, *scales;
     const float* t;
@@ -819,7 +828,10 @@ mor_status_t mor_fp4_quantize(const mor_fp4_quantize_desc_t* host_desc, const mo
         if (!is_aligned(workspace, 16)) return MOR_ERR_ALIGNMENT;
     }
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (empty) return MOR_OK;
+    if (empty) {
+        float *r_t = host_rows != nullptr ? host_rows->tensor_scale : nullptr, *c_t = host_cols != nullptr ? host_cols->tensor_scale : nullptr;
+        return launch(fp4_empty_kernel, 1, 1, 0, st, true, d.format, d.amax, r_t, c_t) == cudaSuccess ? MOR_OK : MOR_ERR_CUDA;
+    }
 
     QuantParams p = {};
     p.x = d.x;

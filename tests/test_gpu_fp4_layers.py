@@ -265,6 +265,19 @@ def test_running_out_of_memory_is_torchs_error(fp4):
         fp4.matmul(a, a)
 
 
+@pytest.mark.parametrize("shape", [(0, 64), (64, 0), (3, 0, 64)])
+def test_tensor_scale_of_nothing(fp4, shape):
+    import torch
+
+    for fmt, t in (("e8m0_32", np.float32(1)), ("e4m3_16", np.float32(2.0 ** -88) * (np.float32(1) / np.float32(2688)))):
+        poison = [torch.full((512,), 255, device="cuda", dtype=torch.uint8) for _ in range(8)]
+        del poison
+        r, c = fp4.quantize(torch.zeros(shape, device="cuda", dtype=torch.bfloat16), fmt, cols=True)
+        assert r.tensor_scale.item() == t and c.tensor_scale.item() == t
+    r, _ = fp4.quantize(torch.zeros(shape, device="cuda", dtype=torch.bfloat16), "e4m3_16", amax=torch.tensor([2688.0], device="cuda"))
+    assert r.tensor_scale.item() == np.float32(2688) * (np.float32(1) / np.float32(2688))
+
+
 # ------------------------------------------------------------------------------------- operands far from one
 
 @pytest.mark.parametrize("m", [5, 300])
