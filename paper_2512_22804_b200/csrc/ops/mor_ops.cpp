@@ -40,7 +40,12 @@ void want(bool ok, const std::string& message)
 }
 int format_of(PyObject* f)
 {
-    if (f != nullptr && PyLong_Check(f)) return (int)PyLong_AsLong(f);
+    if (f != nullptr && PyLong_Check(f)) {
+        int too_large;
+        const long n = PyLong_AsLongAndOverflow(f, &too_large);
+        want(!too_large && (n == MOR_FP4_E4M3_16 || n == MOR_FP4_E8M0_32), "format: \"e4m3_16\" or \"e8m0_32\" (or the library's number of one) is wanted");
+        return (int)n;
+    }
     if (f == nullptr || !PyUnicode_Check(f)) throw py::type_error("format: \"e4m3_16\" or \"e8m0_32\" is wanted");
     if (PyUnicode_CompareWithASCIIString(f, "e4m3_16") == 0) return MOR_FP4_E4M3_16;
     if (PyUnicode_CompareWithASCIIString(f, "e8m0_32") == 0) return MOR_FP4_E8M0_32;

@@ -174,3 +174,18 @@ def test_python_refusals(lib):
         fp4.linear(x, torch.zeros(4, 9), "e8m0_32")
     with pytest.raises(ValueError, match="n_in"):
         experts.linear(x, torch.zeros(2, 4, 9), None, None, "e8m0_32")
+
+
+@pytest.mark.parametrize("format", [2, -1, 1 << 40, 1 << 80, -(1 << 80)])
+def test_numbers_that_name_no_format_are_refused(lib, format):
+    import torch
+
+    from paper_2512_22804_b200 import fp4
+
+    byte = torch.zeros(4, 16, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="format"):
+        fp4.Operand(byte, byte, 4, 8, format, torch.ones(1))
+    with pytest.raises(ValueError, match="format"):
+        fp4.quantize(torch.zeros(4, 8), format)
+    with pytest.raises(ValueError, match="CUDA"):
+        fp4.quantize(torch.zeros(4, 8), 1)
