@@ -307,6 +307,31 @@ def test_zero_rows_beside_large_operands(fp4):
 
 # ------------------------------------------------------------------------------------- 32-bit rows, and one rounding
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("weighted", [False, True])
+@pytest.mark.parametrize("start", [0, 1, 4])
+def test_quantised_gather_of_32_bit_rows(fp4, experts, fmt, weighted, start):
+    import torch
+
+    for tokens, hidden in ((40, 96), (300, 333), (1100, 1544)):
+        rng = np.random.default_rng(tokens)
+        ids = rng.integers(-1, 6, (tokens, 3)).astype(np.int32)
+        plan = experts.sort(torch.from_numpy(ids).cuda(), 6, 128)
+        _, row, slot = plain.sort(ids, 6, 128)
+        x, w = rng.standard_normal((tokens, hidden)).astype(np.float32), rng.random((tokens, 3)).astype(np.float32)
+        rows = np.zeros((len(slot), hidden), np.float32)
+        at = slot >= 0
+        rows[at] = x[slot[at] // 3] * (w.reshape(-1)[slot[at]][:, None] if weighted else np.float32(1))
+        wide = torch.full((tokens, hidden + start), 1e30, device="cuda")
+        wide[:, start:] = torch.from_numpy(x).cuda()
+        r, c = fp4.quantize(wide[:, start:], fmt, cols=True, gather=plan, weight=torch.from_numpy(w).cuda() if weighted else None)
+        for op, v in ((r, rows), (c, np.ascontiguousarray(rows.T))):
+            codes, byte, t = plain.quantize(v, fmt)
+            assert np.array_equal(op.codes.cpu().numpy().reshape(v.shape[0], -1), plain.packed(codes))
+            assert np.array_equal(op.scales.cpu().numpy().reshape(-1), plain.tiled(byte))
+            assert op.tensor_scale.item() == t
+
+
 def between(got, want, room, dtype):
     """got lies between the rounded ends of want -+ room."""
     low, high = ((want + s * room).astype(np.float32) for s in (-1, 1))
@@ -314,6 +339,24 @@ def between(got, want, room, dtype):
         low, high = plain.bf16(low), plain.bf16(high)
     got = got.detach().float().cpu().numpy()
     return bool((low <= got).all() and (got <= high).all())
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("m,n,k", [(5, 33, 100), (200, 136, 300)])
+def test_linear_of_32_bit_tensors(fp4, fmt, m, n, k):
+    import torch
+
+    rng = np.random.default_rng(m)
+    x, w, g = (rng.standard_normal(s).astype(np.float32) for s in ((m, k), (n, k), (m, n)))
+    tx, tw = (torch.from_numpy(v).cuda().requires_grad_() for v in (x, w))
+    y = fp4.linear(tx, tw, fmt)
+    dx, dw = torch.autograd.grad(y, (tx, tw), torch.from_numpy(g).cuda())
+
+    def v(z):
+        return plain.values(*plain.quantize(z, fmt), fmt)
+
+    for got, a, b in ((y, v(x), v(w)), (dx, v(g), v(w.T)), (dw, v(g.T), v(x.T))):
+        assert got.dtype == torch.float32 and between(got, a @ b.T, np.abs(a) @ np.abs(b).T * 2.0 ** -16, "fp32")
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
