@@ -749,9 +749,11 @@ template <typename T, int FMT, bool ROWS, bool COLS, int MODE> cudaError_t quant
     if (smem > 0 && !allow_smem(fp4_quant_kernel<T, FMT, ROWS, COLS, MODE>, smem, done)) return cudaErrorInvalidValue;
     // As many CTAs as are resident, each walking its tiles: the tensor's scale and its table are made once a CTA (8192 x 14336 E4M3_16 rows
     // with the maximum 91 us, 104 with a CTA per tile; 4096 x 4096 15 and 18.5), and the kernel may start early (4096 x 4096 E8M0_32
-    // 8.0 us and 10.3).  E8M0_32 has nothing to share, and a CTA per tile is ahead beyond 2048 tiles (FP32 8192 x 14336: 89 us and 95).
+    // 8.0 us and 10.3).  E8M0_32 has nothing to share, and a CTA per tile is ahead beyond 1024 tiles (rows alone, walked and not, in a graph: 512
+    // tiles BF16 5.3 and 5.6 us, FP32 9.2 and 10.5; 1024: 8.6 and 8.7, 16.0 and 16.1; 2048: 15.8 and 15.2, 30.1 and 28.9; 7168: 47.6 and
+    // 45.2, 97 and 89).
     constexpr uint32_t most = 148 * (kNarrow ? 4 : 2);
-    const bool walk = FMT == MOR_FP4_E4M3_16 || grid <= 2048;
+    const bool walk = FMT == MOR_FP4_E4M3_16 || grid <= 1024;
     return launch(fp4_quant_kernel<T, FMT, ROWS, COLS, MODE>, walk && grid > most ? most : grid, kQThreads, smem, st, walk, p);
 }
 template <typename T, int FMT, int MODE> cudaError_t quant_dirs(const QuantParams& p, uint32_t grid, cudaStream_t st)

@@ -406,3 +406,14 @@ def test_expert_layer_rounds_once(fp4, experts, fmt, dtype, tokens, top, n, k, m
     assert between(y, (taken(ys) * wt[..., None]).sum(1), some * (taken(sy) * wt[..., None]).sum(1), dtype)
     assert between(dwt, (taken(ys) * g[:, None, :]).sum(-1), (2.0 ** -16 + m * 2.0 ** -24) * (taken(sy) * np.abs(g)[:, None, :]).sum(-1), "fp32")
     assert between(dx, taken(dxs).sum(1), some * taken(sx).sum(1), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_more_tiles_than_are_walked(fp4, fmt, dtype):
+    """Rows alone, 1122 tiles: beyond the number up to which resident CTAs walk them whatever the format."""
+    x = drawn((4100, 4228), 3, dtype)
+    codes, byte, t = plain.quantize(x.float().cpu().numpy(), fmt)
+    r, _ = fp4.quantize(x, fmt)
+    assert np.array_equal(r.codes.cpu().numpy().reshape(4100, -1), plain.packed(codes))
+    assert np.array_equal(r.scales.cpu().numpy().reshape(-1), plain.tiled(byte)) and r.tensor_scale.item() == t
