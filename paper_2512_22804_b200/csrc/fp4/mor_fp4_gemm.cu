@@ -645,6 +645,10 @@ template <int FMT, typename T> mor_status_t run_format(GemmParams& p, const mor_
     // 1024 39.6 us against 41.2 by pairs, 1024 -> 2048 52.8 against 59.4)
     if (p.grouping == MOR_GROUP_ROWS) return run_wide<1, 256, FMT, T, MOR_GROUP_ROWS>(p, a, b, enc, st);
     if (p.grouping == MOR_GROUP_REDUCE) return run_wide<2, 256, FMT, T, MOR_GROUP_REDUCE>(p, a, b, enc, st);
+    // The narrow kernel spreads few tokens over the whole GPU, the wide one fetches the weights once for 256.  E8M0_32, weights beyond L2, narrow and
+    // wide by tokens: 4096 x 4096: 32 6.9 and 9.2 us, 64 8.4 and 9.7, 128 11.2 and 10.6, 256 14.9 and 10.7; 4096 outputs x 14336: 64 11.8 and
+    // 21.2, 128 14.8 and 22.1, 256 20.3 and 22.2.  With 14336 outputs the wide kernel has tiles for 56 pairs and is ahead from 32 tokens on (12.7
+    // and 11.8 us; 128: 24.6 and 12.4): the switch at 128 tokens is right for few outputs or a long reduction axis and gives that case away.
     if (p.m <= 16) return run_narrow<16, FMT, T>(p, a, b, enc, st);
     if (p.m <= 32) return run_narrow<32, FMT, T>(p, a, b, enc, st);
     if (p.m <= 64) return run_narrow<64, FMT, T>(p, a, b, enc, st);
