@@ -234,8 +234,9 @@ template <typename T, int COLS> __device__ __forceinline__ void store_row_off16(
 // products.  8192 x 14336 x 4096 E4M3_16 -> BF16: 190-200 us (4.8-5.0 PFLOP/s) in a short run, 226 us at the 1000 W cap (1.4 GHz);
 // 8192 x 4096 x 8192: 100 us (5.5 PFLOP/s).  Its copies alone take 142 us (54 bytes a clock and SM from L2), its products alone 157 us,
 // and without the result's stores it is 30 us faster.  256 x 192 tiles with two accumulator sets: 215 us.
-// Groups of rows, 28,700 rows over 32 groups, E8M0_32: 2048 -> 1024 40 us, 1024 -> 2048 53 us, 29 us each without the stores (64 and 127 MB);
-// groups of the reduction axis, 32 results of 1024 x 2048: 62 us.
+// Groups of rows, 28,956 rows over 32 groups, E8M0_32: 2048 -> 1024 40 us, 1024 -> 2048 54 us, 29 us each without the stores (64 and 127 MB); with FP32
+// results 51 and 78 us.  Groups of the reduction axis, 32 results of 1024 x 2048: 63 us, FP32 87.  The tensor pipe is 18-42 % active and DRAM at
+// 24-35 % of its peak: with 4 to 8 stages a tile, what bounds them is that products and reading out take turns at the one accumulator set.
 template <int CG, int NT, int FMT, typename T, int GROUP>
 __global__ void __launch_bounds__(kWideThreads, 1) fp4_wide_kernel(const __grid_constant__ GemmParams p)
 {

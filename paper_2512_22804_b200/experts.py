@@ -18,7 +18,8 @@
 ``linear(x, w, ids, weight, format=None)``
     y[t] = sum over j of weight[t, j] * Q(x[t]) Q(w[ids[t, j]])^T for x [tokens, n_in].  w is a tensor [experts, n_out, n_in]
     (differentiable in x, w and weight; the rounding is passed straight through) or, for serving, a stored stack (``fp4.Operand`` with one
-    matrix per expert; format is then its own).
+    matrix per expert; format is then its own).  x, w and the gradient may have any strides (rows that overlap or are not contiguous are copied
+    first); ids and weight are contiguous.
 
 Gradients: linear has its own, of x, w and weight, once (its backward pass cannot be differentiated again).  gather, combine, combine_grad and linear
 with a stored stack have none: what they make of tensors that require a gradient raises when it is differentiated.  In a
