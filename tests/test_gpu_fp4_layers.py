@@ -146,11 +146,13 @@ def test_hooks_on_saved_tensors_see_what_is_kept(fp4, which):
     inputs, call = layer(which, "e8m0_32", tokens, n_out, n_in=n_in)
     dy = drawn((tokens, n_out), 9)
     want = torch.autograd.grad(call(), inputs, dy)
-    torch.cuda.synchronize()
-    before = torch.cuda.memory_allocated()
+    def held():                                        # bytes asked for; what the allocator rounds them up to depends on what it has free
+        return torch.cuda.memory_stats()["requested_bytes.all.current"]
+
+    before = held()
     with torch.autograd.graph.save_on_cpu():
         y = call()
-    assert torch.cuda.memory_allocated() - before <= y.numel() * 2 + 65536
+    assert held() - before <= y.numel() * 2
     got = torch.autograd.grad(y, inputs, dy)
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
