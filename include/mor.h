@@ -410,6 +410,117 @@ MOR_API mor_status_t mor_expert_combine(const mor_expert_desc_t* host_desc, cons
 MOR_API mor_status_t mor_expert_combine_grad(const mor_expert_desc_t* host_desc, const void* dy, int64_t lddy, const void* ys,
                                              int64_t ldy, void* dys, int64_t lddys, void* dweight, void* cuda_stream);
 
+/* --------------------------------------------------------------------- norm before a projection ----
+ * Root-mean-square norm of the rows of a matrix, with the residual's addition before it:
+ *   h = x + residual, rounded once to the residual's type (h = x where there is none)
+ *   y = (h * rs) * weight with rs = 1 / sqrt(mean(h^2) + eps) in binary32, rounded once to x's type or to 8 bits.
+ * 8 bits: E4M3 codes of y * s and a scale s for every 128 columns of a row, or for a row: fl32(448 / a) with a the largest finite |y|
+ * (at most the largest binary32; 1 where a is 0), or that cut to a power of two and kept as its biased exponent.  These are the codes and
+ * scales of mor_analyze_quantize with the (1,128) and (1,0) partitions and the FP32-amax and E8M0 scale modes, made from y in binary32.
+ * A NaN's code is 0x7F, an infinity's the largest finite value's. */
+typedef struct mor_norm_desc {
+    int64_t rows, cols;      /* cols < 2^31 - 4096                                             */
+    const void* x;           /* DEVICE [rows, ldx], aligned to its element; full speed where rows start on 16 bytes      */
+    const void* residual;    /* DEVICE [rows, ldr], optional                                   */
+    const void* weight;      /* DEVICE [cols]                                                  */
+    int64_t ldx, ldr;        /* in elements; >= cols                                           */
+    float   eps;
+    int32_t dtype;           /* mor_dtype_t of x and y                                         */
+    int32_t residual_dtype;  /* of residual and h; without a residual ignored                  */
+    int32_t weight_dtype;
+} mor_norm_desc_t;
+typedef struct mor_norm_outputs {
+    void*    h;              /* [rows, ldh] optional, only with a residual; may be the residual itself                   */
+    void*    y;              /* [rows, ldy] optional                                           */
+    uint8_t* codes;          /* [rows, ldc] optional                                           */
+    uint8_t* scale_e8m0;     /* [rows, blocks] with codes: this one or                         */
+    float*   scale_f32;      /* this one                                                       */
+    int64_t  ldh, ldy, ldc;
+    int32_t  block;          /* columns of a scale: 128, or 0 for a whole row                  */
+} mor_norm_outputs_t;
+MOR_API mor_status_t mor_rms_norm(const mor_norm_desc_t* host_desc, const mor_norm_outputs_t* host_out, void* cuda_stream);
+
+/* The gradient.  host_desc->x is h (the sum as it was stored, in `residual_dtype` if `has_residual`, else x in `dtype`), ->residual the
+ * gradient of h from elsewhere (optional, [rows, ldr], h's type).  dy [rows, lddy] in `dtype`.
+ *   dh = rs (g - h rs mean(g h rs)) + residual with g = dy * weight
+ * dx [rows, lddx] in `dtype` and dr [rows, lddr] in residual_dtype get dh (each optional, each rounded once); dweight [cols], optional, in
+ * weight_dtype gets the sum over the rows of dy h rs, taken in binary32 in an order that depends on the shape alone.
+ * `workspace`: mor_rms_norm_grad_workspace_bytes() of DEVICE scratch, 16-byte aligned, no initialisation needed; only for dweight. */
+MOR_API size_t mor_rms_norm_grad_workspace_bytes(int64_t rows, int64_t cols);
+MOR_API mor_status_t mor_rms_norm_grad(const mor_norm_desc_t* host_desc, int has_residual, const void* dy, int64_t lddy, void* dx, int64_t lddx,
+                                       void* dr, int64_t lddr, void* dweight, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Values of E4M3 codes [rows, ldc] with one scale per `block` columns (0: per row), E8M0 or FP32 (one of the two): code / scale rounded once
+ * to `dtype`, [rows, ldo]. */
+MOR_API mor_status_t mor_codes_dequantize(const uint8_t* codes, int64_t rows, int64_t cols, int64_t ldc, int block, const uint8_t* scale_e8m0,
+                                          const float* scale_f32, void* out, int dtype, int64_t ldo, void* cuda_stream);
+
+/* ----------------------------------------------- low-rank adapters beside a shared projection ----
+ * out[t] = base[t] + f scale[g] (x[t] a[g]^T) b[g]^T with g = ids[t], the adapter of token t; a token whose id is no adapter's keeps base[t].  Inner
+ * products of `rank` terms are kept in binary32 and enter the second product as two BF16 that add up to 16 bits and more; out is rounded once. */
+typedef struct mor_adapter_desc {
+    int64_t tokens, n_in, n_out; /* widths 1 .. 2^21                                             */
+    int32_t adapters, rank;      /* adapters <= MOR_MAX_GROUPS - 1; rank 1 .. MOR_MAX_RANK       */
+    const void* a;               /* DEVICE BF16 [adapters][rank][n_in]                           */
+    const void* b;               /* DEVICE BF16 [adapters][n_out][rank]                          */
+    const int32_t* ids;          /* DEVICE [tokens]; NULL = every token has adapter 0            */
+    const float* scale;          /* DEVICE [adapters], optional (1)                              */
+    float factor;                /* f                                                            */
+} mor_adapter_desc_t;
+#define MOR_MAX_RANK 512
+
+/* DEVICE scratch of a call, 256-byte aligned, no initialisation needed; may be 0.  train: the scratch is what mor_adapter_grad reads of the
+ * forward call (tokens sorted by adapter, the inner products), to be kept until then. */
+MOR_API size_t mor_adapter_workspace_bytes(const mor_adapter_desc_t* host_desc, int train);
+/* x BF16 [tokens, ldx]; base and out [tokens, ldb], [tokens, ldo] of `dtype` (mor_dtype_t), out may be base. */
+MOR_API mor_status_t mor_adapter_add(const mor_adapter_desc_t* host_desc, const void* x, int64_t ldx, const void* base, int64_t ldb, void* out,
+                                     int64_t ldo, int dtype, int train, void* workspace, size_t workspace_bytes, void* cuda_stream);
+/* Gradients for dy, BF16 [tokens, lddy], with u[t] = f scale[g] dy[t] b[g]: dx [tokens, lddx] BF16 = base[t] + u[t] a[g] (base optional: the
+ * gradient from the shared projection, BF16 [tokens, ldb]), da = sum u[t]^T x[t], db = sum f scale[g] dy[t]^T (x[t] a[g]^T), BF16 in a's and b's shapes;
+ * zero for an adapter without tokens.  dx, da, db are optional.  `saved`: the workspace of mor_adapter_add with train. */
+MOR_API size_t mor_adapter_grad_workspace_bytes(const mor_adapter_desc_t* host_desc);
+MOR_API mor_status_t mor_adapter_grad(const mor_adapter_desc_t* host_desc, const void* x, int64_t ldx, const void* dy, int64_t lddy, const void* base,
+                                      int64_t ldb, void* dx, int64_t lddx, void* da, void* db, const void* saved, size_t saved_bytes, void* workspace,
+                                      size_t workspace_bytes, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------- an optimizer's step ----
+ * AdamW with the decay apart from the gradient, over many tensors with one launch for every 512.  With g the gradient times grad_scale:
+ *   m = beta1 m + (1 - beta1) g       v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ * in binary32.  Parameters and gradients are BF16 or FP32.  The moments are FP32, or 8 bits: blocks of 128 consecutive elements share a
+ * power of two s, the largest that keeps the block's largest finite magnitude times s within 448 (kept as a biased exponent, at most 253; 127
+ * for a block of zeros); the first moment is an E4M3 code of m s, the second of w = sqrt(v) s, so that an element may be 2^17 below its
+ * block's largest and still count.  Nearest rounding would stop a moment that moves by a thousandth a step, so codes are rounded up or down by a
+ * random number u: with t the magnitude over the distance d of its two neighbours n d and (n + 1) d, m takes the upper where t + u >= n + 1
+ * (its mean is kept), w where u (2 n + 1) < (t - n)(t + n) (the mean of its square is kept), and a w above zero is at least the smallest code, since
+ * it is divided by.  What is not finite becomes NaN.  BF16 parameters are rounded by 16 random bits added below the kept ones.
+ * Random numbers are hashes, in 32 bits: mix(z): z ^= z >> 16; z *= 0x7FEB352D; z ^= z >> 15; z *= 0x846CA68B; z ^= z >> 16.  With key =
+ * mix(mix(seed + 0x9E3779B9 * step) + tensor's number in the call) and z = mix(mix(high half of the element's number ^ key) + low half), the low 16 bits
+ * of z / 65536 are u of m, the high ones u of w, the low ones of mix(z ^ 0x9E3779B9) the parameter's. */
+typedef struct mor_adamw_tensor {
+    void*       param;       /* DEVICE, contiguous, aligned to its element; full speed on 32 bytes  */
+    const void* grad;
+    void*       exp_avg;     /* FP32 or codes                                                  */
+    void*       exp_avg_sq;
+    uint8_t*    scales;      /* codes only: [blocks][2] of exp_avg and exp_avg_sq, 2-byte aligned */
+    int64_t     numel;
+} mor_adamw_tensor_t;
+typedef struct mor_adamw_desc {
+    double  lr, beta1, beta2, eps, weight_decay;
+    int64_t step;            /* number of this step, from 1                                    */
+    const int32_t* device_step;   /* DEVICE, optional: the step's number instead, for a captured call that is replayed   */
+    const float*   device_lr;     /* DEVICE, optional: the learning rate instead               */
+    const float*   grad_scale;    /* DEVICE, optional: factor of every gradient (clipping, loss scale)                   */
+    const float*   found_inf;     /* DEVICE, optional: not zero = the call changes nothing     */
+    uint64_t seed;           /* its low 32 bits count                                          */
+    int32_t param_dtype, grad_dtype;   /* mor_dtype_t                                          */
+    int32_t eight_bits;      /* moments as codes                                               */
+} mor_adamw_desc_t;
+MOR_API mor_status_t mor_adamw(const mor_adamw_desc_t* host_desc, const mor_adamw_tensor_t* host_tensors, int n, void* cuda_stream);
+/* Values of 8-bit moments: m = code / s into exp_avg_out, v = (code / s)^2 into exp_avg_sq_out ([numel] in `dtype`, each optional). */
+MOR_API mor_status_t mor_adamw_moments(const uint8_t* exp_avg, const uint8_t* exp_avg_sq, const uint8_t* scales, int64_t numel, void* exp_avg_out,
+                                       void* exp_avg_sq_out, int dtype, void* cuda_stream);
+
 MOR_API const char* mor_status_string(mor_status_t status);
 MOR_API int mor_version(void);
 

@@ -16,7 +16,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmor_b200.so")
 SOURCES = ["mor_api.cu", "mor_kernels.cu", "mor_static.cu", "mor_main.cu", "mor_main_tensor.cu", "mor_main_row128.cu",
            "mor_main_blk128.cu", "mor_main_blk64.cu", "mor_main_col128.cu", "mor_main_channel.cu", "mor_main_dual.cu", "mor_main_colch.cu",
-           "fp4/mor_fp4_quant.cu", "fp4/mor_fp4_gemm.cu", "fp4/mor_experts.cu"]
+           "fp4/mor_fp4_quant.cu", "fp4/mor_fp4_gemm.cu", "fp4/mor_experts.cu",
+           "layers/mor_norm.cu", "layers/mor_adapters.cu", "layers/mor_adamw.cu"]
 OBJ_DIR = os.path.join(HERE, "_build")
 OPS_SOURCE = os.path.join(CSRC, "ops", "mor_ops.cpp")
 OPS = os.path.join(HERE, "_ops.so")
@@ -76,8 +77,8 @@ def build(force: bool = False, verbose: bool = False, lib: str = LIB, extra_flag
 
 def build_ops(force: bool = False) -> str:
     """Compile the torch operators against the installed torch; they find ``libmor_b200.so`` beside themselves."""
-    header = os.path.join(ROOT, "include", "mor.h")
-    if not force and os.path.exists(OPS) and os.path.getmtime(OPS) > max(os.path.getmtime(OPS_SOURCE), os.path.getmtime(header)):
+    sources = [OPS_SOURCE, os.path.join(CSRC, "ops", "mor_layers.h"), os.path.join(ROOT, "include", "mor.h")]
+    if not force and os.path.exists(OPS) and os.path.getmtime(OPS) > max(os.path.getmtime(f) for f in sources):
         return OPS
     import sysconfig
 

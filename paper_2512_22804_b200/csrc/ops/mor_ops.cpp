@@ -2,7 +2,7 @@
 // small call costs its launches and little else (in Python the same steps took 10 us a call where a launch takes 3 us).  Arguments
 // come by the interpreter's vector calls and objects are plain types: through pybind11's own conversions a call of quantize()
 // spent 1.4 us on them, this way 0.1.  All work happens behind the C boundary (mor.h); this file holds no arithmetic.  Module
-// `_ops`, used through fp4.py and experts.py.
+// `_ops`, used through fp4.py, experts.py, norm.py, adapters.py and optim.py.
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAGraphsC10Utils.h>
@@ -10,10 +10,13 @@
 #include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/extension.h>
 
+#include <algorithm>
+#include <cmath>
 #include <memory>
 #include <mutex>
 #include <optional>
 #include <string>
+#include <vector>
 
 #include "mor.h"
 
@@ -465,6 +468,8 @@ Tensor expert_linear(const Tensor& x, const Matrix& stack, const Tensor& ids, co
     return expert_forward(x, stack, sort_slots(ids, stack.c.batch, 128), weight, false, &ys, &a_t);
 }
 
+#include "mor_layers.h"
+
 // ---- the interpreter's side
 
 struct OperandObject {
@@ -551,6 +556,28 @@ public:
         if (!THPDtype_Check(v_[i])) wrong(i, "a dtype");
         return reinterpret_cast<THPDtype*>(v_[i])->scalar_type;
     }
+    double number(size_t i, double otherwise) const
+    {
+        if (v_[i] == nullptr) return otherwise;
+        const double r = PyFloat_AsDouble(v_[i]);
+        if (r == -1.0 && PyErr_Occurred()) throw py::error_already_set();
+        return r;
+    }
+    bool is_tensor(size_t i) const { return v_[i] != nullptr && THPVariable_Check(v_[i]); }
+    std::vector<Tensor> tensors(size_t i) const
+    {
+        std::vector<Tensor> r;
+        if (v_[i] == nullptr) return r;
+        if (!PyList_Check(v_[i]) && !PyTuple_Check(v_[i])) wrong(i, "a list of tensors");
+        const size_t n = (size_t)PySequence_Fast_GET_SIZE(v_[i]);
+        PyObject** items = PySequence_Fast_ITEMS(v_[i]);
+        r.reserve(n);
+        for (size_t k = 0; k < n; ++k) {
+            if (!THPVariable_Check(items[k])) wrong(i, "a list of tensors");
+            r.push_back(THPVariable_Unpack(items[k]));
+        }
+        return r;
+    }
     bool is_operand(size_t i) const { return v_[i] != nullptr && Py_TYPE(v_[i]) == &operand_type; }
     const Matrix& operand(size_t i) const
     {
@@ -573,7 +600,7 @@ private:
     [[noreturn]] void wrong(size_t i, const char* what) const { throw py::type_error(std::string(function_) + "(): " + names_[i] + ": " + what + " is wanted"); }
     const char* function_;
     const char* const* names_;
-    PyObject* v_[8] = {};
+    PyObject* v_[16] = {};
 };
 
 // A result of a call that has no gradient of its own.
@@ -708,6 +735,106 @@ MOR_CALL(py_expert_linear)
         return give(ExpertFn::apply(x, w, ids, weight, (int64_t)f, needs_grad(x), needs_grad(w), needs_grad(weight)));
     });
 }
+// "e8m0" or "fp32".
+bool is_e8m0(PyObject* s)
+{
+    if (s == nullptr) return true;
+    if (!PyUnicode_Check(s)) throw py::type_error("scale: \"e8m0\" or \"fp32\" is wanted");
+    if (PyUnicode_CompareWithASCIIString(s, "e8m0") == 0) return true;
+    if (PyUnicode_CompareWithASCIIString(s, "fp32") == 0) return false;
+    throw py::key_error(PyUnicode_AsUTF8(s));
+}
+MOR_CALL(py_rms_norm)
+{
+    return guarded([&] {
+        MOR_ARGS("rms_norm", 2, 3, "x", "weight", "residual", "eps");
+        const variable_list r = rms_norm(a.tensor(0), a.tensor(1), a.maybe_tensor(2), a.number(3, 1e-6));
+        return r.size() == 1 ? give(r[0]) : give(give(r[0]), give(r[1]));
+    });
+}
+MOR_CALL(py_rms_norm_quantize)
+{
+    return guarded([&] {
+        MOR_ARGS("rms_norm_quantize", 2, 3, "x", "weight", "residual", "eps", "scale", "block");
+        const std::optional<Tensor> residual = a.maybe_tensor(2);
+        const int64_t block = a.integer(5, 0);           // the caller's module turns None into 0
+        want(block == 0 || block == 128, "block: 128 columns, or None for a whole row, is wanted");
+        const variable_list r = rms_norm_quantize(a.tensor(0), a.tensor(1), residual, a.number(3, 1e-6), block, is_e8m0(a[4]));
+        const std::initializer_list<Tensor> from = {a.tensor(0), a.tensor(1), residual.value_or(Tensor())};
+        PyObject* t = PyTuple_New((Py_ssize_t)r.size());
+        if (t == nullptr) throw py::error_already_set();
+        PyTuple_SET_ITEM(t, 0, give(r[0], from, "norm.rms_norm_quantize"));
+        PyTuple_SET_ITEM(t, 1, give(r[1]));
+        if (r.size() > 2) PyTuple_SET_ITEM(t, 2, give(r[2], from, "norm.rms_norm_quantize"));
+        return t;
+    });
+}
+MOR_CALL(py_codes_values)
+{
+    return guarded([&] {
+        MOR_ARGS("dequantize", 2, 3, "codes", "scales", "dtype");
+        const Tensor &codes = a.tensor(0), &scales = a.tensor(1);
+        return give(codes_values(codes, scales, a.dtype(2, at::kBFloat16)), {codes, scales}, "norm.dequantize");
+    });
+}
+MOR_CALL(py_adapter_add)
+{
+    return guarded([&] {
+        MOR_ARGS("add", 4, 6, "base", "x", "a", "b", "ids", "scale");
+        const bool tensor = a.is_tensor(5);
+        return give(adapter_add(a.tensor(0), a.tensor(1), a.tensor(2), a.tensor(3), a.maybe_tensor(4), tensor ? a.maybe_tensor(5) : std::nullopt, tensor ? 1.0 : a.number(5, 1.0)));
+    });
+}
+MOR_CALL(py_adapter_linear)
+{
+    return guarded([&] {
+        MOR_ARGS("linear", 4, 6, "x", "w", "a", "b", "ids", "scale", "w_t");
+        const bool tensor = a.is_tensor(5);
+        return give(adapter_linear(a.tensor(0), a.operand(1), a.tensor(2), a.tensor(3), a.maybe_tensor(4), tensor ? a.maybe_tensor(5) : std::nullopt, tensor ? 1.0 : a.number(5, 1.0),
+                                   a[6] == nullptr ? nullptr : &a.operand(6)));
+    });
+}
+MOR_CALL(py_adamw)
+{
+    return guarded([&] {
+        MOR_ARGS("adamw_", 4, 5, "params", "grads", "exp_avgs", "exp_avg_sqs", "scales", "step", "lr", "beta1", "beta2", "eps", "weight_decay", "seed", "grad_scale", "found_inf");
+        const AdamwLists lists = {a.tensors(0), a.tensors(1), a.tensors(2), a.tensors(3), a.tensors(4)};
+        mor_adamw_desc_t d = {};
+        if (a.is_tensor(5)) {
+            const Tensor& step = a.tensor(5);
+            on_gpu(step, "step");
+            want(step.scalar_type() == at::kInt && step.numel() == 1, "step: a number, or one int32 on the GPU, is wanted");
+            d.device_step = ptr<int32_t>(step);
+        } else {
+            want(a[5] != nullptr, "step: the number of this step, from 1, is wanted");
+            d.step = a.integer(5, 0);
+            want(d.step >= 1, "step: the number of this step, from 1, is wanted");
+        }
+        if (a.is_tensor(6)) d.device_lr = one_float(a.tensor(6), "lr");
+        else d.lr = a.number(6, 1e-3);
+        d.beta1 = a.number(7, 0.9);
+        d.beta2 = a.number(8, 0.999);
+        d.eps = a.number(9, 1e-8);
+        d.weight_decay = a.number(10, 0.0);
+        if (a[11] != nullptr) {
+            d.seed = PyLong_AsUnsignedLongLongMask(a[11]);
+            if (PyErr_Occurred()) throw py::error_already_set();
+        }
+        const std::optional<Tensor> scale = a.maybe_tensor(12), inf = a.maybe_tensor(13);
+        d.grad_scale = one_float(scale, "grad_scale");
+        d.found_inf = one_float(inf, "found_inf");
+        adamw(lists, d);
+        return give_none();
+    });
+}
+MOR_CALL(py_adamw_moments)
+{
+    return guarded([&] {
+        MOR_ARGS("moments", 3, 4, "exp_avg", "exp_avg_sq", "scales", "dtype");
+        const std::pair<Tensor, Tensor> r = adamw_moments(a.tensor(0), a.tensor(1), a.tensor(2), a.dtype(3, at::kFloat));
+        return give(give(r.first), give(r.second));
+    });
+}
 PyObject* new_operand(PyObject*, PyObject* const* args, size_t n, PyObject* kwnames)
 {
     return guarded([&] {
@@ -748,6 +875,9 @@ PyMethodDef methods[] = {MOR_METHOD("quantize", py_quantize), MOR_METHOD("dequan
                          MOR_METHOD("matmul_rows", py_matmul_rows), MOR_METHOD("matmul_reduce", py_matmul_reduce), MOR_METHOD("linear", py_linear),
                          MOR_METHOD("status_word", py_status_word), MOR_METHOD("sort", py_sort), MOR_METHOD("gather", py_gather),
                          MOR_METHOD("combine", py_combine), MOR_METHOD("combine_grad", py_combine_grad), MOR_METHOD("expert_linear", py_expert_linear),
+                         MOR_METHOD("rms_norm", py_rms_norm), MOR_METHOD("rms_norm_quantize", py_rms_norm_quantize), MOR_METHOD("codes_values", py_codes_values),
+                         MOR_METHOD("adapter_add", py_adapter_add), MOR_METHOD("adapter_linear", py_adapter_linear), MOR_METHOD("adamw_", py_adamw),
+                         MOR_METHOD("adamw_moments", py_adamw_moments),
                          {nullptr, nullptr, 0, nullptr}};
 
 }  // namespace

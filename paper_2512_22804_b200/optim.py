@@ -1,0 +1,92 @@
+"""AdamW over many tensors at once on torch CUDA tensors, with moments in 8 bits or in 32.
+
+    optimizer = optim.AdamW(model.parameters(), lr=1e-4, bits=8)
+    loss.backward(); optimizer.step(); optimizer.zero_grad()
+
+``AdamW(params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, *, bits=8, seed=0, capturable=False)``
+    a torch optimizer; the decay is apart from the gradient.  Parameters are BF16 or FP32, gradients either.  bits: of the moments.  With 8 a block of 128
+    elements keeps E4M3 codes of the first moment and of the second's root and a power-of-two scale for each (2.02 bytes an element instead of 8).  Codes, and
+    BF16 parameters, are rounded up or down at random so that what a step changes by less than half a distance of codes is not lost: ``seed``, the
+    step's number and the element's place give the random numbers, so a run can be repeated.  ``step(grad_scale=None, found_inf=None)``: FP32 tensors of
+    one value; the first multiplies every gradient, and where the second is not zero nothing is changed (the step still counts).  With capturable the steps of a
+    group are counted on the GPU and lr may be a tensor there, so that a captured step can be replayed.
+``adamw_(params, grads, exp_avgs, exp_avg_sqs, scales=None, *, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, seed=0, grad_scale=None,
+found_inf=None)``
+    one step over lists of contiguous tensors, changed in place; all parameters of one type, and all gradients.  The moments are FP32, or float8_e4m3fn with
+    scales uint8 [blocks of 128, 2].  step: its number, from 1, or one int32 on the GPU; lr: a number, or one FP32 on the GPU.
+``moments(exp_avg, exp_avg_sq, scales, dtype=torch.float32)``
+    the values of 8-bit moments.
+
+The formulas are those of ``include/mor.h``.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import fp4  # noqa: F401  (raises if the operators have not been built)
+from ._ops import adamw_
+from ._ops import adamw_moments as moments
+
+__all__ = ["AdamW", "adamw_", "moments"]
+
+
+class AdamW(torch.optim.Optimizer):
+    def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, *, bits=8, seed=0, capturable=False):
+        if bits not in (8, 32):
+            raise ValueError("bits: 8 or 32 is wanted")
+        if not all(0.0 <= b < 1.0 for b in betas):
+            raise ValueError("betas: from 0 to below 1 are wanted")
+        if not isinstance(lr, torch.Tensor) and not lr >= 0.0 or not eps >= 0.0 or not weight_decay >= 0.0:
+            raise ValueError("lr, eps and weight_decay may not be negative")
+        if isinstance(lr, torch.Tensor) and not capturable:
+            raise ValueError("lr may be a tensor with capturable")
+        super().__init__(params, dict(lr=lr, betas=tuple(betas), eps=eps, weight_decay=weight_decay, bits=bits, seed=seed, capturable=capturable, step=None))
+
+    def _new_state(self, p, bits):
+        if bits == 32:
+            return {"exp_avg": torch.zeros_like(p, dtype=torch.float32), "exp_avg_sq": torch.zeros_like(p, dtype=torch.float32)}
+        code = dict(dtype=torch.float8_e4m3fn, device=p.device)
+        return {"exp_avg": torch.zeros(p.shape, **code), "exp_avg_sq": torch.zeros(p.shape, **code),
+                "scales": torch.full(((p.numel() + 127) // 128, 2), 127, dtype=torch.uint8, device=p.device)}
+
+    def load_state_dict(self, state_dict):
+        """As torch's, but the moments keep the types they were stored in (torch's brings them to the parameter's)."""
+        super().load_state_dict(state_dict)
+        stored, ids = state_dict["state"], [i for g in state_dict["param_groups"] for i in g["params"]]
+        for i, p in zip(ids, (p for g in self.param_groups for p in g["params"])):
+            if i in stored:
+                self.state[p] = {k: v.clone().to(p.device) if isinstance(v, torch.Tensor) else v for k, v in stored[i].items()}
+
+    @torch.no_grad()
+    def step(self, closure=None, *, grad_scale=None, found_inf=None):
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        for group in self.param_groups:
+            calls, capturable = {}, group["capturable"]
+            for p in group["params"]:
+                if p.grad is None:
+                    continue
+                if p.grad.is_sparse:
+                    raise RuntimeError("sparse gradients are not supported")
+                state = self.state[p]
+                if not state:
+                    state.update(self._new_state(p, group["bits"]))
+                    state["step"] = 0
+                if capturable:
+                    if group["step"] is None:
+                        group["step"] = torch.zeros((), dtype=torch.int32, device=p.device)
+                else:
+                    state["step"] += 1
+                calls.setdefault((p.device, p.dtype, p.grad.dtype, 0 if capturable else state["step"]), []).append((p, p.grad.contiguous(), state))
+            if capturable and calls:
+                group["step"].add_(1)
+            for (device, _, _, step), items in calls.items():
+                with torch.cuda.device(device):
+                    step = group["step"] if capturable else step
+                    adamw_([i[0] for i in items], [i[1] for i in items], [i[2]["exp_avg"] for i in items], [i[2]["exp_avg_sq"] for i in items],
+                           [i[2]["scales"] for i in items] if group["bits"] == 8 else None, step=step, lr=group["lr"], beta1=group["betas"][0],
+                           beta2=group["betas"][1], eps=group["eps"], weight_decay=group["weight_decay"], seed=group["seed"], grad_scale=grad_scale,
+                           found_inf=found_inf)
+        return loss
