@@ -9,6 +9,8 @@ Low level (one-to-one with ``include/mor.h``):
     mor_analyze_quantize_batched_ex, mor_select_stats, mor_select_stats_batched, mor_group_amax, mor_host_staging_bytes, mor_analyze_quantize_host,
     mor_fp4_scale_bytes, mor_fp4_quantize, mor_fp4_dequantize, mor_fp4_matmul, mor_expert_rows, mor_expert_workspace_bytes,
     mor_expert_sort, mor_expert_gather, mor_expert_combine, mor_expert_combine_grad (used through ``fp4`` and ``experts``),
+    mor_rms_norm, mor_rms_norm_grad_workspace_bytes, mor_rms_norm_grad, mor_codes_dequantize, mor_adapter_workspace_bytes, mor_adapter_add,
+    mor_adapter_grad_workspace_bytes, mor_adapter_grad, mor_adamw, mor_adamw_moments (used through ``norm``, ``adapters`` and ``optim``),
     mor_status_string, mor_version
 
 Helpers that allocate outputs with torch and fill the descriptors:
@@ -103,6 +105,31 @@ class mor_expert_desc_t(C.Structure):
                 ("row_of_slot", C.c_void_p), ("slot_of_row", C.c_void_p), ("weight", C.c_void_p), ("weight_dtype", C.c_int32), ("ys_dtype", C.c_int32)]
 
 
+class mor_norm_desc_t(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("x", C.c_void_p), ("residual", C.c_void_p), ("weight", C.c_void_p),
+                ("ldx", C.c_int64), ("ldr", C.c_int64), ("eps", C.c_float), ("dtype", C.c_int32), ("residual_dtype", C.c_int32), ("weight_dtype", C.c_int32)]
+
+
+class mor_norm_outputs_t(C.Structure):
+    _fields_ = [("h", C.c_void_p), ("y", C.c_void_p), ("codes", C.c_void_p), ("scale_e8m0", C.c_void_p), ("scale_f32", C.c_void_p),
+                ("ldh", C.c_int64), ("ldy", C.c_int64), ("ldc", C.c_int64), ("block", C.c_int32)]
+
+
+class mor_adapter_desc_t(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("n_in", C.c_int64), ("n_out", C.c_int64), ("adapters", C.c_int32), ("rank", C.c_int32),
+                ("a", C.c_void_p), ("b", C.c_void_p), ("ids", C.c_void_p), ("scale", C.c_void_p), ("factor", C.c_float)]
+
+
+class mor_adamw_tensor_t(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("exp_avg", C.c_void_p), ("exp_avg_sq", C.c_void_p), ("scales", C.c_void_p), ("numel", C.c_int64)]
+
+
+class mor_adamw_desc_t(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double), ("step", C.c_int64),
+                ("device_step", C.c_void_p), ("device_lr", C.c_void_p), ("grad_scale", C.c_void_p), ("found_inf", C.c_void_p), ("seed", C.c_uint64),
+                ("param_dtype", C.c_int32), ("grad_dtype", C.c_int32), ("eight_bits", C.c_int32)]
+
+
 BLOCK_STATS_DTYPE = np.dtype([("amax", "f4"), ("min_abs_nz", "f4"), ("nnz", "u4"), ("n_nonfinite", "u4"),
                               ("sum_rel_e4m3", "f4"), ("sum_rel_e5m2", "f4")])
 TENSOR_STATS_DTYPE = np.dtype([("sum_rel_e4m3", "f8"), ("nnz", "u8"), ("mean_rel_e4m3", "f8"),
@@ -165,6 +192,22 @@ def load():
         L.mor_expert_gather.restype = L.mor_expert_combine.restype = L.mor_expert_combine_grad.restype = i32
         L.mor_expert_gather.argtypes = L.mor_expert_combine.argtypes = [pe, vp, i64, vp, i64, vp]
         L.mor_expert_combine_grad.argtypes = [pe, vp, i64, vp, i64, vp, i64, vp, vp]
+        pn, pa = C.POINTER(mor_norm_desc_t), C.POINTER(mor_adapter_desc_t)
+        L.mor_rms_norm.restype = L.mor_rms_norm_grad.restype = L.mor_codes_dequantize.restype = i32
+        L.mor_rms_norm.argtypes = [pn, C.POINTER(mor_norm_outputs_t), vp]
+        L.mor_rms_norm_grad_workspace_bytes.restype = C.c_size_t
+        L.mor_rms_norm_grad_workspace_bytes.argtypes = [i64, i64]
+        L.mor_rms_norm_grad.argtypes = [pn, i32, vp, i64, vp, i64, vp, i64, vp, vp, C.c_size_t, vp]
+        L.mor_codes_dequantize.argtypes = [vp, i64, i64, i64, i32, vp, vp, vp, i32, i64, vp]
+        L.mor_adapter_workspace_bytes.restype = L.mor_adapter_grad_workspace_bytes.restype = C.c_size_t
+        L.mor_adapter_workspace_bytes.argtypes = [pa, i32]
+        L.mor_adapter_grad_workspace_bytes.argtypes = [pa]
+        L.mor_adapter_add.restype = L.mor_adapter_grad.restype = i32
+        L.mor_adapter_add.argtypes = [pa, vp, i64, vp, i64, vp, i64, i32, i32, vp, C.c_size_t, vp]
+        L.mor_adapter_grad.argtypes = [pa, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, C.c_size_t, vp, C.c_size_t, vp]
+        L.mor_adamw.restype = L.mor_adamw_moments.restype = i32
+        L.mor_adamw.argtypes = [C.POINTER(mor_adamw_desc_t), C.POINTER(mor_adamw_tensor_t), i32, vp]
+        L.mor_adamw_moments.argtypes = [vp, vp, vp, i64, vp, vp, i32, vp]
         L.mor_status_string.restype = C.c_char_p
         L.mor_status_string.argtypes = [C.c_int]
         L.mor_version.restype = C.c_int
@@ -178,7 +221,9 @@ EXPORTS = ["mor_workspace_bytes", "mor_analyze_quantize", "mor_analyze_quantize_
            "mor_group_amax", "mor_host_staging_bytes", "mor_analyze_quantize_host",
            "mor_analyze_quantize_static", "mor_fp4_scale_bytes", "mor_fp4_quantize", "mor_fp4_dequantize", "mor_fp4_matmul",
            "mor_expert_rows", "mor_expert_workspace_bytes", "mor_expert_sort", "mor_expert_gather", "mor_expert_combine",
-           "mor_expert_combine_grad", "mor_status_string", "mor_version"]
+           "mor_expert_combine_grad", "mor_rms_norm", "mor_rms_norm_grad_workspace_bytes", "mor_rms_norm_grad", "mor_codes_dequantize",
+           "mor_adapter_workspace_bytes", "mor_adapter_add", "mor_adapter_grad_workspace_bytes", "mor_adapter_grad", "mor_adamw",
+           "mor_adamw_moments", "mor_status_string", "mor_version"]
 
 
 # ------------------------------------------------------------------ C entry points ----

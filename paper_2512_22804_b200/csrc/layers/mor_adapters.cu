@@ -888,8 +888,8 @@ mor_status_t mor_adapter_add(const mor_adapter_desc_t* d, const void* x, int64_t
     out_whole = access_bytes(out, d->tokens > 1 ? ldo * (int64_t)dtype_bytes(dtype) : 0, 0, 1) >= 16;
     const bool a_whole = d->n_in % 8 == 0 && is_aligned(d->a, 16), any = !(x_whole && a_whole);
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (d->tokens == 0) return MOR_OK;
     if (small_call(*d, train != 0)) {
-        if (d->tokens == 0) return MOR_OK;
         SmallParams p = {static_cast<const bf16*>(x), static_cast<const bf16*>(d->a), static_cast<const bf16*>(d->b), d->ids, d->scale, d->factor, d->adapters, d->rank,
                          (int32_t)d->tokens, ldx, d->n_in, d->n_out, base, out, ldb, ldo, rank_whole(d->b, d->rank), base_whole, out_whole};
         const dim3 grid((uint32_t)(d->ids != nullptr ? d->tokens : ceil_div(d->tokens, kSmallRows)) * kMaxCluster);
@@ -910,7 +910,6 @@ mor_status_t mor_adapter_add(const mor_adapter_desc_t* d, const void* x, int64_t
                              const_cast<int32_t*>(f.s.token_of_row), f.sort, f.sort_bytes, cuda_stream);
         if (st != MOR_OK) return st;
     }
-    if (d->tokens == 0) return MOR_OK;
     const int padded = padded_rank(d->rank);
     ShrinkParams sp = {f.s, static_cast<const bf16*>(x), static_cast<const bf16*>(d->a), d->scale, d->factor, ldx, d->n_in, d->n_in, (int64_t)d->rank * d->n_in, d->rank, padded,
                        f.natural, f.turned};
