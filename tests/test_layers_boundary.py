@@ -111,7 +111,7 @@ def test_adapters_refuse(lib):
     need = lib.mor_adapter_workspace_bytes(C.byref(d), 0)
     assert need > 0 and add(lib, d, ws=None) == WORKSPACE and add(lib, d, n=need - 1) == WORKSPACE and add(lib, d, ws=0x100010) == ALIGN
     train = lib.mor_adapter_workspace_bytes(C.byref(d), 1)
-    assert train > need and add(lib, d, train=1, n=train - 1) == WORKSPACE
+    assert train >= need and add(lib, d, train=1, n=train - 1) == WORKSPACE
     few = adapter(tokens=8)
     assert lib.mor_adapter_workspace_bytes(C.byref(few), 0) == 0 and lib.mor_adapter_workspace_bytes(C.byref(few), 1) > 0
     assert lib.mor_adapter_workspace_bytes(C.byref(adapter(tokens=8, rank=65)), 0) > 0
