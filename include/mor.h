@@ -466,6 +466,7 @@ typedef struct mor_adapter_desc {
     const int32_t* ids;          /* DEVICE [tokens]; NULL = every token has adapter 0            */
     const float* scale;          /* DEVICE [adapters], optional (1)                              */
     float factor;                /* f                                                            */
+    uint32_t* status;            /* DEVICE, optional: set to MOR_ERR_TIMEOUT when a bounded wait ran out (never cleared)   */
 } mor_adapter_desc_t;
 #define MOR_MAX_RANK 512
 

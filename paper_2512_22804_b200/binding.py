@@ -117,7 +117,7 @@ class mor_norm_outputs_t(C.Structure):
 
 class mor_adapter_desc_t(C.Structure):
     _fields_ = [("tokens", C.c_int64), ("n_in", C.c_int64), ("n_out", C.c_int64), ("adapters", C.c_int32), ("rank", C.c_int32),
-                ("a", C.c_void_p), ("b", C.c_void_p), ("ids", C.c_void_p), ("scale", C.c_void_p), ("factor", C.c_float)]
+                ("a", C.c_void_p), ("b", C.c_void_p), ("ids", C.c_void_p), ("scale", C.c_void_p), ("factor", C.c_float), ("status", C.c_void_p)]
 
 
 class mor_adamw_tensor_t(C.Structure):

@@ -5,6 +5,9 @@
 // (rows lie wherever the tokens of an adapter are, so the copies are a thread's own and not a tensor map's), fragments from there to the registers of the
 // tensor instructions (mma.sync, BF16 in, FP32 sums).
 //
+// Tiles of 128 rows (and every `outer`) go through the fifth-generation tensor cores, whose operands stay in shared memory and whose sums are in tensor
+// memory: by mma.sync the products of 64 ranks took longer than the memory does.  Where an adapter has few rows, tiles of 32 by mma.sync leave less empty.
+//
 //   shrink   h = s x a^T              reduction over the width, cut over a cluster's CTAs and joined through distributed shared memory
 //   expand   out = base + h b^T       h as the sum of two BF16 (16 bits and more), in registers while the columns pass
 //   outer    db = dy^T h, da = u^T x  reduction over an adapter's tokens, cut and joined like shrink
@@ -12,6 +15,7 @@
 //
 // More tokens are sorted by adapter first; each adapter's rows start at a multiple of a tile.  All sums run in an order that depends on the sizes and
 // ids alone.
+#include "../fp4/mor_tcgen05.cuh"
 #include "mor_layers.cuh"
 
 namespace mor {
@@ -31,12 +35,6 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t a0, const uint
 {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t cluster_rank()
-{
-    uint32_t r;
-    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
 }
 __device__ __forceinline__ uint32_t cluster_size()
 {
@@ -135,10 +133,6 @@ __device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t at)
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
 }
-__device__ __forceinline__ void load_matrices_turned(uint32_t (&r)[4], uint32_t at)
-{
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
-}
 __device__ __forceinline__ uint32_t shared_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ float4 load_remote4(uint32_t own, uint32_t rank)
 {
@@ -163,6 +157,89 @@ __device__ __forceinline__ float4 sum_remote4(uint32_t own, uint32_t ctas)
     return v[0];
 }
 
+// ---- the fifth-generation tensor cores, BF16
+
+constexpr long long kWaitCycles = 400000000;      // a wait that takes longer is given up: something is wrong
+
+// Rows of ROW_BYTES laid down by chunk_at<ROW_BYTES>(), the reduction axis along the rows (K) or across them.  Groups of 8 rows are one after the
+// other; `next`: bytes between pieces of 64 columns (operands whose rows are the reduction axis and that are wider than that).
+template <int ROW_BYTES> __device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t next = 16)
+{
+    constexpr uint64_t kSwizzle = ROW_BYTES == 128 ? 2 : ROW_BYTES == 64 ? 4 : 6;
+    return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)(next >> 4) << 16) | ((uint64_t)(ROW_BYTES * 8 >> 4) << 32) | (1ull << 46) | (kSwizzle << 61);
+}
+// BF16 x BF16 into FP32, 128 x n; across: the reduction axis runs across both operands' rows.
+__host__ __device__ constexpr uint32_t product(int n, bool across) { return (1u << 4) | (1u << 7) | (1u << 10) | (across ? 3u << 15 : 0u) | ((uint32_t)(n >> 3) << 17) | (8u << 24); }
+__device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate)
+{
+    const uint32_t acc = accumulate;
+    asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+// Lanes 16 i .. 16 i + 15 of a warp's and 32 columns, as the results of mma.sync lie: r[4 j + k] is row lane / 4 + 8 (k / 2), column 8 j + 2 (lane % 4) + k % 2.
+__device__ __forceinline__ void tmem_load_frags(float (&r)[4][4], uint32_t addr)
+{
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=f"(r[0][0]), "=f"(r[0][1]), "=f"(r[0][2]), "=f"(r[0][3]), "=f"(r[1][0]), "=f"(r[1][1]), "=f"(r[1][2]), "=f"(r[1][3]), "=f"(r[2][0]), "=f"(r[2][1]), "=f"(r[2][2]),
+                   "=f"(r[2][3]), "=f"(r[3][0]), "=f"(r[3][1]), "=f"(r[3][2]), "=f"(r[3][3])
+                 : "r"(addr));
+}
+struct Products {
+    uint64_t done[4];          // a stage's (or an accumulator set's) products are through
+    uint32_t tmem;
+};
+// Before wait_for_predecessor(), which lets the next kernel start: that one may then take what is left of tensor memory, but nothing that this one still needs.
+__device__ __forceinline__ void products_begin(Products& c, uint32_t columns)
+{
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 4; ++i) mbar_init(&c.done[i], 1);
+        fence_mbar_init();
+    }
+    if (threadIdx.x < 32) tmem_alloc<1>(&c.tmem, columns);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+}
+__device__ __forceinline__ void products_end(const Products& c, uint32_t columns)
+{
+    tc_fence_before();
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        tc_fence_after();
+        tmem_free<1>(c.tmem, columns);
+    }
+}
+// For all threads: the products that were the n-th to be committed to this barrier (from 0) are through.
+__device__ __forceinline__ void products_wait(Products& c, int which, uint32_t n, uint32_t* status, bool& given_up)
+{
+    if (given_up) return;
+    if (!mbar_wait(&c.done[which], n & 1u, nullptr, kWaitCycles)) {
+        given_up = true;
+        if (status != nullptr) *status = MOR_ERR_TIMEOUT;
+    }
+}
+
+// Joins the rows' sums over the cluster's CTAs and stores them as pairs of BF16.  part: [rows][R + 4], of this CTA.
+template <int R> __device__ __forceinline__ void join_rows(float* part, int rows, int64_t first, int r0, float scale, bf16* h, int padded, uint32_t rank, uint32_t ctas)
+{
+    constexpr int kPitch = R + 4;
+    cluster_arrive();
+    cluster_wait();
+    rows /= (int)ctas;                                                            // of each CTA: 1, 2, 4 or 8 divide the tile
+    for (int at = threadIdx.x; at < rows * (R / 4); at += 128) {
+        const int row = (int)rank * rows + at / (R / 4), col = at % (R / 4) * 4;
+        const float4 v = sum_remote4(shared_at(part + row * kPitch + col), ctas);
+        const float f[4] = {v.x * scale, v.y * scale, v.z * scale, v.w * scale};
+        bf16 hi[4], lo[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) split(f[k], hi[k], lo[k]);
+        uint16_t* to = reinterpret_cast<uint16_t*>(h) + (first + row) * 2 * padded + r0 + col;
+        *reinterpret_cast<ushort4*>(to) = make_ushort4(bits_of(hi[0]), bits_of(hi[1]), bits_of(hi[2]), bits_of(hi[3]));
+        *reinterpret_cast<ushort4*>(to + padded) = make_ushort4(bits_of(lo[0]), bits_of(lo[1]), bits_of(lo[2]), bits_of(lo[3]));
+    }
+    cluster_arrive();                    // nobody leaves while its sums are read
+    cluster_wait();
+}
+
 // ------------------------------------------------------------------------------------------- shrink ----
 
 struct ShrinkParams {
@@ -175,51 +252,121 @@ struct ShrinkParams {
     int32_t m_rows;            // rows of m that exist
     int32_t padded;            // rank as the output has it
     bf16* h;                   // [rows][2][padded]
+    uint32_t* status;
 };
 
-// A CTA of 4 warps takes ROWS rows of one adapter (a warp 32 of them, or of 32 rows a quarter of each step's 64 elements) and R of the ranks (blockIdx.y);
-// a cluster's CTAs share the reduction axis.
 constexpr int kShrinkStages = 4;
-template <int R, int ROWS> constexpr int kShrinkSmem = kShrinkStages * (ROWS + R) * 128;
+template <int R, int ROWS> constexpr int kShrinkSmem = kShrinkStages * (ROWS + R) * 128 + 1024;
 
-template <int R, int ROWS, bool ANY> __global__ void __launch_bounds__(128) adapter_shrink_kernel(const __grid_constant__ ShrinkParams p)
+// The copies of a CTA of 128 threads: steps of 64 elements of ROWS rows of x and R of m; a thread's are chunk tid % 8 of every 16th row.
+template <int R, int ROWS, bool ANY> struct ShrinkCopies {
+    static constexpr int kStage = (ROWS + R) * 128;
+    const bf16 *xr[ROWS / 16], *mr[R / 16], *valid;
+    int64_t n;
+    int32_t begin, end;
+    uint32_t ring;
+    __device__ __forceinline__ ShrinkCopies(const ShrinkParams& p, int64_t first, int r0, int adapter, uint32_t rank, uint32_t ctas, uint32_t smem) : valid(p.x), n(p.n), ring(smem)
+    {
+        const int tid = threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < ROWS / 16; ++i) {
+            const int32_t t = token_at(p.s, first + i * 16 + (tid >> 3));
+            xr[i] = t >= 0 ? p.x + (int64_t)t * p.ldx : nullptr;
+        }
+#pragma unroll
+        for (int i = 0; i < R / 16; ++i) {
+            const int r = r0 + i * 16 + (tid >> 3);
+            mr[i] = r < p.m_rows ? p.m + (int64_t)adapter * p.m_stride + (int64_t)r * p.ldm : nullptr;
+        }
+        const int32_t steps = (int32_t)((p.n + 63) / 64), share = (steps + (int32_t)ctas - 1) / (int32_t)ctas;
+        begin = min((int32_t)rank * share, steps);
+        end = min(begin + share, steps);
+    }
+    __device__ __forceinline__ uint32_t stage(int32_t step) const { return ring + (uint32_t)((step - begin) % kShrinkStages) * kStage; }
+    __device__ __forceinline__ void fill(int32_t step) const
+    {
+        if (step < end) {
+            const int tid = threadIdx.x;
+            const uint32_t to = stage(step);
+            const int64_t at = (int64_t)step * 64 + (tid & 7) * 8;
+#pragma unroll
+            for (int i = 0; i < ROWS / 16; ++i) fill_chunk<bf16, ANY>(to + chunk_at<128>(i * 16 + (tid >> 3), tid & 7), xr[i], at, n, valid);
+#pragma unroll
+            for (int i = 0; i < R / 16; ++i) fill_chunk<bf16, ANY>(to + ROWS * 128 + chunk_at<128>(i * 16 + (tid >> 3), tid & 7), mr[i], at, n, valid);
+        }
+        copies_commit();
+    }
+};
+
+// A CTA takes 128 rows of one adapter and all ranks; a cluster's CTAs share the reduction axis.
+template <int R, bool ANY> __global__ void __launch_bounds__(128) adapter_shrink_kernel(const __grid_constant__ ShrinkParams p)
 {
-    constexpr int kStage = (ROWS + R) * 128, kTiles = R / 8, kParts = ROWS == kRows ? 4 : 1, kPitch = R + 4;
-    static_assert(kParts * ROWS * kPitch * 4 <= kShrinkSmem<R, ROWS>, "the sums take the ring's place");
-    extern __shared__ __align__(128) uint8_t ring[];
+    constexpr int kColumns = R < 32 ? 32 : R;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ Products c;
+    products_begin(c, kColumns);
     wait_for_predecessor();
-    const uint32_t rank = cluster_rank(), ctas = cluster_size();
-    const int64_t first = (int64_t)(blockIdx.x / ctas) * ROWS;
+    const uint32_t rank = cluster_rank(), ctas = cluster_size(), smem = (shared_at(smem_raw) + 1023u) & ~1023u;
+    const int64_t first = (int64_t)(blockIdx.x / ctas) * 128;
+    if (first >= used_rows(p.s)) {                                                // the whole cluster
+        products_end(c, kColumns);
+        return;
+    }
+    const int warp = warp_number(), lane = threadIdx.x & 31;
+    const int adapter = adapter_of(p.s, first, lane);
+    const ShrinkCopies<R, 128, ANY> copies(p, first, 0, adapter, rank, ctas, smem);
+    bool given_up = false;
+#pragma unroll
+    for (int s = 0; s < kShrinkStages - 1; ++s) copies.fill(copies.begin + s);
+    for (int32_t step = copies.begin; step < copies.end; ++step) {
+        const int32_t n = step - copies.begin;
+        copies_wait<kShrinkStages - 2>();
+        fence_async_smem();
+        __syncthreads();
+        if (warp == 0 && elect_one()) {
+            const uint64_t x = operand<128>(copies.stage(step)), m = operand<128>(copies.stage(step) + 128 * 128);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mma_bf16(c.tmem, x + 2 * k, m + 2 * k, product(R, false), n > 0 || k > 0);
+            tc_commit<1>(shared_at(&c.done[n % kShrinkStages]));
+        }
+        // the next step's tile goes where the last one's products read from
+        if (n > 0) products_wait(c, (n - 1) % kShrinkStages, (uint32_t)((n - 1) / kShrinkStages), p.status, given_up);
+        copies.fill(step + kShrinkStages - 1);
+    }
+    const int32_t count = copies.end - copies.begin;
+    if (count > 0) products_wait(c, (count - 1) % kShrinkStages, (uint32_t)((count - 1) / kShrinkStages), p.status, given_up);
+    copies_wait<0>();
+    tc_fence_after();
+    __syncthreads();
+    float* part = reinterpret_cast<float*>(smem_raw + (smem - shared_at(smem_raw)));              // [128][R + 4]
+    const uint32_t lanes = c.tmem + ((uint32_t)warp << 21);
+#pragma unroll
+    for (int r = 0; r < R; r += 16) {
+        uint32_t v[16] = {};
+        if (count > 0) {
+            tmem_load16(v, lanes + r);
+            tc_wait_ld();
+        }
+#pragma unroll
+        for (int k = 0; k < 16; k += 4) *reinterpret_cast<uint4*>(part + (warp * 32 + lane) * (R + 4) + r + k) = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+    }
+    products_end(c, kColumns);
+    join_rows<R>(part, 128, first, 0, (p.scale != nullptr ? p.scale[adapter] : 1.f) * p.factor, p.h, p.padded, rank, ctas);
+}
+
+// A CTA takes 32 rows of one adapter and R of the ranks (blockIdx.y); a warp works on a quarter of each step.
+template <int R, bool ANY> __global__ void __launch_bounds__(128) adapter_shrink32_kernel(const __grid_constant__ ShrinkParams p)
+{
+    constexpr int kTiles = R / 8, kPitch = R + 4;
+    static_assert(4 * kRows * kPitch * 4 <= kShrinkSmem<R, kRows> - 1024, "the sums take the ring's place");
+    extern __shared__ uint8_t smem_raw[];
+    wait_for_predecessor();
+    const uint32_t rank = cluster_rank(), ctas = cluster_size(), smem = (shared_at(smem_raw) + 1023u) & ~1023u;
+    const int64_t first = (int64_t)(blockIdx.x / ctas) * kRows;
     if (first >= used_rows(p.s)) return;                                          // the whole cluster
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q = lane & 3;
     const int r0 = blockIdx.y * R, adapter = adapter_of(p.s, first, lane);
-    const float scale = (p.scale != nullptr ? p.scale[adapter] : 1.f) * p.factor;
-    const uint32_t smem = shared_at(ring);
-    // what this thread copies: chunk tid % 8 of every 16th row
-    const bf16* xr[ROWS / 16];
-    const bf16* mr[R / 16];
-#pragma unroll
-    for (int i = 0; i < ROWS / 16; ++i) {
-        const int32_t t = token_at(p.s, first + i * 16 + (tid >> 3));
-        xr[i] = t >= 0 ? p.x + (int64_t)t * p.ldx : nullptr;
-    }
-#pragma unroll
-    for (int i = 0; i < R / 16; ++i) {
-        const int r = r0 + i * 16 + (tid >> 3);
-        mr[i] = r < p.m_rows ? p.m + (int64_t)adapter * p.m_stride + (int64_t)r * p.ldm : nullptr;
-    }
-    const int64_t steps = (p.n + 63) / 64, share = (steps + ctas - 1) / ctas, begin = min((int64_t)rank * share, steps), end = min(begin + share, steps);
-    auto fill = [&](int64_t step) {
-        if (step < end) {
-            const uint32_t stage = smem + (uint32_t)((step - begin) % kShrinkStages) * kStage;
-            const int64_t at = step * 64 + (tid & 7) * 8;
-#pragma unroll
-            for (int i = 0; i < ROWS / 16; ++i) fill_chunk<bf16, ANY>(stage + chunk_at<128>(i * 16 + (tid >> 3), tid & 7), xr[i], at, p.n, p.x);
-#pragma unroll
-            for (int i = 0; i < R / 16; ++i) fill_chunk<bf16, ANY>(stage + ROWS * 128 + chunk_at<128>(i * 16 + (tid >> 3), tid & 7), mr[i], at, p.n, p.x);
-        }
-        copies_commit();
-    };
+    const ShrinkCopies<R, kRows, ANY> copies(p, first, r0, adapter, rank, ctas, smem);
     float acc[2][kTiles][4];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -228,53 +375,31 @@ template <int R, int ROWS, bool ANY> __global__ void __launch_bounds__(128) adap
 #pragma unroll
             for (int k = 0; k < 4; ++k) acc[i][j][k] = 0.f;
 #pragma unroll
-    for (int s = 0; s < kShrinkStages - 1; ++s) fill(begin + s);
-    const int a_row = (ROWS == kRows ? 0 : warp * kRows) + (lane & 15);
-    for (int64_t step = begin; step < end; ++step) {
+    for (int s = 0; s < kShrinkStages - 1; ++s) copies.fill(copies.begin + s);
+    for (int32_t step = copies.begin; step < copies.end; ++step) {
         copies_wait<kShrinkStages - 2>();
         __syncthreads();
-        fill(step + kShrinkStages - 1);
-        const uint32_t stage = smem + (uint32_t)((step - begin) % kShrinkStages) * kStage, ms = stage + ROWS * 128;
-        if constexpr (ROWS == kRows) {
-            uint32_t a[2][4];
+        copies.fill(step + kShrinkStages - 1);
+        const uint32_t xs = copies.stage(step), ms = xs + kRows * 128;
+        uint32_t a[2][4];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) load_matrices(a[i], stage + chunk_at<128>(i * 16 + a_row, warp * 2 + (lane >> 4)));
+        for (int i = 0; i < 2; ++i) load_matrices(a[i], xs + chunk_at<128>(i * 16 + (lane & 15), warp * 2 + (lane >> 4)));
 #pragma unroll
-            for (int j = 0; j < kTiles; j += 2) {
-                uint32_t b[4];
-                load_matrices(b, ms + chunk_at<128>(j * 8 + (lane & 7) + (lane >> 4) * 8, warp * 2 + ((lane >> 3) & 1)));
+        for (int j = 0; j < kTiles; j += 2) {
+            uint32_t b[4];
+            load_matrices(b, ms + chunk_at<128>(j * 8 + (lane & 7) + (lane >> 4) * 8, warp * 2 + ((lane >> 3) & 1)));
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    mma(acc[i][j], a[i][0], a[i][1], a[i][2], a[i][3], b[0], b[1]);
-                    mma(acc[i][j + 1], a[i][0], a[i][1], a[i][2], a[i][3], b[2], b[3]);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                uint32_t a[2][2][4];
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) load_matrices(a[i][k], stage + chunk_at<128>(i * 16 + a_row, half * 4 + k * 2 + (lane >> 4)));
-#pragma unroll
-                for (int j = 0; j < kTiles; ++j) {
-                    uint32_t b[4];
-                    load_matrices(b, ms + chunk_at<128>(j * 8 + (lane & 7), half * 4 + (lane >> 3)));
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        mma(acc[i][j], a[i][0][0], a[i][0][1], a[i][0][2], a[i][0][3], b[0], b[1]);
-                        mma(acc[i][j], a[i][1][0], a[i][1][1], a[i][1][2], a[i][1][3], b[2], b[3]);
-                    }
-                }
+            for (int i = 0; i < 2; ++i) {
+                mma(acc[i][j], a[i][0], a[i][1], a[i][2], a[i][3], b[0], b[1]);
+                mma(acc[i][j + 1], a[i][0], a[i][1], a[i][2], a[i][3], b[2], b[3]);
             }
         }
     }
     copies_wait<0>();
     __syncthreads();
-    float* part = reinterpret_cast<float*>(ring);                                 // [kParts][ROWS][kPitch]
+    float* part = reinterpret_cast<float*>(smem_raw + (smem - shared_at(smem_raw)));              // [4][32][kPitch]
     {
-        float* to = part + (warp * kRows + g) * kPitch + 2 * q;                   // a part's or a warp's 32 rows
+        float* to = part + (warp * kRows + g) * kPitch + 2 * q;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -284,37 +409,20 @@ template <int R, int ROWS, bool ANY> __global__ void __launch_bounds__(128) adap
             }
     }
     __syncthreads();
-    if constexpr (kParts > 1) {
-        for (int at = tid; at < ROWS * R / 4; at += 128) {
-            float4* to = reinterpret_cast<float4*>(part + at / (R / 4) * kPitch + at % (R / 4) * 4);
-            float4 v = *to;
+    for (int at = tid; at < kRows * R / 4; at += 128) {
+        float4* to = reinterpret_cast<float4*>(part + at / (R / 4) * kPitch + at % (R / 4) * 4);
+        float4 v = *to;
 #pragma unroll
-            for (int k = 1; k < kParts; ++k) {
-                const float4 u = to[k * ROWS * kPitch / 4];
-                v.x += u.x;
-                v.y += u.y;
-                v.z += u.z;
-                v.w += u.w;
-            }
-            *to = v;
+        for (int k = 1; k < 4; ++k) {
+            const float4 u = to[k * kRows * kPitch / 4];
+            v.x += u.x;
+            v.y += u.y;
+            v.z += u.z;
+            v.w += u.w;
         }
+        *to = v;
     }
-    cluster_arrive();
-    cluster_wait();
-    const int rows = ROWS / (int)ctas;                                            // of each CTA: 1, 2, 4 or 8 divide the tile
-    for (int at = tid; at < rows * (R / 4); at += 128) {
-        const int row = (int)rank * rows + at / (R / 4), col = at % (R / 4) * 4;
-        const float4 v = sum_remote4(shared_at(part + row * kPitch + col), ctas);
-        const float f[4] = {v.x * scale, v.y * scale, v.z * scale, v.w * scale};
-        bf16 hi[4], lo[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) split(f[k], hi[k], lo[k]);
-        uint16_t* to = reinterpret_cast<uint16_t*>(p.h) + (first + row) * 2 * p.padded + r0 + col;
-        *reinterpret_cast<ushort4*>(to) = make_ushort4(bits_of(hi[0]), bits_of(hi[1]), bits_of(hi[2]), bits_of(hi[3]));
-        *reinterpret_cast<ushort4*>(to + p.padded) = make_ushort4(bits_of(lo[0]), bits_of(lo[1]), bits_of(lo[2]), bits_of(lo[3]));
-    }
-    cluster_arrive();                    // nobody leaves while its sums are read
-    cluster_wait();
+    join_rows<R>(part, kRows, first, r0, (p.scale != nullptr ? p.scale[adapter] : 1.f) * p.factor, p.h, p.padded, rank, ctas);
 }
 
 // ------------------------------------------------------------------------------------------- expand ----
@@ -331,6 +439,7 @@ struct ExpandParams {
     uint32_t row_ctas;         // CTAs of rows; those behind copy the tokens without an adapter
     int32_t share;             // steps of a CTA
     bool m_whole, base_whole, out_whole;
+    uint32_t* status;
 };
 
 // Row `n` of m for the slots of a thread: 8 neighbouring ranks for R >= 32, 4 for R = 16.
@@ -393,92 +502,221 @@ template <typename T> __device__ void copy_row(const ExpandParams& p, int64_t to
     }
 }
 
-// A CTA of 4 warps takes ROWS rows of one adapter and walks columns: 64 a step with a warp on 32 of 128 rows, 128 a step with a warp on 32 of them for 32
-// rows.  h stays in registers.  The rows of m (a column of the result each) are laid down so that the 8 of an instruction's operand follow each other:
-// column c of operand j is column 8 (c / 2) + 2 j + c % 2 of 32, and a thread's results are 8 neighbouring columns.
-constexpr int kExpandStages = 3;
 template <int ROWS> constexpr int kExpandCols = ROWS == kRows ? 128 : 64;
-template <int R, int ROWS, typename T> constexpr int kExpandSmem = kExpandStages * kExpandCols<ROWS> * (ROWS * (int)sizeof(T) + R * 2);
 
-template <int R, int ROWS, typename T, bool ANY> __global__ void __launch_bounds__(128) adapter_expand_kernel(const __grid_constant__ ExpandParams p)
-{
-    constexpr int kCols = kExpandCols<ROWS>, kBase = kCols * ROWS * (int)sizeof(T), kStage = kBase + kCols * R * 2;
-    constexpr int kChunks = 64 * (int)sizeof(T) / 16, kUnits = kCols / 64 * (ROWS == kRows ? 1 : 2);     // of a row's 64 columns; of 32 columns for a warp
-    static_assert(kCols == 64 || kUnits == 2, "");
-    extern __shared__ __align__(128) uint8_t ring[];
-    __shared__ int32_t tokens[ROWS];
-    wait_for_predecessor();
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q = lane & 3;
-    const int64_t steps = (p.n + kCols - 1) / kCols, begin = (int64_t)blockIdx.y * p.share, end = min(begin + (int64_t)p.share, steps);
-    if (blockIdx.x >= p.row_ctas) {
-        const int64_t t0 = (int64_t)(blockIdx.x - p.row_ctas) * 32;
-        const uint32_t none = __ballot_sync(0xFFFFFFFFu, t0 + lane < p.s.tokens && p.s.row_of_token[t0 + lane] < 0);
-        for (int i = warp; i < 32; i += 4)
-            if (none >> i & 1) copy_row<T>(p, t0 + i, begin * kCols, min(end * kCols, p.n), lane);
-        return;
-    }
-    const int64_t first = (int64_t)blockIdx.x * ROWS;
-    if (first >= used_rows(p.s)) return;
-    const int adapter = adapter_of(p.s, first, lane);
-    const bf16* m = p.m + (int64_t)adapter * p.m_stride;
-    if (tid < ROWS) tokens[tid] = token_at(p.s, first + tid);
-    __syncthreads();
-    const uint32_t smem = shared_at(ring);
-    const int chunks = p.padded / R;                                              // of the ranks
-    auto base_at = [&](int row, int col16) {                                      // a 16-byte piece of the tile: blocks of 64 columns one after the other
+// The copies of a CTA of 128 threads: kExpandCols columns of the base of ROWS rows, in blocks of 64, and the rows of m that make them, R of the ranks.  The rows
+// of m are laid down so that column c of block j of 8 is column 8 (c / 2) + 2 j + c % 2 of 32: a thread's results, as the tensor instructions deal them
+// out, are then 8 neighbouring columns.
+template <int R, int ROWS, typename T, bool ANY> struct ExpandCopies {
+    static constexpr int kCols = kExpandCols<ROWS>, kBase = kCols * ROWS * (int)sizeof(T), kStage = kBase + kCols * R * 2;
+    static constexpr int kChunks = 64 * (int)sizeof(T) / 16;                      // of a row's 64 columns
+    // A 16-byte piece of the base: rows alternate between the halves of a line, for threads that read four neighbouring pieces of eight rows.
+    static __device__ __forceinline__ uint32_t base_at(int row, int col16)
+    {
         const int block = col16 / kChunks, chunk = col16 % kChunks;
         return (uint32_t)((block * ROWS + row) * (kChunks * 16) + ((chunk ^ ((row & 1) * (kChunks / 2))) << 4));
-    };
-    auto fill = [&](int64_t turn) {                                               // turn: step and chunk of ranks
-        const int64_t step = begin + turn / chunks;
-        if (step < end) {
-            const int r0 = (int)(turn % chunks) * R;
-            const uint32_t stage = smem + (uint32_t)(turn % kExpandStages) * kStage;
-            if (p.base != nullptr && r0 == 0) {
-                constexpr int kPieces = kCols * (int)sizeof(T) / 16;
+    }
+    static __device__ __forceinline__ void fill_base(const ExpandParams& p, uint32_t stage, const int32_t* tokens, int64_t c0)
+    {
+        constexpr int kPieces = kCols * (int)sizeof(T) / 16;
 #pragma unroll 8
-                for (int i = tid; i < ROWS * kPieces; i += 128) {
-                    const int row = i / kPieces, c = i % kPieces;
-                    const int32_t t = tokens[row];
-                    fill_chunk<T, ANY>(stage + base_at(row, c), t >= 0 ? static_cast<const T*>(p.base) + (int64_t)t * p.ldb : nullptr, step * kCols + c * (16 / (int)sizeof(T)), p.n,
-                                       p.base);
-                }
-            }
+        for (int i = threadIdx.x; i < ROWS * kPieces; i += 128) {
+            const int row = i / kPieces, c = i % kPieces;
+            const int32_t t = tokens[row];
+            fill_chunk<T, ANY>(stage + base_at(row, c), t >= 0 ? static_cast<const T*>(p.base) + (int64_t)t * p.ldb : nullptr, c0 + c * (16 / (int)sizeof(T)), p.n, p.base);
+        }
+    }
+    static __device__ __forceinline__ void fill_m(const ExpandParams& p, uint32_t stage, const bf16* m, int64_t c0, int r0)
+    {
 #pragma unroll 4
-            for (int i = tid; i < kCols * R / 8; i += 128) {
-                const int c = i / (R / 8), k = i % (R / 8), at = r0 + k * 8;
-                const int64_t n = step * kCols + c;
-                const int slot = (c & ~31) + ((c >> 1) & 3) * 8 + ((c >> 3) & 3) * 2 + (c & 1);
-                const uint32_t to = stage + kBase + chunk_at<R * 2>(slot, k);
-                const bf16* row = n < p.n ? m + n * p.ldm : nullptr;
-                if (p.m_whole) {
-                    fill_chunk<bf16, false>(to, row, at, p.m_cols, p.m);
-                } else {
-                    uint32_t w[4];
-                    load_m<32>(w, row, at, p.m_cols, false);
-                    store_chunk(to, w);
-                }
+        for (int i = threadIdx.x; i < kCols * R / 8; i += 128) {
+            const int c = i / (R / 8), k = i % (R / 8), at = r0 + k * 8;
+            const int slot = (c & ~31) + ((c >> 1) & 3) * 8 + ((c >> 3) & 3) * 2 + (c & 1);
+            const uint32_t to = stage + kBase + chunk_at<R * 2>(slot, k);
+            const bf16* row = c0 + c < p.n ? m + (c0 + c) * p.ldm : nullptr;
+            if (p.m_whole) {
+                fill_chunk<bf16, false>(to, row, at, p.m_cols, p.m);
+            } else {
+                uint32_t w[4];
+                load_m<32>(w, row, at, p.m_cols, false);
+                store_chunk(to, w);
             }
+        }
+    }
+    // 8 columns of a row, q's of a block of 32.
+    static __device__ __forceinline__ void read_base(float* v, const uint8_t* stage, int row, int block32, int q)
+    {
+        const int c16 = block32 * (32 * (int)sizeof(T) / 16) + q * (int)sizeof(T) / 2;
+        Piece<T, kPer * (int)sizeof(T), 16> piece;
+#pragma unroll
+        for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
+            const uint4 w = *reinterpret_cast<const uint4*>(stage + base_at(row, c16 + k));
+            piece.w[4 * k] = w.x; piece.w[4 * k + 1] = w.y; piece.w[4 * k + 2] = w.z; piece.w[4 * k + 3] = w.w;
+        }
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) v[k] = piece.get(k);
+    }
+};
+
+// Tokens without an adapter: 32 for a CTA of 4 warps.
+template <typename T> __device__ __forceinline__ void copy_tokens(const ExpandParams& p, int64_t t0, int64_t from, int64_t to)
+{
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t none = __ballot_sync(0xFFFFFFFFu, t0 + lane < p.s.tokens && p.s.row_of_token[t0 + lane] < 0);
+    for (int i = warp; i < 32; i += 4)
+        if (none >> i & 1) copy_row<T>(p, t0 + i, from, to, lane);
+}
+
+// A CTA takes 128 rows of one adapter and walks columns, 64 a step, with h in shared memory.  The products of a step run while the step before is read out
+// of the other set of accumulators, added to its base and stored.
+constexpr int kExpandStages = 4;
+template <int R, typename T> constexpr int kExpandSmem = kExpandStages * 64 * (128 * (int)sizeof(T) + R * 2) + 2 * 128 * R * 2 + 1024;
+
+template <int R, typename T, bool ANY> __global__ void __launch_bounds__(128) adapter_expand_kernel(const __grid_constant__ ExpandParams p)
+{
+    using C = ExpandCopies<R, 128, T, ANY>;
+    constexpr int kColumns = 128;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ Products c;
+    __shared__ int32_t tokens[128];
+    products_begin(c, kColumns);
+    wait_for_predecessor();
+    const int tid = threadIdx.x, warp = warp_number(), lane = tid & 31, g = lane >> 2, q = lane & 3;
+    const int64_t steps = (p.n + 63) / 64, begin = (int64_t)blockIdx.y * p.share;
+    const int32_t count = (int32_t)(min(begin + (int64_t)p.share, steps) - begin);
+    const int64_t first = (int64_t)blockIdx.x * 128;
+    if (blockIdx.x >= p.row_ctas) copy_tokens<T>(p, (int64_t)(blockIdx.x - p.row_ctas) * 32, begin * 64, min((begin + count) * 64, p.n));
+    if (blockIdx.x >= p.row_ctas || first >= used_rows(p.s)) {
+        products_end(c, kColumns);
+        return;
+    }
+    const int adapter = adapter_of(p.s, first, lane);
+    const bf16* m = p.m + (int64_t)adapter * p.m_stride;
+    tokens[tid] = token_at(p.s, first + tid);
+    __syncthreads();
+    const uint32_t smem = (shared_at(smem_raw) + 1023u) & ~1023u, hs = smem + kExpandStages * C::kStage;
+    const uint8_t* const ring = smem_raw + (smem - shared_at(smem_raw));
+    auto stage = [&](int32_t i) { return (uint32_t)(i % kExpandStages) * C::kStage; };
+    auto fill = [&](int32_t i) {
+        if (i < count) {
+            if (p.base != nullptr) C::fill_base(p, smem + stage(i), tokens, (begin + i) * 64);
+            C::fill_m(p, smem + stage(i), m, (begin + i) * 64, 0);
         }
         copies_commit();
     };
-    const int64_t turns = (end - begin) * chunks;
 #pragma unroll
-    for (int s = 0; s < kExpandStages - 1; ++s) fill(s);
-    const int row0 = ROWS == kRows ? 0 : warp * kRows;
+    for (int i = tid; i < 128 * R / 4; i += 128) {
+        const int row = i / (R / 4), part = i % (R / 4) / (R / 8), k = i % (R / 8);
+        fill_chunk<bf16, false>(hs + part * (128 * R * 2) + chunk_at<R * 2>(row, k), p.h + (first + row) * 2 * p.padded + part * p.padded, k * 8, p.padded, p.h);
+    }
+#pragma unroll
+    for (int i = 0; i < kExpandStages - 2; ++i) fill(i);                          // h with the first
+    T* out[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int32_t t = tokens[warp * 32 + i * 8 + g];
+        out[i] = t >= 0 ? static_cast<T*>(p.out) + (int64_t)t * p.ldo : nullptr;
+    }
+    bool given_up = false;
+    for (int32_t n = 0; n <= count; ++n) {
+        if (n < count) {
+            copies_wait<kExpandStages - 3>();
+            fence_async_smem();
+        }
+        tc_fence_before();
+        __syncthreads();                                                          // step n is there, step n - 2 is stored
+        if (n < count && warp == 0 && elect_one()) {
+            tc_fence_after();
+            const uint64_t h = operand<R * 2>(hs), w = operand<R * 2>(smem + stage(n) + C::kBase);
+#pragma unroll
+            for (int part = 0; part < 2; ++part)
+#pragma unroll
+                for (int k = 0; k < R / 16; ++k)
+                    mma_bf16(c.tmem + (n & 1) * 64, h + part * (128 * R * 2 / 16) + 2 * k, w + 2 * k, product(64, false), part > 0 || k > 0);
+            tc_commit<1>(shared_at(&c.done[n & 1]));
+        }
+        fill(n + kExpandStages - 2);
+        if (n == 0) continue;
+        const int32_t i0 = n - 1;
+        products_wait(c, i0 & 1, (uint32_t)(i0 >> 1), p.status, given_up);
+        tc_fence_after();
+        const uint32_t lanes = c.tmem + ((uint32_t)warp << 21) + (i0 & 1) * 64;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            float acc[2][4][4];
+            tmem_load_frags(acc[0], lanes + u * 32);
+            tmem_load_frags(acc[1], lanes + (16u << 16) + u * 32);
+            tc_wait_ld();
+            const int64_t at = (begin + i0) * 64 + u * 32 + q * 8;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float v[kPer] = {};
+                if (p.base != nullptr) C::read_base(v, ring + stage(i0), warp * 32 + i * 8 + g, u, q);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    v[2 * j] += acc[i >> 1][j][(i & 1) * 2];
+                    v[2 * j + 1] += acc[i >> 1][j][(i & 1) * 2 + 1];
+                }
+                if (out[i] != nullptr) store_out(v, out[i], at, p.n, p.out_whole);
+            }
+        }
+    }
+    copies_wait<0>();
+    products_end(c, kColumns);
+}
+
+// A CTA takes 32 rows of one adapter and walks columns, 128 a step and 32 of them a warp; h is in registers.
+constexpr int kExpand32Stages = 3;
+template <int R, typename T> constexpr int kExpand32Smem = kExpand32Stages * 128 * (kRows * (int)sizeof(T) + R * 2) + 128;
+
+template <int R, typename T, bool ANY> __global__ void __launch_bounds__(128) adapter_expand32_kernel(const __grid_constant__ ExpandParams p)
+{
+    using C = ExpandCopies<R, kRows, T, ANY>;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ int32_t tokens[kRows];
+    wait_for_predecessor();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q = lane & 3;
+    const int64_t steps = (p.n + C::kCols - 1) / C::kCols, begin = (int64_t)blockIdx.y * p.share;
+    const int32_t count = (int32_t)(min(begin + (int64_t)p.share, steps) - begin);
+    if (blockIdx.x >= p.row_ctas) {
+        copy_tokens<T>(p, (int64_t)(blockIdx.x - p.row_ctas) * 32, begin * C::kCols, min((begin + count) * C::kCols, p.n));
+        return;
+    }
+    const int64_t first = (int64_t)blockIdx.x * kRows;
+    if (first >= used_rows(p.s)) return;
+    const int adapter = adapter_of(p.s, first, lane);
+    const bf16* m = p.m + (int64_t)adapter * p.m_stride;
+    if (tid < kRows) tokens[tid] = token_at(p.s, first + tid);
+    __syncthreads();
+    const uint32_t smem = (shared_at(smem_raw) + 127u) & ~127u;
+    const uint8_t* const ring = smem_raw + (smem - shared_at(smem_raw));
+    const int chunks = p.padded / R;                                              // of the ranks
+    const int32_t turns = count * chunks;
+    auto stage = [&](int32_t i) { return (uint32_t)(i % kExpand32Stages) * C::kStage; };
+    auto fill = [&](int32_t i) {                                                  // a turn is a step and a chunk of the ranks
+        if (i < turns) {
+            const int64_t c0 = (begin + i / chunks) * C::kCols;
+            const int r0 = i % chunks * R;
+            if (p.base != nullptr && r0 == 0) C::fill_base(p, smem + stage(i), tokens, c0);
+            C::fill_m(p, smem + stage(i), m, c0, r0);
+        }
+        copies_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < kExpand32Stages - 1; ++i) fill(i);
     uint32_t hi[2][R / 16][4], lo[2][R / 16][4];
     auto load_h = [&](int r0) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const uint32_t* h = reinterpret_cast<const uint32_t*>(p.h + (first + row0 + i * 16 + g) * 2 * p.padded + r0) + q;
+            const uint32_t* h = reinterpret_cast<const uint32_t*>(p.h + (first + i * 16 + g) * 2 * p.padded + r0) + q;
             const int64_t below = (int64_t)8 * p.padded;                          // 8 rows, in words
 #pragma unroll
             for (int k = 0; k < R / 16; ++k) {
+                const uint32_t* l = h + p.padded / 2;
                 hi[i][k][0] = h[k * 8];
                 hi[i][k][1] = h[below + k * 8];
                 hi[i][k][2] = h[k * 8 + 4];
                 hi[i][k][3] = h[below + k * 8 + 4];
-                const uint32_t* l = h + p.padded / 2;
                 lo[i][k][0] = l[k * 8];
                 lo[i][k][1] = l[below + k * 8];
                 lo[i][k][2] = l[k * 8 + 4];
@@ -490,94 +728,59 @@ template <int R, int ROWS, typename T, bool ANY> __global__ void __launch_bounds
     T* out[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int32_t t = tokens[row0 + i * 8 + g];
+        const int32_t t = tokens[i * 8 + g];
         out[i] = t >= 0 ? static_cast<T*>(p.out) + (int64_t)t * p.ldo : nullptr;
     }
-    float acc[kUnits / (kCols / 64)][2][4][4];                                    // [units of 32 columns of this warp][16 rows][operand]
-    constexpr int kMine = kUnits / (kCols / 64);
-    for (int64_t turn = 0; turn < turns; ++turn) {
-        copies_wait<kExpandStages - 2>();
+    float acc[2][4][4];
+    for (int32_t turn = 0; turn < turns; ++turn) {
+        copies_wait<kExpand32Stages - 2>();
         __syncthreads();
-        fill(turn + kExpandStages - 1);
-        const uint32_t stage = smem + (uint32_t)(turn % kExpandStages) * kStage, ms = stage + kBase;
-        const int r0 = (int)(turn % chunks) * R;
-        const int64_t c0 = (begin + turn / chunks) * kCols;
+        fill(turn + kExpand32Stages - 1);
+        const uint32_t ms = smem + stage(turn) + C::kBase;
+        const int r0 = turn % chunks * R;
         if (chunks > 1) load_h(r0);
-        // base into the sums, from the first chunk of ranks on
-        if (r0 == 0) {
+        if (r0 == 0) {                                                            // the sums begin with the base
 #pragma unroll
-            for (int u = 0; u < kMine; ++u) {
-                const int c16 = (ROWS == kRows ? warp : u) * (32 * (int)sizeof(T) / 16) + q * (int)sizeof(T) / 2;
+            for (int i = 0; i < 4; ++i) {
+                float v[kPer] = {};
+                if (p.base != nullptr) C::read_base(v, ring + stage(turn), i * 8 + g, warp, q);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float v[kPer];
-                    if (p.base != nullptr) {
-                        Piece<T, kPer * (int)sizeof(T), 16> piece;
-#pragma unroll
-                        for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
-                            const uint4 w = *reinterpret_cast<const uint4*>(ring + (stage - smem) + base_at(row0 + i * 8 + g, c16 + k));
-                            piece.w[4 * k] = w.x; piece.w[4 * k + 1] = w.y; piece.w[4 * k + 2] = w.z; piece.w[4 * k + 3] = w.w;
-                        }
-#pragma unroll
-                        for (int k = 0; k < kPer; ++k) v[k] = piece.get(k);
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < kPer; ++k) v[k] = 0.f;
-                    }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        acc[u][i >> 1][j][(i & 1) * 2] = v[2 * j];
-                        acc[u][i >> 1][j][(i & 1) * 2 + 1] = v[2 * j + 1];
-                    }
+                for (int j = 0; j < 4; ++j) {
+                    acc[i >> 1][j][(i & 1) * 2] = v[2 * j];
+                    acc[i >> 1][j][(i & 1) * 2 + 1] = v[2 * j + 1];
                 }
             }
         }
 #pragma unroll
-        for (int u = 0; u < kMine; ++u) {
-            const int unit = ROWS == kRows ? warp : u;
+        for (int j = 0; j < 4; ++j) {
+            const int slot = warp * 32 + j * 8 + (lane & 7);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int slot = unit * 32 + j * 8;
-                if constexpr (R == 16) {
-                    // two operands of 16 ranks at once would cross j: one, its halves twice
-                    uint32_t b[4];
-                    load_matrices(b, ms + chunk_at<32>(slot + (lane & 7), (lane >> 3) & 1));
+            for (int k = 0; k < (R + 31) / 32; ++k) {
+                uint32_t b[4];                                                    // 32 ranks, or 16 of them twice
+                load_matrices(b, ms + chunk_at<R * 2>(slot, R == 16 ? (lane >> 3) & 1 : k * 4 + (lane >> 3)));
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        mma(acc[u][i][j], hi[i][0][0], hi[i][0][1], hi[i][0][2], hi[i][0][3], b[0], b[1]);
-                        mma(acc[u][i][j], lo[i][0][0], lo[i][0][1], lo[i][0][2], lo[i][0][3], b[0], b[1]);
-                    }
-                } else {
-#pragma unroll
-                    for (int k = 0; k < R / 32; ++k) {
-                        uint32_t b[4];
-                        load_matrices(b, ms + chunk_at<R * 2>(slot + (lane & 7), k * 4 + (lane >> 3)));
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            mma(acc[u][i][j], hi[i][2 * k][0], hi[i][2 * k][1], hi[i][2 * k][2], hi[i][2 * k][3], b[0], b[1]);
-                            mma(acc[u][i][j], hi[i][2 * k + 1][0], hi[i][2 * k + 1][1], hi[i][2 * k + 1][2], hi[i][2 * k + 1][3], b[2], b[3]);
-                            mma(acc[u][i][j], lo[i][2 * k][0], lo[i][2 * k][1], lo[i][2 * k][2], lo[i][2 * k][3], b[0], b[1]);
-                            mma(acc[u][i][j], lo[i][2 * k + 1][0], lo[i][2 * k + 1][1], lo[i][2 * k + 1][2], lo[i][2 * k + 1][3], b[2], b[3]);
-                        }
+                for (int i = 0; i < 2; ++i) {
+                    mma(acc[i][j], hi[i][2 * k][0], hi[i][2 * k][1], hi[i][2 * k][2], hi[i][2 * k][3], b[0], b[1]);
+                    mma(acc[i][j], lo[i][2 * k][0], lo[i][2 * k][1], lo[i][2 * k][2], lo[i][2 * k][3], b[0], b[1]);
+                    if constexpr (R > 16) {
+                        mma(acc[i][j], hi[i][2 * k + 1][0], hi[i][2 * k + 1][1], hi[i][2 * k + 1][2], hi[i][2 * k + 1][3], b[2], b[3]);
+                        mma(acc[i][j], lo[i][2 * k + 1][0], lo[i][2 * k + 1][1], lo[i][2 * k + 1][2], lo[i][2 * k + 1][3], b[2], b[3]);
                     }
                 }
             }
         }
         if (r0 + R < p.padded) continue;
+        const int64_t at = (begin + turn / chunks) * C::kCols + warp * 32 + q * 8;
 #pragma unroll
-        for (int u = 0; u < kMine; ++u) {
-            const int64_t at = c0 + (ROWS == kRows ? warp : u) * 32 + q * 8;
+        for (int i = 0; i < 4; ++i) {
+            if (out[i] == nullptr) continue;
+            float v[kPer];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (out[i] == nullptr) continue;
-                float v[kPer];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    v[2 * j] = acc[u][i >> 1][j][(i & 1) * 2];
-                    v[2 * j + 1] = acc[u][i >> 1][j][(i & 1) * 2 + 1];
-                }
-                store_out(v, out[i], at, p.n, p.out_whole);
+            for (int j = 0; j < 4; ++j) {
+                v[2 * j] = acc[i >> 1][j][(i & 1) * 2];
+                v[2 * j + 1] = acc[i >> 1][j][(i & 1) * 2 + 1];
             }
+            store_out(v, out[i], at, p.n, p.out_whole);
         }
     }
     copies_wait<0>();
@@ -624,122 +827,113 @@ struct OuterParams {
     int64_t ldz, n;
     int32_t rank, padded;
     bf16* out;                 // [adapters][rank][n], or [adapters][n][rank]
+    uint32_t* status;
 };
 
-// R ranks x 256 columns of an adapter by 8 warps, 64 columns each, half of them on the first 32 of each step's 64 rows, half on the others.  The reduction runs over
-// the adapter's rows, cut over a cluster's CTAs.  Both operands have the reduction axis outside and are turned as they are read from shared memory.
-constexpr int kOuterStages = 4, kOuterCols = 256, kOuterRows = 64;
+// 128 columns x R ranks of an adapter: the reduction runs over its rows, 64 a step, cut over a cluster's CTAs.  Both operands have the reduction axis across
+// their rows, as they lie in memory.
+constexpr int kOuterStages = 3, kOuterCols = 128, kOuterRows = 64;
 template <int R> constexpr int kOuterStage = kOuterRows * (kOuterCols + 2 * R) * 2;
-template <int R> constexpr int kOuterSmem = kOuterStages * kOuterStage<R>;
+template <int R> constexpr int kOuterSmem = kOuterStages * kOuterStage<R> + 1024;
 
-template <int R, bool BY_COLUMN, bool ANY> __global__ void __launch_bounds__(256) adapter_outer_kernel(const __grid_constant__ OuterParams p)
+template <int R, bool BY_COLUMN, bool ANY> __global__ void __launch_bounds__(128) adapter_outer_kernel(const __grid_constant__ OuterParams p)
 {
-    constexpr int kTiles = R / 16, kHalf = kOuterRows * R * 2;                    // bytes of h's high parts
-    constexpr int kPitch = (BY_COLUMN ? R : kOuterCols) + 4, kLines = BY_COLUMN ? kOuterCols : R, kLine = BY_COLUMN ? R : kOuterCols;
-    static_assert(kLines * kPitch * 4 <= kOuterSmem<R>, "the sums take the ring's place");
-    extern __shared__ __align__(128) uint8_t ring[];
+    constexpr int kHalf = kOuterRows * R * 2, kColumns = R < 32 ? 32 : R;         // bytes of h's high parts; of tensor memory
+    constexpr int kLines = BY_COLUMN ? kOuterCols : R, kLine = BY_COLUMN ? R : kOuterCols, kPitch = kLine + 4;
+    static_assert(kLines * kPitch * 4 <= kOuterSmem<R> - 1024, "the sums take the ring's place");
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ Products c;
+    products_begin(c, kColumns);
     wait_for_predecessor();
-    const uint32_t rank = cluster_rank(), ctas = cluster_size();
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q = lane & 3;
+    const uint32_t rank = cluster_rank(), ctas = cluster_size(), smem = (shared_at(smem_raw) + 1023u) & ~1023u;
+    const int tid = threadIdx.x, warp = warp_number();
     const int chunks = p.padded / R, adapter = blockIdx.z / chunks, r0 = blockIdx.z % chunks * R;
     const int64_t c0 = (int64_t)blockIdx.y * kOuterCols;
     const int64_t from = p.s.starts != nullptr ? p.s.starts[adapter] : 0, to = p.s.starts != nullptr ? p.s.starts[adapter + 1] : adapter == 0 ? p.s.rows : 0;
-    const uint32_t smem = shared_at(ring);
-    const int64_t steps = (to - from + kOuterRows - 1) / kOuterRows, share = (steps + ctas - 1) / ctas, begin = min((int64_t)rank * share, steps), end = min(begin + share, steps);
-    // a thread copies chunk lane of every 8th row; the tokens of a step's rows are looked up a step ahead
+    const int32_t steps = (int32_t)((to - from + kOuterRows - 1) / kOuterRows), share = (steps + (int32_t)ctas - 1) / (int32_t)ctas;
+    const int32_t begin = min((int32_t)rank * share, steps), count = min(begin + share, steps) - begin;
+    // a thread copies chunk tid % 16 of every 8th row; the tokens of a step's rows are looked up a step ahead
     int32_t ahead[8];
-    auto look = [&](int64_t step) {
+    auto look = [&](int32_t i) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int64_t row = from + step * kOuterRows + i * 8 + warp;
-            ahead[i] = step < end && row < to ? token_at(p.s, row) : -1;
+        for (int k = 0; k < 8; ++k) {
+            const int64_t row = from + (int64_t)(begin + i) * kOuterRows + k * 8 + (tid >> 4);
+            ahead[k] = i < count && row < to ? token_at(p.s, row) : -1;
         }
     };
-    auto fill = [&](int64_t step) {
-        if (step < end) {
-            const uint32_t stage = smem + (uint32_t)((step - begin) % kOuterStages) * kOuterStage<R>;
+    auto stage = [&](int32_t i) { return smem + (uint32_t)(i % kOuterStages) * kOuterStage<R>; };
+    auto fill = [&](int32_t i) {
+        if (i < count) {
+            const uint32_t zs = stage(i), hs = zs + kOuterRows * kOuterCols * 2;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                fill_chunk<bf16, ANY>(stage + (lane >> 3) * (kOuterRows * 128) + chunk_at<128>(i * 8 + warp, lane & 7), ahead[i] >= 0 ? p.z + (int64_t)ahead[i] * p.ldz : nullptr,
-                                      c0 + lane * 8, p.n, p.z);
-            const uint32_t hs = stage + kOuterRows * kOuterCols * 2;
+            for (int k = 0; k < 8; ++k)
+                fill_chunk<bf16, ANY>(zs + ((tid & 15) >> 3) * (kOuterRows * 128) + chunk_at<128>(k * 8 + (tid >> 4), tid & 7), ahead[k] >= 0 ? p.z + (int64_t)ahead[k] * p.ldz : nullptr,
+                                      c0 + (tid & 15) * 8, p.n, p.z);
 #pragma unroll
-            for (int i = tid; i < kOuterRows * R / 4; i += 256) {
-                const int row = i / (R / 4), c = i % (R / 4), part = c / (R / 8), chunk = c % (R / 8);
-                const int64_t at = from + step * kOuterRows + row;
+            for (int k = tid; k < kOuterRows * R / 4; k += 128) {
+                const int row = k / (R / 4), part = k % (R / 4) / (R / 8), chunk = k % (R / 8);
+                const int64_t at = from + (int64_t)(begin + i) * kOuterRows + row;
                 fill_chunk<bf16, false>(hs + part * kHalf + chunk_at<R * 2>(row, chunk), at < to ? p.h + at * 2 * p.padded + part * p.padded : nullptr, r0 + chunk * 8, p.padded, p.h);
             }
         }
         copies_commit();
-        look(step + 1);
+        look(i + 1);
     };
-    float acc[kTiles][8][4];
+    bool given_up = false;
+    look(0);
 #pragma unroll
-    for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) acc[i][j][k] = 0.f;
-    look(begin);
-#pragma unroll
-    for (int s = 0; s < kOuterStages - 1; ++s) fill(begin + s);
-    const int block = warp & 3, row0 = (warp >> 2) * 32;
-    for (int64_t step = begin; step < end; ++step) {
+    for (int i = 0; i < kOuterStages - 1; ++i) fill(i);
+    for (int32_t n = 0; n < count; ++n) {
         copies_wait<kOuterStages - 2>();
+        fence_async_smem();
         __syncthreads();
-        fill(step + kOuterStages - 1);
-        const uint32_t stage = smem + (uint32_t)((step - begin) % kOuterStages) * kOuterStage<R>, zs = stage + block * (kOuterRows * 128), hs = stage + kOuterRows * kOuterCols * 2;
+        if (warp == 0 && elect_one()) {
+            const uint64_t z = operand<128>(stage(n), kOuterRows * 128), h = operand<R * 2>(stage(n) + kOuterRows * kOuterCols * 2);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            uint32_t b[4][4];
+            for (int part = 0; part < 2; ++part)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) load_matrices_turned(b[j], zs + chunk_at<128>(row0 + k * 16 + (lane & 15), j * 2 + (lane >> 4)));
-#pragma unroll
-            for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-                for (int part = 0; part < 2; ++part) {
-                    uint32_t a[4];
-                    load_matrices_turned(a, hs + part * kHalf + chunk_at<R * 2>(row0 + k * 16 + (lane & 7) + (lane >> 4) * 8, i * 2 + ((lane >> 3) & 1)));
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        mma(acc[i][2 * j], a[0], a[1], a[2], a[3], b[j][0], b[j][1]);
-                        mma(acc[i][2 * j + 1], a[0], a[1], a[2], a[3], b[j][2], b[j][3]);
-                    }
-                }
+                for (int k = 0; k < kOuterRows / 16; ++k)                          // 16 rows of either further
+                    mma_bf16(c.tmem, z + k * (16 * 128 / 16), h + part * (kHalf / 16) + k * (16 * R * 2 / 16), product(R, true), n > 0 || part > 0 || k > 0);
+            tc_commit<1>(shared_at(&c.done[n % kOuterStages]));
         }
+        if (n > 0) products_wait(c, (n - 1) % kOuterStages, (uint32_t)((n - 1) / kOuterStages), p.status, given_up);
+        fill(n + kOuterStages - 1);
     }
+    if (count > 0) products_wait(c, (count - 1) % kOuterStages, (uint32_t)((count - 1) / kOuterStages), p.status, given_up);
     copies_wait<0>();
+    tc_fence_after();
     __syncthreads();
-    float* part = reinterpret_cast<float*>(ring);                                 // [kLines][kPitch]
-#pragma unroll 1
-    for (int turn = 0; turn < 2; ++turn) {
-        if (warp >> 2 == turn) {
+    float* part = reinterpret_cast<float*>(smem_raw + (smem - shared_at(smem_raw)));              // [kLines][kPitch]
+    const uint32_t lanes = c.tmem + ((uint32_t)warp << 21);
 #pragma unroll
-            for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int r = i * 16 + (k >> 1) * 8 + g, c = block * 64 + j * 8 + 2 * q + (k & 1);
-                        float* at = part + (BY_COLUMN ? c * kPitch + r : r * kPitch + c);
-                        *at = turn > 0 ? *at + acc[i][j][k] : acc[i][j][k];
-                    }
+    for (int r = 0; r < R; r += 16) {                                             // a thread has a column
+        uint32_t v[16] = {};
+        if (count > 0) {
+            tmem_load16(v, lanes + r);
+            tc_wait_ld();
         }
-        __syncthreads();
+        if constexpr (BY_COLUMN) {
+#pragma unroll
+            for (int k = 0; k < 16; k += 4) *reinterpret_cast<uint4*>(part + tid * kPitch + r + k) = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) part[(r + k) * kPitch + tid] = __uint_as_float(v[k]);
+        }
     }
+    products_end(c, kColumns);
     cluster_arrive();
     cluster_wait();
     bf16* out = p.out + (int64_t)adapter * p.rank * p.n;
     const int lines = kLines / (int)ctas;
-    for (int at = tid; at < lines * (kLine / 4); at += 256) {
+    for (int at = tid; at < lines * (kLine / 4); at += 128) {
         const int line = (int)rank * lines + at / (kLine / 4), e = at % (kLine / 4) * 4;
         const float4 v = sum_remote4(shared_at(part + line * kPitch + e), ctas);
         const float f[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const int r = r0 + (BY_COLUMN ? e + k : line);
-            const int64_t c = c0 + (BY_COLUMN ? line : e + k);
-            if (r < p.rank && c < p.n) out[BY_COLUMN ? c * p.rank + r : (int64_t)r * p.n + c] = __float2bfloat16(f[k]);
+            const int64_t col = c0 + (BY_COLUMN ? line : e + k);
+            if (r < p.rank && col < p.n) out[BY_COLUMN ? col * p.rank + r : (int64_t)r * p.n + col] = __float2bfloat16(f[k]);
         }
     }
     cluster_arrive();
@@ -972,8 +1166,8 @@ int padded_rank(int rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : (rank + 6
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 // Rows of a tile.  128 where there are tokens for it: enough to fill the GPU with such tiles, and as many for an adapter that the rows left empty at its end (64 on
-// average) cost less than what smaller tiles read again of the adapters.
-int tile_rows(const mor_adapter_desc_t& d) { return d.tokens >= 2048 && d.tokens >= 256 * (int64_t)d.adapters ? 128 : kRows; }
+// average) cost less than what smaller tiles read again of the adapters.  Ranks above 64 come in pieces, which only the small tiles take.
+int tile_rows(const mor_adapter_desc_t& d) { return d.rank <= 64 && d.tokens >= 2048 && d.tokens >= 256 * (int64_t)d.adapters ? 128 : kRows; }
 int64_t sorted_rows(const mor_adapter_desc_t& d)
 {
     return d.ids != nullptr ? mor_expert_rows(d.tokens, d.adapters, tile_rows(d)) : up(d.tokens, tile_rows(d));
@@ -1040,7 +1234,8 @@ template <typename F> cudaError_t by_rank(int padded, F&& f)
     return padded == 16 ? f(std::integral_constant<int, 16>{}) : padded == 32 ? f(std::integral_constant<int, 32>{}) : f(std::integral_constant<int, 64>{});
 }
 
-constexpr int64_t kResident = 148 * 2;       // CTAs that the GPU holds of the larger shapes
+// CTAs that the GPU holds at once of a kernel with that much shared memory.
+constexpr int64_t resident(int smem) { return 148 * std::min(227 * 1024 / (smem + 2048), 4); }
 
 // Allows the kernel its shared memory and launches it.
 template <typename K, typename P> cudaError_t launch_ring(K kernel, std::atomic<uint64_t>& done, int smem, dim3 grid, uint32_t cluster, uint32_t block, cudaStream_t st, const P& p)
@@ -1055,8 +1250,10 @@ template <int R, int ROWS, bool ANY> cudaError_t shrink_launch(const ShrinkParam
     const int64_t tiles = p.s.rows / ROWS, steps = (p.n + 63) / 64;
     const uint32_t chunks = (uint32_t)(p.padded / R);
     uint32_t cluster = 1;                     // as many CTAs to a tile as the GPU holds at once, two steps each at least
-    while (cluster < kMaxCluster && tiles * chunks * cluster * 2 <= kResident && steps >= 4 * cluster) cluster *= 2;
-    return launch_ring(adapter_shrink_kernel<R, ROWS, ANY>, done, kShrinkSmem<R, ROWS>, dim3((uint32_t)tiles * cluster, chunks), cluster, 128, st, p);
+    while (cluster < kMaxCluster && tiles * chunks * cluster * 2 <= resident(kShrinkSmem<R, ROWS>) && steps >= 4 * cluster) cluster *= 2;
+    const dim3 grid((uint32_t)tiles * cluster, chunks);
+    if constexpr (ROWS == 128) return launch_ring(adapter_shrink_kernel<R, ANY>, done, kShrinkSmem<R, ROWS>, grid, cluster, 128, st, p);
+    else return launch_ring(adapter_shrink32_kernel<R, ANY>, done, kShrinkSmem<R, ROWS>, grid, cluster, 128, st, p);
 }
 cudaError_t shrink(const ShrinkParams& p, int rows, bool any, cudaStream_t st)
 {
@@ -1073,11 +1270,13 @@ template <int R, int ROWS, typename T, bool ANY> cudaError_t expand_launch(Expan
     p.row_ctas = (uint32_t)(p.s.rows / ROWS);
     const int64_t steps = (p.n + kExpandCols<ROWS> - 1) / kExpandCols<ROWS>;
     // as many CTAs as the GPU holds at once
-    int64_t across = std::max<int64_t>(1, std::min<int64_t>(steps, kResident / std::max<uint32_t>(1, p.row_ctas)));
+    constexpr int kSmem = ROWS == 128 ? kExpandSmem<R, T> : kExpand32Smem<R, T>;
+    int64_t across = std::max<int64_t>(1, std::min<int64_t>(steps, resident(kSmem) / std::max<uint32_t>(1, p.row_ctas)));
     p.share = (int32_t)((steps + across - 1) / across);
     across = (steps + p.share - 1) / p.share;
-    const uint32_t copies = p.s.starts != nullptr ? (uint32_t)(up(p.s.tokens, 32) / 32) : 0;
-    return launch_ring(adapter_expand_kernel<R, ROWS, T, ANY>, done, kExpandSmem<R, ROWS, T>, dim3(p.row_ctas + copies, (uint32_t)across), 0, 128, st, p);
+    const dim3 grid(p.row_ctas + (p.s.starts != nullptr ? (uint32_t)(up(p.s.tokens, 32) / 32) : 0), (uint32_t)across);
+    if constexpr (ROWS == 128) return launch_ring(adapter_expand_kernel<R, T, ANY>, done, kExpandSmem<R, T>, grid, 0, 128, st, p);
+    else return launch_ring(adapter_expand32_kernel<R, T, ANY>, done, kExpand32Smem<R, T>, grid, 0, 128, st, p);
 }
 template <typename T> cudaError_t expand_rows(const ExpandParams& p, int rows, cudaStream_t st)
 {
@@ -1099,8 +1298,8 @@ template <int R, bool BY_COLUMN, bool ANY> cudaError_t outer_launch(const OuterP
     const uint32_t across = (uint32_t)((p.n + kOuterCols - 1) / kOuterCols), deep = (uint32_t)(p.s.adapters * (p.padded / R));
     const int64_t mean = p.s.rows / p.s.adapters;      // two steps each at least, going by the adapters' mean
     uint32_t cluster = 1;
-    while (cluster < kMaxCluster && (int64_t)across * deep * cluster * 2 <= kResident && mean >= 4 * kOuterRows * (int64_t)cluster) cluster *= 2;
-    return launch_ring(adapter_outer_kernel<R, BY_COLUMN, ANY>, done, kOuterSmem<R>, dim3(cluster, across, deep), cluster, 256, st, p);
+    while (cluster < kMaxCluster && (int64_t)across * deep * cluster * 2 <= resident(kOuterSmem<R>) && mean >= 4 * kOuterRows * (int64_t)cluster) cluster *= 2;
+    return launch_ring(adapter_outer_kernel<R, BY_COLUMN, ANY>, done, kOuterSmem<R>, dim3(cluster, across, deep), cluster, 128, st, p);
 }
 cudaError_t outer(const OuterParams& p, bool by_column, bool any, cudaStream_t st)
 {
@@ -1117,7 +1316,7 @@ mor_status_t check_adapter(const mor_adapter_desc_t* d)
     if (d->adapters < 1 || d->adapters >= MOR_MAX_GROUPS || d->rank < 1 || d->rank > MOR_MAX_RANK) return MOR_ERR_INVALID_ARG;
     if (d->a == nullptr || d->b == nullptr) return MOR_ERR_INVALID_ARG;
     if (sorted_rows(*d) < 0) return MOR_ERR_INVALID_ARG;
-    if (!is_aligned(d->a, 2) || !is_aligned(d->b, 2) || !is_aligned(d->ids, 4) || !is_aligned(d->scale, 4)) return MOR_ERR_ALIGNMENT;
+    if (!is_aligned(d->a, 2) || !is_aligned(d->b, 2) || !is_aligned(d->ids, 4) || !is_aligned(d->scale, 4) || !is_aligned(d->status, 4)) return MOR_ERR_ALIGNMENT;
     return MOR_OK;
 }
 // A token matrix: `whole` if its rows start on 16 bytes.
@@ -1181,10 +1380,10 @@ mor_status_t mor_adapter_add(const mor_adapter_desc_t* d, const void* x, int64_t
         if (st != MOR_OK) return st;
     }
     const int padded = padded_rank(d->rank);
-    ShrinkParams sp = {f.s, static_cast<const bf16*>(x), static_cast<const bf16*>(d->a), d->scale, d->factor, ldx, d->n_in, d->n_in, (int64_t)d->rank * d->n_in, d->rank, padded, f.h};
+    ShrinkParams sp = {f.s, static_cast<const bf16*>(x), static_cast<const bf16*>(d->a), d->scale, d->factor, ldx, d->n_in, d->n_in, (int64_t)d->rank * d->n_in, d->rank, padded, f.h, d->status};
     if (shrink(sp, rows, any, stream) != cudaSuccess) return MOR_ERR_CUDA;
     ExpandParams ep = {f.s, f.h, static_cast<const bf16*>(d->b), d->n_out, d->rank, (int64_t)d->n_out * d->rank, d->rank, padded, base, out, ldb, ldo, 0, 0,
-                       d->rank % 8 == 0 && is_aligned(d->b, 16), base_whole, out_whole};
+                       d->rank % 8 == 0 && is_aligned(d->b, 16), base_whole, out_whole, d->status};
     return status(expand(ep, rows, dtype, stream));
 }
 
@@ -1218,19 +1417,19 @@ mor_status_t mor_adapter_grad(const mor_adapter_desc_t* d, const void* x, int64_
         const uint32_t a_ctas = (uint32_t)(ceil_div(padded, 32) * ceil_div(d->n_in, 32)), b_ctas = (uint32_t)(ceil_div(w.wide, 32) * ceil_div(padded, 32));
         TurnParams tp = {static_cast<const bf16*>(d->a), static_cast<const bf16*>(d->b), w.at, w.bt, d->n_in, d->n_out, w.wide, d->rank, padded, a_ctas};
         if (launch_clusters(adapter_turn_kernel, dim3(a_ctas + b_ctas, (uint32_t)d->adapters), 0, 256, 0, stream, tp) != cudaSuccess) return MOR_ERR_CUDA;
-        ShrinkParams sp = {f.s, static_cast<const bf16*>(dy), w.bt, d->scale, d->factor, lddy, d->n_out, w.wide, (int64_t)padded * w.wide, padded, padded, w.u};
+        ShrinkParams sp = {f.s, static_cast<const bf16*>(dy), w.bt, d->scale, d->factor, lddy, d->n_out, w.wide, (int64_t)padded * w.wide, padded, padded, w.u, d->status};
         if (shrink(sp, rows, !dy_whole, stream) != cudaSuccess) return MOR_ERR_CUDA;
     }
     if (db != nullptr) {
-        OuterParams op = {f.s, f.h, static_cast<const bf16*>(dy), lddy, d->n_out, d->rank, padded, static_cast<bf16*>(db)};
+        OuterParams op = {f.s, f.h, static_cast<const bf16*>(dy), lddy, d->n_out, d->rank, padded, static_cast<bf16*>(db), d->status};
         if (outer(op, true, !dy_whole, stream) != cudaSuccess) return MOR_ERR_CUDA;
     }
     if (da != nullptr) {
-        OuterParams op = {f.s, w.u, static_cast<const bf16*>(x), ldx, d->n_in, d->rank, padded, static_cast<bf16*>(da)};
+        OuterParams op = {f.s, w.u, static_cast<const bf16*>(x), ldx, d->n_in, d->rank, padded, static_cast<bf16*>(da), d->status};
         if (outer(op, false, !x_whole, stream) != cudaSuccess) return MOR_ERR_CUDA;
     }
     if (dx != nullptr) {
-        ExpandParams ep = {f.s, w.u, w.at, d->n_in, padded, (int64_t)d->n_in * padded, padded, padded, base, dx, ldb, lddx, 0, 0, true, base_whole, dx_whole};
+        ExpandParams ep = {f.s, w.u, w.at, d->n_in, padded, (int64_t)d->n_in * padded, padded, padded, base, dx, ldb, lddx, 0, 0, true, base_whole, dx_whole, d->status};
         if (expand(ep, rows, MOR_DTYPE_BF16, stream) != cudaSuccess) return MOR_ERR_CUDA;
     }
     return MOR_OK;

@@ -243,6 +243,8 @@ Adapters adapter_args(const Tensor& x, int64_t n_out, const Tensor& a, const Ten
     r.d.ids = r.ids.defined() ? ptr<int32_t>(r.ids) : nullptr;
     r.d.scale = r.scale.defined() ? ptr<float>(r.scale) : nullptr;
     r.d.factor = (float)factor;
+    const Tensor status = status_word(x);
+    r.d.status = status.defined() ? reinterpret_cast<uint32_t*>(ptr<int32_t>(status)) : nullptr;
     return r;
 }
 // Into `out`, which may be the base.  The scratch of a training call is what its backward pass reads.

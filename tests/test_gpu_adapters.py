@@ -54,7 +54,8 @@ def formula(base, x, a, b, ids, scale):
 
 SHAPES = [(1, 64, 64, 8, 1), (1, 4096, 1000, 16, 3), (2, 31, 33, 3, 2), (5, 8, 8, 1, 4), (16, 128, 256, 16, 1), (17, 257, 100, 24, 2), (33, 512, 4096, 32, 5), (100, 1000, 72, 17, 40),
           (255, 64, 520, 64, 3), (256, 320, 96, 33, 7), (257, 320, 96, 33, 7), (300, 100, 1001, 16, 2), (1000, 1024, 513, 48, 9), (2100, 264, 328, 65, 4), (700, 72, 200, 130, 3),
-          (40, 96, 64, 100, 2), (2500, 40, 48, 8, 33), (64, 2056, 130, 64, 64), (129, 24, 16, 12, 1000)]
+          (40, 96, 64, 100, 2), (2500, 40, 48, 8, 33), (64, 2056, 130, 64, 64), (2100, 264, 328, 64, 4), (2048, 100, 1001, 16, 3), (4100, 512, 520, 33, 5), (3000, 1000, 72, 32, 1),
+          (2049, 8, 8, 4, 2), (129, 24, 16, 12, 1000)]
 
 
 @pytest.mark.parametrize("base", ["bf16", "fp32"])
