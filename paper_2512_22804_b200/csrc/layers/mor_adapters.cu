@@ -129,6 +129,31 @@ template <typename T, bool ANY> __device__ __forceinline__ void fill_chunk(uint3
         copy_async(to, bytes > 0 ? static_cast<const void*>(row + at) : valid, bytes);
     }
 }
+// The same chunk of N rows, N of them a thread's, copied step by step along the rows: what does not change from step to step is worked out once (the copies
+// of a tile are most of a step's instructions, and few warps run them).
+template <typename T, int N, bool ANY> struct RowCopies {
+    const T* row[N];           // from the thread's chunk on
+    uint32_t present;
+    __device__ __forceinline__ void set(int k, const T* r, int64_t at, const void* valid)
+    {
+        if (k == 0) present = 0;
+        if (r != nullptr) present |= 1u << k;
+        row[k] = r != nullptr ? r + at : static_cast<const T*>(valid);
+    }
+    // `at`: elements since the first step; `left`: from the chunk's place now to the row's end; `first`: where the rows start, to the chunk
+    __device__ __forceinline__ void copy(int k, uint32_t to, int64_t at, int left, int first) const
+    {
+        constexpr int kElems = 16 / (int)sizeof(T);
+        if constexpr (ANY) {
+            uint32_t w[4] = {0, 0, 0, 0};
+            if ((present >> k & 1) && left > 0) load_any<T, 16>(w, row[k] - first, first + at, first + at + left);
+            store_chunk(to, w);
+        } else {
+            const int bytes = (present >> k & 1) ? (int)sizeof(T) * max(0, min(kElems, left)) : 0;
+            copy_async(to, row[k] + at, bytes);
+        }
+    }
+};
 __device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t at)
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
@@ -225,7 +250,7 @@ template <int R> __device__ __forceinline__ void join_rows(float* part, int rows
     cluster_arrive();
     cluster_wait();
     rows /= (int)ctas;                                                            // of each CTA: 1, 2, 4 or 8 divide the tile
-    for (int at = threadIdx.x; at < rows * (R / 4); at += 128) {
+    for (int at = threadIdx.x; at < rows * (R / 4); at += blockDim.x) {
         const int row = (int)rank * rows + at / (R / 4), col = at % (R / 4) * 4;
         const float4 v = sum_remote4(shared_at(part + row * kPitch + col), ctas);
         const float f[4] = {v.x * scale, v.y * scale, v.z * scale, v.w * scale};
@@ -258,48 +283,49 @@ struct ShrinkParams {
 constexpr int kShrinkStages = 4;
 template <int R, int ROWS> constexpr int kShrinkSmem = kShrinkStages * (ROWS + R) * 128 + 1024;
 
-// The copies of a CTA of 128 threads: steps of 64 elements of ROWS rows of x and R of m; a thread's are chunk tid % 8 of every 16th row.
-template <int R, int ROWS, bool ANY> struct ShrinkCopies {
-    static constexpr int kStage = (ROWS + R) * 128;
-    const bf16 *xr[ROWS / 16], *mr[R / 16], *valid;
-    int64_t n;
-    int32_t begin, end;
-    uint32_t ring;
-    __device__ __forceinline__ ShrinkCopies(const ShrinkParams& p, int64_t first, int r0, int adapter, uint32_t rank, uint32_t ctas, uint32_t smem) : valid(p.x), n(p.n), ring(smem)
+// The copies of a CTA: steps of 64 elements of ROWS rows of x and R of m; a thread's are chunk tid % 8 of every THREADS / 8th row.
+template <int R, int ROWS, int THREADS, bool ANY> struct ShrinkCopies {
+    static constexpr int kStage = (ROWS + R) * 128, kStep = THREADS / 8, kX = ROWS / kStep, kM = R > kStep ? R / kStep : 1;
+    RowCopies<bf16, kX, ANY> x;
+    RowCopies<bf16, kM, ANY> m;
+    int32_t n, begin, end;
+    uint32_t ring, place;
+    __device__ __forceinline__ ShrinkCopies(const ShrinkParams& p, int64_t first, int r0, int adapter, uint32_t rank, uint32_t ctas, uint32_t smem) : n((int32_t)p.n), ring(smem)
     {
-        const int tid = threadIdx.x;
-#pragma unroll
-        for (int i = 0; i < ROWS / 16; ++i) {
-            const int32_t t = token_at(p.s, first + i * 16 + (tid >> 3));
-            xr[i] = t >= 0 ? p.x + (int64_t)t * p.ldx : nullptr;
-        }
-#pragma unroll
-        for (int i = 0; i < R / 16; ++i) {
-            const int r = r0 + i * 16 + (tid >> 3);
-            mr[i] = r < p.m_rows ? p.m + (int64_t)adapter * p.m_stride + (int64_t)r * p.ldm : nullptr;
-        }
-        const int32_t steps = (int32_t)((p.n + 63) / 64), share = (steps + (int32_t)ctas - 1) / (int32_t)ctas;
+        const int line = threadIdx.x >> 3, chunk = threadIdx.x & 7;
+        const int32_t steps = (n + 63) / 64, share = (steps + (int32_t)ctas - 1) / (int32_t)ctas;
         begin = min((int32_t)rank * share, steps);
         end = min(begin + share, steps);
+#pragma unroll
+        for (int i = 0; i < kX; ++i) {
+            const int32_t t = token_at(p.s, first + i * kStep + line);
+            x.set(i, t >= 0 ? p.x + (int64_t)t * p.ldx : nullptr, begin * 64 + chunk * 8, p.x);
+        }
+#pragma unroll
+        for (int i = 0; i < kM; ++i) {
+            const int r = r0 + i * kStep + line;
+            m.set(i, r < p.m_rows ? p.m + (int64_t)adapter * p.m_stride + (int64_t)r * p.ldm : nullptr, begin * 64 + chunk * 8, p.x);
+        }
+        place = chunk_at<128>(line, chunk);                                       // 8 rows further a chunk's place repeats
     }
-    __device__ __forceinline__ uint32_t stage(int32_t step) const { return ring + (uint32_t)((step - begin) % kShrinkStages) * kStage; }
+    __device__ __forceinline__ uint32_t stage(int32_t step) const { return ring + (uint32_t)(step - begin) % kShrinkStages * kStage; }
     __device__ __forceinline__ void fill(int32_t step) const
     {
         if (step < end) {
-            const int tid = threadIdx.x;
-            const uint32_t to = stage(step);
-            const int64_t at = (int64_t)step * 64 + (tid & 7) * 8;
+            const uint32_t to = stage(step) + place;
+            const int at = (step - begin) * 64, first = begin * 64 + (threadIdx.x & 7) * 8, left = n - first - at;
 #pragma unroll
-            for (int i = 0; i < ROWS / 16; ++i) fill_chunk<bf16, ANY>(to + chunk_at<128>(i * 16 + (tid >> 3), tid & 7), xr[i], at, n, valid);
+            for (int i = 0; i < kX; ++i) x.copy(i, to + i * kStep * 128, at, left, first);
 #pragma unroll
-            for (int i = 0; i < R / 16; ++i) fill_chunk<bf16, ANY>(to + ROWS * 128 + chunk_at<128>(i * 16 + (tid >> 3), tid & 7), mr[i], at, n, valid);
+            for (int i = 0; i < kM; ++i)
+                if (R >= kStep || (int)threadIdx.x < R * 8) m.copy(i, to + (ROWS + i * kStep) * 128, at, left, first);
         }
         copies_commit();
     }
 };
 
 // A CTA takes 128 rows of one adapter and all ranks; a cluster's CTAs share the reduction axis.
-template <int R, bool ANY> __global__ void __launch_bounds__(128) adapter_shrink_kernel(const __grid_constant__ ShrinkParams p)
+template <int R, bool ANY> __global__ void __launch_bounds__(256) adapter_shrink_kernel(const __grid_constant__ ShrinkParams p)
 {
     constexpr int kColumns = R < 32 ? 32 : R;
     extern __shared__ uint8_t smem_raw[];
@@ -314,7 +340,7 @@ template <int R, bool ANY> __global__ void __launch_bounds__(128) adapter_shrink
     }
     const int warp = warp_number(), lane = threadIdx.x & 31;
     const int adapter = adapter_of(p.s, first, lane);
-    const ShrinkCopies<R, 128, ANY> copies(p, first, 0, adapter, rank, ctas, smem);
+    const ShrinkCopies<R, 128, 256, ANY> copies(p, first, 0, adapter, rank, ctas, smem);
     bool given_up = false;
 #pragma unroll
     for (int s = 0; s < kShrinkStages - 1; ++s) copies.fill(copies.begin + s);
@@ -339,16 +365,17 @@ template <int R, bool ANY> __global__ void __launch_bounds__(128) adapter_shrink
     tc_fence_after();
     __syncthreads();
     float* part = reinterpret_cast<float*>(smem_raw + (smem - shared_at(smem_raw)));              // [128][R + 4]
-    const uint32_t lanes = c.tmem + ((uint32_t)warp << 21);
+    const uint32_t lanes = c.tmem + ((uint32_t)(warp & 3) << 21);                 // warps w and w + 4 take turns at 16 columns
 #pragma unroll
     for (int r = 0; r < R; r += 16) {
+        if ((r >> 4 & 1) != warp >> 2) continue;
         uint32_t v[16] = {};
         if (count > 0) {
             tmem_load16(v, lanes + r);
             tc_wait_ld();
         }
 #pragma unroll
-        for (int k = 0; k < 16; k += 4) *reinterpret_cast<uint4*>(part + (warp * 32 + lane) * (R + 4) + r + k) = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+        for (int k = 0; k < 16; k += 4) *reinterpret_cast<uint4*>(part + ((warp & 3) * 32 + lane) * (R + 4) + r + k) = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
     }
     products_end(c, kColumns);
     join_rows<R>(part, 128, first, 0, (p.scale != nullptr ? p.scale[adapter] : 1.f) * p.factor, p.h, p.padded, rank, ctas);
@@ -366,7 +393,7 @@ template <int R, bool ANY> __global__ void __launch_bounds__(128) adapter_shrink
     if (first >= used_rows(p.s)) return;                                          // the whole cluster
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q = lane & 3;
     const int r0 = blockIdx.y * R, adapter = adapter_of(p.s, first, lane);
-    const ShrinkCopies<R, kRows, ANY> copies(p, first, r0, adapter, rank, ctas, smem);
+    const ShrinkCopies<R, kRows, 128, ANY> copies(p, first, r0, adapter, rank, ctas, smem);
     float acc[2][kTiles][4];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -476,7 +503,8 @@ template <typename T> __device__ __forceinline__ void load_base(float* v, const 
 #pragma unroll
     for (int i = 0; i < kPer; ++i) v[i] = piece.get(i);
 }
-template <typename T> __device__ __forceinline__ void store_out(const float* v, T* row, int64_t at, int64_t n, bool whole)
+// To the columns from `at` on of a row of n, counted from anywhere.
+template <typename T, typename I> __device__ __forceinline__ void store_out(const float* v, T* row, I at, I n, bool whole)
 {
     if (at >= n) return;
     if (whole && at + kPer <= n) {
@@ -486,7 +514,7 @@ template <typename T> __device__ __forceinline__ void store_out(const float* v, 
         for (int i = 0; i < Piece<T, kPer * (int)sizeof(T)>::kWords; i += 4)
             *reinterpret_cast<uint4*>(reinterpret_cast<uint32_t*>(row + at) + i) = make_uint4(piece.w[i], piece.w[i + 1], piece.w[i + 2], piece.w[i + 3]);
     } else {
-        store8(v, row + at, (int)min((int64_t)kPer, n - at), false);
+        store8(v, row + at, (int)min((I)kPer, n - at), false);
     }
 }
 
@@ -504,41 +532,70 @@ template <typename T> __device__ void copy_row(const ExpandParams& p, int64_t to
 
 template <int ROWS> constexpr int kExpandCols = ROWS == kRows ? 128 : 64;
 
-// The copies of a CTA of 128 threads: kExpandCols columns of the base of ROWS rows, in blocks of 64, and the rows of m that make them, R of the ranks.  The rows
-// of m are laid down so that column c of block j of 8 is column 8 (c / 2) + 2 j + c % 2 of 32: a thread's results, as the tensor instructions deal them
+// The copies of a CTA: kExpandCols columns of the base of ROWS rows, in blocks of 64, and the rows of m that make them, R of the ranks.  The rows of m
+// are laid down so that column c of block j of 8 is column 8 (c / 2) + 2 j + c % 2 of 32: a thread's results, as the tensor instructions deal them
 // out, are then 8 neighbouring columns.
-template <int R, int ROWS, typename T, bool ANY> struct ExpandCopies {
+template <int R, int ROWS, int THREADS, typename T, bool ANY> struct ExpandCopies {
     static constexpr int kCols = kExpandCols<ROWS>, kBase = kCols * ROWS * (int)sizeof(T), kStage = kBase + kCols * R * 2;
     static constexpr int kChunks = 64 * (int)sizeof(T) / 16;                      // of a row's 64 columns
+    static constexpr int kPieces = kCols * (int)sizeof(T) / 16, kStep = THREADS / kPieces, kB = ROWS / kStep;      // of a row; rows apart; a thread's
+    static constexpr int kMChunks = R / 8, kMStep = THREADS / kMChunks, kM = kCols > kMStep ? kCols / kMStep : 1;
+    static_assert(kStep % 2 == 0, "a piece's place repeats from row to row");
+    RowCopies<T, kB, ANY> base;
+    const bf16* m;
+    int32_t n, m_cols;
+    int64_t m_ld;
+    uint32_t base_place, m_place;
+    bool m_whole, has_base;
     // A 16-byte piece of the base: rows alternate between the halves of a line, for threads that read four neighbouring pieces of eight rows.
     static __device__ __forceinline__ uint32_t base_at(int row, int col16)
     {
         const int block = col16 / kChunks, chunk = col16 % kChunks;
         return (uint32_t)((block * ROWS + row) * (kChunks * 16) + ((chunk ^ ((row & 1) * (kChunks / 2))) << 4));
     }
-    static __device__ __forceinline__ void fill_base(const ExpandParams& p, uint32_t stage, const int32_t* tokens, int64_t c0)
+    // c0: the first step's first column
+    __device__ __forceinline__ ExpandCopies(const ExpandParams& p, const int32_t* tokens, int adapter, int64_t c0)
+        : n((int32_t)(p.n - c0)), m_cols(p.m_cols), m_ld(p.ldm), m_whole(p.m_whole), has_base(p.base != nullptr)
     {
-        constexpr int kPieces = kCols * (int)sizeof(T) / 16;
-#pragma unroll 8
-        for (int i = threadIdx.x; i < ROWS * kPieces; i += 128) {
-            const int row = i / kPieces, c = i % kPieces;
-            const int32_t t = tokens[row];
-            fill_chunk<T, ANY>(stage + base_at(row, c), t >= 0 ? static_cast<const T*>(p.base) + (int64_t)t * p.ldb : nullptr, c0 + c * (16 / (int)sizeof(T)), p.n, p.base);
+        const int row = threadIdx.x / kPieces, c = threadIdx.x % kPieces, line = threadIdx.x / kMChunks, k = threadIdx.x % kMChunks;
+        if (has_base) {
+#pragma unroll
+            for (int i = 0; i < kB; ++i) {
+                const int32_t t = tokens[row + i * kStep];
+                base.set(i, t >= 0 ? static_cast<const T*>(p.base) + (int64_t)t * p.ldb : nullptr, c0 + c * (16 / (int)sizeof(T)), p.base);
+            }
         }
+        first = (int32_t)c0 + c * (16 / (int)sizeof(T));
+        base_place = base_at(row, c);
+        m = p.m + (int64_t)adapter * p.m_stride + (c0 + line) * p.ldm + k * 8;
+        m_place = m_at(line, k);
     }
-    static __device__ __forceinline__ void fill_m(const ExpandParams& p, uint32_t stage, const bf16* m, int64_t c0, int r0)
+    static __device__ __forceinline__ uint32_t m_at(int c, int k)
     {
-#pragma unroll 4
-        for (int i = threadIdx.x; i < kCols * R / 8; i += 128) {
-            const int c = i / (R / 8), k = i % (R / 8), at = r0 + k * 8;
-            const int slot = (c & ~31) + ((c >> 1) & 3) * 8 + ((c >> 3) & 3) * 2 + (c & 1);
-            const uint32_t to = stage + kBase + chunk_at<R * 2>(slot, k);
-            const bf16* row = c0 + c < p.n ? m + (c0 + c) * p.ldm : nullptr;
-            if (p.m_whole) {
-                fill_chunk<bf16, false>(to, row, at, p.m_cols, p.m);
+        const int slot = (c & ~31) + ((c >> 1) & 3) * 8 + ((c >> 3) & 3) * 2 + (c & 1);
+        return (uint32_t)kBase + chunk_at<R * 2>(slot, k);
+    }
+    int32_t first;
+    // Columns from `at` on (since c0), ranks from r0 on; the base with the first of them.
+    __device__ __forceinline__ void fill(uint32_t stage, int at, int r0) const
+    {
+        if (has_base && r0 == 0) {
+            const int c = (int)threadIdx.x % kPieces * (16 / (int)sizeof(T));
+#pragma unroll
+            for (int i = 0; i < kB; ++i) base.copy(i, stage + base_place + i * kStep * (kChunks * 16), at, n - at - c, first);
+        }
+        const int k = (int)threadIdx.x % kMChunks * 8 + r0, line = (int)threadIdx.x / kMChunks;
+#pragma unroll
+        for (int i = 0; i < kM; ++i) {
+            if (kMStep > kCols && line >= kCols) break;
+            const uint32_t to = stage + (kMStep % 32 == 0 ? m_place + i * kMStep * (R * 2) : m_at(line + i * kMStep, (int)threadIdx.x % kMChunks));
+            const bf16* from = m + (int64_t)(at + i * kMStep) * m_ld + r0;
+            const int left = at + line + i * kMStep < n ? m_cols - k : 0;
+            if (m_whole) {
+                copy_async(to, left > 0 ? from : m, 2 * max(0, min(8, left)));
             } else {
                 uint32_t w[4];
-                load_m<32>(w, row, at, p.m_cols, false);
+                load_m<32>(w, left > 0 ? from : nullptr, 0, left, false);
                 store_chunk(to, w);
             }
         }
@@ -558,12 +615,12 @@ template <int R, int ROWS, typename T, bool ANY> struct ExpandCopies {
     }
 };
 
-// Tokens without an adapter: 32 for a CTA of 4 warps.
+// Tokens without an adapter: 32 for a CTA.
 template <typename T> __device__ __forceinline__ void copy_tokens(const ExpandParams& p, int64_t t0, int64_t from, int64_t to)
 {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t none = __ballot_sync(0xFFFFFFFFu, t0 + lane < p.s.tokens && p.s.row_of_token[t0 + lane] < 0);
-    for (int i = warp; i < 32; i += 4)
+    for (int i = warp; i < 32; i += (int)blockDim.x / 32)
         if (none >> i & 1) copy_row<T>(p, t0 + i, from, to, lane);
 }
 
@@ -572,9 +629,9 @@ template <typename T> __device__ __forceinline__ void copy_tokens(const ExpandPa
 constexpr int kExpandStages = 4;
 template <int R, typename T> constexpr int kExpandSmem = kExpandStages * 64 * (128 * (int)sizeof(T) + R * 2) + 2 * 128 * R * 2 + 1024;
 
-template <int R, typename T, bool ANY> __global__ void __launch_bounds__(128) adapter_expand_kernel(const __grid_constant__ ExpandParams p)
+template <int R, typename T, bool ANY> __global__ void __launch_bounds__(256) adapter_expand_kernel(const __grid_constant__ ExpandParams p)
 {
-    using C = ExpandCopies<R, 128, T, ANY>;
+    using C = ExpandCopies<R, 128, 256, T, ANY>;
     constexpr int kColumns = 128;
     extern __shared__ uint8_t smem_raw[];
     __shared__ Products c;
@@ -591,32 +648,32 @@ template <int R, typename T, bool ANY> __global__ void __launch_bounds__(128) ad
         return;
     }
     const int adapter = adapter_of(p.s, first, lane);
-    const bf16* m = p.m + (int64_t)adapter * p.m_stride;
-    tokens[tid] = token_at(p.s, first + tid);
+    if (tid < 128) tokens[tid] = token_at(p.s, first + tid);
     __syncthreads();
     const uint32_t smem = (shared_at(smem_raw) + 1023u) & ~1023u, hs = smem + kExpandStages * C::kStage;
     const uint8_t* const ring = smem_raw + (smem - shared_at(smem_raw));
-    auto stage = [&](int32_t i) { return (uint32_t)(i % kExpandStages) * C::kStage; };
+    const C copies(p, tokens, adapter, begin * 64);
+    auto stage = [&](int32_t i) { return (uint32_t)i % kExpandStages * C::kStage; };
     auto fill = [&](int32_t i) {
-        if (i < count) {
-            if (p.base != nullptr) C::fill_base(p, smem + stage(i), tokens, (begin + i) * 64);
-            C::fill_m(p, smem + stage(i), m, (begin + i) * 64, 0);
-        }
+        if (i < count) copies.fill(smem + stage(i), i * 64, 0);
         copies_commit();
     };
 #pragma unroll
-    for (int i = tid; i < 128 * R / 4; i += 128) {
+    for (int i = tid; i < 128 * R / 4; i += 256) {
         const int row = i / (R / 4), part = i % (R / 4) / (R / 8), k = i % (R / 8);
-        fill_chunk<bf16, false>(hs + part * (128 * R * 2) + chunk_at<R * 2>(row, k), p.h + (first + row) * 2 * p.padded + part * p.padded, k * 8, p.padded, p.h);
+        copy_async(hs + part * (128 * R * 2) + chunk_at<R * 2>(row, k), p.h + (first + row) * 2 * p.padded + part * p.padded + k * 8, 16);
     }
 #pragma unroll
     for (int i = 0; i < kExpandStages - 2; ++i) fill(i);                          // h with the first
+    // warps w and w + 4 read the same 32 rows, 32 of the 64 columns each
+    const int row0 = (warp & 3) * 32, block = warp >> 2;
     T* out[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int32_t t = tokens[warp * 32 + i * 8 + g];
-        out[i] = t >= 0 ? static_cast<T*>(p.out) + (int64_t)t * p.ldo : nullptr;
+        const int32_t t = tokens[row0 + i * 8 + g];
+        out[i] = t >= 0 ? static_cast<T*>(p.out) + (int64_t)t * p.ldo + begin * 64 + block * 32 + q * 8 : nullptr;
     }
+    const int width = (int)(p.n - begin * 64) - block * 32 - q * 8;               // columns from the thread's first on
     bool given_up = false;
     for (int32_t n = 0; n <= count; ++n) {
         if (n < count) {
@@ -640,25 +697,21 @@ template <int R, typename T, bool ANY> __global__ void __launch_bounds__(128) ad
         const int32_t i0 = n - 1;
         products_wait(c, i0 & 1, (uint32_t)(i0 >> 1), p.status, given_up);
         tc_fence_after();
-        const uint32_t lanes = c.tmem + ((uint32_t)warp << 21) + (i0 & 1) * 64;
+        const uint32_t lanes = c.tmem + ((uint32_t)row0 << 16) + (i0 & 1) * 64 + block * 32;
+        float acc[2][4][4];
+        tmem_load_frags(acc[0], lanes);
+        tmem_load_frags(acc[1], lanes + (16u << 16));
+        tc_wait_ld();
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            float acc[2][4][4];
-            tmem_load_frags(acc[0], lanes + u * 32);
-            tmem_load_frags(acc[1], lanes + (16u << 16) + u * 32);
-            tc_wait_ld();
-            const int64_t at = (begin + i0) * 64 + u * 32 + q * 8;
+        for (int i = 0; i < 4; ++i) {
+            float v[kPer] = {};
+            if (p.base != nullptr) C::read_base(v, ring + stage(i0), row0 + i * 8 + g, block, q);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float v[kPer] = {};
-                if (p.base != nullptr) C::read_base(v, ring + stage(i0), warp * 32 + i * 8 + g, u, q);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    v[2 * j] += acc[i >> 1][j][(i & 1) * 2];
-                    v[2 * j + 1] += acc[i >> 1][j][(i & 1) * 2 + 1];
-                }
-                if (out[i] != nullptr) store_out(v, out[i], at, p.n, p.out_whole);
+            for (int j = 0; j < 4; ++j) {
+                v[2 * j] += acc[i >> 1][j][(i & 1) * 2];
+                v[2 * j + 1] += acc[i >> 1][j][(i & 1) * 2 + 1];
             }
+            if (out[i] != nullptr) store_out(v, out[i], i0 * 64, width, p.out_whole);
         }
     }
     copies_wait<0>();
@@ -671,7 +724,7 @@ template <int R, typename T> constexpr int kExpand32Smem = kExpand32Stages * 128
 
 template <int R, typename T, bool ANY> __global__ void __launch_bounds__(128) adapter_expand32_kernel(const __grid_constant__ ExpandParams p)
 {
-    using C = ExpandCopies<R, kRows, T, ANY>;
+    using C = ExpandCopies<R, kRows, 128, T, ANY>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ int32_t tokens[kRows];
     wait_for_predecessor();
@@ -685,21 +738,16 @@ template <int R, typename T, bool ANY> __global__ void __launch_bounds__(128) ad
     const int64_t first = (int64_t)blockIdx.x * kRows;
     if (first >= used_rows(p.s)) return;
     const int adapter = adapter_of(p.s, first, lane);
-    const bf16* m = p.m + (int64_t)adapter * p.m_stride;
     if (tid < kRows) tokens[tid] = token_at(p.s, first + tid);
     __syncthreads();
+    const C copies(p, tokens, adapter, begin * C::kCols);
     const uint32_t smem = (shared_at(smem_raw) + 127u) & ~127u;
     const uint8_t* const ring = smem_raw + (smem - shared_at(smem_raw));
     const int chunks = p.padded / R;                                              // of the ranks
     const int32_t turns = count * chunks;
-    auto stage = [&](int32_t i) { return (uint32_t)(i % kExpand32Stages) * C::kStage; };
+    auto stage = [&](int32_t i) { return (uint32_t)i % kExpand32Stages * C::kStage; };
     auto fill = [&](int32_t i) {                                                  // a turn is a step and a chunk of the ranks
-        if (i < turns) {
-            const int64_t c0 = (begin + i / chunks) * C::kCols;
-            const int r0 = i % chunks * R;
-            if (p.base != nullptr && r0 == 0) C::fill_base(p, smem + stage(i), tokens, c0);
-            C::fill_m(p, smem + stage(i), m, c0, r0);
-        }
+        if (i < turns) copies.fill(smem + stage(i), i / chunks * C::kCols, i % chunks * R);
         copies_commit();
     };
 #pragma unroll
@@ -836,7 +884,7 @@ constexpr int kOuterStages = 3, kOuterCols = 128, kOuterRows = 64;
 template <int R> constexpr int kOuterStage = kOuterRows * (kOuterCols + 2 * R) * 2;
 template <int R> constexpr int kOuterSmem = kOuterStages * kOuterStage<R> + 1024;
 
-template <int R, bool BY_COLUMN, bool ANY> __global__ void __launch_bounds__(128) adapter_outer_kernel(const __grid_constant__ OuterParams p)
+template <int R, bool BY_COLUMN, bool ANY> __global__ void __launch_bounds__(256) adapter_outer_kernel(const __grid_constant__ OuterParams p)
 {
     constexpr int kHalf = kOuterRows * R * 2, kColumns = R < 32 ? 32 : R;         // bytes of h's high parts; of tensor memory
     constexpr int kLines = BY_COLUMN ? kOuterCols : R, kLine = BY_COLUMN ? R : kOuterCols, kPitch = kLine + 4;
@@ -852,28 +900,38 @@ template <int R, bool BY_COLUMN, bool ANY> __global__ void __launch_bounds__(128
     const int64_t from = p.s.starts != nullptr ? p.s.starts[adapter] : 0, to = p.s.starts != nullptr ? p.s.starts[adapter + 1] : adapter == 0 ? p.s.rows : 0;
     const int32_t steps = (int32_t)((to - from + kOuterRows - 1) / kOuterRows), share = (steps + (int32_t)ctas - 1) / (int32_t)ctas;
     const int32_t begin = min((int32_t)rank * share, steps), count = min(begin + share, steps) - begin;
-    // a thread copies chunk tid % 16 of every 8th row; the tokens of a step's rows are looked up a step ahead
-    int32_t ahead[8];
+    // a thread copies chunk tid % 16 of every 16th row; the tokens of a step's rows are looked up a step ahead
+    const int line = tid >> 4;
+    int32_t ahead[4];
     auto look = [&](int32_t i) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int64_t row = from + (int64_t)(begin + i) * kOuterRows + k * 8 + (tid >> 4);
+        for (int k = 0; k < 4; ++k) {
+            const int64_t row = from + (int64_t)(begin + i) * kOuterRows + k * 16 + line;
             ahead[k] = i < count && row < to ? token_at(p.s, row) : -1;
         }
     };
-    auto stage = [&](int32_t i) { return smem + (uint32_t)(i % kOuterStages) * kOuterStage<R>; };
+    auto stage = [&](int32_t i) { return smem + (uint32_t)i % kOuterStages * kOuterStage<R>; };
+    const bf16* const z = p.z + c0 + (tid & 15) * 8;
+    const int left = (int)min((int64_t)8, p.n - c0 - (tid & 15) * 8);             // elements of the thread's chunk
+    const uint32_t z_place = ((tid & 15) >> 3) * (kOuterRows * 128) + chunk_at<128>(line, tid & 7);
+    constexpr int kHChunks = R / 4, kHStep = 256 / kHChunks, kH = kOuterRows / kHStep;             // of a row, high and low; rows apart; a thread's
+    const int h_line = tid / kHChunks, h_part = tid % kHChunks / (R / 8), h_chunk = tid % (R / 8);
+    const bf16* const h = p.h + (from + (int64_t)begin * kOuterRows + h_line) * 2 * p.padded + h_part * p.padded + r0 + h_chunk * 8;
+    const uint32_t h_place = kOuterRows * kOuterCols * 2 + h_part * kHalf + chunk_at<R * 2>(h_line, h_chunk);
+    const int32_t rows = (int32_t)min(to - from - (int64_t)begin * kOuterRows, (int64_t)count * kOuterRows);
     auto fill = [&](int32_t i) {
         if (i < count) {
-            const uint32_t zs = stage(i), hs = zs + kOuterRows * kOuterCols * 2;
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                fill_chunk<bf16, ANY>(zs + ((tid & 15) >> 3) * (kOuterRows * 128) + chunk_at<128>(k * 8 + (tid >> 4), tid & 7), ahead[k] >= 0 ? p.z + (int64_t)ahead[k] * p.ldz : nullptr,
-                                      c0 + (tid & 15) * 8, p.n, p.z);
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t at = stage(i) + z_place + k * 16 * 128;
+                if constexpr (ANY) fill_chunk<bf16, true>(at, ahead[k] >= 0 ? p.z + (int64_t)ahead[k] * p.ldz : nullptr, c0 + (tid & 15) * 8, p.n, p.z);
+                else copy_async(at, ahead[k] >= 0 && left > 0 ? z + (int64_t)ahead[k] * p.ldz : p.z, ahead[k] >= 0 ? 2 * max(0, left) : 0);
+            }
 #pragma unroll
-            for (int k = tid; k < kOuterRows * R / 4; k += 128) {
-                const int row = k / (R / 4), part = k % (R / 4) / (R / 8), chunk = k % (R / 8);
-                const int64_t at = from + (int64_t)(begin + i) * kOuterRows + row;
-                fill_chunk<bf16, false>(hs + part * kHalf + chunk_at<R * 2>(row, chunk), at < to ? p.h + at * 2 * p.padded + part * p.padded : nullptr, r0 + chunk * 8, p.padded, p.h);
+            for (int k = 0; k < kH; ++k) {
+                const int row = i * kOuterRows + k * kHStep;
+                const bool there = row + h_line < rows;
+                copy_async(stage(i) + h_place + k * kHStep * (R * 2), there ? h + (int64_t)row * 2 * p.padded : p.h, there ? 16 : 0);
             }
         }
         copies_commit();
@@ -888,12 +946,12 @@ template <int R, bool BY_COLUMN, bool ANY> __global__ void __launch_bounds__(128
         fence_async_smem();
         __syncthreads();
         if (warp == 0 && elect_one()) {
-            const uint64_t z = operand<128>(stage(n), kOuterRows * 128), h = operand<R * 2>(stage(n) + kOuterRows * kOuterCols * 2);
+            const uint64_t zs = operand<128>(stage(n), kOuterRows * 128), hs = operand<R * 2>(stage(n) + kOuterRows * kOuterCols * 2);
 #pragma unroll
             for (int part = 0; part < 2; ++part)
 #pragma unroll
                 for (int k = 0; k < kOuterRows / 16; ++k)                          // 16 rows of either further
-                    mma_bf16(c.tmem, z + k * (16 * 128 / 16), h + part * (kHalf / 16) + k * (16 * R * 2 / 16), product(R, true), n > 0 || part > 0 || k > 0);
+                    mma_bf16(c.tmem, zs + k * (16 * 128 / 16), hs + part * (kHalf / 16) + k * (16 * R * 2 / 16), product(R, true), n > 0 || part > 0 || k > 0);
             tc_commit<1>(shared_at(&c.done[n % kOuterStages]));
         }
         if (n > 0) products_wait(c, (n - 1) % kOuterStages, (uint32_t)((n - 1) / kOuterStages), p.status, given_up);
@@ -904,9 +962,11 @@ template <int R, bool BY_COLUMN, bool ANY> __global__ void __launch_bounds__(128
     tc_fence_after();
     __syncthreads();
     float* part = reinterpret_cast<float*>(smem_raw + (smem - shared_at(smem_raw)));              // [kLines][kPitch]
-    const uint32_t lanes = c.tmem + ((uint32_t)warp << 21);
+    const uint32_t lanes = c.tmem + ((uint32_t)(warp & 3) << 21);                 // warps w and w + 4 take turns at 16 ranks; a thread has a column
+    const int col = tid & 127;
 #pragma unroll
-    for (int r = 0; r < R; r += 16) {                                             // a thread has a column
+    for (int r = 0; r < R; r += 16) {
+        if ((r >> 4 & 1) != warp >> 2) continue;
         uint32_t v[16] = {};
         if (count > 0) {
             tmem_load16(v, lanes + r);
@@ -914,10 +974,10 @@ template <int R, bool BY_COLUMN, bool ANY> __global__ void __launch_bounds__(128
         }
         if constexpr (BY_COLUMN) {
 #pragma unroll
-            for (int k = 0; k < 16; k += 4) *reinterpret_cast<uint4*>(part + tid * kPitch + r + k) = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+            for (int k = 0; k < 16; k += 4) *reinterpret_cast<uint4*>(part + col * kPitch + r + k) = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
         } else {
 #pragma unroll
-            for (int k = 0; k < 16; ++k) part[(r + k) * kPitch + tid] = __uint_as_float(v[k]);
+            for (int k = 0; k < 16; ++k) part[(r + k) * kPitch + col] = __uint_as_float(v[k]);
         }
     }
     products_end(c, kColumns);
@@ -925,15 +985,15 @@ template <int R, bool BY_COLUMN, bool ANY> __global__ void __launch_bounds__(128
     cluster_wait();
     bf16* out = p.out + (int64_t)adapter * p.rank * p.n;
     const int lines = kLines / (int)ctas;
-    for (int at = tid; at < lines * (kLine / 4); at += 128) {
-        const int line = (int)rank * lines + at / (kLine / 4), e = at % (kLine / 4) * 4;
-        const float4 v = sum_remote4(shared_at(part + line * kPitch + e), ctas);
+    for (int at = tid; at < lines * (kLine / 4); at += 256) {
+        const int l = (int)rank * lines + at / (kLine / 4), e = at % (kLine / 4) * 4;
+        const float4 v = sum_remote4(shared_at(part + l * kPitch + e), ctas);
         const float f[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const int r = r0 + (BY_COLUMN ? e + k : line);
-            const int64_t col = c0 + (BY_COLUMN ? line : e + k);
-            if (r < p.rank && col < p.n) out[BY_COLUMN ? col * p.rank + r : (int64_t)r * p.n + col] = __float2bfloat16(f[k]);
+            const int r = r0 + (BY_COLUMN ? e + k : l);
+            const int64_t n = c0 + (BY_COLUMN ? l : e + k);
+            if (r < p.rank && n < p.n) out[BY_COLUMN ? n * p.rank + r : (int64_t)r * p.n + n] = __float2bfloat16(f[k]);
         }
     }
     cluster_arrive();
@@ -1252,7 +1312,7 @@ template <int R, int ROWS, bool ANY> cudaError_t shrink_launch(const ShrinkParam
     uint32_t cluster = 1;                     // as many CTAs to a tile as the GPU holds at once, two steps each at least
     while (cluster < kMaxCluster && tiles * chunks * cluster * 2 <= resident(kShrinkSmem<R, ROWS>) && steps >= 4 * cluster) cluster *= 2;
     const dim3 grid((uint32_t)tiles * cluster, chunks);
-    if constexpr (ROWS == 128) return launch_ring(adapter_shrink_kernel<R, ANY>, done, kShrinkSmem<R, ROWS>, grid, cluster, 128, st, p);
+    if constexpr (ROWS == 128) return launch_ring(adapter_shrink_kernel<R, ANY>, done, kShrinkSmem<R, ROWS>, grid, cluster, 256, st, p);
     else return launch_ring(adapter_shrink32_kernel<R, ANY>, done, kShrinkSmem<R, ROWS>, grid, cluster, 128, st, p);
 }
 cudaError_t shrink(const ShrinkParams& p, int rows, bool any, cudaStream_t st)
@@ -1275,7 +1335,7 @@ template <int R, int ROWS, typename T, bool ANY> cudaError_t expand_launch(Expan
     p.share = (int32_t)((steps + across - 1) / across);
     across = (steps + p.share - 1) / p.share;
     const dim3 grid(p.row_ctas + (p.s.starts != nullptr ? (uint32_t)(up(p.s.tokens, 32) / 32) : 0), (uint32_t)across);
-    if constexpr (ROWS == 128) return launch_ring(adapter_expand_kernel<R, T, ANY>, done, kExpandSmem<R, T>, grid, 0, 128, st, p);
+    if constexpr (ROWS == 128) return launch_ring(adapter_expand_kernel<R, T, ANY>, done, kExpandSmem<R, T>, grid, 0, 256, st, p);
     else return launch_ring(adapter_expand32_kernel<R, T, ANY>, done, kExpand32Smem<R, T>, grid, 0, 128, st, p);
 }
 template <typename T> cudaError_t expand_rows(const ExpandParams& p, int rows, cudaStream_t st)
@@ -1299,7 +1359,7 @@ template <int R, bool BY_COLUMN, bool ANY> cudaError_t outer_launch(const OuterP
     const int64_t mean = p.s.rows / p.s.adapters;      // two steps each at least, going by the adapters' mean
     uint32_t cluster = 1;
     while (cluster < kMaxCluster && (int64_t)across * deep * cluster * 2 <= resident(kOuterSmem<R>) && mean >= 4 * kOuterRows * (int64_t)cluster) cluster *= 2;
-    return launch_ring(adapter_outer_kernel<R, BY_COLUMN, ANY>, done, kOuterSmem<R>, dim3(cluster, across, deep), cluster, 128, st, p);
+    return launch_ring(adapter_outer_kernel<R, BY_COLUMN, ANY>, done, kOuterSmem<R>, dim3(cluster, across, deep), cluster, 256, st, p);
 }
 cudaError_t outer(const OuterParams& p, bool by_column, bool any, cudaStream_t st)
 {
