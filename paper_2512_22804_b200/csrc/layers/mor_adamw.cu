@@ -48,26 +48,52 @@ __host__ __device__ __forceinline__ uint32_t mix(uint32_t z)
     return z ^ (z >> 16);
 }
 
-// Largest finite magnitude of a block of 128: of 16 lanes with 8 elements each.
+// Largest magnitude of a block of 128: of 16 lanes with 8 elements each; NaN if any is NaN.  Where the result is not finite, that of the finite ones is
+// taken with a second look (a check per element would cost every block what few need).
 __device__ __forceinline__ float block_amax(const float* v)
 {
-    float a = 0.f;
+    float a = amax_of<kPer>(v);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const float x = fabsf(v[i]);
-        a = fmaxf(a, x < INFINITY ? x : 0.f);
-    }
+    for (int o = 8; o > 0; o >>= 1) a = max_nan(a, __shfl_xor_sync(0xFFFFFFFFu, a, o));
+    return a;
+}
+__device__ __noinline__ float block_amax_finite(float a)          // of this lane's largest finite magnitude
+{
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, o));
     return a;
 }
-
-// The neighbours of a magnitude w <= 448 among the E4M3 values are floor(t) d and (floor(t) + 1) d with t = w / d.
-__device__ __forceinline__ void between(float w, float& t, float& d)
+__device__ __forceinline__ float largest_finite(const float* v)
 {
-    const uint32_t e = max(__float_as_uint(w) >> 23, 121u);          // 2^-6 has the field 121; below it the distance stays the same
-    t = w * __uint_as_float((257u - e) << 23);
-    d = __uint_as_float((e - 3u) << 23);
+    float a = 0.f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) a = fmaxf(a, fabsf(v[i]) < INFINITY ? fabsf(v[i]) : 0.f);
+    return a;
+}
+
+// Between its neighbours among the E4M3 values a magnitude w <= 448 has 20 fraction bits below the three that are kept, if it is a normal one (2^-6 and up).
+// Below, the distance stays that of 2^-6: with 2^-6 added the bits lie the same way (and the sum is off by 2^-21 of a distance at most).
+__device__ __forceinline__ float to_normal(float w) { return fabsf(w) < 0x1p-6f ? copysignf(0x1p-6f, w) : 0.f; }
+// Up where t + u >= n + 1: the random bits are added below the kept ones and what is below is cut off.
+__device__ __forceinline__ float round_mean(float w, uint32_t z)
+{
+    const float off = to_normal(w);
+    return __uint_as_float((__float_as_uint(w + off) + (z << 16 >> 12)) & 0xFFF00000u) - off;
+}
+// Up where u (2 n + 1) < (t - n)(t + n), all of it times the distance's square; never zero above zero.
+__device__ __forceinline__ float round_square_mean(float w, uint32_t z)
+{
+    const float off = to_normal(w), s = w + off;
+    const float lo = __uint_as_float(__float_as_uint(s) & 0xFFF00000u) - off, d = __uint_as_float(__float_as_uint(s) & 0x7F800000u) * 0.125f;
+    const float u = __uint_as_float(0x3F800000u | (z >> 16 << 7)) - 1.f;
+    const float q = u * d * fmaf(2.f, lo, d) < (w - lo) * (w + lo) ? lo + d : lo;
+    return w > 0.f ? fmaxf(q, 0x1p-9f) : 0.f;
+}
+__device__ __forceinline__ float root_of(float v)
+{
+    float r;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
 }
 
 template <typename P, typename G, bool EIGHT, int N> __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ AdamwParams<N> p)
@@ -126,8 +152,8 @@ template <typename P, typename G, bool EIGHT, int N> __global__ void __launch_bo
             const float x = g[i] * scale;
             m[i] = fmaf(s.rest1, x, s.beta1 * m[i]);
             v[i] = fmaf(s.rest2 * x, x, s.beta2 * v[i]);
-            root[i] = sqrtf(v[i]);
-            w[i] = fmaf(-rate, m[i] / fmaf(root[i], bias2, s.eps), w[i] * keep);
+            root[i] = root_of(v[i]);                                  // both within 2 units of the last place: far below what a step is worth
+            w[i] = fmaf(-rate, __fdividef(m[i], fmaf(root[i], bias2, s.eps)), w[i] * keep);
         }
         const uint32_t high = mix((uint32_t)((uint64_t)at >> 32) ^ key);
         uint32_t z[kPer];
@@ -143,26 +169,29 @@ template <typename P, typename G, bool EIGHT, int N> __global__ void __launch_bo
         }
         store8(w, static_cast<P*>(e.param) + at, left, whole);
         if constexpr (EIGHT) {
-            const uint32_t em = power_scale(block_amax(m), 253u), ev = power_scale(block_amax(root), 253u);
+            float am = block_amax(m), av = block_amax(root);
+            const bool finite = am < INFINITY && av < INFINITY;
+            if (__any_sync(0xFFFFFFFFu, !finite)) {
+                am = block_amax_finite(largest_finite(m));
+                av = block_amax_finite(largest_finite(root));
+            }
+            const uint32_t em = power_scale(am, 253u), ev = power_scale(av, 253u);
             const float sm = __uint_as_float(em << 23), sv = __uint_as_float(ev << 23);
+            uint32_t bad = 0;                                         // elements that are not finite
+            if (!finite)
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) bad |= (fabsf(m[i]) < INFINITY ? 0u : 1u << i) | (root[i] < INFINITY ? 0u : 256u << i);
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
-                float t, d;
-                const float u = (float)(z[i] & 0xFFFFu) * 0x1p-16f;
-                between(fabsf(m[i] * sm), t, d);
-                const float q = copysignf(floorf(t + u) * d, m[i]);
-                m[i] = fabsf(m[i]) < INFINITY ? q : NAN;
+                m[i] = round_mean(m[i] * sm, z[i]);
+                v[i] = round_square_mean(root[i] * sv, z[i]);
             }
+            if (bad != 0)
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                float t, d;
-                const float u = (float)(z[i] >> 16) * 0x1p-16f, x = root[i] * sv;
-                between(x, t, d);
-                float n = floorf(t);
-                if (u * fmaf(2.f, n, 1.f) < (t - n) * (t + n)) n += 1.f;
-                if (x > 0.f) n = fmaxf(n, 1.f);
-                v[i] = root[i] < INFINITY ? n * d : NAN;
-            }
+                for (int i = 0; i < kPer; ++i) {
+                    if (bad >> i & 1) m[i] = NAN;
+                    if (bad >> (8 + i) & 1) v[i] = NAN;
+                }
             store_codes(e4m3x8(m), static_cast<uint8_t*>(e.m) + at, left, whole);
             store_codes(e4m3x8(v), static_cast<uint8_t*>(e.v) + at, left, whole);
             if (left > 0 && (threadIdx.x & 15) == 0) *reinterpret_cast<uint16_t*>(e.scales + at / 128 * 2) = (uint16_t)(em | ev << 8);

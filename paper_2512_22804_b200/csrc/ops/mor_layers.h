@@ -391,8 +391,14 @@ Tensor adapter_linear(const Tensor& x, const Matrix& w, const Tensor& a, const T
 
 // ---- optimizer
 
+// Lists of tensors where the interpreter keeps them.
+struct TensorList {
+    PyObject* const* items = nullptr;
+    size_t n = 0;
+    const Tensor& operator[](size_t i) const { return THPVariable_Unpack(items[i]); }
+};
 struct AdamwLists {
-    std::vector<Tensor> params, grads, m, v, scales;
+    TensorList params, grads, m, v, scales;
 };
 const float* one_float(const std::optional<Tensor>& t, const char* what)
 {
@@ -401,42 +407,55 @@ const float* one_float(const std::optional<Tensor>& t, const char* what)
     want(t->scalar_type() == at::kFloat && t->numel() == 1, std::string(what) + ": one FP32 value is wanted");
     return ptr<float>(*t);
 }
+// A step over hundreds of tensors: messages are made where they are needed only (as arguments they took 100 us of a call with 128 tensors).
 void adamw(const AdamwLists& l, mor_adamw_desc_t& d)
 {
-    const size_t n = l.params.size();
-    want(l.grads.size() == n && l.m.size() == n && l.v.size() == n && (l.scales.empty() || l.scales.size() == n), "the lists have different lengths");
+    const size_t n = l.params.n;
+    want(l.grads.n == n && l.m.n == n && l.v.n == n && (l.scales.n == 0 || l.scales.n == n), "the lists have different lengths");
     if (n == 0) return;
-    d.param_dtype = dtype_of(l.params[0].scalar_type(), "params");
-    d.grad_dtype = dtype_of(l.grads[0].scalar_type(), "grads");
+    const at::ScalarType param = l.params[0].scalar_type(), grad = l.grads[0].scalar_type();
+    d.param_dtype = dtype_of(param, "params");
+    d.grad_dtype = dtype_of(grad, "grads");
     d.eight_bits = l.m[0].scalar_type() == at::kFloat8_e4m3fn;
-    want(!d.eight_bits || !l.scales.empty(), "scales are wanted with moments in 8 bits");
+    want(!d.eight_bits || l.scales.n != 0, "scales are wanted with moments in 8 bits");
     const at::ScalarType state = d.eight_bits ? at::kFloat8_e4m3fn : at::kFloat;
+    const c10::DeviceIndex device = c10::cuda::current_device();
+    auto there = [device](const Tensor& t, const char* what) {
+        if (!t.is_cuda() || t.get_device() != device) on_gpu(t, what);
+    };
     std::vector<mor_adamw_tensor_t> t(n);
     std::vector<std::pair<uintptr_t, uintptr_t>> spans;
     spans.reserve(n);
+    bool in_order = true;
     for (size_t i = 0; i < n; ++i) {
         const Tensor &p = l.params[i], &g = l.grads[i], &m = l.m[i], &v = l.v[i];
-        if (p.scalar_type() != l.params[0].scalar_type() || g.scalar_type() != l.grads[0].scalar_type()) throw py::type_error("the parameters of a call have one type, and so have the gradients");
+        if (p.scalar_type() != param || g.scalar_type() != grad) throw py::type_error("the parameters of a call have one type, and so have the gradients");
         if (m.scalar_type() != state || v.scalar_type() != state) throw py::type_error("moments: all FP32 or all float8_e4m3fn are wanted");
-        on_gpu(p, "params");
-        on_gpu(g, "grads");
-        on_gpu(m, "exp_avgs");
-        on_gpu(v, "exp_avg_sqs");
+        there(p, "params");
+        there(g, "grads");
+        there(m, "exp_avgs");
+        there(v, "exp_avg_sqs");
         const int64_t numel = p.numel();
-        want(g.numel() == numel && m.numel() == numel && v.numel() == numel, "a gradient or moment has another size than its parameter");
-        want(p.is_contiguous() && g.is_contiguous() && m.is_contiguous() && v.is_contiguous(), "parameters, gradients and moments have to be contiguous");
+        if (g.numel() != numel || m.numel() != numel || v.numel() != numel) throw py::value_error("a gradient or moment has another size than its parameter");
+        if (!p.is_contiguous() || !g.is_contiguous() || !m.is_contiguous() || !v.is_contiguous()) throw py::value_error("parameters, gradients and moments have to be contiguous");
         uint8_t* scales = nullptr;
         if (d.eight_bits) {
             const Tensor& s = l.scales[i];
-            on_gpu(s, "scales");
-            want(s.scalar_type() == at::kByte && s.is_contiguous() && s.dim() == 2 && s.size(0) == (numel + 127) / 128 && s.size(1) == 2, "scales: contiguous uint8 [blocks of 128, 2] is wanted");
+            there(s, "scales");
+            if (s.scalar_type() != at::kByte || !s.is_contiguous() || s.dim() != 2 || s.size(0) != (numel + 127) / 128 || s.size(1) != 2)
+                throw py::value_error("scales: contiguous uint8 [blocks of 128, 2] is wanted");
             scales = ptr<uint8_t>(s);
         }
         t[i] = {p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), scales, numel};
-        if (numel > 0) spans.push_back({(uintptr_t)p.data_ptr(), (uintptr_t)p.data_ptr() + p.nbytes()});
+        if (numel == 0) continue;
+        const uintptr_t at = (uintptr_t)t[i].param;
+        in_order = in_order && (spans.empty() || spans.back().second <= at);
+        spans.push_back({at, at + p.nbytes()});
     }
-    std::sort(spans.begin(), spans.end());
-    for (size_t i = 1; i < spans.size(); ++i) want(spans[i].first >= spans[i - 1].second, "parameters may not share memory");
+    if (!in_order) {
+        std::sort(spans.begin(), spans.end());
+        for (size_t i = 1; i < spans.size(); ++i) want(spans[i].first >= spans[i - 1].second, "parameters may not share memory");
+    }
     for (size_t i = 0; i < n; ++i) {                        // changed in place: autograd has to see it
         l.params[i].unsafeGetTensorImpl()->bump_version();
         l.m[i].unsafeGetTensorImpl()->bump_version();

@@ -564,18 +564,15 @@ public:
         return r;
     }
     bool is_tensor(size_t i) const { return v_[i] != nullptr && THPVariable_Check(v_[i]); }
-    std::vector<Tensor> tensors(size_t i) const
+    TensorList tensors(size_t i) const
     {
-        std::vector<Tensor> r;
+        TensorList r;
         if (v_[i] == nullptr) return r;
         if (!PyList_Check(v_[i]) && !PyTuple_Check(v_[i])) wrong(i, "a list of tensors");
-        const size_t n = (size_t)PySequence_Fast_GET_SIZE(v_[i]);
-        PyObject** items = PySequence_Fast_ITEMS(v_[i]);
-        r.reserve(n);
-        for (size_t k = 0; k < n; ++k) {
-            if (!THPVariable_Check(items[k])) wrong(i, "a list of tensors");
-            r.push_back(THPVariable_Unpack(items[k]));
-        }
+        r.n = (size_t)PySequence_Fast_GET_SIZE(v_[i]);
+        r.items = PySequence_Fast_ITEMS(v_[i]);
+        for (size_t k = 0; k < r.n; ++k)
+            if (!THPVariable_Check(r.items[k])) wrong(i, "a list of tensors");
         return r;
     }
     bool is_operand(size_t i) const { return v_[i] != nullptr && Py_TYPE(v_[i]) == &operand_type; }
