@@ -73,27 +73,34 @@ __device__ __forceinline__ float largest_finite(const float* v)
 
 // Between its neighbours among the E4M3 values a magnitude w <= 448 has 20 fraction bits below the three that are kept, if it is a normal one (2^-6 and up).
 // Below, the distance stays that of 2^-6: with 2^-6 added the bits lie the same way (and the sum is off by 2^-21 of a distance at most).
-__device__ __forceinline__ float to_normal(float w) { return fabsf(w) < 0x1p-6f ? copysignf(0x1p-6f, w) : 0.f; }
 // Up where t + u >= n + 1: the random bits are added below the kept ones and what is below is cut off.
 __device__ __forceinline__ float round_mean(float w, uint32_t z)
 {
-    const float off = to_normal(w);
+    const float off = fabsf(w) < 0x1p-6f ? copysignf(0x1p-6f, w) : 0.f;
     return __uint_as_float((__float_as_uint(w + off) + (z << 16 >> 12)) & 0xFFF00000u) - off;
 }
-// Up where u (2 n + 1) < (t - n)(t + n), all of it times the distance's square; never zero above zero.
+// Of a w that is not negative.  Up where u (2 n + 1) < (t - n)(t + n), all of it times the distance's square; never zero above zero.
 __device__ __forceinline__ float round_square_mean(float w, uint32_t z)
 {
-    const float off = to_normal(w), s = w + off;
+    const float off = w < 0x1p-6f ? 0x1p-6f : 0.f, s = w + off;
     const float lo = __uint_as_float(__float_as_uint(s) & 0xFFF00000u) - off, d = __uint_as_float(__float_as_uint(s) & 0x7F800000u) * 0.125f;
     const float u = __uint_as_float(0x3F800000u | (z >> 16 << 7)) - 1.f;
     const float q = u * d * fmaf(2.f, lo, d) < (w - lo) * (w + lo) ? lo + d : lo;
-    return w > 0.f ? fmaxf(q, 0x1p-9f) : 0.f;
+    return fmaxf(q, w > 0.f ? 0x1p-9f : 0.f);
 }
+// One instruction each, within 2 units of the last place: far below what a step is worth.  A second moment below 2^-126 counts as zero, and what is divided by
+// is at least the root of that.
 __device__ __forceinline__ float root_of(float v)
 {
     float r;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
+}
+__device__ __forceinline__ float quotient(float m, float d)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(fmaxf(d, 0x1p-63f)));
+    return m * r;
 }
 
 template <typename P, typename G, bool EIGHT, int N> __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ AdamwParams<N> p)
@@ -152,8 +159,8 @@ template <typename P, typename G, bool EIGHT, int N> __global__ void __launch_bo
             const float x = g[i] * scale;
             m[i] = fmaf(s.rest1, x, s.beta1 * m[i]);
             v[i] = fmaf(s.rest2 * x, x, s.beta2 * v[i]);
-            root[i] = root_of(v[i]);                                  // both within 2 units of the last place: far below what a step is worth
-            w[i] = fmaf(-rate, __fdividef(m[i], fmaf(root[i], bias2, s.eps)), w[i] * keep);
+            root[i] = root_of(v[i]);
+            w[i] = fmaf(-rate, quotient(m[i], fmaf(root[i], bias2, s.eps)), w[i] * keep);
         }
         const uint32_t high = mix((uint32_t)((uint64_t)at >> 32) ^ key);
         uint32_t z[kPer];
@@ -161,13 +168,26 @@ template <typename P, typename G, bool EIGHT, int N> __global__ void __launch_bo
 #pragma unroll
             for (int i = 0; i < kPer; ++i) z[i] = mix(high + (uint32_t)at + i);
         if constexpr (sizeof(P) == 2) {
+            // NaN, whose bits may all be set, must not be carried into the sign
+            const bool any_nan = !(amax_of<kPer>(w) <= INFINITY);
+            uint32_t b[kPer];
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) {
-                const uint32_t b = __float_as_uint(w[i]);
-                if (fabsf(w[i]) < INFINITY) w[i] = __uint_as_float((b + (mix(z[i] ^ 0x9E3779B9u) & 0xFFFFu)) & 0xFFFF0000u);
+            for (int i = 0; i < kPer; ++i) b[i] = __float_as_uint(w[i]) + (mix(z[i] ^ 0x9E3779B9u) & 0xFFFFu);
+            if (any_nan)
+#pragma unroll
+                for (int i = 0; i < kPer; ++i)
+                    if (isnan(w[i])) b[i] = 0x7FC00000u;
+            if (whole) {
+                *reinterpret_cast<uint4*>(static_cast<P*>(e.param) + at) =
+                    make_uint4(__byte_perm(b[0], b[1], 0x7632), __byte_perm(b[2], b[3], 0x7632), __byte_perm(b[4], b[5], 0x7632), __byte_perm(b[6], b[7], 0x7632));
+            } else {
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) w[i] = __uint_as_float(b[i] & 0xFFFF0000u);
+                store8(w, static_cast<P*>(e.param) + at, left, false);
             }
+        } else {
+            store8(w, static_cast<P*>(e.param) + at, left, whole);
         }
-        store8(w, static_cast<P*>(e.param) + at, left, whole);
         if constexpr (EIGHT) {
             float am = block_amax(m), av = block_amax(root);
             const bool finite = am < INFINITY && av < INFINITY;

@@ -66,11 +66,9 @@ __device__ __forceinline__ void store_codes(uint2 c, uint8_t* at, int left, bool
 // Biased exponent of the largest power of two that keeps a >= 0 within 448 = 1.75 * 2^8, at most `most`; 127 for zero.
 __device__ __forceinline__ uint32_t power_scale(float a, uint32_t most)
 {
-    if (a == 0.f) return 127u;
-    const uint32_t b = __float_as_uint(a);
-    // 2 * 127 + 8 - field of a, one less where a's fraction is above 1.75.  Subnormal values are far below what `most` leaves of it.
-    const int e = 262 - (int)(b >> 23) - ((b & 0x7FFFFFu) > 0x600000u ? 1 : 0);
-    return min((uint32_t)max(e, 1), most);
+    // 2 * 127 + 8 - field of a, one less where a's fraction is above 1.75: it then carries.  Subnormal values are far below what `most` leaves of it.
+    const int e = 262 - (int)((__float_as_uint(a) + 0x1FFFFFu) >> 23);
+    return a == 0.f ? 127u : min((uint32_t)max(e, 1), most);
 }
 // 1 / 2^(e - 127) for a biased exponent of 0 .. 254, exact.
 __device__ __forceinline__ float inverse_power(uint32_t e) { return e >= 254u ? 0x1p-127f : __uint_as_float((254u - e) << 23); }
