@@ -488,7 +488,7 @@ MOR_API mor_status_t mor_adapter_grad(const mor_adapter_desc_t* host_desc, const
  * AdamW with the decay apart from the gradient, over many tensors with one launch for every 512.  With g the gradient times grad_scale:
  *   m = beta1 m + (1 - beta1) g       v = beta2 v + (1 - beta2) g^2
  *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
- * in binary32; a second moment below 2^-126 counts as zero, and what is divided by is at least 2^-63.  Parameters and gradients are BF16 or FP32.  The moments are FP32, or 8 bits: blocks of 128 consecutive elements share a
+ * in binary32; a second moment below 2^-126 counts as zero, and eps is 2^-63 at least.  Parameters and gradients are BF16 or FP32.  The moments are FP32, or 8 bits: blocks of 128 consecutive elements share a
  * power of two s, the largest that keeps the block's largest finite magnitude times s within 448 (kept as a biased exponent, at most 253; 127
  * for a block of zeros); the first moment is an E4M3 code of m s, the second of w = sqrt(v) s, so that an element may be 2^17 below its
  * block's largest and still count.  Nearest rounding would stop a moment that moves by a thousandth a step, so codes are rounded up or down by a
