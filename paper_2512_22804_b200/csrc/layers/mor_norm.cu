@@ -121,6 +121,41 @@ __device__ __forceinline__ float make_scale(const NormParams& p, float a, int64_
     return s;
 }
 
+// A thread's pieces of its next row come by asynchronous copies into its own part of shared memory while it works on this one; that asks for no
+// barrier and no registers.  Places are counted in 16 bytes of every thread.
+constexpr int kRing = 2;
+template <typename T, int N, int THREADS, int G> struct RowRing {
+    static constexpr int kUnits = kPer * (int)sizeof(T) / 16, kPlaces = N * kUnits;
+    static __device__ __forceinline__ void fetch(uint32_t to, const T* row, int i, int32_t cols)
+    {
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+            const int32_t at = (c * G + i) * kPer;
+            const int bytes = at < cols ? 16 : 0;
+#pragma unroll
+            for (int k = 0; k < kUnits; ++k)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                             ::"r"(to + (c * kUnits + k) * THREADS * 16), "l"(reinterpret_cast<const uint4*>(row + (at < cols ? at : 0)) + k), "r"(bytes) : "memory");
+        }
+    }
+    static __device__ __forceinline__ void take(float* v, uint32_t from, int c)
+    {
+        Piece<T, kPer * (int)sizeof(T)> piece;
+#pragma unroll
+        for (int k = 0; k < kUnits; ++k)
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(piece.w[4 * k]), "=r"(piece.w[4 * k + 1]), "=r"(piece.w[4 * k + 2]), "=r"(piece.w[4 * k + 3])
+                         : "r"(from + (c * kUnits + k) * THREADS * 16) : "memory");
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) v[k] = piece.get(k);
+    }
+};
+__device__ __forceinline__ void ring_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void ring_wait() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }
+// Rows' bytes that one thread has in the ring.
+template <typename T, typename R, int N> constexpr int kForwardRing = kRing * N * kPer * (int)(sizeof(T) + sizeof(R));
+template <typename T, typename R, int G, int N> constexpr bool kAhead = kForwardRing<T, R, N> * (G > 256 ? G : 256) <= 220 * 1024;    // else the row alone fills it
+template <typename T, typename R, int N> constexpr int kGradRing = kRing * N * kPer * (int)(sizeof(T) + 2 * sizeof(R));
+
 template <int G> constexpr int kForwardThreads = G > 256 ? G : 256;
 
 template <typename T, typename R, int G, int N, bool ANY> __global__ void __launch_bounds__(kForwardThreads<G>) norm_kernel(const __grid_constant__ NormParams p)
@@ -133,17 +168,44 @@ template <typename T, typename R, int G, int N, bool ANY> __global__ void __laun
 #pragma unroll
     for (int c = 0; c < N; ++c) load_weight(w[c], p.w, p.weight_dtype, (c * G + i) * kPer, p.cols);
     const int32_t blocks = p.by_row ? 1 : (p.cols + 127) >> 7;
+    // where there is more than one row for a group, the next one is on its way
+    constexpr int kThreads = kForwardThreads<G>;
+    using XRing = RowRing<T, N, kThreads, G>;
+    using RRing = RowRing<R, N, kThreads, G>;
+    extern __shared__ __align__(16) uint8_t ring[];
+    const int64_t step = (int64_t)gridDim.x * kGroups;
+    const bool ahead = !ANY && kAhead<T, R, G, N> && p.rows > step;
+    const uint32_t own = (uint32_t)__cvta_generic_to_shared(ring) + threadIdx.x * 16;
+    auto place = [&](int turn) { return own + turn * (XRing::kPlaces + RRing::kPlaces) * kThreads * 16; };
+    auto fetch = [&](int64_t row, int turn) {
+        if (row < p.rows) {
+            XRing::fetch(place(turn), static_cast<const T*>(p.x) + row * p.ldx, i, p.cols);
+            if (p.r != nullptr) RRing::fetch(place(turn) + XRing::kPlaces * kThreads * 16, static_cast<const R*>(p.r) + row * p.ldr, i, p.cols);
+        }
+        ring_commit();
+    };
     int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * kGroups + group; row < p.rows; row += (int64_t)gridDim.x * kGroups, turn ^= 1) {
+    if (ahead) fetch((int64_t)blockIdx.x * kGroups + group, 0);
+    for (int64_t row = (int64_t)blockIdx.x * kGroups + group; row < p.rows; row += step, turn ^= 1) {
         float v[N][kPer];
+        if (ahead) {
+            fetch(row + step, turn ^ 1);
+            ring_wait();
+        }
         const T* x = static_cast<const T*>(p.x) + row * p.ldx;
 #pragma unroll
-        for (int c = 0; c < N; ++c) load_piece<T, ANY>(v[c], x, (c * G + i) * kPer, p.cols);
+        for (int c = 0; c < N; ++c) {
+            if (ahead) XRing::take(v[c], place(turn), c);
+            else load_piece<T, ANY>(v[c], x, (c * G + i) * kPer, p.cols);
+        }
         if (p.r != nullptr) {
             const R* r = static_cast<const R*>(p.r) + row * p.ldr;
             float add[N][kPer];
 #pragma unroll
-            for (int c = 0; c < N; ++c) load_piece<R, ANY>(add[c], r, (c * G + i) * kPer, p.cols);
+            for (int c = 0; c < N; ++c) {
+                if (ahead) RRing::take(add[c], place(turn) + XRing::kPlaces * kThreads * 16, c);
+                else load_piece<R, ANY>(add[c], r, (c * G + i) * kPer, p.cols);
+            }
 #pragma unroll
             for (int c = 0; c < N; ++c) {
 #pragma unroll
@@ -284,7 +346,7 @@ template <typename T, typename R, int G, int N, bool ANY> __global__ void __laun
 {
     constexpr int kGroups = kGradThreads<G> / G;
     __shared__ float shared[kGroups][2][2][G / 32];
-    extern __shared__ float total[];                // [cols], with more than one group
+    extern __shared__ __align__(16) float total[];  // [cols] with more than one group, after the rows; before, the ring
     const int group = threadIdx.x / G, i = threadIdx.x % G;
     wait_for_predecessor();
     float w[N][kPer], dw[N][kPer];
@@ -294,15 +356,41 @@ template <typename T, typename R, int G, int N, bool ANY> __global__ void __laun
 #pragma unroll
         for (int k = 0; k < kPer; ++k) dw[c][k] = 0.f;
     }
+    constexpr int kThreads = kGradThreads<G>;
+    using HRing = RowRing<R, N, kThreads, G>;
+    using GRing = RowRing<T, N, kThreads, G>;
+    const int64_t step = (int64_t)gridDim.x * kGroups;
+    const bool ahead = !ANY && p.rows > step;
+    const uint32_t own = (uint32_t)__cvta_generic_to_shared(total) + threadIdx.x * 16;
+    constexpr uint32_t kG = HRing::kPlaces * kThreads * 16, kD = kG + GRing::kPlaces * kThreads * 16, kStage = kD + HRing::kPlaces * kThreads * 16;
+    auto fetch = [&](int64_t row, int turn) {
+        if (row < p.rows) {
+            HRing::fetch(own + turn * kStage, static_cast<const R*>(p.x) + row * p.ldx, i, p.cols);
+            GRing::fetch(own + turn * kStage + kG, static_cast<const T*>(p.dy) + row * p.lddy, i, p.cols);
+            if (p.r != nullptr) HRing::fetch(own + turn * kStage + kD, static_cast<const R*>(p.r) + row * p.ldr, i, p.cols);
+        }
+        ring_commit();
+    };
     int turn = 0;
-    for (int64_t row = (int64_t)blockIdx.x * kGroups + group; row < p.rows; row += (int64_t)gridDim.x * kGroups, turn ^= 1) {
+    if (ahead) fetch((int64_t)blockIdx.x * kGroups + group, 0);
+    for (int64_t row = (int64_t)blockIdx.x * kGroups + group; row < p.rows; row += step, turn ^= 1) {
         float h[N][kPer], g[N][kPer];
+        if (ahead) {
+            fetch(row + step, turn ^ 1);
+            ring_wait();
+        }
         const R* hr = static_cast<const R*>(p.x) + row * p.ldx;
         const T* dy = static_cast<const T*>(p.dy) + row * p.lddy;
 #pragma unroll
-        for (int c = 0; c < N; ++c) load_piece<R, ANY>(h[c], hr, (c * G + i) * kPer, p.cols);
+        for (int c = 0; c < N; ++c) {
+            if (ahead) HRing::take(h[c], own + turn * kStage, c);
+            else load_piece<R, ANY>(h[c], hr, (c * G + i) * kPer, p.cols);
+        }
 #pragma unroll
-        for (int c = 0; c < N; ++c) load_piece<T, ANY>(g[c], dy, (c * G + i) * kPer, p.cols);
+        for (int c = 0; c < N; ++c) {
+            if (ahead) GRing::take(g[c], own + turn * kStage + kG, c);
+            else load_piece<T, ANY>(g[c], dy, (c * G + i) * kPer, p.cols);
+        }
         float square = 0.f, dot = 0.f;
 #pragma unroll
         for (int c = 0; c < N; ++c)
@@ -345,7 +433,8 @@ template <typename T, typename R, int G, int N, bool ANY> __global__ void __laun
             }
             if (p.r != nullptr) {
                 float add[kPer];
-                load_piece<R, ANY>(add, static_cast<const R*>(p.r) + row * p.ldr, at, p.cols);
+                if (ahead) HRing::take(add, own + turn * kStage + kD, c);
+                else load_piece<R, ANY>(add, static_cast<const R*>(p.r) + row * p.ldr, at, p.cols);
 #pragma unroll
                 for (int k = 0; k < kPer; ++k) d[k] += add[k];
             }
@@ -355,6 +444,10 @@ template <typename T, typename R, int G, int N, bool ANY> __global__ void __laun
     }
     if (p.partial == nullptr) return;
     float* out = p.partial + (int64_t)blockIdx.x * p.cols;
+    if constexpr (kGroups > 1) {
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncthreads();                            // the ring's place is free
+    }
 #pragma unroll 1
     for (int turn = 0; turn < kGroups; ++turn) {
         if (group == turn) {
@@ -496,9 +589,13 @@ template <typename T> __global__ void __launch_bounds__(256) codes_values_kernel
 template <typename T, typename R, int G, int N> cudaError_t norm_launch(const NormParams& p, bool any, cudaStream_t st)
 {
     constexpr int kThreads = kForwardThreads<G>, kGroups = kThreads / G;
-    const int64_t need = ceil_div(p.rows, kGroups);
-    const uint32_t grid = (uint32_t)(need < kSms * 2048 / kThreads ? need : kSms * 2048 / kThreads);
-    return any ? launch(norm_kernel<T, R, G, N, true>, grid, kThreads, 0, st, true, p) : launch(norm_kernel<T, R, G, N, false>, grid, kThreads, 0, st, true, p);
+    constexpr int kSmem = kAhead<T, R, G, N> ? kForwardRing<T, R, N> * kThreads : 0, kFit = 227 * 1024 / (kSmem + 1024), kMost = 1024 / kThreads;      // 64 registers a thread
+    static std::atomic<uint64_t> done{0};
+    if (!allow_smem(norm_kernel<T, R, G, N, false>, kSmem, done)) return cudaErrorUnknown;
+    const int64_t need = ceil_div(p.rows, kGroups), held = kSms * (kFit < kMost ? kFit : kMost);
+    const uint32_t grid = (uint32_t)(need < held ? need : held);
+    return any ? launch(norm_kernel<T, R, G, N, true>, grid, kThreads, 0, st, true, p)
+               : launch(norm_kernel<T, R, G, N, false>, grid, kThreads, need > held ? (size_t)kSmem : 0, st, true, p);
 }
 template <typename T, typename R> cudaError_t norm_width(const NormParams& p, bool any, cudaStream_t st)
 {
@@ -522,7 +619,10 @@ int64_t grad_ctas(int64_t rows, int64_t cols)
 template <typename T, typename R, int G, int N> cudaError_t grad_launch(const NormParams& p, uint32_t grid, bool any, cudaStream_t st)
 {
     constexpr int kThreads = kGradThreads<G>, kGroups = kThreads / G;
-    const size_t smem = kGroups > 1 ? (size_t)p.cols * 4 : 0;
+    const size_t sums = kGroups > 1 ? (size_t)p.cols * 4 : 0, ring = (size_t)kGradRing<T, R, N> * kThreads;
+    static std::atomic<uint64_t> done{0};
+    if (!allow_smem(norm_grad_kernel<T, R, G, N, false>, (int)ring, done)) return cudaErrorUnknown;
+    const size_t smem = !any && p.rows > (int64_t)grid * kGroups && ring > sums ? ring : sums;
     return any ? launch(norm_grad_kernel<T, R, G, N, true>, grid, kThreads, smem, st, true, p)
                : launch(norm_grad_kernel<T, R, G, N, false>, grid, kThreads, smem, st, true, p);
 }
