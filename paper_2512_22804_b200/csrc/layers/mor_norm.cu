@@ -550,38 +550,45 @@ template <typename W> __global__ void __launch_bounds__(kJoinCols* kJoinParts) n
 
 // ------------------------------------------------------------------------------------------- values ----
 
-// 16 codes a thread: 16 bytes in, 32 or 64 out.
+// 16 codes a thread at a time, of kValueRows rows: 16 bytes in, 32 or 64 out.
+constexpr int kValueRows = 4;
 template <typename T> __global__ void __launch_bounds__(256) codes_values_kernel(const uint8_t* codes, int64_t rows, int32_t cols, int64_t ldc, int32_t by_row,
                                                                                  const uint8_t* e8m0, const float* f32, T* out, int64_t ldo, bool aligned)
 {
     wait_for_predecessor();
     const int32_t at = (blockIdx.y * blockDim.x + threadIdx.x) * 16, blocks = by_row ? 1 : (cols + 127) >> 7;
-    const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-    if (row >= rows || at >= cols) return;
-    const int64_t s = row * blocks + (by_row ? 0 : at >> 7);
-    const uint8_t* from = codes + row * ldc + at;
-    T* to = out + row * ldo + at;
-    float v[16];
+    const int64_t row0 = (int64_t)blockIdx.x * (kValueRows * blockDim.y) + threadIdx.y;
+    if (at >= cols) return;
     const bool whole = aligned && at + 16 <= cols;
-    if (whole) {
-        const uint4 c = *reinterpret_cast<const uint4*>(from);
-        e4m3x8_values(v, make_uint2(c.x, c.y));
-        e4m3x8_values(v + 8, make_uint2(c.z, c.w));
-    } else {
-        e4m3x8_values(v, load_codes(from, cols - at, false));
-        e4m3x8_values(v + 8, load_codes(from + 8, cols - at - 8, false));
-    }
-    if (e8m0 != nullptr) {
-        const float q = inverse_power(e8m0[s]);
+    uint4 c[kValueRows];
+    float s[kValueRows];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) v[k] *= q;
-    } else {
-        const float d = f32[s];
-#pragma unroll
-        for (int k = 0; k < 16; ++k) v[k] /= d;
+    for (int k = 0; k < kValueRows; ++k) {
+        const int64_t row = row0 + k * blockDim.y;
+        if (row >= rows) break;
+        const uint8_t* from = codes + row * ldc + at;
+        if (whole) {
+            c[k] = *reinterpret_cast<const uint4*>(from);
+        } else {
+            const uint2 lo = load_codes(from, cols - at, false), hi = load_codes(from + 8, cols - at - 8, false);
+            c[k] = make_uint4(lo.x, lo.y, hi.x, hi.y);
+        }
+        const int64_t i = row * blocks + (by_row ? 0 : at >> 7);
+        s[k] = e8m0 != nullptr ? inverse_power(e8m0[i]) : f32[i];
     }
-    store8(v, to, cols - at, whole);
-    store8(v + 8, to + 8, cols - at - 8, whole);
+#pragma unroll
+    for (int k = 0; k < kValueRows; ++k) {
+        const int64_t row = row0 + k * blockDim.y;
+        if (row >= rows) break;
+        float v[16];
+        e4m3x8_values(v, make_uint2(c[k].x, c[k].y));
+        e4m3x8_values(v + 8, make_uint2(c[k].z, c[k].w));
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] = e8m0 != nullptr ? v[j] * s[k] : v[j] / s[k];
+        T* to = out + row * ldo + at;
+        store8(v, to, cols - at, whole);
+        store8(v + 8, to + 8, cols - at - 8, whole);
+    }
 }
 
 // ------------------------------------------------------------------------------------------- host side ----
@@ -786,7 +793,7 @@ mor_status_t mor_codes_dequantize(const uint8_t* codes, int64_t rows, int64_t co
     const int64_t pieces = ceil_div(cols, 16);
     const uint32_t x = pieces >= 256 ? 256u : (uint32_t)ceil_div(pieces, 32) * 32, y = 256 / x;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((uint32_t)ceil_div(rows, y), (uint32_t)ceil_div(pieces, x));
+    cfg.gridDim = dim3((uint32_t)ceil_div(rows, y * kValueRows), (uint32_t)ceil_div(pieces, x));
     if (cfg.gridDim.y > 65535u) return MOR_ERR_INVALID_ARG;
     cfg.blockDim = dim3(x, y);
     cfg.stream = static_cast<cudaStream_t>(cuda_stream);

@@ -30,7 +30,7 @@ int64_t rows_of(const Tensor& t)
 Tensor as_rows(const Tensor& t) { return apart(t.dim() == 2 ? t : t.reshape({rows_of(t), t.size(-1)})); }
 void want_shape(const Tensor& t, const Tensor& like, const char* what)
 {
-    want(t.sizes() == like.sizes(), std::string(what) + " has another shape");
+    if (t.sizes() != like.sizes()) throw py::value_error(std::string(what) + " has another shape");
 }
 
 // ---- norm
@@ -211,7 +211,8 @@ Adapters adapter_args(const Tensor& x, int64_t n_out, const Tensor& a, const Ten
     want(x.dim() >= 1 && (a.dim() == 2 || a.dim() == 3) && b.dim() == a.dim(), "x [..., n_in], a [adapters, rank, n_in] and b [adapters, n_out, rank] are wanted");
     const int64_t n = a.dim() == 3 ? a.size(0) : 1, rank = a.size(-2);
     want(a.size(-1) == x.size(-1) && b.size(-1) == rank && b.size(-2) == n_out && (b.dim() == 2 || b.size(0) == n), "x [..., n_in], a [adapters, rank, n_in] and b [adapters, n_out, rank] are wanted");
-    want(n >= 1 && n < MOR_MAX_GROUPS && rank >= 1 && rank <= MOR_MAX_RANK, "1 to " + std::to_string(MOR_MAX_GROUPS - 1) + " adapters of a rank of 1 to " + std::to_string(MOR_MAX_RANK) + " are wanted");
+    if (n < 1 || n >= MOR_MAX_GROUPS || rank < 1 || rank > MOR_MAX_RANK)
+        throw py::value_error("1 to " + std::to_string(MOR_MAX_GROUPS - 1) + " adapters of a rank of 1 to " + std::to_string(MOR_MAX_RANK) + " are wanted");
     if (x.scalar_type() != at::kBFloat16 || a.scalar_type() != at::kBFloat16 || b.scalar_type() != at::kBFloat16) throw py::type_error("x, a and b: BF16 is wanted");
     on_gpu(x, "x");
     on_gpu(a, "a");

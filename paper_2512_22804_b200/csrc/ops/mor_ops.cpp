@@ -41,6 +41,10 @@ void want(bool ok, const std::string& message)
 {
     if (!ok) throw py::value_error(message);
 }
+void want(bool ok, const char* message)
+{
+    if (!ok) throw py::value_error(message);
+}
 int format_of(PyObject* f)
 {
     if (f != nullptr && PyLong_Check(f)) {
@@ -63,13 +67,13 @@ int dtype_of(at::ScalarType t, const char* what)
 // Calls run on the current device's current stream, so that is where their tensors have to be.
 void on_gpu(const Tensor& t, const char* what)
 {
-    want(t.is_cuda(), std::string(what) + " has to be a CUDA tensor");
+    if (!t.is_cuda()) throw py::value_error(std::string(what) + " has to be a CUDA tensor");
     const int at = t.get_device(), now = c10::cuda::current_device();
-    want(at == now, std::string(what) + " is on device " + std::to_string(at) + ", the current device is " + std::to_string(now));
+    if (at != now) throw py::value_error(std::string(what) + " is on device " + std::to_string(at) + ", the current device is " + std::to_string(now));
 }
 void rows_contiguous(const Tensor& t, const char* what)
 {
-    want(t.size(-1) <= 1 || t.stride(-1) == 1, std::string(what) + ": the last dimension has to be contiguous");
+    if (t.size(-1) > 1 && t.stride(-1) != 1) throw py::value_error(std::string(what) + ": the last dimension has to be contiguous");
 }
 void* stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
 template <typename T> T* ptr(const Tensor& t) { return static_cast<T*>(t.data_ptr()); }
@@ -287,7 +291,7 @@ Tensor dequantize(const Matrix& m, at::ScalarType type)
 
 mor_expert_desc_t expert_desc(const Routes& p, const Tensor& m, const std::optional<Tensor>& weight, const char* what)
 {
-    want(m.dim() == 2, std::string(what) + ": a matrix is wanted");
+    if (m.dim() != 2) throw py::value_error(std::string(what) + ": a matrix is wanted");
     on_gpu(m, what);
     on_gpu(p.row, "plan");
     rows_contiguous(m, what);
