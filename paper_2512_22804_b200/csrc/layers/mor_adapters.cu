@@ -535,8 +535,10 @@ template <int ROWS> constexpr int kExpandCols = ROWS == kRows ? 128 : 64;
 // The copies of a CTA: kExpandCols columns of the base of ROWS rows, in blocks of 64, and the rows of m that make them, R of the ranks.  The rows of m
 // are laid down so that column c of block j of 8 is column 8 (c / 2) + 2 j + c % 2 of 32: a thread's results, as the tensor instructions deal them
 // out, are then 8 neighbouring columns.
-template <int R, int ROWS, int THREADS, typename T, bool ANY> struct ExpandCopies {
-    static constexpr int kCols = kExpandCols<ROWS>, kBase = kCols * ROWS * (int)sizeof(T), kStage = kBase + kCols * R * 2;
+enum Base : int { NO_BASE, WHOLE_BASE, ANY_BASE };      // none; rows that start on 16 bytes; rows that start anywhere
+template <int R, int ROWS, int THREADS, typename T, int BASE> struct ExpandCopies {
+    static constexpr bool ANY = BASE == ANY_BASE, kHas = BASE != NO_BASE;
+    static constexpr int kCols = kExpandCols<ROWS>, kBase = kHas ? kCols * ROWS * (int)sizeof(T) : 0, kStage = kBase + kCols * R * 2;
     static constexpr int kChunks = 64 * (int)sizeof(T) / 16;                      // of a row's 64 columns
     static constexpr int kPieces = kCols * (int)sizeof(T) / 16, kStep = THREADS / kPieces, kB = ROWS / kStep;      // of a row; rows apart; a thread's
     static constexpr int kMChunks = R / 8, kMStep = THREADS / kMChunks, kM = kCols > kMStep ? kCols / kMStep : 1;
@@ -546,7 +548,7 @@ template <int R, int ROWS, int THREADS, typename T, bool ANY> struct ExpandCopie
     int32_t n, m_cols;
     int64_t m_ld;
     uint32_t base_place, m_place;
-    bool m_whole, has_base;
+    bool m_whole;
     // A 16-byte piece of the base: rows alternate between the halves of a line, for threads that read four neighbouring pieces of eight rows.
     static __device__ __forceinline__ uint32_t base_at(int row, int col16)
     {
@@ -555,10 +557,10 @@ template <int R, int ROWS, int THREADS, typename T, bool ANY> struct ExpandCopie
     }
     // c0: the first step's first column
     __device__ __forceinline__ ExpandCopies(const ExpandParams& p, const int32_t* tokens, int adapter, int64_t c0)
-        : n((int32_t)(p.n - c0)), m_cols(p.m_cols), m_ld(p.ldm), m_whole(p.m_whole), has_base(p.base != nullptr)
+        : n((int32_t)(p.n - c0)), m_cols(p.m_cols), m_ld(p.ldm), m_whole(p.m_whole)
     {
         const int row = threadIdx.x / kPieces, c = threadIdx.x % kPieces, line = threadIdx.x / kMChunks, k = threadIdx.x % kMChunks;
-        if (has_base) {
+        if constexpr (kHas) {
 #pragma unroll
             for (int i = 0; i < kB; ++i) {
                 const int32_t t = tokens[row + i * kStep];
@@ -579,7 +581,7 @@ template <int R, int ROWS, int THREADS, typename T, bool ANY> struct ExpandCopie
     // Columns from `at` on (since c0), ranks from r0 on; the base with the first of them.
     __device__ __forceinline__ void fill(uint32_t stage, int at, int r0) const
     {
-        if (has_base && r0 == 0) {
+        if (kHas && r0 == 0) {
             const int c = (int)threadIdx.x % kPieces * (16 / (int)sizeof(T));
 #pragma unroll
             for (int i = 0; i < kB; ++i) base.copy(i, stage + base_place + i * kStep * (kChunks * 16), at, n - at - c, first);
@@ -626,13 +628,17 @@ template <typename T> __device__ __forceinline__ void copy_tokens(const ExpandPa
 
 // A CTA takes 128 rows of one adapter and walks columns, 64 a step, with h in shared memory.  The products of a step run while the step before is read out
 // of the other set of accumulators, added to its base and stored.
-constexpr int kExpandStages = 4;
-template <int R, typename T> constexpr int kExpandSmem = kExpandStages * 64 * (128 * (int)sizeof(T) + R * 2) + 2 * 128 * R * 2 + 1024;
+// Three stages where a fourth would leave room for one CTA an SM only (two are worth more).
+template <int R, typename T, int BASE> constexpr int kExpandStage = 64 * ((BASE != NO_BASE ? 128 * (int)sizeof(T) : 0) + R * 2);
+template <int R, typename T, int BASE> constexpr int kExpandRest = 2 * 128 * R * 2 + 1024;
+template <int R, typename T, int BASE> constexpr int kExpandStages = 4 * kExpandStage<R, T, BASE> + kExpandRest<R, T, BASE> <= 111 * 1024 ? 4 : 3;
+template <int R, typename T, int BASE> constexpr int kExpandSmem = kExpandStages<R, T, BASE> * kExpandStage<R, T, BASE> + kExpandRest<R, T, BASE>;
 
-template <int R, typename T, bool ANY> __global__ void __launch_bounds__(256) adapter_expand_kernel(const __grid_constant__ ExpandParams p)
+template <int R, typename T, int BASE> __global__ void __launch_bounds__(256) adapter_expand_kernel(const __grid_constant__ ExpandParams p)
 {
-    using C = ExpandCopies<R, 128, 256, T, ANY>;
-    constexpr int kColumns = 128;
+    using C = ExpandCopies<R, 128, 256, T, BASE>;
+    constexpr int kColumns = 128, kStages = kExpandStages<R, T, BASE>;
+    static_assert(C::kStage == kExpandStage<R, T, BASE>, "");
     extern __shared__ uint8_t smem_raw[];
     __shared__ Products c;
     __shared__ int32_t tokens[128];
@@ -650,10 +656,10 @@ template <int R, typename T, bool ANY> __global__ void __launch_bounds__(256) ad
     const int adapter = adapter_of(p.s, first, lane);
     if (tid < 128) tokens[tid] = token_at(p.s, first + tid);
     __syncthreads();
-    const uint32_t smem = (shared_at(smem_raw) + 1023u) & ~1023u, hs = smem + kExpandStages * C::kStage;
+    const uint32_t smem = (shared_at(smem_raw) + 1023u) & ~1023u, hs = smem + kStages * C::kStage;
     const uint8_t* const ring = smem_raw + (smem - shared_at(smem_raw));
     const C copies(p, tokens, adapter, begin * 64);
-    auto stage = [&](int32_t i) { return (uint32_t)i % kExpandStages * C::kStage; };
+    auto stage = [&](int32_t i) { return (uint32_t)i % kStages * C::kStage; };
     auto fill = [&](int32_t i) {
         if (i < count) copies.fill(smem + stage(i), i * 64, 0);
         copies_commit();
@@ -664,7 +670,7 @@ template <int R, typename T, bool ANY> __global__ void __launch_bounds__(256) ad
         copy_async(hs + part * (128 * R * 2) + chunk_at<R * 2>(row, k), p.h + (first + row) * 2 * p.padded + part * p.padded + k * 8, 16);
     }
 #pragma unroll
-    for (int i = 0; i < kExpandStages - 2; ++i) fill(i);                          // h with the first
+    for (int i = 0; i < kStages; ++i) fill(i);                                    // h with the first
     // warps w and w + 4 read the same 32 rows, 32 of the 64 columns each
     const int row0 = (warp & 3) * 32, block = warp >> 2;
     T* out[4];
@@ -677,11 +683,10 @@ template <int R, typename T, bool ANY> __global__ void __launch_bounds__(256) ad
     bool given_up = false;
     for (int32_t n = 0; n <= count; ++n) {
         if (n < count) {
-            copies_wait<kExpandStages - 3>();
+            copies_wait<kStages - 2>();
             fence_async_smem();
         }
-        tc_fence_before();
-        __syncthreads();                                                          // step n is there, step n - 2 is stored
+        __syncthreads();                                                          // step n is there
         if (n < count && warp == 0 && elect_one()) {
             tc_fence_after();
             const uint64_t h = operand<R * 2>(hs), w = operand<R * 2>(smem + stage(n) + C::kBase);
@@ -692,7 +697,6 @@ template <int R, typename T, bool ANY> __global__ void __launch_bounds__(256) ad
                     mma_bf16(c.tmem + (n & 1) * 64, h + part * (128 * R * 2 / 16) + 2 * k, w + 2 * k, product(64, false), part > 0 || k > 0);
             tc_commit<1>(shared_at(&c.done[n & 1]));
         }
-        fill(n + kExpandStages - 2);
         if (n == 0) continue;
         const int32_t i0 = n - 1;
         products_wait(c, i0 & 1, (uint32_t)(i0 >> 1), p.status, given_up);
@@ -705,7 +709,7 @@ template <int R, typename T, bool ANY> __global__ void __launch_bounds__(256) ad
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             float v[kPer] = {};
-            if (p.base != nullptr) C::read_base(v, ring + stage(i0), row0 + i * 8 + g, block, q);
+            if constexpr (C::kHas) C::read_base(v, ring + stage(i0), row0 + i * 8 + g, block, q);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 v[2 * j] += acc[i >> 1][j][(i & 1) * 2];
@@ -713,6 +717,9 @@ template <int R, typename T, bool ANY> __global__ void __launch_bounds__(256) ad
             }
             if (out[i] != nullptr) store_out(v, out[i], i0 * 64, width, p.out_whole);
         }
+        tc_fence_before();
+        __syncthreads();                                                          // step n - 1 is read: its place and its sums are free
+        fill(n - 1 + kStages);
     }
     copies_wait<0>();
     products_end(c, kColumns);
@@ -720,11 +727,11 @@ template <int R, typename T, bool ANY> __global__ void __launch_bounds__(256) ad
 
 // A CTA takes 32 rows of one adapter and walks columns, 128 a step and 32 of them a warp; h is in registers.
 constexpr int kExpand32Stages = 3;
-template <int R, typename T> constexpr int kExpand32Smem = kExpand32Stages * 128 * (kRows * (int)sizeof(T) + R * 2) + 128;
+template <int R, typename T, int BASE> constexpr int kExpand32Smem = kExpand32Stages * 128 * ((BASE != NO_BASE ? kRows * (int)sizeof(T) : 0) + R * 2) + 128;
 
-template <int R, typename T, bool ANY> __global__ void __launch_bounds__(128) adapter_expand32_kernel(const __grid_constant__ ExpandParams p)
+template <int R, typename T, int BASE> __global__ void __launch_bounds__(128) adapter_expand32_kernel(const __grid_constant__ ExpandParams p)
 {
-    using C = ExpandCopies<R, kRows, 128, T, ANY>;
+    using C = ExpandCopies<R, kRows, 128, T, BASE>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ int32_t tokens[kRows];
     wait_for_predecessor();
@@ -791,7 +798,7 @@ template <int R, typename T, bool ANY> __global__ void __launch_bounds__(128) ad
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float v[kPer] = {};
-                if (p.base != nullptr) C::read_base(v, ring + stage(turn), i * 8 + g, warp, q);
+                if constexpr (C::kHas) C::read_base(v, ring + stage(turn), i * 8 + g, warp, q);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     acc[i >> 1][j][(i & 1) * 2] = v[2 * j];
@@ -1050,7 +1057,8 @@ struct SmallParams {
 
 // A cluster of 8 for every token (every 16 without ids).  The first of each 16 tokens of an adapter, in token order, leads: its cluster takes all of
 // them and the others' clusters end.  Every CTA sums its part of the width over its warps, then all parts are joined from the 8 shared
-// memories, and each CTA makes an eighth of the columns.  Bound by the latency of four dependent reads (ids, x and a, b and base, and the exchange).
+// memories, and each CTA makes an eighth of the columns (or less: where tiles are few and columns many, several clusters do the first part alike and
+// share the columns).  Bound by the latency of four dependent reads (ids, x and a, b and base, and the exchange).
 template <int R, typename T, bool ANY> __global__ void __cluster_dims__(kMaxCluster, 1, 1) __launch_bounds__(kSmallWarps * 32)
     adapter_small_kernel(const __grid_constant__ SmallParams p)
 {
@@ -1089,8 +1097,8 @@ template <int R, typename T, bool ANY> __global__ void __cluster_dims__(kMaxClus
         members[threadIdx.x] = t < p.tokens ? t : -1;
     }
     __syncthreads();
-    const int64_t steps = (p.n_out + 31) / 32, share = (steps + kMaxCluster - 1) / kMaxCluster;
-    const int64_t c_first = min((int64_t)rank * share, steps), c_last = min(c_first + share, steps);
+    const int64_t parts = (int64_t)gridDim.y * kMaxCluster, steps = (p.n_out + 31) / 32, share = (steps + parts - 1) / parts;
+    const int64_t c_first = min((int64_t)(blockIdx.y * kMaxCluster + rank) * share, steps), c_last = min(c_first + share, steps);
     const int32_t upper = members[g], lower = members[g + 8];
     const T* base0 = upper >= 0 ? static_cast<const T*>(p.base) + (int64_t)upper * p.ldb : nullptr;
     const T* base1 = lower >= 0 ? static_cast<const T*>(p.base) + (int64_t)lower * p.ldb : nullptr;
@@ -1324,32 +1332,32 @@ cudaError_t shrink(const ShrinkParams& p, int rows, bool any, cudaStream_t st)
     });
 }
 
-template <int R, int ROWS, typename T, bool ANY> cudaError_t expand_launch(ExpandParams p, cudaStream_t st)
+template <int R, int ROWS, typename T, int BASE> cudaError_t expand_launch(ExpandParams p, cudaStream_t st)
 {
     static std::atomic<uint64_t> done{0};
     p.row_ctas = (uint32_t)(p.s.rows / ROWS);
     const int64_t steps = (p.n + kExpandCols<ROWS> - 1) / kExpandCols<ROWS>;
     // as many CTAs as the GPU holds at once
-    constexpr int kSmem = ROWS == 128 ? kExpandSmem<R, T> : kExpand32Smem<R, T>;
+    constexpr int kSmem = ROWS == 128 ? kExpandSmem<R, T, BASE> : kExpand32Smem<R, T, BASE>;
     int64_t across = std::max<int64_t>(1, std::min<int64_t>(steps, resident(kSmem) / std::max<uint32_t>(1, p.row_ctas)));
     p.share = (int32_t)((steps + across - 1) / across);
     across = (steps + p.share - 1) / p.share;
     const dim3 grid(p.row_ctas + (p.s.starts != nullptr ? (uint32_t)(up(p.s.tokens, 32) / 32) : 0), (uint32_t)across);
-    if constexpr (ROWS == 128) return launch_ring(adapter_expand_kernel<R, T, ANY>, done, kExpandSmem<R, T>, grid, 0, 256, st, p);
-    else return launch_ring(adapter_expand32_kernel<R, T, ANY>, done, kExpand32Smem<R, T>, grid, 0, 128, st, p);
+    if constexpr (ROWS == 128) return launch_ring(adapter_expand_kernel<R, T, BASE>, done, kSmem, grid, 0, 256, st, p);
+    else return launch_ring(adapter_expand32_kernel<R, T, BASE>, done, kSmem, grid, 0, 128, st, p);
 }
-template <typename T> cudaError_t expand_rows(const ExpandParams& p, int rows, cudaStream_t st)
+template <typename T, int BASE> cudaError_t expand_rows(const ExpandParams& p, int rows, cudaStream_t st)
 {
-    const bool any = p.base != nullptr && !p.base_whole;
     return by_rank(p.padded > 64 ? 64 : p.padded, [&](auto r) {
         constexpr int R = decltype(r)::value;
-        if (rows == kRows) return any ? expand_launch<R, kRows, T, true>(p, st) : expand_launch<R, kRows, T, false>(p, st);
-        return any ? expand_launch<R, 128, T, true>(p, st) : expand_launch<R, 128, T, false>(p, st);
+        return rows == kRows ? expand_launch<R, kRows, T, BASE>(p, st) : expand_launch<R, 128, T, BASE>(p, st);
     });
 }
 cudaError_t expand(const ExpandParams& p, int rows, int dtype, cudaStream_t st)
 {
-    return dtype == MOR_DTYPE_BF16 ? expand_rows<bf16>(p, rows, st) : expand_rows<float>(p, rows, st);
+    if (p.base == nullptr) return expand_rows<bf16, NO_BASE>(p, rows, st);       // a gradient, BF16
+    if (dtype == MOR_DTYPE_BF16) return p.base_whole ? expand_rows<bf16, WHOLE_BASE>(p, rows, st) : expand_rows<bf16, ANY_BASE>(p, rows, st);
+    return p.base_whole ? expand_rows<float, WHOLE_BASE>(p, rows, st) : expand_rows<float, ANY_BASE>(p, rows, st);
 }
 
 template <int R, bool BY_COLUMN, bool ANY> cudaError_t outer_launch(const OuterParams& p, cudaStream_t st)
@@ -1420,7 +1428,10 @@ mor_status_t mor_adapter_add(const mor_adapter_desc_t* d, const void* x, int64_t
         SmallParams p = {static_cast<const bf16*>(x), static_cast<const bf16*>(d->a), static_cast<const bf16*>(d->b), d->ids, d->scale, d->factor, d->adapters, d->rank,
                          (int32_t)d->tokens, ldx, d->n_in, d->n_out, base, out, ldb, ldo, d->rank <= 16 ? d->rank % 4 == 0 && is_aligned(d->b, 8) : d->rank % 8 == 0 && is_aligned(d->b, 16),
                          base_whole && d->n_out % kPer == 0, out_whole};
-        const dim3 grid((uint32_t)(d->ids != nullptr ? d->tokens : ceil_div(d->tokens, kSmallRows)) * kMaxCluster);
+        // no more than two clusters' CTAs an SM, and a step of 32 columns for every warp
+        const int64_t tiles = d->ids != nullptr ? d->tokens : ceil_div(d->tokens, kSmallRows);
+        const int64_t across = std::max<int64_t>(1, std::min(ceil_div(d->n_out, 32 * kSmallWarps * kMaxCluster), 2 * 148 / kMaxCluster / tiles));
+        const dim3 grid((uint32_t)tiles * kMaxCluster, (uint32_t)across);
         return status(by_rank(padded_rank(d->rank), [&](auto r) {
             constexpr int R = decltype(r)::value;
             if (dtype == MOR_DTYPE_BF16)
