@@ -115,18 +115,42 @@ __device__ __forceinline__ void store_chunk(uint32_t to, const uint32_t* w)
 {
     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
 }
-// 16 bytes of a row of n elements from `at` on (zero past its end, or where there is no row); ANY: the row starts anywhere, and the copy is not asynchronous.
-template <typename T, bool ANY> __device__ __forceinline__ void fill_chunk(uint32_t to, const T* row, int64_t at, int64_t n, const void* valid)
+// 16 bytes each of N rows that start anywhere, `at` elements on, of rows of n elements (zero past their ends, or where there is no row): all loads are on their
+// way before the first is put in place.  What reaches past a row's ends goes element by element.
+template <typename T, int N, typename Row, typename Place> __device__ __forceinline__ void fill_shifted(Row row, int64_t at, int64_t n, Place place)
 {
     constexpr int kElems = 16 / (int)sizeof(T);
-    if constexpr (ANY) {
+    uint4 lo[N], hi[N];
+    uint32_t inside = 0;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const T* r = row(k);
+        lo[k] = hi[k] = make_uint4(0, 0, 0, 0);
+        const int phase = phase_of(r + at);
+        if (r != nullptr && at >= phase && at - phase + kElems + (phase != 0 ? kElems : 0) <= n) {
+            inside |= 1u << k;
+            const uint4* from = reinterpret_cast<const uint4*>(r + at - phase);
+            lo[k] = from[0];
+            if (phase != 0) hi[k] = from[1];
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const T* r = row(k);
         uint32_t w[4] = {0, 0, 0, 0};
-        if (row != nullptr && at < n) load_any<T, 16>(w, row, at, n);
-        store_chunk(to, w);
-    } else {
-        const int64_t left = row != nullptr ? n - at : 0;
-        const int bytes = (int)sizeof(T) * (int)max((int64_t)0, min((int64_t)kElems, left));
-        copy_async(to, bytes > 0 ? static_cast<const void*>(row + at) : valid, bytes);
+        if (inside >> k & 1) {
+            const uint32_t bytes = (uint32_t)phase_of(r + at) * (uint32_t)sizeof(T);
+            uint32_t v[8] = {lo[k].x, lo[k].y, lo[k].z, lo[k].w, hi[k].x, hi[k].y, hi[k].z, hi[k].w};
+#pragma unroll
+            for (int i = 0; i < 6; ++i) v[i] = bytes & 8u ? v[i + 2] : v[i];
+#pragma unroll
+            for (int i = 0; i < 5; ++i) v[i] = bytes & 4u ? v[i + 1] : v[i];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = sizeof(T) == 4 ? v[i] : __funnelshift_r(v[i], v[i + 1], (bytes & 2u) * 8u);
+        } else if (r != nullptr && at < n) {
+            load_any<T, 16>(w, r, at, n);
+        }
+        store_chunk(place(k), w);
     }
 }
 // The same chunk of N rows, N of them a thread's, copied step by step along the rows: what does not change from step to step is worked out once (the copies
@@ -140,17 +164,17 @@ template <typename T, int N, bool ANY> struct RowCopies {
         if (r != nullptr) present |= 1u << k;
         row[k] = r != nullptr ? r + at : static_cast<const T*>(valid);
     }
-    // `at`: elements since the first step; `left`: from the chunk's place now to the row's end; `first`: where the rows start, to the chunk
-    __device__ __forceinline__ void copy(int k, uint32_t to, int64_t at, int left, int first) const
+    // To `to` and every `apart` bytes from there.  `at`: elements since the first step; `left`: from the chunk's place now to the row's end; `first`: from where the
+    // rows start to the chunk
+    __device__ __forceinline__ void copy(uint32_t to, uint32_t apart, int64_t at, int left, int first) const
     {
         constexpr int kElems = 16 / (int)sizeof(T);
         if constexpr (ANY) {
-            uint32_t w[4] = {0, 0, 0, 0};
-            if ((present >> k & 1) && left > 0) load_any<T, 16>(w, row[k] - first, first + at, first + at + left);
-            store_chunk(to, w);
+            fill_shifted<T, N>([&](int k) { return (present >> k & 1) && left > 0 ? row[k] - first : nullptr; }, first + at, first + at + left, [&](int k) { return to + k * apart; });
         } else {
-            const int bytes = (present >> k & 1) ? (int)sizeof(T) * max(0, min(kElems, left)) : 0;
-            copy_async(to, row[k] + at, bytes);
+            const int bytes = (int)sizeof(T) * max(0, min(kElems, left));
+#pragma unroll
+            for (int k = 0; k < N; ++k) copy_async(to + k * apart, row[k] + at, (present >> k & 1) ? bytes : 0);
         }
     }
 };
@@ -209,14 +233,14 @@ __device__ __forceinline__ void tmem_load_frags(float (&r)[4][4], uint32_t addr)
                  : "r"(addr));
 }
 struct Products {
-    uint64_t done[4];          // a stage's (or an accumulator set's) products are through
+    uint64_t done[8];          // a stage's (or an accumulator set's) products are through
     uint32_t tmem;
 };
 // Before wait_for_predecessor(), which lets the next kernel start: that one may then take what is left of tensor memory, but nothing that this one still needs.
 __device__ __forceinline__ void products_begin(Products& c, uint32_t columns)
 {
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 4; ++i) mbar_init(&c.done[i], 1);
+        for (int i = 0; i < 8; ++i) mbar_init(&c.done[i], 1);
         fence_mbar_init();
     }
     if (threadIdx.x < 32) tmem_alloc<1>(&c.tmem, columns);
@@ -283,42 +307,41 @@ struct ShrinkParams {
 constexpr int kShrinkStages = 4;
 template <int R, int ROWS> constexpr int kShrinkSmem = kShrinkStages * (ROWS + R) * 128 + 1024;
 
-// The copies of a CTA: steps of 64 elements of ROWS rows of x and R of m; a thread's are chunk tid % 8 of every THREADS / 8th row.
+// The copies of a CTA: steps of 64 elements of ROWS rows of x and R of m; a thread's are chunk tid % 8 of every THREADS / 8th row.  The cluster's CTAs take the
+// steps in turn, so that what they read at the same time lies side by side in memory.
 template <int R, int ROWS, int THREADS, bool ANY> struct ShrinkCopies {
     static constexpr int kStage = (ROWS + R) * 128, kStep = THREADS / 8, kX = ROWS / kStep, kM = R > kStep ? R / kStep : 1;
     RowCopies<bf16, kX, ANY> x;
     RowCopies<bf16, kM, ANY> m;
-    int32_t n, begin, end;
+    int32_t n, first, stride, count;   // elements: the row's, to the thread's chunk of the first step, from step to step; steps
     uint32_t ring, place;
-    __device__ __forceinline__ ShrinkCopies(const ShrinkParams& p, int64_t first, int r0, int adapter, uint32_t rank, uint32_t ctas, uint32_t smem) : n((int32_t)p.n), ring(smem)
+    __device__ __forceinline__ ShrinkCopies(const ShrinkParams& p, int64_t row0, int r0, int adapter, uint32_t rank, uint32_t ctas, uint32_t smem) : n((int32_t)p.n), ring(smem)
     {
         const int line = threadIdx.x >> 3, chunk = threadIdx.x & 7;
-        const int32_t steps = (n + 63) / 64, share = (steps + (int32_t)ctas - 1) / (int32_t)ctas;
-        begin = min((int32_t)rank * share, steps);
-        end = min(begin + share, steps);
+        const int32_t steps = (n + 63) / 64;
+        first = (int32_t)rank * 64 + chunk * 8;
+        stride = (int32_t)ctas * 64;
+        count = (steps - (int32_t)rank + (int32_t)ctas - 1) / (int32_t)ctas;
 #pragma unroll
         for (int i = 0; i < kX; ++i) {
-            const int32_t t = token_at(p.s, first + i * kStep + line);
-            x.set(i, t >= 0 ? p.x + (int64_t)t * p.ldx : nullptr, begin * 64 + chunk * 8, p.x);
+            const int32_t t = token_at(p.s, row0 + i * kStep + line);
+            x.set(i, t >= 0 ? p.x + (int64_t)t * p.ldx : nullptr, first, p.x);
         }
 #pragma unroll
         for (int i = 0; i < kM; ++i) {
             const int r = r0 + i * kStep + line;
-            m.set(i, r < p.m_rows ? p.m + (int64_t)adapter * p.m_stride + (int64_t)r * p.ldm : nullptr, begin * 64 + chunk * 8, p.x);
+            m.set(i, r < p.m_rows ? p.m + (int64_t)adapter * p.m_stride + (int64_t)r * p.ldm : nullptr, first, p.x);
         }
         place = chunk_at<128>(line, chunk);                                       // 8 rows further a chunk's place repeats
     }
-    __device__ __forceinline__ uint32_t stage(int32_t step) const { return ring + (uint32_t)(step - begin) % kShrinkStages * kStage; }
+    __device__ __forceinline__ uint32_t stage(int32_t i) const { return ring + (uint32_t)i % kShrinkStages * kStage; }
     __device__ __forceinline__ void fill(int32_t step) const
     {
-        if (step < end) {
+        if (step < count) {
             const uint32_t to = stage(step) + place;
-            const int at = (step - begin) * 64, first = begin * 64 + (threadIdx.x & 7) * 8, left = n - first - at;
-#pragma unroll
-            for (int i = 0; i < kX; ++i) x.copy(i, to + i * kStep * 128, at, left, first);
-#pragma unroll
-            for (int i = 0; i < kM; ++i)
-                if (R >= kStep || (int)threadIdx.x < R * 8) m.copy(i, to + (ROWS + i * kStep) * 128, at, left, first);
+            const int at = step * stride, left = n - first - at;
+            x.copy(to, kStep * 128, at, left, first);
+            if (R >= kStep || (int)threadIdx.x < R * 8) m.copy(to + ROWS * 128, kStep * 128, at, left, first);
         }
         copies_commit();
     }
@@ -343,23 +366,22 @@ template <int R, bool ANY> __global__ void __launch_bounds__(256) adapter_shrink
     const ShrinkCopies<R, 128, 256, ANY> copies(p, first, 0, adapter, rank, ctas, smem);
     bool given_up = false;
 #pragma unroll
-    for (int s = 0; s < kShrinkStages - 1; ++s) copies.fill(copies.begin + s);
-    for (int32_t step = copies.begin; step < copies.end; ++step) {
-        const int32_t n = step - copies.begin;
+    for (int s = 0; s < kShrinkStages - 1; ++s) copies.fill(s);
+    for (int32_t n = 0; n < copies.count; ++n) {
         copies_wait<kShrinkStages - 2>();
         fence_async_smem();
         __syncthreads();
         if (warp == 0 && elect_one()) {
-            const uint64_t x = operand<128>(copies.stage(step)), m = operand<128>(copies.stage(step) + 128 * 128);
+            const uint64_t x = operand<128>(copies.stage(n)), m = operand<128>(copies.stage(n) + 128 * 128);
 #pragma unroll
             for (int k = 0; k < 4; ++k) mma_bf16(c.tmem, x + 2 * k, m + 2 * k, product(R, false), n > 0 || k > 0);
             tc_commit<1>(shared_at(&c.done[n % kShrinkStages]));
         }
         // the next step's tile goes where the last one's products read from
         if (n > 0) products_wait(c, (n - 1) % kShrinkStages, (uint32_t)((n - 1) / kShrinkStages), p.status, given_up);
-        copies.fill(step + kShrinkStages - 1);
+        copies.fill(n + kShrinkStages - 1);
     }
-    const int32_t count = copies.end - copies.begin;
+    const int32_t count = copies.count;
     if (count > 0) products_wait(c, (count - 1) % kShrinkStages, (uint32_t)((count - 1) / kShrinkStages), p.status, given_up);
     copies_wait<0>();
     tc_fence_after();
@@ -402,8 +424,8 @@ template <int R, bool ANY> __global__ void __launch_bounds__(128) adapter_shrink
 #pragma unroll
             for (int k = 0; k < 4; ++k) acc[i][j][k] = 0.f;
 #pragma unroll
-    for (int s = 0; s < kShrinkStages - 1; ++s) copies.fill(copies.begin + s);
-    for (int32_t step = copies.begin; step < copies.end; ++step) {
+    for (int s = 0; s < kShrinkStages - 1; ++s) copies.fill(s);
+    for (int32_t step = 0; step < copies.count; ++step) {
         copies_wait<kShrinkStages - 2>();
         __syncthreads();
         copies.fill(step + kShrinkStages - 1);
@@ -463,8 +485,7 @@ struct ExpandParams {
     const void* base;          // optional
     void* out;
     int64_t ldb, ldo;
-    uint32_t row_ctas;         // CTAs of rows; those behind copy the tokens without an adapter
-    int32_t share;             // steps of a CTA
+    uint32_t tiles, across;    // CTAs: across for each tile of rows
     bool m_whole, base_whole, out_whole;
     uint32_t* status;
 };
@@ -518,18 +539,6 @@ template <typename T, typename I> __device__ __forceinline__ void store_out(cons
     }
 }
 
-template <typename T> __device__ void copy_row(const ExpandParams& p, int64_t token, int64_t from, int64_t to, int lane)
-{
-    const T* base = p.base != nullptr ? static_cast<const T*>(p.base) + token * p.ldb : nullptr;
-    T* out = static_cast<T*>(p.out) + token * p.ldo;
-    const bool whole = p.base_whole && p.n % kPer == 0;
-    for (int64_t at = from + lane * kPer; at < to; at += 32 * kPer) {
-        float v[kPer];
-        load_base(v, base, at, p.n, whole);
-        store_out(v, out, at, p.n, p.out_whole);
-    }
-}
-
 template <int ROWS> constexpr int kExpandCols = ROWS == kRows ? 128 : 64;
 
 // The copies of a CTA: kExpandCols columns of the base of ROWS rows, in blocks of 64, and the rows of m that make them, R of the ranks.  The rows of m
@@ -578,13 +587,13 @@ template <int R, int ROWS, int THREADS, typename T, int BASE> struct ExpandCopie
         return (uint32_t)kBase + chunk_at<R * 2>(slot, k);
     }
     int32_t first;
-    // Columns from `at` on (since c0), ranks from r0 on; the base with the first of them.
+    // Columns from `at` on (since c0), ranks from r0 on; the base with the first of them.  A row's CTAs take the steps in turn: what they read and write at the
+    // same time lies side by side in memory.
     __device__ __forceinline__ void fill(uint32_t stage, int at, int r0) const
     {
         if (kHas && r0 == 0) {
             const int c = (int)threadIdx.x % kPieces * (16 / (int)sizeof(T));
-#pragma unroll
-            for (int i = 0; i < kB; ++i) base.copy(i, stage + base_place + i * kStep * (kChunks * 16), at, n - at - c, first);
+            base.copy(stage + base_place, kStep * (kChunks * 16), at, n - at - c, first);
         }
         const int k = (int)threadIdx.x % kMChunks * 8 + r0, line = (int)threadIdx.x / kMChunks;
 #pragma unroll
@@ -617,13 +626,28 @@ template <int R, int ROWS, int THREADS, typename T, int BASE> struct ExpandCopie
     }
 };
 
-// Tokens without an adapter: 32 for a CTA.
-template <typename T> __device__ __forceinline__ void copy_tokens(const ExpandParams& p, int64_t t0, int64_t from, int64_t to)
+// Tokens without an adapter: every CTA of the grid takes some, the next token the next CTA's (those of a request lie side by side, and CTAs of their own for
+// neighbouring tokens had all the work: 200 us for 480 of 8192 tokens).
+template <typename T> __device__ __forceinline__ void copy_tokens(const ExpandParams& p)
 {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t none = __ballot_sync(0xFFFFFFFFu, t0 + lane < p.s.tokens && p.s.row_of_token[t0 + lane] < 0);
-    for (int i = warp; i < 32; i += (int)blockDim.x / 32)
-        if (none >> i & 1) copy_row<T>(p, t0 + i, from, to, lane);
+    if (p.s.starts == nullptr) return;
+    const bool whole = p.base_whole && p.n % kPer == 0;
+    const int64_t step = (int64_t)blockDim.x * kPer;
+    for (int64_t t0 = 0; t0 < p.s.tokens; t0 += 32 * (int64_t)gridDim.x) {
+        const int64_t mine = t0 + blockIdx.x + (int64_t)(threadIdx.x & 31) * gridDim.x;
+        for (uint32_t none = __ballot_sync(0xFFFFFFFFu, mine < p.s.tokens && p.s.row_of_token[mine] < 0); none != 0; none &= none - 1) {
+            const int64_t token = t0 + blockIdx.x + (int64_t)(__ffs(none) - 1) * gridDim.x;
+            const T* base = p.base != nullptr ? static_cast<const T*>(p.base) + token * p.ldb : nullptr;
+            T* out = static_cast<T*>(p.out) + token * p.ldo;
+            for (int64_t at = threadIdx.x * kPer; at < p.n; at += 2 * step) {
+                float v[2][kPer];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) load_base(v[k], base, at + k * step, p.n, whole);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) store_out(v[k], out, at + k * step, p.n, p.out_whole);
+            }
+        }
+    }
 }
 
 // A CTA takes 128 rows of one adapter and walks columns, 64 a step, with h in shared memory.  The products of a step run while the step before is read out
@@ -634,7 +658,7 @@ template <int R, typename T, int BASE> constexpr int kExpandRest = 2 * 128 * R *
 template <int R, typename T, int BASE> constexpr int kExpandStages = 4 * kExpandStage<R, T, BASE> + kExpandRest<R, T, BASE> <= 111 * 1024 ? 4 : 3;
 template <int R, typename T, int BASE> constexpr int kExpandSmem = kExpandStages<R, T, BASE> * kExpandStage<R, T, BASE> + kExpandRest<R, T, BASE>;
 
-template <int R, typename T, int BASE> __global__ void __launch_bounds__(256) adapter_expand_kernel(const __grid_constant__ ExpandParams p)
+template <int R, typename T, int BASE> __global__ void __launch_bounds__(256, BASE == NO_BASE ? 3 : 2) adapter_expand_kernel(const __grid_constant__ ExpandParams p)
 {
     using C = ExpandCopies<R, 128, 256, T, BASE>;
     constexpr int kColumns = 128, kStages = kExpandStages<R, T, BASE>;
@@ -645,12 +669,11 @@ template <int R, typename T, int BASE> __global__ void __launch_bounds__(256) ad
     products_begin(c, kColumns);
     wait_for_predecessor();
     const int tid = threadIdx.x, warp = warp_number(), lane = tid & 31, g = lane >> 2, q = lane & 3;
-    const int64_t steps = (p.n + 63) / 64, begin = (int64_t)blockIdx.y * p.share;
-    const int32_t count = (int32_t)(min(begin + (int64_t)p.share, steps) - begin);
-    const int64_t first = (int64_t)blockIdx.x * 128;
-    if (blockIdx.x >= p.row_ctas) copy_tokens<T>(p, (int64_t)(blockIdx.x - p.row_ctas) * 32, begin * 64, min((begin + count) * 64, p.n));
-    if (blockIdx.x >= p.row_ctas || first >= used_rows(p.s)) {
+    const int32_t part = (int32_t)(blockIdx.x / p.tiles), count = ((int32_t)((p.n + 63) / 64) - part + (int32_t)p.across - 1) / (int32_t)p.across, stride = (int32_t)p.across * 64;
+    const int64_t first = (int64_t)(blockIdx.x % p.tiles) * 128;
+    if (first >= used_rows(p.s)) {
         products_end(c, kColumns);
+        copy_tokens<T>(p);
         return;
     }
     const int adapter = adapter_of(p.s, first, lane);
@@ -658,16 +681,16 @@ template <int R, typename T, int BASE> __global__ void __launch_bounds__(256) ad
     __syncthreads();
     const uint32_t smem = (shared_at(smem_raw) + 1023u) & ~1023u, hs = smem + kStages * C::kStage;
     const uint8_t* const ring = smem_raw + (smem - shared_at(smem_raw));
-    const C copies(p, tokens, adapter, begin * 64);
+    const C copies(p, tokens, adapter, (int64_t)part * 64);
     auto stage = [&](int32_t i) { return (uint32_t)i % kStages * C::kStage; };
     auto fill = [&](int32_t i) {
-        if (i < count) copies.fill(smem + stage(i), i * 64, 0);
+        if (i < count) copies.fill(smem + stage(i), i * stride, 0);
         copies_commit();
     };
 #pragma unroll
     for (int i = tid; i < 128 * R / 4; i += 256) {
-        const int row = i / (R / 4), part = i % (R / 4) / (R / 8), k = i % (R / 8);
-        copy_async(hs + part * (128 * R * 2) + chunk_at<R * 2>(row, k), p.h + (first + row) * 2 * p.padded + part * p.padded + k * 8, 16);
+        const int row = i / (R / 4), half = i % (R / 4) / (R / 8), k = i % (R / 8);
+        copy_async(hs + half * (128 * R * 2) + chunk_at<R * 2>(row, k), p.h + (first + row) * 2 * p.padded + half * p.padded + k * 8, 16);
     }
 #pragma unroll
     for (int i = 0; i < kStages; ++i) fill(i);                                    // h with the first
@@ -677,9 +700,9 @@ template <int R, typename T, int BASE> __global__ void __launch_bounds__(256) ad
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int32_t t = tokens[row0 + i * 8 + g];
-        out[i] = t >= 0 ? static_cast<T*>(p.out) + (int64_t)t * p.ldo + begin * 64 + block * 32 + q * 8 : nullptr;
+        out[i] = t >= 0 ? static_cast<T*>(p.out) + (int64_t)t * p.ldo + (int64_t)part * 64 + block * 32 + q * 8 : nullptr;
     }
-    const int width = (int)(p.n - begin * 64) - block * 32 - q * 8;               // columns from the thread's first on
+    const int width = (int)p.n - part * 64 - block * 32 - q * 8;               // columns from the thread's first on
     bool given_up = false;
     for (int32_t n = 0; n <= count; ++n) {
         if (n < count) {
@@ -691,10 +714,10 @@ template <int R, typename T, int BASE> __global__ void __launch_bounds__(256) ad
             tc_fence_after();
             const uint64_t h = operand<R * 2>(hs), w = operand<R * 2>(smem + stage(n) + C::kBase);
 #pragma unroll
-            for (int part = 0; part < 2; ++part)
+            for (int half = 0; half < 2; ++half)
 #pragma unroll
                 for (int k = 0; k < R / 16; ++k)
-                    mma_bf16(c.tmem + (n & 1) * 64, h + part * (128 * R * 2 / 16) + 2 * k, w + 2 * k, product(64, false), part > 0 || k > 0);
+                    mma_bf16(c.tmem + (n & 1) * 64, h + half * (128 * R * 2 / 16) + 2 * k, w + 2 * k, product(64, false), half > 0 || k > 0);
             tc_commit<1>(shared_at(&c.done[n & 1]));
         }
         if (n == 0) continue;
@@ -715,7 +738,7 @@ template <int R, typename T, int BASE> __global__ void __launch_bounds__(256) ad
                 v[2 * j] += acc[i >> 1][j][(i & 1) * 2];
                 v[2 * j + 1] += acc[i >> 1][j][(i & 1) * 2 + 1];
             }
-            if (out[i] != nullptr) store_out(v, out[i], i0 * 64, width, p.out_whole);
+            if (out[i] != nullptr) store_out(v, out[i], i0 * stride, width, p.out_whole);
         }
         tc_fence_before();
         __syncthreads();                                                          // step n - 1 is read: its place and its sums are free
@@ -723,6 +746,7 @@ template <int R, typename T, int BASE> __global__ void __launch_bounds__(256) ad
     }
     copies_wait<0>();
     products_end(c, kColumns);
+    copy_tokens<T>(p);
 }
 
 // A CTA takes 32 rows of one adapter and walks columns, 128 a step and 32 of them a warp; h is in registers.
@@ -736,25 +760,24 @@ template <int R, typename T, int BASE> __global__ void __launch_bounds__(128) ad
     __shared__ int32_t tokens[kRows];
     wait_for_predecessor();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, q = lane & 3;
-    const int64_t steps = (p.n + C::kCols - 1) / C::kCols, begin = (int64_t)blockIdx.y * p.share;
-    const int32_t count = (int32_t)(min(begin + (int64_t)p.share, steps) - begin);
-    if (blockIdx.x >= p.row_ctas) {
-        copy_tokens<T>(p, (int64_t)(blockIdx.x - p.row_ctas) * 32, begin * C::kCols, min((begin + count) * C::kCols, p.n));
+    const int32_t part = (int32_t)(blockIdx.x / p.tiles), count = ((int32_t)((p.n + C::kCols - 1) / C::kCols) - part + (int32_t)p.across - 1) / (int32_t)p.across;
+    const int32_t stride = (int32_t)p.across * C::kCols;
+    const int64_t first = (int64_t)(blockIdx.x % p.tiles) * kRows;
+    if (first >= used_rows(p.s)) {
+        copy_tokens<T>(p);
         return;
     }
-    const int64_t first = (int64_t)blockIdx.x * kRows;
-    if (first >= used_rows(p.s)) return;
     const int adapter = adapter_of(p.s, first, lane);
     if (tid < kRows) tokens[tid] = token_at(p.s, first + tid);
     __syncthreads();
-    const C copies(p, tokens, adapter, begin * C::kCols);
+    const C copies(p, tokens, adapter, (int64_t)part * C::kCols);
     const uint32_t smem = (shared_at(smem_raw) + 127u) & ~127u;
     const uint8_t* const ring = smem_raw + (smem - shared_at(smem_raw));
     const int chunks = p.padded / R;                                              // of the ranks
     const int32_t turns = count * chunks;
     auto stage = [&](int32_t i) { return (uint32_t)i % kExpand32Stages * C::kStage; };
     auto fill = [&](int32_t i) {                                                  // a turn is a step and a chunk of the ranks
-        if (i < turns) copies.fill(smem + stage(i), i / chunks * C::kCols, i % chunks * R);
+        if (i < turns) copies.fill(smem + stage(i), i / chunks * stride, i % chunks * R);
         copies_commit();
     };
 #pragma unroll
@@ -825,7 +848,7 @@ template <int R, typename T, int BASE> __global__ void __launch_bounds__(128) ad
             }
         }
         if (r0 + R < p.padded) continue;
-        const int64_t at = (begin + turn / chunks) * C::kCols + warp * 32 + q * 8;
+        const int64_t at = (int64_t)part * C::kCols + turn / chunks * stride + warp * 32 + q * 8;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (out[i] == nullptr) continue;
@@ -839,6 +862,7 @@ template <int R, typename T, int BASE> __global__ void __launch_bounds__(128) ad
         }
     }
     copies_wait<0>();
+    copy_tokens<T>(p);
 }
 
 // Fragments of 16 rows of h in registers, for the slots that load_m() gives a thread.
@@ -928,11 +952,14 @@ template <int R, bool BY_COLUMN, bool ANY> __global__ void __launch_bounds__(256
     const int32_t rows = (int32_t)min(to - from - (int64_t)begin * kOuterRows, (int64_t)count * kOuterRows);
     auto fill = [&](int32_t i) {
         if (i < count) {
+            const uint32_t zs = stage(i) + z_place;
+            if constexpr (ANY) {
+                fill_shifted<bf16, 4>([&](int k) { return ahead[k] >= 0 ? p.z + (int64_t)ahead[k] * p.ldz : nullptr; }, c0 + (tid & 15) * 8, p.n,
+                                      [&](int k) { return zs + k * 16 * 128; });
+            } else {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t at = stage(i) + z_place + k * 16 * 128;
-                if constexpr (ANY) fill_chunk<bf16, true>(at, ahead[k] >= 0 ? p.z + (int64_t)ahead[k] * p.ldz : nullptr, c0 + (tid & 15) * 8, p.n, p.z);
-                else copy_async(at, ahead[k] >= 0 && left > 0 ? z + (int64_t)ahead[k] * p.ldz : p.z, ahead[k] >= 0 ? 2 * max(0, left) : 0);
+                for (int k = 0; k < 4; ++k)
+                    copy_async(zs + k * 16 * 128, ahead[k] >= 0 && left > 0 ? z + (int64_t)ahead[k] * p.ldz : p.z, ahead[k] >= 0 ? 2 * max(0, left) : 0);
             }
 #pragma unroll
             for (int k = 0; k < kH; ++k) {
@@ -1312,13 +1339,20 @@ template <typename K, typename P> cudaError_t launch_ring(K kernel, std::atomic<
     return launch_clusters(kernel, grid, cluster, block, (size_t)smem, st, p);
 }
 
+// Tiles that are expected to hold tokens: of the rows that there may be, about half a tile of each adapter is empty.
+int64_t filled_tiles(const Sorted& s, int rows)
+{
+    return std::max<int64_t>(1, s.starts != nullptr ? std::min(s.rows / rows, ceil_div(s.tokens, rows) + s.adapters / 2) : s.rows / rows);
+}
+
 template <int R, int ROWS, bool ANY> cudaError_t shrink_launch(const ShrinkParams& p, cudaStream_t st)
 {
     static std::atomic<uint64_t> done{0};
     const int64_t tiles = p.s.rows / ROWS, steps = (p.n + 63) / 64;
+    const int64_t filled = filled_tiles(p.s, ROWS);
     const uint32_t chunks = (uint32_t)(p.padded / R);
-    uint32_t cluster = 1;                     // as many CTAs to a tile as the GPU holds at once, two steps each at least
-    while (cluster < kMaxCluster && tiles * chunks * cluster * 2 <= resident(kShrinkSmem<R, ROWS>) && steps >= 4 * cluster) cluster *= 2;
+    uint32_t cluster = 1;                     // as many CTAs to a tile as the GPU holds at once (clusters do not fill it quite), two steps each at least
+    while (cluster < kMaxCluster && filled * chunks * cluster * 20 <= resident(kShrinkSmem<R, ROWS>) * 9 && steps >= 4 * cluster) cluster *= 2;
     const dim3 grid((uint32_t)tiles * cluster, chunks);
     if constexpr (ROWS == 128) return launch_ring(adapter_shrink_kernel<R, ANY>, done, kShrinkSmem<R, ROWS>, grid, cluster, 256, st, p);
     else return launch_ring(adapter_shrink32_kernel<R, ANY>, done, kShrinkSmem<R, ROWS>, grid, cluster, 128, st, p);
@@ -1335,14 +1369,12 @@ cudaError_t shrink(const ShrinkParams& p, int rows, bool any, cudaStream_t st)
 template <int R, int ROWS, typename T, int BASE> cudaError_t expand_launch(ExpandParams p, cudaStream_t st)
 {
     static std::atomic<uint64_t> done{0};
-    p.row_ctas = (uint32_t)(p.s.rows / ROWS);
+    p.tiles = (uint32_t)(p.s.rows / ROWS);
     const int64_t steps = (p.n + kExpandCols<ROWS> - 1) / kExpandCols<ROWS>;
     // as many CTAs as the GPU holds at once
     constexpr int kSmem = ROWS == 128 ? kExpandSmem<R, T, BASE> : kExpand32Smem<R, T, BASE>;
-    int64_t across = std::max<int64_t>(1, std::min<int64_t>(steps, resident(kSmem) / std::max<uint32_t>(1, p.row_ctas)));
-    p.share = (int32_t)((steps + across - 1) / across);
-    across = (steps + p.share - 1) / p.share;
-    const dim3 grid(p.row_ctas + (p.s.starts != nullptr ? (uint32_t)(up(p.s.tokens, 32) / 32) : 0), (uint32_t)across);
+    p.across = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(steps, resident(kSmem) / filled_tiles(p.s, ROWS)));
+    const dim3 grid(p.tiles * p.across);
     if constexpr (ROWS == 128) return launch_ring(adapter_expand_kernel<R, T, BASE>, done, kSmem, grid, 0, 256, st, p);
     else return launch_ring(adapter_expand32_kernel<R, T, BASE>, done, kSmem, grid, 0, 128, st, p);
 }
