@@ -16,6 +16,7 @@
 // More tokens are sorted by adapter first; each adapter's rows start at a multiple of a tile.  All sums run in an order that depends on the sizes and
 // ids alone.
 #include "../fp4/mor_tcgen05.cuh"
+#include "../mor_internal.h"
 #include "mor_layers.cuh"
 
 namespace mor {
@@ -208,7 +209,13 @@ __device__ __forceinline__ float4 sum_remote4(uint32_t own, uint32_t ctas)
 
 // ---- the fifth-generation tensor cores, BF16
 
-constexpr long long kWaitCycles = 400000000;      // a wait that takes longer is given up: something is wrong
+// Bounds of the waits: one that takes longer is given up, and the status word says so.  A test makes one run out: the CTA `skip` does not announce its first
+// products.
+struct Waits {
+    uint32_t* status;
+    long long cycles;
+    uint32_t skip;
+};
 
 // Rows of ROW_BYTES laid down by chunk_at<ROW_BYTES>(), the reduction axis along the rows (K) or across them.  Groups of 8 rows are one after the
 // other; `next`: bytes between pieces of 64 columns (operands whose rows are the reduction axis and that are wider than that).
@@ -248,8 +255,10 @@ __device__ __forceinline__ void products_begin(Products& c, uint32_t columns)
     __syncthreads();
     tc_fence_after();
 }
-__device__ __forceinline__ void products_end(const Products& c, uint32_t columns)
+__device__ __forceinline__ void products_end(const Products& c, uint32_t columns, bool given_up = false)
 {
+    if (given_up)                                     // whatever still runs in tensor memory: long enough for all of it
+        for (const long long t0 = clock64(); clock64() - t0 < 400000;) {}
     tc_fence_before();
     __syncthreads();
     if (threadIdx.x < 32) {
@@ -258,17 +267,24 @@ __device__ __forceinline__ void products_end(const Products& c, uint32_t columns
     }
 }
 // For all threads: the products that were the n-th to be committed to this barrier (from 0) are through.
-__device__ __forceinline__ void products_wait(Products& c, int which, uint32_t n, uint32_t* status, bool& given_up)
+__device__ __forceinline__ void products_wait(Products& c, int which, uint32_t n, const Waits& w, bool& given_up)
 {
     if (given_up) return;
-    if (!mbar_wait(&c.done[which], n & 1u, nullptr, kWaitCycles)) {
+    if (!mbar_wait(&c.done[which], n & 1u, nullptr, w.cycles)) {
         given_up = true;
-        if (status != nullptr) *status = MOR_ERR_TIMEOUT;
+        if (w.status != nullptr) atomicExch(w.status, (uint32_t)MOR_ERR_TIMEOUT);
     }
 }
+// For the thread that issued them: the products so far are the step's.
+__device__ __forceinline__ void products_commit(Products& c, int which, int32_t step, const Waits& w)
+{
+    if (step > 0 || blockIdx.x != w.skip) tc_commit<1>(shared_at(&c.done[which]));
+}
 
-// Joins the rows' sums over the cluster's CTAs and stores them as pairs of BF16.  part: [rows][R + 4], of this CTA.
-template <int R> __device__ __forceinline__ void join_rows(float* part, int rows, int64_t first, int r0, float scale, bf16* h, int padded, uint32_t rank, uint32_t ctas)
+// Joins the rows' sums over the cluster's CTAs and stores them as pairs of BF16.  part: [rows][R + 4], of this CTA.  What is past the ranks that there are is
+// zero whatever x holds.
+template <int R>
+__device__ __forceinline__ void join_rows(float* part, int rows, int64_t first, int r0, float scale, bf16* h, int padded, int ranks, uint32_t rank, uint32_t ctas)
 {
     constexpr int kPitch = R + 4;
     cluster_arrive();
@@ -280,7 +296,7 @@ template <int R> __device__ __forceinline__ void join_rows(float* part, int rows
         const float f[4] = {v.x * scale, v.y * scale, v.z * scale, v.w * scale};
         bf16 hi[4], lo[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) split(f[k], hi[k], lo[k]);
+        for (int k = 0; k < 4; ++k) split(r0 + col + k < ranks ? f[k] : 0.f, hi[k], lo[k]);
         uint16_t* to = reinterpret_cast<uint16_t*>(h) + (first + row) * 2 * padded + r0 + col;
         *reinterpret_cast<ushort4*>(to) = make_ushort4(bits_of(hi[0]), bits_of(hi[1]), bits_of(hi[2]), bits_of(hi[3]));
         *reinterpret_cast<ushort4*>(to + padded) = make_ushort4(bits_of(lo[0]), bits_of(lo[1]), bits_of(lo[2]), bits_of(lo[3]));
@@ -299,9 +315,9 @@ struct ShrinkParams {
     float factor;
     int64_t ldx, n, ldm, m_stride;
     int32_t m_rows;            // rows of m that exist
-    int32_t padded;            // rank as the output has it
+    int32_t rank, padded;      // and as the output has it
     bf16* h;                   // [rows][2][padded]
-    uint32_t* status;
+    Waits waits;
 };
 
 constexpr int kShrinkStages = 4;
@@ -375,14 +391,14 @@ template <int R, bool ANY> __global__ void __launch_bounds__(256) adapter_shrink
             const uint64_t x = operand<128>(copies.stage(n)), m = operand<128>(copies.stage(n) + 128 * 128);
 #pragma unroll
             for (int k = 0; k < 4; ++k) mma_bf16(c.tmem, x + 2 * k, m + 2 * k, product(R, false), n > 0 || k > 0);
-            tc_commit<1>(shared_at(&c.done[n % kShrinkStages]));
+            products_commit(c, n % kShrinkStages, n, p.waits);
         }
         // the next step's tile goes where the last one's products read from
-        if (n > 0) products_wait(c, (n - 1) % kShrinkStages, (uint32_t)((n - 1) / kShrinkStages), p.status, given_up);
+        if (n > 0) products_wait(c, (n - 1) % kShrinkStages, (uint32_t)((n - 1) / kShrinkStages), p.waits, given_up);
         copies.fill(n + kShrinkStages - 1);
     }
     const int32_t count = copies.count;
-    if (count > 0) products_wait(c, (count - 1) % kShrinkStages, (uint32_t)((count - 1) / kShrinkStages), p.status, given_up);
+    if (count > 0) products_wait(c, (count - 1) % kShrinkStages, (uint32_t)((count - 1) / kShrinkStages), p.waits, given_up);
     copies_wait<0>();
     tc_fence_after();
     __syncthreads();
@@ -399,8 +415,8 @@ template <int R, bool ANY> __global__ void __launch_bounds__(256) adapter_shrink
 #pragma unroll
         for (int k = 0; k < 16; k += 4) *reinterpret_cast<uint4*>(part + ((warp & 3) * 32 + lane) * (R + 4) + r + k) = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
     }
-    products_end(c, kColumns);
-    join_rows<R>(part, 128, first, 0, (p.scale != nullptr ? p.scale[adapter] : 1.f) * p.factor, p.h, p.padded, rank, ctas);
+    products_end(c, kColumns, given_up);
+    join_rows<R>(part, 128, first, 0, (p.scale != nullptr ? p.scale[adapter] : 1.f) * p.factor, p.h, p.padded, p.rank, rank, ctas);
 }
 
 // A CTA takes 32 rows of one adapter and R of the ranks (blockIdx.y); a warp works on a quarter of each step.
@@ -471,7 +487,7 @@ template <int R, bool ANY> __global__ void __launch_bounds__(128) adapter_shrink
         }
         *to = v;
     }
-    join_rows<R>(part, kRows, first, r0, (p.scale != nullptr ? p.scale[adapter] : 1.f) * p.factor, p.h, p.padded, rank, ctas);
+    join_rows<R>(part, kRows, first, r0, (p.scale != nullptr ? p.scale[adapter] : 1.f) * p.factor, p.h, p.padded, p.rank, rank, ctas);
 }
 
 // ------------------------------------------------------------------------------------------- expand ----
@@ -487,7 +503,7 @@ struct ExpandParams {
     int64_t ldb, ldo;
     uint32_t tiles, across;    // CTAs: across for each tile of rows
     bool m_whole, base_whole, out_whole;
-    uint32_t* status;
+    Waits waits;
 };
 
 // Row `n` of m for the slots of a thread: 8 neighbouring ranks for R >= 32, 4 for R = 16.
@@ -718,11 +734,11 @@ template <int R, typename T, int BASE> __global__ void __launch_bounds__(256, BA
 #pragma unroll
                 for (int k = 0; k < R / 16; ++k)
                     mma_bf16(c.tmem + (n & 1) * 64, h + half * (128 * R * 2 / 16) + 2 * k, w + 2 * k, product(64, false), half > 0 || k > 0);
-            tc_commit<1>(shared_at(&c.done[n & 1]));
+            products_commit(c, n & 1, n, p.waits);
         }
         if (n == 0) continue;
         const int32_t i0 = n - 1;
-        products_wait(c, i0 & 1, (uint32_t)(i0 >> 1), p.status, given_up);
+        products_wait(c, i0 & 1, (uint32_t)(i0 >> 1), p.waits, given_up);
         tc_fence_after();
         const uint32_t lanes = c.tmem + ((uint32_t)row0 << 16) + (i0 & 1) * 64 + block * 32;
         float acc[2][4][4];
@@ -745,7 +761,7 @@ template <int R, typename T, int BASE> __global__ void __launch_bounds__(256, BA
         fill(n - 1 + kStages);
     }
     copies_wait<0>();
-    products_end(c, kColumns);
+    products_end(c, kColumns, given_up);
     copy_tokens<T>(p);
 }
 
@@ -906,7 +922,7 @@ struct OuterParams {
     int64_t ldz, n;
     int32_t rank, padded;
     bf16* out;                 // [adapters][rank][n], or [adapters][n][rank]
-    uint32_t* status;
+    Waits waits;
 };
 
 // 128 columns x R ranks of an adapter: the reduction runs over its rows, 64 a step, cut over a cluster's CTAs.  Both operands have the reduction axis across
@@ -986,12 +1002,12 @@ template <int R, bool BY_COLUMN, bool ANY> __global__ void __launch_bounds__(256
 #pragma unroll
                 for (int k = 0; k < kOuterRows / 16; ++k)                          // 16 rows of either further
                     mma_bf16(c.tmem, zs + k * (16 * 128 / 16), hs + part * (kHalf / 16) + k * (16 * R * 2 / 16), product(R, true), n > 0 || part > 0 || k > 0);
-            tc_commit<1>(shared_at(&c.done[n % kOuterStages]));
+            products_commit(c, n % kOuterStages, n, p.waits);
         }
-        if (n > 0) products_wait(c, (n - 1) % kOuterStages, (uint32_t)((n - 1) / kOuterStages), p.status, given_up);
+        if (n > 0) products_wait(c, (n - 1) % kOuterStages, (uint32_t)((n - 1) / kOuterStages), p.waits, given_up);
         fill(n + kOuterStages - 1);
     }
-    if (count > 0) products_wait(c, (count - 1) % kOuterStages, (uint32_t)((count - 1) / kOuterStages), p.status, given_up);
+    if (count > 0) products_wait(c, (count - 1) % kOuterStages, (uint32_t)((count - 1) / kOuterStages), p.waits, given_up);
     copies_wait<0>();
     tc_fence_after();
     __syncthreads();
@@ -1014,7 +1030,7 @@ template <int R, bool BY_COLUMN, bool ANY> __global__ void __launch_bounds__(256
             for (int k = 0; k < 16; ++k) part[(r + k) * kPitch + col] = __uint_as_float(v[k]);
         }
     }
-    products_end(c, kColumns);
+    products_end(c, kColumns, given_up);
     cluster_arrive();
     cluster_wait();
     bf16* out = p.out + (int64_t)adapter * p.rank * p.n;
@@ -1192,7 +1208,7 @@ template <int R, typename T, bool ANY> __global__ void __cluster_dims__(kMaxClus
     const float s = (p.scale != nullptr ? p.scale[adapter] : 1.f) * p.factor;
     for (int i = threadIdx.x; i < kSmallRows * R; i += kSmallWarps * 32) {
         float sum = 0.f;
-        if (members[i / R] >= 0)
+        if (members[i / R] >= 0 && i % R < p.rank)
 #pragma unroll
             for (uint32_t c = 0; c < kMaxCluster; ++c) sum += load_remote(&own[i / R][i % R], c);
         whole[i / R][i % R] = sum * s;
@@ -1410,6 +1426,13 @@ cudaError_t outer(const OuterParams& p, bool by_column, bool any, cudaStream_t s
     });
 }
 
+Waits waits_of(const mor_adapter_desc_t& d)
+{
+    Waits w = {d.status, 0, 0};
+    test_hook_main(w.skip, w.cycles);
+    return w;
+}
+
 mor_status_t check_adapter(const mor_adapter_desc_t* d)
 {
     if (d == nullptr || d->tokens < 0 || d->tokens >= (1ll << 30) || d->n_in < 1 || d->n_out < 1 || d->n_in > kMaxWidth || d->n_out > kMaxWidth) return MOR_ERR_INVALID_ARG;
@@ -1483,10 +1506,10 @@ mor_status_t mor_adapter_add(const mor_adapter_desc_t* d, const void* x, int64_t
         if (st != MOR_OK) return st;
     }
     const int padded = padded_rank(d->rank);
-    ShrinkParams sp = {f.s, static_cast<const bf16*>(x), static_cast<const bf16*>(d->a), d->scale, d->factor, ldx, d->n_in, d->n_in, (int64_t)d->rank * d->n_in, d->rank, padded, f.h, d->status};
+    ShrinkParams sp = {f.s, static_cast<const bf16*>(x), static_cast<const bf16*>(d->a), d->scale, d->factor, ldx, d->n_in, d->n_in, (int64_t)d->rank * d->n_in, d->rank, d->rank, padded, f.h, waits_of(*d)};
     if (shrink(sp, rows, any, stream) != cudaSuccess) return MOR_ERR_CUDA;
     ExpandParams ep = {f.s, f.h, static_cast<const bf16*>(d->b), d->n_out, d->rank, (int64_t)d->n_out * d->rank, d->rank, padded, base, out, ldb, ldo, 0, 0,
-                       d->rank % 8 == 0 && is_aligned(d->b, 16), base_whole, out_whole, d->status};
+                       d->rank % 8 == 0 && is_aligned(d->b, 16), base_whole, out_whole, waits_of(*d)};
     return status(expand(ep, rows, dtype, stream));
 }
 
@@ -1520,19 +1543,19 @@ mor_status_t mor_adapter_grad(const mor_adapter_desc_t* d, const void* x, int64_
         const uint32_t a_ctas = (uint32_t)(ceil_div(padded, 32) * ceil_div(d->n_in, 32)), b_ctas = (uint32_t)(ceil_div(w.wide, 32) * ceil_div(padded, 32));
         TurnParams tp = {static_cast<const bf16*>(d->a), static_cast<const bf16*>(d->b), w.at, w.bt, d->n_in, d->n_out, w.wide, d->rank, padded, a_ctas};
         if (launch_clusters(adapter_turn_kernel, dim3(a_ctas + b_ctas, (uint32_t)d->adapters), 0, 256, 0, stream, tp) != cudaSuccess) return MOR_ERR_CUDA;
-        ShrinkParams sp = {f.s, static_cast<const bf16*>(dy), w.bt, d->scale, d->factor, lddy, d->n_out, w.wide, (int64_t)padded * w.wide, padded, padded, w.u, d->status};
+        ShrinkParams sp = {f.s, static_cast<const bf16*>(dy), w.bt, d->scale, d->factor, lddy, d->n_out, w.wide, (int64_t)padded * w.wide, padded, d->rank, padded, w.u, waits_of(*d)};
         if (shrink(sp, rows, !dy_whole, stream) != cudaSuccess) return MOR_ERR_CUDA;
     }
     if (db != nullptr) {
-        OuterParams op = {f.s, f.h, static_cast<const bf16*>(dy), lddy, d->n_out, d->rank, padded, static_cast<bf16*>(db), d->status};
+        OuterParams op = {f.s, f.h, static_cast<const bf16*>(dy), lddy, d->n_out, d->rank, padded, static_cast<bf16*>(db), waits_of(*d)};
         if (outer(op, true, !dy_whole, stream) != cudaSuccess) return MOR_ERR_CUDA;
     }
     if (da != nullptr) {
-        OuterParams op = {f.s, w.u, static_cast<const bf16*>(x), ldx, d->n_in, d->rank, padded, static_cast<bf16*>(da), d->status};
+        OuterParams op = {f.s, w.u, static_cast<const bf16*>(x), ldx, d->n_in, d->rank, padded, static_cast<bf16*>(da), waits_of(*d)};
         if (outer(op, false, !x_whole, stream) != cudaSuccess) return MOR_ERR_CUDA;
     }
     if (dx != nullptr) {
-        ExpandParams ep = {f.s, w.u, w.at, d->n_in, padded, (int64_t)d->n_in * padded, padded, padded, base, dx, ldb, lddx, 0, 0, true, base_whole, dx_whole, d->status};
+        ExpandParams ep = {f.s, w.u, w.at, d->n_in, padded, (int64_t)d->n_in * padded, padded, padded, base, dx, ldb, lddx, 0, 0, true, base_whole, dx_whole, waits_of(*d)};
         if (expand(ep, rows, MOR_DTYPE_BF16, stream) != cudaSuccess) return MOR_ERR_CUDA;
     }
     return MOR_OK;

@@ -56,6 +56,9 @@ class AdamW(torch.optim.Optimizer):
         for i, p in zip(ids, (p for g in self.param_groups for p in g["params"])):
             if i in stored:
                 self.state[p] = {k: v.clone().to(p.device) if isinstance(v, torch.Tensor) else v for k, v in stored[i].items()}
+        for group in self.param_groups:
+            if group["step"] is not None:
+                group["step"] = group["step"].to(group["params"][0].device)
 
     @torch.no_grad()
     def step(self, closure=None, *, grad_scale=None, found_inf=None):

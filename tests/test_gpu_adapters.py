@@ -223,6 +223,54 @@ def test_what_is_not_finite_stays_in_its_row(adapters):
         assert (y[rest] == clean[rest]).all() and not y[3].isfinite().any() and not y[8].isfinite().any()
 
 
+def test_infinities_of_ranks_that_do_not_fill_an_instruction(adapters):
+    """Where all factors are positive an infinite x gives an infinite result, whatever the ranks are filled up with."""
+    import torch
+
+    bf16 = dict(device="cuda", dtype=torch.bfloat16)
+    for tokens, rank in ((5, 3), (300, 3), (2500, 3), (300, 70), (2500, 40)):
+        x, a, b = torch.ones(tokens, 40, **bf16), torch.ones(1, rank, 40, **bf16), torch.ones(1, 48, rank, **bf16)
+        x[3, 7] = float("inf")
+        y = adapters.add(torch.zeros(tokens, 48, **bf16), x, a, b)
+        assert (y[3] == float("inf")).all() and (y[4] == 40 * rank).all()
+
+
+def test_a_wait_that_runs_out_is_reported(adapters):
+    """The library's test hook keeps one CTA from announcing its first products and shortens the limit to about a millisecond: the call returns, the status word says
+    so, and the same call without the hook is right."""
+    import ctypes
+
+    import torch
+
+    from paper_2512_22804_b200 import binding as mb
+    from paper_2512_22804_b200 import fp4
+
+    hook = mb.load().mor_test_skip_tile_load
+    hook.argtypes, hook.restype = [ctypes.c_uint32, ctypes.c_longlong], None
+    x, y0, a, b, ids, scale = draw(3000, 640, 712, 16, 2, seed=8)
+    dy = torch.randn(y0.shape, device="cuda").to(torch.bfloat16)
+    want = run_grads(adapters, y0, x, a, b, ids, scale, dy)
+    y = adapters.add(y0, x, a, b, ids, scale)
+    torch.cuda.synchronize()
+    fp4.check()
+    for kind in ("forward", "backward"):
+        leaves = [t.detach().requires_grad_() for t in (x, a, b)]
+        out = adapters.add(y0, *leaves, ids, scale)
+        torch.cuda.synchronize()
+        hook(0, 2_000_000)
+        try:
+            adapters.add(y0, x, a, b, ids, scale) if kind == "forward" else torch.autograd.grad(out, leaves, dy)
+            torch.cuda.synchronize()
+        finally:
+            hook(0xFFFFFFFF, 0)
+        with pytest.raises(mb.MorError) as error:
+            fp4.check()
+        assert error.value.status == mb.MOR_ERR_TIMEOUT
+        assert (adapters.add(y0, x, a, b, ids, scale) == y).all()
+        assert all((p == q).all() for p, q in zip(want, run_grads(adapters, y0, x, a, b, ids, scale, dy)))
+        fp4.check()
+
+
 def test_captured_and_on_another_stream(adapters):
     import torch
 

@@ -423,6 +423,14 @@ def test_optimizer_captured(optim):
         graph.replay()
     torch.cuda.synchronize()
     assert int(c.param_groups[0]["step"]) == 5
+    r, again = fresh(True)                     # the count goes through a stored state, on whatever device that was loaded
+    state = c.state_dict()
+    state["param_groups"][0]["step"] = state["param_groups"][0]["step"].cpu()
+    again.load_state_dict(state)
+    for t, g in zip(r, grads):
+        t.grad = g.to(t.dtype)
+    again.step()
+    assert int(again.param_groups[0]["step"]) == 6 and int(c.param_groups[0]["step"]) == 5
     for a, b in zip(p, q):                     # the bias corrections are made another way: an update differs by some u, a BF16 rounding may fall the other way
         d = (a.detach().double() - b.detach().double()).abs()
         assert (d <= 5e-6 + a.detach().double().abs() * (2.0 ** -7 if a.dtype == torch.bfloat16 else 1e-5)).all() and (d > 1e-6).double().mean() < 0.01
