@@ -502,6 +502,7 @@ mor_status_t mor_adamw(const mor_adamw_desc_t* d, const mor_adamw_tensor_t* t, i
             !is_aligned(x.exp_avg_sq, state) || (d->eight_bits && !is_aligned(x.scales, 2)))
             return MOR_ERR_ALIGNMENT;
     }
+    if (all == 0) return MOR_OK;
     AdamwScalars s = {};
     s.lr = (float)d->lr;
     s.beta1 = (float)d->beta1;
