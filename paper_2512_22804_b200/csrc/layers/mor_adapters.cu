@@ -1,15 +1,15 @@
 // Low-rank adapters beside a shared projection: out = base + s (x a^T) b^T with an adapter for every token, and the gradients.
 //
-// The ranks are small, so every product here moves far more than it multiplies: the wide matrices (x, base, out, dy) are read and written once, and
-// what has to be kept in flight for that decides the shape of the kernels.  Tiles come by asynchronous copies of 16 bytes into rings of shared memory
-// (rows lie wherever the tokens of an adapter are, so the copies are a thread's own and not a tensor map's), fragments from there to the registers of the
-// tensor instructions (mma.sync, BF16 in, FP32 sums).
+// The ranks are small, so every product here moves far more than it multiplies: the wide matrices (x, base, out, dy) are read and written once by each
+// kernel, and what has to be kept in flight for that decides the shape of the kernels.  Tiles come by asynchronous copies of 16 bytes into rings of shared memory
+// (rows lie wherever the tokens of an adapter are, so the copies are a thread's own and not a tensor map's).
 //
 // Tiles of 128 rows (and every `outer`) go through the fifth-generation tensor cores, whose operands stay in shared memory and whose sums are in tensor
-// memory: by mma.sync the products of 64 ranks took longer than the memory does.  Where an adapter has few rows, tiles of 32 by mma.sync leave less empty.
+// memory: by mma.sync the products of 64 ranks took longer than the memory does (8192 tokens, 4096 -> 4096, rank 64, training: 308 us, 148 now, of which the bytes
+// take 53).  Where an adapter has few rows, tiles of 32 by mma.sync (BF16 in, FP32 sums) leave less empty.
 //
 //   shrink   h = s x a^T              reduction over the width, cut over a cluster's CTAs and joined through distributed shared memory
-//   expand   out = base + h b^T       h as the sum of two BF16 (16 bits and more), in registers while the columns pass
+//   expand   out = base + h b^T       h as the sum of two BF16 (16 bits and more), kept while the columns pass
 //   outer    db = dy^T h, da = u^T x  reduction over an adapter's tokens, cut and joined like shrink
 //   small    shrink and expand of up to 16 tokens of an adapter by one cluster, in one launch, for few tokens
 //
@@ -281,10 +281,10 @@ __device__ __forceinline__ void products_commit(Products& c, int which, int32_t 
     if (step > 0 || blockIdx.x != w.skip) tc_commit<1>(shared_at(&c.done[which]));
 }
 
-// Joins the rows' sums over the cluster's CTAs and stores them as pairs of BF16.  part: [rows][R + 4], of this CTA.  What is past the ranks that there are is
-// zero whatever x holds.
+// Joins the rows' sums over the cluster's CTAs and stores them as pairs of BF16.  part: [rows][R + 4], of this CTA; there: a bit for every row that has a token.
+// What is past the ranks that there are, and rows without a token, are zero whatever x and m hold (zero times infinity).
 template <int R>
-__device__ __forceinline__ void join_rows(float* part, int rows, int64_t first, int r0, float scale, bf16* h, int padded, int ranks, uint32_t rank, uint32_t ctas)
+__device__ __forceinline__ void join_rows(float* part, const uint32_t* there, int rows, int64_t first, int r0, float scale, bf16* h, int padded, int ranks, uint32_t rank, uint32_t ctas)
 {
     constexpr int kPitch = R + 4;
     cluster_arrive();
@@ -296,7 +296,7 @@ __device__ __forceinline__ void join_rows(float* part, int rows, int64_t first, 
         const float f[4] = {v.x * scale, v.y * scale, v.z * scale, v.w * scale};
         bf16 hi[4], lo[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) split(r0 + col + k < ranks ? f[k] : 0.f, hi[k], lo[k]);
+        for (int k = 0; k < 4; ++k) split((there[row >> 5] >> (row & 31) & 1u) != 0 && r0 + col + k < ranks ? f[k] : 0.f, hi[k], lo[k]);
         uint16_t* to = reinterpret_cast<uint16_t*>(h) + (first + row) * 2 * padded + r0 + col;
         *reinterpret_cast<ushort4*>(to) = make_ushort4(bits_of(hi[0]), bits_of(hi[1]), bits_of(hi[2]), bits_of(hi[3]));
         *reinterpret_cast<ushort4*>(to + padded) = make_ushort4(bits_of(lo[0]), bits_of(lo[1]), bits_of(lo[2]), bits_of(lo[3]));
@@ -363,12 +363,14 @@ template <int R, int ROWS, int THREADS, bool ANY> struct ShrinkCopies {
     }
 };
 
-// A CTA takes 128 rows of one adapter and all ranks; a cluster's CTAs share the reduction axis.
+// A CTA takes 128 rows of one adapter and all ranks; a cluster's CTAs share the reduction axis.  Bound by latency: 8192 rows of 4096, rank 64, take 19-21 us, 10 of
+// them for the 67 MB at the copy rate, the others launch, first loads and join.
 template <int R, bool ANY> __global__ void __launch_bounds__(256) adapter_shrink_kernel(const __grid_constant__ ShrinkParams p)
 {
     constexpr int kColumns = R < 32 ? 32 : R;
     extern __shared__ uint8_t smem_raw[];
     __shared__ Products c;
+    __shared__ uint32_t there[4];
     products_begin(c, kColumns);
     wait_for_predecessor();
     const uint32_t rank = cluster_rank(), ctas = cluster_size(), smem = (shared_at(smem_raw) + 1023u) & ~1023u;
@@ -383,6 +385,10 @@ template <int R, bool ANY> __global__ void __launch_bounds__(256) adapter_shrink
     bool given_up = false;
 #pragma unroll
     for (int s = 0; s < kShrinkStages - 1; ++s) copies.fill(s);
+    if (warp < 4) {
+        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, token_at(p.s, first + warp * 32 + lane) >= 0);
+        if (lane == 0) there[warp] = mask;
+    }
     for (int32_t n = 0; n < copies.count; ++n) {
         copies_wait<kShrinkStages - 2>();
         fence_async_smem();
@@ -416,15 +422,16 @@ template <int R, bool ANY> __global__ void __launch_bounds__(256) adapter_shrink
         for (int k = 0; k < 16; k += 4) *reinterpret_cast<uint4*>(part + ((warp & 3) * 32 + lane) * (R + 4) + r + k) = make_uint4(v[k], v[k + 1], v[k + 2], v[k + 3]);
     }
     products_end(c, kColumns, given_up);
-    join_rows<R>(part, 128, first, 0, (p.scale != nullptr ? p.scale[adapter] : 1.f) * p.factor, p.h, p.padded, p.rank, rank, ctas);
+    join_rows<R>(part, there, 128, first, 0, (p.scale != nullptr ? p.scale[adapter] : 1.f) * p.factor, p.h, p.padded, p.rank, rank, ctas);
 }
 
-// A CTA takes 32 rows of one adapter and R of the ranks (blockIdx.y); a warp works on a quarter of each step.
+// A CTA takes 32 rows of one adapter and R of the ranks (blockIdx.y); a warp works on a quarter of each step.  1187 tokens of 1500, rank 24: 12 us, latency.
 template <int R, bool ANY> __global__ void __launch_bounds__(128) adapter_shrink32_kernel(const __grid_constant__ ShrinkParams p)
 {
     constexpr int kTiles = R / 8, kPitch = R + 4;
     static_assert(4 * kRows * kPitch * 4 <= kShrinkSmem<R, kRows> - 1024, "the sums take the ring's place");
     extern __shared__ uint8_t smem_raw[];
+    __shared__ uint32_t there[1];
     wait_for_predecessor();
     const uint32_t rank = cluster_rank(), ctas = cluster_size(), smem = (shared_at(smem_raw) + 1023u) & ~1023u;
     const int64_t first = (int64_t)(blockIdx.x / ctas) * kRows;
@@ -441,6 +448,10 @@ template <int R, bool ANY> __global__ void __launch_bounds__(128) adapter_shrink
             for (int k = 0; k < 4; ++k) acc[i][j][k] = 0.f;
 #pragma unroll
     for (int s = 0; s < kShrinkStages - 1; ++s) copies.fill(s);
+    if (warp == 0) {
+        const uint32_t mask = __ballot_sync(0xFFFFFFFFu, token_at(p.s, first + lane) >= 0);
+        if (lane == 0) there[0] = mask;
+    }
     for (int32_t step = 0; step < copies.count; ++step) {
         copies_wait<kShrinkStages - 2>();
         __syncthreads();
@@ -487,7 +498,7 @@ template <int R, bool ANY> __global__ void __launch_bounds__(128) adapter_shrink
         }
         *to = v;
     }
-    join_rows<R>(part, kRows, first, r0, (p.scale != nullptr ? p.scale[adapter] : 1.f) * p.factor, p.h, p.padded, p.rank, rank, ctas);
+    join_rows<R>(part, there, kRows, first, r0, (p.scale != nullptr ? p.scale[adapter] : 1.f) * p.factor, p.h, p.padded, p.rank, rank, ctas);
 }
 
 // ------------------------------------------------------------------------------------------- expand ----
@@ -667,7 +678,8 @@ template <typename T> __device__ __forceinline__ void copy_tokens(const ExpandPa
 }
 
 // A CTA takes 128 rows of one adapter and walks columns, 64 a step, with h in shared memory.  The products of a step run while the step before is read out
-// of the other set of accumulators, added to its base and stored.
+// of the other set of accumulators, added to its base and stored.  4096 -> 14336, rank 32, 8192 tokens: 94 us, 4.9 TB/s (a copy: 6.5) with
+// 42 % of the issue slots and no byte read twice.  A tile's CTAs side by side in the grid, more and shorter CTAs, streaming stores: no difference.
 // Three stages where a fourth would leave room for one CTA an SM only (two are worth more).
 template <int R, typename T, int BASE> constexpr int kExpandStage = 64 * ((BASE != NO_BASE ? 128 * (int)sizeof(T) : 0) + R * 2);
 template <int R, typename T, int BASE> constexpr int kExpandRest = 2 * 128 * R * 2 + 1024;
@@ -765,7 +777,7 @@ template <int R, typename T, int BASE> __global__ void __launch_bounds__(256, BA
     copy_tokens<T>(p);
 }
 
-// A CTA takes 32 rows of one adapter and walks columns, 128 a step and 32 of them a warp; h is in registers.
+// A CTA takes 32 rows of one adapter and walks columns, 128 a step and 32 of them a warp; h is in registers.  1187 tokens, rank 24, 1500 -> 2731: 15 us, latency.
 constexpr int kExpand32Stages = 3;
 template <int R, typename T, int BASE> constexpr int kExpand32Smem = kExpand32Stages * 128 * ((BASE != NO_BASE ? kRows * (int)sizeof(T) : 0) + R * 2) + 128;
 
@@ -926,7 +938,7 @@ struct OuterParams {
 };
 
 // 128 columns x R ranks of an adapter: the reduction runs over its rows, 64 a step, cut over a cluster's CTAs.  Both operands have the reduction axis across
-// their rows, as they lie in memory.
+// their rows, as they lie in memory.  Bound by latency like shrink: 8192 rows, 4096 columns, rank 64 take 25-27 us.
 constexpr int kOuterStages = 3, kOuterCols = 128, kOuterRows = 64;
 template <int R> constexpr int kOuterStage = kOuterRows * (kOuterCols + 2 * R) * 2;
 template <int R> constexpr int kOuterSmem = kOuterStages * kOuterStage<R> + 1024;
@@ -1060,7 +1072,7 @@ struct TurnParams {
     uint32_t a_ctas;           // CTAs of a for one adapter
 };
 
-// Both matrices of the adapters with their axes swapped, for the gradients' products: tiles of 32 x 32.
+// Both matrices of the adapters with their axes swapped, for the gradients' products: tiles of 32 x 32.  Rank 64, 4096 and 4096: 3.6 us, a launch's latency.
 __global__ void __launch_bounds__(256) adapter_turn_kernel(const __grid_constant__ TurnParams p)
 {
     __shared__ bf16 tile[32][33];
@@ -1101,7 +1113,8 @@ struct SmallParams {
 // A cluster of 8 for every token (every 16 without ids).  The first of each 16 tokens of an adapter, in token order, leads: its cluster takes all of
 // them and the others' clusters end.  Every CTA sums its part of the width over its warps, then all parts are joined from the 8 shared
 // memories, and each CTA makes an eighth of the columns (or less: where tiles are few and columns many, several clusters do the first part alike and
-// share the columns).  Bound by the latency of four dependent reads (ids, x and a, b and base, and the exchange).
+// share the columns).  Bound by the latency of four dependent reads (ids, x and a, b and base, and the exchange): one token, rank 16, 4096 -> 14336 4.8 us in a graph,
+// 48 tokens of 24 adapters, rank 32, 4096 -> 4096 7.7.
 template <int R, typename T, bool ANY> __global__ void __cluster_dims__(kMaxCluster, 1, 1) __launch_bounds__(kSmallWarps * 32)
     adapter_small_kernel(const __grid_constant__ SmallParams p)
 {

@@ -235,6 +235,26 @@ def test_infinities_of_ranks_that_do_not_fill_an_instruction(adapters):
         assert (y[3] == float("inf")).all() and (y[4] == 40 * rank).all()
 
 
+def test_infinite_adapters_and_rows_that_only_fill_a_tile_up(adapters):
+    """Where all factors are positive, the gradients of an adapter with an infinite element are infinite where it counts and not NaN, however many rows its last tile has
+    left; another adapter's are what they are without it."""
+    import torch
+
+    bf16 = dict(device="cuda", dtype=torch.bfloat16)
+    for tokens, rank in ((5, 3), (300, 16), (2500, 16), (2500, 40), (300, 70)):
+        for n in (1, 2):
+            ids = (torch.arange(tokens, device="cuda") % n).to(torch.int32) if n > 1 else None
+            x, base, dy = torch.ones(tokens, 40, **bf16), torch.zeros(tokens, 48, **bf16), torch.ones(tokens, 48, **bf16)
+            a, b = torch.ones(n, rank, 40, **bf16), torch.ones(n, 48, rank, **bf16)
+            a[0, 1, 7], b[0, 3, 2] = float("inf"), float("inf")
+            leaves = [t.requires_grad_() for t in (x, a, b)]
+            _, da, db = torch.autograd.grad(adapters.add(base, *leaves, ids), leaves, dy)
+            assert not da.isnan().any() and not db.isnan().any()
+            want_da, want_db = torch.zeros_like(da, dtype=torch.bool), torch.zeros_like(db, dtype=torch.bool)
+            want_da[0, 2], want_db[0, :, 1] = True, True
+            assert (da.isinf() == want_da).all() and (db.isinf() == want_db).all()
+
+
 def test_a_wait_that_runs_out_is_reported(adapters):
     """The library's test hook keeps one CTA from announcing its first products and shortens the limit to about a millisecond: the call returns, the status word says
     so, and the same call without the hook is right."""
