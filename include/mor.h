@@ -419,7 +419,7 @@ MOR_API mor_status_t mor_expert_combine_grad(const mor_expert_desc_t* host_desc,
  * scales of mor_analyze_quantize with the (1,128) and (1,0) partitions and the FP32-amax and E8M0 scale modes, made from y in binary32.
  * A NaN's code is 0x7F, an infinity's the largest finite value's. */
 typedef struct mor_norm_desc {
-    int64_t rows, cols;      /* cols < 2^31 - 4096                                             */
+    int64_t rows, cols;      /* cols < 2^31 - 16384                                            */
     const void* x;           /* DEVICE [rows, ldx], aligned to its element; full speed where rows start on 16 bytes      */
     const void* residual;    /* DEVICE [rows, ldr], optional                                   */
     const void* weight;      /* DEVICE [cols]                                                  */
@@ -451,7 +451,7 @@ MOR_API mor_status_t mor_rms_norm_grad(const mor_norm_desc_t* host_desc, int has
                                        void* dr, int64_t lddr, void* dweight, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /* Values of E4M3 codes [rows, ldc] with one scale per `block` columns (0: per row), E8M0 or FP32 (one of the two): code / scale rounded once
- * to `dtype`, [rows, ldo]. */
+ * to `dtype`, [rows, ldo].  cols <= 2^28. */
 MOR_API mor_status_t mor_codes_dequantize(const uint8_t* codes, int64_t rows, int64_t cols, int64_t ldc, int block, const uint8_t* scale_e8m0,
                                           const float* scale_f32, void* out, int dtype, int64_t ldo, void* cuda_stream);
 

@@ -1,8 +1,9 @@
 // One AdamW step over many tensors, moments in 32 bits or as E4M3 codes with one scale for 128 elements, and the values of such codes.
 //
-// Every element is read and written once: the kernel is bound by memory.  A launch takes the addresses of up to 512 tensors as its
+// Every element is read and written once.  With FP32 moments the kernel is bound by memory (103 M elements, 2.88 GB: 421 us, 6.8 TB/s), with 8-bit ones by its
+// instructions (80 an element: 285 us for 1.44 GB; with the read-back of the moments' values 400).  A launch takes the addresses of up to 512 tensors as its
 // parameters (a captured graph then needs no table in memory that has to outlive it), the smallest of three sizes of that table that holds them,
-// since a launch costs more the more it carries; each CTA finds its tensor by bisection and takes 4096 of its elements.
+// since a launch costs more the more it carries; each CTA finds its tensor by bisection and takes 2048 or 4096 of its elements.
 // A thread holds 8 consecutive elements, so 16 lanes hold a block of 128 and its maximum takes four shuffles.
 #include <math.h>
 
@@ -400,6 +401,7 @@ template <typename P, typename G, bool EIGHT, int N> __global__ void __launch_bo
     }
 }
 
+// The values that codes stand for, 8 elements a thread: 29 M elements to BF16 28 us, 6.3 TB/s.
 template <typename T> __global__ void __launch_bounds__(kThreads) moments_kernel(const uint8_t* m, const uint8_t* v, const uint8_t* scales, int64_t numel, T* m_out,
                                                                                 T* v_out, bool aligned)
 {

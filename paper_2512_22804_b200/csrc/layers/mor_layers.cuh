@@ -62,7 +62,6 @@ __device__ __forceinline__ void store_codes(uint2 c, uint8_t* at, int left, bool
         if (i < left) at[i] = (uint8_t)((i < 4 ? c.x : c.y) >> (8 * (i & 3)));
 }
 
-
 // Biased exponent of the largest power of two that keeps a >= 0 within 448 = 1.75 * 2^8, at most `most`; 127 for zero.
 __device__ __forceinline__ uint32_t power_scale(float a, uint32_t most)
 {

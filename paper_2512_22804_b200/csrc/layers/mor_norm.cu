@@ -156,6 +156,7 @@ template <typename T, typename R, int N> constexpr int kForwardRing = kRing * N 
 template <typename T, typename R, int G, int N> constexpr bool kAhead = kForwardRing<T, R, N> * (G > 256 ? G : 256) <= 220 * 1024;    // else the row alone fills it
 template <typename T, typename R, int N> constexpr int kGradRing = kRing * N * kPer * (int)(sizeof(T) + 2 * sizeof(R));
 
+// 8192 x 4096 BF16 with a residual: 40 us for h and y (268 MB, the copy rate), 42 for h and codes (235 MB, 5.6 TB/s; conversions fill 73 % of the issue slots).
 template <int G> constexpr int kForwardThreads = G > 256 ? G : 256;
 
 template <typename T, typename R, int G, int N, bool ANY> __global__ void __launch_bounds__(kForwardThreads<G>) norm_kernel(const __grid_constant__ NormParams p)
@@ -258,7 +259,7 @@ template <typename T, typename R, int G, int N, bool ANY> __global__ void __laun
     }
 }
 
-// Rows of any width.
+// Rows of any width, one a CTA.
 template <typename T, typename R> __global__ void __launch_bounds__(kWideThreads) norm_wide_kernel(const __grid_constant__ NormParams p)
 {
     __shared__ float shared[2][kWideThreads / 32];
@@ -339,7 +340,8 @@ template <typename T, typename R> __global__ void __launch_bounds__(kWideThreads
 // ------------------------------------------------------------------------------------------- gradient ----
 
 // dh = rs (g - xh mean(g xh)) + dh_in with g = dy w, xh = h rs: both sums of a row come from one reduction.  The weight's gradient is summed by
-// each thread over its group's rows, then over the CTA's groups in shared memory and over the CTAs by the join, always in the same order.
+// each thread over its group's rows, then over the CTA's groups in shared memory and over the CTAs by the join, always in the same order.  One CTA an SM, since every
+// CTA's sums are written and read again: 8192 x 4096 BF16, 46 us (268 MB, 5.8 TB/s), and 6 for the join, which is latency.
 template <int G> constexpr int kGradThreads = G > 512 ? G : 512;
 
 template <typename T, typename R, int G, int N, bool ANY> __global__ void __launch_bounds__(kGradThreads<G>) norm_grad_kernel(const __grid_constant__ NormParams p)
@@ -550,7 +552,7 @@ template <typename W> __global__ void __launch_bounds__(kJoinCols* kJoinParts) n
 
 // ------------------------------------------------------------------------------------------- values ----
 
-// 16 codes a thread at a time, of kValueRows rows: 16 bytes in, 32 or 64 out.
+// 16 codes a thread at a time, of kValueRows rows: 16 bytes in, 32 or 64 out.  8192 x 4096 to BF16: 25 us (101 MB), issue slots 68 % full.
 constexpr int kValueRows = 4;
 template <typename T> __global__ void __launch_bounds__(256) codes_values_kernel(const uint8_t* codes, int64_t rows, int32_t cols, int64_t ldc, int32_t by_row,
                                                                                  const uint8_t* e8m0, const float* f32, T* out, int64_t ldo, bool aligned)
