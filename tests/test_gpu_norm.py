@@ -121,6 +121,21 @@ def test_quantised(norm, rows, cols, types, block, kind):
         assert v.dtype == dtype and (v == exact.float().to(dtype)).all()
 
 
+def test_values_of_every_code_and_scales_of_any_size(norm):
+    """Bit for bit the quotient in 32 bits, whatever the scale: random ones of every exponent, the ends of the range, zero, infinity."""
+    import torch
+
+    g = torch.Generator(device="cuda").manual_seed(31)
+    codes = torch.arange(256, device="cuda", dtype=torch.int32).to(torch.uint8).view(torch.float8_e4m3fn).repeat(4096, 1)
+    scales = torch.exp2(torch.rand(4096, 1, generator=g, device="cuda", dtype=torch.float64) * 276 - 148).float()
+    scales[:8, 0] = torch.tensor([0.0, float("inf"), 2.0 ** -149, 3.402823466e+38, 2.0 ** -100, 2.0 ** 100, 1.0, -3.0])
+    want = codes.float() / scales
+    for dtype in (torch.float32, torch.bfloat16):
+        v, exact = norm.dequantize(codes, scales.expand(4096, 1), dtype), want.to(dtype)
+        whole = torch.int32 if dtype == torch.float32 else torch.int16
+        assert (exact.isnan() == v.isnan()).all() and ((v.view(whole) == exact.view(whole)) | exact.isnan()).all()
+
+
 @pytest.mark.parametrize("block,kind", [(128, 1), (128, 2), (None, 1), (None, 2)])
 def test_codes_are_those_of_the_analysis(norm, block, kind):
     """Rows of +-1 are normed to +-weight exactly (eps 0), a BF16 tensor that the analysis takes too: the codes and scales are the same bytes."""
