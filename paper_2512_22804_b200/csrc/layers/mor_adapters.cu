@@ -938,23 +938,20 @@ struct OuterParams {
 };
 
 // 128 columns x R ranks of an adapter: the reduction runs over its rows, 64 a step, cut over a cluster's CTAs.  Both operands have the reduction axis across
-// their rows, as they lie in memory.  Bound by latency like shrink: 8192 rows, 4096 columns, rank 64 take 25-27 us.
+// their rows, as they lie in memory.  Bound by latency like shrink: 8192 rows, 4096 columns, rank 64 took 25-27 us each.
 constexpr int kOuterStages = 3, kOuterCols = 128, kOuterRows = 64;
 template <int R> constexpr int kOuterStage = kOuterRows * (kOuterCols + 2 * R) * 2;
+template <int R> constexpr uint32_t kOuterColumns = R < 32 ? 32 : R;
 template <int R> constexpr int kOuterSmem = kOuterStages * kOuterStage<R> + 1024;
 
-template <int R, bool BY_COLUMN, bool ANY> __global__ void __launch_bounds__(256) adapter_outer_kernel(const __grid_constant__ OuterParams p)
+template <int R, bool BY_COLUMN, bool ANY> __device__ __forceinline__ void outer_part(const OuterParams& p, uint32_t z_block, Products& c, uint8_t* smem_raw)
 {
-    constexpr int kHalf = kOuterRows * R * 2, kColumns = R < 32 ? 32 : R;         // bytes of h's high parts; of tensor memory
+    constexpr int kHalf = kOuterRows * R * 2, kColumns = kOuterColumns<R>;        // bytes of h's high parts; of tensor memory
     constexpr int kLines = BY_COLUMN ? kOuterCols : R, kLine = BY_COLUMN ? R : kOuterCols, kPitch = kLine + 4;
     static_assert(kLines * kPitch * 4 <= kOuterSmem<R> - 1024, "the sums take the ring's place");
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ Products c;
-    products_begin(c, kColumns);
-    wait_for_predecessor();
     const uint32_t rank = cluster_rank(), ctas = cluster_size(), smem = (shared_at(smem_raw) + 1023u) & ~1023u;
     const int tid = threadIdx.x, warp = warp_number();
-    const int chunks = p.padded / R, adapter = blockIdx.z / chunks, r0 = blockIdx.z % chunks * R;
+    const int chunks = p.padded / R, adapter = z_block / chunks, r0 = z_block % chunks * R;
     const int64_t c0 = (int64_t)blockIdx.y * kOuterCols;
     const int64_t from = p.s.starts != nullptr ? p.s.starts[adapter] : 0, to = p.s.starts != nullptr ? p.s.starts[adapter + 1] : adapter == 0 ? p.s.rows : 0;
     const int32_t steps = (int32_t)((to - from + kOuterRows - 1) / kOuterRows), share = (steps + (int32_t)ctas - 1) / (int32_t)ctas;
@@ -1060,6 +1057,23 @@ template <int R, bool BY_COLUMN, bool ANY> __global__ void __launch_bounds__(256
     }
     cluster_arrive();
     cluster_wait();
+}
+
+// Both gradients in one launch, db = dy^T h for the first `split` of blockIdx.z, da = u^T x for the others: with half as many CTAs for each, the ramps are paid once.
+struct OuterPair {
+    OuterParams b, a;
+    uint32_t split;
+};
+template <int R, bool ANY> __global__ void __launch_bounds__(256) adapter_outer_kernel(const __grid_constant__ OuterPair p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ Products c;
+    const bool of_b = blockIdx.z < p.split;
+    if ((int64_t)blockIdx.y * kOuterCols >= (of_b ? p.b.n : p.a.n)) return;       // the whole cluster
+    products_begin(c, kOuterColumns<R>);
+    wait_for_predecessor();
+    if (of_b) outer_part<R, true, ANY>(p.b, blockIdx.z, c, smem_raw);
+    else outer_part<R, false, ANY>(p.a, blockIdx.z - p.split, c, smem_raw);
 }
 
 // ---------------------------------------------------------------------------------------- transposes ----
@@ -1427,21 +1441,25 @@ cudaError_t expand(const ExpandParams& p, int rows, int dtype, cudaStream_t st)
     return p.base_whole ? expand_rows<float, WHOLE_BASE>(p, rows, st) : expand_rows<float, ANY_BASE>(p, rows, st);
 }
 
-template <int R, bool BY_COLUMN, bool ANY> cudaError_t outer_launch(const OuterParams& p, cudaStream_t st)
+template <int R, bool ANY> cudaError_t outer_launch(const OuterPair& p, uint32_t deep, cudaStream_t st)
 {
     static std::atomic<uint64_t> done{0};
-    const uint32_t across = (uint32_t)((p.n + kOuterCols - 1) / kOuterCols), deep = (uint32_t)(p.s.adapters * (p.padded / R));
-    const int64_t mean = p.s.rows / p.s.adapters;      // two steps each at least, going by the adapters' mean
+    const int64_t nb = p.split > 0 ? ceil_div(p.b.n, kOuterCols) : 0, na = deep > p.split ? ceil_div(p.a.n, kOuterCols) : 0;
+    const Sorted& s = p.split > 0 ? p.b.s : p.a.s;
+    const int64_t mean = s.rows / s.adapters, all = nb * p.split + na * (deep - p.split);      // two steps each at least, going by the adapters' mean
     uint32_t cluster = 1;
-    while (cluster < kMaxCluster && (int64_t)across * deep * cluster * 2 <= resident(kOuterSmem<R>) && mean >= 4 * kOuterRows * (int64_t)cluster) cluster *= 2;
-    return launch_ring(adapter_outer_kernel<R, BY_COLUMN, ANY>, done, kOuterSmem<R>, dim3(cluster, across, deep), cluster, 256, st, p);
+    while (cluster < kMaxCluster && all * cluster * 2 <= resident(kOuterSmem<R>) && mean >= 4 * kOuterRows * (int64_t)cluster) cluster *= 2;
+    return launch_ring(adapter_outer_kernel<R, ANY>, done, kOuterSmem<R>, dim3(cluster, (uint32_t)std::max(na, nb), deep), cluster, 256, st, p);
 }
-cudaError_t outer(const OuterParams& p, bool by_column, bool any, cudaStream_t st)
+// Of b, of a or of both; the other's `out` is null.
+cudaError_t outer(const OuterParams& b, const OuterParams& a, bool any, cudaStream_t st)
 {
-    return by_rank(p.padded > 64 ? 64 : p.padded, [&](auto r) {
+    const OuterParams& one = b.out != nullptr ? b : a;
+    return by_rank(one.padded > 64 ? 64 : one.padded, [&](auto r) {
         constexpr int R = decltype(r)::value;
-        if (by_column) return any ? outer_launch<R, true, true>(p, st) : outer_launch<R, true, false>(p, st);
-        return any ? outer_launch<R, false, true>(p, st) : outer_launch<R, false, false>(p, st);
+        const uint32_t each = (uint32_t)(one.s.adapters * (one.padded / R)), deep = (b.out != nullptr ? each : 0) + (a.out != nullptr ? each : 0);
+        const OuterPair p = {b, a, b.out != nullptr ? each : 0};
+        return any ? outer_launch<R, true>(p, deep, st) : outer_launch<R, false>(p, deep, st);
     });
 }
 
@@ -1565,13 +1583,10 @@ mor_status_t mor_adapter_grad(const mor_adapter_desc_t* d, const void* x, int64_
         ShrinkParams sp = {f.s, static_cast<const bf16*>(dy), w.bt, d->scale, d->factor, lddy, d->n_out, w.wide, (int64_t)padded * w.wide, padded, d->rank, padded, w.u, waits_of(*d)};
         if (shrink(sp, rows, !dy_whole, stream) != cudaSuccess) return MOR_ERR_CUDA;
     }
-    if (db != nullptr) {
-        OuterParams op = {f.s, f.h, static_cast<const bf16*>(dy), lddy, d->n_out, d->rank, padded, static_cast<bf16*>(db), waits_of(*d)};
-        if (outer(op, true, !dy_whole, stream) != cudaSuccess) return MOR_ERR_CUDA;
-    }
-    if (da != nullptr) {
-        OuterParams op = {f.s, w.u, static_cast<const bf16*>(x), ldx, d->n_in, d->rank, padded, static_cast<bf16*>(da), waits_of(*d)};
-        if (outer(op, false, !x_whole, stream) != cudaSuccess) return MOR_ERR_CUDA;
+    if (da != nullptr || db != nullptr) {
+        const OuterParams b = {f.s, f.h, static_cast<const bf16*>(dy), lddy, d->n_out, d->rank, padded, static_cast<bf16*>(db), waits_of(*d)};
+        const OuterParams a = {f.s, w.u, static_cast<const bf16*>(x), ldx, d->n_in, d->rank, padded, static_cast<bf16*>(da), waits_of(*d)};
+        if (outer(b, a, (db != nullptr && !dy_whole) || (da != nullptr && !x_whole), stream) != cudaSuccess) return MOR_ERR_CUDA;
     }
     if (dx != nullptr) {
         ExpandParams ep = {f.s, w.u, w.at, d->n_in, padded, (int64_t)d->n_in * padded, padded, padded, base, dx, ldb, lddx, 0, 0, true, base_whole, dx_whole, waits_of(*d)};
