@@ -5,7 +5,7 @@
 // (rows lie wherever the tokens of an adapter are, so the copies are a thread's own and not a tensor map's).
 //
 // Tiles of 128 rows (and every `outer`) go through the fifth-generation tensor cores, whose operands stay in shared memory and whose sums are in tensor
-// memory: by mma.sync the products of 64 ranks took longer than the memory does (8192 tokens, 4096 -> 4096, rank 64, training: 308 us, 148 now, of which the bytes
+// memory: by mma.sync the products of 64 ranks took longer than the memory does (8192 tokens, 4096 -> 4096, rank 64, training: 308 us, 141 now, of which the bytes
 // take 53).  Where an adapter has few rows, tiles of 32 by mma.sync (BF16 in, FP32 sums) leave less empty.
 //
 //   shrink   h = s x a^T              reduction over the width, cut over a cluster's CTAs and joined through distributed shared memory
