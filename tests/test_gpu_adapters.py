@@ -321,6 +321,37 @@ def test_captured_and_on_another_stream(adapters):
         assert (y1 == want).all() and (y2 == want).all() and all((p == q).all() for p, q in zip(grads, g1))
 
 
+def test_two_streams_at_once(adapters):
+    """Calls on two streams, forward and backward and the 4-bit product beside them, give bit for bit what they give one after the other."""
+    import torch
+
+    from paper_2512_22804_b200 import fp4
+
+    calls = []
+    for seed in (11, 12):
+        x, y0, a, b, ids, scale = draw(3000, 640, 712, 24, 3, seed=seed)
+        dy = torch.randn(y0.shape, device="cuda").to(torch.bfloat16)
+        w = fp4.quantize(torch.randn(704, 640, device="cuda").to(torch.bfloat16), "e8m0_32")[0]
+        calls.append((x, y0, a, b, ids, scale, dy, w))
+
+    def run(x, y0, a, b, ids, scale, dy, w):
+        return [adapters.add(y0, x, a, b, ids, scale), *run_grads(adapters, y0, x, a, b, ids, scale, dy),
+                adapters.linear(x, w, a, b[:, :704].contiguous(), ids, scale)]
+
+    want = [run(*c) for c in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = []
+    for _ in range(5):
+        for c, s in zip(calls, streams):
+            with torch.cuda.stream(s):
+                got.append(run(*c))
+    torch.cuda.synchronize()
+    for n, results in enumerate(got):
+        assert all((p == q).all() for p, q in zip(want[n % 2], results))
+    fp4.check()
+
+
 @pytest.mark.parametrize("fmt", ["e8m0_32", "e4m3_16"])
 @pytest.mark.parametrize("tokens", [3, 300])
 def test_linear(adapters, fmt, tokens):
