@@ -1,7 +1,8 @@
 // One AdamW step over many tensors, moments in 32 bits or as E4M3 codes with one scale for 128 elements, and the values of such codes.
 //
 // Every element is read and written once.  With FP32 moments the kernel is bound by memory (103 M elements, 2.88 GB: 421 us, 6.8 TB/s), with 8-bit ones by its
-// instructions (80 an element: 285 us for 1.44 GB; with the read-back of the moments' values 400).  A launch takes the addresses of up to 512 tensors as its
+// instructions (80 an element: 285 us for 1.44 GB; with the read-back of the moments' values 400, and 418 since sums and roots are
+// rounded as formulas without fused operations round them).  A launch takes the addresses of up to 512 tensors as its
 // parameters (a captured graph then needs no table in memory that has to outlive it), the smallest of three sizes of that table that holds them,
 // since a launch costs more the more it carries; each CTA finds its tensor by bisection and takes 2048 or 4096 of its elements.
 // A thread holds 8 consecutive elements, so 16 lanes hold a block of 128 and its maximum takes four shuffles.
@@ -32,6 +33,7 @@ struct AdamwEntry {
 
 struct AdamwScalars {
     float lr, beta1, beta2, rest1, rest2, eps, decay;      // rest: 1 - beta; decay: weight decay
+    float one;                                             // 1
     float bias1, bias2;                                    // 1 / (1 - beta1^step), 1 / sqrt(1 - beta2^step)
     float log1, log2;                                      // log beta
     uint32_t seed, step, number, count;                    // number: of the first tensor in the call; count: tensors of this launch
@@ -90,6 +92,13 @@ __device__ __forceinline__ Pair fma(Pair a, Pair b, Pair c)
     return r;
 }
 
+__device__ __forceinline__ Pair fma_cut(Pair a, Pair b, Pair c)
+{
+    Pair r;
+    asm("fma.rz.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
 // What power_scale() needs of a magnitude, as a whole number that grows with it (a 16-bit one, above 254 for what is not finite), so that the maxima of both
 // moments of a block of 128 take one exchange: 16 lanes with 8 elements each.
 __device__ __forceinline__ uint32_t rank_of(float a) { return (__float_as_uint(a) + 0x1FFFFFu) >> 23; }
@@ -119,7 +128,7 @@ __device__ __forceinline__ float largest_finite(const float* v)
 }
 
 // Between its neighbours among the E4M3 values a magnitude w <= 448 has 20 fraction bits below the three that are kept, if it is a normal one (2^-6 and up).
-// Below, the distance stays that of 2^-6: with 2^-6 added the bits lie the same way (and the sum is off by 2^-21 of a distance at most).  Where w is below, 2^30
+// Below, the distance stays that of 2^-6: with 2^-6 added the bits lie the same way (what is cut off there lies below the 16 random bits).  Where w is below, 2^30
 // times the (exact) difference is at least 1, and for squares 2^37 times theirs.
 // Up where t + u >= n + 1: the random bits (16 of them) are added below the kept ones and what is below is cut off.
 __device__ __forceinline__ Pair round_mean(Pair w, uint32_t r0, uint32_t r1)
@@ -128,7 +137,7 @@ __device__ __forceinline__ Pair round_mean(Pair w, uint32_t r0, uint32_t r1)
     apart(w, w0, w1);
     apart(mul(w, w), x0, x1);
     const Pair below = pair(copysignf(__saturatef(fmaf(x0, -0x1p37f, 0x1p25f)), w0), copysignf(__saturatef(fmaf(x1, -0x1p37f, 0x1p25f)), w1));
-    apart(fma(below, both(0x1p-6f), w), s0, s1);
+    apart(fma_cut(below, both(0x1p-6f), w), s0, s1);
     s0 = __uint_as_float((r0 * 16u + __float_as_uint(s0)) & 0xFFF00000u);
     s1 = __uint_as_float((r1 * 16u + __float_as_uint(s1)) & 0xFFF00000u);
     return fma(below, both(-0x1p-6f), pair(s0, s1));
@@ -139,11 +148,11 @@ __device__ __forceinline__ Pair round_square_mean(Pair w, uint32_t r0, uint32_t 
     float w0, w1, s0, s1, n0, n1, l0, l1, c0, c1;
     apart(w, w0, w1);
     const Pair below = pair(__saturatef(fmaf(w0, -0x1p30f, 0x1p24f)), __saturatef(fmaf(w1, -0x1p30f, 0x1p24f)));
-    const Pair s = fma(below, both(0x1p-6f), w);
+    const Pair s = fma_cut(below, both(0x1p-6f), w);
     apart(s, s0, s1);
     const uint32_t b0 = __float_as_uint(s0), b1 = __float_as_uint(s1);
     const Pair kept = pair(__uint_as_float(b0 & 0xFFF00000u), __uint_as_float(b1 & 0xFFF00000u));
-    const Pair lo = fma(below, both(-0x1p-6f), kept), f = fma(kept, both(-1.f), s);                                  // w is lo + f
+    const Pair lo = fma(below, both(-0x1p-6f), kept), f = fma(lo, both(-1.f), w);                                    // w is lo + f, exactly
     apart(lo, n0, n1);
     const Pair d = mul(pair(__uint_as_float(b0 & 0x7F800000u), __uint_as_float(b1 & 0x7F800000u)), both(0.125f));
     // both sides are 2^-60 or more apart, or the same: 2^100 times the difference is 0 or at least 1.  From lo = 0 the random side is 0.
@@ -156,11 +165,26 @@ __device__ __forceinline__ Pair round_square_mean(Pair w, uint32_t r0, uint32_t 
 }
 // One instruction each, within 2 units of the last place: far below what a step is worth.  A second moment below 2^-126 counts as zero; eps is at least the
 // root of that, so that nothing is divided by zero.
-__device__ __forceinline__ float root_of(float v)
+__device__ __forceinline__ Pair about_root_of(Pair v)
 {
-    float r;
-    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
+    float v0, v1, r0, r1;
+    apart(v, v0, v1);
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(v0));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(v1));
+    return pair(r0, r1);
+}
+// With Newton's step, r + (v - r^2) / 2 r, for roots that become codes: one unit off, and of 103 M elements some twenty were rounded to the other neighbour.  The
+// quotient needs a digit only, so 1 / 2 r is read off r's exponent and fraction (within a tenth).  An infinite root's remainder is NaN and counts as anything finite.
+__device__ __forceinline__ Pair root_of(Pair v)
+{
+    const Pair r = about_root_of(v);
+    float r0, r1, e0, e1;
+    apart(r, r0, r1);
+    Pair e;
+    asm("fma.rn.ftz.f32x2 %0, %1, %2, %3;" : "=l"(e) : "l"(mul(r, both(-1.f))), "l"(r), "l"(v));
+    apart(e, e0, e1);
+    const Pair half = pair(__uint_as_float(0x7E740000u - __float_as_uint(r0)), __uint_as_float(0x7E740000u - __float_as_uint(r1)));
+    return fma(pair(fmaxf(e0, -0x1p127f), fmaxf(e1, -0x1p127f)), half, r);
 }
 __device__ __forceinline__ float reciprocal(float d)
 {
@@ -240,7 +264,7 @@ template <typename P, typename G, bool EIGHT, int N> __global__ void __launch_bo
     using M = std::conditional_t<EIGHT, uint8_t, float>;
     M *const em = static_cast<M*>(e.m) + begin, *const ev = static_cast<M*>(e.v) + begin;
     uint8_t* const scales = EIGHT ? e.scales + begin / 64 : nullptr;
-    const Pair beta1 = both(s.beta1), beta2 = both(s.beta2), rest1 = both(s.rest1), rest2 = both(s.rest2);
+    const Pair one = both(s.one), beta1 = both(s.beta1), beta2 = both(s.beta2), rest1 = both(s.rest1), rest2 = both(s.rest2);
     // whole passes of an aligned tensor are copied ahead
     const int ahead = EIGHT && aligned ? count / kPass : 0;
     extern __shared__ __align__(16) uint8_t own[];
@@ -315,13 +339,13 @@ template <typename P, typename G, bool EIGHT, int N> __global__ void __launch_bo
         float root[kPer];
 #pragma unroll
         for (int i = 0; i < kPer / 2; ++i) {
-            m[i] = fma(rest1, g[i], mul(beta1, m[i]));
-            v[i] = fma(mul(rest2, g[i]), g[i], mul(beta2, v[i]));
-            float v0, v1, d0, d1;
-            apart(v[i], v0, v1);
-            root[2 * i] = root_of(v0);
-            root[2 * i + 1] = root_of(v1);
-            apart(fma(pair(root[2 * i], root[2 * i + 1]), both(bias2), both(s.eps)), d0, d1);
+            // each product and sum rounded by itself, so that a formula without fused operations rounds its codes alike; the sums' factor of 1 keeps the compiler from fusing
+            m[i] = fma(mul(beta1, m[i]), one, mul(rest1, g[i]));
+            v[i] = fma(mul(beta2, v[i]), one, mul(mul(rest2, g[i]), g[i]));
+            float d0, d1;
+            const Pair r = EIGHT ? root_of(v[i]) : about_root_of(v[i]);
+            apart(r, root[2 * i], root[2 * i + 1]);
+            apart(fma(r, both(bias2), both(s.eps)), d0, d1);
             const Pair q = mul(m[i], pair(reciprocal(d0), reciprocal(d1)));
             apart(fma(both(-rate), q, mul(pair(w[2 * i], w[2 * i + 1]), both(keep))), w[2 * i], w[2 * i + 1]);
         }
@@ -507,6 +531,7 @@ mor_status_t mor_adamw(const mor_adamw_desc_t* d, const mor_adamw_tensor_t* t, i
     if (all == 0) return MOR_OK;
     AdamwScalars s = {};
     s.lr = (float)d->lr;
+    s.one = 1.f;
     s.beta1 = (float)d->beta1;
     s.beta2 = (float)d->beta2;
     s.rest1 = (float)(1.0 - d->beta1);
