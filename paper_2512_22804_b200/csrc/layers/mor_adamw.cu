@@ -155,8 +155,10 @@ __device__ __forceinline__ Pair round_square_mean(Pair w, uint32_t r0, uint32_t 
     const Pair lo = fma(below, both(-0x1p-6f), kept), f = fma(lo, both(-1.f), w);                                    // w is lo + f, exactly
     apart(lo, n0, n1);
     const Pair d = mul(pair(__uint_as_float(b0 & 0x7F800000u), __uint_as_float(b1 & 0x7F800000u)), both(0.125f));
-    // both sides are 2^-60 or more apart, or the same: 2^100 times the difference is 0 or at least 1.  From lo = 0 the random side is 0.
-    const Pair a = mul(mul(d, pair(__saturatef(n0 * 0x1p10f), __saturatef(n1 * 0x1p10f))), fma(both(2.f), lo, d)), c = mul(f, fma(both(2.f), lo, f));
+    // From lo > 0 both sides are 2^-60 or more apart, or the same: 2^100 times the difference is 0 or at least 1.  From lo = 0 the random side is 0 and the other
+    // one w (w + 2^20) instead of w^2: a root is 2^-63 at least (or 0) and a scale that of a maximum below 2^64, so w is 2^-120 at least and 2^100 times this at least 1.
+    const Pair some = pair(__saturatef(n0 * 0x1p10f), __saturatef(n1 * 0x1p10f));                                     // 0 from lo = 0, else 1
+    const Pair a = mul(mul(d, some), fma(both(2.f), lo, d)), c = mul(f, fma(both(2.f), lo, add(f, fma(some, both(-0x1p20f), both(0x1p20f)))));
     const Pair u = add(pair(__uint_as_float(r0 * 128u + 0x3F800000u), __uint_as_float(r1 * 128u + 0x3F800000u)), both(-1.f));
     apart(mul(mul(u, both(-0x1p100f)), a), l0, l1);
     apart(c, c0, c1);

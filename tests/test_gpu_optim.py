@@ -265,6 +265,27 @@ def test_a_root_above_zero_stays_above_zero_and_zeros_stay(optim):
     assert (v.float()[:128] > 0).all() and (v.float()[128:] == 0).all() and p.isfinite().all()
 
 
+def test_the_smallest_roots_beside_the_largest(optim):
+    """Roots from 2^62 down to 2^-62 in blocks of one largest each (without memory of the step before a root is the gradient's magnitude, exactly): a root above zero is at
+    least the smallest code however far below its block's largest it lies, up to a ratio of 2^-124."""
+    import torch
+
+    k = torch.arange(-62, 63, device="cuda")
+    for top in (62, 30, 0, -30):
+        g = torch.zeros(256, device="cuda")
+        low = k[k <= top]
+        g[:low.numel()] = torch.exp2(low.float()) * torch.where(low % 2 == 0, 1.0, -1.0)
+        g[128:][:low.numel()] = torch.exp2(low.float()) * 1.375
+        p, (m, v) = torch.zeros(256, device="cuda"), (torch.zeros(256, device="cuda").to(torch.float8_e4m3fn) for _ in range(2))
+        s = torch.full((2, 2), 127, dtype=torch.uint8, device="cuda")
+        optim.adamw_([p], [g], [m], [v], [s], step=1, beta2=0.0)
+        roots = v.float().view(2, 128)
+        w = g.abs().view(2, 128) * torch.exp2(s[:, 1:].float() - 127)
+        assert (roots[:, low.numel():] == 0).all() and (roots[:, :low.numel()] >= 2.0 ** -9).all()
+        assert (roots[w < 2.0 ** -9] <= 2.0 ** -9).all() and p.isfinite().all()
+        check_codes(v, s, 1, g.double().abs(), words(256, 0, 1, 0)[0])
+
+
 def test_extremes(optim):
     import torch
 
