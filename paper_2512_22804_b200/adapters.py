@@ -16,7 +16,7 @@
 Few tokens without gradients (up to 224, fewer with ranks above 32 or wide results) are one launch; more are sorted by adapter first.  x, base and the gradient
 may have any strides (rows that overlap or are not contiguous are copied first); rows of results start on multiples of 16 bytes.
 
-Gradients: of x, a and b (and base), once (the backward pass cannot be differentiated again).  ids and scale have none.  The gradient of an FP32 result is
+Gradients: of x, a and b (and base), once (the backward pass cannot be differentiated again).  ids and scale have none.  Forward-mode derivatives are refused.  The gradient of an FP32 result is
 rounded to BF16 for the adapters' products.
 
 The formulas are those of ``include/mor.h``.

@@ -150,6 +150,7 @@ struct NormFn : torch::autograd::Function<NormFn> {
 
 variable_list rms_norm(const Tensor& x, const Tensor& weight, const std::optional<Tensor>& residual, double eps)
 {
+    no_tangent({x, weight, residual ? *residual : x}, "norm.rms_norm");
     if (needs_grad(x) || needs_grad(weight) || (residual && needs_grad(*residual))) return NormFn::apply(x, weight, residual, eps);
     const std::pair<Tensor, Tensor> r = norm_rows(norm_args(x, weight, residual, eps), x);
     return residual ? variable_list{r.first, r.second} : variable_list{r.first};
@@ -320,6 +321,7 @@ struct AdapterFn : torch::autograd::Function<AdapterFn> {
 
 Tensor adapter_add(const Tensor& base, const Tensor& x, const Tensor& a, const Tensor& b, const std::optional<Tensor>& ids, const std::optional<Tensor>& scale, double factor)
 {
+    no_tangent({base, x, a, b, scale ? *scale : x}, "adapters.add");
     const bool train = needs_grad(x) || needs_grad(a) || needs_grad(b);
     if (train || needs_grad(base)) return AdapterFn::apply(base, x, a, b, ids, scale, factor, train);
     check_base(base, x);
@@ -371,6 +373,7 @@ struct AdapterLinearFn : torch::autograd::Function<AdapterLinearFn> {
 Tensor adapter_linear(const Tensor& x, const Matrix& w, const Tensor& a, const Tensor& b, const std::optional<Tensor>& ids, const std::optional<Tensor>& scale, double factor,
                       const Matrix* w_t)
 {
+    no_tangent({x, a, b, scale ? *scale : x}, "adapters.linear");
     want(w.c.batch == 1 && x.dim() >= 1 && x.size(-1) == w.c.cols, "x [..., n_in] and an operand [n_out, n_in] are wanted");
     if (w_t != nullptr)
         want(w_t->c.batch == 1 && w_t->c.rows == w.c.cols && w_t->c.cols == w.c.rows && w_t->c.format == w.c.format, "w_t: the operand of w's transpose, in its format, is wanted");
@@ -434,6 +437,7 @@ void adamw(const AdamwLists& l, mor_adamw_desc_t& d)
         if (m.scalar_type() != state || v.scalar_type() != state) throw py::type_error("moments: all FP32 or all float8_e4m3fn are wanted");
         there(p, "params");
         there(g, "grads");
+        no_tangent({p, g}, "optim.adamw_");
         there(m, "exp_avgs");
         there(v, "exp_avg_sqs");
         const int64_t numel = p.numel();

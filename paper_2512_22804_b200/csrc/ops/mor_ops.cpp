@@ -12,6 +12,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <functional>
 #include <memory>
 #include <mutex>
 #include <optional>
@@ -368,7 +369,14 @@ void add_edge(torch::autograd::edge_list& edges, const Tensor& t)
 {
     if (t.defined() && t.requires_grad()) edges.push_back(torch::autograd::impl::gradient_edge(t));
 }
-// The same for results of a backward pass that keeps a graph (create_graph): they depend on the layer's inputs and on the gradient.
+// Nothing here has a forward-mode derivative (torch refuses those of the autograd functions by itself): a result without a tangent would read as a derivative of
+// zero.
+void no_tangent(std::initializer_list<std::reference_wrapper<const Tensor>> inputs, const char* call)
+{
+    for (const Tensor& t : inputs)
+        TORCH_CHECK(!t.defined() || !t._fw_grad(0).defined(), call, " has no forward-mode derivative");
+}
+// The same as no_derivative() for results of a backward pass that keeps a graph (create_graph): they depend on the layer's inputs and on the gradient.
 void once_differentiable(std::initializer_list<Tensor*> results, const Tensor& grad, const char* layer)
 {
     if (!at::GradMode::is_enabled()) return;
@@ -607,6 +615,7 @@ private:
 // A result of a call that has no gradient of its own.
 PyObject* give(Tensor out, std::initializer_list<Tensor> inputs, const char* call)
 {
+    for (const Tensor& t : inputs) no_tangent({t}, call);
     if (at::GradMode::is_enabled()) {
         torch::autograd::edge_list edges;
         for (const Tensor& t : inputs) add_edge(edges, t);

@@ -22,7 +22,7 @@
     first); ids and weight are contiguous.
 
 Gradients: linear has its own, of x, w and weight, once (its backward pass cannot be differentiated again).  gather, combine, combine_grad and linear
-with a stored stack have none: what they make of tensors that require a gradient raises when it is differentiated.  In a
+with a stored stack have none: what they make of tensors that require a gradient raises when it is differentiated.  Forward-mode derivatives are refused.  In a
 torch.autograd.Function of a caller's own, the gradient of gather(x, plan) is combine(dxs, plan) and that of combine is combine_grad.
 
 The formulas are those of ``include/mor.h``.

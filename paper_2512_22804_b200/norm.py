@@ -18,7 +18,7 @@ Results have rows that start on multiples of 16 bytes, so one of another width h
 overlap or are not contiguous are copied first).  A row of zeros is zero; with eps = 0 it is NaN.
 
 Gradients: rms_norm has its own, of x, weight and residual, once (its backward pass cannot be differentiated again).  The others have none: what they make
-of tensors that require one raises when it is differentiated.
+of tensors that require one raises when it is differentiated.  Forward-mode derivatives are refused.
 
 The formulas are those of ``include/mor.h``.
 """

@@ -401,6 +401,24 @@ def test_autograd(adapters):
     assert len(seen) >= 5
 
 
+def test_forward_mode_is_refused(adapters):
+    import torch
+    import torch.autograd.forward_ad as forward
+
+    from paper_2512_22804_b200 import fp4
+
+    x, y0, a, b, ids, scale = draw(20, 64, 72, 8, 2)
+    w, w_t = fp4.quantize(torch.zeros(72, 64, device="cuda", dtype=torch.bfloat16), "e8m0_32", cols=True)
+    with forward.dual_level():
+        for i in (0, 1, 2, 3, 5):
+            args = [forward.make_dual(t, torch.ones_like(t)) if k == i else t for k, t in enumerate((y0, x, a, b, ids, scale))]
+            with pytest.raises(RuntimeError, match="forward-mode"):
+                adapters.add(*args)
+            if i > 0:
+                with pytest.raises(RuntimeError, match="forward-mode"):
+                    adapters.linear(args[1], w, *args[2:], w_t=w_t)
+
+
 def test_refusals(adapters):
     import torch
 

@@ -362,3 +362,23 @@ def test_refusals(norm):
             bad()
     with pytest.raises(KeyError):
         norm.rms_norm_quantize(x, w, scale="e5m2")
+
+
+def test_forward_mode_is_refused(norm):
+    """A dual tensor may not lose its tangent in silence, whether something else needs a gradient or not."""
+    import torch
+    import torch.autograd.forward_ad as forward
+
+    from paper_2512_22804_b200 import experts
+
+    x, r, w = draw(6, 64, "bf16", "fp32", "bf16")
+    codes, scales = norm.rms_norm_quantize(x, w, scale="fp32")
+    plan = experts.sort(torch.zeros(6, 1, dtype=torch.int32, device="cuda"), 1)
+    with forward.dual_level():
+        dual = lambda t: forward.make_dual(t, torch.ones_like(t))  # noqa: E731
+        for call in (lambda: norm.rms_norm(dual(x), w), lambda: norm.rms_norm(x, dual(w)), lambda: norm.rms_norm(x, w, dual(r)), lambda: norm.rms_norm(dual(x), w.clone().requires_grad_()),
+                     lambda: norm.rms_norm_quantize(dual(x), w), lambda: norm.rms_norm_quantize(x, w, dual(r)), lambda: norm.dequantize(codes, dual(scales)),
+                     lambda: experts.gather(dual(x), plan), lambda: experts.combine(dual(x), plan)):
+            with pytest.raises(RuntimeError, match="forward-mode"):
+                call()
+        assert (norm.rms_norm(x, w, r)[0] == norm.rms_norm(dual(x).detach(), w, r)[0]).all()

@@ -467,6 +467,18 @@ def test_autograd_sees_the_change(optim):
         y.backward()
 
 
+def test_forward_mode_is_refused(optim):
+    import torch
+    import torch.autograd.forward_ad as forward
+
+    z = lambda: torch.zeros(64, device="cuda")  # noqa: E731
+    with forward.dual_level():
+        for i in range(2):
+            args = [[forward.make_dual(t, torch.ones_like(t)) if k == i else t] for k, t in enumerate((z(), z(), z(), z()))]
+            with pytest.raises(RuntimeError, match="forward-mode"):
+                optim.adamw_(*args, step=1)
+
+
 def test_refusals(optim):
     import torch
 
