@@ -89,6 +89,7 @@ struct NormFn : torch::autograd::Function<NormFn> {
     {
         const NormArgs n = norm_args(x, weight, residual, eps);
         const std::pair<Tensor, Tensor> r = norm_rows(n, x);
+        ctx->set_materialize_grads(false);               // of y and h one may go unused
         ctx->saved_data["eps"] = eps;
         ctx->saved_data["types"] = std::vector<int64_t>{(int64_t)x.scalar_type(), residual ? (int64_t)residual->scalar_type() : -1};
         if (!residual) {
@@ -103,6 +104,7 @@ struct NormFn : torch::autograd::Function<NormFn> {
         const variable_list kept = ctx->get_saved_variables();
         const std::vector<int64_t> types = ctx->saved_data["types"].toIntVector();
         const bool has = types[1] >= 0;
+        if (!grads[0].defined() && !(has && grads[1].defined())) return variable_list(4);
         const at::ScalarType type = (at::ScalarType)types[0], other = has ? (at::ScalarType)types[1] : type;
         const bool need_x = ctx->needs_input_grad(0), need_w = ctx->needs_input_grad(1), need_r = has && ctx->needs_input_grad(2);
         const Tensor h = as_rows(kept[0]), weight = kept[1].contiguous();

@@ -364,6 +364,36 @@ def test_refusals(norm):
         norm.rms_norm_quantize(x, w, scale="e5m2")
 
 
+@pytest.mark.parametrize("residual", ["bf16", "fp32"])
+def test_an_unused_result_costs_nothing(norm, residual):
+    """Gradients of y alone and of h alone are those with zeros for the other, and y alone fills and reads no such zeros: what the pass takes beyond its results is the
+    workspace of the weight's gradient."""
+    import torch
+
+    x, r, w = draw(1000, 4096, "bf16", residual, "bf16")
+    dy, dh = torch.randn(1000, 4096, device="cuda").to(T("bf16")), torch.randn(1000, 4096, device="cuda").to(T(residual))
+
+    def grads(used, given):
+        leaves = [t.detach().requires_grad_() for t in (x, w, r)]
+        results = norm.rms_norm(*leaves)
+        out = [results[i] for i in used]
+        del results
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_allocated()
+        torch.cuda.reset_peak_memory_stats()
+        g = torch.autograd.grad(out, leaves, given)
+        return g, torch.cuda.max_memory_allocated() - before
+
+    both, _ = grads((0, 1), (dy, torch.zeros_like(dh)))
+    alone, most = grads((0,), (dy,))
+    assert all((a == b).all() for a, b in zip(both, alone))
+    made = sum(1000 * 4096 * t.element_size() for t in ((x,) if residual == "bf16" else (x, r)))
+    assert most <= made + 148 * 4096 * 4 + 2 ** 20
+    both, _ = grads((0, 1), (torch.zeros_like(dy), dh))
+    alone, _ = grads((1,), (dh,))
+    assert all((a == b).all() for a, b in zip(both, alone)) and (alone[1] == 0).all()
+
+
 def test_forward_mode_is_refused(norm):
     """A dual tensor may not lose its tangent in silence, whether something else needs a gradient or not."""
     import torch
