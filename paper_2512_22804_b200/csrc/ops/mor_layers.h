@@ -143,9 +143,9 @@ struct NormFn : torch::autograd::Function<NormFn> {
         if (need_r && !dr.defined()) dr = dx;
         if (!need_x) dx = Tensor();
         const bool shared = dx.defined() && dr.is_same(dx);
-        once_differentiable({&dx, &dw}, grads[0], "norm.rms_norm");
+        once_differentiable({&dx, &dw}, grads, "norm.rms_norm");
         if (shared) dr = dx;
-        else once_differentiable({&dr}, grads[0], "norm.rms_norm");
+        else once_differentiable({&dr}, grads, "norm.rms_norm");
         return {dx, dw, dr, Tensor()};
     }
 };

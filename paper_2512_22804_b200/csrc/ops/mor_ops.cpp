@@ -376,14 +376,14 @@ void no_tangent(std::initializer_list<std::reference_wrapper<const Tensor>> inpu
     for (const Tensor& t : inputs)
         TORCH_CHECK(!t.defined() || !t._fw_grad(0).defined(), call, " has no forward-mode derivative");
 }
-// The same as no_derivative() for results of a backward pass that keeps a graph (create_graph): they depend on the layer's inputs and on the gradient.
-void once_differentiable(std::initializer_list<Tensor*> results, const Tensor& grad, const char* layer)
+// The same as no_derivative() for results of a backward pass that keeps a graph (create_graph): they depend on the layer's inputs and on the gradients.
+void once_differentiable(std::initializer_list<Tensor*> results, at::ArrayRef<Tensor> grads, const char* layer)
 {
     if (!at::GradMode::is_enabled()) return;
     torch::autograd::edge_list edges;
     for (const torch::autograd::Edge& e : torch::autograd::get_current_node()->next_edges())
         if (e.is_valid()) edges.push_back(e);
-    add_edge(edges, grad);
+    for (const Tensor& t : grads) add_edge(edges, t);
     for (Tensor* t : results) no_derivative(*t, edges, std::string(layer) + " cannot be differentiated twice");
 }
 

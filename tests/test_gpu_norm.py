@@ -394,6 +394,20 @@ def test_an_unused_result_costs_nothing(norm, residual):
     assert all((a == b).all() for a, b in zip(both, alone)) and (alone[1] == 0).all()
 
 
+@pytest.mark.parametrize("residual", ["bf16", "fp32"])
+def test_no_second_derivative_by_either_gradient(norm, residual):
+    import torch
+
+    x, r, w = draw(6, 64, "bf16", residual, "bf16")
+    for i in range(2):
+        given = [torch.ones(6, 64, device="cuda", dtype=T(t)) for t in ("bf16", residual)]
+        given[i].requires_grad_()
+        leaves = [t.detach().requires_grad_() for t in (x, w, r)]
+        for g in torch.autograd.grad(norm.rms_norm(*leaves), leaves, given, create_graph=True):
+            with pytest.raises(RuntimeError, match="differentiated twice"):
+                torch.autograd.grad(g.sum(), given[i], allow_unused=True, retain_graph=True)
+
+
 def test_forward_mode_is_refused(norm):
     """A dual tensor may not lose its tangent in silence, whether something else needs a gradient or not."""
     import torch
