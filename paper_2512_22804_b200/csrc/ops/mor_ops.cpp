@@ -354,6 +354,7 @@ std::pair<std::optional<Tensor>, Tensor> combine_grad(const Tensor& dy, const Te
 Tensor apart(const Tensor& t)
 {
     const bool ok = (t.size(-1) <= 1 || t.stride(-1) == 1) && (t.size(-2) <= 1 || t.stride(-2) >= t.size(-1));
+    if (!ok && t.numel() == 0) return at::empty(t.sizes(), t.options());          // contiguous() returns it as it is, whatever its strides
     return ok ? t : t.contiguous();
 }
 

@@ -208,6 +208,26 @@ def test_more_dimensions_and_none(adapters):
     y.sum().backward()
 
 
+def test_no_tokens_through_a_layer(adapters):
+    """The gradient of a sum has strides of zero, that of nothing too."""
+    import torch
+
+    from paper_2512_22804_b200 import fp4
+
+    x, y0, a, b, ids, scale = draw(5, 64, 72, 8, 2)
+    w, w_t = fp4.quantize(torch.randn(72, 64, device="cuda").to(torch.bfloat16), "e8m0_32", cols=True)
+    for layer in (lambda x, a, b: adapters.linear(x, w, a, b, ids[:0], scale, w_t=w_t), lambda x, a, b: adapters.add(y0[:0], x, a, b, ids[:0], scale)):
+        leaves = [t.detach().requires_grad_() for t in (x[:0], a, b)]
+        y = layer(*leaves)
+        assert y.shape == (0, 72)
+        g = torch.autograd.grad(y.sum(), leaves)
+        assert g[0].shape == (0, 64) and (g[1] == 0).all() and (g[2] == 0).all()
+    leaves = [x[:0].detach().requires_grad_(), b[0, :, :1].expand(72, 64).contiguous().requires_grad_()]
+    g = torch.autograd.grad(fp4.linear(*leaves, "e8m0_32").sum(), leaves)
+    assert g[0].shape == (0, 64) and (g[1] == 0).all()
+    fp4.check()
+
+
 def test_what_is_not_finite_stays_in_its_row(adapters):
     import torch
 
