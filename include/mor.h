@@ -436,7 +436,7 @@ typedef struct mor_norm_outputs {
     uint8_t* scale_e8m0;     /* [rows, blocks] with codes: this one or                         */
     float*   scale_f32;      /* this one                                                       */
     int64_t  ldh, ldy, ldc;
-    int32_t  block;          /* columns of a scale: 128, or 0 for a whole row                  */
+    int32_t  block;          /* columns of a scale: 128, or 0 for a whole row (1 where it has no columns)  */
 } mor_norm_outputs_t;
 MOR_API mor_status_t mor_rms_norm(const mor_norm_desc_t* host_desc, const mor_norm_outputs_t* host_out, void* cuda_stream);
 

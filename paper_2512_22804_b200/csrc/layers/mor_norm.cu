@@ -259,6 +259,14 @@ template <typename T, typename R, int G, int N, bool ANY> __global__ void __laun
     }
 }
 
+// Scales of rows without columns, that of a largest magnitude of 0.
+__global__ void __launch_bounds__(256) norm_no_columns_kernel(const __grid_constant__ NormParams p)
+{
+    wait_for_predecessor();
+    const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (row < p.rows) make_scale(p, 0.f, row, true);
+}
+
 // Rows of any width, one a CTA.
 template <typename T, typename R> __global__ void __launch_bounds__(kWideThreads) norm_wide_kernel(const __grid_constant__ NormParams p)
 {
@@ -700,9 +708,16 @@ mor_status_t mor_rms_norm(const mor_norm_desc_t* d, const mor_norm_outputs_t* o,
     if (o->y != nullptr && (s = check_matrix_arg(o->y, d->rows, d->cols, o->ldy, es, any)) != MOR_OK) return s;
     if (o->codes != nullptr && (s = check_matrix_arg(o->codes, d->rows, d->cols, o->ldc, 1, any)) != MOR_OK) return s;
     if (!is_aligned(o->scale_f32, 4)) return MOR_ERR_ALIGNMENT;
-    if (empty) return MOR_OK;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     NormParams p = {};
     p.rows = d->rows;
+    if (empty) {                                            // a scale for a row is there without columns too
+        if (d->rows == 0 || o->block != 0 || (o->scale_e8m0 == nullptr) == (o->scale_f32 == nullptr)) return MOR_OK;
+        p.e8m0 = o->scale_e8m0;
+        p.f32 = o->scale_f32;
+        const uint32_t grid = (uint32_t)ceil_div(d->rows, 256);
+        return launch(norm_no_columns_kernel, grid, 256, 0, st, grid <= kEarlyGrid, p) == cudaSuccess ? MOR_OK : MOR_ERR_CUDA;
+    }
     p.cols = (int32_t)d->cols;
     p.weight_dtype = d->weight_dtype;
     p.x = d->x;
@@ -721,7 +736,6 @@ mor_status_t mor_rms_norm(const mor_norm_desc_t* d, const mor_norm_outputs_t* o,
     p.ldy = o->ldy;
     p.ldc = o->ldc;
     p.by_row = o->block == 0;
-    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     return by_types(d->dtype, rt, [&](auto t, auto r) { return norm_width<decltype(t), decltype(r)>(p, any, st); });
 }
 

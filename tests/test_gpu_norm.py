@@ -364,6 +364,23 @@ def test_refusals(norm):
         norm.rms_norm_quantize(x, w, scale="e5m2")
 
 
+@pytest.mark.parametrize("scale", ["e8m0", "fp32"])
+def test_rows_without_columns_have_a_scale(norm, scale):
+    """The largest magnitude of nothing is 0, whose scale is 1; the scales' memory held something else before."""
+    import torch
+
+    kind = torch.uint8 if scale == "e8m0" else torch.float32
+    x = torch.zeros(700, 0, device="cuda", dtype=torch.bfloat16)
+    for _ in range(3):
+        junk = torch.full((700,), 7, device="cuda", dtype=kind)
+        del junk
+        codes, scales = norm.rms_norm_quantize(x, x[0], scale=scale, block=None)
+        assert codes.shape == (700, 0) and scales.shape == (700, 1) and (scales == (127 if scale == "e8m0" else 1)).all()
+        assert norm.dequantize(codes, scales).shape == (700, 0)
+    assert norm.rms_norm_quantize(x, x[0], scale=scale)[1].shape == (700, 0)
+    assert norm.rms_norm_quantize(x[:0], x[0], scale=scale, block=None)[1].shape == (0, 1)
+
+
 @pytest.mark.parametrize("residual", ["bf16", "fp32"])
 def test_an_unused_result_costs_nothing(norm, residual):
     """Gradients of y alone and of h alone are those with zeros for the other, and y alone fills and reads no such zeros: what the pass takes beyond its results is the
