@@ -496,7 +496,7 @@ MOR_API mor_status_t mor_adapter_grad(const mor_adapter_desc_t* host_desc, const
  * (its mean is kept), w where u (2 n + 1) < (t - n)(t + n) (the mean of its square is kept), and a w above zero is at least the smallest code, since
  * it is divided by.  What is not finite becomes NaN.  BF16 parameters are rounded by 16 random bits added below the kept ones.
  * Random numbers are hashes, in 32 bits: mix(z): z ^= z >> 16; z *= 0x7FEB352D; z ^= z >> 15; z *= 0x846CA68B; z ^= z >> 16.  With key =
- * mix(mix(seed + 0x9E3779B9 * step) + tensor's number in the call) and z = mix(mix(high half of the element's number ^ key) + low half), the low 16 bits
+ * mix(mix(seed + 0x9E3779B9 * step) + tensor's number) and z = mix(mix(high half of the element's number ^ key) + low half), the low 16 bits
  * of z / 65536 are u of m, the high ones u of w, the low ones of mix(z ^ 0x9E3779B9) the parameter's. */
 typedef struct mor_adamw_tensor {
     void*       param;       /* DEVICE, contiguous, aligned to its element; full speed on 32 bytes  */
@@ -516,6 +516,8 @@ typedef struct mor_adamw_desc {
     uint64_t seed;           /* its low 32 bits count                                          */
     int32_t param_dtype, grad_dtype;   /* mor_dtype_t                                          */
     int32_t eight_bits;      /* moments as codes                                               */
+    const uint32_t* numbers; /* HOST [n], optional: the tensors' numbers, below 2^31, instead of their places 0 .. n - 1 in the call: tensors of several calls
+                              * of a step are rounded by random numbers of their own if they have numbers of their own */
 } mor_adamw_desc_t;
 MOR_API mor_status_t mor_adamw(const mor_adamw_desc_t* host_desc, const mor_adamw_tensor_t* host_tensors, int n, void* cuda_stream);
 /* Values of 8-bit moments: m = code / s into exp_avg_out, v = (code / s)^2 into exp_avg_sq_out ([numel] in `dtype`, each optional). */

@@ -28,7 +28,7 @@ struct AdamwEntry {
     uint8_t* scales;
     int64_t numel;
     uint32_t first;            // first CTA
-    uint32_t aligned;          // whole pieces may be read and written
+    uint32_t number_aligned;   // twice the tensor's number, and whether whole pieces may be read and written
 };
 
 struct AdamwScalars {
@@ -36,7 +36,7 @@ struct AdamwScalars {
     float one;                                             // 1
     float bias1, bias2;                                    // 1 / (1 - beta1^step), 1 / sqrt(1 - beta2^step)
     float log1, log2;                                      // log beta
-    uint32_t seed, step, number, count;                    // number: of the first tensor in the call; count: tensors of this launch
+    uint32_t seed, step, count;                            // count: tensors of this launch
     int32_t chunk;                                         // elements of a CTA
     const int32_t* device_step;
     const float *device_lr, *grad_scale, *found_inf;
@@ -256,11 +256,11 @@ template <typename P, typename G, bool EIGHT, int N> __global__ void __launch_bo
     }
     const float scale = s.grad_scale != nullptr ? *s.grad_scale : 1.f;
     const float keep = fmaf(-lr, s.decay, 1.f), rate = lr * bias1;
-    const uint32_t key = mix(mix(s.seed + 0x9E3779B9u * step) + s.number + lo);
+    const uint32_t key = mix(mix(s.seed + 0x9E3779B9u * step) + (e.number_aligned >> 1));
     // from here on everything is counted from the CTA's first element
     const int64_t begin = (int64_t)(blockIdx.x - e.first) * s.chunk;
     const int count = (int)min((int64_t)s.chunk, e.numel - begin);
-    const bool aligned = e.aligned != 0;
+    const bool aligned = (e.number_aligned & 1u) != 0;
     P* const param = static_cast<P*>(e.param) + begin;
     const G* const grad = static_cast<const G*>(e.grad) + begin;
     using M = std::conditional_t<EIGHT, uint8_t, float>;
@@ -461,7 +461,7 @@ template <typename T> __global__ void __launch_bounds__(kThreads) moments_kernel
 }
 
 template <typename P, typename G, bool EIGHT, int N>
-mor_status_t adamw_launch(const AdamwScalars& s, const mor_adamw_tensor_t* t, int n, cudaStream_t st)
+mor_status_t adamw_launch(const AdamwScalars& s, const mor_adamw_tensor_t* t, const uint32_t* numbers, int n, cudaStream_t st)
 {
     static std::atomic<uint64_t> done{0};
     constexpr int kSmem = EIGHT ? OwnRing<P, G>::kBytes : 0;
@@ -477,29 +477,29 @@ mor_status_t adamw_launch(const AdamwScalars& s, const mor_adamw_tensor_t* t, in
         int64_t per = passes / (148 * 4);
         per = per < 1 ? 1 : per > kMostPasses ? kMostPasses : per;
         p.s.chunk = (int32_t)per * kPass;
-        p.s.number = s.number + (uint32_t)at;
         p.s.count = (uint32_t)k;
         int64_t ctas = 0;
         for (int i = 0; i < k; ++i) {
             const mor_adamw_tensor_t& x = t[at + i];
             const size_t state = EIGHT ? 8 : 32;
-            p.e[i] = {x.param, x.grad, x.exp_avg, x.exp_avg_sq, x.scales, x.numel, (uint32_t)ctas,
-                      (uint32_t)(is_aligned(x.param, kPer * sizeof(P)) && is_aligned(x.grad, kPer * sizeof(G)) && is_aligned(x.exp_avg, state) && is_aligned(x.exp_avg_sq, state))};
+            const bool aligned = is_aligned(x.param, kPer * sizeof(P)) && is_aligned(x.grad, kPer * sizeof(G)) && is_aligned(x.exp_avg, state) && is_aligned(x.exp_avg_sq, state);
+            const uint32_t number = numbers != nullptr ? numbers[at + i] : (uint32_t)(at + i);
+            p.e[i] = {x.param, x.grad, x.exp_avg, x.exp_avg_sq, x.scales, x.numel, (uint32_t)ctas, number * 2 + (aligned ? 1u : 0u)};
             ctas += ceil_div(x.numel, p.s.chunk);
         }
         if (launch(adamw_kernel<P, G, EIGHT, N>, (uint32_t)ctas, kThreads, kSmem, st, ctas <= kEarlyGrid, p) != cudaSuccess) return MOR_ERR_CUDA;
     }
     return MOR_OK;
 }
-template <typename P, typename G, bool EIGHT> mor_status_t adamw_table(const AdamwScalars& s, const mor_adamw_tensor_t* t, int n, cudaStream_t st)
+template <typename P, typename G, bool EIGHT> mor_status_t adamw_table(const AdamwScalars& s, const mor_adamw_tensor_t* t, const uint32_t* numbers, int n, cudaStream_t st)
 {
-    if (n <= 16) return adamw_launch<P, G, EIGHT, 16>(s, t, n, st);
-    if (n <= 128) return adamw_launch<P, G, EIGHT, 128>(s, t, n, st);
-    return adamw_launch<P, G, EIGHT, 512>(s, t, n, st);
+    if (n <= 16) return adamw_launch<P, G, EIGHT, 16>(s, t, numbers, n, st);
+    if (n <= 128) return adamw_launch<P, G, EIGHT, 128>(s, t, numbers, n, st);
+    return adamw_launch<P, G, EIGHT, 512>(s, t, numbers, n, st);
 }
-template <typename P, typename G> mor_status_t adamw_state(bool eight, const AdamwScalars& s, const mor_adamw_tensor_t* t, int n, cudaStream_t st)
+template <typename P, typename G> mor_status_t adamw_state(const mor_adamw_desc_t& d, const AdamwScalars& s, const mor_adamw_tensor_t* t, int n, cudaStream_t st)
 {
-    return eight ? adamw_table<P, G, true>(s, t, n, st) : adamw_table<P, G, false>(s, t, n, st);
+    return d.eight_bits ? adamw_table<P, G, true>(s, t, d.numbers, n, st) : adamw_table<P, G, false>(s, t, d.numbers, n, st);
 }
 
 bool in_unit(double v) { return v >= 0.0 && v < 1.0; }
@@ -523,6 +523,7 @@ mor_status_t mor_adamw(const mor_adamw_desc_t* d, const mor_adamw_tensor_t* t, i
     int64_t all = 0;
     for (int i = 0; i < n; ++i) {
         const mor_adamw_tensor_t& x = t[i];
+        if (d->numbers != nullptr && d->numbers[i] >= 1u << 31) return MOR_ERR_INVALID_ARG;
         if (x.numel < 0 || x.numel >= (1ll << 40) || (all += x.numel) >= (1ll << 42)) return MOR_ERR_INVALID_ARG;     // what a grid holds
         if (x.numel == 0) continue;
         if (x.param == nullptr || x.grad == nullptr || x.exp_avg == nullptr || x.exp_avg_sq == nullptr || (d->eight_bits && x.scales == nullptr)) return MOR_ERR_INVALID_ARG;
@@ -551,10 +552,10 @@ mor_status_t mor_adamw(const mor_adamw_desc_t* d, const mor_adamw_tensor_t* t, i
     s.grad_scale = d->grad_scale;
     s.found_inf = d->found_inf;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    const bool eight = d->eight_bits != 0, g16 = d->grad_dtype == MOR_DTYPE_BF16;
+    const bool g16 = d->grad_dtype == MOR_DTYPE_BF16;
     if (d->param_dtype == MOR_DTYPE_BF16)
-        return g16 ? adamw_state<__nv_bfloat16, __nv_bfloat16>(eight, s, t, n, st) : adamw_state<__nv_bfloat16, float>(eight, s, t, n, st);
-    return g16 ? adamw_state<float, __nv_bfloat16>(eight, s, t, n, st) : adamw_state<float, float>(eight, s, t, n, st);
+        return g16 ? adamw_state<__nv_bfloat16, __nv_bfloat16>(*d, s, t, n, st) : adamw_state<__nv_bfloat16, float>(*d, s, t, n, st);
+    return g16 ? adamw_state<float, __nv_bfloat16>(*d, s, t, n, st) : adamw_state<float, float>(*d, s, t, n, st);
 }
 
 mor_status_t mor_adamw_moments(const uint8_t* exp_avg, const uint8_t* exp_avg_sq, const uint8_t* scales, int64_t numel, void* exp_avg_out, void* exp_avg_sq_out,

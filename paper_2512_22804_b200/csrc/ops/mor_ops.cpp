@@ -588,6 +588,23 @@ public:
             if (!THPVariable_Check(r.items[k])) wrong(i, "a list of tensors");
         return r;
     }
+    std::vector<uint32_t> numbers(size_t i) const
+    {
+        std::vector<uint32_t> r;
+        if (v_[i] == nullptr) return r;
+        if (!PyList_Check(v_[i]) && !PyTuple_Check(v_[i])) wrong(i, "a list of whole numbers");
+        const size_t n = (size_t)PySequence_Fast_GET_SIZE(v_[i]);
+        r.reserve(n);
+        for (size_t k = 0; k < n; ++k) {
+            PyObject* const item = PySequence_Fast_GET_ITEM(v_[i], (Py_ssize_t)k);
+            if (!PyLong_Check(item)) wrong(i, "a list of whole numbers");
+            int too_large;
+            const long long v = PyLong_AsLongLongAndOverflow(item, &too_large);
+            if (too_large || v < 0 || v >= 1ll << 31) throw py::value_error(std::string(names_[i]) + ": from 0 to below 2^31 is wanted");
+            r.push_back((uint32_t)v);
+        }
+        return r;
+    }
     bool is_operand(size_t i) const { return v_[i] != nullptr && Py_TYPE(v_[i]) == &operand_type; }
     const Matrix& operand(size_t i) const
     {
@@ -808,7 +825,7 @@ MOR_CALL(py_adapter_linear)
 MOR_CALL(py_adamw)
 {
     return guarded([&] {
-        MOR_ARGS("adamw_", 4, 5, "params", "grads", "exp_avgs", "exp_avg_sqs", "scales", "step", "lr", "beta1", "beta2", "eps", "weight_decay", "seed", "grad_scale", "found_inf");
+        MOR_ARGS("adamw_", 4, 5, "params", "grads", "exp_avgs", "exp_avg_sqs", "scales", "step", "lr", "beta1", "beta2", "eps", "weight_decay", "seed", "grad_scale", "found_inf", "numbers");
         const AdamwLists lists = {a.tensors(0), a.tensors(1), a.tensors(2), a.tensors(3), a.tensors(4)};
         mor_adamw_desc_t d = {};
         if (a.is_tensor(5)) {
@@ -834,6 +851,9 @@ MOR_CALL(py_adamw)
         const std::optional<Tensor> scale = a.maybe_tensor(12), inf = a.maybe_tensor(13);
         d.grad_scale = one_float(scale, "grad_scale");
         d.found_inf = one_float(inf, "found_inf");
+        const std::vector<uint32_t> numbers = a.numbers(14);
+        want(a[14] == nullptr || numbers.size() == lists.params.n, "numbers: one for each parameter is wanted");
+        if (!numbers.empty()) d.numbers = numbers.data();
         adamw(lists, d);
         return give_none();
     });

@@ -7,13 +7,14 @@
     a torch optimizer; the decay is apart from the gradient.  Parameters are BF16 or FP32, gradients either.  bits: of the moments.  With 8 a block of 128
     elements keeps E4M3 codes of the first moment and of the second's root and a power-of-two scale for each (2.02 bytes an element instead of 8).  Codes, and
     BF16 parameters, are rounded up or down at random so that what a step changes by less than half a distance of codes is not lost: ``seed``, the
-    step's number and the element's place give the random numbers, so a run can be repeated.  ``step(grad_scale=None, found_inf=None)``: FP32 tensors of
+    step's number, the parameter's place in the optimizer and the element's in it give the random numbers, so a run can be repeated and no two parameters share them.  ``step(grad_scale=None, found_inf=None)``: FP32 tensors of
     one value; the first multiplies every gradient, and where the second is not zero nothing is changed (the step still counts).  With capturable the steps of a
     group are counted on the GPU and lr may be a tensor there, so that a captured step can be replayed.
 ``adamw_(params, grads, exp_avgs, exp_avg_sqs, scales=None, *, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, seed=0, grad_scale=None,
-found_inf=None)``
+found_inf=None, numbers=None)``
     one step over lists of contiguous tensors, changed in place and none of them given twice; all parameters of one type, and all gradients.  The moments are
-    FP32, or float8_e4m3fn with scales uint8 [blocks of 128, 2].  step: its number, from 1, or one int32 on the GPU; lr: a number, or one FP32 on the GPU.
+    FP32, or float8_e4m3fn with scales uint8 [blocks of 128, 2].  step: its number, from 1, or one int32 on the GPU; lr: a number, or one FP32 on the GPU.  numbers: one below 2^31
+    for each parameter, which its random numbers go by (None: its place in the list); parameters of one step that come in several calls want different ones.
 ``moments(exp_avg, exp_avg_sq, scales, dtype=torch.float32)``
     the values of 8-bit moments.
 
@@ -66,9 +67,11 @@ class AdamW(torch.optim.Optimizer):
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
+        place = -1
         for group in self.param_groups:
             calls, capturable = {}, group["capturable"]
             for p in group["params"]:
+                place += 1
                 if p.grad is None:
                     continue
                 if p.grad.is_sparse:
@@ -82,7 +85,7 @@ class AdamW(torch.optim.Optimizer):
                         group["step"] = torch.zeros((), dtype=torch.int32, device=p.device)
                 else:
                     state["step"] += 1
-                calls.setdefault((p.device, p.dtype, p.grad.dtype, 0 if capturable else state["step"]), []).append((p, p.grad.contiguous(), state))
+                calls.setdefault((p.device, p.dtype, p.grad.dtype, 0 if capturable else state["step"]), []).append((p, p.grad.contiguous(), state, place))
             if capturable and calls:
                 group["step"].add_(1)
             for (device, _, _, step), items in calls.items():
@@ -91,5 +94,5 @@ class AdamW(torch.optim.Optimizer):
                     adamw_([i[0] for i in items], [i[1] for i in items], [i[2]["exp_avg"] for i in items], [i[2]["exp_avg_sq"] for i in items],
                            [i[2]["scales"] for i in items] if group["bits"] == 8 else None, step=step, lr=group["lr"], beta1=group["betas"][0],
                            beta2=group["betas"][1], eps=group["eps"], weight_decay=group["weight_decay"], seed=group["seed"], grad_scale=grad_scale,
-                           found_inf=found_inf)
+                           found_inf=found_inf, numbers=[i[3] for i in items])
         return loss

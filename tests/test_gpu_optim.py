@@ -197,6 +197,67 @@ def test_many_tensors_are_each_their_own(optim, count):
         check_param(t, want, size, zero, words(t.numel(), i, 1, 0)[1], torch.bfloat16)
 
 
+def test_numbers_of_tensors(optim):
+    """A tensor's number takes the place of its place: two calls with numbers give what one call gives, in launches of up to 512 tensors, and the largest number is
+    the formula's too."""
+    import torch
+
+    def make():
+        g = torch.Generator(device="cuda").manual_seed(5)
+        sizes = [200 + i for i in range(600)]
+        m, v, s = (list(t) for t in zip(*(new_state(n, n) for n in sizes)))
+        return [torch.zeros(n, device="cuda", dtype=torch.bfloat16) for n in sizes], [torch.randn(n, generator=g, device="cuda") for n in sizes], m, v, s
+
+    one, two = make(), make()
+    optim.adamw_(*one, step=3, seed=8)
+    odd, even = ([t[k::2] for t in two] for k in (1, 0))
+    optim.adamw_(*odd, step=3, seed=8, numbers=list(range(1, 600, 2)))
+    optim.adamw_(*even, step=3, seed=8, numbers=tuple(range(0, 600, 2)))
+    assert all((a.float() == b.float()).all() for i in (0, 2, 3, 4) for a, b in zip(one[i], two[i]))
+    n = 3000
+    p, g = torch.zeros(n, device="cuda", dtype=torch.bfloat16), torch.randn(n, device="cuda")
+    optim.adamw_([p], [g], [torch.zeros(n, device="cuda")], [torch.zeros(n, device="cuda")], step=2, lr=1e-2, seed=4, numbers=[2 ** 31 - 1])
+    zero = torch.zeros(n, dtype=torch.float64, device="cuda")
+    want, _, _, size = formula(zero, g.double(), zero, zero, 2, 1e-2, 0.9, 0.999, 1e-8, 0.0)
+    check_param(p, want, size, zero, words(n, 2 ** 31 - 1, 2, 4)[1], torch.bfloat16)
+    for bad in ([1, 2], [-1], [2 ** 31]):
+        with pytest.raises(ValueError):
+            optim.adamw_([p], [g], [g.clone()], [g.clone()], step=1, numbers=bad)
+    for bad in ([1.0], 3):
+        with pytest.raises(TypeError):
+            optim.adamw_([p], [g], [g.clone()], [g.clone()], step=1, numbers=bad)
+
+
+def test_no_two_parameters_share_random_numbers(optim):
+    """Equal parameters with equal gradients in two groups, or of two gradients' types, are rounded apart, as in one call; a parameter's random numbers do not depend on
+    which others have a gradient."""
+    import torch
+
+    torch.manual_seed(0)
+    d = torch.randn(4096, device="cuda").to(torch.bfloat16)
+    g = torch.randn(4096, device="cuda").to(torch.bfloat16) * 1e-3
+
+    def run(groups, types=(torch.bfloat16, torch.bfloat16), missing=()):
+        p = [torch.nn.Parameter(d.clone()) for _ in range(2)]
+        o = optim.AdamW([{"params": [t]} for t in p] if groups else p, seed=1)
+        for i, t in enumerate(p):
+            if i not in missing:
+                if types[i] == torch.float32:
+                    t.grad_dtype = None
+                t.grad = g.to(types[i])
+        o.step()
+        return p, [o.state[t] for t in p]
+
+    p, s = run(False)
+    assert (p[0] != p[1]).float().mean() > 0.1 and (s[0]["exp_avg"].float() != s[1]["exp_avg"].float()).float().mean() > 0.1
+    q, t = run(True)
+    assert all((a == b).all() for a, b in zip(p, q)) and all((a["exp_avg"].float() == b["exp_avg"].float()).all() for a, b in zip(s, t))
+    q, t = run(False, (torch.bfloat16, torch.float32))
+    assert all((a == b).all() for a, b in zip(p, q)) and all((a["exp_avg"].float() == b["exp_avg"].float()).all() for a, b in zip(s, t))
+    q, t = run(False, missing=(0,))
+    assert (p[1] == q[1]).all() and (s[1]["exp_avg"].float() == t[1]["exp_avg"].float()).all()
+
+
 def test_views_that_start_anywhere(optim):
     import torch
 

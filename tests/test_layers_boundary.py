@@ -157,3 +157,10 @@ def test_moments_refuse(lib):
     assert f(1, 1, 2, -1, 4, 4, 0, None) == INVALID and f(1, 1, 2, 8, 4, 4, 2, None) == INVALID and f(1, 1, None, 8, 4, 4, 0, None) == INVALID
     assert f(None, 1, 2, 8, 4, 4, 0, None) == INVALID and f(1, None, 2, 8, 4, 4, 0, None) == INVALID and f(1, 1, 2, 8, None, None, 0, None) == INVALID
     assert f(1, 1, 3, 8, 4, 4, 0, None) == ALIGN and f(1, 1, 2, 8, 5, 4, 0, None) == ALIGN and f(1, 1, 2, 8, 4, 6, 1, None) == ALIGN and f(None, None, None, 0, None, None, 0, None) == OK
+
+
+def test_adamw_refuses_numbers(lib):
+    for last, want in ((1 << 31, INVALID), ((1 << 32) - 1, INVALID), ((1 << 31) - 1, OK)):
+        numbers = (C.c_uint32 * 2)(0, last)
+        t = (mb.mor_adamw_tensor_t * 2)(tensor(numel=0), tensor(numel=0))
+        assert lib.mor_adamw(C.byref(step(numbers=C.addressof(numbers))), t, 2, None) == want
