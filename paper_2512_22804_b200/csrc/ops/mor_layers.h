@@ -440,6 +440,7 @@ void adamw(const AdamwLists& l, mor_adamw_desc_t& d)
         there(p, "params");
         there(g, "grads");
         no_tangent({p, g}, "optim.adamw_");
+        TORCH_CHECK(!(needs_grad(p) || needs_grad(m) || needs_grad(v)), "optim.adamw_ changes its tensors in place: those that require a gradient are wanted under torch.no_grad()");
         there(m, "exp_avgs");
         there(v, "exp_avg_sqs");
         const int64_t numel = p.numel();

@@ -528,6 +528,26 @@ def test_autograd_sees_the_change(optim):
         y.backward()
 
 
+def test_what_requires_a_gradient_is_changed_under_no_grad_only(optim):
+    import torch
+
+    z = lambda: torch.zeros(64, device="cuda")  # noqa: E731
+    for i in (0, 2, 3):
+        args = [z() if k != 1 else z() + 1 for k in range(4)]
+        args[i].requires_grad_()
+        with pytest.raises(RuntimeError, match="no_grad"):
+            optim.adamw_(*[[t] for t in args], step=1)
+        assert all((t == 0).all() for k, t in enumerate(args) if k != 1) and args[i]._version == 0
+        with torch.no_grad():
+            optim.adamw_(*[[t] for t in args], step=1)
+        assert (args[0] != 0).all() and args[0].requires_grad == (i == 0)
+        between = args[i] * 1
+        args = [t.detach() for t in args]
+        args[i] = between                                                         # nor what was made of one
+        with pytest.raises(RuntimeError, match="no_grad"):
+            optim.adamw_(*[[t] for t in args], step=1)
+
+
 def test_forward_mode_is_refused(optim):
     import torch
     import torch.autograd.forward_ad as forward
