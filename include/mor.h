@@ -485,7 +485,7 @@ MOR_API mor_status_t mor_adapter_grad(const mor_adapter_desc_t* host_desc, const
                                       size_t workspace_bytes, void* cuda_stream);
 
 /* ------------------------------------------------------------------------------- an optimizer's step ----
- * AdamW with the decay apart from the gradient, over many tensors with one launch for every 512.  With g the gradient times grad_scale:
+ * AdamW with the decay apart from the gradient, over many tensors with one launch for every 512; what is written shares memory with nothing else of the call.  With g the gradient times grad_scale:
  *   m = beta1 m + (1 - beta1) g       v = beta2 v + (1 - beta2) g^2
  *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
  * in binary32; a second moment below 2^-126 counts as zero, and eps is 2^-63 at least.  Parameters and gradients are BF16 or FP32.  The moments are FP32, or 8 bits: blocks of 128 consecutive elements share a

@@ -413,6 +413,43 @@ const float* one_float(const std::optional<Tensor>& t, const char* what)
     want(t->scalar_type() == at::kFloat && t->numel() == 1, std::string(what) + ": one FP32 value is wanted");
     return ptr<float>(*t);
 }
+// What a step reads and changes, by its place in memory.
+struct Spans {
+    struct Span {
+        uintptr_t from, to;
+        bool written;
+        bool operator<(const Span& o) const { return from < o.from; }
+    };
+    std::vector<Span> all;
+    size_t list = 0;                                        // where the present list starts
+    void add(const void* at, int64_t size, bool written)
+    {
+        if (size > 0) all.push_back({(uintptr_t)at, (uintptr_t)at + (uintptr_t)size, written});
+    }
+    // Lists mostly lie in memory as they were allocated, one way or the other (gradients the other): they are merged, sorted only where they do not (128 tensors:
+    // 7 us of a call's 26 on the host, 8 of 34 in no order).
+    void end_list()
+    {
+        const auto from = all.begin() + (std::ptrdiff_t)list;
+        if (!std::is_sorted(from, all.end())) {
+            std::reverse(from, all.end());
+            if (!std::is_sorted(from, all.end())) std::sort(from, all.end());
+        }
+        std::inplace_merge(all.begin(), from, all.end());
+        list = all.size();
+    }
+    // What is written may overlap with nothing.
+    bool apart() const
+    {
+        uintptr_t any = 0, written = 0;                     // ends of what lies before
+        for (const Span& s : all) {
+            if (s.from < (s.written ? any : written)) return false;
+            any = std::max(any, s.to);
+            if (s.written) written = std::max(written, s.to);
+        }
+        return true;
+    }
+};
 // A step over hundreds of tensors: messages are made where they are needed only (as arguments they took 100 us of a call with 128 tensors).
 void adamw(const AdamwLists& l, mor_adamw_desc_t& d)
 {
@@ -430,9 +467,6 @@ void adamw(const AdamwLists& l, mor_adamw_desc_t& d)
         if (!t.is_cuda() || t.get_device() != device) on_gpu(t, what);
     };
     std::vector<mor_adamw_tensor_t> t(n);
-    std::vector<std::pair<uintptr_t, uintptr_t>> spans;
-    spans.reserve(n);
-    bool in_order = true;
     for (size_t i = 0; i < n; ++i) {
         const Tensor &p = l.params[i], &g = l.grads[i], &m = l.m[i], &v = l.v[i];
         if (p.scalar_type() != param || g.scalar_type() != grad) throw py::type_error("the parameters of a call have one type, and so have the gradients");
@@ -455,15 +489,21 @@ void adamw(const AdamwLists& l, mor_adamw_desc_t& d)
             scales = ptr<uint8_t>(s);
         }
         t[i] = {p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), scales, numel};
-        if (numel == 0) continue;
-        const uintptr_t at = (uintptr_t)t[i].param;
-        in_order = in_order && (spans.empty() || spans.back().second <= at);
-        spans.push_back({at, at + p.nbytes()});
     }
-    if (!in_order) {
-        std::sort(spans.begin(), spans.end());
-        for (size_t i = 1; i < spans.size(); ++i) want(spans[i].first >= spans[i - 1].second, "parameters may not share memory");
-    }
+    Spans spans;
+    spans.all.reserve(5 * n);
+    const int64_t per = (int64_t)c10::elementSize(state);
+    for (const mor_adamw_tensor_t& x : t) spans.add(x.param, x.numel * (int64_t)c10::elementSize(param), true);
+    spans.end_list();
+    for (const mor_adamw_tensor_t& x : t) spans.add(x.exp_avg, x.numel * per, true);
+    spans.end_list();
+    for (const mor_adamw_tensor_t& x : t) spans.add(x.exp_avg_sq, x.numel * per, true);
+    spans.end_list();
+    for (const mor_adamw_tensor_t& x : t) spans.add(x.scales, d.eight_bits ? (x.numel + 127) / 128 * 2 : 0, true);
+    spans.end_list();
+    for (const mor_adamw_tensor_t& x : t) spans.add(x.grad, x.numel * (int64_t)c10::elementSize(grad), false);
+    spans.end_list();
+    want(spans.apart(), "parameters, moments and scales may not share memory, and gradients not with them");
     for (size_t i = 0; i < n; ++i) {                        // changed in place: autograd has to see it
         l.params[i].unsafeGetTensorImpl()->bump_version();
         l.m[i].unsafeGetTensorImpl()->bump_version();

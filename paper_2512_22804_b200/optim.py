@@ -12,7 +12,7 @@
     group are counted on the GPU and lr may be a tensor there, so that a captured step can be replayed.
 ``adamw_(params, grads, exp_avgs, exp_avg_sqs, scales=None, *, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, seed=0, grad_scale=None,
 found_inf=None, numbers=None)``
-    one step over lists of contiguous tensors, changed in place (under torch.no_grad() where they require a gradient) and none of them given twice; all parameters of one type, and all gradients.  The moments are
+    one step over lists of contiguous tensors, changed in place (under torch.no_grad() where they require a gradient) and none of them given twice nor sharing memory with another; all parameters of one type, and all gradients.  The moments are
     FP32, or float8_e4m3fn with scales uint8 [blocks of 128, 2].  step: its number, from 1, or one int32 on the GPU; lr: a number, or one FP32 on the GPU.  numbers: one below 2^31
     for each parameter, which its random numbers go by (None: its place in the list); parameters of one step that come in several calls want different ones.
 ``moments(exp_avg, exp_avg_sq, scales, dtype=torch.float32)``

@@ -548,6 +548,33 @@ def test_what_requires_a_gradient_is_changed_under_no_grad_only(optim):
             optim.adamw_(*[[t] for t in args], step=1)
 
 
+def test_nothing_that_is_written_may_be_shared(optim):
+    """Each refused call leaves all tensors alone; gradients may be shared among themselves."""
+    import torch
+
+    f = lambda n=256: torch.zeros(n, device="cuda")  # noqa: E731
+    e = lambda n=256: torch.zeros(n, device="cuda").to(torch.float8_e4m3fn)  # noqa: E731
+    s = lambda n=256: torch.full((n // 128, 2), 127, dtype=torch.uint8, device="cuda")  # noqa: E731
+    one = torch.ones(256, device="cuda")
+    x, y, z, t, u = f(), f(512), e(), e(512), s()
+    cases = [([f(), f()], [one, one], [x, x], [f(), f()]), ([f(), f()], [one, one], [f(), f()], [x, x]), ([f()], [one], [x], [x]), ([x], [one], [x], [f()]), ([x], [one], [f()], [x]),
+             ([f(), f()], [one, one], [x, f()], [f(), x]), ([f(), f()], [one, one], [y[:256], y[128:384]], [f(), f()]), ([y[:256]], [one], [f()], [y[255:511]]), ([x], [x], [f()], [f()]),
+             ([f(), f()], [one, y[1:257]], [y[:256], f()], [f(), f()]), ([f(), f()], [one, one], [z, z], [e(), e()], [s(), s()]), ([f(), f()], [one, one], [e(), e()], [e(), e()], [u, u]),
+             ([f(), f()], [one, one], [e(), t[:256]], [t[200:456], e()], [s(), s()])]
+    for case in cases:
+        with pytest.raises(ValueError, match="share memory"):
+            optim.adamw_(*case, step=1)
+    torch.cuda.synchronize()
+    assert all((v.float() == 0).all() for v in (x, y, z, t)) and (u == 127).all()
+    p, q = [f(), f()], [f(), f()]
+    optim.adamw_(p, [one, one], [f(), f()], [f(), f()], step=1)
+    optim.adamw_(q, [one, one.clone()], [f(), f()], [f(), f()], step=1)
+    assert all((a == b).all() and (a != 0).all() for a, b in zip(p, q))
+    buf = f(3 * 256)                                                              # neighbours share nothing
+    optim.adamw_([buf[256:512]], [one], [buf[512:]], [buf[:256]], step=1)
+    assert (buf[256:512] == p[0]).all() and (buf[512:] != 0).all() and (buf[:256] != 0).all()
+
+
 def test_forward_mode_is_refused(optim):
     import torch
     import torch.autograd.forward_ad as forward
