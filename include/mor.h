@@ -518,6 +518,7 @@ typedef struct mor_adamw_desc {
     int32_t eight_bits;      /* moments as codes                                               */
     const uint32_t* numbers; /* HOST [n], optional: the tensors' numbers, below 2^31, instead of their places 0 .. n - 1 in the call: tensors of several calls
                               * of a step are rounded by random numbers of their own if they have numbers of their own */
+    int32_t device_step_each;     /* not zero: device_step is [n], a step's number for every tensor                     */
 } mor_adamw_desc_t;
 MOR_API mor_status_t mor_adamw(const mor_adamw_desc_t* host_desc, const mor_adamw_tensor_t* host_tensors, int n, void* cuda_stream);
 /* Values of 8-bit moments: m = code / s into exp_avg_out, v = (code / s)^2 into exp_avg_sq_out ([numel] in `dtype`, each optional). */

@@ -127,7 +127,7 @@ class mor_adamw_tensor_t(C.Structure):
 class mor_adamw_desc_t(C.Structure):
     _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double), ("step", C.c_int64),
                 ("device_step", C.c_void_p), ("device_lr", C.c_void_p), ("grad_scale", C.c_void_p), ("found_inf", C.c_void_p), ("seed", C.c_uint64),
-                ("param_dtype", C.c_int32), ("grad_dtype", C.c_int32), ("eight_bits", C.c_int32), ("numbers", C.c_void_p)]
+                ("param_dtype", C.c_int32), ("grad_dtype", C.c_int32), ("eight_bits", C.c_int32), ("numbers", C.c_void_p), ("device_step_each", C.c_int32)]
 
 
 BLOCK_STATS_DTYPE = np.dtype([("amax", "f4"), ("min_abs_nz", "f4"), ("nnz", "u4"), ("n_nonfinite", "u4"),

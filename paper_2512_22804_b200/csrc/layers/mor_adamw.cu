@@ -38,6 +38,7 @@ struct AdamwScalars {
     float log1, log2;                                      // log beta
     uint32_t seed, step, count;                            // count: tensors of this launch
     int32_t chunk;                                         // elements of a CTA
+    uint32_t each;                                         // tensors' steps apart in device_step: 1, or 0 if they share one
     const int32_t* device_step;
     const float *device_lr, *grad_scale, *found_inf;
 };
@@ -250,7 +251,7 @@ template <typename P, typename G, bool EIGHT, int N> __global__ void __launch_bo
     uint32_t step = s.step;
     if (s.device_lr != nullptr) lr = *s.device_lr;
     if (s.device_step != nullptr) {
-        step = (uint32_t)*s.device_step;
+        step = (uint32_t)s.device_step[lo * s.each];
         bias1 = 1.f / -expm1f((float)step * s.log1);
         bias2 = rsqrtf(-expm1f((float)step * s.log2));
     }
@@ -478,6 +479,7 @@ mor_status_t adamw_launch(const AdamwScalars& s, const mor_adamw_tensor_t* t, co
         per = per < 1 ? 1 : per > kMostPasses ? kMostPasses : per;
         p.s.chunk = (int32_t)per * kPass;
         p.s.count = (uint32_t)k;
+        if (s.each != 0) p.s.device_step = s.device_step + at;
         int64_t ctas = 0;
         for (int i = 0; i < k; ++i) {
             const mor_adamw_tensor_t& x = t[at + i];
@@ -548,6 +550,7 @@ mor_status_t mor_adamw(const mor_adamw_desc_t* d, const mor_adamw_tensor_t* t, i
     s.seed = (uint32_t)d->seed;
     s.step = (uint32_t)d->step;
     s.device_step = d->device_step;
+    s.each = d->device_step != nullptr && d->device_step_each ? 1 : 0;
     s.device_lr = d->device_lr;
     s.grad_scale = d->grad_scale;
     s.found_inf = d->found_inf;

@@ -831,8 +831,10 @@ MOR_CALL(py_adamw)
         if (a.is_tensor(5)) {
             const Tensor& step = a.tensor(5);
             on_gpu(step, "step");
-            want(step.scalar_type() == at::kInt && step.numel() == 1, "step: a number, or one int32 on the GPU, is wanted");
+            want(step.scalar_type() == at::kInt && (step.numel() == 1 || (step.numel() == (int64_t)lists.params.n && step.is_contiguous())),
+                 "step: a number, or one int32 on the GPU or one for each parameter, is wanted");
             d.device_step = ptr<int32_t>(step);
+            d.device_step_each = step.numel() != 1;
         } else {
             want(a[5] != nullptr, "step: the number of this step, from 1, is wanted");
             d.step = a.integer(5, 0);

@@ -8,12 +8,13 @@
     elements keeps E4M3 codes of the first moment and of the second's root and a power-of-two scale for each (2.02 bytes an element instead of 8).  Codes, and
     BF16 parameters, are rounded up or down at random so that what a step changes by less than half a distance of codes is not lost: ``seed``, the
     step's number, the parameter's place in the optimizer and the element's in it give the random numbers, so a run can be repeated and no two parameters share them.  ``step(grad_scale=None, found_inf=None)``: FP32 tensors of
-    one value; the first multiplies every gradient, and where the second is not zero nothing is changed (the step still counts).  With capturable the steps of a
-    group are counted on the GPU and lr may be a tensor there, so that a captured step can be replayed.
+    one value; the first multiplies every gradient, and where the second is not zero nothing is changed (the step still counts).  With capturable each
+    parameter's steps are counted on the GPU (those of the group in its "step") and lr may be a tensor there, so that a captured step can be replayed.
 ``adamw_(params, grads, exp_avgs, exp_avg_sqs, scales=None, *, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, seed=0, grad_scale=None,
 found_inf=None, numbers=None)``
     one step over lists of contiguous tensors, changed in place (under torch.no_grad() where they require a gradient) and none of them given twice nor sharing memory with another; all parameters of one type, and all gradients.  The moments are
-    FP32, or float8_e4m3fn with scales uint8 [blocks of 128, 2].  step: its number, from 1, or one int32 on the GPU; lr: a number, or one FP32 on the GPU.  numbers: one below 2^31
+    FP32, or float8_e4m3fn with scales uint8 [blocks of 128, 2].  step: its number, from 1, or int32 on the GPU, one or one for
+    each parameter; lr: a number, or one FP32 on the GPU.  numbers: one below 2^31
     for each parameter, which its random numbers go by (None: its place in the list); parameters of one step that come in several calls want different ones.
 ``moments(exp_avg, exp_avg_sq, scales, dtype=torch.float32)``
     the values of 8-bit moments.
@@ -58,7 +59,16 @@ class AdamW(torch.optim.Optimizer):
             if i in stored:
                 self.state[p] = {k: v.clone().to(p.device) if isinstance(v, torch.Tensor) else v for k, v in stored[i].items()}
         for group in self.param_groups:
-            if group["step"] is not None:
+            kept = {}
+            for p in group["params"]:
+                if group["capturable"] and self.state.get(p):
+                    state = self.state[p]
+                    if not isinstance(state["step"], torch.Tensor) and group["step"] is not None:      # stored when a group's parameters shared its count
+                        state["step"] = int(group["step"])
+                    kept.setdefault((p.device, p.dtype), []).append(state)
+            for (device, _), states in kept.items():
+                _count_together(states, device)
+            if group["step"] is not None and group["params"]:
                 group["step"] = group["step"].to(group["params"][0].device)
 
     @torch.no_grad()
@@ -80,19 +90,52 @@ class AdamW(torch.optim.Optimizer):
                 if not state:
                     state.update(self._new_state(p, group["bits"]))
                     state["step"] = 0
-                if capturable:
-                    if group["step"] is None:
-                        group["step"] = torch.zeros((), dtype=torch.int32, device=p.device)
-                else:
-                    state["step"] += 1
+                if not capturable:
+                    state["step"] = int(state["step"]) + 1
                 calls.setdefault((p.device, p.dtype, p.grad.dtype, 0 if capturable else state["step"]), []).append((p, p.grad.contiguous(), state, place))
             if capturable and calls:
-                group["step"].add_(1)
-            for (device, _, _, step), items in calls.items():
-                with torch.cuda.device(device):
-                    step = group["step"] if capturable else step
+                steps = self._count(group, calls)
+            for key, items in calls.items():
+                with torch.cuda.device(key[0]):
+                    step = key[3]
+                    if capturable:
+                        step = steps[key] if isinstance(steps[key], torch.Tensor) else torch.stack(steps[key])
                     adamw_([i[0] for i in items], [i[1] for i in items], [i[2]["exp_avg"] for i in items], [i[2]["exp_avg_sq"] for i in items],
                            [i[2]["scales"] for i in items] if group["bits"] == 8 else None, step=step, lr=group["lr"], beta1=group["betas"][0],
                            beta2=group["betas"][1], eps=group["eps"], weight_decay=group["weight_decay"], seed=group["seed"], grad_scale=grad_scale,
                            found_inf=found_inf, numbers=[i[3] for i in items])
         return loss
+
+    @staticmethod
+    def _count(group, calls):
+        """One more step on the GPU for the group and for each parameter in `calls`; for each call its parameters' counts, as one tensor where they lie in one."""
+        if group["step"] is None:
+            group["step"] = torch.zeros((), dtype=torch.int32, device=next(iter(calls))[0])
+        steps, more = {}, {group["step"].device: [group["step"]]}
+        for key, items in calls.items():
+            states = [i[2] for i in items]
+            fresh = [s for s in states if not isinstance(s["step"], torch.Tensor)]
+            if fresh:
+                _count_together(fresh, key[0])
+            counts = [s["step"] for s in states]
+            whole = counts[0]._base if counts[0]._base is not None else counts[0]
+            if whole.numel() != len(counts) or not all(c.data_ptr() == whole.data_ptr() + 4 * i for i, c in enumerate(counts)):
+                whole = counts
+            steps[key] = whole
+            more.setdefault(key[0], []).extend(whole if isinstance(whole, list) else [whole])
+        for tensors in more.values():
+            torch._foreach_add_(tensors, 1)
+        return steps
+
+
+def _count_together(states, device):
+    """The steps of these parameters in one tensor on the GPU, an element each: one operation counts for all of them and a call reads them as they lie."""
+    counts = [s["step"] for s in states]
+    if any(isinstance(c, torch.Tensor) for c in counts):
+        whole = torch.stack([c if isinstance(c, torch.Tensor) else torch.tensor(c, dtype=torch.int32, device=device) for c in counts]).to(torch.int32)
+    elif any(counts):
+        whole = torch.tensor(counts, dtype=torch.int32, device=device)
+    else:
+        whole = torch.zeros(len(counts), dtype=torch.int32, device=device)
+    for i, s in enumerate(states):
+        s["step"] = whole[i]

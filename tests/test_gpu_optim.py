@@ -518,6 +518,118 @@ def test_optimizer_captured(optim):
         assert (d <= 5e-6 + a.detach().double().abs() * (2.0 ** -7 if a.dtype == torch.bfloat16 else 1e-5)).all() and (d > 1e-6).double().mean() < 0.01
 
 
+@pytest.mark.parametrize("captured", [False, True])
+def test_each_parameter_counts_its_own_steps_with_capturable(optim, captured):
+    """Parameters that start later or miss steps, beside the optimizer that counts on the host: the moments are the same, and an update differs by the bias corrections,
+    made in 32 bits (their arguments by 2 u, their values by 4 u more) on top of the 16 u of its size, which for these gradients is within 4 lr."""
+    import torch
+
+    lr, sizes = 1e-2, (300, 5000, 40, 77)
+    with_grad = [(0, 1, 2)] * 3 + [(0, 2)] * 4 + [(0, 1, 2, 3)] * 2 + [(1, 3)] * 3 + [(0, 1, 2, 3)]
+
+    def fresh(capturable):
+        torch.manual_seed(1)
+        p = [torch.nn.Parameter(torch.randn(n, device="cuda")) for n in sizes]
+        return p, optim.AdamW(p, lr=lr, bits=32, capturable=capturable)
+
+    grads = [torch.randn(n, device="cuda", generator=torch.Generator(device="cuda").manual_seed(n)) for n in sizes]
+    p, o = fresh(False)
+    q, c = fresh(True)
+    graphs = {}
+    for k, some in enumerate(with_grad):
+        for ps in (p, q):
+            for i, t in enumerate(ps):
+                t.grad = grads[i].clone() * (k + 1) if i in some and (ps is p or not captured) else None
+        o.step()
+        if not captured:
+            c.step()
+            continue
+        for i in some:
+            if not hasattr(q[i], "static"):
+                q[i].static = torch.empty_like(q[i])
+            q[i].static.copy_(grads[i] * (k + 1))
+            q[i].grad = q[i].static
+        seen = {i for before in with_grad[:k] for i in before}
+        if not set(some) <= seen:
+            c.step()                                       # a parameter's first step takes its memory
+        else:
+            if some not in graphs:
+                graphs[some] = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(graphs[some]):
+                    c.step()
+            graphs[some].replay()
+    torch.cuda.synchronize()
+    assert int(c.param_groups[0]["step"]) == len(with_grad)
+    for a, b in zip(p, q):
+        assert int(c.state[b]["step"]) == o.state[a]["step"]
+        assert all((o.state[a][m] == c.state[b][m]).all() for m in ("exp_avg", "exp_avg_sq"))
+        assert ((a.detach().double() - b.detach().double()).abs() <= len(with_grad) * (4 * lr * 32 * U + 8 * U * a.detach().abs())).all()
+
+
+def test_counts_of_steps_are_stored_and_loaded(optim):
+    import copy
+    import io
+
+    import torch
+
+    def fresh():
+        torch.manual_seed(1)
+        p = [torch.nn.Parameter(torch.randn(n, device="cuda").to(t)) for n, t in ((5000, torch.bfloat16), (700, torch.float32), (300, torch.bfloat16), (10, torch.float32))]
+        return p, optim.AdamW([{"params": p[:2]}, {"params": p[2:]}], lr=1e-2, seed=3, capturable=True)
+
+    def run(p, o, steps):
+        for k in steps:
+            for i, t in enumerate(p):
+                t.grad = torch.randn(t.shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(k)).to(t.dtype) if i != 2 or k > 1 else None
+            o.step()
+
+    p, o = fresh()
+    run(p, o, range(6))
+    q, o2 = fresh()
+    run(q, o2, range(3))
+    assert [int(o2.state[t]["step"]) for t in q] == [3, 3, 1, 3]
+    file = io.BytesIO()
+    torch.save((o2.state_dict(), [t.detach() for t in q]), file)
+    file.seek(0)
+    state, data = torch.load(file, weights_only=True)
+    r, o3 = fresh()
+    with torch.no_grad():
+        for t, d in zip(r, data):
+            t.copy_(d)
+    o3.load_state_dict(state)
+    run(r, o3, range(3, 6))
+    assert all((a == b).all() for a, b in zip(p, r)) and [int(o3.state[t]["step"]) for t in r] == [6, 6, 4, 6]
+    assert [int(o2.state[t]["step"]) for t in q] == [3, 3, 1, 3]                 # the stored ones were no aliases
+    both = copy.deepcopy((q, o2))                                                # counts that lie anywhere
+    run(both[0], both[1], range(3, 6))
+    assert all((a == b).all() for a, b in zip(p, both[0]))
+    assert all((a == b).all() for a, b in zip(p, both[0]))
+    old = o2.state_dict()                                                        # as it was stored when a group's parameters shared its count
+    old = {"state": {i: dict(s, step=0) for i, s in old["state"].items()}, "param_groups": old["param_groups"]}
+    r, o3 = fresh()
+    o3.load_state_dict(old)
+    assert [int(o3.state[t]["step"]) for t in r] == [3, 3, 3, 3]
+
+
+def test_steps_of_several_tensors_on_the_gpu(optim):
+    """One call with a step's number for every tensor is the calls one by one, in launches of up to 512 tensors."""
+    import torch
+
+    n = 520
+    make = lambda: [[torch.full((130,), 1.0, device="cuda") for _ in range(n)], [torch.full((130,), 0.5, device="cuda") for _ in range(n)],  # noqa: E731
+                    [torch.full((130,), 0.1, device="cuda") for _ in range(n)], [torch.full((130,), 0.01, device="cuda") for _ in range(n)]]
+    a, b = make(), make()
+    steps = torch.arange(1, n + 1, dtype=torch.int32, device="cuda") % 37 + 1
+    optim.adamw_(*a, step=steps)
+    for i in range(n):
+        optim.adamw_(*[[t[i]] for t in b], step=steps[i])
+    assert all((x == y).all() for s, t in zip(a, b) for x, y in zip(s, t))
+    assert (a[0][0] != a[0][1]).any()
+    for bad in (steps[:-1], steps[:2], torch.stack((steps, steps), 1)[:, 0], steps.long(), steps.cpu()):
+        with pytest.raises(ValueError):
+            optim.adamw_(*a, step=bad)
+
+
 def test_autograd_sees_the_change(optim):
     import torch
 
