@@ -9,7 +9,8 @@
     BF16 parameters, are rounded up or down at random so that what a step changes by less than half a distance of codes is not lost: ``seed``, the
     step's number, the parameter's place in the optimizer and the element's in it give the random numbers, so a run can be repeated and no two parameters share them.  ``step(grad_scale=None, found_inf=None)``: FP32 tensors of
     one value; the first multiplies every gradient, and where the second is not zero nothing is changed (the step still counts).  With capturable each
-    parameter's steps are counted on the GPU (those of the group in its "step") and lr may be a tensor there, so that a captured step can be replayed.
+    parameter's steps are counted on the GPU (those of the group in its "step") and lr may be a tensor there, so that a captured step can be replayed; a parameter's first
+    step has to be taken before the capture, and without capturable none is captured.
 ``adamw_(params, grads, exp_avgs, exp_avg_sqs, scales=None, *, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, seed=0, grad_scale=None,
 found_inf=None, numbers=None)``
     one step over lists of contiguous tensors, changed in place (under torch.no_grad() where they require a gradient) and none of them given twice nor sharing memory with another; all parameters of one type, and all gradients.  The moments are
@@ -77,6 +78,7 @@ class AdamW(torch.optim.Optimizer):
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
+        self._check_capture()
         place = -1
         for group in self.param_groups:
             calls, capturable = {}, group["capturable"]
@@ -105,6 +107,17 @@ class AdamW(torch.optim.Optimizer):
                            beta2=group["betas"][1], eps=group["eps"], weight_decay=group["weight_decay"], seed=group["seed"], grad_scale=grad_scale,
                            found_inf=found_inf, numbers=[i[3] for i in items])
         return loss
+
+    def _check_capture(self):
+        """A captured step whose number is the host's, or that makes its parameter's moments anew, would not go on from replay to replay."""
+        params = ((group, p) for group in self.param_groups for p in group["params"] if p.grad is not None)
+        for i, (group, p) in enumerate(params):
+            if i == 0 and not (p.is_cuda and torch.cuda.is_current_stream_capturing()):
+                return
+            if not group["capturable"]:
+                raise RuntimeError("a step can be captured with capturable=True only: its number would stay the same in every replay")
+            if not isinstance(self.state.get(p, {}).get("step"), torch.Tensor):
+                raise RuntimeError("a parameter's first step has to be taken before a capture: every replay would begin with new moments")
 
     @staticmethod
     def _count(group, calls):

@@ -566,6 +566,35 @@ def test_each_parameter_counts_its_own_steps_with_capturable(optim, captured):
         assert ((a.detach().double() - b.detach().double()).abs() <= len(with_grad) * (4 * lr * 32 * U + 8 * U * a.detach().abs())).all()
 
 
+def test_captures_that_could_not_go_on_are_refused(optim):
+    """Nothing is changed by a refused capture, and the optimizer goes on after it."""
+    import torch
+
+    def fresh(capturable):
+        p = [torch.nn.Parameter(torch.zeros(300, device="cuda")) for _ in range(2)]
+        return p, optim.AdamW([{"params": p[:1]}, {"params": p[1:]}], bits=32, lr=1e-2, capturable=capturable)
+
+    def capture(o, message):
+        with pytest.raises(RuntimeError, match=message):
+            with torch.cuda.graph(torch.cuda.CUDAGraph()):
+                o.step()
+
+    one = torch.ones(300, device="cuda")
+    for capturable in (True, False):
+        p, o = fresh(capturable)
+        p[0].grad = one
+        if capturable:
+            capture(o, "first step")
+            assert not o.state[p[0]]
+        o.step()
+        p[1].grad = one
+        capture(o, "first step" if capturable else "capturable=True")
+        assert int(o.state[p[0]]["step"]) == 1 and (p[1] == 0).all()
+        o.step()
+        assert int(o.state[p[0]]["step"]) == 2 and int(o.state[p[1]]["step"]) == 1
+        assert ((p[1] + 1e-2).abs() <= 1e-2 * 32 * U).all()
+
+
 def test_counts_of_steps_are_stored_and_loaded(optim):
     import copy
     import io
