@@ -457,7 +457,9 @@ MOR_API mor_status_t mor_codes_dequantize(const uint8_t* codes, int64_t rows, in
 
 /* ----------------------------------------------- low-rank adapters beside a shared projection ----
  * out[t] = base[t] + f scale[g] (x[t] a[g]^T) b[g]^T with g = ids[t], the adapter of token t; a token whose id is no adapter's keeps base[t].  Inner
- * products of `rank` terms are kept in binary32 and enter the second product as two BF16 that add up to 16 bits and more; out is rounded once. */
+ * products of `rank` terms are kept in binary32 and enter the second product as two BF16 that add up to 16 bits and more; out is rounded once.  Where what they
+ * are multiplied with is infinite (b here, in the gradients a in dx, dy in db and x in da) the result is not finite, but NaN where the second of the two is zero
+ * or of the other sign, also where the formula has an infinity; no other result is touched. */
 typedef struct mor_adapter_desc {
     int64_t tokens, n_in, n_out; /* widths 1 .. 2^21                                             */
     int32_t adapters, rank;      /* adapters <= MOR_MAX_GROUPS - 1; rank 1 .. MOR_MAX_RANK       */

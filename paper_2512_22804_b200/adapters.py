@@ -7,7 +7,7 @@
     x BF16 [..., n_in], base BF16 or FP32 [..., n_out]; a BF16 [adapters, rank, n_in] and b BF16 [adapters, n_out, rank] (or one adapter's matrices, without
     the first dimension), rank up to 512; ids int32 [...], one for every token: an id outside 0..adapters-1 means no adapter, and the token's base comes
     back as it is.  Without ids every token has the one adapter.  scale: a number, or FP32 [adapters].  The result has base's type, is rounded
-    once, and is a tensor of its own.
+    once, and is a tensor of its own.  Infinities pass through as such but for those of b (in the gradients a, dy and x), which may become NaN.
 ``linear(x, w, a, b, ids=None, scale=1.0, *, w_t=None)``
     x [..., n_in] quantised to w's format and multiplied with it, the adapters added to the BF16 result.  The projection is frozen.  For a gradient of x
     the operand of w's transpose is wanted too: ``w, w_t = fp4.quantize(weight, format, cols=True)``; dy is then quantised along n_out and the rounding passed

@@ -90,7 +90,8 @@ template <bool ANY> __device__ __forceinline__ uint4 load_frag(const bf16* row, 
 }
 
 __device__ __forceinline__ uint16_t bits_of(bf16 v) { return __bfloat16_as_ushort(v); }
-// v as the sum of two BF16; a value that is not finite is the first alone.
+// v as the sum of two BF16; a value that is not finite is the first alone.  An infinite factor of both gives NaN where the second is zero or of the other sign: kept so,
+// since a second part that always has the first's sign would be a bit shorter for all values.
 __device__ __forceinline__ void split(float v, bf16& hi, bf16& lo)
 {
     hi = __float2bfloat16(v);

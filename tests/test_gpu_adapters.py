@@ -275,6 +275,43 @@ def test_infinite_adapters_and_rows_that_only_fill_a_tile_up(adapters):
             assert (da.isinf() == want_da).all() and (db.isinf() == want_db).all()
 
 
+@pytest.mark.parametrize("tokens,rank", [(20, 3), (300, 16), (2500, 16), (300, 70), (2500, 40)])
+def test_infinities_touch_what_they_are_part_of(adapters, tokens, rank):
+    """An infinite element of x, a, b or dy: a result is not finite exactly where the formula's is not (an infinity of its second product may have become NaN), and all others
+    are bit for bit what they are without it."""
+    import torch
+
+    x, y0, a, b, _, scale = draw(tokens, 72, 56, rank, 2, seed=9)
+    ids = (torch.arange(tokens, device="cuda") % 3 - 1).to(torch.int32)
+    dy = torch.randn(y0.shape, device="cuda").to(torch.bfloat16)
+    on = [(ids == g).nonzero().reshape(-1) for g in range(2)]
+
+    def run(x, a, b, dy):
+        return [adapters.add(y0, x, a, b, ids, scale), *run_grads(adapters, y0, x, a, b, ids, scale, dy)[1:]]
+
+    def plain(x, a, b, dy):
+        x, a, b, dy = (t.double() for t in (x, a, b, dy))
+        y, dx, da, db = y0.double(), torch.zeros_like(x), torch.zeros_like(a), torch.zeros_like(b)
+        for g, at in enumerate(on):
+            h, u = (x[at].unsqueeze(1) * a[g]).sum(2), (dy[at].unsqueeze(2) * b[g]).sum(1)          # no library's zeros beside infinities
+            y[at] += (h.unsqueeze(1) * b[g]).sum(2)
+            dx[at] = (u.unsqueeze(2) * a[g]).sum(1)
+            da[g] = (u.unsqueeze(2) * x[at].unsqueeze(1)).sum(0)
+            db[g] = (dy[at].unsqueeze(2) * h.unsqueeze(1)).sum(0)
+        return y, dx, da, db
+
+    clean = run(x, a, b, dy)
+    assert all(t.isfinite().all() for t in clean)
+    for which, place in ((0, (4, 7)), (1, (1, 2, 7)), (2, (1, 5, 1)), (3, (4, 5))):
+        for value in (float("inf"), -float("inf")):
+            args = [t.clone() for t in (x, a, b, dy)]
+            args[which][place] = value
+            got, want = run(*args), plain(*args)
+            for p, q, c in zip(got, want, clean):
+                assert (p.isfinite() == q.isfinite()).all() and (p[q.isfinite()] == c[q.isfinite()]).all()
+            assert any(not q.isfinite().all() for q in want)
+
+
 def test_a_wait_that_runs_out_is_reported(adapters):
     """The library's test hook keeps one CTA from announcing its first products and shortens the limit to about a millisecond: the call returns, the status word says
     so, and the same call without the hook is right."""
