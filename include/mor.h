@@ -497,7 +497,7 @@ MOR_API mor_status_t mor_adapter_grad(const mor_adapter_desc_t* host_desc, const
  * random number u: with t the magnitude over the distance d of its two neighbours n d and (n + 1) d, m takes the upper where t + u >= n + 1
  * (its mean is kept), w where u (2 n + 1) < (t - n)(t + n) (the mean of its square is kept), and a w above zero is at least the smallest code, since
  * it is divided by.  What is not finite becomes NaN.  BF16 parameters are rounded by 16 random bits added below the kept ones.
- * Random numbers are hashes, in 32 bits: mix(z): z ^= z >> 16; z *= 0x7FEB352D; z ^= z >> 15; z *= 0x846CA68B; z ^= z >> 16.  With key =
+ * Random numbers are hashes, in 32 bits (C. Wellons, "Prospecting for hash functions", 2018): mix(z): z ^= z >> 16; z *= 0x7FEB352D; z ^= z >> 15; z *= 0x846CA68B; z ^= z >> 16.  With key =
  * mix(mix(seed + 0x9E3779B9 * step) + tensor's number) and z = mix(mix(high half of the element's number ^ key) + low half), the low 16 bits
  * of z / 65536 are u of m, the high ones u of w, the low ones of mix(z ^ 0x9E3779B9) the parameter's. */
 typedef struct mor_adamw_tensor {

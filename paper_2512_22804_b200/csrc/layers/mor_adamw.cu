@@ -1,10 +1,11 @@
 // One AdamW step over many tensors, moments in 32 bits or as E4M3 codes with one scale for 128 elements, and the values of such codes.
 //
 // Every element is read and written once.  With FP32 moments the kernel is bound by memory (103 M elements, 2.88 GB: 421 us, 6.8 TB/s), with 8-bit ones by its
-// instructions (80 an element: 285 us for 1.44 GB; with the read-back of the moments' values 400, and 418 since sums and roots are
+// instructions (84 an element: 285-289 us for 1.44 GB; with the read-back of the moments' values 411-421, of which about 8 are the sums and roots that are
 // rounded as formulas without fused operations round them).  A launch takes the addresses of up to 512 tensors as its
 // parameters (a captured graph then needs no table in memory that has to outlive it), the smallest of three sizes of that table that holds them,
-// since a launch costs more the more it carries; each CTA finds its tensor by bisection and takes 2048 or 4096 of its elements.
+// since a launch costs the host more the more it carries (tensors of 4096 elements: 16 take a call 4.5 us, 17 5.8; 128 17.2, 129 18.7; on the GPU there is
+// no difference, 4.1 and 6.2 us as graphs on either side); each CTA finds its tensor by bisection and takes 2048 or 4096 of its elements.
 // A thread holds 8 consecutive elements, so 16 lanes hold a block of 128 and its maximum takes four shuffles.
 #include <math.h>
 
@@ -18,7 +19,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kPass = kThreads * kPer;
-constexpr int kMostPasses = 2;                // of a CTA (1: 433 us for a layer of 103 M elements and its moments' values, 2: 400-412, 4: 445)
+constexpr int kMostPasses = 2;                // of a CTA (1: 427 us for a layer of 103 M elements and its moments' values, 2: 411-421, 4: 449)
 constexpr int kRing = 2;                      // passes whose inputs a thread has in its part of shared memory
 
 struct AdamwEntry {
@@ -48,7 +49,7 @@ template <int N> struct AdamwParams {
     AdamwEntry e[N];
 };
 
-// All of mix() but its last step.
+// A published hash of 32 bits (C. Wellons, "Prospecting for hash functions", 2018, in the public domain); all of mix() but its last step.
 __device__ __forceinline__ uint32_t mix_most(uint32_t z)
 {
     z ^= z >> 16;
@@ -62,7 +63,7 @@ __device__ __forceinline__ uint32_t mix(uint32_t z)
     return z ^ (z >> 16);
 }
 
-// The kernel with 8-bit moments has to make some seventy instructions an element fit beside 14 bytes of traffic.  Two things help: operations on two values in
+// The kernel with 8-bit moments has to make some eighty instructions an element fit beside 14 bytes of traffic.  Two things help: operations on two values in
 // a register pair, and steps written as saturating products where a comparison and a choice would go to the integer pipe, which is half as wide and was
 // what bounded the kernel (38 of 80 instructions an element; a layer of 103 M elements 322 us).
 using Pair = unsigned long long;

@@ -349,7 +349,7 @@ template <typename T, typename R> __global__ void __launch_bounds__(kWideThreads
 
 // dh = rs (g - xh mean(g xh)) + dh_in with g = dy w, xh = h rs: both sums of a row come from one reduction.  The weight's gradient is summed by
 // each thread over its group's rows, then over the CTA's groups in shared memory and over the CTAs by the join, always in the same order.  One CTA an SM, since every
-// CTA's sums are written and read again: 8192 x 4096 BF16, 46 us (268 MB, 5.8 TB/s), and 6 for the join, which is latency.
+// CTA's sums are written and read again: 8192 x 4096 BF16, 47 us (268 MB, 5.7 TB/s), and 6 for the join, which is latency.
 template <int G> constexpr int kGradThreads = G > 512 ? G : 512;
 
 template <typename T, typename R, int G, int N, bool ANY> __global__ void __launch_bounds__(kGradThreads<G>) norm_grad_kernel(const __grid_constant__ NormParams p)
@@ -560,7 +560,8 @@ template <typename W> __global__ void __launch_bounds__(kJoinCols* kJoinParts) n
 
 // ------------------------------------------------------------------------------------------- values ----
 
-// 16 codes a thread at a time, of kValueRows rows: 16 bytes in, 32 or 64 out.  8192 x 4096 to BF16: 25 us (101 MB), issue slots 68 % full.
+// 16 codes a thread at a time, of kValueRows rows: 16 bytes in, 32 or 64 out.  8192 x 4096 to BF16: 25 us (101 MB, 4.0 TB/s),
+// issue slots 68 % full: neither is a bound, what is left are the loads' latency and the quotients one after the other.
 constexpr int kValueRows = 4;
 template <typename T> __global__ void __launch_bounds__(256) codes_values_kernel(const uint8_t* codes, int64_t rows, int32_t cols, int64_t ldc, int32_t by_row,
                                                                                  const uint8_t* e8m0, const float* f32, T* out, int64_t ldo, bool aligned)
