@@ -7,16 +7,16 @@
     a torch optimizer; the decay is apart from the gradient.  Parameters are BF16 or FP32, gradients either.  bits: of the moments.  With 8 a block of 128
     elements keeps E4M3 codes of the first moment and of the second's root and a power-of-two scale for each (2.02 bytes an element instead of 8).  Codes, and
     BF16 parameters, are rounded up or down at random so that what a step changes by less than half a distance of codes is not lost: ``seed``, the
-    step's number, the parameter's place in the optimizer and the element's in it give the random numbers, so a run can be repeated and no two parameters share them.  ``step(grad_scale=None, found_inf=None)``: FP32 tensors of
-    one value; the first multiplies every gradient, and where the second is not zero nothing is changed (the step still counts).  With capturable each
-    parameter's steps are counted on the GPU (those of the group in its "step") and lr may be a tensor there, so that a captured step can be replayed; a parameter's first
-    step has to be taken before the capture, and without capturable none is captured.
+    step's number, the parameter's place in the optimizer and the element's in it give the random numbers, so a run can be repeated and no two parameters
+    share them.  ``step(grad_scale=None, found_inf=None)``: FP32 tensors of one value; the first multiplies every gradient, and where the second is not zero
+    nothing is changed (the step still counts).  With capturable each parameter's steps are counted on the GPU (those of the group in its "step") and lr may be
+    a tensor there, so that a captured step can be replayed; a parameter's first step has to be taken before the capture, and without capturable none is captured.
 ``adamw_(params, grads, exp_avgs, exp_avg_sqs, scales=None, *, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, seed=0, grad_scale=None,
 found_inf=None, numbers=None)``
-    one step over lists of contiguous tensors, changed in place (under torch.no_grad() where they require a gradient) and none of them given twice nor sharing memory with another; all parameters of one type, and all gradients.  The moments are
-    FP32, or float8_e4m3fn with scales uint8 [blocks of 128, 2].  step: its number, from 1, or int32 on the GPU, one or one for
-    each parameter; lr: a number, or one FP32 on the GPU.  numbers: one below 2^31
-    for each parameter, which its random numbers go by (None: its place in the list); parameters of one step that come in several calls want different ones.
+    one step over lists of contiguous tensors, changed in place (under torch.no_grad() where they require a gradient), none of them given twice or sharing
+    memory with another; all parameters of one type, and all gradients.  The moments are FP32, or float8_e4m3fn with scales uint8 [blocks of 128, 2].  step: its
+    number, from 1, or int32 on the GPU, one or one for each parameter; lr: a number, or one FP32 on the GPU.  numbers: one below 2^31 for each parameter, which
+    its random numbers go by (None: its place in the list); parameters of one step that come in several calls want different ones.
 ``moments(exp_avg, exp_avg_sq, scales, dtype=torch.float32)``
     the values of 8-bit moments.
 
@@ -64,8 +64,8 @@ class AdamW(torch.optim.Optimizer):
             for p in group["params"]:
                 if group["capturable"] and self.state.get(p):
                     state = self.state[p]
-                    if not isinstance(state["step"], torch.Tensor) and group["step"] is not None:      # stored when a group's parameters shared its count
-                        state["step"] = int(group["step"])
+                    if not isinstance(state["step"], torch.Tensor) and state["step"] == 0 and group["step"] is not None:
+                        state["step"] = int(group["step"])                     # stored when a group's parameters shared its count
                     kept.setdefault((p.device, p.dtype), []).append(state)
             for (device, _), states in kept.items():
                 _count_together(states, device)
@@ -116,7 +116,7 @@ class AdamW(torch.optim.Optimizer):
                 return
             if not group["capturable"]:
                 raise RuntimeError("a step can be captured with capturable=True only: its number would stay the same in every replay")
-            if not isinstance(self.state.get(p, {}).get("step"), torch.Tensor):
+            if not isinstance(self.state.get(p, {}).get("step"), torch.Tensor) or group["step"] is None:
                 raise RuntimeError("a parameter's first step has to be taken before a capture: every replay would begin with new moments")
 
     @staticmethod

@@ -638,6 +638,16 @@ def test_counts_of_steps_are_stored_and_loaded(optim):
     r, o3 = fresh()
     o3.load_state_dict(old)
     assert [int(o3.state[t]["step"]) for t in r] == [3, 3, 3, 3]
+    for group in o2.param_groups:                                                # counted on the host for a while, and a parameter waits there
+        group["capturable"] = False
+    run(q, o2, range(3, 5))
+    for group in o2.param_groups:
+        group["capturable"] = True
+    q[1].grad = None
+    o2.step()
+    assert [int(o2.state[t]["step"]) for t in q] == [6, 5, 4, 6]
+    o3.load_state_dict(o2.state_dict())
+    assert [int(o3.state[t]["step"]) for t in r] == [6, 5, 4, 6]
 
 
 def test_steps_of_several_tensors_on_the_gpu(optim):
