@@ -615,11 +615,11 @@ template <int R, int ROWS, int THREADS, typename T, int BASE> struct ExpandCopie
         return (uint32_t)kBase + chunk_at<R * 2>(slot, k);
     }
     int32_t first;
-    // Columns from `at` on (since c0), ranks from r0 on; the base with the first of them.  A row's CTAs take the steps in turn: what they read and write at the
+    // Columns from `at` on (since c0), ranks from r0 on, and the base if it is wanted.  A row's CTAs take the steps in turn: what they read and write at the
     // same time lies side by side in memory.
-    __device__ __forceinline__ void fill(uint32_t stage, int at, int r0) const
+    __device__ __forceinline__ void fill(uint32_t stage, int at, int r0, bool with_base) const
     {
-        if (kHas && r0 == 0) {
+        if (kHas && with_base) {
             const int c = (int)threadIdx.x % kPieces * (16 / (int)sizeof(T));
             base.copy(stage + base_place, kStep * (kChunks * 16), at, n - at - c, first);
         }
@@ -713,7 +713,7 @@ template <int R, typename T, int BASE> __global__ void __launch_bounds__(256, BA
     const C copies(p, tokens, adapter, (int64_t)part * 64);
     auto stage = [&](int32_t i) { return (uint32_t)i % kStages * C::kStage; };
     auto fill = [&](int32_t i) {
-        if (i < count) copies.fill(smem + stage(i), i * stride, 0);
+        if (i < count) copies.fill(smem + stage(i), i * stride, 0, true);
         copies_commit();
     };
 #pragma unroll
@@ -806,7 +806,7 @@ template <int R, typename T, int BASE> __global__ void __launch_bounds__(128) ad
     const int32_t turns = count * chunks;
     auto stage = [&](int32_t i) { return (uint32_t)i % kExpand32Stages * C::kStage; };
     auto fill = [&](int32_t i) {                                                  // a turn is a step and a chunk of the ranks
-        if (i < turns) copies.fill(smem + stage(i), i / chunks * stride, i % chunks * R);
+        if (i < turns) copies.fill(smem + stage(i), i / chunks * stride, i % chunks * R, i % chunks == chunks - 1);
         copies_commit();
     };
 #pragma unroll
@@ -846,17 +846,13 @@ template <int R, typename T, int BASE> __global__ void __launch_bounds__(128) ad
         const uint32_t ms = smem + stage(turn) + C::kBase;
         const int r0 = turn % chunks * R;
         if (chunks > 1) load_h(r0);
-        if (r0 == 0) {                                                            // the sums begin with the base
+        if (r0 == 0) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float v[kPer] = {};
-                if constexpr (C::kHas) C::read_base(v, ring + stage(turn), i * 8 + g, warp, q);
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    acc[i >> 1][j][(i & 1) * 2] = v[2 * j];
-                    acc[i >> 1][j][(i & 1) * 2 + 1] = v[2 * j + 1];
-                }
-            }
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) acc[i][j][k] = 0.f;
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -881,11 +877,13 @@ template <int R, typename T, int BASE> __global__ void __launch_bounds__(128) ad
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (out[i] == nullptr) continue;
-            float v[kPer];
+            // the base last, in one addition: the tensor instructions cut what they add to, and sums that began with an FP32 base lost its last digits (64 ranks: 14 units)
+            float v[kPer] = {};
+            if constexpr (C::kHas) C::read_base(v, ring + stage(turn), i * 8 + g, warp, q);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                v[2 * j] = acc[i >> 1][j][(i & 1) * 2];
-                v[2 * j + 1] = acc[i >> 1][j][(i & 1) * 2 + 1];
+                v[2 * j] += acc[i >> 1][j][(i & 1) * 2];
+                v[2 * j + 1] += acc[i >> 1][j][(i & 1) * 2 + 1];
             }
             store_out(v, out[i], at, p.n, p.out_whole);
         }

@@ -72,6 +72,20 @@ def test_add(adapters, tokens, n_in, n_out, rank, n, base):
     assert (y == again).all()
 
 
+@pytest.mark.parametrize("tokens,rank", [(20, 16), (20, 100), (300, 2), (1000, 24), (1000, 64), (1000, 70), (1000, 512), (3000, 40), (3000, 64)])
+def test_an_fp32_base_is_rounded_once(adapters, tokens, rank):
+    """Beside a base of 2^20 times the adapters' part all that counts is the last addition, half a step (u) of the result, and what 2^-17 of the part adds."""
+    import torch
+
+    x, y0, a, b, ids, scale = draw(tokens, 72, 104, rank, 2, base="fp32")
+    y0, b = y0.abs() + 1, b * 2.0 ** -20
+    y = adapters.add(y0, x, a, b, ids, scale)
+    want, off = formula(y0, x, a, b, ids, scale)
+    part = off - U * y0.double().abs()                                            # the bound without the base's share
+    assert ((y.double() - want).abs() <= 1.001 * U * want.abs() + part).all()
+    assert part.max() < U and (y != y0).any()
+
+
 @pytest.mark.parametrize("tokens", [1, 15, 16, 100, 256, 300, 1000])
 def test_one_adapter_without_ids(adapters, tokens):
     import torch
